@@ -379,6 +379,100 @@ rdkv_status rdkv_calibrate_eps(const rdkv_config* cfg, const void* K, const void
 int32_t rdkv_k_row_words(const uint8_t* bits_ch);
 int32_t rdkv_k_row_words_max(void);
 
+/*
+ * Slot caches: a cache that stays at a fixed size while a generation grows.  Every item, a (sequence, KV head), has
+ * `capacity` slots; a slot holds one token's K row and V row, its position, and the attention weight it has gathered.  A
+ * prompt fills the slots with its first tokens, its last ones, and those of largest weight (rdkv_slots_fill, with the weights
+ * of rdkv_weights or others); every generated token takes a free slot, or that of the token of least weight
+ * (rdkv_slots_append); a decode step attends to the slots and adds to their weights (rdkv_slots_decode_attn).
+ *
+ * All memory is the caller's, on the device the calls are made on: this struct names it.  No call allocates or waits, and each
+ * may be recorded under graph capture; lengths and positions live on the device, so that replays go on from token to token.
+ * The calls on one cache follow each other in stream order (steps that change the same cache must not overlap); on different
+ * caches they may overlap where their workspaces are apart.  Outputs share no memory with inputs.  A len outside
+ * 0..capacity is taken for the nearer of the two.
+ * Rows are aligned to 16 bytes: so are k, v, q, out and the rows of prompts and new tokens.
+ */
+typedef struct rdkv_slots {
+  int32_t batch;            /* number of sequences */
+  int32_t hq, hkv;          /* query heads, KV heads; hq / hkv in {1, 2, 4, 8} */
+  int32_t head_dim;         /* must be 128 */
+  int32_t capacity;         /* slots of an item, >= 1 */
+  int32_t bits;             /* 16: rows are bf16, k and v [batch][hkv][capacity][128];
+                               4: codes with an fp16 scale and offset per 32 channels of a row, quantized as rdkv_pack does (values
+                               within fp16's range), k and
+                               v [batch][hkv][ceil(capacity / 64)][5120 bytes]: tiles of 64 slots in the layout of rdkv_pack's
+                               4-bit tiers, 4096 bytes of codes, then 1024 of scales and offsets */
+  int32_t sinks, recent;    /* never evicted: tokens at positions below `sinks`, and the newest `recent` ones;
+                               sinks + max(recent, 1) <= capacity */
+  int32_t window;           /* 0, or: a step sees tokens less than `window` positions back, and those below `sinks` */
+  float score_cap;          /* 0, or c > 0: scores become c tanh(score / c) */
+  float decay;              /* in [0, 1]: what a step multiplies gathered weights by before it adds its own */
+  const float* slopes;      /* DEVICE [hq] or NULL: slopes[h] times the distance in positions is taken from a score of head h */
+  void* k;                  /* DEVICE, rdkv_slots_side_bytes() each */
+  void* v;
+  int32_t* pos;             /* DEVICE [batch][hkv][capacity]: position of a slot's token */
+  float* weight;            /* DEVICE [batch][hkv][capacity] or NULL: attention weight gathered (NULL: none is kept, and the oldest
+                               token that may go is evicted) */
+  int32_t* len;             /* DEVICE [batch][hkv]: slots in use, the first ones; zero in an empty cache */
+  int32_t* next;            /* DEVICE [batch][hkv]: position of the next token; zero in an empty cache */
+} rdkv_slots;
+
+/* head_dim 128, bits 16, decay 1; everything else zero. */
+rdkv_status rdkv_slots_default(rdkv_slots* slots);
+/* Bytes of k, and of v; 0 for an invalid struct (its memory is not looked at). */
+size_t rdkv_slots_side_bytes(const rdkv_slots* slots);
+
+/*
+ * Prompts of `n` sequences into the slots of sequences first .. first + n - 1 of the cache; the others stay as they are.
+ *   seq_lens  HOST [n]: T_s >= 0 tokens
+ *   K, V      DEVICE bf16, ragged [hkv][T_s][d] blocks of the n sequences
+ *   w_tok     DEVICE fp32, ragged [hkv][T_s], or NULL: token weights, as rdkv_weights returns them; needed where some
+ *             T_s > capacity
+ *   workspace DEVICE scratch of at least rdkv_slots_fill_workspace_bytes(), 16-byte aligned (NULL where that is 0)
+ * An item of T <= capacity tokens keeps them all.  Of a longer one stay the first `sinks`, the last `recent` and, of the others,
+ * the capacity - sinks - recent of largest weight; of equal ones those at lower positions, and NaN is less than any number.
+ * Kept tokens lie in slots 0, 1, .. in the order of their positions; weight becomes w_tok of the kept tokens (0 where that is
+ * NULL), len their number, next T.  What lies in slots from len on is left as it is, but for the codes, scales and offsets of a
+ * 4-bit tile's rows behind its last: those become zero.
+ */
+size_t rdkv_slots_fill_workspace_bytes(const rdkv_slots* slots, int32_t n, const int32_t* seq_lens);
+rdkv_status rdkv_slots_fill(const rdkv_slots* slots, int32_t first, int32_t n, const int32_t* seq_lens, const void* K,
+                            const void* V, const float* w_tok, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One new token per sequence, at position next.  With a free slot it takes slot len; in a full cache that of the token of
+ * least weight among those that are neither below `sinks` nor among the newest `recent` (the new one counts as the newest); of
+ * equal ones that at the lowest position, and NaN is less than any number.  Its weight starts at 0; next grows by one.
+ *   k_new, v_new  DEVICE bf16 [batch][hkv][d]
+ *   slot          DEVICE int32 [batch][hkv] out, or NULL: the slot it took
+ */
+rdkv_status rdkv_slots_append(const rdkv_slots* slots, const void* k_new, const void* v_new, int32_t* slot, void* stream);
+
+/*
+ * One decode step: every query head attends to the slots of its item; the query sits at position next - 1, where the last
+ * appended token is.
+ *   score = q k / sqrt d, capped (score_cap), less slope x (next - 1 - pos); tokens that `window` hides take no part, whatever
+ *   their rows hold
+ *   q       DEVICE bf16 [batch][hq][d]
+ *   out     DEVICE fp32 [batch][hq][d]: softmax(scores) V; 0 where no token is seen
+ *   lse     DEVICE fp32 [batch][hq] or NULL: natural-log sum of exp of the scores; -inf where no token is seen
+ *   weight (of the cache) becomes decay x weight + the softmax's value, summed over the heads of the group, in slots below len
+ *   workspace  DEVICE scratch of at least rdkv_slots_decode_workspace_bytes(), 16-byte aligned
+ * A score that is NaN or +inf makes its head's out, lse and weights NaN.
+ */
+size_t rdkv_slots_decode_workspace_bytes(const rdkv_slots* slots);
+rdkv_status rdkv_slots_decode_attn(const rdkv_slots* slots, const void* q, float* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
+ * Rows of the slots as bf16 (4-bit rows: scale x code + offset in fp32, rounded once).
+ *   index  DEVICE int32 [batch][hkv][n] or NULL (slots 0 .. n - 1): which slots; a row of zeros where an index is negative or not
+ *          below len
+ *   K, V   DEVICE bf16 out [batch][hkv][n][d]
+ */
+rdkv_status rdkv_slots_read(const rdkv_slots* slots, const int32_t* index, int32_t n, void* K, void* V, void* stream);
+
 /* Introspection (tests, benchmarks). */
 rdkv_status rdkv_cache_stats(const rdkv_cache* cache, rdkv_stats* out);
 /* Size in bytes of an export; 0 for an unknown `what`. */

@@ -32,6 +32,8 @@ EXPORTED_SYMBOLS = [
     "rdkv_cache_rebudget_tail", "rdkv_cache_generations", "rdkv_cache_generation",
     "rdkv_cache_stats", "rdkv_cache_export_bytes", "rdkv_cache_export", "rdkv_cache_free",
     "rdkv_kernel_timing_enable", "rdkv_kernel_timing_read", "rdkv_k_row_words", "rdkv_k_row_words_max",
+    "rdkv_slots_default", "rdkv_slots_side_bytes", "rdkv_slots_fill_workspace_bytes", "rdkv_slots_fill", "rdkv_slots_append",
+    "rdkv_slots_decode_workspace_bytes", "rdkv_slots_decode_attn", "rdkv_slots_read",
 ]
 (RDKV_TIME_DECODE_TIERED, RDKV_TIME_DECODE_BF16, RDKV_TIME_WEIGHTS, RDKV_TIME_ALLOCATE, RDKV_TIME_PACK,
  RDKV_TIME_CALIBRATE) = range(6)
@@ -52,6 +54,16 @@ class rdkv_config(ctypes.Structure):
         ("eps_v", ctypes.c_float * 5), ("eps_k", ctypes.c_float * 5),
         ("rel_tol", ctypes.c_float), ("max_iters", ctypes.c_int32),
         ("alloc", _ALLOC_FN), ("free_", _FREE_FN), ("alloc_user", ctypes.c_void_p),
+    ]
+
+
+class rdkv_slots(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("hq", ctypes.c_int32), ("hkv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("capacity", ctypes.c_int32), ("bits", ctypes.c_int32), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+        ("window", ctypes.c_int32), ("score_cap", ctypes.c_float), ("decay", ctypes.c_float), ("slopes", ctypes.c_void_p),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+        ("len", ctypes.c_void_p), ("next", ctypes.c_void_p),
     ]
 
 
@@ -117,6 +129,18 @@ def _load():
     lib.rdkv_k_row_words.restype = i32
     lib.rdkv_k_row_words_max.argtypes = []
     lib.rdkv_k_row_words_max.restype = i32
+    slp = ctypes.POINTER(rdkv_slots)
+    lib.rdkv_slots_default.argtypes = [slp]
+    lib.rdkv_slots_side_bytes.argtypes = [slp]
+    lib.rdkv_slots_side_bytes.restype = sz
+    lib.rdkv_slots_fill_workspace_bytes.argtypes = [slp, i32, ctypes.POINTER(i32)]
+    lib.rdkv_slots_fill_workspace_bytes.restype = sz
+    lib.rdkv_slots_fill.argtypes = [slp, i32, i32, ctypes.POINTER(i32), vp, vp, vp, vp, sz, vp]
+    lib.rdkv_slots_append.argtypes = [slp, vp, vp, vp, vp]
+    lib.rdkv_slots_decode_workspace_bytes.argtypes = [slp]
+    lib.rdkv_slots_decode_workspace_bytes.restype = sz
+    lib.rdkv_slots_decode_attn.argtypes = [slp, vp, vp, vp, vp, sz, vp]
+    lib.rdkv_slots_read.argtypes = [slp, vp, i32, vp, vp, vp]
     lib.rdkv_kernel_timing_enable.argtypes = [i32]
     lib.rdkv_kernel_timing_read.argtypes = [i32, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double)]
     return lib
@@ -402,6 +426,156 @@ def rdkv_decode_attn_bf16_noalloc(K, V, seq_lens, hq, hkv, q, out, lse=None, hea
     _check(lib.rdkv_decode_attn_bf16_noalloc(_ptr(K), _ptr(V), arr, len(seq_lens), hq, hkv, head_dim, _ptr(q),
                                              _ptr(out), _ptr(lse), _stream()))
     return out, lse
+
+
+class Slots:
+    """A slot cache (rdkv_slots): its parameters and the device tensors that hold it, made here unless the caller brings them.
+
+      k, v      bits 16: bfloat16 [batch, hkv, capacity, 128]; bits 4: uint8 [batch, hkv, ceil(capacity / 64), 5120]
+      pos       int32 [batch, hkv, capacity]
+      weight    float32 [batch, hkv, capacity], or None with track=False: no attention weights are kept
+      lens      int32 [batch, hkv]: slots in use;  next_pos: int32 [batch, hkv]: position of the next token
+      slopes    float32 [hq] or None
+
+    The calls on it run on the current stream of its device.  A call leaves tensors it was given where they are, so that views
+    of them stay good."""
+
+    def __init__(self, batch, hq, hkv, capacity, bits=16, head_dim=128, sinks=0, recent=0, window=0, score_cap=0.0, decay=1.0,
+                 slopes=None, k=None, v=None, pos=None, weight=None, lens=None, next_pos=None, track=True, device=None):
+        self.c = rdkv_slots()
+        _check(lib.rdkv_slots_default(ctypes.byref(self.c)))
+        c = self.c
+        for name, x in (("batch", batch), ("hq", hq), ("hkv", hkv), ("head_dim", head_dim), ("capacity", capacity), ("bits", bits),
+                        ("sinks", sinks), ("recent", recent), ("window", window)):
+            if not -2 ** 31 <= int(x) < 2 ** 31:
+                raise ValueError(f"{name} = {x} is no 32-bit number")
+            setattr(c, name, int(x))
+        c.score_cap, c.decay = float(score_cap), float(decay)
+        c.k = c.v = c.pos = c.len = c.next = 16        # (what the library checks of memory is that there is some)
+        _check(lib.rdkv_slots_read(ctypes.byref(c), None, 0, None, None, None))
+        held = [t for t in (k, v, pos, weight, lens, next_pos) if t is not None]
+        self.device = torch.device(device) if device is not None else held[0].device if held else torch.device("cuda")
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.batch, self.hq, self.hkv, self.capacity, self.bits, self.d = c.batch, c.hq, c.hkv, c.capacity, c.bits, c.head_dim
+        items = (c.batch, c.hkv)
+        side = items + ((c.capacity, c.head_dim) if c.bits == 16 else ((c.capacity + 63) // 64, 5120))
+        kind = torch.bfloat16 if c.bits == 16 else torch.uint8
+
+        def tensor(t, shape, dtype, name):
+            if t is None:
+                return torch.zeros(shape, dtype=dtype, device=self.device)
+            return _tensor(t, shape, dtype, self.device, name)
+
+        self.k, self.v = tensor(k, side, kind, "k"), tensor(v, side, kind, "v")
+        self.pos = tensor(pos, items + (c.capacity,), torch.int32, "pos")
+        self.weight = tensor(weight, items + (c.capacity,), torch.float32, "weight") if track or weight is not None else None
+        self.lens, self.next_pos = tensor(lens, items, torch.int32, "lens"), tensor(next_pos, items, torch.int32, "next_pos")
+        self.slopes = None if slopes is None else _tensor(slopes, (c.hq,), torch.float32, self.device, "slopes")
+        for name, t in (("k", self.k), ("v", self.v), ("pos", self.pos), ("weight", self.weight), ("len", self.lens),
+                        ("next", self.next_pos), ("slopes", self.slopes)):
+            setattr(c, name, None if t is None else t.data_ptr())
+        self.workspace_bytes = lib.rdkv_slots_decode_workspace_bytes(ctypes.byref(c))
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+    def workspace(self):
+        """Scratch of a decode step, for callers that keep it."""
+        return torch.empty(max(self.workspace_bytes, 16), dtype=torch.uint8, device=self.device)
+
+
+def _tensor(t, shape, dtype, device, name):
+    """`t`, if it is what the library takes for `name`: it reads and writes plain memory."""
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}: "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
+    return t
+
+
+def _on(slots):
+    """The slots' device as the current one."""
+    index = slots.device.index
+    return _SAME if index is None or _current_device is None or _current_device() == index else torch.cuda.device(index)
+
+
+class _Same:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
+
+
+_SAME = _Same()
+
+
+def rdkv_slots_fill(slots, K, V, seq_lens, w_tok=None, first=0):
+    """Prompts of len(seq_lens) sequences into the slots of sequences first, first + 1, ..: K, V bfloat16, w_tok float32 or
+    None, ragged as everywhere."""
+    n = len(seq_lens)
+    lens = (ctypes.c_int32 * max(n, 1))(*[int(x) for x in seq_lens])
+    rows = sum(max(x, 0) for x in lens[:n]) * slots.hkv
+    for t, name in ((K, "K"), (V, "V")):
+        _tensor(t.view(-1), (rows * slots.d,), torch.bfloat16, slots.device, name)
+    if w_tok is not None:
+        _tensor(w_tok.view(-1), (rows,), torch.float32, slots.device, "w_tok")
+    with _on(slots):
+        need = lib.rdkv_slots_fill_workspace_bytes(slots.ref(), n, lens)
+        workspace = torch.empty(need, dtype=torch.uint8, device=slots.device) if need else None
+        _check(lib.rdkv_slots_fill(slots.ref(), int(first), n, lens, _ptr(K), _ptr(V), _ptr(w_tok), _ptr(workspace), need, _stream()))
+
+
+def rdkv_slots_append(slots, k_new, v_new, slot=None):
+    """The slot that each item's new token took: int32 [batch, hkv]."""
+    items = (slots.batch, slots.hkv)
+    _tensor(k_new, items + (slots.d,), torch.bfloat16, slots.device, "k_new")
+    _tensor(v_new, items + (slots.d,), torch.bfloat16, slots.device, "v_new")
+    if slot is None:
+        slot = torch.empty(items, dtype=torch.int32, device=slots.device)
+    else:
+        _tensor(slot, items, torch.int32, slots.device, "slot")
+    with _on(slots):
+        _check(lib.rdkv_slots_append(slots.ref(), k_new.data_ptr(), v_new.data_ptr(), slot.data_ptr(), _stream()))
+    return slot
+
+
+def rdkv_slots_decode_attn(slots, q, out=None, lse=None, workspace=None):
+    rows = (slots.batch, slots.hq)
+    _tensor(q, rows + (slots.d,), torch.bfloat16, slots.device, "q")
+    if out is None:
+        out = _empty_f32(rows + (slots.d,), (slots.hq * slots.d, slots.d, 1), slots.device)
+    else:
+        _tensor(out, rows + (slots.d,), torch.float32, slots.device, "out")
+    if lse is None:
+        lse = _empty_f32(rows, (slots.hq, 1), slots.device)
+    else:
+        _tensor(lse, rows, torch.float32, slots.device, "lse")
+    if workspace is None:
+        workspace = slots.workspace()
+    elif workspace.dtype != torch.uint8 or workspace.device != slots.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {slots.device}")
+    with _on(slots):
+        _check(lib.rdkv_slots_decode_attn(slots.ref(), q.data_ptr(), out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+                                          workspace.numel(), _stream()))
+    return out, lse
+
+
+def rdkv_slots_read(slots, index=None, n=None, K=None, V=None):
+    """(K, V) bfloat16 [batch, hkv, n, 128]: rows of slots `index` (int32 [batch, hkv, n]), or of the first n slots (all)."""
+    if index is not None:
+        if index.dim() != 3 or n not in (None, index.shape[2]):
+            raise ValueError(f"index must be [batch, hkv, n]: got {tuple(index.shape)}")
+        n = index.shape[2]
+        _tensor(index, (slots.batch, slots.hkv, n), torch.int32, slots.device, "index")
+    elif n is None:
+        n = slots.capacity
+    shape = (slots.batch, slots.hkv, int(n), slots.d)
+    K = torch.empty(shape, dtype=torch.bfloat16, device=slots.device) if K is None else _tensor(K, shape, torch.bfloat16, slots.device, "K")
+    V = torch.empty(shape, dtype=torch.bfloat16, device=slots.device) if V is None else _tensor(V, shape, torch.bfloat16, slots.device, "V")
+    with _on(slots):
+        _check(lib.rdkv_slots_read(slots.ref(), _ptr(index), int(n), K.data_ptr(), V.data_ptr(), _stream()))
+    return K, V
 
 
 def rdkv_kernel_timing_enable(enable):

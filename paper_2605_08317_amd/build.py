@@ -42,6 +42,9 @@ SOURCES = [
     # (its copies into LDS set m0, a reserved register, and say so)
     ("weights_kernels.hip", "weights_kernels.o", ["-Wno-inline-asm"] + EXACT_PRESSURE),
     ("calib_kernels.hip", "calib_kernels.o", []),
+    ("slots_decode.hip", "slots_decode.o", []),
+    ("slots_rows.hip", "slots_rows.o", []),
+    ("slots_api.hip", "slots_api.o", []),
 ]
 
 FLAGS = [

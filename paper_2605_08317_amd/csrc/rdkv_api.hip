@@ -48,12 +48,9 @@ hipError_t launch_calibrate(const uint16_t* K, const uint16_t* V, const int64_t*
 
 using namespace rdkv;
 
+static thread_local std::string g_err;
 
-namespace {
-
-thread_local std::string g_err;
-
-rdkv_status fail(rdkv_status s, const char* fmt, ...) {
+rdkv_status rdkv::fail(rdkv_status s, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -63,11 +60,7 @@ rdkv_status fail(rdkv_status s, const char* fmt, ...) {
   return s;
 }
 
-#define RDKV_HIP(expr)                                                                      \
-  do {                                                                                      \
-    hipError_t e_ = (expr);                                                                 \
-    if (e_ != hipSuccess) return fail(RDKV_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
+namespace {
 
 int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 

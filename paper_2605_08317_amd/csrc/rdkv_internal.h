@@ -159,6 +159,14 @@ struct PlanArgs {
   int32_t n_items, per_unit;     // per_unit: one K scale per channel
 };
 
+// Leaves a message for rdkv_last_error and returns `s` (rdkv_api.hip).
+rdkv_status fail(rdkv_status s, const char* fmt, ...);
+#define RDKV_HIP(expr)                                                                      \
+  do {                                                                                      \
+    hipError_t e_ = (expr);                                                                 \
+    if (e_ != hipSuccess) return rdkv::fail(RDKV_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
+  } while (0)
+
 // Lets a kernel use more dynamic LDS than the runtime grants by default; asked once per kernel and device (a call costs
 // 0.5 us).
 template <class K>
