@@ -45,7 +45,7 @@ struct FillArgs {
 hipError_t launch_fill(const FillArgs& a, int n_seqs, int bits, hipStream_t st);
 hipError_t launch_append(const Args& a, int bits, int items, const uint16_t* k_new, const uint16_t* v_new, int32_t* slot, hipStream_t st);
 hipError_t launch_read(const Args& a, int bits, int items, const int32_t* index, int n, uint16_t* K, uint16_t* V, hipStream_t st);
-size_t decode_workspace_floats(int64_t items, int g, int capacity);
+size_t decode_workspace_floats(int64_t items, int g, int capacity, int bits, bool weights);
 hipError_t launch_decode(const Args& a, int bits, int items, const uint16_t* q, float* out, float* lse, float* workspace, hipStream_t st);
 
 }  // namespace slots

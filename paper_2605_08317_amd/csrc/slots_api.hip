@@ -15,6 +15,7 @@ rdkv_status check_slots(const rdkv_slots* s, bool memory) {
   if (s->hq % s->hkv != 0) return fail(RDKV_ERR_SHAPE, "hq %d is not a multiple of hkv %d", s->hq, s->hkv);
   const int g = s->hq / s->hkv;
   if (!(g == 1 || g == 2 || g == 4 || g == 8)) return fail(RDKV_ERR_SHAPE, "hq/hkv = %d unsupported (1,2,4,8)", g);
+  if (s->hkv > 65535) return fail(RDKV_ERR_SHAPE, "hkv %d unsupported (at most 65535)", s->hkv);
   if (s->capacity < 1) return fail(RDKV_ERR_SHAPE, "capacity %d must be positive", s->capacity);
   if (s->bits != 16 && s->bits != 4) return fail(RDKV_ERR_SHAPE, "bits %d unsupported (16 or 4)", s->bits);
   if (s->sinks < 0 || s->recent < 0 || s->window < 0) return fail(RDKV_ERR_INVALID_ARG, "sinks, recent and window must not be negative");
@@ -148,7 +149,7 @@ rdkv_status rdkv_slots_append(const rdkv_slots* s, const void* k_new, const void
 
 size_t rdkv_slots_decode_workspace_bytes(const rdkv_slots* s) {
   if (check_slots(s, false) != RDKV_OK || s->batch == 0) return 0;
-  return slots::decode_workspace_floats(static_cast<int64_t>(s->batch) * s->hkv, s->hq / s->hkv, s->capacity) * sizeof(float);
+  return slots::decode_workspace_floats(static_cast<int64_t>(s->batch) * s->hkv, s->hq / s->hkv, s->capacity, s->bits, s->weight != nullptr) * sizeof(float);
 }
 
 rdkv_status rdkv_slots_decode_attn(const rdkv_slots* s, const void* q, float* out, float* lse, void* workspace,

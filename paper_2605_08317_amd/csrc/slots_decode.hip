@@ -1,112 +1,774 @@
-// Slot caches: the decode step.  One workgroup per (item, query head), scores in the workspace.
+// Slot caches: the decode step.
+//
+// One pass over the rows, as in the other decode kernels (decode_rows.h, decode_mfma_kernels.hip): a wavefront takes tiles of 64 slots,
+// makes their scores with four query heads on one side of v_mfma_f32_4x4x4, keeps a running maximum and sum of its softmax, and
+// adds P V to accumulators in registers.  What is its own here:
+//
+//   scores     lane = slot, four heads in a lane's registers: capped, biased and hidden there, and stored for the weights, which need
+//              every probability once the whole sum is known: 4 bytes per slot and query head, which stay in the caches
+//   precision  products of the query and of probabilities lose nothing that fp32 holds: bf16 rows meet a probability in three bf16 terms
+//              (24 bits), codes in two fp16 terms (22 bits), scaled so that the largest V scale seen stands just below fp16's largest
+//              and the query's largest value near one
+//   work       lengths are on the device.  The tiles of all items are one line, in which every workgroup takes an equal share; a
+//              piece of an item that does not hold all of it leaves a partial result for the launch that follows
+#include <algorithm>
+
+#include "decode_rows.h"
 #include "slots.h"
-#include "wave_ops.h"
 
 namespace rdkv {
 namespace slots {
 
 namespace {
 
-constexpr int kThreads = 256;
+using namespace tile;
 
-// value of one channel of a slot's row
-template <int BITS, bool V>
-__device__ __forceinline__ float value(const Args& a, int64_t item, int slot, int c) {
-  const uint8_t* side = V ? a.v : a.k;
-  if constexpr (BITS == 16) {
-    return __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(side)[(item * a.capacity + slot) * kHeadDim + c]) << 16);
-  } else {
-    const uint8_t* tile = side + (item * a.tiles + slot / kTileRows) * kTileBytes;
-    const int r = slot % kTileRows, lane = V ? 32 * (r >> 5) + (c & 31) : r, k = V ? r & 31 : c & 31;
-    const int word = 4 * (c >> 5) + 2 * (k >> 4) + ((k >> 1) & 1);
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + 1024 * (word >> 2) + 16 * lane + 4 * (word & 3));
-    const _Float16* meta = reinterpret_cast<const _Float16*>(tile + kTileCodes);
-    const int m = V ? 32 * (r >> 2) + 8 * (c >> 5) + (r & 3) : 8 * r + (c >> 5);
-    return static_cast<float>(meta[m]) * static_cast<float>(w >> (16 * (k & 1) + 4 * ((k >> 2) & 3)) & 15u) + static_cast<float>(meta[m + 4]);
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.0e38f;          // a finite maximum of nothing
+
+struct DecodeArgs {
+  Args s;
+  const uint16_t* q;
+  float* out;
+  float* lse;
+  float* scores;       // [items][g][score_rows], times log2(e); null: no weights are kept
+  float* part_acc;     // [slot][g][128]: partials; slot = workgroup + item
+  float* part_ml;      // [slot][g][2]
+  int32_t items, score_rows, least;     // least: tiles of a workgroup's share
+};
+
+// How the tiles of all items are shared out among the workgroups: workgroup w has those from w * share on.
+struct Line {
+  int total, share;
+};
+__device__ __forceinline__ int tiles_of(const Args& a, int64_t item) { return (a.length(item) + kTile - 1) / kTile; }
+
+// Tiles of all items together, and the share of one of n_groups workgroups.
+__device__ __forceinline__ Line make_line(const DecodeArgs& a, int n_groups) {
+  const int lane = threadIdx.x & 63;
+  int sum = 0;
+  for (int i = lane; i < a.items; i += 64) sum += tiles_of(a.s, i);
+  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+  Line l;
+  l.total = __builtin_amdgcn_readfirstlane(sum);
+  l.share = max(a.least, (l.total + n_groups - 1) / n_groups);
+  return l;
+}
+// Tiles before `item`.
+__device__ __forceinline__ int tiles_before(const DecodeArgs& a, int item) {
+  const int lane = threadIdx.x & 63;
+  int sum = 0;
+  for (int i = lane; i < item; i += 64) sum += tiles_of(a.s, i);
+  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+  return __builtin_amdgcn_readfirstlane(sum);
+}
+// The item that holds tile `at` of the line (at < total), and its first tile.
+__device__ __forceinline__ int item_at(const DecodeArgs& a, int at, int* first) {
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  for (int i0 = 0;; i0 += 64) {
+    const int n = i0 + lane < a.items ? tiles_of(a.s, i0 + lane) : 0;
+    const int up_to = base + static_cast<int>(wave_scan(static_cast<uint32_t>(n)));
+    const uint64_t past = __ballot(up_to > at);
+    if (past != 0 || i0 + 64 >= a.items) {
+      const int k = past != 0 ? __builtin_ctzll(past) : 63;
+      *first = __builtin_amdgcn_readlane(up_to - n, k);
+      return i0 + k;
+    }
+    base = __builtin_amdgcn_readlane(up_to, 63);
   }
 }
 
-template <int BITS>
-__global__ __launch_bounds__(kThreads) void decode_kernel(Args a, const uint16_t* __restrict__ q, float* __restrict__ out,
-                                                          float* __restrict__ lse, float* __restrict__ scores) {
-  __shared__ float s_q[kHeadDim], s_red[kThreads / 64], s_out[kHeadDim], s_top[8], s_inv[8];
-  const int64_t item = blockIdx.x;
-  const int tid = threadIdx.x, n = a.length(item), at = a.next[item] - 1;
-  for (int h = 0; h < a.g; ++h) {
-    const int64_t qh = item * a.g + h;
-    float* x = scores + qh * a.capacity;
-    __syncthreads();
-    if (tid < kHeadDim) {
-      s_q[tid] = __uint_as_float(static_cast<uint32_t>(q[qh * kHeadDim + tid]) << 16);
-      s_out[tid] = 0.f;
+// cap * tanh(s / cap).  Below 0.8 the fifth convergent of Lambert's continued fraction y / (1 + y^2 / (3 + y^2 / (5 + ..))), off by
+// less than 1e-8 of its value there; above, 1 - 2 / (e^2y + 1), which would lose the digits of small values.
+__device__ __forceinline__ float capped(float s, float cap, float inv_cap) {
+  const float y = s * inv_cap, y2 = y * y;
+  const float num = __builtin_fmaf(y2, y2 + 105.f, 945.f), den = __builtin_fmaf(y2, __builtin_fmaf(y2, 15.f, 420.f), 945.f);
+  const float small = y * num * __builtin_amdgcn_rcpf(den);
+  const float large = 1.f - 2.f * __builtin_amdgcn_rcpf(fast_exp2(fabsf(y) * (2.f * kLog2e)) + 1.f);
+  return cap * (fabsf(y) < 0.8f ? small : __builtin_copysignf(large, y));
+}
+
+// What a segment's wavefronts need to make scores of products.
+struct Scoring {
+  int n, at;                     // slots in use; the query's position
+  int g, sinks, window;
+  float cap, inv_cap;
+  bool where;                    // positions matter
+  const int32_t* pos;            // of the item
+  const float* slopes;           // of the item's heads, or null
+  float* scores;                 // of the item's heads, or null
+  int score_rows;
+};
+
+// xt: products q k times 1 / unit[head]; comes back as scores times log2(e), -inf where the slot is not seen.  The slots that are.
+template <int HS>
+__device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int pos, const float (&unit)[HS][4], float (&xt)[HS][4]) {
+  const int lane = threadIdx.x & 63, row = tile * kTile + lane;
+  bool seen = row < sc.n;
+  const int away = sc.at - pos;
+  if (sc.window > 0) seen = seen && (away < sc.window || pos < sc.sinks);
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int head = 4 * hs + i;
+      float s = xt[hs][i] * unit[hs][i];
+      if (sc.cap > 0.f) s = capped(s, sc.cap, sc.inv_cap);
+      if (sc.slopes != nullptr && head < sc.g) s = __builtin_fmaf(-sc.slopes[head], static_cast<float>(away), s);
+      xt[hs][i] = seen ? s * kLog2e : -INFINITY;
+      if (sc.scores != nullptr && head < sc.g) sc.scores[static_cast<int64_t>(head) * sc.score_rows + row] = xt[hs][i];
     }
-    __syncthreads();
-    float top = -INFINITY;
-    bool bad = false;
-    for (int i = tid; i < n; i += kThreads) {
-      float s = 0.f;
-      for (int c = 0; c < kHeadDim; ++c) s = fmaf(s_q[c], value<BITS, false>(a, item, i, c), s);
-      s *= 0.08838834764831845f;
-      if (a.cap > 0.f) s = a.cap * tanhf(s / a.cap);
-      const int pos = a.pos[item * a.capacity + i];
-      if (a.slopes) s -= a.slopes[qh % (a.hkv * a.g)] * static_cast<float>(at - pos);
-      if (a.window > 0 && at - pos >= a.window && pos >= a.sinks) s = -INFINITY;
-      x[i] = s;
-      bad |= s != s;
-      top = fmaxf(top, s);
-    }
-    top = bad ? NAN : top;
-    const auto all = [&](float v, bool sum) {
-      for (int d = 1; d < 64; d <<= 1) {
-        const float o = __shfl_xor(v, d);
-        v = sum ? v + o : (v != v || o != o) ? NAN : fmaxf(v, o);
+  return __builtin_amdgcn_ballot_w64(seen);
+}
+
+// Online softmax in the lanes (block, head); acc: whatever is scaled with the sums
+template <int HS>
+__device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& run, float (&p)[HS][4], float exponent) {
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) {
+    const float most = max_of_four(x[hs][0], x[hs][1], x[hs][2], x[hs][3]);
+    if (__any(most > run.m[hs])) {
+      const float m_new = fmaxf(run.m[hs], head_max(most));
+      const float alpha = fast_exp2(run.m[hs] - m_new);
+      run.l[hs] *= alpha;
+      const uint32_t au = __builtin_bit_cast(uint32_t, alpha);
+      const float ah[4] = {__builtin_bit_cast(float, quad_bcast<0>(au)), __builtin_bit_cast(float, quad_bcast<1>(au)),
+                           __builtin_bit_cast(float, quad_bcast<2>(au)), __builtin_bit_cast(float, quad_bcast<3>(au))};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) run.acc[hs][grp][i] *= ah[i];
+        run.offv[hs][i] *= ah[i];
       }
-      __syncthreads();
-      if ((tid & 63) == 0) s_red[tid >> 6] = v;
-      __syncthreads();
-      v = s_red[0];
-      for (int w = 1; w < kThreads / 64; ++w) v = sum ? v + s_red[w] : (v != v || s_red[w] != s_red[w]) ? NAN : fmaxf(v, s_red[w]);
-      return v;
-    };
-    top = all(top, false);
-    float l = 0.f;
-    for (int i = tid; i < n; i += kThreads) l += x[i] == -INFINITY ? 0.f : expf(x[i] - top);
-    l = all(l, true);
-    const float inv = 1.0f / l;
-    // channel, half of the slots
-    const int c = tid & 127, half = tid >> 7;
-    float o = 0.f;
-    for (int i = half; i < n; i += 2)
-      if (x[i] != -INFINITY) o = fmaf(expf(x[i] - top) * inv, value<BITS, true>(a, item, i, c), o);
-    if (half == 1) s_out[c] = o;
+      run.m[hs] = m_new;
+    }
+    const float up = exponent - run.m[hs];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[hs][i] = fast_exp2(x[hs][i] + up);
+      run.l[hs] += p[hs][i];
+    }
+  }
+}
+
+template <int HS>
+__device__ __forceinline__ void init(Run<HS>& run) {
+  run.init();
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) run.m[hs] = kLowest;
+}
+
+// ---- bf16 rows ---------------------------------------------------------------------------------------------------------------------
+
+// a probability as three truncated bf16 terms: all of its 24 bits
+__device__ __forceinline__ void split_bf16_3(const float (&p)[4], short4v (&t)[3]) {
+  float r[4] = {p[0], p[1], p[2], p[3]};
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      b[i] = __float_as_uint(r[i]) & 0xFFFF0000u;
+      r[i] -= __uint_as_float(b[i]);
+    }
+    t[k] = bf4((b[0] >> 16) | b[1], (b[2] >> 16) | b[3]);
+  }
+}
+
+template <int A, int HS>
+__device__ __forceinline__ void pv_rows_step(const uint8_t* s_stage, int lane, const short4v (&t)[HS][3], Run<HS>& run) {
+  uint32_t w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t*>(s_stage + (4 * A + k) * kRowStride + 4 * lane);
+  const short4v be = bf4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u));
+  const short4v bo = bf4(__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u));
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      run.acc[hs][0] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(t[hs][k], be, run.acc[hs][0], 4, A, 0);
+      run.acc[hs][1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(t[hs][k], bo, run.acc[hs][1], 4, A, 0);
+    }
+}
+template <int HS, int... A>
+__device__ __forceinline__ void pv_rows(const uint8_t* s_stage, int lane, const short4v (&t)[HS][3], Run<HS>& run, std::integer_sequence<int, A...>) {
+  (pv_rows_step<A, HS>(s_stage, lane, t, run), ...);
+}
+
+// Tiles t0 .. t1 - 1 of an item, the workgroup's wavefronts in turn.  kd, vd: the item's rows.
+template <int HS, int NWV>
+__device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
+                                             const Scoring& sc, int t0, int t1, uint8_t* s_stage, Run<HS>& run) {
+  const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int last = sc.n - 1;
+  const int lr = lane >> 4, lc = lane & 15;
+  uint4 st[16];
+  auto load_tile = [&](const uint8_t* __restrict__ base, int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st[i] = load_row_chunk(base, min(t * kTile + 4 * i + lr, last), lc);
+  };
+  auto store_tile = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(s_stage + (4 * i + lr) * kRowStride + 16 * lc) = st[i];
+  };
+  auto load_pos = [&](int t) __attribute__((always_inline)) { return sc.where ? sc.pos[min(t * kTile + lane, last)] : 0; };
+  uint4 qa[HS];
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) qa[hs] = load_query(q, 4 * hs + j, sc.g, blk);
+  int pos = 0;
+  if (t0 + wave < t1) {
+    pos = load_pos(t0 + wave);
+    load_tile(kd, t0 + wave);
+  }
+  float unit[HS][4];
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unit[hs][i] = 0.08838834764831845f;      // 1 / sqrt(128)
+  const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
+  for (int tile = t0 + wave; tile < t1; tile += NWV) {
+    const int next = tile + NWV;
+    store_tile();                       // K rows of this tile
+    load_tile(vd, tile);                // V rows: in flight during the scores
+    const int pos_now = pos;
+    if (next < t1) pos = load_pos(next);
+    wave_lds_sync();
+    floatx4 a16[HS];
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs) a16[hs] = zero4;
+#define RDKV_ROWS_K(I_)                                                                                              \
+  {                                                                                                                 \
+    const uint4 kr = *reinterpret_cast<const uint4*>(s_stage + lane * kRowStride + 16 * (I_));                      \
+    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) {                                                             \
+      a16[hs] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(bf4(qa[hs].x, qa[hs].y), bf4(kr.x, kr.y), a16[hs], 4, I_, 0); \
+      a16[hs] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(bf4(qa[hs].z, qa[hs].w), bf4(kr.z, kr.w), a16[hs], 4, I_, 0); \
+    }                                                                                                               \
+  }
+    RDKV_ROWS_K(0) RDKV_ROWS_K(1) RDKV_ROWS_K(2) RDKV_ROWS_K(3) RDKV_ROWS_K(4) RDKV_ROWS_K(5) RDKV_ROWS_K(6)
+    RDKV_ROWS_K(7) RDKV_ROWS_K(8) RDKV_ROWS_K(9) RDKV_ROWS_K(10) RDKV_ROWS_K(11) RDKV_ROWS_K(12) RDKV_ROWS_K(13)
+    RDKV_ROWS_K(14) RDKV_ROWS_K(15)
+#undef RDKV_ROWS_K
+    float xt[HS][4], x[HS][4];
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xt[hs][i] = a16[hs][i];
+    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
+    to_head_lanes<HS, HS == 2>(xt, j, x);
+    float p[HS][4];
+    softmax_step<HS>(x, run, p, 0.f);
+    short4v t[HS][3];
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs) split_bf16_3(p[hs], t[hs]);
+    if (seen != ~0ull) {                // rows that are not seen may hold anything: 0 x NaN
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!((seen >> (4 * i + lr)) & 1)) st[i] = make_uint4(0, 0, 0, 0);
+    }
+    wave_lds_sync();                    // every lane is done with the K rows
+    store_tile();                       // V rows
+    if (next < t1) load_tile(kd, next);
+    wave_lds_sync();
+    pv_rows<HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 16>{});
+    wave_lds_sync();                    // before the next tile's K rows overwrite the region
+  }
+}
+
+// ---- 4-bit rows --------------------------------------------------------------------------------------------------------------------
+// (operand layouts and the codes as fp16 subnormals: decode_mfma_kernels.hip)
+
+// The four codes of step S of a group's words as fp16 numbers code 2^-18: subnormals with the code's highest bit in the mantissa's.
+// (As code 2^-24, one AND less in two, they cost precision: the matrix unit lines up a product by its operands' exponents, a
+// subnormal's being the lowest whatever zeros it starts with, and cuts the sum off 24 bits below; the products of codes 2^-24 left
+// the accumulators 18 bits.)
+__device__ __forceinline__ half4 code_operand(const uint4& gw, int s) {
+  constexpr uint32_t kMask = 0x03C003C0u;
+  const uint32_t w0 = s < 4 ? gw.x : gw.z, w1 = s < 4 ? gw.y : gw.w;
+  Pack4 r;
+  switch (s & 3) {
+    case 0: r.u[0] = (w0 << 6) & kMask; r.u[1] = (w1 << 6) & kMask; break;
+    case 1: r.u[0] = (w0 << 2) & kMask; r.u[1] = (w1 << 2) & kMask; break;
+    case 2: r.u[0] = (w0 >> 2) & kMask; r.u[1] = (w1 >> 2) & kMask; break;
+    default: r.u[0] = (w0 >> 6) & kMask; r.u[1] = (w1 >> 6) & kMask; break;
+  }
+  return r.h;
+}
+constexpr float kCode = 262144.0f;       // 2^18
+
+constexpr int kQUp = 8;                  // the query's largest value is near 2^kQUp
+constexpr float kPUp = 15.0f;            // probabilities are carried times 2^kPUp
+
+__device__ __forceinline__ int exponent_of(float x) {      // of a number > 0; bounds for the others
+  return static_cast<int>((__float_as_uint(x) >> 23) & 255u) - 127;
+}
+
+template <int HS, int NWV>
+__device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
+                                               const Scoring& sc, int t0, int t1, Run<HS>& run) {
+  const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint4 qraw[HS];
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) qraw[hs] = load_query(q, 4 * hs + j, sc.g, blk);
+  uint4 kr[4], vr[4], kmeta = make_uint4(0, 0, 0, 0), vmeta = kmeta;
+  int pos = 0;
+  auto load_k = [&](int t) __attribute__((always_inline)) {
+    const uint8_t* p = kd + static_cast<int64_t>(t) * kTileBytes + lane * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) kr[i] = *reinterpret_cast<const uint4*>(p + 1024 * i);
+    kmeta = *reinterpret_cast<const uint4*>(p + 4096);
+    if (sc.where) pos = sc.pos[min(t * kTile + lane, sc.n - 1)];
+  };
+  auto load_v = [&](int t) __attribute__((always_inline)) {
+    const uint8_t* p = vd + static_cast<int64_t>(t) * kTileBytes + lane * 16;
+    vmeta = *reinterpret_cast<const uint4*>(p + 4096);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + 1024 * i);
+  };
+  if (t0 + wave < t1) {
+    load_k(t0 + wave);
+    load_v(t0 + wave);
+  }
+
+  // ---- query operands: every head times its own power of two, so that its largest value is near 2^kQUp ---------------
+  half4 qop[HS][2], qhi[HS], qlo[HS];
+  float unit[HS][4];
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) {
+    const uint32_t w[4] = {qraw[hs].x, qraw[hs].y, qraw[hs].z, qraw[hs].w};
+    float v[8], most = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = __uint_as_float(w[k] << 16);
+      v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      most = fmaxf(most, fmaxf(fabsf(v[2 * k]), fabsf(v[2 * k + 1])));
+    }
+    most = head_max(most);
+    const int up = max(-120, min(120, kQUp - exponent_of(most)));      // (zeros, NaN and infinities stay what they are)
+    float psum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      v[k] = ldexpf(v[k], up);
+      psum += v[k];
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      qop[hs][e] = half4{static_cast<_Float16>(v[4 * e]), static_cast<_Float16>(v[4 * e + 1]), static_cast<_Float16>(v[4 * e + 2]),
+                         static_cast<_Float16>(v[4 * e + 3])};
+    psum += dpp_f32<0x124>(psum);
+    psum += dpp_f32<0x128>(psum);
+    float s0 = psum, s1 = psum;          // rows 0 .. 3 of 16 lanes = groups 0 .. 3: every lane gets all four
+    swap_rows(s0, s1);
+    float s2 = s0, s3 = s1;
+    swap_halves(s0, s2);
+    swap_halves(s1, s3);
+    const float sg[4] = {s0, s1, s2, s3};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      qhi[hs][k] = static_cast<_Float16>(sg[k]);
+      qlo[hs][k] = static_cast<_Float16>(sg[k] - static_cast<float>(qhi[hs][k]));
+    }
+    const uint32_t u = __float_as_uint(ldexpf(0.08838834764831845f, -up));
+    unit[hs][0] = __uint_as_float(quad_bcast<0>(u));
+    unit[hs][1] = __uint_as_float(quad_bcast<1>(u));
+    unit[hs][2] = __uint_as_float(quad_bcast<2>(u));
+    unit[hs][3] = __uint_as_float(quad_bcast<3>(u));
+  }
+  int ve = -126;                         // exponent of the largest V scale so far
+  float vf = 0.f;                        // what p is multiplied by for it
+  const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
+
+  for (int tile = t0 + wave; tile < t1; tile += NWV) {
+    const int next = tile + NWV;
+    const bool more = next < t1;
+    float xt[HS][4], x[HS][4];
+    const int pos_now = pos;
+    {
+      Pack4 boff;
+      boff.u[0] = kmeta.z;
+      boff.u[1] = kmeta.w;
+#pragma unroll
+      for (int hs = 0; hs < HS; ++hs) {
+        floatx4 d = __builtin_amdgcn_mfma_f32_4x4x4f16(qhi[hs], boff.h, zero4, 0, 0, 0);
+        d = __builtin_amdgcn_mfma_f32_4x4x4f16(qlo[hs], boff.h, d, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xt[hs][i] = d[i];
+      }
+#define RDKV_K_STEP(G_, S_)                                                                                        \
+  {                                                                                                               \
+    const half4 b = code_operand(gw, S_);                                                                      \
+    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs)                                                             \
+        dg[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(qop[hs][(S_) & 1], b, dg[hs], 4, (G_) * 4 + (S_) / 2, 0);     \
+  }
+#define RDKV_K_GROUP(G_)                                                                                           \
+  {                                                                                                               \
+    __builtin_amdgcn_sched_barrier(0);                                                                            \
+    const uint4 gw = kr[G_];                                                                                      \
+    floatx4 dg[HS];                                                                                               \
+    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) dg[hs] = zero4;                                             \
+    RDKV_K_STEP(G_, 0) RDKV_K_STEP(G_, 1) RDKV_K_STEP(G_, 2) RDKV_K_STEP(G_, 3)                                   \
+    RDKV_K_STEP(G_, 4) RDKV_K_STEP(G_, 5) RDKV_K_STEP(G_, 6) RDKV_K_STEP(G_, 7)                                   \
+    const float sf = kCode * static_cast<float>(__builtin_bit_cast(half2v, (G_) < 2 ? kmeta.x : kmeta.y)[(G_) & 1]); \
+    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs)                                                             \
+      _Pragma("unroll") for (int i = 0; i < 4; ++i) xt[hs][i] = __builtin_fmaf(sf, dg[hs][i], xt[hs][i]);         \
+  }
+      RDKV_K_GROUP(0) RDKV_K_GROUP(1) RDKV_K_GROUP(2) RDKV_K_GROUP(3)
+#undef RDKV_K_GROUP
+#undef RDKV_K_STEP
+    }
+    if (more) load_k(next);
+    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
+    to_head_lanes<HS, HS == 2>(xt, j, x);
+    float p[HS][4];
+    softmax_step<HS>(x, run, p, kPUp);
+
+    // ---- P V ---------------------------------------------------------------------------------------------------------
+    uint4 vm = vmeta;
+    if (seen != ~0ull) {                 // scales and offsets of rows that are not seen may be anything
+      const uint32_t four = static_cast<uint32_t>(seen >> (4 * blk)) & 15u;
+      const uint32_t lo = ((four & 1u) ? 0xFFFFu : 0u) | ((four & 2u) ? 0xFFFF0000u : 0u);
+      const uint32_t hi = ((four & 4u) ? 0xFFFFu : 0u) | ((four & 8u) ? 0xFFFF0000u : 0u);
+      vm = make_uint4(vm.x & lo, vm.y & hi, vm.z & lo, vm.w & hi);
+    }
+    {
+      // a scale above all before: everything gathered so far goes down by as much
+      const half2v a = __builtin_bit_cast(half2v, vm.x), c = __builtin_bit_cast(half2v, vm.y);
+      const float most = fmaxf(fmaxf(static_cast<float>(a[0]), static_cast<float>(a[1])), fmaxf(static_cast<float>(c[0]), static_cast<float>(c[1])));
+      if (__any(most >= ldexpf(1.0f, ve + 1))) {
+        const int e = __builtin_amdgcn_readfirstlane(max(ve, min(16, exponent_of(wave_max(most)))));
+        const float down = ldexpf(1.0f, ve - e);
+#pragma unroll
+        for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+          for (int grp = 0; grp < 4; ++grp)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) run.acc[hs][grp][i] *= down;
+        ve = e;
+        vf = ldexpf(1.0f, -1 - ve);
+      }
+    }
+    Pack4 ob;
+    ob.u[0] = vm.z;
+    ob.u[1] = vm.w;
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs) {
+      Pack4 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const auto h = __builtin_amdgcn_cvt_pkrtz(p[hs][2 * i], p[hs][2 * i + 1]);
+        hi.p[i] = __builtin_bit_cast(half2v, h);
+        lo.p[i] = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(p[hs][2 * i] - static_cast<float>(hi.p[i][0]), p[hs][2 * i + 1] - static_cast<float>(hi.p[i][1])));
+      }
+      run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi.h, ob.h, run.offv[hs], 0, 0, 0);
+      run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo.h, ob.h, run.offv[hs], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[hs][i] *= vf;
+    }
+#define RDKV_PV_STEP(G_, A_)                                                                                   \
+  {                                                                                                            \
+    const half4 b = code_operand(gw, A_);                                                                      \
+    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) {                                                        \
+      run.acc[hs][G_] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi[hs].h, b, run.acc[hs][G_], 3, A_, 0);            \
+      run.acc[hs][G_] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo[hs].h, b, run.acc[hs][G_], 3, A_, 0);            \
+    }                                                                                                          \
+  }
+#define RDKV_PV_GROUP(G_)                                                                                      \
+  {                                                                                                            \
+    __builtin_amdgcn_sched_barrier(0);                                                                         \
+    Pack4 sv, hi[HS], lo[HS];                                                                                  \
+    sv.u[0] = quad_bcast<G_>(vm.x); sv.u[1] = quad_bcast<G_>(vm.y);                                            \
+    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) {                                                        \
+      _Pragma("unroll") for (int i = 0; i < 2; ++i) {                                                          \
+        const float p0 = p[hs][2 * i] * static_cast<float>(sv.p[i][0]), p1 = p[hs][2 * i + 1] * static_cast<float>(sv.p[i][1]); \
+        hi[hs].p[i] = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(p0, p1));                          \
+        lo[hs].p[i] = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(p0 - static_cast<float>(hi[hs].p[i][0]), p1 - static_cast<float>(hi[hs].p[i][1]))); \
+      }                                                                                                        \
+    }                                                                                                          \
+    const uint4 gw = vr[G_];                                                                                   \
+    RDKV_PV_STEP(G_, 0) RDKV_PV_STEP(G_, 1) RDKV_PV_STEP(G_, 2) RDKV_PV_STEP(G_, 3)                            \
+    RDKV_PV_STEP(G_, 4) RDKV_PV_STEP(G_, 5) RDKV_PV_STEP(G_, 6) RDKV_PV_STEP(G_, 7)                            \
+  }
+    RDKV_PV_GROUP(0) RDKV_PV_GROUP(1) RDKV_PV_GROUP(2) RDKV_PV_GROUP(3)
+#undef RDKV_PV_GROUP
+#undef RDKV_PV_STEP
+    if (more) load_v(next);
+  }
+  // what brings the accumulators to the sums' scale: 2^18 of the codes, 2^(1 + ve) of vf
+  return ldexpf(1.0f, 19 + ve);
+}
+
+// ---- the end of a piece --------------------------------------------------------------------------------------------------------------
+
+// LDS of the wavefronts' merge, floats: per wavefront, head and channel group (maximum, sum, offset sum, -), then the sums [wave][g][128];
+// then the heads' log-sum-exps for the weights.
+template <int NWV, int HS>
+constexpr int ml_floats() { return ml_lds_floats(NWV, HS); }
+
+// weights of slots r0 .. r1 - 1 of an item: lse2 of its heads, log2
+__device__ __forceinline__ void add_weights(const Args& a, int64_t item, const float* __restrict__ scores, int score_rows, int g, const float* lse2,
+                                            int r0, int r1, int thread, int threads) {
+  float* __restrict__ weight = a.weight + item * a.capacity;
+  for (int i = r0 + thread; i < r1; i += threads) {
+    float p = 0.f;
+    for (int h = 0; h < g; ++h) p += fast_exp2(scores[static_cast<int64_t>(h) * score_rows + i] - lse2[h]);
+    weight[i] = __builtin_fmaf(a.decay, weight[i], p);
+  }
+}
+
+// log2 of the sum of 2^score over everything: sum l, relative to 2^m; +inf where nothing was seen, which makes every weight 0
+__device__ __forceinline__ float total_log2(float m, float l) { return l == 0.f ? INFINITY : m + __log2f(l); }
+
+template <int BITS, int HS, int NWV>
+__global__ __launch_bounds__(NWV * 64, BITS == 16 ? 2 : HS == 1 ? 4 : 3) void decode_kernel(DecodeArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = a.s.g;
+  const Line line = make_line(a, gridDim.x);
+  int at = static_cast<int>(blockIdx.x) * line.share;
+  // items without a token have no tile: their outputs are the first workgroups' to write
+  for (int item = blockIdx.x; item < a.items; item += gridDim.x)
+    if (a.s.length(item) == 0) {
+      for (int i = tid; i < g * kHeadDim; i += NWV * 64) a.out[static_cast<int64_t>(item) * g * kHeadDim + i] = 0.f;
+      if (a.lse != nullptr && tid < g) a.lse[static_cast<int64_t>(item) * g + tid] = -INFINITY;
+    }
+  if (at >= line.total) return;
+  const int end = min(at + line.share, line.total);
+  int first;
+  int item = item_at(a, at, &first);
+  float* s_ml = reinterpret_cast<float*>(smem + (BITS == 16 ? NWV * kStageBytes : 0));
+  float* s_acc = BITS == 16 ? reinterpret_cast<float*>(smem) : s_ml + ml_floats<NWV, HS>();
+  float* s_lse = BITS == 16 ? s_ml + ml_floats<NWV, HS>() : s_acc + NWV * g * kHeadDim;
+  while (at < end) {
+    const int n = a.s.length(item), tiles = (n + kTile - 1) / kTile;
+    const int t0 = at - first, t1 = min(tiles, end - first);
+    if (t1 <= t0) {                      // an item without tiles
+      ++item;
+      continue;
+    }
+    const bool whole = t0 == 0 && t1 == tiles;
+    Scoring sc;
+    sc.n = n;
+    sc.at = a.s.next[item] - 1;
+    sc.g = g;
+    sc.sinks = a.s.sinks;
+    sc.window = a.s.window;
+    sc.cap = a.s.cap;
+    sc.inv_cap = a.s.cap > 0.f ? 1.0f / a.s.cap : 0.f;
+    sc.where = a.s.window > 0 || a.s.slopes != nullptr;
+    sc.pos = a.s.pos + static_cast<int64_t>(item) * a.s.capacity;
+    sc.slopes = a.s.slopes ? a.s.slopes + (item % a.s.hkv) * g : nullptr;
+    sc.scores = a.scores ? a.scores + static_cast<int64_t>(item) * g * a.score_rows : nullptr;
+    sc.score_rows = a.score_rows;
+    const uint16_t* q = a.q + static_cast<int64_t>(item) * g * kHeadDim;
+    Run<HS> run;
+    init(run);
+    float scale = 1.f;
+    if constexpr (BITS == 16) {
+      const int64_t base = static_cast<int64_t>(item) * a.s.capacity * (kHeadDim * 2);
+      rows_segment<HS, NWV>(a.s.k + base, a.s.v + base, q, sc, t0, t1, smem + wave * kStageBytes, run);
+      __syncthreads();                   // the staging regions become the accumulator area
+    } else {
+      const int64_t base = static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
+      scale = tiles_segment<HS, NWV>(a.s.k + base, a.s.v + base, q, sc, t0, t1, run);
+    }
+    // ---- the wavefronts' results into LDS ------------------------------------------------------------------------------
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs) {
+      run.l[hs] = head_sum(run.l[hs]);
+      float off = 0.f;
+      if constexpr (BITS == 4) {         // lanes (block, j): head i's sum of p m of group j over the block's tokens
+        float o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = run.offv[hs][i];
+        swap_rows(o[0], o[1]);
+        swap_rows(o[2], o[3]);
+        float lo = o[0] + o[1], hi = o[2] + o[3];
+        swap_halves(lo, hi);
+        off = lo + hi;
+        off += dpp_f32<0x124>(off);
+        off += dpp_f32<0x128>(off);
+        if ((lane & 12) == 0) s_ml[ml_at<HS>(wave, 4 * hs + (lane >> 4), lane & 3) + 2] = off;
+      }
+      if (lane < 16)                     // (block, j) -> group block of head j
+        *reinterpret_cast<float2*>(s_ml + ml_at<HS>(wave, 4 * hs + (lane & 3), lane >> 2)) =
+            make_float2(BITS == 4 ? run.m[hs] - kPUp : run.m[hs], run.l[hs]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int head = 4 * hs + i;
+        float* dst = s_acc + (wave * g + head) * kHeadDim;
+        if constexpr (BITS == 16) {
+          if (head < g) *reinterpret_cast<float2*>(dst + 2 * lane) = make_float2(run.acc[hs][0][i], run.acc[hs][1][i]);
+        } else {
+          const float v0 = halves_sum(run.acc[hs][0][i], run.acc[hs][1][i]), v1 = halves_sum(run.acc[hs][2][i], run.acc[hs][3][i]);
+          if (head < g) {
+            dst[lane] = v0 * scale;
+            dst[64 + lane] = v1 * scale;
+          }
+        }
+      }
+    }
     __syncthreads();
-    if (half == 0) out[qh * kHeadDim + c] = n == 0 || l == 0.f ? 0.f : o + s_out[c];
-    if (tid == 0 && lse) lse[qh] = l == 0.f ? -INFINITY : top + logf(l);
-    if (tid == 0) {
-      s_top[h] = top;
-      s_inv[h] = l == 0.f ? 0.f : inv;
+    // ---- a wavefront per head adds them up -----------------------------------------------------------------------------
+    const int64_t qh0 = static_cast<int64_t>(item) * g, slot = static_cast<int64_t>(blockIdx.x) + item;
+    for (int head = wave; head < g; head += NWV) {
+      const int ch = 2 * lane;
+      float mm = kLowest;
+#pragma unroll
+      for (int w = 0; w < NWV; ++w) mm = fmaxf(mm, s_ml[ml_at<HS>(w, head, 0)]);
+      float l = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < NWV; ++w) {
+        const float2 ml = *reinterpret_cast<const float2*>(s_ml + ml_at<HS>(w, head, 0));
+        const float2 acc = *reinterpret_cast<const float2*>(s_acc + (w * g + head) * kHeadDim + ch);
+        const float off = BITS == 4 ? s_ml[ml_at<HS>(w, head, lane >> 4) + 2] : 0.f;
+        const float f = fast_exp2(ml.x - mm);
+        l = __builtin_fmaf(ml.y, f, l);
+        v0 = __builtin_fmaf(acc.x + off, f, v0);
+        v1 = __builtin_fmaf(acc.y + off, f, v1);
+      }
+      if (whole) {
+        const float inv = 1.0f / l;
+        *reinterpret_cast<float2*>(a.out + (qh0 + head) * kHeadDim + ch) = l == 0.f ? make_float2(0.f, 0.f) : make_float2(v0 * inv, v1 * inv);
+        if (lane == 0) {
+          if (a.lse != nullptr) a.lse[qh0 + head] = l == 0.f ? -INFINITY : (mm + __log2f(l)) * 0.6931471805599453f;
+          s_lse[head] = total_log2(mm, l);
+        }
+      } else {
+        *reinterpret_cast<float2*>(a.part_acc + (slot * g + head) * kHeadDim + ch) = make_float2(v0, v1);
+        if (lane == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * g + head) * 2) = make_float2(mm, l);
+      }
+    }
+    __syncthreads();
+    if (whole && a.scores != nullptr) {
+      add_weights(a.s, item, sc.scores, sc.score_rows, g, s_lse, 0, n, tid, NWV * 64);
+      __syncthreads();
+    }
+    at = first + t1;
+    if (t1 == tiles) {
+      first += tiles;
+      ++item;
+    }
+  }
+}
+
+// The items whose tiles several workgroups shared: their partials into the outputs, and their weights.  n_groups: workgroups of
+// the launch before.  `rows` workgroups an item.
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int n_groups, int rows) {
+  __shared__ float s_lse[8], s_top[8], s_half[kHeadDim];
+  const int item = blockIdx.x / rows, row = blockIdx.x % rows, tid = threadIdx.x, lane = tid & 63, g = a.s.g;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Line line = make_line(a, n_groups);
+  const int n = a.s.length(item), tiles = (n + kTile - 1) / kTile;
+  if (tiles == 0) return;
+  const int before = tiles_before(a, item);
+  const int w0 = before / line.share, w1 = (before + tiles - 1) / line.share;
+  if (w0 == w1) return;
+  const int64_t slot0 = static_cast<int64_t>(w0) + item, qh0 = static_cast<int64_t>(item) * g;
+  const int parts = w1 - w0 + 1;
+  for (int head = wave; head < g; head += kJoinThreads / 64) {
+    float m = kLowest, l = 0.f;
+    for (int k = lane; k < parts; k += 64) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * g + head) * 2);
+      const float mm = fmaxf(m, ml.x);
+      l = l * fast_exp2(m - mm) + ml.y * fast_exp2(ml.x - mm);
+      m = mm;
+    }
+    float top = m;
+    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    l *= fast_exp2(m - top);
+    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+    if (lane == 0) {
+      s_top[head] = top;
+      s_lse[head] = total_log2(top, l);
     }
   }
   __syncthreads();
-  if (a.weight)
-    for (int i = tid; i < n; i += kThreads) {
-      float p = 0.f;
-      for (int h = 0; h < a.g; ++h) {
-        const float x = scores[(item * a.g + h) * a.capacity + i];
-        p += s_inv[h] == 0.f || (x == -INFINITY && s_inv[h] == s_inv[h]) ? 0.f : expf(x - s_top[h]) * s_inv[h];
-      }
-      float& w = a.weight[item * a.capacity + i];
-      w = a.decay * w + p;
+  // heads among the row's workgroups: two halves of the partials, a channel a thread
+  for (int head = row; head < g; head += rows) {
+    const int c = tid & (kHeadDim - 1), half = tid >> 7;
+    const float top = s_top[head];
+    float v = 0.f, l = 0.f;
+    for (int k = half; k < parts; k += 2) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * g + head) * 2);
+      const float f = fast_exp2(ml.x - top);
+      v = __builtin_fmaf(a.part_acc[((slot0 + k) * g + head) * kHeadDim + c], f, v);
     }
+    if (half == 1) s_half[c] = v;
+    __syncthreads();
+    if (half == 0) {
+      v += s_half[c];
+      l = s_lse[head];
+      a.out[(qh0 + head) * kHeadDim + c] = l == INFINITY ? 0.f : v * fast_exp2(top - l);
+      if (c == 0 && a.lse != nullptr) a.lse[qh0 + head] = l == INFINITY ? -INFINITY : l * 0.6931471805599453f;
+    }
+    __syncthreads();
+  }
+  if (a.scores == nullptr) return;
+  const int each = (tiles + rows - 1) / rows * kTile, r0 = row * each;
+  add_weights(a.s, item, a.scores + qh0 * a.score_rows, a.score_rows, g, s_lse, r0, min(n, r0 + each), tid, kJoinThreads);
+}
+
+struct Plan {
+  int groups, least, score_rows;
+  size_t scores, part_acc, part_ml;      // floats
+};
+Plan make_plan(int64_t items, int g, int capacity, int bits) {
+  Plan p;
+  const int64_t tiles = (capacity + kTile - 1) / kTile;
+  const int waves = bits == 4 && g <= 4 ? 8 : 4;
+  p.least = waves;
+  p.score_rows = static_cast<int>(tiles) * kTile;
+  const int64_t most = (items * tiles + waves - 1) / waves;
+  const int64_t resident = bits == 4 && g > 4 ? 768 : 512;
+  p.groups = static_cast<int>(most < resident ? most : resident);
+  p.scores = static_cast<size_t>(items) * g * p.score_rows;
+  const size_t slots = static_cast<size_t>(p.groups) + items;
+  p.part_acc = slots * g * kHeadDim;
+  p.part_ml = slots * g * 2;
+  return p;
+}
+
+template <int BITS, int HS, int NWV>
+hipError_t launch(const DecodeArgs& a, const Plan& p, hipStream_t st) {
+  const size_t ml = ml_floats<NWV, HS>() * sizeof(float), acc = static_cast<size_t>(NWV) * a.s.g * kHeadDim * sizeof(float), lse = 8 * sizeof(float);
+  const size_t lds = BITS == 16 ? NWV * kStageBytes + ml + lse : ml + acc + lse;
+  constexpr size_t kMost = BITS == 16 ? NWV * kStageBytes + ml_floats<NWV, HS>() * 4 + 32 : ml_floats<NWV, HS>() * 4 + NWV * 4 * HS * kHeadDim * 4 + 32;
+  const hipError_t e = RDKV_ALLOW_LDS((decode_kernel<BITS, HS, NWV>), kMost);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((decode_kernel<BITS, HS, NWV>), dim3(p.groups), dim3(NWV * 64), lds, st, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t decode_workspace_floats(int64_t items, int g, int capacity) { return static_cast<size_t>(items) * g * capacity; }
+size_t decode_workspace_floats(int64_t items, int g, int capacity, int bits, bool weights) {
+  const Plan p = make_plan(items, g, capacity, bits);
+  return (weights ? p.scores : 0) + p.part_acc + p.part_ml;
+}
 
-hipError_t launch_decode(const Args& a, int bits, int items, const uint16_t* q, float* out, float* lse, float* workspace, hipStream_t st) {
-  if (bits == 16) hipLaunchKernelGGL(decode_kernel<16>, dim3(items), dim3(kThreads), 0, st, a, q, out, lse, workspace);
-  else hipLaunchKernelGGL(decode_kernel<4>, dim3(items), dim3(kThreads), 0, st, a, q, out, lse, workspace);
+hipError_t launch_decode(const Args& s, int bits, int items, const uint16_t* q, float* out, float* lse, float* workspace, hipStream_t st) {
+  const Plan p = make_plan(items, s.g, s.capacity, bits);
+  DecodeArgs a;
+  a.s = s;
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.part_acc = workspace;                // (two floats at a time)
+  a.part_ml = workspace + p.part_acc;
+  a.scores = s.weight ? a.part_ml + p.part_ml : nullptr;
+  a.items = items;
+  a.score_rows = p.score_rows;
+  a.least = p.least;
+  hipError_t e;
+  if (bits == 16) e = s.g > 4 ? launch<16, 2, 4>(a, p, st) : launch<16, 1, 4>(a, p, st);
+  else e = s.g > 4 ? launch<4, 2, 4>(a, p, st) : launch<4, 1, 8>(a, p, st);
+  if (e != hipSuccess || p.groups == 1) return e;
+  const int rows = std::max(1, std::min({64, (p.score_rows + 2047) / 2048, 8192 / items}));
+  hipLaunchKernelGGL(join_kernel, dim3(items * rows), dim3(kJoinThreads), 0, st, a, p.groups, rows);
   return hipGetLastError();
 }
 

@@ -268,10 +268,10 @@ __device__ __forceinline__ uint32_t to_bf16(float x) {
 }
 
 template <int BITS>
-__global__ __launch_bounds__(256) void read_kernel(Args a, const int32_t* __restrict__ index, int n, uint16_t* __restrict__ K,
+__global__ __launch_bounds__(256) void read_kernel(Args a, const int32_t* __restrict__ index, int n, int groups, uint16_t* __restrict__ K,
                                                    uint16_t* __restrict__ V) {
-  const int64_t item = blockIdx.y;
-  const int i = blockIdx.x * 16 + (threadIdx.x >> 4), c16 = threadIdx.x & 15;
+  const int64_t item = blockIdx.x / groups;
+  const int i = static_cast<int>(blockIdx.x % groups) * 16 + (threadIdx.x >> 4), c16 = threadIdx.x & 15;
   if (i >= n) return;
   const int slot = index ? index[item * n + i] : i;
   const int64_t to = (item * n + i) * 16 + c16;
@@ -334,10 +334,11 @@ hipError_t launch_append(const Args& a, int bits, int items, const uint16_t* k_n
 }
 
 hipError_t launch_read(const Args& a, int bits, int items, const int32_t* index, int n, uint16_t* K, uint16_t* V, hipStream_t st) {
+  const int groups = (n + 15) / 16;        // (of 16 rows; less than 2^27 in all)
   if (bits == 16)
-    hipLaunchKernelGGL(read_kernel<16>, dim3((n + 15) / 16, items), dim3(256), 0, st, a, index, n, K, V);
+    hipLaunchKernelGGL(read_kernel<16>, dim3(groups * items), dim3(256), 0, st, a, index, n, groups, K, V);
   else
-    hipLaunchKernelGGL(read_kernel<4>, dim3((n + 15) / 16, items), dim3(256), 0, st, a, index, n, K, V);
+    hipLaunchKernelGGL(read_kernel<4>, dim3(groups * items), dim3(256), 0, st, a, index, n, groups, K, V);
   return hipGetLastError();
 }
 

@@ -24,6 +24,18 @@ def held(rows, bits):
     return O.dequantize_groups(c.reshape(n, 4, 32), s, m).reshape(n, D)
 
 
+def terms(rows, bits):
+    """Sizes of the terms that a kernel adds up for these rows' values.  Of 4-bit rows those are scale x code and the offset, each
+    multiplied and summed by itself and rounded relative to itself, wherever they nearly cancel: off by 2^-24 of their sizes per
+    operation, not of the value's."""
+    rows = np.asarray(rows, np.float32)
+    if bits == 16:
+        return np.abs(rows).astype(np.float64)
+    c, s, m = O.quantize_rows(rows, 4)
+    n = rows.shape[0]
+    return (np.abs(O.dequantize_groups(c.reshape(n, 4, 32), s, 0 * m)) + np.abs(m.astype(np.float64))[..., None]).reshape(n, D)
+
+
 def choose(T, capacity, sinks, recent, w):
     """Positions a filled item keeps, ascending."""
     if T <= capacity:
@@ -44,8 +56,9 @@ def evict(pos, weight, nxt, sinks, recent):
     return int(may[np.lexsort((pos[may], np.where(np.isnan(v), 0.0, v), ~np.isnan(v)))[0]])
 
 
-def attend(q, K, V, pos, nxt, sinks=0, window=0, cap=0.0, slopes=None):
-    """q [g, 128], K, V [n, 128] float64 values -> out [g, 128], lse [g], p [g, n], and the bound of what fp32 scores can be off.
+def attend(q, K, V, pos, nxt, K_size, sinks=0, window=0, cap=0.0, slopes=None):
+    """q [g, 128], K, V [n, 128] float64 values, K_size = terms() -> out [g, 128], lse [g], p [g, n], and the bound of what fp32 scores
+    can be off.
 
     A score is a sum of 128 products (exact in fp32: 8 bits by 8, or 8 by 4 and a scale): in any order it is off by at most
     130 x 2^-24 times the sum of their sizes; the cap, the bias and their rounding add a few units in the last place of the
@@ -58,7 +71,7 @@ def attend(q, K, V, pos, nxt, sinks=0, window=0, cap=0.0, slopes=None):
     if not seen.any():
         return out, lse, p, np.zeros(g)
     x = q @ K[seen].T / math.sqrt(D)
-    size = (np.abs(q) @ np.abs(K[seen]).T / math.sqrt(D)).max(axis=1)
+    size = (np.abs(q) @ K_size[seen].T / math.sqrt(D)).max(axis=1)
     most = np.abs(x).max(axis=1)
     if cap:
         x = cap * np.tanh(x / cap)
@@ -86,15 +99,20 @@ class Item:
 
     def __init__(self, capacity, bits, sinks, recent):
         self.capacity, self.bits, self.sinks, self.recent = capacity, bits, sinks, recent
-        self.K, self.V = np.zeros((capacity, D)), np.zeros((capacity, D))
+        self.K, self.V, self.K_size, self.V_size = (np.zeros((capacity, D)) for _ in range(4))
         self.pos, self.weight = np.zeros(capacity, np.int64), np.zeros(capacity)
         self.n = self.next = 0
+
+    def put(self, at, k, v):
+        """float32 rows into slots `at`."""
+        self.K[at], self.V[at] = held(k, self.bits), held(v, self.bits)
+        self.K_size[at], self.V_size[at] = terms(k, self.bits), terms(v, self.bits)
 
     def fill(self, K, V, w):
         T = K.shape[0]
         at = choose(T, self.capacity, self.sinks, self.recent, w)
         self.n, self.next = len(at), T
-        self.K[:self.n], self.V[:self.n] = held(K[at], self.bits), held(V[at], self.bits)
+        self.put(slice(0, self.n), K[at], V[at])
         self.pos[:self.n] = at
         self.weight[:self.n] = 0.0 if w is None else w[at]
 
@@ -105,13 +123,13 @@ class Item:
             self.n += 1
         elif slot is None:
             slot = evict(self.pos, self.weight if tracked else None, self.next, self.sinks, self.recent)
-        self.K[slot], self.V[slot] = held(k[None], self.bits)[0], held(v[None], self.bits)[0]
+        self.put(slice(slot, slot + 1), k[None], v[None])
         self.pos[slot], self.weight[slot] = self.next, 0.0
         self.next += 1
         return slot
 
     def decode(self, q, decay=1.0, **kw):
         n = self.n
-        out, lse, p, off = attend(q, self.K[:n], self.V[:n], self.pos[:n], self.next, sinks=self.sinks, **kw)
+        out, lse, p, off = attend(q, self.K[:n], self.V[:n], self.pos[:n], self.next, self.K_size[:n], sinks=self.sinks, **kw)
         self.weight[:n] = decay * self.weight[:n] + p.sum(axis=0)
         return out, lse, p, off

@@ -57,7 +57,7 @@ def loaded(rng, lens, hq, hkv, capacity, bits, garbage=True, gap=3, **kw):
         it.next = int(at[-1]) + 1 if n else 0
         it.pos[:n] = at = rng.permutation(at)
         it.weight[:n] = rng.exponential(2.0, n).astype(np.float32)
-        it.K[:n], it.V[:n] = P.held(kr, bits), P.held(vr, bits)
+        it.put(slice(0, n), kr, vr)
         pos[i, :n], weight[i, :n] = at, it.weight[:n]
         if n == 0:
             continue
@@ -90,8 +90,7 @@ def check_step(s, items, q, out, lse, weight, before, **kw):
         n = it.n
         o, l, p, off = it.decode(qs[sl, h0:h0 + g], slopes=None if slopes is None else slopes[h0:h0 + g], **kw)
         rel = (2 * off + P.sums_off(n) + 2.0 ** -20)[:, None]           # of a probability (exponentials and the quotient: 2^-21)
-        V = np.abs(it.V[:n])
-        assert np.all(np.abs(out[sl, h0:h0 + g] - o) <= rel * (p @ V) + 1e-30), (i, np.abs(out[sl, h0:h0 + g] - o).max())
+        assert np.all(np.abs(out[sl, h0:h0 + g] - o) <= rel * (p @ it.V_size[:n]) + 1e-30), (i, np.abs(out[sl, h0:h0 + g] - o).max())
         seen = np.isfinite(l)
         assert np.array_equal(np.isneginf(lse[sl, h0:h0 + g]), ~seen)
         assert np.all(np.abs(lse[sl, h0:h0 + g][seen] - l[seen]) <= off[seen] + P.sums_off(n) + 2.0 ** -22 * (1 + np.abs(l[seen])))
@@ -202,7 +201,7 @@ def test_magnitudes(bits, scale_q, scale_k, scale_v):
     for i, it in enumerate(items):
         n, sl, h = it.n, i // 2, i % 2
         kr, vr = P.bf16(rows_of(rng, n, True) * scale_k), P.bf16(rows_of(rng, n) * scale_v)
-        it.K[:n], it.V[:n] = P.held(kr, bits), P.held(vr, bits)
+        it.put(slice(0, n), kr, vr)
         for t, rows, side in ((s.k, kr, "k"), (s.v, vr, "v")):
             if bits == 16:
                 t[sl, h, :n] = cuda(rows, BF)
