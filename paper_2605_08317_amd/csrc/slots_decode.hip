@@ -24,6 +24,7 @@ namespace {
 using namespace tile;
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kRoot = 0.08838834764831845f;      // 1 / sqrt(128)
 constexpr float kLowest = -3.0e38f;          // a finite maximum of nothing
 
 struct DecodeArgs {
@@ -31,10 +32,11 @@ struct DecodeArgs {
   const uint16_t* q;
   float* out;
   float* lse;
-  float* scores;       // [items][g][score_rows], times log2(e); null: no weights are kept
+  float* scores;       // [items][score_rows][g], times log2(e); null: no weights are kept
   float* part_acc;     // [slot][g][128]: partials; slot = workgroup + item
   float* part_ml;      // [slot][g][2]
-  int32_t items, score_rows, least;     // least: tiles of a workgroup's share
+  int2* parts;         // [items]: an item's first partial and their number, 0 where it has none
+  int32_t items, score_rows, least;     // least: tiles of a workgroup's share; 0: a workgroup takes an item
 };
 
 // How the tiles of all items are shared out among the workgroups: workgroup w has those from w * share on.
@@ -53,14 +55,6 @@ __device__ __forceinline__ Line make_line(const DecodeArgs& a, int n_groups) {
   l.total = __builtin_amdgcn_readfirstlane(sum);
   l.share = max(a.least, (l.total + n_groups - 1) / n_groups);
   return l;
-}
-// Tiles before `item`.
-__device__ __forceinline__ int tiles_before(const DecodeArgs& a, int item) {
-  const int lane = threadIdx.x & 63;
-  int sum = 0;
-  for (int i = lane; i < item; i += 64) sum += tiles_of(a.s, i);
-  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-  return __builtin_amdgcn_readfirstlane(sum);
 }
 // The item that holds tile `at` of the line (at < total), and its first tile.
 __device__ __forceinline__ int item_at(const DecodeArgs& a, int at, int* first) {
@@ -96,14 +90,22 @@ struct Scoring {
   float cap, inv_cap;
   bool where;                    // positions matter
   const int32_t* pos;            // of the item
-  const float* slopes;           // of the item's heads, or null
-  float* scores;                 // of the item's heads, or null
-  int score_rows;
+  bool biased;
+  float slope[8];                // of the item's heads, where biased
+  bool tracked;
+  float* scores;                 // of the item: [slot][g]
 };
 
-// xt: products q k times 1 / unit[head]; comes back as scores times log2(e), -inf where the slot is not seen.  The slots that are.
+// the position of this lane's slot of a tile; 0 where there is none or positions do not matter
+__device__ __forceinline__ int position(const Scoring& sc, int tile, int t1) {
+  const int rows = sc.where && tile < t1 ? min(sc.n - tile * kTile, kTile) : 0;
+  const auto of = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(sc.pos + static_cast<int64_t>(tile) * kTile), 0, rows * 4, 0x00027000);
+  return static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(of, 4 * (threadIdx.x & 63), 0, 0));
+}
+
+// xt: products q k over unit; comes back as scores times log2(e), -inf where the slot is not seen.  The slots that are.
 template <int HS>
-__device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int pos, const float (&unit)[HS][4], float (&xt)[HS][4]) {
+__device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int pos, float unit, float (&xt)[HS][4]) {
   const int lane = threadIdx.x & 63, row = tile * kTile + lane;
   bool seen = row < sc.n;
   const int away = sc.at - pos;
@@ -111,14 +113,36 @@ __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int 
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int head = 4 * hs + i;
-      float s = xt[hs][i] * unit[hs][i];
-      if (sc.cap > 0.f) s = capped(s, sc.cap, sc.inv_cap);
-      if (sc.slopes != nullptr && head < sc.g) s = __builtin_fmaf(-sc.slopes[head], static_cast<float>(away), s);
-      xt[hs][i] = seen ? s * kLog2e : -INFINITY;
-      if (sc.scores != nullptr && head < sc.g) sc.scores[static_cast<int64_t>(head) * sc.score_rows + row] = xt[hs][i];
-    }
+    for (int i = 0; i < 4; ++i) xt[hs][i] *= unit;
+  if (sc.cap > 0.f) {
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xt[hs][i] = capped(xt[hs][i], sc.cap, sc.inv_cap);
+  }
+  if (sc.biased) {
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xt[hs][i] = __builtin_fmaf(-sc.slope[4 * hs + i], static_cast<float>(away), xt[hs][i]);
+  }
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) xt[hs][i] = seen ? xt[hs][i] * kLog2e : -INFINITY;
+  // (no weights: an empty buffer)
+  const auto dst = __builtin_amdgcn_make_buffer_rsrc(sc.scores + static_cast<int64_t>(tile) * kTile * sc.g, 0, sc.tracked ? kTile * 4 * sc.g : 0, 0x00027000);
+  const auto u = [&](int hs, int i) __attribute__((always_inline)) { return __float_as_uint(xt[hs][i]); };
+  using Four = __attribute__((ext_vector_type(4))) uint32_t;
+  using Two = __attribute__((ext_vector_type(2))) uint32_t;
+  if constexpr (HS == 2) {
+    __builtin_amdgcn_raw_buffer_store_b128((Four{u(0, 0), u(0, 1), u(0, 2), u(0, 3)}), dst, 32 * lane, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128((Four{u(1, 0), u(1, 1), u(1, 2), u(1, 3)}), dst, 32 * lane + 16, 0, 0);
+  } else {
+    if (sc.g == 4) __builtin_amdgcn_raw_buffer_store_b128((Four{u(0, 0), u(0, 1), u(0, 2), u(0, 3)}), dst, 16 * lane, 0, 0);
+    else if (sc.g == 2) __builtin_amdgcn_raw_buffer_store_b64((Two{u(0, 0), u(0, 1)}), dst, 8 * lane, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(u(0, 0), dst, 4 * lane, 0, 0);
+  }
   return __builtin_amdgcn_ballot_w64(seen);
 }
 
@@ -157,6 +181,15 @@ __device__ __forceinline__ void init(Run<HS>& run) {
   run.init();
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) run.m[hs] = kLowest;
+}
+
+// Sixteen bytes of a tile.  STREAM: non-temporal, so that rows, which a step reads once, do not push scores out of the caches: 4 x 8 items of
+// 128K slots in bf16 432 -> 388 us, without weights 357 -> 313 (6.8 TB/s).  Small caches may still be there from the step before: 32 of 2
+// items of 1000 slots 16.0 us each with it, 13.3 without.
+template <bool STREAM, class Buffer>
+__device__ __forceinline__ uint4 stream_load(Buffer tile, int at) {
+  const auto v = __builtin_amdgcn_raw_buffer_load_b128(tile, at, 0, STREAM ? 2 : 0);
+  return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // ---- bf16 rows ---------------------------------------------------------------------------------------------------------------------
@@ -202,38 +235,40 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
                                              const Scoring& sc, int t0, int t1, uint8_t* s_stage, Run<HS>& run) {
   const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int last = sc.n - 1;
   const int lr = lane >> 4, lc = lane & 15;
-  uint4 st[16];
-  auto load_tile = [&](const uint8_t* __restrict__ base, int t) __attribute__((always_inline)) {
+  // K and V of a tile in registers of their own, each loaded again right after it went to LDS: two tiles' sides are always on their way.
+  // A tile is a buffer that ends with the item's last row, and what is behind it reads as zeros; behind the last tile it is empty.  (With
+  // loads under a condition the compiler cannot count on them, and waits for all there are.)
+  uint4 kq[16], vq[16];
+  auto load_tile = [&](uint4 (&st)[16], const uint8_t* __restrict__ base, int t) __attribute__((always_inline)) {
+    const int rows = t < t1 ? min(sc.n - t * kTile, kTile) : 0;
+    const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + static_cast<int64_t>(t) * (kTile * kHeadDim * 2)), 0,
+                                                        rows * (kHeadDim * 2), 0x00027000);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) st[i] = load_row_chunk(base, min(t * kTile + 4 * i + lr, last), lc);
+    for (int i = 0; i < 16; ++i) st[i] = stream_load<NWV == 4>(tile, lane * 16 + i * 1024);
   };
-  auto store_tile = [&]() __attribute__((always_inline)) {
+  auto store_tile = [&](const uint4 (&st)[16]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(s_stage + (4 * i + lr) * kRowStride + 16 * lc) = st[i];
   };
-  auto load_pos = [&](int t) __attribute__((always_inline)) { return sc.where ? sc.pos[min(t * kTile + lane, last)] : 0; };
+  auto load_pos = [&](int t) __attribute__((always_inline)) { return position(sc, t, t1); };
   uint4 qa[HS];
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) qa[hs] = load_query(q, 4 * hs + j, sc.g, blk);
-  int pos = 0;
-  if (t0 + wave < t1) {
-    pos = load_pos(t0 + wave);
-    load_tile(kd, t0 + wave);
-  }
-  float unit[HS][4];
+  int pos = load_pos(t0 + wave);
+  load_tile(kq, kd, t0 + wave);
+  load_tile(vq, vd, t0 + wave);
+  __builtin_amdgcn_sched_barrier(0);
+  // the query is here before the loop: waited for inside, it would have every pass wait for all loads under way
 #pragma unroll
-  for (int hs = 0; hs < HS; ++hs)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) unit[hs][i] = 0.08838834764831845f;      // 1 / sqrt(128)
+  for (int hs = 0; hs < HS; ++hs) asm volatile("" : "+v"(qa[hs].x), "+v"(qa[hs].y), "+v"(qa[hs].z), "+v"(qa[hs].w));
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
     const int next = tile + NWV;
-    store_tile();                       // K rows of this tile
-    load_tile(vd, tile);                // V rows: in flight during the scores
+    store_tile(kq);
     const int pos_now = pos;
-    if (next < t1) pos = load_pos(next);
+    pos = load_pos(next);
+    load_tile(kq, kd, next);
     wave_lds_sync();
     floatx4 a16[HS];
 #pragma unroll
@@ -255,7 +290,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
     for (int hs = 0; hs < HS; ++hs)
 #pragma unroll
       for (int i = 0; i < 4; ++i) xt[hs][i] = a16[hs][i];
-    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
+    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, kRoot, xt);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
     softmax_step<HS>(x, run, p, 0.f);
@@ -265,11 +300,11 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
     if (seen != ~0ull) {                // rows that are not seen may hold anything: 0 x NaN
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (!((seen >> (4 * i + lr)) & 1)) st[i] = make_uint4(0, 0, 0, 0);
+        if (!((seen >> (4 * i + lr)) & 1)) vq[i] = make_uint4(0, 0, 0, 0);
     }
     wave_lds_sync();                    // every lane is done with the K rows
-    store_tile();                       // V rows
-    if (next < t1) load_tile(kd, next);
+    store_tile(vq);
+    load_tile(vq, vd, next);
     wave_lds_sync();
     pv_rows<HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 16>{});
     wave_lds_sync();                    // before the next tile's K rows overwrite the region
@@ -297,6 +332,14 @@ __device__ __forceinline__ half4 code_operand(const uint4& gw, int s) {
 }
 constexpr float kCode = 262144.0f;       // 2^18
 
+// two numbers as fp16 pairs whose sums they are, to 22 bits, rounded to nearest (cut off they were low by 2^-21 on average, which the
+// codes' sum and the offsets' do not share)
+typedef float float2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void split_halves(float a, float b, half2v& hi, half2v& lo) {
+  hi = __builtin_convertvector((float2v{a, b}), half2v);
+  lo = __builtin_convertvector((float2v{a - static_cast<float>(hi[0]), b - static_cast<float>(hi[1])}), half2v);
+}
+
 constexpr int kQUp = 8;                  // the query's largest value is near 2^kQUp
 constexpr float kPUp = 15.0f;            // probabilities are carried times 2^kPUp
 
@@ -312,41 +355,49 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   uint4 qraw[HS];
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) qraw[hs] = load_query(q, 4 * hs + j, sc.g, blk);
-  uint4 kr[4], vr[4], kmeta = make_uint4(0, 0, 0, 0), vmeta = kmeta;
-  int pos = 0;
-  auto load_k = [&](int t) __attribute__((always_inline)) {
-    const uint8_t* p = kd + static_cast<int64_t>(t) * kTileBytes + lane * 16;
+  uint4 kr[4], vr[4], kmeta, vmeta;
+  int pos;
+  auto load_k = [&](int t) __attribute__((always_inline)) {      // (as in rows_segment: no bytes behind the last tile)
+    const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(kd + static_cast<int64_t>(t) * kTileBytes), 0, t < t1 ? kTileBytes : 0, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) kr[i] = *reinterpret_cast<const uint4*>(p + 1024 * i);
-    kmeta = *reinterpret_cast<const uint4*>(p + 4096);
-    if (sc.where) pos = sc.pos[min(t * kTile + lane, sc.n - 1)];
+    for (int i = 0; i < 4; ++i) kr[i] = stream_load<NWV == 4>(tile, lane * 16 + 1024 * i);
+    kmeta = stream_load<NWV == 4>(tile, lane * 16 + 4096);
+    pos = position(sc, t, t1);
   };
   auto load_v = [&](int t) __attribute__((always_inline)) {
-    const uint8_t* p = vd + static_cast<int64_t>(t) * kTileBytes + lane * 16;
-    vmeta = *reinterpret_cast<const uint4*>(p + 4096);
+    const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(vd + static_cast<int64_t>(t) * kTileBytes), 0, t < t1 ? kTileBytes : 0, 0x00027000);
+    vmeta = stream_load<NWV == 4>(tile, lane * 16 + 4096);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vr[i] = *reinterpret_cast<const uint4*>(p + 1024 * i);
+    for (int i = 0; i < 4; ++i) vr[i] = stream_load<NWV == 4>(tile, lane * 16 + 1024 * i);
   };
-  if (t0 + wave < t1) {
-    load_k(t0 + wave);
-    load_v(t0 + wave);
-  }
+  load_k(t0 + wave);
+  load_v(t0 + wave);
 
-  // ---- query operands: every head times its own power of two, so that its largest value is near 2^kQUp ---------------
+  // ---- query operands: times the power of two that puts the largest value of all heads near 2^kQUp ------------------
   half4 qop[HS][2], qhi[HS], qlo[HS];
-  float unit[HS][4];
+  float most = 0.f;
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
     const uint32_t w[4] = {qraw[hs].x, qraw[hs].y, qraw[hs].z, qraw[hs].w};
-    float v[8], most = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t u = (e == 0 ? w[k] << 16 : w[k] & 0xFFFF0000u) & 0x7FFFFFFFu;
+        most = fmaxf(most, u < 0x7F800000u ? __uint_as_float(u) : 0.f);      // (a head that is not finite stays by itself)
+      }
+  }
+  const int up = __builtin_amdgcn_readfirstlane(max(-120, min(120, kQUp - exponent_of(wave_max(most)))));
+  const float unit = ldexpf(kRoot, -up);
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) {
+    const uint32_t w[4] = {qraw[hs].x, qraw[hs].y, qraw[hs].z, qraw[hs].w};
+    float v[8];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       v[2 * k] = __uint_as_float(w[k] << 16);
       v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-      most = fmaxf(most, fmaxf(fabsf(v[2 * k]), fabsf(v[2 * k + 1])));
     }
-    most = head_max(most);
-    const int up = max(-120, min(120, kQUp - exponent_of(most)));      // (zeros, NaN and infinities stay what they are)
     float psum = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -370,11 +421,6 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
       qhi[hs][k] = static_cast<_Float16>(sg[k]);
       qlo[hs][k] = static_cast<_Float16>(sg[k] - static_cast<float>(qhi[hs][k]));
     }
-    const uint32_t u = __float_as_uint(ldexpf(0.08838834764831845f, -up));
-    unit[hs][0] = __uint_as_float(quad_bcast<0>(u));
-    unit[hs][1] = __uint_as_float(quad_bcast<1>(u));
-    unit[hs][2] = __uint_as_float(quad_bcast<2>(u));
-    unit[hs][3] = __uint_as_float(quad_bcast<3>(u));
   }
   int ve = -126;                         // exponent of the largest V scale so far
   float vf = 0.f;                        // what p is multiplied by for it
@@ -382,7 +428,6 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
     const int next = tile + NWV;
-    const bool more = next < t1;
     float xt[HS][4], x[HS][4];
     const int pos_now = pos;
     {
@@ -418,7 +463,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 #undef RDKV_K_GROUP
 #undef RDKV_K_STEP
     }
-    if (more) load_k(next);
+    load_k(next);
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
@@ -457,9 +502,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
       Pack4 hi, lo;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const auto h = __builtin_amdgcn_cvt_pkrtz(p[hs][2 * i], p[hs][2 * i + 1]);
-        hi.p[i] = __builtin_bit_cast(half2v, h);
-        lo.p[i] = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(p[hs][2 * i] - static_cast<float>(hi.p[i][0]), p[hs][2 * i + 1] - static_cast<float>(hi.p[i][1])));
+        split_halves(p[hs][2 * i], p[hs][2 * i + 1], hi.p[i], lo.p[i]);
       }
       run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi.h, ob.h, run.offv[hs], 0, 0, 0);
       run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo.h, ob.h, run.offv[hs], 0, 0, 0);
@@ -481,9 +524,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     sv.u[0] = quad_bcast<G_>(vm.x); sv.u[1] = quad_bcast<G_>(vm.y);                                            \
     _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) {                                                        \
       _Pragma("unroll") for (int i = 0; i < 2; ++i) {                                                          \
-        const float p0 = p[hs][2 * i] * static_cast<float>(sv.p[i][0]), p1 = p[hs][2 * i + 1] * static_cast<float>(sv.p[i][1]); \
-        hi[hs].p[i] = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(p0, p1));                          \
-        lo[hs].p[i] = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(p0 - static_cast<float>(hi[hs].p[i][0]), p1 - static_cast<float>(hi[hs].p[i][1]))); \
+        split_halves(p[hs][2 * i] * static_cast<float>(sv.p[i][0]), p[hs][2 * i + 1] * static_cast<float>(sv.p[i][1]), hi[hs].p[i], lo[hs].p[i]); \
       }                                                                                                        \
     }                                                                                                          \
     const uint4 gw = vr[G_];                                                                                   \
@@ -493,7 +534,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     RDKV_PV_GROUP(0) RDKV_PV_GROUP(1) RDKV_PV_GROUP(2) RDKV_PV_GROUP(3)
 #undef RDKV_PV_GROUP
 #undef RDKV_PV_STEP
-    if (more) load_v(next);
+    load_v(next);
   }
   // what brings the accumulators to the sums' scale: 2^18 of the codes, 2^(1 + ve) of vf
   return ldexpf(1.0f, 19 + ve);
@@ -506,38 +547,71 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 template <int NWV, int HS>
 constexpr int ml_floats() { return ml_lds_floats(NWV, HS); }
 
-// weights of slots r0 .. r1 - 1 of an item: lse2 of its heads, log2
-__device__ __forceinline__ void add_weights(const Args& a, int64_t item, const float* __restrict__ scores, int score_rows, int g, const float* lse2,
-                                            int r0, int r1, int thread, int threads) {
+// Weights of slots r0 .. r1 - 1 of an item; lse2 of its heads, log2.  A thread has kEach slots under way.
+template <int G>
+__device__ __forceinline__ void add_weights_g(const Args& a, int64_t item, const float* __restrict__ scores, const float* lse2, int r0, int r1,
+                                              int thread, int threads) {
+  constexpr int kEach = G == 8 ? 2 : 4, kWide = G < 4 ? G : 4;
+  using Wide = __attribute__((ext_vector_type(kWide))) float;
   float* __restrict__ weight = a.weight + item * a.capacity;
-  for (int i = r0 + thread; i < r1; i += threads) {
-    float p = 0.f;
-    for (int h = 0; h < g; ++h) p += fast_exp2(scores[static_cast<int64_t>(h) * score_rows + i] - lse2[h]);
-    weight[i] = __builtin_fmaf(a.decay, weight[i], p);
+  float l[G];
+#pragma unroll
+  for (int h = 0; h < G; ++h) l[h] = lse2[h];
+  for (int i0 = r0 + thread; i0 < r1; i0 += kEach * threads) {
+    Wide x[kEach][G / kWide];
+    float w[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int i = min(i0 + k * threads, r1 - 1);
+#pragma unroll
+      for (int h = 0; h < G / kWide; ++h) x[k][h] = *reinterpret_cast<const Wide*>(scores + static_cast<int64_t>(i) * G + h * kWide);
+      w[k] = weight[i];
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      float p = 0.f;
+#pragma unroll
+      for (int h = 0; h < G; ++h) p += fast_exp2(x[k][h / kWide][h % kWide] - l[h]);
+      if (i0 + k * threads < r1) weight[i0 + k * threads] = __builtin_fmaf(a.decay, w[k], p);
+    }
   }
+}
+__device__ __forceinline__ void add_weights(const Args& a, int64_t item, const float* scores, int g, const float* lse2, int r0, int r1, int thread,
+                                            int threads) {
+  if (g == 8) add_weights_g<8>(a, item, scores, lse2, r0, r1, thread, threads);
+  else if (g == 4) add_weights_g<4>(a, item, scores, lse2, r0, r1, thread, threads);
+  else if (g == 2) add_weights_g<2>(a, item, scores, lse2, r0, r1, thread, threads);
+  else add_weights_g<1>(a, item, scores, lse2, r0, r1, thread, threads);
 }
 
 // log2 of the sum of 2^score over everything: sum l, relative to 2^m; +inf where nothing was seen, which makes every weight 0
 __device__ __forceinline__ float total_log2(float m, float l) { return l == 0.f ? INFINITY : m + __log2f(l); }
 
 template <int BITS, int HS, int NWV>
-__global__ __launch_bounds__(NWV * 64, BITS == 16 ? 2 : HS == 1 ? 4 : 3) void decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decode_kernel(DecodeArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = a.s.g;
-  const Line line = make_line(a, gridDim.x);
-  int at = static_cast<int>(blockIdx.x) * line.share;
   // items without a token have no tile: their outputs are the first workgroups' to write
   for (int item = blockIdx.x; item < a.items; item += gridDim.x)
     if (a.s.length(item) == 0) {
       for (int i = tid; i < g * kHeadDim; i += NWV * 64) a.out[static_cast<int64_t>(item) * g * kHeadDim + i] = 0.f;
       if (a.lse != nullptr && tid < g) a.lse[static_cast<int64_t>(item) * g + tid] = -INFINITY;
+      if (tid == 0 && a.least > 0) a.parts[item] = make_int2(0, 0);
     }
-  if (at >= line.total) return;
-  const int end = min(at + line.share, line.total);
-  int first;
-  int item = item_at(a, at, &first);
+  // where on the line this workgroup is (or at its item)
+  int at = 0, end, first = 0, item = blockIdx.x, share = 0;
+  if (a.least > 0) {
+    const Line line = make_line(a, gridDim.x);
+    share = line.share;
+    at = static_cast<int>(blockIdx.x) * share;
+    if (at >= line.total) return;
+    end = min(at + share, line.total);
+    item = item_at(a, at, &first);
+  } else {
+    end = tiles_of(a.s, item);
+  }
   float* s_ml = reinterpret_cast<float*>(smem + (BITS == 16 ? NWV * kStageBytes : 0));
   float* s_acc = BITS == 16 ? reinterpret_cast<float*>(smem) : s_ml + ml_floats<NWV, HS>();
   float* s_lse = BITS == 16 ? s_ml + ml_floats<NWV, HS>() : s_acc + NWV * g * kHeadDim;
@@ -549,6 +623,8 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 ? 2 : HS == 1 ? 4 : 3) void de
       continue;
     }
     const bool whole = t0 == 0 && t1 == tiles;
+    if (t0 == 0 && tid == 0 && a.least > 0)
+      a.parts[item] = whole ? make_int2(0, 0) : make_int2(static_cast<int>(blockIdx.x) + item, (first + tiles - 1) / share - static_cast<int>(blockIdx.x) + 1);
     Scoring sc;
     sc.n = n;
     sc.at = a.s.next[item] - 1;
@@ -559,9 +635,15 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 ? 2 : HS == 1 ? 4 : 3) void de
     sc.inv_cap = a.s.cap > 0.f ? 1.0f / a.s.cap : 0.f;
     sc.where = a.s.window > 0 || a.s.slopes != nullptr;
     sc.pos = a.s.pos + static_cast<int64_t>(item) * a.s.capacity;
-    sc.slopes = a.s.slopes ? a.s.slopes + (item % a.s.hkv) * g : nullptr;
-    sc.scores = a.scores ? a.scores + static_cast<int64_t>(item) * g * a.score_rows : nullptr;
-    sc.score_rows = a.score_rows;
+    sc.biased = a.s.slopes != nullptr;
+    if (sc.biased) {                     // (constant address space: scalar loads, which no wait for rows waits for)
+      typedef const __attribute__((address_space(4))) float* ConstFloats;
+      const ConstFloats slopes = (ConstFloats)(a.s.slopes) + (item % a.s.hkv) * g;
+#pragma unroll
+      for (int h = 0; h < 4 * HS; ++h) sc.slope[h] = slopes[min(h, g - 1)];
+    }
+    sc.tracked = a.s.weight != nullptr;
+    sc.scores = a.scores + static_cast<int64_t>(item) * g * a.score_rows;
     const uint16_t* q = a.q + static_cast<int64_t>(item) * g * kHeadDim;
     Run<HS> run;
     init(run);
@@ -642,8 +724,8 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 ? 2 : HS == 1 ? 4 : 3) void de
       }
     }
     __syncthreads();
-    if (whole && a.scores != nullptr) {
-      add_weights(a.s, item, sc.scores, sc.score_rows, g, s_lse, 0, n, tid, NWV * 64);
+    if (whole && a.s.weight != nullptr) {
+      add_weights(a.s, item, sc.scores, g, s_lse, 0, n, tid, NWV * 64);
       __syncthreads();
     }
     at = first + t1;
@@ -654,21 +736,22 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 ? 2 : HS == 1 ? 4 : 3) void de
   }
 }
 
-// The items whose tiles several workgroups shared: their partials into the outputs, and their weights.  n_groups: workgroups of
-// the launch before.  `rows` workgroups an item.
+__device__ __forceinline__ float wave_sum(float v) {
+  float o = v = sum_xor16(row_sum(v));
+  swap_halves(v, o);
+  return v + o;
+}
+
+// The items whose tiles several workgroups shared: their partials into the outputs, and their weights.  `rows` workgroups an item.
 constexpr int kJoinThreads = 256;
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int n_groups, int rows) {
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int rows) {
   __shared__ float s_lse[8], s_top[8], s_half[kHeadDim];
   const int item = blockIdx.x / rows, row = blockIdx.x % rows, tid = threadIdx.x, lane = tid & 63, g = a.s.g;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Line line = make_line(a, n_groups);
-  const int n = a.s.length(item), tiles = (n + kTile - 1) / kTile;
-  if (tiles == 0) return;
-  const int before = tiles_before(a, item);
-  const int w0 = before / line.share, w1 = (before + tiles - 1) / line.share;
-  if (w0 == w1) return;
-  const int64_t slot0 = static_cast<int64_t>(w0) + item, qh0 = static_cast<int64_t>(item) * g;
-  const int parts = w1 - w0 + 1;
+  const int2 of = a.parts[item];
+  const int n = a.s.length(item), tiles = (n + kTile - 1) / kTile, parts = of.y;
+  if (parts == 0) return;
+  const int64_t slot0 = of.x, qh0 = static_cast<int64_t>(item) * g;
   for (int head = wave; head < g; head += kJoinThreads / 64) {
     float m = kLowest, l = 0.f;
     for (int k = lane; k < parts; k += 64) {
@@ -677,10 +760,13 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int n_
       l = l * fast_exp2(m - mm) + ml.y * fast_exp2(ml.x - mm);
       m = mm;
     }
-    float top = m;
-    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-    l *= fast_exp2(m - top);
-    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+    const float mm = row_max(m);
+    float o = mm, top = mm;
+    swap_rows(top, o);
+    top = o = fmaxf(top, o);
+    swap_halves(top, o);
+    top = fmaxf(top, o);
+    l = wave_sum(l * fast_exp2(m - top));
     if (lane == 0) {
       s_top[head] = top;
       s_lse[head] = total_log2(top, l);
@@ -691,44 +777,52 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int n_
   for (int head = row; head < g; head += rows) {
     const int c = tid & (kHeadDim - 1), half = tid >> 7;
     const float top = s_top[head];
-    float v = 0.f, l = 0.f;
+    float v = 0.f;
     for (int k = half; k < parts; k += 2) {
       const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * g + head) * 2);
-      const float f = fast_exp2(ml.x - top);
-      v = __builtin_fmaf(a.part_acc[((slot0 + k) * g + head) * kHeadDim + c], f, v);
+      v = __builtin_fmaf(a.part_acc[((slot0 + k) * g + head) * kHeadDim + c], fast_exp2(ml.x - top), v);
     }
     if (half == 1) s_half[c] = v;
     __syncthreads();
     if (half == 0) {
       v += s_half[c];
-      l = s_lse[head];
+      const float l = s_lse[head];
       a.out[(qh0 + head) * kHeadDim + c] = l == INFINITY ? 0.f : v * fast_exp2(top - l);
       if (c == 0 && a.lse != nullptr) a.lse[qh0 + head] = l == INFINITY ? -INFINITY : l * 0.6931471805599453f;
     }
     __syncthreads();
   }
-  if (a.scores == nullptr) return;
+  if (a.s.weight == nullptr) return;
   const int each = (tiles + rows - 1) / rows * kTile, r0 = row * each;
-  add_weights(a.s, item, a.scores + qh0 * a.score_rows, a.score_rows, g, s_lse, r0, min(n, r0 + each), tid, kJoinThreads);
+  add_weights(a.s, item, a.scores + qh0 * a.score_rows, g, s_lse, r0, min(n, r0 + each), tid, kJoinThreads);
 }
 
 struct Plan {
-  int groups, least, score_rows;
-  size_t scores, part_acc, part_ml;      // floats
+  int waves, groups, least, score_rows, join_rows;
+  size_t scores, part_acc, part_ml, parts;      // floats
 };
 Plan make_plan(int64_t items, int g, int capacity, int bits) {
   Plan p;
   const int64_t tiles = (capacity + kTile - 1) / kTile;
-  const int waves = bits == 4 && g <= 4 ? 8 : 4;
-  p.least = waves;
   p.score_rows = static_cast<int>(tiles) * kTile;
-  const int64_t most = (items * tiles + waves - 1) / waves;
-  const int64_t resident = bits == 4 && g > 4 ? 768 : 512;
-  p.groups = static_cast<int>(most < resident ? most : resident);
   p.scores = static_cast<size_t>(items) * g * p.score_rows;
+  p.waves = 8;
+  if (tiles <= 3 * p.waves) {
+    p.least = p.join_rows = 0;
+    p.groups = static_cast<int>(items);
+    p.part_acc = p.part_ml = p.parts = 0;
+    return p;
+  }
+  p.waves = 4;
+  p.least = p.waves;
+  const int64_t most = (items * tiles + p.waves - 1) / p.waves;
+  const int64_t resident = 512;
+  p.groups = static_cast<int>(std::min(most, resident));
+  p.join_rows = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((p.score_rows + 1023) / 1024, 16384 / items)));
   const size_t slots = static_cast<size_t>(p.groups) + items;
   p.part_acc = slots * g * kHeadDim;
   p.part_ml = slots * g * 2;
+  p.parts = 2 * static_cast<size_t>(items);
   return p;
 }
 
@@ -747,7 +841,7 @@ hipError_t launch(const DecodeArgs& a, const Plan& p, hipStream_t st) {
 
 size_t decode_workspace_floats(int64_t items, int g, int capacity, int bits, bool weights) {
   const Plan p = make_plan(items, g, capacity, bits);
-  return (weights ? p.scores : 0) + p.part_acc + p.part_ml;
+  return std::max<size_t>((weights ? p.scores : 0) + p.part_acc + p.part_ml + p.parts, 4);
 }
 
 hipError_t launch_decode(const Args& s, int bits, int items, const uint16_t* q, float* out, float* lse, float* workspace, hipStream_t st) {
@@ -757,18 +851,24 @@ hipError_t launch_decode(const Args& s, int bits, int items, const uint16_t* q, 
   a.q = q;
   a.out = out;
   a.lse = lse;
-  a.part_acc = workspace;                // (two floats at a time)
-  a.part_ml = workspace + p.part_acc;
-  a.scores = s.weight ? a.part_ml + p.part_ml : nullptr;
+  a.scores = workspace;                  // (of a cache without weights: nothing)
+  if (s.weight) workspace += p.scores;
+  a.part_acc = workspace;
+  a.part_ml = a.part_acc + p.part_acc;
+  a.parts = reinterpret_cast<int2*>(a.part_ml + p.part_ml);
   a.items = items;
   a.score_rows = p.score_rows;
   a.least = p.least;
   hipError_t e;
-  if (bits == 16) e = s.g > 4 ? launch<16, 2, 4>(a, p, st) : launch<16, 1, 4>(a, p, st);
-  else e = s.g > 4 ? launch<4, 2, 4>(a, p, st) : launch<4, 1, 8>(a, p, st);
-  if (e != hipSuccess || p.groups == 1) return e;
-  const int rows = std::max(1, std::min({64, (p.score_rows + 2047) / 2048, 8192 / items}));
-  hipLaunchKernelGGL(join_kernel, dim3(items * rows), dim3(kJoinThreads), 0, st, a, p.groups, rows);
+  if (bits == 16) {
+    if (p.waves == 8) e = s.g > 4 ? launch<16, 2, 8>(a, p, st) : launch<16, 1, 8>(a, p, st);
+    else e = s.g > 4 ? launch<16, 2, 4>(a, p, st) : launch<16, 1, 4>(a, p, st);
+  } else {
+    if (s.g <= 4) e = p.waves == 8 ? launch<4, 1, 8>(a, p, st) : launch<4, 1, 4>(a, p, st);
+    else e = p.waves == 8 ? launch<4, 2, 8>(a, p, st) : launch<4, 2, 4>(a, p, st);
+  }
+  if (e != hipSuccess || p.join_rows == 0) return e;
+  hipLaunchKernelGGL(join_kernel, dim3(items * p.join_rows), dim3(kJoinThreads), 0, st, a, p.join_rows);
   return hipGetLastError();
 }
 

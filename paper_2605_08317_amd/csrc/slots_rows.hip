@@ -7,30 +7,50 @@ namespace slots {
 
 namespace {
 
-constexpr int kSelectThreads = 1024;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 
-// sum over the workgroup's wavefronts below this one, and over all of them; v: this wavefront's
-template <int WAVES>
-__device__ __forceinline__ uint32_t waves_below(uint32_t v, uint32_t* s_waves, uint32_t* all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  __syncthreads();
-  if (lane == 0) s_waves[wave] = v;
-  __syncthreads();
-  uint32_t below = 0, sum = 0;
-  for (int w = 0; w < WAVES; ++w) {
-    if (w < wave) below += s_waves[w];
-    sum += s_waves[w];
+// Sums over the threads below this one (x0, x1: this thread's own), and over all of them.
+struct Scan {
+  uint32_t s_wave[2][kSelectWaves];
+  __device__ __forceinline__ void run(uint32_t x0, uint32_t x1, uint32_t& below0, uint32_t& below1, uint32_t& all0) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t up0 = wave_scan(x0), up1 = wave_scan(x1);
+    __syncthreads();
+    if (lane == 63) {
+      s_wave[0][wave] = up0;
+      s_wave[1][wave] = up1;
+    }
+    __syncthreads();
+    below0 = up0 - x0;
+    below1 = up1 - x1;
+    all0 = 0;
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w) {
+      const uint32_t a = s_wave[0][w], b = s_wave[1][w];
+      if (w < wave) {
+        below0 += a;
+        below1 += b;
+      }
+      all0 += a;
+    }
   }
-  *all = sum;
-  return below;
-}
+};
 
-// Which tokens of an item stay: their positions and weights into the slots.  The weight that the last of the kept ones has is found
-// digit by digit, from the highest (radix selection); a token stays if it is a sink, recent, above that weight, or one of the
-// first of those at it.
+// Which tokens of an item stay: their positions and weights into the slots.  Weights become unsigned numbers of the same order, with
+// sinks and recent tokens above all; the capacity's largest stay, found digit by digit from the highest (radix selection: 11, 11 and
+// 10 bits), the first of equal ones before the later.  One workgroup an item, its weights in the threads' registers.
+// A pass counts digits in LDS, with four counters a digit that lanes take in turn: weights share their few exponents, and lanes on one
+// counter wait for each other.  Bound: one compute unit's loads and atomics.
+// REGS: weights a thread holds; WHOLE: they are all of the item, otherwise every pass goes through it in blocks.
+constexpr int kCopies = 4, kDigits = 2048;
+template <int REGS, bool WHOLE>
 __global__ __launch_bounds__(kSelectThreads) void fill_select_kernel(FillArgs a) {
-  __shared__ uint32_t s_hist[256], s_waves[kSelectThreads / 64], s_digit[2];
-  const int head = blockIdx.x, sl = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  constexpr int kBlock = REGS * kSelectThreads, kEntries = REGS * kSelectWaves;
+  static_assert(kEntries <= kSelectThreads && 3 * kEntries <= kDigits * kCopies, "an entry a thread");
+  __shared__ uint32_t s_hist[kDigits * kCopies];          // later what stays of (register, wavefront), and sums before it
+  __shared__ Scan s_scan;
+  __shared__ uint32_t s_found[2];
+  const int head = blockIdx.x, sl = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int T = a.T[sl], cap = a.s.capacity;
   const int64_t item = static_cast<int64_t>(a.seq0 + sl) * a.s.hkv + head;
   const float* w = a.w_tok ? a.w_tok + a.row0[sl] + static_cast<int64_t>(head) * T : nullptr;
@@ -47,55 +67,97 @@ __global__ __launch_bounds__(kSelectThreads) void fill_select_kernel(FillArgs a)
     }
     return;
   }
-  const int lo = a.s.sinks, hi = T - a.s.recent;          // the tokens that may go
-  uint32_t left = cap - a.s.sinks - a.s.recent;           // of them, so many stay
-  uint32_t prefix = 0;
-  if (left > 0)
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kSelectThreads) s_hist[i] = 0;
-      __syncthreads();
-      for (int t = lo + tid; t < hi; t += kSelectThreads) {
-        const uint32_t key = weight_key(w[t]);
-        if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[(key >> shift) & 255u], 1u);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        uint32_t n = left;
-        int d = 255;
-        for (; d > 0 && s_hist[d] < n; --d) n -= s_hist[d];
-        s_digit[0] = d;
-        s_digit[1] = n;
-      }
-      __syncthreads();
-      prefix |= s_digit[0] << shift;
-      left = s_digit[1];
+  const int lo = a.s.sinks, hi = T - a.s.recent;
+  uint32_t keys[REGS];                                    // token t0 + i kSelectThreads + tid
+  const auto load = [&](int t0) __attribute__((always_inline)) {
+    float x[REGS];
+#pragma unroll
+    for (int i = 0; i < REGS; ++i) x[i] = w[min(t0 + i * kSelectThreads + tid, T - 1)];
+#pragma unroll
+    for (int i = 0; i < REGS; ++i) {
+      const int t = t0 + i * kSelectThreads + tid;
+      keys[i] = t < lo || t >= hi ? 0xFFFFFFFFu : weight_key(x[i]);
     }
-  // prefix: the weight at the border; left: how many at it stay
-  uint32_t above = 0, ties = 0;                           // so far: tokens that stay for more than a tie, tokens at the border
-  const bool none = cap == a.s.sinks + a.s.recent;
-  for (int t0 = 0; t0 < T; t0 += kSelectThreads) {
-    const int t = t0 + tid;
-    bool stay = false, tie = false;
-    if (t < T) {
-      stay = t < lo || t >= hi;
-      if (!stay && !none) {
-        const uint32_t key = weight_key(w[t]);
-        stay = key > prefix;
-        tie = key == prefix;
+  };
+  if constexpr (WHOLE) load(0);
+  uint32_t left = cap, border = 0;                        // how many stay of what is in question: keys that begin as border does
+  const auto pass = [&](int shift, int bits, int above) __attribute__((always_inline)) {
+    __syncthreads();
+    for (int i = tid; i < kDigits * kCopies; i += kSelectThreads) s_hist[i] = 0;
+    __syncthreads();
+    for (int t0 = 0; t0 < T; t0 += kBlock) {
+      if constexpr (!WHOLE) load(t0);
+#pragma unroll
+      for (int i = 0; i < REGS; ++i) {
+        if (t0 + i * kSelectThreads >= T) break;
+        if (t0 + i * kSelectThreads + tid < T && (above == 32 || (keys[i] >> above) == (border >> above)))
+          atomicAdd(&s_hist[((keys[i] >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
       }
     }
-    const uint64_t bs = __ballot(stay), bt = __ballot(tie), under = (1ull << lane) - 1;
-    uint32_t all;
-    const uint32_t mine = static_cast<uint32_t>(__popcll(bs)) | static_cast<uint32_t>(__popcll(bt)) << 16;
-    const uint32_t below = waves_below<kSelectThreads / 64>(mine, s_waves, &all);
-    const uint32_t my_ties = ties + (below >> 16) + __popcll(bt & under);
-    const uint32_t at = above + (below & 0xFFFFu) + __popcll(bs & under) + min(my_ties, left);
-    if (stay || (tie && my_ties < left)) {
-      pos[at] = t;
-      if (weight) weight[at] = w[t];
+    __syncthreads();
+    uint32_t n[2] = {0, 0};                               // of digits 2047 - 2 tid and the one below
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int c = 0; c < kCopies; ++c) n[e] += s_hist[(kDigits - 1 - 2 * tid - e) * kCopies + c];
+    uint32_t higher, unused0, unused1;
+    s_scan.run(n[0] + n[1], 0, higher, unused0, unused1);
+    if (higher < left && left <= higher + n[0] + n[1]) {
+      const int e = left > higher + n[0];
+      s_found[0] = kDigits - 1 - 2 * tid - e;
+      s_found[1] = left - higher - (e ? n[0] : 0);
     }
-    above += all & 0xFFFFu;
-    ties += all >> 16;
+    __syncthreads();
+    border |= s_found[0] << shift;
+    left = s_found[1];
+  };
+  pass(21, 11, 32);
+  pass(10, 11, 21);
+  pass(0, 10, 10);
+  // Their slots.  For every (register, wavefront), in the order of tokens: how many are above the border, how many at it
+  uint32_t sure_so_far = 0, ties_so_far = 0;
+  for (int t0 = 0; t0 < T; t0 += kBlock) {
+    if constexpr (!WHOLE) load(t0);
+    uint64_t sure, tie;
+    const auto vote = [&](int i) __attribute__((always_inline)) {
+      uint32_t k = keys[i];
+      asm volatile("" : "+v"(k));                         // (or both loops' votes are kept for the other)
+      const bool in = t0 + i * kSelectThreads + tid < T;
+      sure = __ballot(in && k > border);
+      tie = __ballot(in && k == border);
+    };
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < REGS; ++i) {
+      vote(i);
+      if (lane == 0) s_hist[i * kSelectWaves + wave] = static_cast<uint32_t>(__popcll(sure)) | static_cast<uint32_t>(__popcll(tie)) << 16;
+    }
+    __syncthreads();
+    const uint32_t mine = tid < kEntries ? s_hist[tid] : 0u;
+    uint32_t sure_before, ties_before, all_sure;
+    s_scan.run(mine & 0xFFFFu, mine >> 16, sure_before, ties_before, all_sure);
+    if (tid < kEntries) {
+      s_hist[kEntries + tid] = sure_so_far + sure_before;
+      s_hist[2 * kEntries + tid] = ties_so_far + ties_before;
+    }
+    if (tid == kSelectThreads - 1) s_found[0] = ties_so_far + ties_before + (mine >> 16);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < REGS; ++i) {
+      if (t0 + i * kSelectThreads >= T) break;
+      vote(i);
+      if ((sure | tie) == 0) continue;
+      const uint64_t under = (1ull << lane) - 1, me = 1ull << lane;
+      const uint32_t ties = s_hist[2 * kEntries + i * kSelectWaves + wave] + __popcll(tie & under);
+      const uint32_t at = s_hist[kEntries + i * kSelectWaves + wave] + __popcll(sure & under) + min(ties, left);
+      if ((sure & me) || ((tie & me) && ties < left)) {
+        const int t = t0 + i * kSelectThreads + tid;
+        pos[at] = t;
+        if (weight) weight[at] = w[t];
+      }
+    }
+    sure_so_far += all_sure;
+    ties_so_far = s_found[0];
   }
 }
 
@@ -156,14 +218,21 @@ __global__ __launch_bounds__(256) void fill_tiles_kernel(FillArgs a) {
   const int64_t item = static_cast<int64_t>(a.seq0 + sl) * a.s.hkv + head, src = a.row0[sl] + static_cast<int64_t>(head) * T;
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, row0 = 16 * (tid >> 6) + 4 * (lane >> 4);
   const int32_t* pos = a.s.pos + item * a.s.capacity;
+  const int at = tile * kTileRows + row0;
   uint4 kq[4], vq[4];
+  int p[4];                                // all positions, then all rows
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = pos[min(at + i, n - 1)];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int at = tile * kTileRows + row0 + i;
-    const int64_t from = (src + pos[min(at, n - 1)]) * 16 + c16;
+    const int64_t from = (src + p[i]) * 16 + c16;
     kq[i] = reinterpret_cast<const uint4*>(a.K)[from];
     vq[i] = reinterpret_cast<const uint4*>(a.V)[from];
-    if (at >= n) kq[i] = vq[i] = make_uint4(0, 0, 0, 0);
+  }
+  if (tile * kTileRows + kTileRows > n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + i >= n) kq[i] = vq[i] = make_uint4(0, 0, 0, 0);
   }
   uint8_t* kt = a.s.k + (item * a.s.tiles + tile) * kTileBytes;
   uint8_t* vt = a.s.v + (item * a.s.tiles + tile) * kTileBytes;
@@ -173,50 +242,71 @@ __global__ __launch_bounds__(256) void fill_tiles_kernel(FillArgs a) {
   if (tid < kTileRows) *reinterpret_cast<uint4*>(kt + kTileCodes + 16 * tid) = *reinterpret_cast<const uint4*>(&s_km[tid][0]);
 }
 
-constexpr int kAppendThreads = 256;
+// A token into an item.  In a full one the least of (weight, position) among what may go is found by the whole workgroup, kEach slots of a
+// thread under way at once; the first lanes have the token's rows by then.  Bound: latency; 8 bytes a slot.
+constexpr int kAppendThreads = 1024, kAppendWaves = kAppendThreads / 64;
 
 template <int BITS>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(Args a, const uint16_t* __restrict__ k_new,
                                                                 const uint16_t* __restrict__ v_new, int32_t* __restrict__ slot_out) {
-  __shared__ uint64_t s_key[kAppendThreads / 64];
-  __shared__ int s_at[kAppendThreads / 64];
+  constexpr int kEach = 8;
+  __shared__ uint64_t s_key[kAppendWaves];
+  __shared__ int s_at[kAppendWaves];
   const int64_t item = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63, cap = a.capacity, n = a.length(item), next = a.next[item];
+  const int tid = threadIdx.x, lane = tid & 63, cap = a.capacity;
+  // lanes 0..15 hold the new K row, 16..31 the V row
+  const int c16 = tid & 15, grp = c16 >> 2, p = c16 & 3;
+  const bool is_v = tid >= 16;
+  uint4 row = make_uint4(0, 0, 0, 0);
+  if (tid < 32) row = reinterpret_cast<const uint4*>(is_v ? v_new : k_new)[item * 16 + c16];
+  const int n = a.length(item), next = a.next[item];
   int32_t* pos = a.pos + item * cap;
   int slot = n;
   if (n == cap) {
     // least weight, then lowest position; what may not go is behind everything else
     uint64_t best = ~0ull;
     int at = 0;
-    for (int i = tid; i < cap; i += kAppendThreads) {
-      const int p = pos[i];
-      if (p < a.sinks || p > next - a.recent) continue;
-      const uint64_t key = static_cast<uint64_t>(a.weight ? weight_key(a.weight[item * cap + i]) : 0u) << 32 | static_cast<uint32_t>(p);
-      if (key < best) {
-        best = key;
-        at = i;
+    const float* weight = a.weight ? a.weight + item * cap : nullptr;
+    for (int i0 = tid; i0 < cap; i0 += kEach * kAppendThreads) {
+      int at_pos[kEach];
+      float w[kEach];
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        const int i = min(i0 + k * kAppendThreads, cap - 1);
+        at_pos[k] = pos[i];
+        w[k] = weight ? weight[i] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        const int i = i0 + k * kAppendThreads;
+        const uint64_t key = static_cast<uint64_t>(weight_key(w[k])) << 32 | static_cast<uint32_t>(at_pos[k]);
+        if (i < cap && at_pos[k] >= a.sinks && at_pos[k] <= next - a.recent && key < best) {
+          best = key;
+          at = i;
+        }
       }
     }
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint64_t other = __shfl_xor(best, d);
-      const int other_at = __shfl_xor(at, d);
+    const auto least = [&](uint64_t other, int other_at) __attribute__((always_inline)) {
       if (other < best || (other == best && other_at < at)) {
         best = other;
         at = other_at;
       }
+    };
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint64_t other = __shfl_xor(best, d);
+      least(other, __shfl_xor(at, d));
     }
     if (lane == 0) {
       s_key[tid >> 6] = best;
       s_at[tid >> 6] = at;
     }
     __syncthreads();
-    best = s_key[0];
-    at = s_at[0];
-    for (int w = 1; w < kAppendThreads / 64; ++w)
-      if (s_key[w] < best || (s_key[w] == best && s_at[w] < at)) {
-        best = s_key[w];
-        at = s_at[w];
-      }
+    best = s_key[lane & (kAppendWaves - 1)];
+    at = s_at[lane & (kAppendWaves - 1)];
+    for (int d = 1; d < kAppendWaves; d <<= 1) {
+      const uint64_t other = __shfl_xor(best, d);
+      least(other, __shfl_xor(at, d));
+    }
     slot = at;
   }
   __syncthreads();                 // len, next and the arrays have been read
@@ -228,10 +318,6 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(Args a, const ui
     if (slot_out) slot_out[item] = slot;
   }
   if (tid >= 32) return;
-  // lanes 0..15 K, 16..31 V
-  const int c16 = tid & 15, grp = c16 >> 2, p = c16 & 3;
-  const bool is_v = tid >= 16;
-  const uint4 row = reinterpret_cast<const uint4*>(is_v ? v_new : k_new)[item * 16 + c16];
   uint8_t* side = is_v ? a.v : a.k;
   if constexpr (BITS == 16) {
     reinterpret_cast<uint4*>(side)[(item * cap + slot) * 16 + c16] = row;
@@ -260,11 +346,86 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(Args a, const ui
   }
 }
 
-// nearest bf16, ties to even (NaN stays one)
-__device__ __forceinline__ uint32_t to_bf16(float x) {
-  const uint32_t u = __float_as_uint(x);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (u >> 16) | 0x40u;
-  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+// scale x code + offset of two values, as bf16
+__device__ __forceinline__ uint32_t two_values(uint32_t c0, uint32_t c1, float s0, float s1, float z0, float z1) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v{s0 * static_cast<float>(c0) + z0, s1 * static_cast<float>(c1) + z1}), bf16x2));
+}
+__device__ __forceinline__ float half_of(uint32_t w, int h) { return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(h ? w >> 16 : w))); }
+
+// Tiles of 4-bit rows, slot after slot.  A workgroup has a tile, a lane eight channels of four rows, as where tiles are filled.  V words
+// hold a channel's four rows together and pass through LDS (a group's words 16 bytes apart from where the next's would fall on the same
+// banks).  Bound: HBM, 80 bytes read and 256 written a row and side.
+constexpr int kGroupStride = 1024 + 64, kBlockPad = 16;       // of 8 lanes' words
+__global__ __launch_bounds__(256) void read_tiles_kernel(Args a, int n, int groups, uint16_t* __restrict__ K, uint16_t* __restrict__ V) {
+  __shared__ __align__(16) uint8_t s_v[4 * (kGroupStride + 8 * kBlockPad)];
+  const int64_t item = blockIdx.x / groups;
+  const int tile = static_cast<int>(blockIdx.x % groups), tid = threadIdx.x, lane = tid & 63;
+  const int c16 = lane & 15, grp = c16 >> 2, p = c16 & 3, row0 = 16 * (tid >> 6) + 4 * (lane >> 4);
+  const int len = min(a.length(item), n);
+  uint16_t* k_out = K + (item * n + static_cast<int64_t>(tile) * kTileRows) * kHeadDim;
+  uint16_t* v_out = V + (item * n + static_cast<int64_t>(tile) * kTileRows) * kHeadDim;
+  const int rows = min(kTileRows, n - tile * kTileRows), held = len - tile * kTileRows;      // to write; of them with a token
+  uint4 kq[4], vq[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) kq[i] = vq[i] = make_uint4(0, 0, 0, 0);
+  if (held > 0) {
+    const uint8_t* kt = a.k + (item * a.tiles + tile) * kTileBytes;
+    const uint8_t* vt = a.v + (item * a.tiles + tile) * kTileBytes;
+    const uint4 raw = *reinterpret_cast<const uint4*>(vt + 16 * tid);
+    uint2 kw[4];
+    uint4 km[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      kw[i] = *reinterpret_cast<const uint2*>(kt + 1024 * grp + 16 * (row0 + i) + 8 * (p >> 1));
+      km[i] = *reinterpret_cast<const uint4*>(kt + kTileCodes + 16 * (row0 + i));
+    }
+    const uint4 vm = *reinterpret_cast<const uint4*>(vt + kTileCodes + 16 * row0 + 16 * grp);
+    const auto v_at = [](int g, int l) { return g * (kGroupStride + 8 * kBlockPad) + 16 * l + kBlockPad * (l >> 3); };
+    *reinterpret_cast<uint4*>(s_v + v_at(tid >> 6, lane)) = raw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {        // codes 8 p .. of the group: fields 2 (p % 2) and the next of word pair p / 2
+      const uint32_t w0 = kw[i].x >> (8 * (p & 1)), w1 = kw[i].y >> (8 * (p & 1));
+      const float s = half_of(grp < 2 ? km[i].x : km[i].y, grp & 1), z = half_of(grp < 2 ? km[i].z : km[i].w, grp & 1);
+      kq[i].x = two_values(w0 & 15u, (w0 >> 16) & 15u, s, s, z, z);
+      kq[i].y = two_values(w1 & 15u, (w1 >> 16) & 15u, s, s, z, z);
+      kq[i].z = two_values((w0 >> 4) & 15u, (w0 >> 20) & 15u, s, s, z, z);
+      kq[i].w = two_values((w1 >> 4) & 15u, (w1 >> 20) & 15u, s, s, z, z);
+    }
+    __syncthreads();
+    const int k = row0 & 31, shift = 4 * ((k >> 2) & 3);      // rows row0 .. row0 + 3: a field of words 2 (k / 16), and the next
+    uint2 vw[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      vw[j] = *reinterpret_cast<const uint2*>(s_v + v_at(grp, 32 * (row0 >> 5) + 8 * p + j) + 8 * (k >> 4));
+      vw[j].x >>= shift;
+      vw[j].y >>= shift;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float s = half_of(i < 2 ? vm.x : vm.y, i & 1), z = half_of(i < 2 ? vm.z : vm.w, i & 1);
+      uint32_t o[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w0 = i < 2 ? vw[2 * j].x : vw[2 * j].y, w1 = i < 2 ? vw[2 * j + 1].x : vw[2 * j + 1].y;
+        o[j] = two_values((w0 >> (16 * (i & 1))) & 15u, (w1 >> (16 * (i & 1))) & 15u, s, s, z, z);
+      }
+      vq[i] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row0 + i >= held) kq[i] = vq[i] = make_uint4(0, 0, 0, 0);
+  }
+  // No load is on its way here.  (With one that a branch above may have left, every store under a condition would wait for the one before
+  // it: 4 x 8 items of 32K slots 437 us.)
+  __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0)
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (row0 + i < rows) {
+      *reinterpret_cast<uint4*>(k_out + (row0 + i) * kHeadDim + c16 * 8) = kq[i];
+      *reinterpret_cast<uint4*>(v_out + (row0 + i) * kHeadDim + c16 * 8) = vq[i];
+    }
 }
 
 template <int BITS>
@@ -286,23 +447,27 @@ __global__ __launch_bounds__(256) void read_kernel(Args a, const int32_t* __rest
       const uint8_t* vt = a.v + (item * a.tiles + slot / kTileRows) * kTileBytes;
       const _Float16* km = reinterpret_cast<const _Float16*>(kt + kTileCodes);
       const _Float16* vm = reinterpret_cast<const _Float16*>(vt + kTileCodes);
-      uint32_t ko[8], vo[8];
+      uint32_t kc[8], vc[8];
+      const int grp = c16 >> 2;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int c = c16 * 8 + j, grp = c >> 5;
+        const int c = c16 * 8 + j;
         const auto code = [&](const uint8_t* tile, int lane, int k) {
           const int word = 4 * grp + 2 * (k >> 4) + ((k >> 1) & 1);
           return *reinterpret_cast<const uint32_t*>(tile + 1024 * (word >> 2) + 16 * lane + 4 * (word & 3)) >>
                      (16 * (k & 1) + 4 * ((k >> 2) & 3)) & 15u;
         };
-        const float ks = km[8 * r + grp], kz = km[8 * r + 4 + grp];
-        const int m = 32 * (r >> 2) + 8 * grp + (r & 3);
-        const float vs = vm[m], vz = vm[m + 4];
-        ko[j] = to_bf16(ks * static_cast<float>(code(kt, r, c & 31)) + kz);
-        vo[j] = to_bf16(vs * static_cast<float>(code(vt, 32 * (r >> 5) + (c & 31), r & 31)) + vz);
+        kc[j] = code(kt, r, c & 31);
+        vc[j] = code(vt, 32 * (r >> 5) + (c & 31), r & 31);
       }
-      kq = make_uint4(ko[0] | ko[1] << 16, ko[2] | ko[3] << 16, ko[4] | ko[5] << 16, ko[6] | ko[7] << 16);
-      vq = make_uint4(vo[0] | vo[1] << 16, vo[2] | vo[3] << 16, vo[4] | vo[5] << 16, vo[6] | vo[7] << 16);
+      const int m = 32 * (r >> 2) + 8 * grp + (r & 3);
+      const float ks = km[8 * r + grp], kz = km[8 * r + 4 + grp], vs = vm[m], vz = vm[m + 4];
+      const auto four = [](const uint32_t (&x)[8], float s, float z) {
+        return make_uint4(two_values(x[0], x[1], s, s, z, z), two_values(x[2], x[3], s, s, z, z), two_values(x[4], x[5], s, s, z, z),
+                          two_values(x[6], x[7], s, s, z, z));
+      };
+      kq = four(kc, ks, kz);
+      vq = four(vc, vs, vz);
     }
   }
   reinterpret_cast<uint4*>(K)[to] = kq;
@@ -315,7 +480,11 @@ hipError_t launch_fill(const FillArgs& a, int n_seqs, int bits, hipStream_t st) 
   int most = 0;
   for (int i = 0; i < n_seqs; ++i) most = a.T[i] > most ? a.T[i] : most;
   const int n = most < a.s.capacity ? most : a.s.capacity;
-  hipLaunchKernelGGL(fill_select_kernel, dim3(a.s.hkv, n_seqs), dim3(kSelectThreads), 0, st, a);
+  const dim3 items(a.s.hkv, n_seqs), threads(kSelectThreads);
+  if (most <= 8 * kSelectThreads) hipLaunchKernelGGL((fill_select_kernel<8, true>), items, threads, 0, st, a);
+  else if (most <= 32 * kSelectThreads) hipLaunchKernelGGL((fill_select_kernel<32, true>), items, threads, 0, st, a);
+  else if (most <= 64 * kSelectThreads) hipLaunchKernelGGL((fill_select_kernel<64, true>), items, threads, 0, st, a);
+  else hipLaunchKernelGGL((fill_select_kernel<32, false>), items, threads, 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 0) return e;
   if (bits == 16)
@@ -335,7 +504,10 @@ hipError_t launch_append(const Args& a, int bits, int items, const uint16_t* k_n
 
 hipError_t launch_read(const Args& a, int bits, int items, const int32_t* index, int n, uint16_t* K, uint16_t* V, hipStream_t st) {
   const int groups = (n + 15) / 16;        // (of 16 rows; less than 2^27 in all)
-  if (bits == 16)
+  const int tiles = (n + kTileRows - 1) / kTileRows;
+  if (bits == 4 && !index)
+    hipLaunchKernelGGL(read_tiles_kernel, dim3(tiles * items), dim3(256), 0, st, a, n, tiles, K, V);
+  else if (bits == 16)
     hipLaunchKernelGGL(read_kernel<16>, dim3(groups * items), dim3(256), 0, st, a, index, n, groups, K, V);
   else
     hipLaunchKernelGGL(read_kernel<4>, dim3(groups * items), dim3(256), 0, st, a, index, n, groups, K, V);
