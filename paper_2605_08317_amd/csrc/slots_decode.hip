@@ -36,6 +36,7 @@ struct DecodeArgs {
   float* part_acc;     // [slot][g][128]: partials; slot = workgroup + item
   float* part_ml;      // [slot][g][2]
   int2* parts;         // [items]: an item's first partial and their number, 0 where it has none
+  int32_t held_bytes;  // of scores that a wavefront keeps
   int32_t items, score_rows, least;     // least: tiles of a workgroup's share; 0: a workgroup takes an item
 };
 
@@ -130,19 +131,6 @@ __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int 
   for (int hs = 0; hs < HS; ++hs)
 #pragma unroll
     for (int i = 0; i < 4; ++i) xt[hs][i] = seen ? xt[hs][i] * kLog2e : -INFINITY;
-  // (no weights: an empty buffer)
-  const auto dst = __builtin_amdgcn_make_buffer_rsrc(sc.scores + static_cast<int64_t>(tile) * kTile * sc.g, 0, sc.tracked ? kTile * 4 * sc.g : 0, 0x00027000);
-  const auto u = [&](int hs, int i) __attribute__((always_inline)) { return __float_as_uint(xt[hs][i]); };
-  using Four = __attribute__((ext_vector_type(4))) uint32_t;
-  using Two = __attribute__((ext_vector_type(2))) uint32_t;
-  if constexpr (HS == 2) {
-    __builtin_amdgcn_raw_buffer_store_b128((Four{u(0, 0), u(0, 1), u(0, 2), u(0, 3)}), dst, 32 * lane, 0, 0);
-    __builtin_amdgcn_raw_buffer_store_b128((Four{u(1, 0), u(1, 1), u(1, 2), u(1, 3)}), dst, 32 * lane + 16, 0, 0);
-  } else {
-    if (sc.g == 4) __builtin_amdgcn_raw_buffer_store_b128((Four{u(0, 0), u(0, 1), u(0, 2), u(0, 3)}), dst, 16 * lane, 0, 0);
-    else if (sc.g == 2) __builtin_amdgcn_raw_buffer_store_b64((Two{u(0, 0), u(0, 1)}), dst, 8 * lane, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(u(0, 0), dst, 4 * lane, 0, 0);
-  }
   return __builtin_amdgcn_ballot_w64(seen);
 }
 
@@ -176,6 +164,56 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& r
   }
 }
 
+// A tile's scores into the workspace.
+template <int HS>
+__device__ __forceinline__ void store_scores(const Scoring& sc, int tile, const float (&xt)[HS][4]) {
+  const int lane = threadIdx.x & 63;
+  // (no weights: an empty buffer)
+  const auto dst = __builtin_amdgcn_make_buffer_rsrc(sc.scores + static_cast<int64_t>(tile) * kTile * sc.g, 0, sc.tracked ? kTile * 4 * sc.g : 0, 0x00027000);
+  const auto u = [&](int hs, int i) __attribute__((always_inline)) { return __float_as_uint(xt[hs][i]); };
+  using Four = __attribute__((ext_vector_type(4))) uint32_t;
+  using Two = __attribute__((ext_vector_type(2))) uint32_t;
+  if constexpr (HS == 2) {
+    __builtin_amdgcn_raw_buffer_store_b128((Four{u(0, 0), u(0, 1), u(0, 2), u(0, 3)}), dst, 32 * lane, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128((Four{u(1, 0), u(1, 1), u(1, 2), u(1, 3)}), dst, 32 * lane + 16, 0, 0);
+  } else {
+    if (sc.g == 4) __builtin_amdgcn_raw_buffer_store_b128((Four{u(0, 0), u(0, 1), u(0, 2), u(0, 3)}), dst, 16 * lane, 0, 0);
+    else if (sc.g == 2) __builtin_amdgcn_raw_buffer_store_b64((Two{u(0, 0), u(0, 1)}), dst, 8 * lane, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(u(0, 0), dst, 4 * lane, 0, 0);
+  }
+}
+
+// The same by way of LDS, which wavefronts that do not pass rows through it have room in.  Where a workgroup has all of an item they stay
+// there until its sums are known.  Otherwise kHeldBytes of a wavefront's scores go out together: writes among the reads of rows cost more
+// than their bytes, and wavefronts that began together write together.  (4 x 8 items of 128K slots, 4 heads: 103 us without scores, 139
+// with a store a tile, 128 so; 32 x 8 of 8K 71 -> 64.5.)
+constexpr int kHeldBytes = 16384;
+template <int HS>
+__device__ __forceinline__ void hold_scores(const Scoring& sc, int held, const float (&xt)[HS][4], uint8_t* s_held) {
+  const int lane = threadIdx.x & 63;
+  float* dst = reinterpret_cast<float*>(s_held) + (held * kTile + lane) * sc.g;
+  if constexpr (HS == 2) {
+    *reinterpret_cast<float4*>(dst) = make_float4(xt[0][0], xt[0][1], xt[0][2], xt[0][3]);
+    *reinterpret_cast<float4*>(dst + 4) = make_float4(xt[1][0], xt[1][1], xt[1][2], xt[1][3]);
+  } else {
+    if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(xt[0][0], xt[0][1], xt[0][2], xt[0][3]);
+    else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(xt[0][0], xt[0][1]);
+    else *dst = xt[0][0];
+  }
+}
+// held tiles, `step` apart and the last of them `tile`, into the workspace
+template <int HS>
+__device__ __forceinline__ void flush_scores(const Scoring& sc, int tile, int step, int held, const uint8_t* s_held) {
+  const int lane = threadIdx.x & 63, bytes = kTile * 4 * sc.g;
+  wave_lds_sync();
+  for (int k = 0; k < held; ++k) {
+    float* dst = sc.scores + static_cast<int64_t>(tile - (held - 1 - k) * step) * kTile * sc.g;
+    for (int at = 16 * lane; at < bytes; at += 1024)
+      *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(dst) + at) = *reinterpret_cast<const uint4*>(s_held + k * bytes + at);
+  }
+  wave_lds_sync();
+}
+
 template <int HS>
 __device__ __forceinline__ void init(Run<HS>& run) {
   run.init();
@@ -185,7 +223,7 @@ __device__ __forceinline__ void init(Run<HS>& run) {
 
 // Sixteen bytes of a tile.  STREAM: non-temporal, so that rows, which a step reads once, do not push scores out of the caches: 4 x 8 items of
 // 128K slots in bf16 432 -> 388 us, without weights 357 -> 313 (6.8 TB/s).  Small caches may still be there from the step before: 32 of 2
-// items of 1000 slots 16.0 us each with it, 13.3 without.
+// items of 1000 slots 16.0 us each with it, 13.3 without, 4 of 32 items of 8K in 4 bits (40 MB) 22.3, 20.8.  The line is at 64 MiB of rows.
 template <bool STREAM, class Buffer>
 __device__ __forceinline__ uint4 stream_load(Buffer tile, int at) {
   const auto v = __builtin_amdgcn_raw_buffer_load_b128(tile, at, 0, STREAM ? 2 : 0);
@@ -230,7 +268,7 @@ __device__ __forceinline__ void pv_rows(const uint8_t* s_stage, int lane, const 
 }
 
 // Tiles t0 .. t1 - 1 of an item, the workgroup's wavefronts in turn.  kd, vd: the item's rows.
-template <int HS, int NWV>
+template <int HS, int NWV, bool STREAM>
 __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
                                              const Scoring& sc, int t0, int t1, uint8_t* s_stage, Run<HS>& run) {
   const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
@@ -245,7 +283,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
     const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + static_cast<int64_t>(t) * (kTile * kHeadDim * 2)), 0,
                                                         rows * (kHeadDim * 2), 0x00027000);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) st[i] = stream_load<NWV == 4>(tile, lane * 16 + i * 1024);
+    for (int i = 0; i < 16; ++i) st[i] = stream_load<STREAM>(tile, lane * 16 + i * 1024);
   };
   auto store_tile = [&](const uint4 (&st)[16]) __attribute__((always_inline)) {
 #pragma unroll
@@ -291,6 +329,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
 #pragma unroll
       for (int i = 0; i < 4; ++i) xt[hs][i] = a16[hs][i];
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, kRoot, xt);
+    store_scores<HS>(sc, tile, xt);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
     softmax_step<HS>(x, run, p, 0.f);
@@ -347,9 +386,12 @@ __device__ __forceinline__ int exponent_of(float x) {      // of a number > 0; b
   return static_cast<int>((__float_as_uint(x) >> 23) & 255u) - 127;
 }
 
-template <int HS, int NWV>
+template <int HS, int NWV, bool STREAM>
 __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
-                                               const Scoring& sc, int t0, int t1, Run<HS>& run) {
+                                               const Scoring& sc, int t0, int t1, uint8_t* s_held, Run<HS>& run) {
+  constexpr bool kKeep = NWV == 8;       // for the end of the kernel
+  int held = 0;
+  const int most_held = kHeldBytes / (kTile * 4 * sc.g);
   const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint4 qraw[HS];
@@ -360,15 +402,15 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   auto load_k = [&](int t) __attribute__((always_inline)) {      // (as in rows_segment: no bytes behind the last tile)
     const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(kd + static_cast<int64_t>(t) * kTileBytes), 0, t < t1 ? kTileBytes : 0, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) kr[i] = stream_load<NWV == 4>(tile, lane * 16 + 1024 * i);
-    kmeta = stream_load<NWV == 4>(tile, lane * 16 + 4096);
+    for (int i = 0; i < 4; ++i) kr[i] = stream_load<STREAM>(tile, lane * 16 + 1024 * i);
+    kmeta = stream_load<STREAM>(tile, lane * 16 + 4096);
     pos = position(sc, t, t1);
   };
   auto load_v = [&](int t) __attribute__((always_inline)) {
     const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(vd + static_cast<int64_t>(t) * kTileBytes), 0, t < t1 ? kTileBytes : 0, 0x00027000);
-    vmeta = stream_load<NWV == 4>(tile, lane * 16 + 4096);
+    vmeta = stream_load<STREAM>(tile, lane * 16 + 4096);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vr[i] = stream_load<NWV == 4>(tile, lane * 16 + 1024 * i);
+    for (int i = 0; i < 4; ++i) vr[i] = stream_load<STREAM>(tile, lane * 16 + 1024 * i);
   };
   load_k(t0 + wave);
   load_v(t0 + wave);
@@ -465,6 +507,13 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     }
     load_k(next);
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
+    if (sc.tracked) {
+      hold_scores<HS>(sc, held++, xt, s_held);
+      if (!kKeep && (held == most_held || next >= t1)) {
+        flush_scores<HS>(sc, tile, NWV, held, s_held);
+        held = 0;
+      }
+    }
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
     softmax_step<HS>(x, run, p, kPUp);
@@ -547,47 +596,79 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 template <int NWV, int HS>
 constexpr int ml_floats() { return ml_lds_floats(NWV, HS); }
 
-// Weights of slots r0 .. r1 - 1 of an item; lse2 of its heads, log2.  A thread has kEach slots under way.
-template <int G>
-__device__ __forceinline__ void add_weights_g(const Args& a, int64_t item, const float* __restrict__ scores, const float* lse2, int r0, int r1,
-                                              int thread, int threads) {
-  constexpr int kEach = G == 8 ? 2 : 4, kWide = G < 4 ? G : 4;
+// What a thread adds to the weights of its slots: their scores and weights are loaded before the heads' log-sum-exps are known.
+// EACH slots, `step` apart.
+template <int G, int EACH>
+struct WeightPart {
+  static constexpr int kWide = G < 4 ? G : 4;
   using Wide = __attribute__((ext_vector_type(kWide))) float;
-  float* __restrict__ weight = a.weight + item * a.capacity;
-  float l[G];
+  Wide x[EACH][G / kWide];
+  float w[EACH];
+  // slots i0, i0 + step, ..; the loads stay below `end`, a slot at least there is
+  __device__ __forceinline__ void load(const float* __restrict__ scores, const float* __restrict__ weight, int i0, int step, int end) {
 #pragma unroll
-  for (int h = 0; h < G; ++h) l[h] = lse2[h];
-  for (int i0 = r0 + thread; i0 < r1; i0 += kEach * threads) {
-    Wide x[kEach][G / kWide];
-    float w[kEach];
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int i = min(i0 + k * threads, r1 - 1);
+    for (int k = 0; k < EACH; ++k) {
+      const int i = min(i0 + k * step, end - 1);
 #pragma unroll
       for (int h = 0; h < G / kWide; ++h) x[k][h] = *reinterpret_cast<const Wide*>(scores + static_cast<int64_t>(i) * G + h * kWide);
       w[k] = weight[i];
     }
+  }
+  // lse2: of the heads, log2
+  __device__ __forceinline__ void store(float* __restrict__ weight, float decay, const float* lse2, int i0, int step, int end) const {
+    float l[G];
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) {
+    for (int h = 0; h < G; ++h) l[h] = lse2[h];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
       float p = 0.f;
 #pragma unroll
       for (int h = 0; h < G; ++h) p += fast_exp2(x[k][h / kWide][h % kWide] - l[h]);
-      if (i0 + k * threads < r1) weight[i0 + k * threads] = __builtin_fmaf(a.decay, w[k], p);
+      if (i0 + k * step < end) weight[i0 + k * step] = __builtin_fmaf(decay, w[k], p);
     }
   }
+};
+template <int G>
+__device__ __forceinline__ void add_weights(const Args& a, int64_t item, const float* scores, const float* lse2, int n, int thread, int threads) {
+  constexpr int kEach = G == 8 ? 2 : 4;
+  float* weight = a.weight + item * a.capacity;
+  for (int i = thread; i < n; i += kEach * threads) {
+    WeightPart<G, kEach> part;
+    part.load(scores, weight, i, threads, n);
+    part.store(weight, a.decay, lse2, i, threads, n);
+  }
 }
-__device__ __forceinline__ void add_weights(const Args& a, int64_t item, const float* scores, int g, const float* lse2, int r0, int r1, int thread,
-                                            int threads) {
-  if (g == 8) add_weights_g<8>(a, item, scores, lse2, r0, r1, thread, threads);
-  else if (g == 4) add_weights_g<4>(a, item, scores, lse2, r0, r1, thread, threads);
-  else if (g == 2) add_weights_g<2>(a, item, scores, lse2, r0, r1, thread, threads);
-  else add_weights_g<1>(a, item, scores, lse2, r0, r1, thread, threads);
+
+// The same from scores that a wavefront has kept: tiles wave, wave + NWV, .. of an item.
+template <int HS, int NWV>
+__device__ __forceinline__ void add_held(const Args& a, int64_t item, const float* s_held, const float* lse2, int n, int wave, int tiles) {
+  const int lane = threadIdx.x & 63;
+  float* __restrict__ weight = a.weight + item * a.capacity;
+  float l[4 * HS];
+#pragma unroll
+  for (int h = 0; h < 4 * HS; ++h) l[h] = lse2[h < a.g ? h : 0];
+  for (int t0 = wave, k = 0; t0 < tiles; t0 += 4 * NWV, k += 4) {
+    float w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = weight[min((t0 + j * NWV) * kTile + lane, n - 1)];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = (t0 + j * NWV) * kTile + lane;
+      if (i >= n) break;
+      const float* x = s_held + ((k + j) * kTile + lane) * a.g;
+      float p = 0.f;
+#pragma unroll
+      for (int h = 0; h < 4 * HS; ++h)
+        if (HS == 2 || h < a.g) p += fast_exp2(x[h] - l[h]);
+      weight[i] = __builtin_fmaf(a.decay, w[j], p);
+    }
+  }
 }
 
 // log2 of the sum of 2^score over everything: sum l, relative to 2^m; +inf where nothing was seen, which makes every weight 0
 __device__ __forceinline__ float total_log2(float m, float l) { return l == 0.f ? INFINITY : m + __log2f(l); }
 
-template <int BITS, int HS, int NWV>
+template <int BITS, int HS, int NWV, bool STREAM>
 __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decode_kernel(DecodeArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -612,9 +693,13 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
   } else {
     end = tiles_of(a.s, item);
   }
-  float* s_ml = reinterpret_cast<float*>(smem + (BITS == 16 ? NWV * kStageBytes : 0));
-  float* s_acc = BITS == 16 ? reinterpret_cast<float*>(smem) : s_ml + ml_floats<NWV, HS>();
-  float* s_lse = BITS == 16 ? s_ml + ml_floats<NWV, HS>() : s_acc + NWV * g * kHeadDim;
+  // LDS: the wavefronts' staging regions or held scores, which the accumulators' area [NWV][g][128] shares unless they are kept; then the
+  // wavefronts' maxima and sums, and the heads' log-sum-exps
+  constexpr bool kKeep = BITS == 4 && NWV == 8;
+  const int wave_bytes = BITS == 16 ? kStageBytes : kKeep ? a.held_bytes : kHeldBytes;
+  float* s_acc = reinterpret_cast<float*>(smem + (kKeep ? NWV * wave_bytes : 0));
+  float* s_ml = kKeep ? s_acc + NWV * g * kHeadDim : reinterpret_cast<float*>(smem + NWV * wave_bytes);
+  float* s_lse = s_ml + ml_floats<NWV, HS>();
   while (at < end) {
     const int n = a.s.length(item), tiles = (n + kTile - 1) / kTile;
     const int t0 = at - first, t1 = min(tiles, end - first);
@@ -650,11 +735,12 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     float scale = 1.f;
     if constexpr (BITS == 16) {
       const int64_t base = static_cast<int64_t>(item) * a.s.capacity * (kHeadDim * 2);
-      rows_segment<HS, NWV>(a.s.k + base, a.s.v + base, q, sc, t0, t1, smem + wave * kStageBytes, run);
+      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, smem + wave * kStageBytes, run);
       __syncthreads();                   // the staging regions become the accumulator area
     } else {
       const int64_t base = static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
-      scale = tiles_segment<HS, NWV>(a.s.k + base, a.s.v + base, q, sc, t0, t1, run);
+      scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, smem + wave * wave_bytes, run);
+      if constexpr (!kKeep) __syncthreads();      // the held scores' memory becomes the accumulator area
     }
     // ---- the wavefronts' results into LDS ------------------------------------------------------------------------------
 #pragma unroll
@@ -724,8 +810,13 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
       }
     }
     __syncthreads();
-    if (whole && a.s.weight != nullptr) {
-      add_weights(a.s, item, sc.scores, g, s_lse, 0, n, tid, NWV * 64);
+    if (kKeep && a.s.weight != nullptr) {
+      add_held<HS, NWV>(a.s, item, reinterpret_cast<const float*>(smem + wave * wave_bytes), s_lse, n, wave, tiles);
+    } else if (whole && a.s.weight != nullptr) {
+      if (HS == 2) add_weights<8>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
+      else if (g == 4) add_weights<4>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
+      else if (g == 2) add_weights<2>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
+      else add_weights<1>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
       __syncthreads();
     }
     at = first + t1;
@@ -742,26 +833,31 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v + o;
 }
 
-// The items whose tiles several workgroups shared: their partials into the outputs, and their weights.  `rows` workgroups an item.
-constexpr int kJoinThreads = 256;
+// The items whose tiles several workgroups shared: their partials into the outputs, and their weights.  `rows` workgroups an item, each
+// with kJoinSlots slots of it; its loads of them are under way while the heads' sums are made.
+constexpr int kJoinThreads = 256, kJoinEach = 4, kJoinSlots = kJoinThreads * kJoinEach;
+template <int G>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int rows) {
-  __shared__ float s_lse[8], s_top[8], s_half[kHeadDim];
-  const int item = blockIdx.x / rows, row = blockIdx.x % rows, tid = threadIdx.x, lane = tid & 63, g = a.s.g;
+  __shared__ float s_lse[G], s_top[G], s_half[kHeadDim];
+  const int item = blockIdx.x / rows, row = blockIdx.x % rows, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int2 of = a.parts[item];
-  const int n = a.s.length(item), tiles = (n + kTile - 1) / kTile, parts = of.y;
+  const int n = a.s.length(item), parts = of.y, i0 = row * kJoinSlots + tid;
+  const int64_t slot0 = of.x, qh0 = static_cast<int64_t>(item) * G;
+  const bool tracked = a.s.weight != nullptr && row * kJoinSlots < a.s.capacity;
+  float* weight = a.s.weight + static_cast<int64_t>(item) * a.s.capacity;
+  WeightPart<G, kJoinEach> part;
+  if (tracked) part.load(a.scores + qh0 * a.score_rows, weight, i0, kJoinThreads, a.s.capacity);
   if (parts == 0) return;
-  const int64_t slot0 = of.x, qh0 = static_cast<int64_t>(item) * g;
-  for (int head = wave; head < g; head += kJoinThreads / 64) {
+  for (int head = wave; head < G; head += kJoinThreads / 64) {
     float m = kLowest, l = 0.f;
     for (int k = lane; k < parts; k += 64) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * g + head) * 2);
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * G + head) * 2);
       const float mm = fmaxf(m, ml.x);
       l = l * fast_exp2(m - mm) + ml.y * fast_exp2(ml.x - mm);
       m = mm;
     }
-    const float mm = row_max(m);
-    float o = mm, top = mm;
+    float top = row_max(m), o = top;
     swap_rows(top, o);
     top = o = fmaxf(top, o);
     swap_halves(top, o);
@@ -773,14 +869,14 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
     }
   }
   __syncthreads();
-  // heads among the row's workgroups: two halves of the partials, a channel a thread
-  for (int head = row; head < g; head += rows) {
+  // heads among the item's workgroups: two halves of the partials, a channel a thread
+  for (int head = row; head < G; head += rows) {
     const int c = tid & (kHeadDim - 1), half = tid >> 7;
     const float top = s_top[head];
     float v = 0.f;
     for (int k = half; k < parts; k += 2) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * g + head) * 2);
-      v = __builtin_fmaf(a.part_acc[((slot0 + k) * g + head) * kHeadDim + c], fast_exp2(ml.x - top), v);
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * G + head) * 2);
+      v = __builtin_fmaf(a.part_acc[((slot0 + k) * G + head) * kHeadDim + c], fast_exp2(ml.x - top), v);
     }
     if (half == 1) s_half[c] = v;
     __syncthreads();
@@ -792,22 +888,27 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
     }
     __syncthreads();
   }
-  if (a.s.weight == nullptr) return;
-  const int each = (tiles + rows - 1) / rows * kTile, r0 = row * each;
-  add_weights(a.s, item, a.scores + qh0 * a.score_rows, g, s_lse, r0, min(n, r0 + each), tid, kJoinThreads);
+  if (tracked) part.store(weight, a.s.decay, s_lse, i0, kJoinThreads, n);
 }
 
+constexpr size_t kMostLds = 160 << 10;
 struct Plan {
-  int waves, groups, least, score_rows, join_rows;
+  bool stream;         // rows past the caches' order
+  int waves, groups, least, score_rows, join_rows, held_bytes;
   size_t scores, part_acc, part_ml, parts;      // floats
 };
-Plan make_plan(int64_t items, int g, int capacity, int bits) {
+Plan make_plan(int64_t items, int g, int capacity, int bits, bool weights) {
   Plan p;
   const int64_t tiles = (capacity + kTile - 1) / kTile;
   p.score_rows = static_cast<int>(tiles) * kTile;
   p.scores = static_cast<size_t>(items) * g * p.score_rows;
+  p.stream = items * capacity * (bits == 16 ? 512 : 160) >= (static_cast<int64_t>(64) << 20);
   p.waves = 8;
-  if (tiles <= 3 * p.waves) {
+  // scores that a wavefront keeps, where a workgroup has an item's tiles
+  const size_t held = weights ? (tiles + p.waves - 1) / p.waves * kTile * g * sizeof(float) : 0;
+  const bool fits = bits == 4 && p.waves * (held + g * kHeadDim * sizeof(float)) + (ml_lds_floats(p.waves, g > 4 ? 2 : 1) + 8) * sizeof(float) <= kMostLds;
+  p.held_bytes = fits ? static_cast<int>(held) : 0;
+  if (tiles <= 3 * p.waves || (fits && items >= 192)) {
     p.least = p.join_rows = 0;
     p.groups = static_cast<int>(items);
     p.part_acc = p.part_ml = p.parts = 0;
@@ -818,7 +919,7 @@ Plan make_plan(int64_t items, int g, int capacity, int bits) {
   const int64_t most = (items * tiles + p.waves - 1) / p.waves;
   const int64_t resident = 512;
   p.groups = static_cast<int>(std::min(most, resident));
-  p.join_rows = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((p.score_rows + 1023) / 1024, 16384 / items)));
+  p.join_rows = weights ? (capacity + kJoinSlots - 1) / kJoinSlots : g;
   const size_t slots = static_cast<size_t>(p.groups) + items;
   p.part_acc = slots * g * kHeadDim;
   p.part_ml = slots * g * 2;
@@ -826,26 +927,33 @@ Plan make_plan(int64_t items, int g, int capacity, int bits) {
   return p;
 }
 
-template <int BITS, int HS, int NWV>
-hipError_t launch(const DecodeArgs& a, const Plan& p, hipStream_t st) {
-  const size_t ml = ml_floats<NWV, HS>() * sizeof(float), acc = static_cast<size_t>(NWV) * a.s.g * kHeadDim * sizeof(float), lse = 8 * sizeof(float);
-  const size_t lds = BITS == 16 ? NWV * kStageBytes + ml + lse : ml + acc + lse;
-  constexpr size_t kMost = BITS == 16 ? NWV * kStageBytes + ml_floats<NWV, HS>() * 4 + 32 : ml_floats<NWV, HS>() * 4 + NWV * 4 * HS * kHeadDim * 4 + 32;
-  const hipError_t e = RDKV_ALLOW_LDS((decode_kernel<BITS, HS, NWV>), kMost);
+template <int BITS, int HS, int NWV, bool STREAM>
+hipError_t launch_one(const DecodeArgs& a, const Plan& p, hipStream_t st) {
+  constexpr bool kKeep = BITS == 4 && NWV == 8;
+  constexpr size_t kEnd = (ml_floats<NWV, HS>() + 8) * sizeof(float);
+  const size_t wave = BITS == 16 ? kStageBytes : kKeep ? a.held_bytes + a.s.g * kHeadDim * sizeof(float) : kHeldBytes;
+  static_assert(kHeldBytes >= 4 * HS * kHeadDim * 4, "the accumulators fit");
+  const hipError_t e = RDKV_ALLOW_LDS((decode_kernel<BITS, HS, NWV, STREAM>), kKeep ? kMostLds : NWV * wave + kEnd);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((decode_kernel<BITS, HS, NWV>), dim3(p.groups), dim3(NWV * 64), lds, st, a);
+  hipLaunchKernelGGL((decode_kernel<BITS, HS, NWV, STREAM>), dim3(p.groups), dim3(NWV * 64), NWV * wave + kEnd, st, a);
   return hipGetLastError();
+}
+
+template <int BITS, int HS>
+hipError_t launch(const DecodeArgs& a, const Plan& p, hipStream_t st) {
+  if (p.waves == 8) return p.stream ? launch_one<BITS, HS, 8, true>(a, p, st) : launch_one<BITS, HS, 8, false>(a, p, st);
+  return p.stream ? launch_one<BITS, HS, 4, true>(a, p, st) : launch_one<BITS, HS, 4, false>(a, p, st);
 }
 
 }  // namespace
 
 size_t decode_workspace_floats(int64_t items, int g, int capacity, int bits, bool weights) {
-  const Plan p = make_plan(items, g, capacity, bits);
+  const Plan p = make_plan(items, g, capacity, bits, weights);
   return std::max<size_t>((weights ? p.scores : 0) + p.part_acc + p.part_ml + p.parts, 4);
 }
 
 hipError_t launch_decode(const Args& s, int bits, int items, const uint16_t* q, float* out, float* lse, float* workspace, hipStream_t st) {
-  const Plan p = make_plan(items, s.g, s.capacity, bits);
+  const Plan p = make_plan(items, s.g, s.capacity, bits, s.weight != nullptr);
   DecodeArgs a;
   a.s = s;
   a.q = q;
@@ -859,16 +967,17 @@ hipError_t launch_decode(const Args& s, int bits, int items, const uint16_t* q, 
   a.items = items;
   a.score_rows = p.score_rows;
   a.least = p.least;
-  hipError_t e;
-  if (bits == 16) {
-    if (p.waves == 8) e = s.g > 4 ? launch<16, 2, 8>(a, p, st) : launch<16, 1, 8>(a, p, st);
-    else e = s.g > 4 ? launch<16, 2, 4>(a, p, st) : launch<16, 1, 4>(a, p, st);
-  } else {
-    if (s.g <= 4) e = p.waves == 8 ? launch<4, 1, 8>(a, p, st) : launch<4, 1, 4>(a, p, st);
-    else e = p.waves == 8 ? launch<4, 2, 8>(a, p, st) : launch<4, 2, 4>(a, p, st);
-  }
+  a.held_bytes = p.held_bytes;
+  const hipError_t e = bits == 16 ? s.g > 4 ? launch<16, 2>(a, p, st) : launch<16, 1>(a, p, st)
+                                  : s.g > 4 ? launch<4, 2>(a, p, st) : launch<4, 1>(a, p, st);
   if (e != hipSuccess || p.join_rows == 0) return e;
-  hipLaunchKernelGGL(join_kernel, dim3(items * p.join_rows), dim3(kJoinThreads), 0, st, a, p.join_rows);
+  const dim3 grid(items * p.join_rows), threads(kJoinThreads);
+  switch (s.g) {
+    case 8: hipLaunchKernelGGL(join_kernel<8>, grid, threads, 0, st, a, p.join_rows); break;
+    case 4: hipLaunchKernelGGL(join_kernel<4>, grid, threads, 0, st, a, p.join_rows); break;
+    case 2: hipLaunchKernelGGL(join_kernel<2>, grid, threads, 0, st, a, p.join_rows); break;
+    default: hipLaunchKernelGGL(join_kernel<1>, grid, threads, 0, st, a, p.join_rows); break;
+  }
   return hipGetLastError();
 }
 
