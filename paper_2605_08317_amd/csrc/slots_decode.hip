@@ -164,55 +164,43 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& r
   }
 }
 
-// A tile's scores into the workspace.
-template <int HS>
-__device__ __forceinline__ void store_scores(const Scoring& sc, int tile, const float (&xt)[HS][4]) {
-  const int lane = threadIdx.x & 63;
-  // (no weights: an empty buffer)
-  const auto dst = __builtin_amdgcn_make_buffer_rsrc(sc.scores + static_cast<int64_t>(tile) * kTile * sc.g, 0, sc.tracked ? kTile * 4 * sc.g : 0, 0x00027000);
-  const auto u = [&](int hs, int i) __attribute__((always_inline)) { return __float_as_uint(xt[hs][i]); };
-  using Four = __attribute__((ext_vector_type(4))) uint32_t;
-  using Two = __attribute__((ext_vector_type(2))) uint32_t;
-  if constexpr (HS == 2) {
-    __builtin_amdgcn_raw_buffer_store_b128((Four{u(0, 0), u(0, 1), u(0, 2), u(0, 3)}), dst, 32 * lane, 0, 0);
-    __builtin_amdgcn_raw_buffer_store_b128((Four{u(1, 0), u(1, 1), u(1, 2), u(1, 3)}), dst, 32 * lane + 16, 0, 0);
-  } else {
-    if (sc.g == 4) __builtin_amdgcn_raw_buffer_store_b128((Four{u(0, 0), u(0, 1), u(0, 2), u(0, 3)}), dst, 16 * lane, 0, 0);
-    else if (sc.g == 2) __builtin_amdgcn_raw_buffer_store_b64((Two{u(0, 0), u(0, 1)}), dst, 8 * lane, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(u(0, 0), dst, 4 * lane, 0, 0);
+// Scores on their way to the weights, which need them once the item's sums are known.  They wait in LDS: where a workgroup has all of an
+// item until then (KEEP), otherwise until a wavefront's part is full, which then goes to the workspace at once.  Writes among the reads
+// of rows cost more than their bytes, and wavefronts that began together write together (4 x 8 items of 128K slots in 4 bits, 4 heads: 103 us
+// without scores, 139 with a store a tile, 128 so; 32 x 8 of 8K 71 -> 64.5).
+struct Held {
+  uint8_t* at;         // of this wavefront: [tiles][64][g]
+  int n, most;         // tiles there, and room; most 0: all of the item's stay
+  template <int HS, int NWV>
+  __device__ __forceinline__ void put(const Scoring& sc, int tile, bool last, const float (&xt)[HS][4]) {
+    if (!sc.tracked) return;
+    const int lane = threadIdx.x & 63;
+    float* dst = reinterpret_cast<float*>(at) + (n * kTile + lane) * sc.g;
+    if constexpr (HS == 2) {
+      *reinterpret_cast<float4*>(dst) = make_float4(xt[0][0], xt[0][1], xt[0][2], xt[0][3]);
+      *reinterpret_cast<float4*>(dst + 4) = make_float4(xt[1][0], xt[1][1], xt[1][2], xt[1][3]);
+    } else {
+      if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(xt[0][0], xt[0][1], xt[0][2], xt[0][3]);
+      else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(xt[0][0], xt[0][1]);
+      else *dst = xt[0][0];
+    }
+    ++n;
+    if (n == most || (last && most > 0)) {
+      const int bytes = kTile * 4 * sc.g;
+      wave_lds_sync();
+      for (int k = 0; k < n; ++k) {
+        uint8_t* to = reinterpret_cast<uint8_t*>(sc.scores + static_cast<int64_t>(tile - (n - 1 - k) * NWV) * kTile * sc.g);
+        for (int i = 16 * lane; i < bytes; i += 1024) *reinterpret_cast<uint4*>(to + i) = *reinterpret_cast<const uint4*>(at + k * bytes + i);
+      }
+      wave_lds_sync();
+      n = 0;
+    }
   }
-}
-
-// The same by way of LDS, which wavefronts that do not pass rows through it have room in.  Where a workgroup has all of an item they stay
-// there until its sums are known.  Otherwise kHeldBytes of a wavefront's scores go out together: writes among the reads of rows cost more
-// than their bytes, and wavefronts that began together write together.  (4 x 8 items of 128K slots, 4 heads: 103 us without scores, 139
-// with a store a tile, 128 so; 32 x 8 of 8K 71 -> 64.5.)
-constexpr int kHeldBytes = 16384;
-template <int HS>
-__device__ __forceinline__ void hold_scores(const Scoring& sc, int held, const float (&xt)[HS][4], uint8_t* s_held) {
-  const int lane = threadIdx.x & 63;
-  float* dst = reinterpret_cast<float*>(s_held) + (held * kTile + lane) * sc.g;
-  if constexpr (HS == 2) {
-    *reinterpret_cast<float4*>(dst) = make_float4(xt[0][0], xt[0][1], xt[0][2], xt[0][3]);
-    *reinterpret_cast<float4*>(dst + 4) = make_float4(xt[1][0], xt[1][1], xt[1][2], xt[1][3]);
-  } else {
-    if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(xt[0][0], xt[0][1], xt[0][2], xt[0][3]);
-    else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(xt[0][0], xt[0][1]);
-    else *dst = xt[0][0];
-  }
-}
-// held tiles, `step` apart and the last of them `tile`, into the workspace
-template <int HS>
-__device__ __forceinline__ void flush_scores(const Scoring& sc, int tile, int step, int held, const uint8_t* s_held) {
-  const int lane = threadIdx.x & 63, bytes = kTile * 4 * sc.g;
-  wave_lds_sync();
-  for (int k = 0; k < held; ++k) {
-    float* dst = sc.scores + static_cast<int64_t>(tile - (held - 1 - k) * step) * kTile * sc.g;
-    for (int at = 16 * lane; at < bytes; at += 1024)
-      *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(dst) + at) = *reinterpret_cast<const uint4*>(s_held + k * bytes + at);
-  }
-  wave_lds_sync();
-}
+};
+// of a wavefront in a workgroup of four, two of which share a compute unit's LDS
+__host__ __device__ constexpr int held_bytes_of_four(int bits) { return bits == 16 ? 10240 : 16384; }
+// behind everything else: the query's rows of two head sets
+constexpr int kQueryBytes = 8 * kRowStride;
 
 template <int HS>
 __device__ __forceinline__ void init(Run<HS>& run) {
@@ -224,6 +212,11 @@ __device__ __forceinline__ void init(Run<HS>& run) {
 // Sixteen bytes of a tile.  STREAM: non-temporal, so that rows, which a step reads once, do not push scores out of the caches: 4 x 8 items of
 // 128K slots in bf16 432 -> 388 us, without weights 357 -> 313 (6.8 TB/s).  Small caches may still be there from the step before: 32 of 2
 // items of 1000 slots 16.0 us each with it, 13.3 without, 4 of 32 items of 8K in 4 bits (40 MB) 22.3, 20.8.  The line is at 64 MiB of rows.
+// (here(): a value that the compiler sees the loop make, so that constants added to it become the loads' offsets and not registers each.)
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 template <bool STREAM, class Buffer>
 __device__ __forceinline__ uint4 stream_load(Buffer tile, int at) {
   const auto v = __builtin_amdgcn_raw_buffer_load_b128(tile, at, 0, STREAM ? 2 : 0);
@@ -247,11 +240,13 @@ __device__ __forceinline__ void split_bf16_3(const float (&p)[4], short4v (&t)[3
   }
 }
 
+constexpr int kStageRows = 32, kHalfBytes = kStageRows * kRowStride;      // V rows that a wavefront has in LDS at a time
+
 template <int A, int HS>
 __device__ __forceinline__ void pv_rows_step(const uint8_t* s_stage, int lane, const short4v (&t)[HS][3], Run<HS>& run) {
   uint32_t w[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t*>(s_stage + (4 * A + k) * kRowStride + 4 * lane);
+  for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t*>(s_stage + ((4 * A) % kStageRows + k) * kRowStride + 4 * lane);
   const short4v be = bf4(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u));
   const short4v bo = bf4(__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u));
 #pragma unroll
@@ -262,74 +257,111 @@ __device__ __forceinline__ void pv_rows_step(const uint8_t* s_stage, int lane, c
       run.acc[hs][1] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(t[hs][k], bo, run.acc[hs][1], 4, A, 0);
     }
 }
-template <int HS, int... A>
+template <int A0, int HS, int... A>
 __device__ __forceinline__ void pv_rows(const uint8_t* s_stage, int lane, const short4v (&t)[HS][3], Run<HS>& run, std::integer_sequence<int, A...>) {
-  (pv_rows_step<A, HS>(s_stage, lane, t, run), ...);
+  (pv_rows_step<A0 + A, HS>(s_stage, lane, t, run), ...);
 }
 
 // Tiles t0 .. t1 - 1 of an item, the workgroup's wavefronts in turn.  kd, vd: the item's rows.
+// Rows pass through LDS, half a tile at a time, which leaves room there for scores: loads want whole rows, the matrix unit columns of them.
+// Scores: v_mfma_f32_16x16x32 has sixteen slots on one side, a lane eight channels of one; four heads on the other, four times over, so
+// that every row of lanes has them, and lane 16 b + c takes those of its slot, c of block b.
+// P V: lanes want a channel of four slots (decode_rows.h).
 template <int HS, int NWV, bool STREAM>
 __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
-                                             const Scoring& sc, int t0, int t1, uint8_t* s_stage, Run<HS>& run) {
-  const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
+                                             const Scoring& sc, int t0, int t1, uint8_t* s_stage, uint8_t* s_query, Held& held, Run<HS>& run) {
+  using Bf8 = __attribute__((ext_vector_type(8))) __bf16;
+  const int lane = threadIdx.x & 63, j = lane & 3;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane >> 4, lc = lane & 15;
-  // K and V of a tile in registers of their own, each loaded again right after it went to LDS: two tiles' sides are always on their way.
+  // K and V of a tile in registers of their own, each loaded again right after its last use: two tiles' sides are always on their way.
   // A tile is a buffer that ends with the item's last row, and what is behind it reads as zeros; behind the last tile it is empty.  (With
   // loads under a condition the compiler cannot count on them, and waits for all there are.)
   uint4 kq[16], vq[16];
-  auto load_tile = [&](uint4 (&st)[16], const uint8_t* __restrict__ base, int t) __attribute__((always_inline)) {
+  const auto tile_at = [&](const uint8_t* base, int t) __attribute__((always_inline)) {
     const int rows = t < t1 ? min(sc.n - t * kTile, kTile) : 0;
-    const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + static_cast<int64_t>(t) * (kTile * kHeadDim * 2)), 0,
-                                                        rows * (kHeadDim * 2), 0x00027000);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) st[i] = stream_load<STREAM>(tile, lane * 16 + i * 1024);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + static_cast<int64_t>(t) * (kTile * kHeadDim * 2)), 0, rows * (kHeadDim * 2),
+                                             0x00027000);
   };
-  auto store_tile = [&](const uint4 (&st)[16]) __attribute__((always_inline)) {
+  const auto load_tile = [&](uint4 (&st)[16], const uint8_t* base, int t) __attribute__((always_inline)) {
+    const auto tile = tile_at(base, t);
+    const int at = here(lane * 16);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4*>(s_stage + (4 * i + lr) * kRowStride + 16 * lc) = st[i];
+    for (int i = 0; i < 16; ++i) st[i] = stream_load<STREAM>(tile, at + i * 1024);
   };
-  auto load_pos = [&](int t) __attribute__((always_inline)) { return position(sc, t, t1); };
-  uint4 qa[HS];
+  const auto store_half = [&](const uint4 (&st)[16], int half) __attribute__((always_inline)) {
 #pragma unroll
-  for (int hs = 0; hs < HS; ++hs) qa[hs] = load_query(q, 4 * hs + j, sc.g, blk);
-  int pos = load_pos(t0 + wave);
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(s_stage + (4 * i + lr) * kRowStride + 16 * lc) = st[8 * half + i];
+  };
+  // The query: head 4 hs + lane % 4, channels 32 i + 8 (lane / 16) ..  Two head sets' would take the registers of a wavefront with two
+  // tiles' sides, and are in LDS.
+  constexpr bool kQueryInLds = HS == 2;
+  uint4 qa[HS][4];
+  const auto query = [&](int hs, int i) __attribute__((always_inline)) {
+    return 4 * hs + j < sc.g ? *reinterpret_cast<const uint4*>(q + (4 * hs + j) * kHeadDim + 32 * i + 8 * lr) : make_uint4(0, 0, 0, 0);
+  };
+  uint4 q_row;
+  if constexpr (kQueryInLds) {
+    if (threadIdx.x < 128) q_row = *reinterpret_cast<const uint4*>(q + 8 * threadIdx.x);
+  } else {
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) qa[hs][i] = query(hs, i);
+  }
+  int pos = position(sc, t0 + wave, t1);
   load_tile(kq, kd, t0 + wave);
   load_tile(vq, vd, t0 + wave);
   __builtin_amdgcn_sched_barrier(0);
   // the query is here before the loop: waited for inside, it would have every pass wait for all loads under way
-#pragma unroll
-  for (int hs = 0; hs < HS; ++hs) asm volatile("" : "+v"(qa[hs].x), "+v"(qa[hs].y), "+v"(qa[hs].z), "+v"(qa[hs].w));
-  const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
-  for (int tile = t0 + wave; tile < t1; tile += NWV) {
-    const int next = tile + NWV;
-    store_tile(kq);
-    const int pos_now = pos;
-    pos = load_pos(next);
-    load_tile(kq, kd, next);
-    wave_lds_sync();
-    floatx4 a16[HS];
-#pragma unroll
-    for (int hs = 0; hs < HS; ++hs) a16[hs] = zero4;
-#define RDKV_ROWS_K(I_)                                                                                              \
-  {                                                                                                                 \
-    const uint4 kr = *reinterpret_cast<const uint4*>(s_stage + lane * kRowStride + 16 * (I_));                      \
-    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) {                                                             \
-      a16[hs] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(bf4(qa[hs].x, qa[hs].y), bf4(kr.x, kr.y), a16[hs], 4, I_, 0); \
-      a16[hs] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(bf4(qa[hs].z, qa[hs].w), bf4(kr.z, kr.w), a16[hs], 4, I_, 0); \
-    }                                                                                                               \
-  }
-    RDKV_ROWS_K(0) RDKV_ROWS_K(1) RDKV_ROWS_K(2) RDKV_ROWS_K(3) RDKV_ROWS_K(4) RDKV_ROWS_K(5) RDKV_ROWS_K(6)
-    RDKV_ROWS_K(7) RDKV_ROWS_K(8) RDKV_ROWS_K(9) RDKV_ROWS_K(10) RDKV_ROWS_K(11) RDKV_ROWS_K(12) RDKV_ROWS_K(13)
-    RDKV_ROWS_K(14) RDKV_ROWS_K(15)
-#undef RDKV_ROWS_K
-    float xt[HS][4], x[HS][4];
+  if constexpr (kQueryInLds) {
+    if (threadIdx.x < 128) *reinterpret_cast<uint4*>(s_query + (threadIdx.x >> 4) * kRowStride + 16 * (threadIdx.x & 15)) = q_row;
+    __syncthreads();
+  } else {
 #pragma unroll
     for (int hs = 0; hs < HS; ++hs)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) xt[hs][i] = a16[hs][i];
+      for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(qa[hs][i].x), "+v"(qa[hs][i].y), "+v"(qa[hs][i].z), "+v"(qa[hs][i].w));
+  }
+  const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
+  for (int tile = t0 + wave; tile < t1; tile += NWV) {
+    const int next = tile + NWV;
+    float xt[HS][4], x[HS][4];
+    const int pos_now = pos;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      store_half(kq, half);
+      if (half == 1) {
+        __builtin_amdgcn_sched_barrier(0);     // (the next rows into the same registers)
+        pos = position(sc, next, t1);
+        load_tile(kq, kd, next);
+      }
+      wave_lds_sync();
+      floatx4 d[2][HS];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint4 k[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) k[b] = *reinterpret_cast<const uint4*>(s_stage + (16 * b + lc) * kRowStride + 64 * i + 16 * lr);
+#pragma unroll
+        for (int hs = 0; hs < HS; ++hs) {
+          if constexpr (kQueryInLds) qa[hs][i] = *reinterpret_cast<const uint4*>(s_query + (4 * hs + j) * kRowStride + 64 * i + 16 * lr);
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+            d[b][hs] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, qa[hs][i]), __builtin_bit_cast(Bf8, k[b]), i == 0 ? zero4 : d[b][hs], 0, 0, 0);
+        }
+      }
+      wave_lds_sync();
+#pragma unroll
+      for (int hs = 0; hs < HS; ++hs)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = (lr & 1) ? d[1][hs][i] : d[0][hs][i];
+          xt[hs][i] = half == 0 || !(lr & 2) ? (half == 0 ? v : xt[hs][i]) : v;
+        }
+    }
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, kRoot, xt);
-    store_scores<HS>(sc, tile, xt);
+    held.put<HS, NWV>(sc, tile, next >= t1, xt);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
     softmax_step<HS>(x, run, p, 0.f);
@@ -341,12 +373,16 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
       for (int i = 0; i < 16; ++i)
         if (!((seen >> (4 * i + lr)) & 1)) vq[i] = make_uint4(0, 0, 0, 0);
     }
-    wave_lds_sync();                    // every lane is done with the K rows
-    store_tile(vq);
+    store_half(vq, 0);
+    wave_lds_sync();
+    pv_rows<0, HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 8>{});
+    wave_lds_sync();
+    store_half(vq, 1);
+    __builtin_amdgcn_sched_barrier(0);
     load_tile(vq, vd, next);
     wave_lds_sync();
-    pv_rows<HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 16>{});
-    wave_lds_sync();                    // before the next tile's K rows overwrite the region
+    pv_rows<8, HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 8>{});
+    wave_lds_sync();                    // before the next rows overwrite the region
   }
 }
 
@@ -388,10 +424,7 @@ __device__ __forceinline__ int exponent_of(float x) {      // of a number > 0; b
 
 template <int HS, int NWV, bool STREAM>
 __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
-                                               const Scoring& sc, int t0, int t1, uint8_t* s_held, Run<HS>& run) {
-  constexpr bool kKeep = NWV == 8;       // for the end of the kernel
-  int held = 0;
-  const int most_held = kHeldBytes / (kTile * 4 * sc.g);
+                                               const Scoring& sc, int t0, int t1, Held& held, Run<HS>& run) {
   const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint4 qraw[HS];
@@ -401,16 +434,18 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   int pos;
   auto load_k = [&](int t) __attribute__((always_inline)) {      // (as in rows_segment: no bytes behind the last tile)
     const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(kd + static_cast<int64_t>(t) * kTileBytes), 0, t < t1 ? kTileBytes : 0, 0x00027000);
+    const int at = here(lane * 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) kr[i] = stream_load<STREAM>(tile, lane * 16 + 1024 * i);
-    kmeta = stream_load<STREAM>(tile, lane * 16 + 4096);
+    for (int i = 0; i < 4; ++i) kr[i] = stream_load<STREAM>(tile, at + 1024 * i);
+    kmeta = stream_load<STREAM>(tile, at + 4096);
     pos = position(sc, t, t1);
   };
   auto load_v = [&](int t) __attribute__((always_inline)) {
     const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(vd + static_cast<int64_t>(t) * kTileBytes), 0, t < t1 ? kTileBytes : 0, 0x00027000);
-    vmeta = stream_load<STREAM>(tile, lane * 16 + 4096);
+    const int at = here(lane * 16);
+    vmeta = stream_load<STREAM>(tile, at + 4096);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vr[i] = stream_load<STREAM>(tile, lane * 16 + 1024 * i);
+    for (int i = 0; i < 4; ++i) vr[i] = stream_load<STREAM>(tile, at + 1024 * i);
   };
   load_k(t0 + wave);
   load_v(t0 + wave);
@@ -507,13 +542,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     }
     load_k(next);
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
-    if (sc.tracked) {
-      hold_scores<HS>(sc, held++, xt, s_held);
-      if (!kKeep && (held == most_held || next >= t1)) {
-        flush_scores<HS>(sc, tile, NWV, held, s_held);
-        held = 0;
-      }
-    }
+    held.put<HS, NWV>(sc, tile, next >= t1, xt);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
     softmax_step<HS>(x, run, p, kPUp);
@@ -693,12 +722,15 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
   } else {
     end = tiles_of(a.s, item);
   }
-  // LDS: the wavefronts' staging regions or held scores, which the accumulators' area [NWV][g][128] shares unless they are kept; then the
-  // wavefronts' maxima and sums, and the heads' log-sum-exps
-  constexpr bool kKeep = BITS == 4 && NWV == 8;
-  const int wave_bytes = BITS == 16 ? kStageBytes : kKeep ? a.held_bytes : kHeldBytes;
-  float* s_acc = reinterpret_cast<float*>(smem + (kKeep ? NWV * wave_bytes : 0));
-  float* s_ml = kKeep ? s_acc + NWV * g * kHeadDim : reinterpret_cast<float*>(smem + NWV * wave_bytes);
+  // LDS: the wavefronts' staging regions; their scores; the accumulators' area [NWV][g][128], which is the staging regions' memory, or the
+  // scores' unless they are kept; the wavefronts' maxima and sums, and the heads' log-sum-exps
+  constexpr bool kKeep = NWV == 8, kOwnAcc = BITS == 4 && kKeep;
+  const int held_bytes = kKeep ? a.held_bytes : held_bytes_of_four(BITS);
+  uint8_t* s_stage = smem + wave * kHalfBytes;
+  uint8_t* s_held = smem + (BITS == 16 ? NWV * kHalfBytes : 0);
+  uint8_t* s_end = s_held + NWV * held_bytes;
+  float* s_acc = reinterpret_cast<float*>(kOwnAcc ? s_end : smem);
+  float* s_ml = reinterpret_cast<float*>(s_end) + (kOwnAcc ? NWV * g * kHeadDim : 0);
   float* s_lse = s_ml + ml_floats<NWV, HS>();
   while (at < end) {
     const int n = a.s.length(item), tiles = (n + kTile - 1) / kTile;
@@ -733,15 +765,15 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     Run<HS> run;
     init(run);
     float scale = 1.f;
+    Held held{s_held + wave * held_bytes, 0, kKeep ? 0 : held_bytes / (kTile * 4 * g)};
     if constexpr (BITS == 16) {
       const int64_t base = static_cast<int64_t>(item) * a.s.capacity * (kHeadDim * 2);
-      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, smem + wave * kStageBytes, run);
-      __syncthreads();                   // the staging regions become the accumulator area
+      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, s_stage, reinterpret_cast<uint8_t*>(s_lse + 8), held, run);
     } else {
       const int64_t base = static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
-      scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, smem + wave * wave_bytes, run);
-      if constexpr (!kKeep) __syncthreads();      // the held scores' memory becomes the accumulator area
+      scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, held, run);
     }
+    if constexpr (!kOwnAcc) __syncthreads();      // staging regions or scores become the accumulators' area
     // ---- the wavefronts' results into LDS ------------------------------------------------------------------------------
 #pragma unroll
     for (int hs = 0; hs < HS; ++hs) {
@@ -811,8 +843,8 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     }
     __syncthreads();
     if (kKeep && a.s.weight != nullptr) {
-      add_held<HS, NWV>(a.s, item, reinterpret_cast<const float*>(smem + wave * wave_bytes), s_lse, n, wave, tiles);
-    } else if (whole && a.s.weight != nullptr) {
+      add_held<HS, NWV>(a.s, item, reinterpret_cast<const float*>(held.at), s_lse, n, wave, tiles);
+    } else if (!kKeep && whole && a.s.weight != nullptr) {
       if (HS == 2) add_weights<8>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
       else if (g == 4) add_weights<4>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
       else if (g == 2) add_weights<2>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
@@ -892,6 +924,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
 }
 
 constexpr size_t kMostLds = 160 << 10;
+// LDS of a workgroup of eight wavefronts that keep `held` bytes of scores each
+size_t lds_of_eight(int bits, int g, size_t held) {
+  return 8 * (held + (bits == 16 ? kHalfBytes : g * kHeadDim * sizeof(float))) + (ml_lds_floats(8, g > 4 ? 2 : 1) + 8) * sizeof(float) +
+         (bits == 16 && g > 4 ? kQueryBytes : 0);
+}
 struct Plan {
   bool stream;         // rows past the caches' order
   int waves, groups, least, score_rows, join_rows, held_bytes;
@@ -906,7 +943,7 @@ Plan make_plan(int64_t items, int g, int capacity, int bits, bool weights) {
   p.waves = 8;
   // scores that a wavefront keeps, where a workgroup has an item's tiles
   const size_t held = weights ? (tiles + p.waves - 1) / p.waves * kTile * g * sizeof(float) : 0;
-  const bool fits = bits == 4 && p.waves * (held + g * kHeadDim * sizeof(float)) + (ml_lds_floats(p.waves, g > 4 ? 2 : 1) + 8) * sizeof(float) <= kMostLds;
+  const bool fits = lds_of_eight(bits, g, held) <= kMostLds;
   p.held_bytes = fits ? static_cast<int>(held) : 0;
   if (tiles <= 3 * p.waves || (fits && items >= 192)) {
     p.least = p.join_rows = 0;
@@ -929,13 +966,13 @@ Plan make_plan(int64_t items, int g, int capacity, int bits, bool weights) {
 
 template <int BITS, int HS, int NWV, bool STREAM>
 hipError_t launch_one(const DecodeArgs& a, const Plan& p, hipStream_t st) {
-  constexpr bool kKeep = BITS == 4 && NWV == 8;
-  constexpr size_t kEnd = (ml_floats<NWV, HS>() + 8) * sizeof(float);
-  const size_t wave = BITS == 16 ? kStageBytes : kKeep ? a.held_bytes + a.s.g * kHeadDim * sizeof(float) : kHeldBytes;
-  static_assert(kHeldBytes >= 4 * HS * kHeadDim * 4, "the accumulators fit");
-  const hipError_t e = RDKV_ALLOW_LDS((decode_kernel<BITS, HS, NWV, STREAM>), kKeep ? kMostLds : NWV * wave + kEnd);
+  const size_t lds = NWV == 8 ? lds_of_eight(BITS, a.s.g, a.held_bytes)
+                              : NWV * ((BITS == 16 ? kHalfBytes : 0) + held_bytes_of_four(BITS)) + (ml_floats<NWV, HS>() + 8) * sizeof(float) +
+                                    (BITS == 16 && HS == 2 ? kQueryBytes : 0);
+  static_assert(held_bytes_of_four(4) >= 4 * HS * kHeadDim * 4 && kHalfBytes >= 4 * HS * kHeadDim * 4, "the accumulators fit");
+  const hipError_t e = RDKV_ALLOW_LDS((decode_kernel<BITS, HS, NWV, STREAM>), NWV == 8 ? kMostLds : lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((decode_kernel<BITS, HS, NWV, STREAM>), dim3(p.groups), dim3(NWV * 64), NWV * wave + kEnd, st, a);
+  hipLaunchKernelGGL((decode_kernel<BITS, HS, NWV, STREAM>), dim3(p.groups), dim3(NWV * 64), lds, st, a);
   return hipGetLastError();
 }
 
