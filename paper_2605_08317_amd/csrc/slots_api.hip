@@ -75,6 +75,29 @@ rdkv_status check_prompts(const rdkv_slots* s, int32_t n, const int32_t* seq_len
   return RDKV_OK;
 }
 
+// What the launches of a fill's selection have in the workspace, one group of sequences after the other: the largest group's.
+struct SelectBytes { size_t counts, open, part, found, total; };
+SelectBytes select_bytes(const rdkv_slots* s, int32_t n, const int32_t* seq_lens) {
+  SelectBytes b{};
+  for (int s0 = 0; s0 < n; s0 += slots::kFillSeqs) {
+    const int ns = std::min(slots::kFillSeqs, n - s0);
+    int64_t rows = 0, longest = 0;
+    for (int i = 0; i < ns; ++i) {
+      rows += static_cast<int64_t>(seq_lens[s0 + i]) * s->hkv;
+      longest = std::max<int64_t>(longest, seq_lens[s0 + i]);
+    }
+    const slots::SelectPlan p = slots::plan_select(longest);
+    if (p.parts == 0 || longest <= s->capacity) continue;
+    const size_t items = static_cast<size_t>(ns) * s->hkv, parts = items * p.parts;
+    b.counts = std::max(b.counts, parts * slots::kSelectDigits * sizeof(uint16_t));
+    b.open = std::max(b.open, (static_cast<size_t>(rows) * sizeof(uint32_t) + 15) / 16 * 16);
+    b.part = std::max(b.part, (parts * sizeof(int2) + 15) / 16 * 16);
+    b.found = std::max(b.found, items * sizeof(int4));
+  }
+  b.total = b.counts + b.open + b.part + b.found;
+  return b;
+}
+
 }  // namespace
 
 extern "C" {
@@ -98,7 +121,7 @@ size_t rdkv_slots_side_bytes(const rdkv_slots* s) {
 size_t rdkv_slots_fill_workspace_bytes(const rdkv_slots* s, int32_t n, const int32_t* seq_lens) {
   int32_t longest;
   if (check_slots(s, false) != RDKV_OK || check_prompts(s, n, seq_lens, &longest) != RDKV_OK) return 0;
-  return 0;
+  return select_bytes(s, n, seq_lens).total;
 }
 
 rdkv_status rdkv_slots_fill(const rdkv_slots* s, int32_t first, int32_t n, const int32_t* seq_lens, const void* K, const void* V,
@@ -113,9 +136,9 @@ rdkv_status rdkv_slots_fill(const rdkv_slots* s, int32_t first, int32_t n, const
   if (longest > 0 && (!K || !V)) return fail(RDKV_ERR_INVALID_ARG, "K and V must not be null");
   if (longest > s->capacity && !w_tok)
     return fail(RDKV_ERR_INVALID_ARG, "a prompt of %d tokens for %d slots needs w_tok", longest, s->capacity);
-  const size_t need = rdkv_slots_fill_workspace_bytes(s, n, seq_lens);
-  if (need > 0 && (!workspace || workspace_bytes < need))
-    return fail(RDKV_ERR_INVALID_ARG, "workspace of %zu bytes is smaller than the %zu required", workspace ? workspace_bytes : 0, need);
+  const SelectBytes need = select_bytes(s, n, seq_lens);
+  if (need.total > 0 && (!workspace || workspace_bytes < need.total))
+    return fail(RDKV_ERR_INVALID_ARG, "workspace of %zu bytes is smaller than the %zu required", workspace ? workspace_bytes : 0, need.total);
   if (!aligned16({K, V, workspace})) return fail(RDKV_ERR_INVALID_ARG, "K, V and workspace must be aligned to 16 bytes");
   int64_t row = 0;
   for (int s0 = 0; s0 < n; s0 += slots::kFillSeqs) {
@@ -126,12 +149,22 @@ rdkv_status rdkv_slots_fill(const rdkv_slots* s, int32_t first, int32_t n, const
     a.V = static_cast<const uint16_t*>(V);
     a.w_tok = w_tok;
     a.seq0 = first + s0;
+    int32_t most = 0;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    a.counts = reinterpret_cast<uint16_t*>(ws);
+    a.open = reinterpret_cast<uint32_t*>(ws + need.counts);
+    a.part = reinterpret_cast<int2*>(ws + need.counts + need.open);
+    a.found = reinterpret_cast<int4*>(ws + need.counts + need.open + need.part);
     for (int i = 0; i < ns; ++i) {
+      most = std::max(most, seq_lens[s0 + i]);
       a.T[i] = seq_lens[s0 + i];
       a.row0[i] = row;
       row += static_cast<int64_t>(seq_lens[s0 + i]) * s->hkv;
     }
-    RDKV_HIP(slots::launch_fill(a, ns, s->bits, static_cast<hipStream_t>(stream)));
+    const slots::SelectPlan plan = slots::plan_select(most);
+    a.parts = plan.parts;
+    a.part_rows = plan.part_rows;
+    RDKV_HIP(slots::launch_fill(a, ns, most, s->bits, static_cast<hipStream_t>(stream)));
   }
   return RDKV_OK;
 }

@@ -9,10 +9,11 @@ namespace {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 
-// Sums over the threads below this one (x0, x1: this thread's own), and over all of them.
+// Sums over the threads below this one; x0, x1: this thread's own.
+template <int WAVES>
 struct Scan {
-  uint32_t s_wave[2][kSelectWaves];
-  __device__ __forceinline__ void run(uint32_t x0, uint32_t x1, uint32_t& below0, uint32_t& below1, uint32_t& all0) {
+  uint32_t s_wave[2][WAVES];
+  __device__ __forceinline__ void run(uint32_t x0, uint32_t x1, uint32_t& below0, uint32_t& below1) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t up0 = wave_scan(x0), up1 = wave_scan(x1);
     __syncthreads();
@@ -23,85 +24,96 @@ struct Scan {
     __syncthreads();
     below0 = up0 - x0;
     below1 = up1 - x1;
-    all0 = 0;
 #pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) {
-      const uint32_t a = s_wave[0][w], b = s_wave[1][w];
+    for (int w = 0; w < WAVES; ++w)
       if (w < wave) {
-        below0 += a;
-        below1 += b;
+        below0 += s_wave[0][w];
+        below1 += s_wave[1][w];
       }
-      all0 += a;
-    }
   }
 };
 
-// Which tokens of an item stay: their positions and weights into the slots.  Weights become unsigned numbers of the same order, with
-// sinks and recent tokens above all; the capacity's largest stay, found digit by digit from the highest (radix selection: 11, 11 and
-// 10 bits), the first of equal ones before the later.  One workgroup an item, its weights in the threads' registers.
-// A pass counts digits in LDS, with four counters a digit that lanes take in turn: weights share their few exponents, and lanes on one
-// counter wait for each other.  Bound: one compute unit's loads and atomics.
-// REGS: weights a thread holds; WHOLE: they are all of the item, otherwise every pass goes through it in blocks.
-constexpr int kCopies = 4, kDigits = 2048;
-template <int REGS, bool WHOLE>
-__global__ __launch_bounds__(kSelectThreads) void fill_select_kernel(FillArgs a) {
-  constexpr int kBlock = REGS * kSelectThreads, kEntries = REGS * kSelectWaves;
-  static_assert(kEntries <= kSelectThreads && 3 * kEntries <= kDigits * kCopies, "an entry a thread");
-  __shared__ uint32_t s_hist[kDigits * kCopies];          // later what stays of (register, wavefront), and sums before it
-  __shared__ Scan s_scan;
-  __shared__ uint32_t s_found[2];
-  const int head = blockIdx.x, sl = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int T = a.T[sl], cap = a.s.capacity;
-  const int64_t item = static_cast<int64_t>(a.seq0 + sl) * a.s.hkv + head;
-  const float* w = a.w_tok ? a.w_tok + a.row0[sl] + static_cast<int64_t>(head) * T : nullptr;
-  int32_t* pos = a.s.pos + item * cap;
-  float* weight = a.s.weight ? a.s.weight + item * cap : nullptr;
-  if (tid == 0) {
+// An item of a fill: its prompt's weights as numbers to select by.
+struct Prompt {
+  int T, cap, lo, hi;
+  const float* w;
+  int32_t* pos;
+  float* weight;
+  __device__ __forceinline__ Prompt(const FillArgs& a, int head, int sl) {
+    T = a.T[sl];
+    cap = a.s.capacity;
+    const int64_t item = static_cast<int64_t>(a.seq0 + sl) * a.s.hkv + head;
+    w = a.w_tok ? a.w_tok + a.row0[sl] + static_cast<int64_t>(head) * T : nullptr;
+    pos = a.s.pos + item * cap;
+    weight = a.s.weight ? a.s.weight + item * cap : nullptr;
+    lo = a.s.sinks;
+    hi = T - a.s.recent;
+  }
+  // sinks and recent tokens above every weight
+  __device__ __forceinline__ uint32_t key(int t, float x) const { return t < lo || t >= hi ? 0xFFFFFFFFu : weight_key(x); }
+  __device__ __forceinline__ void lengths(const FillArgs& a, int head, int sl) const {
+    const int64_t item = static_cast<int64_t>(a.seq0 + sl) * a.s.hkv + head;
     a.s.len[item] = min(T, cap);
     a.s.next[item] = T;
   }
-  if (T <= cap) {
-    for (int t = tid; t < T; t += kSelectThreads) {
+  // tokens first, first + step, .. below `end` of a prompt that stays whole
+  __device__ __forceinline__ void keep_all(int first, int end, int step) const {
+    for (int t = first; t < end; t += step) {
       pos[t] = t;
       if (weight) weight[t] = w ? w[t] : 0.f;
     }
+  }
+  __device__ __forceinline__ void keep(int at, int t, float x) const {      // x: w[t]
+    pos[at] = t;
+    if (weight) weight[at] = x;
+  }
+};
+
+// Which tokens of an item stay: their positions and weights into the slots.  Weights become unsigned numbers of the same order; the
+// capacity's largest stay, found digit by digit from the highest (radix selection: 11, 11 and 10 bits), the first of equal ones before the
+// later.
+//
+// Short prompts: one workgroup an item, its weights in the threads' registers.  A pass counts digits in LDS, with four counters a digit
+// that lanes take in turn: weights share their few exponents, and lanes on one counter wait for each other.  Bound: latency.
+constexpr int kCopies = 4, kDigits = kSelectDigits;
+template <int REGS>      // prompts of up to REGS kSelectThreads tokens, and those that stay whole
+__global__ __launch_bounds__(kSelectThreads) void fill_select_kernel(FillArgs a) {
+  constexpr int kEntries = REGS * kSelectWaves;
+  static_assert(kEntries <= kSelectThreads && 3 * kEntries <= kDigits * kCopies, "an entry a thread");
+  __shared__ uint32_t s_hist[kDigits * kCopies];          // later what stays of (register, wavefront), and sums before it
+  __shared__ Scan<kSelectWaves> s_scan;
+  __shared__ uint32_t s_found[2];
+  const int head = blockIdx.x, sl = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Prompt it(a, head, sl);
+  const int T = it.T;
+  if (tid == 0) it.lengths(a, head, sl);
+  if (T <= it.cap) {
+    it.keep_all(tid, T, kSelectThreads);
     return;
   }
-  const int lo = a.s.sinks, hi = T - a.s.recent;
-  uint32_t keys[REGS];                                    // token t0 + i kSelectThreads + tid
-  const auto load = [&](int t0) __attribute__((always_inline)) {
-    float x[REGS];
+  uint32_t keys[REGS];                                    // token i kSelectThreads + tid
+  float x[REGS];
 #pragma unroll
-    for (int i = 0; i < REGS; ++i) x[i] = w[min(t0 + i * kSelectThreads + tid, T - 1)];
+  for (int i = 0; i < REGS; ++i) x[i] = it.w[min(i * kSelectThreads + tid, T - 1)];
 #pragma unroll
-    for (int i = 0; i < REGS; ++i) {
-      const int t = t0 + i * kSelectThreads + tid;
-      keys[i] = t < lo || t >= hi ? 0xFFFFFFFFu : weight_key(x[i]);
-    }
-  };
-  if constexpr (WHOLE) load(0);
-  uint32_t left = cap, border = 0;                        // how many stay of what is in question: keys that begin as border does
+  for (int i = 0; i < REGS; ++i) keys[i] = it.key(i * kSelectThreads + tid, x[i]);
+  uint32_t left = it.cap, border = 0;                     // how many stay of what is in question: keys that begin as border does
   const auto pass = [&](int shift, int bits, int above) __attribute__((always_inline)) {
     __syncthreads();
     for (int i = tid; i < kDigits * kCopies; i += kSelectThreads) s_hist[i] = 0;
     __syncthreads();
-    for (int t0 = 0; t0 < T; t0 += kBlock) {
-      if constexpr (!WHOLE) load(t0);
 #pragma unroll
-      for (int i = 0; i < REGS; ++i) {
-        if (t0 + i * kSelectThreads >= T) break;
-        if (t0 + i * kSelectThreads + tid < T && (above == 32 || (keys[i] >> above) == (border >> above)))
-          atomicAdd(&s_hist[((keys[i] >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
-      }
-    }
+    for (int i = 0; i < REGS; ++i)
+      if (i * kSelectThreads + tid < T && (above == 32 || (keys[i] >> above) == (border >> above)))
+        atomicAdd(&s_hist[((keys[i] >> shift) & ((1u << bits) - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
     __syncthreads();
     uint32_t n[2] = {0, 0};                               // of digits 2047 - 2 tid and the one below
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int c = 0; c < kCopies; ++c) n[e] += s_hist[(kDigits - 1 - 2 * tid - e) * kCopies + c];
-    uint32_t higher, unused0, unused1;
-    s_scan.run(n[0] + n[1], 0, higher, unused0, unused1);
+    uint32_t higher, unused;
+    s_scan.run(n[0] + n[1], 0, higher, unused);
     if (higher < left && left <= higher + n[0] + n[1]) {
       const int e = left > higher + n[0];
       s_found[0] = kDigits - 1 - 2 * tid - e;
@@ -115,50 +127,297 @@ __global__ __launch_bounds__(kSelectThreads) void fill_select_kernel(FillArgs a)
   pass(10, 11, 21);
   pass(0, 10, 10);
   // Their slots.  For every (register, wavefront), in the order of tokens: how many are above the border, how many at it
-  uint32_t sure_so_far = 0, ties_so_far = 0;
-  for (int t0 = 0; t0 < T; t0 += kBlock) {
-    if constexpr (!WHOLE) load(t0);
-    uint64_t sure, tie;
-    const auto vote = [&](int i) __attribute__((always_inline)) {
-      uint32_t k = keys[i];
-      asm volatile("" : "+v"(k));                         // (or both loops' votes are kept for the other)
-      const bool in = t0 + i * kSelectThreads + tid < T;
-      sure = __ballot(in && k > border);
-      tie = __ballot(in && k == border);
-    };
-    __syncthreads();
+  uint64_t sure, tie;
+  const auto vote = [&](int i) __attribute__((always_inline)) {
+    uint32_t k = keys[i];
+    asm volatile("" : "+v"(k));                           // (or both loops' votes are kept for the other)
+    const bool in = i * kSelectThreads + tid < T;
+    sure = __ballot(in && k > border);
+    tie = __ballot(in && k == border);
+  };
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < REGS; ++i) {
-      vote(i);
-      if (lane == 0) s_hist[i * kSelectWaves + wave] = static_cast<uint32_t>(__popcll(sure)) | static_cast<uint32_t>(__popcll(tie)) << 16;
-    }
-    __syncthreads();
-    const uint32_t mine = tid < kEntries ? s_hist[tid] : 0u;
-    uint32_t sure_before, ties_before, all_sure;
-    s_scan.run(mine & 0xFFFFu, mine >> 16, sure_before, ties_before, all_sure);
-    if (tid < kEntries) {
-      s_hist[kEntries + tid] = sure_so_far + sure_before;
-      s_hist[2 * kEntries + tid] = ties_so_far + ties_before;
-    }
-    if (tid == kSelectThreads - 1) s_found[0] = ties_so_far + ties_before + (mine >> 16);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < REGS; ++i) {
-      if (t0 + i * kSelectThreads >= T) break;
-      vote(i);
-      if ((sure | tie) == 0) continue;
-      const uint64_t under = (1ull << lane) - 1, me = 1ull << lane;
-      const uint32_t ties = s_hist[2 * kEntries + i * kSelectWaves + wave] + __popcll(tie & under);
-      const uint32_t at = s_hist[kEntries + i * kSelectWaves + wave] + __popcll(sure & under) + min(ties, left);
-      if ((sure & me) || ((tie & me) && ties < left)) {
-        const int t = t0 + i * kSelectThreads + tid;
-        pos[at] = t;
-        if (weight) weight[at] = w[t];
-      }
-    }
-    sure_so_far += all_sure;
-    ties_so_far = s_found[0];
+  for (int i = 0; i < REGS; ++i) {
+    vote(i);
+    if (lane == 0) s_hist[i * kSelectWaves + wave] = static_cast<uint32_t>(__popcll(sure)) | static_cast<uint32_t>(__popcll(tie)) << 16;
   }
+  __syncthreads();
+  const uint32_t mine = tid < kEntries ? s_hist[tid] : 0u;
+  uint32_t sure_before, ties_before;
+  s_scan.run(mine & 0xFFFFu, mine >> 16, sure_before, ties_before);
+  if (tid < kEntries) {
+    s_hist[kEntries + tid] = sure_before;
+    s_hist[2 * kEntries + tid] = ties_before;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < REGS; ++i) {
+    if (i * kSelectThreads >= T) break;
+    vote(i);
+    const uint64_t under = (1ull << lane) - 1, me = 1ull << lane;
+    const uint32_t ties = s_hist[2 * kEntries + i * kSelectWaves + wave] + __popcll(tie & under);
+    const uint32_t at = s_hist[kEntries + i * kSelectWaves + wave] + __popcll(sure & under) + min(ties, left);
+    if ((sure & me) || ((tie & me) && ties < left)) it.keep(at, i * kSelectThreads + tid, x[i]);
+  }
+}
+
+// Long prompts: an item in parts, a workgroup each, in three launches.  count: a part's weights by their first digit.  open: every part
+// adds up the counts of all, finds the digit at the border, and puts its weights at that digit into a list of the item's, in the order of
+// tokens.  place: every part goes through the list, some hundredths of the weights, for the other two digits, and knows from it what the
+// parts before it keep.  Bound: latency of three launches; 4 bytes a token twice.
+// (One workgroup an item took 32 us for 8 items of 32K tokens and 128 for 128K.)
+constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPartEach = 16, kPartBlock = kPartThreads * kPartEach;
+
+struct PartOf {
+  int g, head, sl, tid, t0, t1;       // part of the item; its tokens
+  int64_t local;                      // item of the launch
+  __device__ __forceinline__ PartOf(const FillArgs& a) {
+    g = blockIdx.x;
+    head = blockIdx.y;
+    sl = blockIdx.z;
+    tid = threadIdx.x;
+    local = static_cast<int64_t>(sl) * a.s.hkv + head;
+    t0 = g * a.part_rows;
+    t1 = t0 + min(a.part_rows, a.T[sl] - t0);      // (t0, if there are none)
+  }
+};
+// weights of tokens t + i kPartThreads + tid (t < t1), and their keys
+__device__ __forceinline__ void load_weights(const Prompt& it, int t, int t1, int tid, float (&x)[kPartEach]) {
+#pragma unroll
+  for (int i = 0; i < kPartEach; ++i) x[i] = it.w[min(t + i * kPartThreads + tid, t1 - 1)];
+}
+__device__ __forceinline__ void make_keys(const Prompt& it, int t, int tid, const float (&x)[kPartEach], uint32_t (&keys)[kPartEach]) {
+#pragma unroll
+  for (int i = 0; i < kPartEach; ++i) keys[i] = it.key(t + i * kPartThreads + tid, x[i]);
+}
+// sums over (i, wavefront) entries before each, of packed pairs of 16 bits (a block has 4096 tokens); s_entries: kPartEach x kPartWaves
+__device__ __forceinline__ void scan_entries(uint2* s_entries, uint2* all) {
+  static_assert(kPartEach * kPartWaves == 64, "an entry a lane");
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const uint2 x = s_entries[threadIdx.x];
+    const uint2 up = make_uint2(wave_scan(x.x), wave_scan(x.y));
+    s_entries[threadIdx.x] = make_uint2(up.x - x.x, up.y - x.y);
+    if (threadIdx.x == 63) *all = up;
+  }
+  __syncthreads();
+}
+
+__global__ __launch_bounds__(kPartThreads) void select_count_kernel(FillArgs a) {
+  __shared__ uint32_t s_hist[kDigits * kCopies];
+  const PartOf p(a);
+  const Prompt it(a, p.head, p.sl);
+  if (p.g == 0 && p.tid == 0) it.lengths(a, p.head, p.sl);
+  if (p.t0 >= it.T) return;
+  if (it.T <= it.cap) {
+    it.keep_all(p.t0 + p.tid, p.t1, kPartThreads);
+    return;
+  }
+  for (int i = p.tid; i < kDigits * kCopies; i += kPartThreads) s_hist[i] = 0;
+  __syncthreads();
+  for (int t = p.t0; t < p.t1; t += kPartBlock) {
+    float x[kPartEach];
+    uint32_t keys[kPartEach];
+    load_weights(it, t, p.t1, p.tid, x);
+    make_keys(it, t, p.tid, x, keys);
+#pragma unroll
+    for (int i = 0; i < kPartEach; ++i)
+      if (t + i * kPartThreads + p.tid < p.t1) atomicAdd(&s_hist[(keys[i] >> 21) * kCopies + (p.tid & (kCopies - 1))], 1u);
+  }
+  __syncthreads();
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.counts + (p.local * a.parts + p.g) * kDigits);
+  for (int i = p.tid; i < kDigits / 2; i += kPartThreads) {
+    uint32_t n[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int c = 0; c < kCopies; ++c) n[e] += s_hist[(2 * i + e) * kCopies + c];
+    out[i] = n[0] | n[1] << 16;
+  }
+}
+
+// The digit (a thread has PER of them, the highest first: digits first - k) in which the `left` largest end; n: their counts.
+template <int PER>
+__device__ __forceinline__ uint2 find_digit(Scan<kPartWaves>& scan, uint2* s_found, uint32_t left, int first, const uint32_t (&n)[PER]) {
+  uint32_t sum = 0, higher, unused;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) sum += n[k];
+  scan.run(sum, 0, higher, unused);
+  if (higher < left && left <= higher + sum) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      if (higher < left && left <= higher + n[k]) *s_found = make_uint2(first - k, left - higher);
+      higher += n[k];
+    }
+  }
+  __syncthreads();
+  return *s_found;
+}
+
+__global__ __launch_bounds__(kPartThreads) void select_open_kernel(FillArgs a) {
+  __shared__ Scan<kPartWaves> s_scan;
+  __shared__ uint2 s_found, s_all, s_entries[kPartEach * kPartWaves];
+  __shared__ uint32_t s_sum[3];
+  const PartOf p(a);
+  const Prompt it(a, p.head, p.sl);
+  if (p.t0 >= it.T || it.T <= it.cap) return;
+  const int parts = (it.T + a.part_rows - 1) / a.part_rows, lane = p.tid & 63, wave = p.tid >> 6;
+  float x[kPartEach];                  // of the block; the first is under way during what comes before it
+  load_weights(it, p.t0, p.t1, p.tid, x);
+  const uint16_t* counts = a.counts + p.local * a.parts * kDigits;
+  // eight digits a thread, thread 0 the highest
+  constexpr int kPer = kDigits / kPartThreads;
+  static_assert(kPer == 8, "sixteen bytes of counts");
+  const int at = kDigits - kPer * (p.tid + 1);
+  uint32_t n[kPer], own[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) n[k] = own[k] = 0;
+#pragma unroll 8
+  for (int g = 0; g < parts; ++g) {
+    const uint4 c = *reinterpret_cast<const uint4*>(counts + static_cast<int64_t>(g) * kDigits + at);
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const uint32_t x = (w[3 - k / 2] >> (k % 2 ? 0 : 16)) & 0xFFFFu;
+      n[k] += x;
+      own[k] = g == p.g ? x : own[k];
+    }
+  }
+  if (p.tid < 3) s_sum[p.tid] = 0;
+  const uint2 f = find_digit<kPer>(s_scan, &s_found, it.cap, kDigits - 1 - kPer * p.tid, n);
+  const uint32_t digit = f.x;
+  uint32_t sure = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k)
+    if (static_cast<uint32_t>(kDigits - 1 - kPer * p.tid - k) > digit) sure += own[k];
+  uint32_t before = 0, all = 0;
+  for (int g = p.tid; g < parts; g += kPartThreads) {
+    const uint32_t x = counts[static_cast<int64_t>(g) * kDigits + digit];
+    all += x;
+    if (g < p.g) before += x;
+  }
+  if (sure) atomicAdd(&s_sum[0], sure);
+  if (before) atomicAdd(&s_sum[1], before);
+  if (all) atomicAdd(&s_sum[2], all);
+  __syncthreads();
+  before = s_sum[1];
+  if (p.tid == 0) {
+    a.part[p.local * a.parts + p.g] = make_int2(static_cast<int>(s_sum[0]), static_cast<int>(before));
+    if (p.g == 0) a.found[p.local] = make_int4(static_cast<int>(digit), static_cast<int>(f.y), static_cast<int>(s_sum[2]), 0);
+  }
+  uint32_t* list = a.open + (a.row0[p.sl] - a.row0[0]) + static_cast<int64_t>(p.head) * it.T;
+  for (int t = p.t0; t < p.t1; t += kPartBlock) {
+    uint32_t keys[kPartEach];
+    make_keys(it, t, p.tid, x, keys);
+    if (t + kPartBlock < p.t1) load_weights(it, t + kPartBlock, p.t1, p.tid, x);
+    uint64_t in[kPartEach];
+#pragma unroll
+    for (int i = 0; i < kPartEach; ++i) {
+      in[i] = __ballot(t + i * kPartThreads + p.tid < p.t1 && (keys[i] >> 21) == digit);
+      if (lane == 0) s_entries[i * kPartWaves + wave] = make_uint2(__popcll(in[i]), 0);
+    }
+    scan_entries(s_entries, &s_all);
+#pragma unroll
+    for (int i = 0; i < kPartEach; ++i)
+      if ((in[i] >> lane) & 1) list[before + s_entries[i * kPartWaves + wave].x + __popcll(in[i] & ((1ull << lane) - 1))] = keys[i];
+    before += s_all.x;
+    __syncthreads();
+  }
+}
+
+__global__ __launch_bounds__(kPartThreads) void select_place_kernel(FillArgs a) {
+  __shared__ uint32_t s_hist[kDigits];
+  __shared__ Scan<kPartWaves> s_scan;
+  __shared__ uint2 s_found, s_all, s_entries[kPartEach * kPartWaves];
+  __shared__ uint32_t s_sum[2];
+  const PartOf p(a);
+  const Prompt it(a, p.head, p.sl);
+  if (p.t0 >= it.T || it.T <= it.cap) return;
+  const int lane = p.tid & 63, wave = p.tid >> 6;
+  const int4 found = a.found[p.local];
+  const int2 own = a.part[p.local * a.parts + p.g];
+  const int open = found.z;
+  float x[kPartEach];                  // of the block; the first is under way during what comes before it
+  load_weights(it, p.t0, p.t1, p.tid, x);
+  uint32_t left = found.y, border = static_cast<uint32_t>(found.x) << 21;
+  const uint32_t* list = a.open + (a.row0[p.sl] - a.row0[0]) + static_cast<int64_t>(p.head) * it.T;
+  // the first of the list's weights stay with their threads
+  constexpr int kHold = 16;
+  uint32_t held[kHold];
+#pragma unroll
+  for (int i = 0; i < kHold; ++i) held[i] = list[min(i * kPartThreads + p.tid, open - 1)];
+  const auto each = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kHold; ++i)
+      if (i * kPartThreads + p.tid < open) f(held[i], i * kPartThreads + p.tid);
+    for (int i = kHold * kPartThreads + p.tid; i < open; i += kPartThreads) f(list[i], i);
+  };
+  constexpr int kPer = kDigits / kPartThreads;
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {
+    const int shift = pass == 0 ? 10 : 0, above = pass == 0 ? 21 : 10;
+    __syncthreads();
+    for (int i = p.tid; i < kDigits; i += kPartThreads) s_hist[i] = 0;
+    __syncthreads();
+    each([&](uint32_t k, int) {
+      if ((k >> above) == (border >> above)) atomicAdd(&s_hist[(k >> shift) & (pass == 0 ? 2047u : 1023u)], 1u);
+    });
+    __syncthreads();
+    uint32_t n[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) n[k] = s_hist[kDigits - 1 - kPer * p.tid - k];
+    const uint2 f = find_digit<kPer>(s_scan, &s_found, left, kDigits - 1 - kPer * p.tid, n);
+    border |= f.x << shift;
+    left = f.y;
+  }
+  // what the parts before keep: all above the border digit, and of the list's
+  if (p.tid < 2) s_sum[p.tid] = 0;
+  __syncthreads();
+  uint32_t sure = 0, ties = 0;
+  for (int g = p.tid; g < p.g; g += kPartThreads) sure += static_cast<uint32_t>(a.part[p.local * a.parts + g].x);
+  each([&](uint32_t k, int i) {
+    if (i < own.y) {
+      sure += k > border;
+      ties += k == border;
+    }
+  });
+  if (sure) atomicAdd(&s_sum[0], sure);
+  if (ties) atomicAdd(&s_sum[1], ties);
+  __syncthreads();
+  sure = s_sum[0];
+  ties = s_sum[1];
+  for (int t = p.t0; t < p.t1; t += kPartBlock) {
+    uint32_t keys[kPartEach];
+    if (t > p.t0) load_weights(it, t, p.t1, p.tid, x);
+    make_keys(it, t, p.tid, x, keys);
+    uint64_t more[kPartEach], same[kPartEach];
+#pragma unroll
+    for (int i = 0; i < kPartEach; ++i) {
+      const bool in = t + i * kPartThreads + p.tid < p.t1;
+      more[i] = __ballot(in && keys[i] > border);
+      same[i] = __ballot(in && keys[i] == border);
+      if (lane == 0) s_entries[i * kPartWaves + wave] = make_uint2(__popcll(more[i]), __popcll(same[i]));
+    }
+    scan_entries(s_entries, &s_all);
+    const uint64_t under = (1ull << lane) - 1, me = 1ull << lane;
+#pragma unroll
+    for (int i = 0; i < kPartEach; ++i) {
+      const uint2 b = s_entries[i * kPartWaves + wave];
+      const uint32_t tie = ties + b.y + __popcll(same[i] & under);
+      if ((more[i] & me) || ((same[i] & me) && tie < left)) 
+        it.keep(sure + b.x + __popcll(more[i] & under) + min(tie, left), t + i * kPartThreads + p.tid, x[i]);
+    }
+    sure += s_all.x;
+    ties += s_all.y;
+    __syncthreads();
+  }
+}
+
+// sixteen bytes of a prompt's row, which is read once
+__device__ __forceinline__ uint4 prompt_row(const uint16_t* rows, int64_t at) {
+  using Four = __attribute__((ext_vector_type(4))) uint32_t;
+  const Four v = __builtin_nontemporal_load(reinterpret_cast<const Four*>(rows) + at);
+  return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // bf16 rows: 16 lanes a row
@@ -168,8 +427,9 @@ __global__ __launch_bounds__(256) void fill_rows_kernel(FillArgs a) {
   const int i = blockIdx.x * 16 + (threadIdx.x >> 4), c = threadIdx.x & 15;
   if (i >= min(T, a.s.capacity)) return;
   const int64_t from = (src + a.s.pos[item * a.s.capacity + i]) * 16 + c, to = (item * a.s.capacity + i) * 16 + c;
-  reinterpret_cast<uint4*>(a.s.k)[to] = reinterpret_cast<const uint4*>(a.K)[from];
-  reinterpret_cast<uint4*>(a.s.v)[to] = reinterpret_cast<const uint4*>(a.V)[from];
+  const uint4 k = prompt_row(a.K, from), v = prompt_row(a.V, from);
+  reinterpret_cast<uint4*>(a.s.k)[to] = k;
+  reinterpret_cast<uint4*>(a.s.v)[to] = v;
 }
 
 // One tile of 64 slots in 4 bits, as the packing kernels quantize and lay out theirs: 16 lanes a row, four rows a lane.
@@ -226,8 +486,8 @@ __global__ __launch_bounds__(256) void fill_tiles_kernel(FillArgs a) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t from = (src + p[i]) * 16 + c16;
-    kq[i] = reinterpret_cast<const uint4*>(a.K)[from];
-    vq[i] = reinterpret_cast<const uint4*>(a.V)[from];
+    kq[i] = prompt_row(a.K, from);
+    vq[i] = prompt_row(a.V, from);
   }
   if (tile * kTileRows + kTileRows > n) {
 #pragma unroll
@@ -476,15 +736,18 @@ __global__ __launch_bounds__(256) void read_kernel(Args a, const int32_t* __rest
 
 }  // namespace
 
-hipError_t launch_fill(const FillArgs& a, int n_seqs, int bits, hipStream_t st) {
-  int most = 0;
-  for (int i = 0; i < n_seqs; ++i) most = a.T[i] > most ? a.T[i] : most;
-  const int n = most < a.s.capacity ? most : a.s.capacity;
-  const dim3 items(a.s.hkv, n_seqs), threads(kSelectThreads);
-  if (most <= 8 * kSelectThreads) hipLaunchKernelGGL((fill_select_kernel<8, true>), items, threads, 0, st, a);
-  else if (most <= 32 * kSelectThreads) hipLaunchKernelGGL((fill_select_kernel<32, true>), items, threads, 0, st, a);
-  else if (most <= 64 * kSelectThreads) hipLaunchKernelGGL((fill_select_kernel<64, true>), items, threads, 0, st, a);
-  else hipLaunchKernelGGL((fill_select_kernel<32, false>), items, threads, 0, st, a);
+hipError_t launch_fill(const FillArgs& a, int n_seqs, int longest, int bits, hipStream_t st) {
+  const int n = longest < a.s.capacity ? longest : a.s.capacity;
+  if (a.parts > 0) {
+    const dim3 grid(a.parts, a.s.hkv, n_seqs), threads(kPartThreads);
+    hipLaunchKernelGGL(select_count_kernel, grid, threads, 0, st, a);
+    if (longest > a.s.capacity) {
+      hipLaunchKernelGGL(select_open_kernel, grid, threads, 0, st, a);
+      hipLaunchKernelGGL(select_place_kernel, grid, threads, 0, st, a);
+    }
+  } else {
+    hipLaunchKernelGGL(fill_select_kernel<8>, dim3(a.s.hkv, n_seqs), dim3(kSelectThreads), 0, st, a);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 0) return e;
   if (bits == 16)
