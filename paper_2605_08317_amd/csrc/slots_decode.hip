@@ -87,6 +87,7 @@ __device__ __forceinline__ float capped(float s, float cap, float inv_cap) {
 // What a segment's wavefronts need to make scores of products.
 struct Scoring {
   int n, at;                     // slots in use; the query's position
+  int sure;                      // slots whose memory there is: a workgroup that has an item alone begins before it knows n
   int g, sinks, window;
   float cap, inv_cap;
   bool where;                    // positions matter
@@ -97,10 +98,11 @@ struct Scoring {
   float* scores;                 // of the item: [slot][g]
 };
 
-// the position of this lane's slot of a tile; 0 where there is none or positions do not matter
-__device__ __forceinline__ int position(const Scoring& sc, int tile, int t1) {
-  const int rows = sc.where && tile < t1 ? min(sc.n - tile * kTile, kTile) : 0;
-  const auto of = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(sc.pos + static_cast<int64_t>(tile) * kTile), 0, rows * 4, 0x00027000);
+// rows of a tile of an item with n
+__device__ __forceinline__ int rows_known(const Scoring& sc, int tile, int n) { return __builtin_amdgcn_readfirstlane(max(0, min(n - tile * kTile, kTile))); }
+// the position of this lane's slot of a tile that has `rows`; 0 where there is none or positions do not matter
+__device__ __forceinline__ int position(const Scoring& sc, int tile, int rows) {
+  const auto of = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(sc.pos + static_cast<int64_t>(tile) * kTile), 0, sc.where ? rows * 4 : 0, 0x00027000);
   return static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(of, 4 * (threadIdx.x & 63), 0, 0));
 }
 
@@ -278,13 +280,12 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
   // A tile is a buffer that ends with the item's last row, and what is behind it reads as zeros; behind the last tile it is empty.  (With
   // loads under a condition the compiler cannot count on them, and waits for all there are.)
   uint4 kq[16], vq[16];
-  const auto tile_at = [&](const uint8_t* base, int t) __attribute__((always_inline)) {
-    const int rows = t < t1 ? min(sc.n - t * kTile, kTile) : 0;
+  const auto tile_at = [&](const uint8_t* base, int t, int rows) __attribute__((always_inline)) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + static_cast<int64_t>(t) * (kTile * kHeadDim * 2)), 0, rows * (kHeadDim * 2),
                                              0x00027000);
   };
-  const auto load_tile = [&](uint4 (&st)[16], const uint8_t* base, int t) __attribute__((always_inline)) {
-    const auto tile = tile_at(base, t);
+  const auto load_tile = [&](uint4 (&st)[16], const uint8_t* base, int t, int rows) __attribute__((always_inline)) {
+    const auto tile = tile_at(base, t, rows);
     const int at = here(lane * 16);
 #pragma unroll
     for (int i = 0; i < 16; ++i) st[i] = stream_load<STREAM>(tile, at + i * 1024);
@@ -309,9 +310,10 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
 #pragma unroll
       for (int i = 0; i < 4; ++i) qa[hs][i] = query(hs, i);
   }
-  int pos = position(sc, t0 + wave, t1);
-  load_tile(kq, kd, t0 + wave);
-  load_tile(vq, vd, t0 + wave);
+  const int first_rows = rows_known(sc, t0 + wave, sc.sure);
+  int pos = position(sc, t0 + wave, first_rows);
+  load_tile(kq, kd, t0 + wave, first_rows);
+  load_tile(vq, vd, t0 + wave, first_rows);
   __builtin_amdgcn_sched_barrier(0);
   // the query is here before the loop: waited for inside, it would have every pass wait for all loads under way
   if constexpr (kQueryInLds) {
@@ -325,7 +327,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
   }
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
-    const int next = tile + NWV;
+    const int next = tile + NWV, next_rows = next < t1 ? rows_known(sc, next, sc.n) : 0;
     float xt[HS][4], x[HS][4];
     const int pos_now = pos;
 #pragma unroll
@@ -333,8 +335,8 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
       store_half(kq, half);
       if (half == 1) {
         __builtin_amdgcn_sched_barrier(0);     // (the next rows into the same registers)
-        pos = position(sc, next, t1);
-        load_tile(kq, kd, next);
+        pos = position(sc, next, next_rows);
+        load_tile(kq, kd, next, next_rows);
       }
       wave_lds_sync();
       floatx4 d[2][HS];
@@ -379,7 +381,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
     wave_lds_sync();
     store_half(vq, 1);
     __builtin_amdgcn_sched_barrier(0);
-    load_tile(vq, vd, next);
+    load_tile(vq, vd, next, next_rows);
     wave_lds_sync();
     pv_rows<8, HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 8>{});
     wave_lds_sync();                    // before the next rows overwrite the region
@@ -432,23 +434,24 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   for (int hs = 0; hs < HS; ++hs) qraw[hs] = load_query(q, 4 * hs + j, sc.g, blk);
   uint4 kr[4], vr[4], kmeta, vmeta;
   int pos;
-  auto load_k = [&](int t) __attribute__((always_inline)) {      // (as in rows_segment: no bytes behind the last tile)
-    const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(kd + static_cast<int64_t>(t) * kTileBytes), 0, t < t1 ? kTileBytes : 0, 0x00027000);
+  // (as in rows_segment: a tile that is there, or an empty one)
+  auto load_k = [&](int t, int rows) __attribute__((always_inline)) {
+    const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(kd + static_cast<int64_t>(t) * kTileBytes), 0, rows > 0 ? kTileBytes : 0, 0x00027000);
     const int at = here(lane * 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) kr[i] = stream_load<STREAM>(tile, at + 1024 * i);
     kmeta = stream_load<STREAM>(tile, at + 4096);
-    pos = position(sc, t, t1);
+    pos = position(sc, t, rows);
   };
-  auto load_v = [&](int t) __attribute__((always_inline)) {
-    const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(vd + static_cast<int64_t>(t) * kTileBytes), 0, t < t1 ? kTileBytes : 0, 0x00027000);
+  auto load_v = [&](int t, int rows) __attribute__((always_inline)) {
+    const auto tile = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(vd + static_cast<int64_t>(t) * kTileBytes), 0, rows > 0 ? kTileBytes : 0, 0x00027000);
     const int at = here(lane * 16);
     vmeta = stream_load<STREAM>(tile, at + 4096);
 #pragma unroll
     for (int i = 0; i < 4; ++i) vr[i] = stream_load<STREAM>(tile, at + 1024 * i);
   };
-  load_k(t0 + wave);
-  load_v(t0 + wave);
+  load_k(t0 + wave, rows_known(sc, t0 + wave, sc.sure));
+  load_v(t0 + wave, rows_known(sc, t0 + wave, sc.sure));
 
   // ---- query operands: times the power of two that puts the largest value of all heads near 2^kQUp ------------------
   half4 qop[HS][2], qhi[HS], qlo[HS];
@@ -504,7 +507,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
 
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
-    const int next = tile + NWV;
+    const int next = tile + NWV, next_rows = next < t1 ? rows_known(sc, next, sc.n) : 0;
     float xt[HS][4], x[HS][4];
     const int pos_now = pos;
     {
@@ -540,7 +543,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 #undef RDKV_K_GROUP
 #undef RDKV_K_STEP
     }
-    load_k(next);
+    load_k(next, next_rows);
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
     held.put<HS, NWV>(sc, tile, next >= t1, xt);
     to_head_lanes<HS, HS == 2>(xt, j, x);
@@ -612,7 +615,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     RDKV_PV_GROUP(0) RDKV_PV_GROUP(1) RDKV_PV_GROUP(2) RDKV_PV_GROUP(3)
 #undef RDKV_PV_GROUP
 #undef RDKV_PV_STEP
-    load_v(next);
+    load_v(next, next_rows);
   }
   // what brings the accumulators to the sums' scale: 2^18 of the codes, 2^(1 + ve) of vf
   return ldexpf(1.0f, 19 + ve);
@@ -669,17 +672,21 @@ __device__ __forceinline__ void add_weights(const Args& a, int64_t item, const f
 }
 
 // The same from scores that a wavefront has kept: tiles wave, wave + NWV, .. of an item.
+template <int NWV>
+__device__ __forceinline__ void held_weights(const Args& a, int64_t item, int n, int t0, float (&w)[4]) {      // of tiles t0, t0 + NWV, .. of n > 0 slots
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = a.weight[item * a.capacity + min((t0 + j * NWV) * kTile + static_cast<int>(threadIdx.x & 63), n - 1)];
+}
+// w: held_weights of the first tiles
 template <int HS, int NWV>
-__device__ __forceinline__ void add_held(const Args& a, int64_t item, const float* s_held, const float* lse2, int n, int wave, int tiles) {
+__device__ __forceinline__ void add_held(const Args& a, int64_t item, const float* s_held, const float* lse2, int n, int wave, int tiles, float (&w)[4]) {
   const int lane = threadIdx.x & 63;
   float* __restrict__ weight = a.weight + item * a.capacity;
   float l[4 * HS];
 #pragma unroll
   for (int h = 0; h < 4 * HS; ++h) l[h] = lse2[h < a.g ? h : 0];
   for (int t0 = wave, k = 0; t0 < tiles; t0 += 4 * NWV, k += 4) {
-    float w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = weight[min((t0 + j * NWV) * kTile + lane, n - 1)];
+    if (k > 0) held_weights<NWV>(a, item, n, t0, w);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int i = (t0 + j * NWV) * kTile + lane;
@@ -703,24 +710,22 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = a.s.g;
-  // items without a token have no tile: their outputs are the first workgroups' to write
-  for (int item = blockIdx.x; item < a.items; item += gridDim.x)
-    if (a.s.length(item) == 0) {
-      for (int i = tid; i < g * kHeadDim; i += NWV * 64) a.out[static_cast<int64_t>(item) * g * kHeadDim + i] = 0.f;
-      if (a.lse != nullptr && tid < g) a.lse[static_cast<int64_t>(item) * g + tid] = -INFINITY;
-      if (tid == 0 && a.least > 0) a.parts[item] = make_int2(0, 0);
-    }
-  // where on the line this workgroup is (or at its item)
-  int at = 0, end, first = 0, item = blockIdx.x, share = 0;
-  if (a.least > 0) {
+  // where on the line this workgroup is; a workgroup of eight wavefronts is at its item
+  int at = 0, end = 0, first = 0, item = blockIdx.x, share = 0;
+  if constexpr (NWV == 4) {
+    // items without a token have no tile: their outputs are the first workgroups' to write
+    for (int i = blockIdx.x; i < a.items; i += gridDim.x)
+      if (a.s.length(i) == 0) {
+        for (int k = tid; k < g * kHeadDim; k += NWV * 64) a.out[static_cast<int64_t>(i) * g * kHeadDim + k] = 0.f;
+        if (a.lse != nullptr && tid < g) a.lse[static_cast<int64_t>(i) * g + tid] = -INFINITY;
+        if (tid == 0) a.parts[i] = make_int2(0, 0);
+      }
     const Line line = make_line(a, gridDim.x);
     share = line.share;
     at = static_cast<int>(blockIdx.x) * share;
     if (at >= line.total) return;
     end = min(at + share, line.total);
     item = item_at(a, at, &first);
-  } else {
-    end = tiles_of(a.s, item);
   }
   // LDS: the wavefronts' staging regions; their scores; the accumulators' area [NWV][g][128], which is the staging regions' memory, or the
   // scores' unless they are kept; the wavefronts' maxima and sums, and the heads' log-sum-exps
@@ -732,19 +737,22 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
   float* s_acc = reinterpret_cast<float*>(kOwnAcc ? s_end : smem);
   float* s_ml = reinterpret_cast<float*>(s_end) + (kOwnAcc ? NWV * g * kHeadDim : 0);
   float* s_lse = s_ml + ml_floats<NWV, HS>();
-  while (at < end) {
-    const int n = a.s.length(item), tiles = (n + kTile - 1) / kTile;
-    const int t0 = at - first, t1 = min(tiles, end - first);
-    if (t1 <= t0) {                      // an item without tiles
+  do {
+    // (all the same for every lane, which buffers need to be known of)
+    item = __builtin_amdgcn_readfirstlane(item);
+    const int n = __builtin_amdgcn_readfirstlane(a.s.length(item)), tiles = (n + kTile - 1) / kTile;
+    const int t0 = __builtin_amdgcn_readfirstlane(at - first), t1 = NWV == 8 ? tiles : __builtin_amdgcn_readfirstlane(min(tiles, end - first));
+    if (NWV == 4 && t1 <= t0) {          // an item without tiles
       ++item;
       continue;
     }
-    const bool whole = t0 == 0 && t1 == tiles;
-    if (t0 == 0 && tid == 0 && a.least > 0)
+    const bool whole = NWV == 8 || (t0 == 0 && t1 == tiles);
+    if (NWV == 4 && t0 == 0 && tid == 0)
       a.parts[item] = whole ? make_int2(0, 0) : make_int2(static_cast<int>(blockIdx.x) + item, (first + tiles - 1) / share - static_cast<int>(blockIdx.x) + 1);
     Scoring sc;
     sc.n = n;
-    sc.at = a.s.next[item] - 1;
+    sc.sure = NWV == 8 ? a.s.capacity : n;
+    sc.at = __builtin_amdgcn_readfirstlane(a.s.next[item]) - 1;
     sc.g = g;
     sc.sinks = a.s.sinks;
     sc.window = a.s.window;
@@ -773,6 +781,8 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
       const int64_t base = static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
       scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, held, run);
     }
+    float w_first[4];
+    if (kKeep && n > 0 && a.s.weight != nullptr) held_weights<NWV>(a.s, item, n, wave, w_first);
     if constexpr (!kOwnAcc) __syncthreads();      // staging regions or scores become the accumulators' area
     // ---- the wavefronts' results into LDS ------------------------------------------------------------------------------
 #pragma unroll
@@ -843,7 +853,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     }
     __syncthreads();
     if (kKeep && a.s.weight != nullptr) {
-      add_held<HS, NWV>(a.s, item, reinterpret_cast<const float*>(held.at), s_lse, n, wave, tiles);
+      add_held<HS, NWV>(a.s, item, reinterpret_cast<const float*>(held.at), s_lse, n, wave, tiles, w_first);
     } else if (!kKeep && whole && a.s.weight != nullptr) {
       if (HS == 2) add_weights<8>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
       else if (g == 4) add_weights<4>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
@@ -856,7 +866,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
       first += tiles;
       ++item;
     }
-  }
+  } while (NWV == 4 && at < end);
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -924,6 +934,19 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
 }
 
 constexpr size_t kMostLds = 160 << 10;
+// Whether a workgroup takes an item alone (if its scores fit).  Then a compute unit's reading bounds a step, 6 us and for every tile 0.42
+// (bf16; 0.53 for 8 heads) or 0.31 (4 bits; 0.47), in as many turns as there are items for a compute unit.  Shared out, a step is two
+// launches, 13 us (16 for 8 heads; 4 bits 13.5 and 18), and bound by memory: 3.5 ns a tile in bf16, 2.4 in 4 bits.  Alone and shared, us:
+//   bf16, 4 heads     8 items of 500 slots  9.4, 14.6   of 1000  13.3, 16.5   of 2000  19.9, 14.6   32 of 1500  22.1, 17.1
+//                     64 of 1500  23.7, 22.9   of 4000  51, 40   128 of 4000  58, 63   256 of 4000  90, 114
+//   4 bits, 4 heads   8 of 1500  11.7, 12.6   of 2000  14.3, 13.0   64 of 3000  20.9, 23.4   of 4000  26, 23   256 of 8000  66, 85
+//   4 bits, 8 heads   8 of 1500  15.9, 16.7   of 2000  19.7, 17.8   128 of 3000  29.9, 38.0
+bool one_each(int64_t items, int g, int64_t tiles, int bits) {
+  const bool wide = g > 4;
+  const double own = bits == 16 ? (wide ? 0.53 : 0.42) : (wide ? 0.47 : 0.31), base = bits == 16 ? (wide ? 16.0 : 13.0) : (wide ? 18.0 : 13.5);
+  const double turns = static_cast<double>((items + 255) / 256);
+  return 6.0 + own * turns * static_cast<double>(tiles) <= base + (bits == 16 ? 0.0035 : 0.0024) * static_cast<double>(items) * static_cast<double>(tiles);
+}
 // LDS of a workgroup of eight wavefronts that keep `held` bytes of scores each
 size_t lds_of_eight(int bits, int g, size_t held) {
   return 8 * (held + (bits == 16 ? kHalfBytes : g * kHeadDim * sizeof(float))) + (ml_lds_floats(8, g > 4 ? 2 : 1) + 8) * sizeof(float) +
@@ -945,7 +968,7 @@ Plan make_plan(int64_t items, int g, int capacity, int bits, bool weights) {
   const size_t held = weights ? (tiles + p.waves - 1) / p.waves * kTile * g * sizeof(float) : 0;
   const bool fits = lds_of_eight(bits, g, held) <= kMostLds;
   p.held_bytes = fits ? static_cast<int>(held) : 0;
-  if (tiles <= 3 * p.waves || (fits && items >= 192)) {
+  if (fits && one_each(items, g, tiles, bits)) {
     p.least = p.join_rows = 0;
     p.groups = static_cast<int>(items);
     p.part_acc = p.part_ml = p.parts = 0;
