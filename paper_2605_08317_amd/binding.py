@@ -428,6 +428,13 @@ def rdkv_decode_attn_bf16_noalloc(K, V, seq_lens, hq, hkv, q, out, lse=None, hea
     return out, lse
 
 
+def _int32(name, x):
+    """A number that ctypes would otherwise cut to 32 bits."""
+    if not -2 ** 31 <= int(x) < 2 ** 31:
+        raise ValueError(f"{name} = {x} is no 32-bit number")
+    return int(x)
+
+
 class Slots:
     """A slot cache (rdkv_slots): its parameters and the device tensors that hold it, made here unless the caller brings them.
 
@@ -447,9 +454,7 @@ class Slots:
         c = self.c
         for name, x in (("batch", batch), ("hq", hq), ("hkv", hkv), ("head_dim", head_dim), ("capacity", capacity), ("bits", bits),
                         ("sinks", sinks), ("recent", recent), ("window", window)):
-            if not -2 ** 31 <= int(x) < 2 ** 31:
-                raise ValueError(f"{name} = {x} is no 32-bit number")
-            setattr(c, name, int(x))
+            setattr(c, name, _int32(name, x))
         c.score_cap, c.decay = float(score_cap), float(decay)
         c.k = c.v = c.pos = c.len = c.next = 16        # (what the library checks of memory is that there is some)
         _check(lib.rdkv_slots_read(ctypes.byref(c), None, 0, None, None, None))
@@ -495,6 +500,8 @@ def _tensor(t, shape, dtype, device, name):
 
 def _on(slots):
     """The slots' device as the current one."""
+    if slots.device.type != "cuda":
+        raise ValueError(f"the slots lie on {slots.device}: the calls on them run on a GPU")
     index = slots.device.index
     return _SAME if index is None or _current_device is None or _current_device() == index else torch.cuda.device(index)
 
@@ -513,8 +520,8 @@ _SAME = _Same()
 def rdkv_slots_fill(slots, K, V, seq_lens, w_tok=None, first=0):
     """Prompts of len(seq_lens) sequences into the slots of sequences first, first + 1, ..: K, V bfloat16, w_tok float32 or
     None, ragged as everywhere."""
-    n = len(seq_lens)
-    lens = (ctypes.c_int32 * max(n, 1))(*[int(x) for x in seq_lens])
+    n, first = len(seq_lens), _int32("first", first)
+    lens = (ctypes.c_int32 * max(n, 1))(*[_int32("seq_lens", x) for x in seq_lens])
     rows = sum(max(x, 0) for x in lens[:n]) * slots.hkv
     for t, name in ((K, "K"), (V, "V")):
         _tensor(t.view(-1), (rows * slots.d,), torch.bfloat16, slots.device, name)
@@ -523,7 +530,7 @@ def rdkv_slots_fill(slots, K, V, seq_lens, w_tok=None, first=0):
     with _on(slots):
         need = lib.rdkv_slots_fill_workspace_bytes(slots.ref(), n, lens)
         workspace = torch.empty(need, dtype=torch.uint8, device=slots.device) if need else None
-        _check(lib.rdkv_slots_fill(slots.ref(), int(first), n, lens, _ptr(K), _ptr(V), _ptr(w_tok), _ptr(workspace), need, _stream()))
+        _check(lib.rdkv_slots_fill(slots.ref(), first, n, lens, _ptr(K), _ptr(V), _ptr(w_tok), _ptr(workspace), need, _stream()))
 
 
 def rdkv_slots_append(slots, k_new, v_new, slot=None):
@@ -570,11 +577,12 @@ def rdkv_slots_read(slots, index=None, n=None, K=None, V=None):
         _tensor(index, (slots.batch, slots.hkv, n), torch.int32, slots.device, "index")
     elif n is None:
         n = slots.capacity
-    shape = (slots.batch, slots.hkv, int(n), slots.d)
+    n = _int32("n", n)
+    shape = (slots.batch, slots.hkv, max(n, 0), slots.d)
     K = torch.empty(shape, dtype=torch.bfloat16, device=slots.device) if K is None else _tensor(K, shape, torch.bfloat16, slots.device, "K")
     V = torch.empty(shape, dtype=torch.bfloat16, device=slots.device) if V is None else _tensor(V, shape, torch.bfloat16, slots.device, "V")
     with _on(slots):
-        _check(lib.rdkv_slots_read(slots.ref(), _ptr(index), int(n), K.data_ptr(), V.data_ptr(), _stream()))
+        _check(lib.rdkv_slots_read(slots.ref(), _ptr(index), n, K.data_ptr(), V.data_ptr(), _stream()))
     return K, V
 
 

@@ -8,6 +8,8 @@ using namespace rdkv;
 
 namespace {
 
+constexpr int64_t kMostThreads = 1ll << 32;      // of a launch
+
 rdkv_status check_slots(const rdkv_slots* s, bool memory) {
   if (!s) return fail(RDKV_ERR_INVALID_ARG, "slots is null");
   if (s->batch < 0 || s->hq <= 0 || s->hkv <= 0) return fail(RDKV_ERR_INVALID_ARG, "batch/hq/hkv must be positive");
@@ -24,8 +26,9 @@ rdkv_status check_slots(const rdkv_slots* s, bool memory) {
   if (!(s->score_cap >= 0.f) || !std::isfinite(s->score_cap)) return fail(RDKV_ERR_INVALID_ARG, "score_cap must be finite and >= 0");
   if (!(s->decay >= 0.f) || s->decay > 1.f) return fail(RDKV_ERR_INVALID_ARG, "decay must be in [0, 1]");
   const int64_t items = static_cast<int64_t>(s->batch) * s->hkv;
-  if (items * (static_cast<int64_t>(s->capacity) + kTile64) >= (1ll << 31) || static_cast<int64_t>(s->batch) * s->hq >= (1ll << 24))
-    return fail(RDKV_ERR_SHAPE, "batch * hkv * capacity exceeds 2^31 slots");
+  if (items * (static_cast<int64_t>(s->capacity) + kTile64) >= (1ll << 31)) return fail(RDKV_ERR_SHAPE, "batch * hkv * capacity exceeds 2^31 slots");
+  if (static_cast<int64_t>(s->batch) * s->hq >= kMostThreads / 1024)        // (a workgroup of up to 1024 threads for each item)
+    return fail(RDKV_ERR_SHAPE, "batch * hq exceeds 2^22 query heads");
   if (memory && s->batch > 0) {
     if (!s->k || !s->v || !s->pos || !s->len || !s->next) return fail(RDKV_ERR_INVALID_ARG, "k, v, pos, len and next must not be null");
     if (((reinterpret_cast<uintptr_t>(s->k) | reinterpret_cast<uintptr_t>(s->v)) & 15) != 0)
@@ -136,6 +139,8 @@ rdkv_status rdkv_slots_fill(const rdkv_slots* s, int32_t first, int32_t n, const
   if (longest > 0 && (!K || !V)) return fail(RDKV_ERR_INVALID_ARG, "K and V must not be null");
   if (longest > s->capacity && !w_tok)
     return fail(RDKV_ERR_INVALID_ARG, "a prompt of %d tokens for %d slots needs w_tok", longest, s->capacity);
+  // sixteen threads a row (four in tiles), an item after the other
+  if (std::min(longest, s->capacity) >= kMostThreads / 16) return fail(RDKV_ERR_SHAPE, "%d rows of an item exceed 2^28", std::min(longest, s->capacity));
   const SelectBytes need = select_bytes(s, n, seq_lens);
   if (need.total > 0 && (!workspace || workspace_bytes < need.total))
     return fail(RDKV_ERR_INVALID_ARG, "workspace of %zu bytes is smaller than the %zu required", workspace ? workspace_bytes : 0, need.total);
@@ -207,8 +212,8 @@ rdkv_status rdkv_slots_read(const rdkv_slots* s, const int32_t* index, int32_t n
   if (s->batch == 0 || n == 0) return RDKV_OK;
   if (!K || !V) return fail(RDKV_ERR_INVALID_ARG, "K and V must not be null");
   if (!aligned16({K, V})) return fail(RDKV_ERR_INVALID_ARG, "K and V must be aligned to 16 bytes");
-  if (static_cast<int64_t>(s->batch) * s->hkv * (static_cast<int64_t>(n) + 64) >= (1ll << 31))
-    return fail(RDKV_ERR_SHAPE, "batch * hkv * n exceeds 2^31 rows");
+  if (static_cast<int64_t>(s->batch) * s->hkv * (static_cast<int64_t>(n) + kTile64) >= kMostThreads / 16)
+    return fail(RDKV_ERR_SHAPE, "batch * hkv * n exceeds 2^28 rows");
   RDKV_HIP(slots::launch_read(args_of(s), s->bits, s->batch * s->hkv, index, n, static_cast<uint16_t*>(K),
                               static_cast<uint16_t*>(V), static_cast<hipStream_t>(stream)));
   return RDKV_OK;

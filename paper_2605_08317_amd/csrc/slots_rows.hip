@@ -766,7 +766,7 @@ hipError_t launch_append(const Args& a, int bits, int items, const uint16_t* k_n
 }
 
 hipError_t launch_read(const Args& a, int bits, int items, const int32_t* index, int n, uint16_t* K, uint16_t* V, hipStream_t st) {
-  const int groups = (n + 15) / 16;        // (of 16 rows; less than 2^27 in all)
+  const int groups = (n + 15) / 16;        // of 16 rows
   const int tiles = (n + kTileRows - 1) / kTileRows;
   if (bits == 4 && !index)
     hipLaunchKernelGGL(read_tiles_kernel, dim3(tiles * items), dim3(256), 0, st, a, n, tiles, K, V);

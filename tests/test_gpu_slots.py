@@ -546,3 +546,174 @@ def test_views_that_share_memory_with_others():
         b.rdkv_slots_decode_attn(s, cuda(rng.standard_normal((2, 4, D)), BF))
     for t in whole.values():
         assert (t[0] == 9).all() and (t[3] == 9).all()
+
+
+# ---- many items, long items, few tokens in large caches --------------------------------------------------------------------------------
+# What shape of launch a step takes follows from the cache's sizes, not from the tokens in it: large caches with few tokens go the ways of
+# large ones.  Items shared out among workgroups, with empty ones between; items one each to a workgroup, in several turns; rows read past
+# the caches (64 MiB on) or through them.
+
+def some_lens(rng, batch, most):
+    lens = rng.integers(0, 130, batch)
+    lens[rng.integers(0, batch, batch // 4)] = 0
+    lens[batch // 2], lens[-1] = most, most - 70
+    lens[0] = 0
+    return [int(x) for x in lens]
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("g, batch, hkv, capacity", [
+    (1, 40, 2, 6000), (2, 85, 1, 5950), (4, 40, 2, 6000), (8, 80, 1, 6001), (1, 4, 1, 4000), (4, 4, 2, 3500), (2, 2, 1, 9000),       # shared out
+    (1, 130, 2, 600), (4, 300, 1, 500), (8, 65, 4, 513), (2, 260, 1, 1700), (4, 260, 1, 1700)])                                     # one each
+def test_decode_in_large_caches(g, batch, hkv, capacity, bits):
+    rng = np.random.default_rng(21 + g + batch + capacity)
+    lens = some_lens(rng, batch, capacity)
+    s, items = loaded(rng, lens, g * hkv, hkv, capacity, bits, gap=2, window=3000, sinks=2, score_cap=40.0, decay=0.75)
+    q = cuda(rng.standard_normal((batch, g * hkv, D)), BF)
+    before = host(s.weight)
+    out, lse = b.rdkv_slots_decode_attn(s, q)
+    check_step(s, items, q, out, lse, s.weight, before, window=3000, cap=40.0, decay=0.75)
+    t = b.Slots(batch, g * hkv, hkv, capacity, bits=bits, k=s.k, v=s.v, pos=s.pos, lens=s.lens, next_pos=s.next_pos, track=False, window=3000, sinks=2, score_cap=40.0)
+    out1, lse1 = b.rdkv_slots_decode_attn(t, q)
+    for it in items:
+        it.weight[:] = 0
+    zeros = np.zeros((batch * hkv, capacity))
+    w = [it.decode(P.bf16(host(q)).astype(np.float64)[i // hkv, (i % hkv) * g:(i % hkv + 1) * g], window=3000, cap=40.0)[2].sum(0) for i, it in enumerate(items)]
+    for i, p in enumerate(w):
+        zeros[i, :len(p)] = p
+        items[i].weight[:] = 0
+    check_step(t, items, q, out1, lse1, torch.as_tensor(zeros), zeros, window=3000, cap=40.0)       # (the outputs; no weights are there)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("hq, capacity", [(8, 300), (8, 4000), (2, 5000), (16, 4000)])
+def test_scores_that_are_no_numbers_whichever_way_items_are_taken(hq, capacity, bits):
+    rng = np.random.default_rng(22)
+    s, _ = loaded(rng, [capacity, capacity - 50], hq, 2, capacity, bits)
+    q = cuda(rng.standard_normal((2, hq, D)), BF)
+    good, lse = b.rdkv_slots_decode_attn(s, q)
+    for bad, head in ((float("nan"), 0), (float("inf"), hq // 2 - 1)):
+        t = clone(s)
+        qb = q.clone()
+        qb[1, head, 77] = bad
+        out, lse1 = b.rdkv_slots_decode_attn(t, qb)
+        assert out[1, head].isnan().all() and lse1[1, head].isnan()
+        keep = torch.ones(2, hq, dtype=torch.bool)
+        keep[1, head] = False
+        assert torch.equal(out[keep], good[keep]) and torch.equal(lse1[keep], lse[keep])
+        n = capacity - 50
+        assert t.weight[1, 0, :n].isnan().all() and not t.weight[1, 1, :n].isnan().any() and not t.weight[0].isnan().any()
+
+
+LONG_FILLS = [
+    # prompts, hkv, capacity, sinks, recent, weights
+    ([8192], 1, 8191, 0, 0, "any"), ([8193], 2, 8192, 1, 1, "any"), ([12289, 300, 0, 9000], 2, 9500, 4, 64, "any"), ([20000, 15000], 1, 20000, 3, 5, "any"),
+    ([300000], 1, 1000, 4, 32, "any"), ([270001, 4096, 1001], 1, 1000, 0, 900, "ties"), ([280000], 1, 5, 0, 0, "equal"), ([9000, 10000], 2, 500, 3, 9, "infinite"),
+    ([30000], 1, 2000, 0, 17, "nan"), ([16384], 1, 4096, 4096 - 17, 17, "any"), ([33333], 1, 1, 0, 1, "any"), ([40000], 1, 39999, 10, 10, "ties"),
+]
+
+
+@pytest.mark.parametrize("prompts, hkv, capacity, sinks, recent, how", LONG_FILLS)
+def test_fill_of_long_prompts(prompts, hkv, capacity, sinks, recent, how):
+    rng = np.random.default_rng(hash((tuple(prompts), hkv, capacity)) % 2 ** 32)
+    K, V = ragged(rng, prompts, hkv)
+    W = [weights_of(rng, len(k), how) for k in K]
+    for track in (True, False):
+        s = b.Slots(len(prompts), hkv, hkv, capacity, sinks=sinks, recent=recent, track=track)
+        items = [P.Item(capacity, 16, sinks, recent) for _ in K]
+        for it, k, v, w in zip(items, K, V, W):
+            it.fill(k, v, w)
+        b.rdkv_slots_fill(s, cat(K), cat(V), prompts, cuda(np.concatenate(W), F32))
+        if not track:
+            s.weight = cuda(np.stack([it.weight for it in items]), F32).view(len(prompts), hkv, capacity)
+        check_filled(s, items)
+
+
+def test_fill_of_many_sequences_some_of_them_long():
+    """Several launches' worth, the tables of each in the same workspace."""
+    rng = np.random.default_rng(23)
+    prompts = [int(x) for x in rng.integers(0, 400, 140)]
+    prompts[3], prompts[70], prompts[100], prompts[139] = 9001, 30011, 8500, 13000
+    K, V = ragged(rng, prompts, 1)
+    W = [weights_of(rng, len(k), "any") for k in K]
+    s = b.Slots(140, 1, 1, 120, bits=4, sinks=2, recent=5)
+    items = [P.Item(120, 4, 2, 5) for _ in K]
+    for it, k, v, w in zip(items, K, V, W):
+        it.fill(k, v, w)
+    b.rdkv_slots_fill(s, cat(K), cat(V), prompts, cuda(np.concatenate(W), F32))
+    check_filled(s, items)
+
+
+def test_a_captured_fill_of_a_long_prompt():
+    rng = np.random.default_rng(24)
+    prompts = [300, 21000]
+    K, V = ragged(rng, prompts, 2)
+    Kd, Vd, wd = cat(K), cat(V), cuda(np.zeros(2 * sum(prompts)), F32)
+    s = b.Slots(2, 2, 2, 500, sinks=4, recent=30)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        b.rdkv_slots_fill(s, Kd, Vd, prompts, wd)
+    for how in ("any", "ties", "nan", "any"):
+        w = [weights_of(rng, len(k), how) for k in K]
+        wd.copy_(cuda(np.concatenate(w), F32))
+        graph.replay()
+        torch.cuda.synchronize()
+        items = [P.Item(500, 16, 4, 30) for _ in K]
+        for it, k, v, x in zip(items, K, V, w):
+            it.fill(k, v, x)
+        check_filled(s, items)
+        b.rdkv_slots_fill(s, Kd[:0], Vd[:0], [0, 0])            # between replays: an empty cache, by an eager call
+        assert not s.lens.any()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_past_four_gigabytes(bits):
+    """Items whose rows lie further than 32 bits reach: appended to, attended to, read, and filled."""
+    n = 17_000_003 if bits == 16 else 54_000_005
+    s = b.Slots(1, 1, 1, n, bits=bits, sinks=3, recent=8)
+    s.lens.fill_(n)
+    s.next_pos.fill_(n)
+    s.pos.view(-1).copy_(torch.arange(n, dtype=I32, device="cuda"))
+    s.weight.fill_(1.0)
+    gone = n - 1000
+    s.weight[0, 0, gone] = 0.5
+    rng = np.random.default_rng(25)
+    k, v, q = (P.bf16(rng.standard_normal((1, 1, D))) for _ in range(3))
+    k = P.bf16(q * 0.5)
+    slot = b.rdkv_slots_append(s, cuda(k, BF), cuda(v, BF))
+    assert slot.item() == gone and s.next_pos.item() == n + 1 and s.pos[0, 0, gone].item() == n
+    out, lse = b.rdkv_slots_decode_attn(s, cuda(q, BF))
+    # every other row is zeros: their scores are 0, their values nothing
+    kh, vh, kt, vt = (f(x[0], bits) for f in (P.held, P.terms) for x in (k, v))
+    x = (q[0].astype(np.float64) @ kh[0]).item() / math.sqrt(D)
+    off = 2.0 ** -24 * 138 * (np.abs(q[0]).astype(np.float64) @ kt[0]).item() / math.sqrt(D)
+    total = math.exp(x) + n - 1
+    p = math.exp(x) / total
+    # sums: shares of tiles in steps of four, each wavefront's at most n / 2000 slots of 64 lanes, then parts in turn
+    rel = 2 * off + P.sums_off(n // 2000 + 2048) + 2.0 ** -20
+    assert np.all(np.abs(host(out)[0, 0] - p * vh[0]) <= rel * p * vt[0] + 1e-30)
+    assert abs(lse.item() - math.log(total)) <= rel + 2.0 ** -22 * math.log(total)
+    w = s.weight[0, 0]
+    assert abs(w[gone].item() - p) <= rel * p
+    for at in (0, 1, n // 3, n - 1):
+        assert abs(w[at].item() - (1 + 1 / total)) <= 2.0 ** -22
+    K, V = b.rdkv_slots_read(s, torch.tensor([[[gone, 5, n - 1, n]]], device="cuda", dtype=I32))
+    for got, want in ((K, kh), (V, vh)):
+        assert np.all(np.abs(host(got)[0, 0, 0] - want[0]) <= 2.0 ** -8 * np.abs(want[0]) + 2.0 ** -22 * np.abs(want).max())
+        assert not got[0, 0, 1:].any()
+    if bits == 4:
+        return
+    rows = torch.zeros((n + 7, D), device="cuda", dtype=BF)
+    mark = torch.arange(n + 7, device="cuda", dtype=torch.int64)
+    for c in range(4):                                         # a row's number in its channels, 6 bits in each
+        rows[:, c] = ((mark >> (6 * c)) & 63).to(BF)
+    w_tok = torch.ones(n + 7, device="cuda")
+    lost = torch.tensor([3, 4, 1000, n // 2, n - 900, n - 5, n - 2], device="cuda")
+    w_tok[lost] = 0.25
+    b.rdkv_slots_fill(s, rows, rows, [n + 7], w_tok)
+    kept = torch.ones(n + 7, dtype=torch.bool, device="cuda")
+    kept[lost] = False
+    assert torch.equal(s.pos[0, 0].long(), mark[kept]) and s.lens.item() == n
+    for c in range(4):
+        assert torch.equal(s.k[0, 0, :, c], rows[:, c][kept]) and torch.equal(s.v[0, 0, :, c], rows[:, c][kept])

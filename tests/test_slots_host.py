@@ -36,7 +36,7 @@ def calls(c, seq=(5, 5), first=0, w=16, ws=None, ws_bytes=0):
     (dict(sinks=-1), INVALID), (dict(recent=-1), INVALID), (dict(window=-1), INVALID), (dict(sinks=100), SHAPE), (dict(sinks=60, recent=41), SHAPE),
     (dict(sinks=2 ** 31 - 1, recent=2 ** 31 - 1), SHAPE), (dict(score_cap=-1.0), INVALID), (dict(score_cap=float("nan")), INVALID),
     (dict(score_cap=float("inf")), INVALID), (dict(decay=-0.1), INVALID), (dict(decay=1.5), INVALID), (dict(decay=float("nan")), INVALID),
-    (dict(batch=2 ** 20, capacity=2 ** 12), SHAPE), (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(pos=None), INVALID), (dict(len=None), INVALID),
+    (dict(batch=2 ** 20, capacity=2 ** 12), SHAPE), (dict(batch=2 ** 19, capacity=1), SHAPE), (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(pos=None), INVALID), (dict(len=None), INVALID),
     (dict(next=None), INVALID), (dict(k=24), INVALID), (dict(v=17), INVALID)])
 def test_a_bad_struct_is_refused_by_every_call(kw, status):
     for name, call in calls(struct(**kw)).items():
@@ -56,6 +56,9 @@ def test_bad_arguments_are_refused():
     assert lib.rdkv_slots_read(r, None, -1, 16, 16, None) == INVALID
     assert lib.rdkv_slots_read(r, None, 4, None, 16, None) == INVALID
     assert lib.rdkv_slots_read(r, None, 2 ** 30, 16, 16, None) == SHAPE
+    assert lib.rdkv_slots_read(r, None, 2 ** 26 - 64, 16, 16, None) == SHAPE                       # a launch's threads: 2^28 rows
+    for bits in (16, 4):
+        assert calls(struct(batch=1, hq=1, hkv=1, capacity=2 ** 29, bits=bits), seq=(2 ** 28,))["fill"]() == SHAPE
     c = struct()
     assert calls(c, seq=(5, -1))["fill"]() == SHAPE
     assert calls(c, seq=(5, 5), first=1)["fill"]() == INVALID and calls(c, seq=(5,), first=-1)["fill"]() == INVALID
@@ -115,6 +118,20 @@ def test_the_binding_refuses_tensors_the_library_would_misread():
                  lambda: b.rdkv_slots_read(s, torch.zeros(2, 2, 3, dtype=torch.int64)), lambda: b.rdkv_slots_read(s, torch.zeros(2, 2, dtype=torch.int32)),
                  lambda: b.rdkv_slots_fill(s, new, new, [5, 5])):
         with pytest.raises(ValueError):
+            call()
+
+
+def test_the_binding_refuses_what_would_be_cut_to_32_bits_and_host_memory():
+    s = b.Slots(2, 8, 2, 100, device="cpu")
+    new, q = torch.zeros(2, 2, 128, dtype=torch.bfloat16), torch.zeros(2, 8, 128, dtype=torch.bfloat16)
+    rows = torch.zeros(2 * 2 * 5, 128, dtype=torch.bfloat16)
+    for call in (lambda: b.rdkv_slots_fill(s, rows, rows, [5, 5], first=2 ** 32), lambda: b.rdkv_slots_fill(s, rows, rows, [2 ** 32 + 5, 5]),
+                 lambda: b.rdkv_slots_read(s, n=2 ** 32)):
+        with pytest.raises(ValueError, match="32-bit"):
+            call()
+    for call in (lambda: b.rdkv_slots_fill(s, rows, rows, [5, 5]), lambda: b.rdkv_slots_append(s, new, new), lambda: b.rdkv_slots_decode_attn(s, q),
+                 lambda: b.rdkv_slots_read(s, n=3)):
+        with pytest.raises(ValueError, match="cpu"):
             call()
 
 
