@@ -9,8 +9,8 @@
 //   precision  products of the query and of probabilities lose nothing that fp32 holds: bf16 rows meet a probability in three bf16 terms
 //              (24 bits), codes in two fp16 terms (22 bits), scaled so that the largest V scale seen stands just below fp16's largest
 //              and the query's largest value near one
-//   work       lengths are on the device.  The tiles of all items are one line, in which every workgroup takes an equal share; a
-//              piece of an item that does not hold all of it leaves a partial result for the launch that follows
+//   work       lengths are on the device.  A workgroup takes an item, where there are enough for the card; otherwise it finds its piece
+//              of one by itself, nearly equal ones, which leave partial results for the launch that follows
 #include <algorithm>
 
 #include "decode_rows.h"
@@ -40,38 +40,89 @@ struct DecodeArgs {
   int32_t items, score_rows, least;     // least: tiles of a workgroup's share; 0: a workgroup takes an item
 };
 
-// How the tiles of all items are shared out among the workgroups: workgroup w has those from w * share on.
-struct Line {
-  int total, share;
+// How the tiles of all items are shared out among the workgroups.  An item is cut into pieces, one for each of its workgroups: the largest
+// piece is the smallest of the line's share (below) and up to 8 tiles more that leaves no more pieces than workgroups.  If none of these
+// does, the tiles are a line, workgroup w has those from w * share on, and some have the end of one item and the begin of the next, which
+// is a second start and a second merge.  (Pieces and the line, us: 128 items of 4000 slots in 4 bits, 8 heads, 36.1 and 41.0, 64 of them 26.6
+// and 31.5, 8 19.2 and 22.5; 8 of 2000 17.7 and 17.1: finding the pieces costs half a microsecond.)
+constexpr int kHeldLengths = 1024;
+struct Lengths {                         // of the items: in LDS, where there is room
+  const DecodeArgs& a;
+  const int* s_len;
+  __device__ __forceinline__ int operator()(int i) const { return a.items <= kHeldLengths ? s_len[i] : a.s.length(i); }
+  __device__ __forceinline__ int tiles(int i) const { return ((*this)(i) + kTile - 1) / kTile; }
 };
-__device__ __forceinline__ int tiles_of(const Args& a, int64_t item) { return (a.length(item) + kTile - 1) / kTile; }
-
-// Tiles of all items together, and the share of one of n_groups workgroups.
-__device__ __forceinline__ Line make_line(const DecodeArgs& a, int n_groups) {
-  const int lane = threadIdx.x & 63;
-  int sum = 0;
-  for (int i = lane; i < a.items; i += 64) sum += tiles_of(a.s, i);
-  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-  Line l;
-  l.total = __builtin_amdgcn_readfirstlane(sum);
-  l.share = max(a.least, (l.total + n_groups - 1) / n_groups);
-  return l;
-}
-// The item that holds tile `at` of the line (at < total), and its first tile.
-__device__ __forceinline__ int item_at(const DecodeArgs& a, int at, int* first) {
+__device__ __forceinline__ int lanes_sum(int v) { return __builtin_amdgcn_readlane(static_cast<int>(wave_scan(static_cast<uint32_t>(v))), 63); }
+// The item that holds unit `at` (of sum over units(i)), and its first unit.
+template <class Units>
+__device__ __forceinline__ int item_at(int items, const Units& units, int at, int* first) {
   const int lane = threadIdx.x & 63;
   int base = 0;
   for (int i0 = 0;; i0 += 64) {
-    const int n = i0 + lane < a.items ? tiles_of(a.s, i0 + lane) : 0;
+    const int n = i0 + lane < items ? units(i0 + lane) : 0;
     const int up_to = base + static_cast<int>(wave_scan(static_cast<uint32_t>(n)));
     const uint64_t past = __ballot(up_to > at);
-    if (past != 0 || i0 + 64 >= a.items) {
+    if (past != 0 || i0 + 64 >= items) {
       const int k = past != 0 ? __builtin_ctzll(past) : 63;
       *first = __builtin_amdgcn_readlane(up_to - n, k);
       return i0 + k;
     }
     base = __builtin_amdgcn_readlane(up_to, 63);
   }
+}
+// Of a workgroup: its first item; on the line, or within the item where that is cut into `pieces`, the item's first tile and the tiles from
+// `at` to `end`.  Nothing to do: at == end.
+struct Place {
+  int item, first, at, end, share, pieces;
+};
+constexpr int kTries = 2;                // of a wavefront
+__device__ __forceinline__ Place find_place(const DecodeArgs& a, const Lengths& len, uint64_t* s_tries) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = gridDim.x, group = blockIdx.x;
+  int sum = 0;
+  for (int i = lane; i < a.items; i += 64) sum += len.tiles(i);
+  const int total = lanes_sum(sum);
+  Place p{};
+  p.share = max(a.least, (total + groups - 1) / groups);
+  if (a.items <= groups) {
+    // shares + 0, 1, 2, 3, 4, 5, 6, 8: two a wavefront
+    const auto more = [](int k) { return k + (k == 7); };
+    uint32_t size[kTries], pieces[kTries];
+#pragma unroll
+    for (int k = 0; k < kTries; ++k) {
+      size[k] = p.share + more(kTries * wave + k);
+      pieces[k] = 0;
+    }
+    for (int i = lane; i < a.items; i += 64) {
+      const uint32_t t = len.tiles(i);
+#pragma unroll
+      for (int k = 0; k < kTries; ++k) pieces[k] += (t + size[k] - 1) / size[k];
+    }
+#pragma unroll
+    for (int k = 0; k < kTries; ++k) {
+      const uint32_t n = lanes_sum(pieces[k]);
+      if (lane == 0) s_tries[kTries * wave + k] = n;
+    }
+    __syncthreads();
+    const uint64_t ok = __ballot(lane < 4 * kTries && s_tries[lane & (4 * kTries - 1)] <= static_cast<uint64_t>(groups));
+    if (ok != 0) {
+      const int k = __builtin_ctzll(ok);
+      if (group >= static_cast<int>(s_tries[k])) return p;
+      const uint32_t most = p.share + more(k);
+      int before;
+      p.item = item_at(a.items, [&](int i) { return static_cast<int>((len.tiles(i) + most - 1) / most); }, group, &before);
+      const int t = len.tiles(p.item);
+      p.pieces = (t + most - 1) / most;
+      const int each = t / p.pieces, rest = t % p.pieces, j = group - before;
+      p.at = j * each + min(j, rest);
+      p.end = p.at + each + (j < rest);
+      return p;
+    }
+  }
+  p.at = group * p.share;
+  p.end = max(p.at, min(p.at + p.share, total));
+  if (p.at < p.end) p.item = item_at(a.items, [&](int i) { return len.tiles(i); }, p.at, &p.first);
+  return p;
 }
 
 // cap * tanh(s / cap).  Below 0.8 the fifth convergent of Lambert's continued fraction y / (1 + y^2 / (3 + y^2 / (5 + ..))), off by
@@ -710,23 +761,28 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = a.s.g;
-  // where on the line this workgroup is; a workgroup of eight wavefronts is at its item
-  int at = 0, end = 0, first = 0, item = blockIdx.x, share = 0;
+  // what this workgroup has; one of eight wavefronts has its item
+  Place p{};
+  p.item = blockIdx.x;
   if constexpr (NWV == 4) {
+    int* s_len = reinterpret_cast<int*>(smem);
+    if (a.items <= kHeldLengths) {
+      for (int i = tid; i < a.items; i += NWV * 64) s_len[i] = a.s.length(i);
+      __syncthreads();
+    }
+    const Lengths len{a, s_len};
     // items without a token have no tile: their outputs are the first workgroups' to write
     for (int i = blockIdx.x; i < a.items; i += gridDim.x)
-      if (a.s.length(i) == 0) {
+      if (len(i) == 0) {
         for (int k = tid; k < g * kHeadDim; k += NWV * 64) a.out[static_cast<int64_t>(i) * g * kHeadDim + k] = 0.f;
         if (a.lse != nullptr && tid < g) a.lse[static_cast<int64_t>(i) * g + tid] = -INFINITY;
         if (tid == 0) a.parts[i] = make_int2(0, 0);
       }
-    const Line line = make_line(a, gridDim.x);
-    share = line.share;
-    at = static_cast<int>(blockIdx.x) * share;
-    if (at >= line.total) return;
-    end = min(at + share, line.total);
-    item = item_at(a, at, &first);
+    p = find_place(a, len, reinterpret_cast<uint64_t*>(s_len + kHeldLengths));
+    if (p.at == p.end) return;
+    __syncthreads();
   }
+  int item = p.item, first = p.first, at = p.at;
   // LDS: the wavefronts' staging regions; their scores; the accumulators' area [NWV][g][128], which is the staging regions' memory, or the
   // scores' unless they are kept; the wavefronts' maxima and sums, and the heads' log-sum-exps
   constexpr bool kKeep = NWV == 8, kOwnAcc = BITS == 4 && kKeep;
@@ -741,18 +797,18 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     // (all the same for every lane, which buffers need to be known of)
     item = __builtin_amdgcn_readfirstlane(item);
     const int n = __builtin_amdgcn_readfirstlane(a.s.length(item)), tiles = (n + kTile - 1) / kTile;
-    const int t0 = __builtin_amdgcn_readfirstlane(at - first), t1 = NWV == 8 ? tiles : __builtin_amdgcn_readfirstlane(min(tiles, end - first));
+    const int t0 = __builtin_amdgcn_readfirstlane(at - first), t1 = NWV == 8 ? tiles : __builtin_amdgcn_readfirstlane(min(tiles, p.end - first));
     if (NWV == 4 && t1 <= t0) {          // an item without tiles
       ++item;
       continue;
     }
     const bool whole = NWV == 8 || (t0 == 0 && t1 == tiles);
     if (NWV == 4 && t0 == 0 && tid == 0)
-      a.parts[item] = whole ? make_int2(0, 0) : make_int2(static_cast<int>(blockIdx.x) + item, (first + tiles - 1) / share - static_cast<int>(blockIdx.x) + 1);
+      a.parts[item] = whole ? make_int2(0, 0)
+                            : make_int2(static_cast<int>(blockIdx.x) + item, p.pieces > 0 ? p.pieces : (first + tiles - 1) / p.share - static_cast<int>(blockIdx.x) + 1);
     Scoring sc;
     sc.n = n;
     sc.sure = NWV == 8 ? a.s.capacity : n;
-    sc.at = __builtin_amdgcn_readfirstlane(a.s.next[item]) - 1;
     sc.g = g;
     sc.sinks = a.s.sinks;
     sc.window = a.s.window;
@@ -761,7 +817,9 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     sc.where = a.s.window > 0 || a.s.slopes != nullptr;
     sc.pos = a.s.pos + static_cast<int64_t>(item) * a.s.capacity;
     sc.biased = a.s.slopes != nullptr;
-    if (sc.biased) {                     // (constant address space: scalar loads, which no wait for rows waits for)
+    typedef const __attribute__((address_space(4))) int32_t* ConstInts;      // (scalar loads, which no wait for rows waits for)
+    sc.at = ((ConstInts)(a.s.next))[item] - 1;
+    if (sc.biased) {
       typedef const __attribute__((address_space(4))) float* ConstFloats;
       const ConstFloats slopes = (ConstFloats)(a.s.slopes) + (item % a.s.hkv) * g;
 #pragma unroll
@@ -866,7 +924,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
       first += tiles;
       ++item;
     }
-  } while (NWV == 4 && at < end);
+  } while (NWV == 4 && at < p.end);
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -934,18 +992,24 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
 }
 
 constexpr size_t kMostLds = 160 << 10;
-// Whether a workgroup takes an item alone (if its scores fit).  Then a compute unit's reading bounds a step, 6 us and for every tile 0.42
-// (bf16; 0.53 for 8 heads) or 0.31 (4 bits; 0.47), in as many turns as there are items for a compute unit.  Shared out, a step is two
-// launches, 13 us (16 for 8 heads; 4 bits 13.5 and 18), and bound by memory: 3.5 ns a tile in bf16, 2.4 in 4 bits.  Alone and shared, us:
-//   bf16, 4 heads     8 items of 500 slots  9.4, 14.6   of 1000  13.3, 16.5   of 2000  19.9, 14.6   32 of 1500  22.1, 17.1
-//                     64 of 1500  23.7, 22.9   of 4000  51, 40   128 of 4000  58, 63   256 of 4000  90, 114
-//   4 bits, 4 heads   8 of 1500  11.7, 12.6   of 2000  14.3, 13.0   64 of 3000  20.9, 23.4   of 4000  26, 23   256 of 8000  66, 85
-//   4 bits, 8 heads   8 of 1500  15.9, 16.7   of 2000  19.7, 17.8   128 of 3000  29.9, 38.0
-bool one_each(int64_t items, int g, int64_t tiles, int bits) {
+// Whether a workgroup takes an item alone (if its scores fit).  Then a compute unit's reading bounds a step: 6 us and `own` us a tile, more
+// where rows come from memory (`stream`), or all units' reading, `rate`; 256 items at a time.  Shared out, a step is two launches, `base`
+// us, and bound by `rate`.  Alone and shared, us, rows of several caches in turn:
+//   bf16, 4 heads     8 items of 500 slots  9.3, 13.5   of 1000  13.1, 15.0   of 2000  20.0, 14.9   32 of 1500  17.4, 16.2
+//                     64 of 1500  22.5, 22.6   of 4000  47.0, 32.6   128 of 2500  38.4, 39.2   of 4000  51.9, 52.4 (lengths of 1300 to
+//                     4000 46.8, 37.1)   256 of 4000  82.5, 98.6   512 of 2000  87.6, 100.9
+//   bf16, 8 heads     8 of 2000  24.2, 19.1   32 of 1500  20.4, 19.9   64 of 1500  24.7, 26.6   128 of 2500  39.1, 43.5   512 of 2000  90.5, 111.8
+//   4 bits, 4 heads   8 of 1000  8.8, 13.5   of 2000  13.8, 13.0   32 of 3000  19.8, 18.2   64 of 4000  25.7, 21.2   128 of 4000  26.9, 28.1
+//                     256 of 4000  33.9, 44.4
+//   4 bits, 8 heads   8 of 1000  12.1, 18.9   of 2000  19.4, 17.7   32 of 3000  27.3, 23.0   128 of 2500  26.5, 31.9   512 of 2000  47.5, 55.1
+bool one_each(int64_t items, int g, int64_t tiles, int bits, bool stream) {
   const bool wide = g > 4;
-  const double own = bits == 16 ? (wide ? 0.53 : 0.42) : (wide ? 0.47 : 0.31), base = bits == 16 ? (wide ? 16.0 : 13.0) : (wide ? 18.0 : 13.5);
-  const double turns = static_cast<double>((items + 255) / 256);
-  return 6.0 + own * turns * static_cast<double>(tiles) <= base + (bits == 16 ? 0.0035 : 0.0024) * static_cast<double>(items) * static_cast<double>(tiles);
+  const double own = bits == 4 ? (wide ? 0.5 : 0.31) : stream ? (wide ? 0.85 : 0.77) : (wide ? 0.53 : 0.42);
+  const double rate = bits == 4 ? (wide ? 0.0024 : 0.0020) : stream ? 0.0050 : 0.0035;
+  const double base = bits == 4 ? (wide ? 18.0 : 13.5) : (wide ? 16.0 : 13.0);
+  const int64_t turns = items / 256, rest = items % 256;
+  const double alone = static_cast<double>(turns) * std::max(own, 256 * rate) + (rest > 0 ? std::max(own, static_cast<double>(rest) * rate) : 0.0);
+  return 6.0 + alone * static_cast<double>(tiles) <= base + rate * static_cast<double>(items) * static_cast<double>(tiles);
 }
 // LDS of a workgroup of eight wavefronts that keep `held` bytes of scores each
 size_t lds_of_eight(int bits, int g, size_t held) {
@@ -968,7 +1032,7 @@ Plan make_plan(int64_t items, int g, int capacity, int bits, bool weights) {
   const size_t held = weights ? (tiles + p.waves - 1) / p.waves * kTile * g * sizeof(float) : 0;
   const bool fits = lds_of_eight(bits, g, held) <= kMostLds;
   p.held_bytes = fits ? static_cast<int>(held) : 0;
-  if (fits && one_each(items, g, tiles, bits)) {
+  if (fits && one_each(items, g, tiles, bits, p.stream)) {
     p.least = p.join_rows = 0;
     p.groups = static_cast<int>(items);
     p.part_acc = p.part_ml = p.parts = 0;
