@@ -165,8 +165,10 @@ __global__ __launch_bounds__(kSelectThreads) void fill_select_kernel(FillArgs a)
 // adds up the counts of all, finds the digit at the border, and puts its weights at that digit into a list of the item's, in the order of
 // tokens.  place: every part goes through the list, some hundredths of the weights, for the other two digits, and knows from it what the
 // parts before it keep.  Bound: latency of three launches; 4 bytes a token twice.
-// (One workgroup an item took 32 us for 8 items of 32K tokens and 128 for 128K.)
-constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPartEach = 16, kPartBlock = kPartThreads * kPartEach;
+// 8 items of 32K tokens, 4K kept: 4.5, 6.4 and 9.8 us; of 128K with many ties, 32K kept: 4.8, 9.4 and 10.7 (one workgroup an item took 32 us
+// for 32K and 128 for 128K).  Workgroups of 256 threads 5.8, 7.8, 12.6 and of 1024 3.8, 5.8, 8.9, but 128 items of up to 32K then 49 us in
+// all, and 36 with 512.
+constexpr int kPartBlock = 4096, kPartThreads = 512, kPartWaves = kPartThreads / 64, kPartEach = kPartBlock / kPartThreads;
 
 struct PartOf {
   int g, head, sl, tid, t0, t1;       // part of the item; its tokens
@@ -265,20 +267,19 @@ __global__ __launch_bounds__(kPartThreads) void select_open_kernel(FillArgs a) {
   float x[kPartEach];                  // of the block; the first is under way during what comes before it
   load_weights(it, p.t0, p.t1, p.tid, x);
   const uint16_t* counts = a.counts + p.local * a.parts * kDigits;
-  // eight digits a thread, thread 0 the highest
+  // a few digits a thread, thread 0 the highest
   constexpr int kPer = kDigits / kPartThreads;
-  static_assert(kPer == 8, "sixteen bytes of counts");
+  using Counts = __attribute__((ext_vector_type(kPer / 2))) uint32_t;
   const int at = kDigits - kPer * (p.tid + 1);
   uint32_t n[kPer], own[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) n[k] = own[k] = 0;
 #pragma unroll 8
   for (int g = 0; g < parts; ++g) {
-    const uint4 c = *reinterpret_cast<const uint4*>(counts + static_cast<int64_t>(g) * kDigits + at);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    const Counts c = *reinterpret_cast<const Counts*>(counts + static_cast<int64_t>(g) * kDigits + at);
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-      const uint32_t x = (w[3 - k / 2] >> (k % 2 ? 0 : 16)) & 0xFFFFu;
+      const uint32_t x = (c[kPer / 2 - 1 - k / 2] >> (k % 2 ? 0 : 16)) & 0xFFFFu;
       n[k] += x;
       own[k] = g == p.g ? x : own[k];
     }
@@ -342,7 +343,7 @@ __global__ __launch_bounds__(kPartThreads) void select_place_kernel(FillArgs a) 
   uint32_t left = found.y, border = static_cast<uint32_t>(found.x) << 21;
   const uint32_t* list = a.open + (a.row0[p.sl] - a.row0[0]) + static_cast<int64_t>(p.head) * it.T;
   // the first of the list's weights stay with their threads
-  constexpr int kHold = 16;
+  constexpr int kHold = 4096 / kPartThreads;
   uint32_t held[kHold];
 #pragma unroll
   for (int i = 0; i < kHold; ++i) held[i] = list[min(i * kPartThreads + p.tid, open - 1)];
