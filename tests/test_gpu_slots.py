@@ -585,6 +585,30 @@ def test_decode_in_large_caches(g, batch, hkv, capacity, bits):
     check_step(t, items, q, out1, lse1, torch.as_tensor(zeros), zeros, window=3000, cap=40.0)       # (the outputs; no weights are there)
 
 
+@pytest.mark.parametrize("batch, bits, capacity", [(135, 4, 3600), (280, 4, 3600), (75, 16, 2600)])
+def test_decode_of_items_that_share_workgroups(batch, bits, capacity):
+    """More items than workgroups, and as many as leave some workgroups the end of one and the begin of the next."""
+    rng = np.random.default_rng(batch)
+    lens = [int(x) for x in np.where(rng.random(batch) < 0.3, 0, rng.integers(1, 260, batch))] if bits == 4 else [1500] * batch
+    lens[0], lens[batch // 3], lens[-1] = 0, capacity, 0
+    s, items = loaded(rng, lens, 32, 4, capacity, bits)
+    q = cuda(rng.standard_normal((batch, 32, D)), BF)
+    before = host(s.weight)
+    out, lse = b.rdkv_slots_decode_attn(s, q)
+    check_step(s, items, q, out, lse, s.weight, before)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("hq, batch, capacity", [(2, 1, 300), (8, 3, 9000), (16, 140, 3600)])
+def test_empty_caches(hq, batch, capacity, bits):
+    s = b.Slots(batch, hq, 2, capacity, bits=bits)
+    s.weight.fill_(3.0)
+    for _ in range(2):
+        out, lse = torch.full((batch, hq, D), 7.0, device="cuda"), torch.zeros((batch, hq), device="cuda")
+        b.rdkv_slots_decode_attn(s, torch.ones((batch, hq, D), device="cuda", dtype=BF), out, lse)
+        assert not out.any() and torch.isneginf(lse).all() and (s.weight == 3).all()
+
+
 @pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("hq, capacity", [(8, 300), (8, 4000), (2, 5000), (16, 4000)])
 def test_scores_that_are_no_numbers_whichever_way_items_are_taken(hq, capacity, bits):
