@@ -9,6 +9,8 @@
 //   precision  products of the query and of probabilities lose nothing that fp32 holds: bf16 rows meet a probability in three bf16 terms
 //              (24 bits), codes in two fp16 terms (22 bits), scaled so that the largest V scale seen stands just below fp16's largest
 //              and the query's largest value near one
+//   bound      HBM: 512 bytes a slot in bf16, 160 in 4 bits, and the scores.  4 x 8 items of 128K slots 6.8 and 6.1 TB/s without weights, 5.5
+//              and 4.6 with them; items one each to a workgroup 6.3 TB/s (256 of 4000 slots in bf16) and 4.8.  Small caches: latency
 //   work       lengths are on the device.  A workgroup takes an item, where there are enough for the card; otherwise it finds its piece
 //              of one by itself, nearly equal ones, which leave partial results for the launch that follows
 #include <algorithm>
@@ -37,14 +39,19 @@ struct DecodeArgs {
   float* part_ml;      // [slot][g][2]
   int2* parts;         // [items]: an item's first partial and their number, 0 where it has none
   int32_t held_bytes;  // of scores that a wavefront keeps
-  int32_t items, score_rows, least;     // least: tiles of a workgroup's share; 0: a workgroup takes an item
+  int32_t items, score_rows;
+  int32_t least, start;                 // of a workgroup's share, tiles; 0: a workgroup takes an item.  What a start on one is worth
 };
 
 // How the tiles of all items are shared out among the workgroups.  An item is cut into pieces, one for each of its workgroups: the largest
-// piece is the smallest of the line's share (below) and up to 8 tiles more that leaves no more pieces than workgroups.  If none of these
-// does, the tiles are a line, workgroup w has those from w * share on, and some have the end of one item and the begin of the next, which
-// is a second start and a second merge.  (Pieces and the line, us: 128 items of 4000 slots in 4 bits, 8 heads, 36.1 and 41.0, 64 of them 26.6
-// and 31.5, 8 19.2 and 22.5; 8 of 2000 17.7 and 17.1: finding the pieces costs half a microsecond.)
+// piece is the smallest of an equal share of all tiles and up to 8 tiles more that leaves no more pieces than workgroups.  If none of these
+// does, the items are a line, on which each has `start` places and then its tiles, workgroup w has the places from w * share on, and some
+// have the end of one item and the begin of the next, or several: each is a start and a merge, as long as `start` tiles take to pass (4 in
+// bf16, 8 in 4 bits).
+//   pieces and the line, us: 4 bits, 8 heads, 128 items of 4000 slots 36.1 and 41.0, 64 of them 26.6 and 31.5, 8 19.2 and 22.5; 8 of 2000
+//   17.7 and 17.1 (finding the pieces costs half a microsecond)
+//   starts of 0, 4, 8 and 14 places: bf16, 8 heads, 320 items of 1 to 4000 slots 100, 77, 78, 82, all of 4000 143, 142, 143, 145, 240 of 20
+//   to 20000, more short ones than long, 194, 133, 134, 136; 4 bits 68, 56, 49, 51; 71, 69, 68, 74; 123, 70, 65, 66
 constexpr int kHeldLengths = 1024;
 struct Lengths {                         // of the items: in LDS, where there is room
   const DecodeArgs& a;
@@ -79,11 +86,15 @@ constexpr int kTries = 2;                // of a wavefront
 __device__ __forceinline__ Place find_place(const DecodeArgs& a, const Lengths& len, uint64_t* s_tries) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int groups = gridDim.x, group = blockIdx.x;
-  int sum = 0;
-  for (int i = lane; i < a.items; i += 64) sum += len.tiles(i);
-  const int total = lanes_sum(sum);
+  int sum = 0, some = 0;
+  for (int i = lane; i < a.items; i += 64) {
+    const int t = len.tiles(i);
+    sum += t;
+    some += t > 0;
+  }
+  const int tiles = lanes_sum(sum), total = tiles + a.start * lanes_sum(some);
   Place p{};
-  p.share = max(a.least, (total + groups - 1) / groups);
+  p.share = max(a.least, (tiles + groups - 1) / groups);
   if (a.items <= groups) {
     // shares + 0, 1, 2, 3, 4, 5, 6, 8: two a wavefront
     const auto more = [](int k) { return k + (k == 7); };
@@ -119,9 +130,14 @@ __device__ __forceinline__ Place find_place(const DecodeArgs& a, const Lengths& 
       return p;
     }
   }
+  p.share = max(a.least, (total + groups - 1) / groups);
   p.at = group * p.share;
   p.end = max(p.at, min(p.at + p.share, total));
-  if (p.at < p.end) p.item = item_at(a.items, [&](int i) { return len.tiles(i); }, p.at, &p.first);
+  if (p.at < p.end) {
+    p.item = item_at(a.items, [&](int i) { const int t = len.tiles(i); return t > 0 ? t + a.start : 0; }, p.at, &p.first);
+    p.first += a.start;                  // where its tiles begin
+    p.at = min(max(p.at, p.first), p.end);
+  }
   return p;
 }
 
@@ -218,9 +234,10 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& r
 }
 
 // Scores on their way to the weights, which need them once the item's sums are known.  They wait in LDS: where a workgroup has all of an
-// item until then (KEEP), otherwise until a wavefront's part is full, which then goes to the workspace at once.  Writes among the reads
-// of rows cost more than their bytes, and wavefronts that began together write together (4 x 8 items of 128K slots in 4 bits, 4 heads: 103 us
-// without scores, 139 with a store a tile, 128 so; 32 x 8 of 8K 71 -> 64.5).
+// item until then, otherwise until a wavefront's part is full, which then goes to the workspace at once.  Writes among the reads of rows
+// cost more than their bytes.  4 x 8 items of 128K slots, 4 heads, us, with the launch that joins them: bf16 318 without weights, 401 with a
+// store a tile, 391 so; 4 bits 110, 158, 147.  (334 and 126 of them if nothing is written; with waits that count these stores, or with
+// non-temporal ones, no less.)
 struct Held {
   uint8_t* at;         // of this wavefront: [tiles][64][g]
   int n, most;         // tiles there, and room; most 0: all of the item's stay
@@ -921,7 +938,8 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     }
     at = first + t1;
     if (t1 == tiles) {
-      first += tiles;
+      first += tiles + a.start;
+      at += a.start;
       ++item;
     }
   } while (NWV == 4 && at < p.end);
@@ -1018,7 +1036,7 @@ size_t lds_of_eight(int bits, int g, size_t held) {
 }
 struct Plan {
   bool stream;         // rows past the caches' order
-  int waves, groups, least, score_rows, join_rows, held_bytes;
+  int waves, groups, least, start, score_rows, join_rows, held_bytes;
   size_t scores, part_acc, part_ml, parts;      // floats
 };
 Plan make_plan(int64_t items, int g, int capacity, int bits, bool weights) {
@@ -1033,13 +1051,14 @@ Plan make_plan(int64_t items, int g, int capacity, int bits, bool weights) {
   const bool fits = lds_of_eight(bits, g, held) <= kMostLds;
   p.held_bytes = fits ? static_cast<int>(held) : 0;
   if (fits && one_each(items, g, tiles, bits, p.stream)) {
-    p.least = p.join_rows = 0;
+    p.least = p.start = p.join_rows = 0;
     p.groups = static_cast<int>(items);
     p.part_acc = p.part_ml = p.parts = 0;
     return p;
   }
   p.waves = 4;
   p.least = p.waves;
+  p.start = bits == 16 ? 4 : 8;
   const int64_t most = (items * tiles + p.waves - 1) / p.waves;
   const int64_t resident = 512;
   p.groups = static_cast<int>(std::min(most, resident));
@@ -1091,6 +1110,7 @@ hipError_t launch_decode(const Args& s, int bits, int items, const uint16_t* q, 
   a.items = items;
   a.score_rows = p.score_rows;
   a.least = p.least;
+  a.start = p.start;
   a.held_bytes = p.held_bytes;
   const hipError_t e = bits == 16 ? s.g > 4 ? launch<16, 2>(a, p, st) : launch<16, 1>(a, p, st)
                                   : s.g > 4 ? launch<4, 2>(a, p, st) : launch<4, 1>(a, p, st);

