@@ -477,12 +477,45 @@ __device__ __forceinline__ half4 code_operand(const uint4& gw, int s) {
 }
 constexpr float kCode = 262144.0f;       // 2^18
 
+// V codes less 8: in the mantissa of 1024 or 64, from which 1032 or 72 is taken.  A value is then scale x (code - 8) + (offset + 8 scale), whose
+// terms are about as large as the value.  (With scale x code + offset the sums of P V are differences of two sums many times as large:
+// 4 x 8 items of 90K to 128K slots 3.0e-6 of the outputs' norm off, 1.1e-6 so, for 1 to 3 % more time.  Scores, differences of single products' sums, gain
+// nothing by it.)
+struct Ones {                            // 1024 and 64 twice, in registers: an instruction takes one constant, the mask
+  uint32_t thousand = 0x64006400u, sixty = 0x54005400u;
+  __device__ __forceinline__ Ones() { asm volatile("" : "+v"(thousand), "+v"(sixty)); }
+};
+__device__ __forceinline__ half4 centred_operand(const uint4& gw, int s, const Ones& ones) {
+  uint32_t w0 = s < 4 ? gw.x : gw.z, w1 = s < 4 ? gw.y : gw.w;
+  if (s & 2) {
+    w0 >>= 8;
+    w1 >>= 8;
+  }
+  const uint32_t mask = s & 1 ? 0x00F000F0u : 0x000F000Fu, one = s & 1 ? ones.sixty : ones.thousand;
+  const half2v down = s & 1 ? half2v{-72, -72} : half2v{-1032, -1032};
+  Pack4 r;
+  r.p[0] = __builtin_bit_cast(half2v, (w0 & mask) | one) + down;
+  r.p[1] = __builtin_bit_cast(half2v, (w1 & mask) | one) + down;
+  return r.h;
+}
+
 // two numbers as fp16 pairs whose sums they are, to 22 bits, rounded to nearest (cut off they were low by 2^-21 on average, which the
 // codes' sum and the offsets' do not share)
 typedef float float2v __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void split_halves(float a, float b, half2v& hi, half2v& lo) {
   hi = __builtin_convertvector((float2v{a, b}), half2v);
   lo = __builtin_convertvector((float2v{a - static_cast<float>(hi[0]), b - static_cast<float>(hi[1])}), half2v);
+}
+
+// offset + 8 scale of four pairs
+__device__ __forceinline__ void centres(uint32_t s01, uint32_t s23, uint32_t m01, uint32_t m23, Pack4& hi, Pack4& lo) {
+  const uint32_t sc[2] = {s01, s23}, of[2] = {m01, m23};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const half2v a = __builtin_bit_cast(half2v, sc[i]), b = __builtin_bit_cast(half2v, of[i]);
+    split_halves(__builtin_fmaf(8.f, static_cast<float>(a[0]), static_cast<float>(b[0])), __builtin_fmaf(8.f, static_cast<float>(a[1]), static_cast<float>(b[1])),
+                 hi.p[i], lo.p[i]);
+  }
 }
 
 constexpr int kQUp = 8;                  // the query's largest value is near 2^kQUp
@@ -570,6 +603,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
       qlo[hs][k] = static_cast<_Float16>(sg[k] - static_cast<float>(qhi[hs][k]));
     }
   }
+  const Ones ones;
   int ve = -126;                         // exponent of the largest V scale so far
   float vf = 0.f;                        // what p is multiplied by for it
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
@@ -597,7 +631,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   }
 #define RDKV_K_GROUP(G_)                                                                                           \
   {                                                                                                               \
-    __builtin_amdgcn_sched_barrier(0);                                                                            \
+    \
     const uint4 gw = kr[G_];                                                                                      \
     floatx4 dg[HS];                                                                                               \
     _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) dg[hs] = zero4;                                             \
@@ -643,9 +677,8 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
         vf = ldexpf(1.0f, -1 - ve);
       }
     }
-    Pack4 ob;
-    ob.u[0] = vm.z;
-    ob.u[1] = vm.w;
+    Pack4 ch, cl;
+    centres(vm.x, vm.y, vm.z, vm.w, ch, cl);
 #pragma unroll
     for (int hs = 0; hs < HS; ++hs) {
       Pack4 hi, lo;
@@ -653,40 +686,42 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
       for (int i = 0; i < 2; ++i) {
         split_halves(p[hs][2 * i], p[hs][2 * i + 1], hi.p[i], lo.p[i]);
       }
-      run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi.h, ob.h, run.offv[hs], 0, 0, 0);
-      run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo.h, ob.h, run.offv[hs], 0, 0, 0);
+      run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi.h, ch.h, run.offv[hs], 0, 0, 0);
+      run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo.h, ch.h, run.offv[hs], 0, 0, 0);
+      run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi.h, cl.h, run.offv[hs], 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < 4; ++i) p[hs][i] *= vf;
     }
-#define RDKV_PV_STEP(G_, A_)                                                                                   \
-  {                                                                                                            \
-    const half4 b = code_operand(gw, A_);                                                                      \
-    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) {                                                        \
-      run.acc[hs][G_] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi[hs].h, b, run.acc[hs][G_], 3, A_, 0);            \
-      run.acc[hs][G_] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo[hs].h, b, run.acc[hs][G_], 3, A_, 0);            \
-    }                                                                                                          \
+// (two channel groups side by side: a product waits for the one before it on the same accumulator)
+#define RDKV_PV_STEP(G_, A_)                                                                                              \
+  {                                                                                                                       \
+    const half4 b0 = centred_operand(vr[G_], A_, ones), b1 = centred_operand(vr[G_ + 1], A_, ones);                       \
+    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) {                                                                   \
+      run.acc[hs][G_] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi[hs][0].h, b0, run.acc[hs][G_], 3, A_, 0);                   \
+      run.acc[hs][G_ + 1] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi[hs][1].h, b1, run.acc[hs][G_ + 1], 3, A_, 0);           \
+      run.acc[hs][G_] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo[hs][0].h, b0, run.acc[hs][G_], 3, A_, 0);                   \
+      run.acc[hs][G_ + 1] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo[hs][1].h, b1, run.acc[hs][G_ + 1], 3, A_, 0);           \
+    }                                                                                                                     \
   }
-#define RDKV_PV_GROUP(G_)                                                                                      \
-  {                                                                                                            \
-    __builtin_amdgcn_sched_barrier(0);                                                                         \
-    Pack4 sv, hi[HS], lo[HS];                                                                                  \
-    sv.u[0] = quad_bcast<G_>(vm.x); sv.u[1] = quad_bcast<G_>(vm.y);                                            \
-    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs) {                                                        \
-      _Pragma("unroll") for (int i = 0; i < 2; ++i) {                                                          \
-        split_halves(p[hs][2 * i] * static_cast<float>(sv.p[i][0]), p[hs][2 * i + 1] * static_cast<float>(sv.p[i][1]), hi[hs].p[i], lo[hs].p[i]); \
-      }                                                                                                        \
-    }                                                                                                          \
-    const uint4 gw = vr[G_];                                                                                   \
-    RDKV_PV_STEP(G_, 0) RDKV_PV_STEP(G_, 1) RDKV_PV_STEP(G_, 2) RDKV_PV_STEP(G_, 3)                            \
-    RDKV_PV_STEP(G_, 4) RDKV_PV_STEP(G_, 5) RDKV_PV_STEP(G_, 6) RDKV_PV_STEP(G_, 7)                            \
+#define RDKV_PV_GROUPS(G_)                                                                                                \
+  {                                                                                                                       \
+    Pack4 sv[2], hi[HS][2], lo[HS][2];                                                                                    \
+    sv[0].u[0] = quad_bcast<G_>(vm.x); sv[0].u[1] = quad_bcast<G_>(vm.y);                                                 \
+    sv[1].u[0] = quad_bcast<G_ + 1>(vm.x); sv[1].u[1] = quad_bcast<G_ + 1>(vm.y);                                         \
+    _Pragma("unroll") for (int hs = 0; hs < HS; ++hs)                                                                     \
+      _Pragma("unroll") for (int k = 0; k < 2; ++k)                                                                       \
+        _Pragma("unroll") for (int i = 0; i < 2; ++i)                                                                     \
+          split_halves(p[hs][2 * i] * static_cast<float>(sv[k].p[i][0]), p[hs][2 * i + 1] * static_cast<float>(sv[k].p[i][1]), \
+                       hi[hs][k].p[i], lo[hs][k].p[i]);                                                                   \
+    RDKV_PV_STEP(G_, 0) RDKV_PV_STEP(G_, 1) RDKV_PV_STEP(G_, 2) RDKV_PV_STEP(G_, 3)                                       \
+    RDKV_PV_STEP(G_, 4) RDKV_PV_STEP(G_, 5) RDKV_PV_STEP(G_, 6) RDKV_PV_STEP(G_, 7)                                       \
   }
-    RDKV_PV_GROUP(0) RDKV_PV_GROUP(1) RDKV_PV_GROUP(2) RDKV_PV_GROUP(3)
-#undef RDKV_PV_GROUP
+    RDKV_PV_GROUPS(0) RDKV_PV_GROUPS(2)
+#undef RDKV_PV_GROUPS
 #undef RDKV_PV_STEP
     load_v(next, next_rows);
   }
-  // what brings the accumulators to the sums' scale: 2^18 of the codes, 2^(1 + ve) of vf
-  return ldexpf(1.0f, 19 + ve);
+  return ldexpf(1.0f, 1 + ve);           // what brings the accumulators to the sums' scale, vf's inverse
 }
 
 // ---- the end of a piece --------------------------------------------------------------------------------------------------------------

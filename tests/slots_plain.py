@@ -24,16 +24,17 @@ def held(rows, bits):
     return O.dequantize_groups(c.reshape(n, 4, 32), s, m).reshape(n, D)
 
 
-def terms(rows, bits):
-    """Sizes of the terms that a kernel adds up for these rows' values.  Of 4-bit rows those are scale x code and the offset, each
-    multiplied and summed by itself and rounded relative to itself, wherever they nearly cancel: off by 2^-24 of their sizes per
-    operation, not of the value's."""
+def terms(rows, bits, centre=0):
+    """Sizes of the terms that a kernel adds up for these rows' values.  Of 4-bit rows those are scale x (code - centre) and
+    offset + centre x scale (centre 0 in K rows, 8 in V rows), each multiplied and summed by itself and rounded relative to itself,
+    wherever they nearly cancel: off by 2^-24 of their sizes per operation, not of the value's."""
     rows = np.asarray(rows, np.float32)
     if bits == 16:
         return np.abs(rows).astype(np.float64)
     c, s, m = O.quantize_rows(rows, 4)
     n = rows.shape[0]
-    return (np.abs(O.dequantize_groups(c.reshape(n, 4, 32), s, 0 * m)) + np.abs(m.astype(np.float64))[..., None]).reshape(n, D)
+    s, m = s.astype(np.float64), m.astype(np.float64)
+    return (np.abs(s[..., None] * (c.reshape(n, 4, 32).astype(np.float64) - centre)) + np.abs(m + centre * s)[..., None]).reshape(n, D)
 
 
 def choose(T, capacity, sinks, recent, w):
@@ -106,7 +107,7 @@ class Item:
     def put(self, at, k, v):
         """float32 rows into slots `at`."""
         self.K[at], self.V[at] = held(k, self.bits), held(v, self.bits)
-        self.K_size[at], self.V_size[at] = terms(k, self.bits), terms(v, self.bits)
+        self.K_size[at], self.V_size[at] = terms(k, self.bits), terms(v, self.bits, 8)
 
     def fill(self, K, V, w):
         T = K.shape[0]

@@ -709,7 +709,7 @@ def test_past_four_gigabytes(bits):
     assert slot.item() == gone and s.next_pos.item() == n + 1 and s.pos[0, 0, gone].item() == n
     out, lse = b.rdkv_slots_decode_attn(s, cuda(q, BF))
     # every other row is zeros: their scores are 0, their values nothing
-    kh, vh, kt, vt = (f(x[0], bits) for f in (P.held, P.terms) for x in (k, v))
+    kh, vh, kt, vt = P.held(k[0], bits), P.held(v[0], bits), P.terms(k[0], bits), P.terms(v[0], bits, 8)
     x = (q[0].astype(np.float64) @ kh[0]).item() / math.sqrt(D)
     off = 2.0 ** -24 * 138 * (np.abs(q[0]).astype(np.float64) @ kt[0]).item() / math.sqrt(D)
     total = math.exp(x) + n - 1
