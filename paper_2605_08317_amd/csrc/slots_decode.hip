@@ -52,7 +52,7 @@ struct DecodeArgs {
 //   17.7 and 17.1 (finding the pieces costs half a microsecond)
 //   starts of 0, 4, 8 and 14 places: bf16, 8 heads, 320 items of 1 to 4000 slots 100, 77, 78, 82, all of 4000 143, 142, 143, 145, 240 of 20
 //   to 20000, more short ones than long, 194, 133, 134, 136; 4 bits 68, 56, 49, 51; 71, 69, 68, 74; 123, 70, 65, 66
-constexpr int kHeldLengths = 1024;
+constexpr int kHeldLengths = 8192;
 struct Lengths {                         // of the items: in LDS, where there is room
   const DecodeArgs& a;
   const int* s_len;
@@ -819,6 +819,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
   if constexpr (NWV == 4) {
     int* s_len = reinterpret_cast<int*>(smem);
     if (a.items <= kHeldLengths) {
+#pragma unroll 8
       for (int i = tid; i < a.items; i += NWV * 64) s_len[i] = a.s.length(i);
       __syncthreads();
     }
@@ -1110,6 +1111,7 @@ hipError_t launch_one(const DecodeArgs& a, const Plan& p, hipStream_t st) {
   const size_t lds = NWV == 8 ? lds_of_eight(BITS, a.s.g, a.held_bytes)
                               : NWV * ((BITS == 16 ? kHalfBytes : 0) + held_bytes_of_four(BITS)) + (ml_floats<NWV, HS>() + 8) * sizeof(float) +
                                     (BITS == 16 && HS == 2 ? kQueryBytes : 0);
+  static_assert(NWV * held_bytes_of_four(BITS) >= kHeldLengths * 4 + 4 * kTries * 8, "the lengths fit");
   static_assert(held_bytes_of_four(4) >= 4 * HS * kHeadDim * 4 && kHalfBytes >= 4 * HS * kHeadDim * 4, "the accumulators fit");
   const hipError_t e = RDKV_ALLOW_LDS((decode_kernel<BITS, HS, NWV, STREAM>), NWV == 8 ? kMostLds : lds);
   if (e != hipSuccess) return e;

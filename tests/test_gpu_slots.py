@@ -598,6 +598,34 @@ def test_decode_of_items_that_share_workgroups(batch, bits, capacity):
     check_step(s, items, q, out, lse, s.weight, before)
 
 
+def test_decode_of_thousands_of_items():
+    """One step of 8240 items against steps of 412 of them.  Both add up the same fp32 scores' exponentials in another order: each is off by
+    (2 x the scores' error + sums + 2^-20) of the largest value, as in check_step."""
+    g = torch.Generator(device="cuda").manual_seed(26)
+    batch, capacity, some = 2060, 2600, 150
+    rand = lambda *shape: torch.randn(shape, device="cuda", generator=g)
+    s = b.Slots(batch, 32, 4, capacity)
+    s.k[:, :, :some], s.v[:, :, :some] = rand(batch, 4, some, D).to(BF), rand(batch, 4, some, D).to(BF)
+    s.lens.copy_(torch.randint(0, some + 1, (batch, 4), device="cuda", generator=g, dtype=I32))
+    s.lens[7, 2] = s.lens[2000, 3] = capacity
+    s.lens[-1] = 0
+    q = rand(batch, 32, D).to(BF)
+    out, lse = b.rdkv_slots_decode_attn(s, q)
+    weight = s.weight.clone()
+    s.weight.zero_()
+    # a score: 130 roundings of the sum of its terms' sizes, at most |q| |k| / sqrt d < 30
+    off = 2.0 ** -24 * 138 * 30
+    rel = 2 * (2 * off + P.sums_off(capacity) + 2.0 ** -20)
+    for i in range(0, batch, 103):
+        part = slice(i, i + 103)
+        t = b.Slots(103, 32, 4, capacity, k=s.k[part], v=s.v[part], pos=s.pos[part], weight=s.weight[part], lens=s.lens[part], next_pos=s.next_pos[part])
+        out1, lse1 = b.rdkv_slots_decode_attn(t, q[part])
+        assert (out[part] - out1).abs().max() <= rel * s.v.abs().max()
+        assert torch.equal(lse[part].isneginf(), lse1.isneginf())
+        assert (lse[part] - lse1).nan_to_num().abs().max() <= rel
+        assert ((weight[part] - s.weight[part]).abs() <= rel * s.weight[part] + 1e-30).all()
+
+
 @pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("hq, batch, capacity", [(2, 1, 300), (8, 3, 9000), (16, 140, 3600)])
 def test_empty_caches(hq, batch, capacity, bits):
