@@ -408,7 +408,7 @@ typedef struct rdkv_slots {
   int32_t sinks, recent;    /* never evicted: tokens at positions below `sinks`, and the newest `recent` ones;
                                sinks + max(recent, 1) <= capacity */
   int32_t window;           /* 0, or: a step sees tokens less than `window` positions back, and those below `sinks` */
-  float score_cap;          /* 0, or c > 0: scores become c tanh(score / c) */
+  float score_cap;          /* 0, or a normal number c > 0: scores become c tanh(score / c) */
   float decay;              /* in [0, 1]: what a step multiplies gathered weights by before it adds its own */
   const float* slopes;      /* DEVICE [hq] or NULL: slopes[h] times the distance in positions is taken from a score of head h */
   void* k;                  /* DEVICE, rdkv_slots_side_bytes() each */

@@ -23,7 +23,8 @@ rdkv_status check_slots(const rdkv_slots* s, bool memory) {
   if (s->sinks < 0 || s->recent < 0 || s->window < 0) return fail(RDKV_ERR_INVALID_ARG, "sinks, recent and window must not be negative");
   if (static_cast<int64_t>(s->sinks) + std::max(s->recent, 1) > s->capacity)
     return fail(RDKV_ERR_SHAPE, "%d sinks and %d recent tokens leave no slot of %d to evict from", s->sinks, s->recent, s->capacity);
-  if (!(s->score_cap >= 0.f) || !std::isfinite(s->score_cap)) return fail(RDKV_ERR_INVALID_ARG, "score_cap must be finite and >= 0");
+  if (s->score_cap != 0.f && !(s->score_cap > 0.f && std::isnormal(s->score_cap)))        // (its inverse is finite)
+    return fail(RDKV_ERR_INVALID_ARG, "score_cap must be 0 or a normal number > 0");
   if (!(s->decay >= 0.f) || s->decay > 1.f) return fail(RDKV_ERR_INVALID_ARG, "decay must be in [0, 1]");
   const int64_t items = static_cast<int64_t>(s->batch) * s->hkv;
   if (items * (static_cast<int64_t>(s->capacity) + kTile64) >= (1ll << 31)) return fail(RDKV_ERR_SHAPE, "batch * hkv * capacity exceeds 2^31 slots");

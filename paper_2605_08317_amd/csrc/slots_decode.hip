@@ -8,7 +8,7 @@
 //              every probability once the whole sum is known: 4 bytes per slot and query head, which stay in the caches
 //   precision  products of the query and of probabilities lose nothing that fp32 holds: bf16 rows meet a probability in three bf16 terms
 //              (24 bits), codes in two fp16 terms (22 bits), scaled so that the largest V scale seen stands just below fp16's largest
-//              and the query's largest value near one
+//              and the query's largest value near 2^8
 //   bound      HBM: 512 bytes a slot in bf16, 160 in 4 bits, and the scores.  4 x 8 items of 128K slots 6.8 and 6.1 TB/s without weights, 5.5
 //              and 4.6 with them; items one each to a workgroup 6.3 TB/s (256 of 4000 slots in bf16) and 4.8.  Small caches: latency
 //   work       lengths are on the device.  A workgroup takes an item, where there are enough for the card; otherwise it finds its piece

@@ -35,7 +35,7 @@ def calls(c, seq=(5, 5), first=0, w=16, ws=None, ws_bytes=0):
     (dict(hq=6), SHAPE), (dict(hq=32), SHAPE), (dict(capacity=0), SHAPE), (dict(capacity=-5), SHAPE), (dict(bits=8), SHAPE), (dict(bits=2), SHAPE),
     (dict(sinks=-1), INVALID), (dict(recent=-1), INVALID), (dict(window=-1), INVALID), (dict(sinks=100), SHAPE), (dict(sinks=60, recent=41), SHAPE),
     (dict(sinks=2 ** 31 - 1, recent=2 ** 31 - 1), SHAPE), (dict(score_cap=-1.0), INVALID), (dict(score_cap=float("nan")), INVALID),
-    (dict(score_cap=float("inf")), INVALID), (dict(decay=-0.1), INVALID), (dict(decay=1.5), INVALID), (dict(decay=float("nan")), INVALID),
+    (dict(score_cap=float("inf")), INVALID), (dict(score_cap=1e-40), INVALID), (dict(decay=-0.1), INVALID), (dict(decay=1.5), INVALID), (dict(decay=float("nan")), INVALID),
     (dict(batch=2 ** 20, capacity=2 ** 12), SHAPE), (dict(batch=2 ** 19, capacity=1), SHAPE), (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(pos=None), INVALID), (dict(len=None), INVALID),
     (dict(next=None), INVALID), (dict(k=24), INVALID), (dict(v=17), INVALID)])
 def test_a_bad_struct_is_refused_by_every_call(kw, status):
