@@ -205,7 +205,7 @@ __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int 
 
 // Online softmax in the lanes (block, head); acc: whatever is scaled with the sums
 template <int HS>
-__device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& run, float (&p)[HS][4], float exponent) {
+__device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& run, float (&p)[HS][4]) {
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
     const float most = max_of_four(x[hs][0], x[hs][1], x[hs][2], x[hs][3]);
@@ -224,10 +224,9 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& r
       }
       run.m[hs] = m_new;
     }
-    const float up = exponent - run.m[hs];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      p[hs][i] = fast_exp2(x[hs][i] + up);
+      p[hs][i] = fast_exp2(x[hs][i] - run.m[hs]);
       run.l[hs] += p[hs][i];
     }
   }
@@ -434,7 +433,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
     held.put<HS, NWV>(sc, tile, next >= t1, xt);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
-    softmax_step<HS>(x, run, p, 0.f);
+    softmax_step<HS>(x, run, p);
     short4v t[HS][3];
 #pragma unroll
     for (int hs = 0; hs < HS; ++hs) split_bf16_3(p[hs], t[hs]);
@@ -479,7 +478,7 @@ constexpr float kCode = 262144.0f;       // 2^18
 
 // V codes less 8: in the mantissa of 1024 or 64, from which 1032 or 72 is taken.  A value is then scale x (code - 8) + (offset + 8 scale), whose
 // terms are about as large as the value.  (With scale x code + offset the sums of P V are differences of two sums many times as large:
-// 4 x 8 items of 90K to 128K slots 3.0e-6 of the outputs' norm off, 1.1e-6 so, for 1 to 3 % more time.  Scores, differences of single products' sums, gain
+// 4 x 8 items of 90K to 128K slots 3.0e-6 of the outputs' norm off, 1.0e-6 so, for 1 to 3 % more time.  Scores, differences of single products' sums, gain
 // nothing by it.)
 struct Ones {                            // 1024 and 64 twice, in registers: an instruction takes one constant, the mask
   uint32_t thousand = 0x64006400u, sixty = 0x54005400u;
@@ -519,8 +518,10 @@ __device__ __forceinline__ void centres(uint32_t s01, uint32_t s23, uint32_t m01
 }
 
 constexpr int kQUp = 8;                  // the query's largest value is near 2^kQUp
-constexpr float kPUp = 15.0f;            // probabilities are carried times 2^kPUp
+constexpr int kPUp = 15;                 // probabilities go into fp16 terms times 2^kPUp.  (Not through the exponentials: x - m + 15 has four bits
+                                         // less behind the point than x - m near 0, 5e-7 of a probability)
 
+constexpr float kPScale = 1 << kPUp;
 __device__ __forceinline__ int exponent_of(float x) {      // of a number > 0; bounds for the others
   return static_cast<int>((__float_as_uint(x) >> 23) & 255u) - 127;
 }
@@ -650,7 +651,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     held.put<HS, NWV>(sc, tile, next >= t1, xt);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
-    softmax_step<HS>(x, run, p, kPUp);
+    softmax_step<HS>(x, run, p);
 
     // ---- P V ---------------------------------------------------------------------------------------------------------
     uint4 vm = vmeta;
@@ -674,7 +675,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 #pragma unroll
             for (int i = 0; i < 4; ++i) run.acc[hs][grp][i] *= down;
         ve = e;
-        vf = ldexpf(1.0f, -1 - ve);
+        vf = ldexpf(1.0f, kPUp - 1 - ve);
       }
     }
     Pack4 ch, cl;
@@ -684,7 +685,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
       Pack4 hi, lo;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        split_halves(p[hs][2 * i], p[hs][2 * i + 1], hi.p[i], lo.p[i]);
+        split_halves(p[hs][2 * i] * kPScale, p[hs][2 * i + 1] * kPScale, hi.p[i], lo.p[i]);
       }
       run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(hi.h, ch.h, run.offv[hs], 0, 0, 0);
       run.offv[hs] = __builtin_amdgcn_mfma_f32_4x4x4f16(lo.h, ch.h, run.offv[hs], 0, 0, 0);
@@ -721,7 +722,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 #undef RDKV_PV_STEP
     load_v(next, next_rows);
   }
-  return ldexpf(1.0f, 1 + ve);           // what brings the accumulators to the sums' scale, vf's inverse
+  return ldexpf(1.0f, 1 + ve - kPUp);    // what brings the accumulators to the sums' scale, vf's inverse
 }
 
 // ---- the end of a piece --------------------------------------------------------------------------------------------------------------
@@ -911,11 +912,11 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
         off = lo + hi;
         off += dpp_f32<0x124>(off);
         off += dpp_f32<0x128>(off);
-        if ((lane & 12) == 0) s_ml[ml_at<HS>(wave, 4 * hs + (lane >> 4), lane & 3) + 2] = off;
+        if ((lane & 12) == 0) s_ml[ml_at<HS>(wave, 4 * hs + (lane >> 4), lane & 3) + 2] = off * (1.0f / kPScale);
       }
       if (lane < 16)                     // (block, j) -> group block of head j
         *reinterpret_cast<float2*>(s_ml + ml_at<HS>(wave, 4 * hs + (lane & 3), lane >> 2)) =
-            make_float2(BITS == 4 ? run.m[hs] - kPUp : run.m[hs], run.l[hs]);
+            make_float2(run.m[hs], run.l[hs]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int head = 4 * hs + i;
