@@ -48,8 +48,8 @@ struct DecodeArgs {
 // does, the items are a line, on which each has `start` places and then its tiles, workgroup w has the places from w * share on, and some
 // have the end of one item and the begin of the next, or several: each is a start and a merge, as long as `start` tiles take to pass (4 in
 // bf16, 8 in 4 bits).
-//   pieces and the line, us: 4 bits, 8 heads, 128 items of 4000 slots 36.1 and 41.0, 64 of them 26.6 and 31.5, 8 19.2 and 22.5; 8 of 2000
-//   17.7 and 17.1 (finding the pieces costs half a microsecond)
+//   pieces and the line (a start counting nothing), us: 4 bits, 8 heads, 128 items of 4000 slots 35.0 and 41.0, 64 of them 26.9 and 31.5, 8
+//   19.1 and 22.5; 8 of 2000 17.8 and 17.1 (finding the pieces costs half a microsecond)
 //   starts of 0, 4, 8 and 14 places: bf16, 8 heads, 320 items of 1 to 4000 slots 100, 77, 78, 82, all of 4000 143, 142, 143, 145, 240 of 20
 //   to 20000, more short ones than long, 194, 133, 134, 136; 4 bits 68, 56, 49, 51; 71, 69, 68, 74; 123, 70, 65, 66
 constexpr int kHeldLengths = 8192;
@@ -1054,9 +1054,9 @@ constexpr size_t kMostLds = 160 << 10;
 //                     64 of 1500  22.5, 22.6   of 4000  47.0, 32.6   128 of 2500  38.4, 39.2   of 4000  51.9, 52.4 (lengths of 1300 to
 //                     4000 46.8, 37.1)   256 of 4000  82.5, 98.6   512 of 2000  87.6, 100.9
 //   bf16, 8 heads     8 of 2000  24.2, 19.1   32 of 1500  20.4, 19.9   64 of 1500  24.7, 26.6   128 of 2500  39.1, 43.5   512 of 2000  90.5, 111.8
-//   4 bits, 4 heads   8 of 1000  8.8, 13.5   of 2000  13.8, 13.0   32 of 3000  19.8, 18.2   64 of 4000  25.7, 21.2   128 of 4000  26.9, 28.1
-//                     256 of 4000  33.9, 44.4
-//   4 bits, 8 heads   8 of 1000  12.1, 18.9   of 2000  19.4, 17.7   32 of 3000  27.3, 23.0   128 of 2500  26.5, 31.9   512 of 2000  47.5, 55.1
+//   4 bits, 4 heads   8 of 1000  9.0, 13.4   of 2000  14.3, 12.9   32 of 3000  20.5, 17.8   64 of 4000  26.6, 20.8   128 of 4000  27.1, 27.7
+//                     256 of 4000  33.7, 44.8
+//   4 bits, 8 heads   8 of 1000  12.4, 18.7   of 2000  20.0, 17.8   32 of 3000  28.3, 23.3   128 of 2500  27.0, 32.1   512 of 2000  49.8, 58.6
 bool one_each(int64_t items, int g, int64_t tiles, int bits, bool stream) {
   const bool wide = g > 4;
   const double own = bits == 4 ? (wide ? 0.5 : 0.31) : stream ? (wide ? 0.85 : 0.77) : (wide ? 0.53 : 0.42);
