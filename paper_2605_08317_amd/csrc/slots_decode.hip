@@ -27,7 +27,7 @@ using namespace tile;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRoot = 0.08838834764831845f;      // 1 / sqrt(128)
-constexpr float kLowest = -3.0e38f;          // a finite maximum of nothing
+constexpr float kLowest = -3.402823466e38f;        // a finite maximum of nothing: no score is below it
 
 struct DecodeArgs {
   Args s;

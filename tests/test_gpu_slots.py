@@ -638,6 +638,28 @@ def test_empty_caches(hq, batch, capacity, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("capacity", [100, 9000])
+def test_scores_near_the_lowest_number(capacity, bits):
+    """A bias of -2.2e38 a position: alone it takes the probability, beside another token none; -3e38, past what a score holds, is not seen."""
+    rng = np.random.default_rng(27)
+    for slope, seen in ((2.2e38, True), (3.0e38, False)):
+        s, items = loaded(rng, [1, 2], 4, 1, capacity, bits, slopes=torch.full((4,), slope, device="cuda"))
+        s.pos[0, 0, 0] = 10
+        s.next_pos[0] = 12                              # the token is one position back
+        s.pos[1, 0, :2] = torch.tensor([11, 10], device="cuda", dtype=I32)
+        s.next_pos[1] = 12
+        before = s.weight.clone()
+        out, lse = b.rdkv_slots_decode_attn(s, cuda(rng.standard_normal((2, 4, D)), BF))
+        if seen:
+            assert np.abs(host(out)[0] - items[0].V[0]).max() <= 2.0 ** -20 * items[0].V_size[0].max()
+            assert ((lse[0] + 2.2e38).abs() <= 2.2e38 * 2.0 ** -22).all() and abs((s.weight - before)[0, 0, 0].item() - 4) <= 2.0 ** -20 * (4 + before[0, 0, 0].item())
+        else:
+            assert not out[0].any() and torch.isneginf(lse[0]).all()
+        assert np.abs(host(out)[1] - items[1].V[0]).max() <= 2.0 ** -20 * items[1].V_size[0].max()
+        assert torch.isfinite(lse[1]).all() and s.weight[1, 0, 1] == before[1, 0, 1]
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("hq, capacity", [(8, 300), (8, 4000), (2, 5000), (16, 4000)])
 def test_scores_that_are_no_numbers_whichever_way_items_are_taken(hq, capacity, bits):
     rng = np.random.default_rng(22)
