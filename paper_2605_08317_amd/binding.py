@@ -150,6 +150,8 @@ lib = _load()
 try:
     from . import _rdkv_call as _call
     _call.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.rdkv_decode_attn, lib.rdkv_cache_append)))
+    _call.bind_slots(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.rdkv_slots_append, lib.rdkv_slots_decode_attn, lib.rdkv_slots_read, lib.rdkv_slots_fill, lib.rdkv_slots_fill_workspace_bytes)))
 except ImportError as e:
     _call = None
     warnings.warn(f"_rdkv_call.so is not built or does not fit this PyTorch ({e}): a decode step takes the host 2 us more; "
@@ -481,6 +483,7 @@ class Slots:
                         ("next", self.next_pos), ("slopes", self.slopes)):
             setattr(c, name, None if t is None else t.data_ptr())
         self.workspace_bytes = lib.rdkv_slots_decode_workspace_bytes(ctypes.byref(c))
+        self.address = ctypes.addressof(c)
 
     def ref(self):
         return ctypes.byref(self.c)
@@ -506,6 +509,12 @@ def _on(slots):
     return _SAME if index is None or _current_device is None or _current_device() == index else torch.cuda.device(index)
 
 
+def _fast(slots):
+    """Whether a call may go through the native code, which looks at the tensors itself: the slots lie on the current device."""
+    index = slots.device.index
+    return _call is not None and index is not None and _current_device is not None and _current_device() == index
+
+
 class _Same:
     def __enter__(self):
         pass
@@ -520,6 +529,9 @@ _SAME = _Same()
 def rdkv_slots_fill(slots, K, V, seq_lens, w_tok=None, first=0):
     """Prompts of len(seq_lens) sequences into the slots of sequences first, first + 1, ..: K, V bfloat16, w_tok float32 or
     None, ragged as everywhere."""
+    status = _call.slots_fill(slots.address, _stream(), slots.device.index, K, V, seq_lens, w_tok, first) if _fast(slots) else None
+    if status is not None:
+        return _check(status)
     n, first = len(seq_lens), _int32("first", first)
     lens = (ctypes.c_int32 * max(n, 1))(*[_int32("seq_lens", x) for x in seq_lens])
     rows = sum(max(x, 0) for x in lens[:n]) * slots.hkv
@@ -535,6 +547,11 @@ def rdkv_slots_fill(slots, K, V, seq_lens, w_tok=None, first=0):
 
 def rdkv_slots_append(slots, k_new, v_new, slot=None):
     """The slot that each item's new token took: int32 [batch, hkv]."""
+    done = _fast(slots) and _call.slots_append(slots.address, _stream(), slots.device.index, k_new, v_new, slot)
+    if done:
+        if done[0] != RDKV_OK:
+            _check(done[0])
+        return done[1]
     items = (slots.batch, slots.hkv)
     _tensor(k_new, items + (slots.d,), torch.bfloat16, slots.device, "k_new")
     _tensor(v_new, items + (slots.d,), torch.bfloat16, slots.device, "v_new")
@@ -548,6 +565,11 @@ def rdkv_slots_append(slots, k_new, v_new, slot=None):
 
 
 def rdkv_slots_decode_attn(slots, q, out=None, lse=None, workspace=None):
+    done = _fast(slots) and _call.slots_decode(slots.address, _stream(), slots.device.index, q, out, lse, workspace, slots.workspace_bytes)
+    if done:
+        if done[0] != RDKV_OK:
+            _check(done[0])
+        return done[1:]
     rows = (slots.batch, slots.hq)
     _tensor(q, rows + (slots.d,), torch.bfloat16, slots.device, "q")
     if out is None:
@@ -570,6 +592,11 @@ def rdkv_slots_decode_attn(slots, q, out=None, lse=None, workspace=None):
 
 def rdkv_slots_read(slots, index=None, n=None, K=None, V=None):
     """(K, V) bfloat16 [batch, hkv, n, 128]: rows of slots `index` (int32 [batch, hkv, n]), or of the first n slots (all)."""
+    done = _fast(slots) and _call.slots_read(slots.address, _stream(), slots.device.index, index, n, K, V)
+    if done:
+        if done[0] != RDKV_OK:
+            _check(done[0])
+        return done[1:]
     if index is not None:
         if index.dim() != 3 or n not in (None, index.shape[2]):
             raise ValueError(f"index must be [batch, hkv, n]: got {tuple(index.shape)}")

@@ -791,3 +791,73 @@ def test_past_four_gigabytes(bits):
     assert torch.equal(s.pos[0, 0].long(), mark[kept]) and s.lens.item() == n
     for c in range(4):
         assert torch.equal(s.k[0, 0, :, c], rows[:, c][kept]) and torch.equal(s.v[0, 0, :, c], rows[:, c][kept])
+
+
+# ---- the calls from Python: native code and ctypes --------------------------------------------------------------------------------------
+
+def test_native_code_and_ctypes_make_the_same_calls(monkeypatch):
+    rng = np.random.default_rng(28)
+    s, _ = loaded(rng, [300, 120], 8, 2, 300, 4, garbage=False)
+    k, v, q = (cuda(rng.standard_normal((2, n, D)), BF) for n in (2, 2, 8))
+    index = cuda(rng.integers(-2, 310, (2, 2, 9)), I32)
+
+    prompts = [310, 9000]
+    K, V, w = (cuda(rng.standard_normal(n), t) for n, t in ((2 * sum(prompts) * D, BF), (2 * sum(prompts) * D, BF), (2 * sum(prompts), F32)))
+
+    def every(s):
+        t = clone(s)
+        assert b.rdkv_slots_fill(t, K, V.view(-1, D), prompts, w.view(2, -1)) is None
+        b.rdkv_slots_fill(t, K[:2 * 310 * D], V[:2 * 310 * D], (310,), w[:620], first=1)
+        b.rdkv_slots_fill(t, K[:0], V[:0], [0])
+        filled = [t.k.clone(), t.v.clone(), t.pos.clone(), t.weight.clone(), t.lens.clone(), t.next_pos.clone()]
+        made = [b.rdkv_slots_append(s, k, v), *b.rdkv_slots_decode_attn(s, q), *b.rdkv_slots_read(s, index), *b.rdkv_slots_read(s), *b.rdkv_slots_read(s, n=7)]
+        given = [torch.zeros_like(t) for t in made[:5]]
+        r = [b.rdkv_slots_append(s, k, v, given[0]), *b.rdkv_slots_decode_attn(s, q, given[1], given[2], s.workspace()), *b.rdkv_slots_read(s, index, 9, given[3], given[4])]
+        assert all(x is y for x, y in zip(r, given))
+        one = b.rdkv_slots_decode_attn(s, q, lse=given[2])
+        assert isinstance(one, tuple) and one[1] is given[2]
+        return filled + [t.clone() for t in made + given] + [one[0], s.weight.clone(), s.k.clone(), s.lens.clone(), s.next_pos.clone()]
+    assert b._call is not None
+    a = every(clone(s))
+    monkeypatch.setattr(b, "_call", None)
+    for x, y in zip(a, every(clone(s))):
+        assert x.dtype == y.dtype and x.shape == y.shape and x.device == y.device and x.is_contiguous() and torch.equal(x, y)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_the_binding_refuses_on_the_gpu_what_it_refuses_elsewhere(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(b, "_call", None)
+    s = b.Slots(2, 8, 2, 100)
+    new, q = torch.zeros((2, 2, D), device="cuda", dtype=BF), torch.zeros((2, 8, D), device="cuda", dtype=BF)
+    wide = torch.zeros((2, 8, 2 * D), device="cuda", dtype=BF)[:, :, ::2]
+    index = torch.zeros((2, 2, 3), device="cuda", dtype=I32)
+    for call in (lambda: b.rdkv_slots_append(s, new.float(), new), lambda: b.rdkv_slots_append(s, new, new[:1]), lambda: b.rdkv_slots_append(s, new, new.cpu()),
+                 lambda: b.rdkv_slots_append(s, new, new, torch.zeros((2, 2), device="cuda")), lambda: b.rdkv_slots_append(s, new, new, index),
+                 lambda: b.rdkv_slots_decode_attn(s, wide), lambda: b.rdkv_slots_decode_attn(s, q.cpu()), lambda: b.rdkv_slots_decode_attn(s, q, q),
+                 lambda: b.rdkv_slots_decode_attn(s, q, lse=torch.zeros((2, 7), device="cuda")), lambda: b.rdkv_slots_decode_attn(s, q, workspace=s.workspace().cpu()),
+                 lambda: b.rdkv_slots_decode_attn(s, q, workspace=torch.zeros(4096, device="cuda")), lambda: b.rdkv_slots_read(s, index.long()),
+                 lambda: b.rdkv_slots_read(s, index, 4), lambda: b.rdkv_slots_read(s, index[0]), lambda: b.rdkv_slots_read(s, n=2 ** 32),
+                 lambda: b.rdkv_slots_read(s, index, K=new), lambda: b.rdkv_slots_fill(s, new, new, [3]), lambda: b.rdkv_slots_fill(s, q, q, [4, 4], new),
+                 lambda: b.rdkv_slots_fill(s, q.cpu(), q, [4, 4]), lambda: b.rdkv_slots_fill(s, wide[:, :, :D], q, [4, 4]),
+                 lambda: b.rdkv_slots_fill(s, q, q, [4, 2 ** 32 + 4]), lambda: b.rdkv_slots_fill(s, q, q, [4, 4], first=2 ** 32)):
+        with pytest.raises((ValueError, RuntimeError)) as e:
+            call()
+        assert not isinstance(e.value, b.RdkvError)
+    for call in (lambda: b.rdkv_slots_read(s, n=-1), lambda: b.rdkv_slots_fill(s, q, q, [4, 4], first=1), lambda: b.rdkv_slots_fill(s, q, q, [4, 4], first=-1),
+                 lambda: b.rdkv_slots_fill(s, q, q, [8, -1]), lambda: b.rdkv_slots_fill(b.Slots(1, 8, 2, 7), q, q, [8]),
+                 lambda: b.rdkv_slots_decode_attn(b.Slots(2, 8, 2, 9000), q, workspace=torch.zeros(64, device="cuda", dtype=torch.uint8))):
+        with pytest.raises(b.RdkvError):
+            call()
+    assert not s.lens.any() and not s.next_pos.any()
+
+
+def test_subclasses_take_the_way_that_asks_them():
+    class Own(torch.Tensor):
+        pass
+    s = b.Slots(2, 8, 2, 100)
+    new, q = torch.ones((2, 2, D), device="cuda", dtype=BF), torch.ones((2, 8, D), device="cuda", dtype=BF)
+    slot = b.rdkv_slots_append(s, new.as_subclass(Own), new)
+    assert not slot.any() and (s.lens == 1).all()
+    out, lse = b.rdkv_slots_decode_attn(s, q.as_subclass(Own))
+    assert torch.equal(out, torch.ones_like(out))
