@@ -1,5 +1,5 @@
-"""Thin binding of librdkv (include/rdkv.h): ctypes, and for the two calls of a
-decode loop native code (_rdkv_call, csrc/rdkv_call.cpp), which makes the same calls
+"""Thin binding of librdkv (include/rdkv.h): ctypes, and for the calls of decode
+loops native code (_rdkv_call, csrc/rdkv_call.cpp), which makes the same calls
 for less host time; where it does not load, ctypes makes them and a warning says so.
 
 Argument marshalling only: every step of the path runs in the HIP kernels of the
