@@ -27,6 +27,7 @@ using namespace tile;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRoot = 0.08838834764831845f;      // 1 / sqrt(128)
+constexpr float kRootLog2e = 0.12751743f;          // both: 0.0883883476 x 1.4426950409 = 0.12751743 (to 2^-25)
 constexpr float kLowest = -3.402823466e38f;        // a finite maximum of nothing: no score is below it
 
 struct DecodeArgs {
@@ -173,17 +174,22 @@ __device__ __forceinline__ int position(const Scoring& sc, int tile, int rows) {
   return static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(of, 4 * (threadIdx.x & 63), 0, 0));
 }
 
-// xt: products q k over unit; comes back as scores times log2(e), -inf where the slot is not seen.  The slots that are.
+// What makes scores times log2(e) of what score_tile leaves: their last product, which the exponentials take in with the maximum's
+// difference, so that what is rounded is small where the probability is not (8 items of 3700 slots in bf16: outputs 6.4e-7 -> 5.8e-7 off).
+__device__ __forceinline__ float last_factor(const Scoring& sc, float unit) { return sc.cap > 0.f || sc.biased ? kLog2e : unit * kRootLog2e; }
+// xt: products q k over a power of two, unit; comes back as scores over last_factor, -inf where the slot is not seen.  The slots that are.
 template <int HS>
 __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int pos, float unit, float (&xt)[HS][4]) {
   const int lane = threadIdx.x & 63, row = tile * kTile + lane;
   bool seen = row < sc.n;
   const int away = sc.at - pos;
   if (sc.window > 0) seen = seen && (away < sc.window || pos < sc.sinks);
+  if (sc.cap > 0.f || sc.biased) {
 #pragma unroll
-  for (int hs = 0; hs < HS; ++hs)
+    for (int hs = 0; hs < HS; ++hs)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) xt[hs][i] *= unit;
+      for (int i = 0; i < 4; ++i) xt[hs][i] *= unit * kRoot;
+  }
   if (sc.cap > 0.f) {
 #pragma unroll
     for (int hs = 0; hs < HS; ++hs)
@@ -199,16 +205,16 @@ __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int 
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) xt[hs][i] = seen ? xt[hs][i] * kLog2e : -INFINITY;
+    for (int i = 0; i < 4; ++i) xt[hs][i] = seen ? xt[hs][i] : -INFINITY;
   return __builtin_amdgcn_ballot_w64(seen);
 }
 
-// Online softmax in the lanes (block, head); acc: whatever is scaled with the sums
+// Online softmax of scores x times factor in the lanes (block, head); acc: whatever is scaled with the sums
 template <int HS>
-__device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& run, float (&p)[HS][4]) {
+__device__ __forceinline__ void softmax_step(const float (&x)[HS][4], float factor, Run<HS>& run, float (&p)[HS][4]) {
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
-    const float most = max_of_four(x[hs][0], x[hs][1], x[hs][2], x[hs][3]);
+    const float most = max_of_four(x[hs][0], x[hs][1], x[hs][2], x[hs][3]) * factor;
     if (__any(most > run.m[hs])) {
       const float m_new = fmaxf(run.m[hs], head_max(most));
       const float alpha = fast_exp2(run.m[hs] - m_new);
@@ -226,7 +232,7 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], Run<HS>& r
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      p[hs][i] = fast_exp2(x[hs][i] - run.m[hs]);
+      p[hs][i] = fast_exp2(__builtin_fmaf(x[hs][i], factor, -run.m[hs]));
       run.l[hs] += p[hs][i];
     }
   }
@@ -241,17 +247,17 @@ struct Held {
   uint8_t* at;         // of this wavefront: [tiles][64][g]
   int n, most;         // tiles there, and room; most 0: all of the item's stay
   template <int HS, int NWV>
-  __device__ __forceinline__ void put(const Scoring& sc, int tile, bool last, const float (&xt)[HS][4]) {
+  __device__ __forceinline__ void put(const Scoring& sc, int tile, bool last, const float (&xt)[HS][4], float f) {
     if (!sc.tracked) return;
     const int lane = threadIdx.x & 63;
     float* dst = reinterpret_cast<float*>(at) + (n * kTile + lane) * sc.g;
     if constexpr (HS == 2) {
-      *reinterpret_cast<float4*>(dst) = make_float4(xt[0][0], xt[0][1], xt[0][2], xt[0][3]);
-      *reinterpret_cast<float4*>(dst + 4) = make_float4(xt[1][0], xt[1][1], xt[1][2], xt[1][3]);
+      *reinterpret_cast<float4*>(dst) = make_float4(f * xt[0][0], f * xt[0][1], f * xt[0][2], f * xt[0][3]);
+      *reinterpret_cast<float4*>(dst + 4) = make_float4(f * xt[1][0], f * xt[1][1], f * xt[1][2], f * xt[1][3]);
     } else {
-      if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(xt[0][0], xt[0][1], xt[0][2], xt[0][3]);
-      else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(xt[0][0], xt[0][1]);
-      else *dst = xt[0][0];
+      if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(f * xt[0][0], f * xt[0][1], f * xt[0][2], f * xt[0][3]);
+      else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(f * xt[0][0], f * xt[0][1]);
+      else *dst = f * xt[0][0];
     }
     ++n;
     if (n == most || (last && most > 0)) {
@@ -393,6 +399,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
       for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(qa[hs][i].x), "+v"(qa[hs][i].y), "+v"(qa[hs][i].z), "+v"(qa[hs][i].w));
   }
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
+  const float factor = last_factor(sc, 1.f);
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
     const int next = tile + NWV, next_rows = next < t1 ? rows_known(sc, next, sc.n) : 0;
     float xt[HS][4], x[HS][4];
@@ -429,11 +436,11 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
           xt[hs][i] = half == 0 || !(lr & 2) ? (half == 0 ? v : xt[hs][i]) : v;
         }
     }
-    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, kRoot, xt);
-    held.put<HS, NWV>(sc, tile, next >= t1, xt);
+    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, 1.f, xt);
+    held.put<HS, NWV>(sc, tile, next >= t1, xt, factor);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
-    softmax_step<HS>(x, run, p);
+    softmax_step<HS>(x, factor, run, p);
     short4v t[HS][3];
 #pragma unroll
     for (int hs = 0; hs < HS; ++hs) split_bf16_3(p[hs], t[hs]);
@@ -570,7 +577,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
       }
   }
   const int up = __builtin_amdgcn_readfirstlane(max(-120, min(120, kQUp - exponent_of(wave_max(most)))));
-  const float unit = ldexpf(kRoot, -up);
+  const float unit = ldexpf(1.0f, -up);
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
     const uint32_t w[4] = {qraw[hs].x, qraw[hs].y, qraw[hs].z, qraw[hs].w};
@@ -608,6 +615,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   int ve = -126;                         // exponent of the largest V scale so far
   float vf = 0.f;                        // what p is multiplied by for it
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
+  const float factor = last_factor(sc, unit);
 
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
     const int next = tile + NWV, next_rows = next < t1 ? rows_known(sc, next, sc.n) : 0;
@@ -648,10 +656,10 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     }
     load_k(next, next_rows);
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
-    held.put<HS, NWV>(sc, tile, next >= t1, xt);
+    held.put<HS, NWV>(sc, tile, next >= t1, xt, factor);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
-    softmax_step<HS>(x, run, p);
+    softmax_step<HS>(x, factor, run, p);
 
     // ---- P V ---------------------------------------------------------------------------------------------------------
     uint4 vm = vmeta;
