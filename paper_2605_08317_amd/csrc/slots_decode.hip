@@ -174,8 +174,8 @@ __device__ __forceinline__ int position(const Scoring& sc, int tile, int rows) {
   return static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(of, 4 * (threadIdx.x & 63), 0, 0));
 }
 
-// What makes scores times log2(e) of what score_tile leaves: their last product, which the exponentials take in with the maximum's
-// difference, so that what is rounded is small where the probability is not (8 items of 3700 slots in bf16: outputs 6.4e-7 -> 5.8e-7 off).
+// What makes scores times log2(e) of what score_tile leaves: their last product, taken of the differences from the maximum, so that what is
+// rounded is small where the probability is not (8 items of 3700 slots in bf16: outputs 6.4e-7 -> 5.8e-7 off).
 __device__ __forceinline__ float last_factor(const Scoring& sc, float unit) { return sc.cap > 0.f || sc.biased ? kLog2e : unit * kRootLog2e; }
 // xt: products q k over a power of two, unit; comes back as scores over last_factor, -inf where the slot is not seen.  The slots that are.
 template <int HS>
@@ -209,15 +209,15 @@ __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int 
   return __builtin_amdgcn_ballot_w64(seen);
 }
 
-// Online softmax of scores x times factor in the lanes (block, head); acc: whatever is scaled with the sums
+// Online softmax of scores x times factor in the lanes (block, head), maxima as the x are; acc: whatever is scaled with the sums
 template <int HS>
 __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], float factor, Run<HS>& run, float (&p)[HS][4]) {
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
-    const float most = max_of_four(x[hs][0], x[hs][1], x[hs][2], x[hs][3]) * factor;
+    const float most = max_of_four(x[hs][0], x[hs][1], x[hs][2], x[hs][3]);
     if (__any(most > run.m[hs])) {
       const float m_new = fmaxf(run.m[hs], head_max(most));
-      const float alpha = fast_exp2(run.m[hs] - m_new);
+      const float alpha = fast_exp2((run.m[hs] - m_new) * factor);
       run.l[hs] *= alpha;
       const uint32_t au = __builtin_bit_cast(uint32_t, alpha);
       const float ah[4] = {__builtin_bit_cast(float, quad_bcast<0>(au)), __builtin_bit_cast(float, quad_bcast<1>(au)),
@@ -232,9 +232,20 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], float fact
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      p[hs][i] = fast_exp2(__builtin_fmaf(x[hs][i], factor, -run.m[hs]));
+      p[hs][i] = fast_exp2((x[hs][i] - run.m[hs]) * factor);
       run.l[hs] += p[hs][i];
     }
+  }
+}
+
+// The maxima times factor at the end, and what they lose to rounding (far from 0 as much as the scores' own).
+template <int HS>
+__device__ __forceinline__ void end_maxima(float factor, Run<HS>& run, float (&rest)[HS]) {
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) {
+    const float m = run.m[hs] * factor;
+    rest[hs] = fabsf(m) < 1048576.f ? __builtin_fmaf(run.m[hs], factor, -m) : 0.f;
+    run.m[hs] = m;
   }
 }
 
@@ -344,7 +355,8 @@ __device__ __forceinline__ void pv_rows(const uint8_t* s_stage, int lane, const 
 // P V: lanes want a channel of four slots (decode_rows.h).
 template <int HS, int NWV, bool STREAM>
 __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
-                                             const Scoring& sc, int t0, int t1, uint8_t* s_stage, uint8_t* s_query, Held& held, Run<HS>& run) {
+                                             const Scoring& sc, int t0, int t1, uint8_t* s_stage, uint8_t* s_query, Held& held, Run<HS>& run,
+                                             float (&rest)[HS]) {
   using Bf8 = __attribute__((ext_vector_type(8))) __bf16;
   const int lane = threadIdx.x & 63, j = lane & 3;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -460,6 +472,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
     pv_rows<8, HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 8>{});
     wave_lds_sync();                    // before the next rows overwrite the region
   }
+  end_maxima<HS>(factor, run, rest);
 }
 
 // ---- 4-bit rows --------------------------------------------------------------------------------------------------------------------
@@ -535,7 +548,7 @@ __device__ __forceinline__ int exponent_of(float x) {      // of a number > 0; b
 
 template <int HS, int NWV, bool STREAM>
 __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
-                                               const Scoring& sc, int t0, int t1, Held& held, Run<HS>& run) {
+                                               const Scoring& sc, int t0, int t1, Held& held, Run<HS>& run, float (&rest)[HS]) {
   const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint4 qraw[HS];
@@ -730,12 +743,13 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 #undef RDKV_PV_STEP
     load_v(next, next_rows);
   }
+  end_maxima<HS>(factor, run, rest);
   return ldexpf(1.0f, 1 + ve - kPUp);    // what brings the accumulators to the sums' scale, vf's inverse
 }
 
 // ---- the end of a piece --------------------------------------------------------------------------------------------------------------
 
-// LDS of the wavefronts' merge, floats: per wavefront, head and channel group (maximum, sum, offset sum, -), then the sums [wave][g][128];
+// LDS of the wavefronts' merge, floats: per wavefront, head and channel group (maximum, sum, offset sum, what the maximum lost), then the sums [wave][g][128];
 // then the heads' log-sum-exps for the weights.
 template <int NWV, int HS>
 constexpr int ml_floats() { return ml_lds_floats(NWV, HS); }
@@ -892,14 +906,14 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     const uint16_t* q = a.q + static_cast<int64_t>(item) * g * kHeadDim;
     Run<HS> run;
     init(run);
-    float scale = 1.f;
+    float scale = 1.f, rest[HS];
     Held held{s_held + wave * held_bytes, 0, kKeep ? 0 : held_bytes / (kTile * 4 * g)};
     if constexpr (BITS == 16) {
       const int64_t base = static_cast<int64_t>(item) * a.s.capacity * (kHeadDim * 2);
-      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, s_stage, reinterpret_cast<uint8_t*>(s_lse + 8), held, run);
+      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, s_stage, reinterpret_cast<uint8_t*>(s_lse + 8), held, run, rest);
     } else {
       const int64_t base = static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
-      scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, held, run);
+      scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, held, run, rest);
     }
     float w_first[4];
     if (kKeep && n > 0 && a.s.weight != nullptr) held_weights<NWV>(a.s, item, n, wave, w_first);
@@ -922,9 +936,11 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
         off += dpp_f32<0x128>(off);
         if ((lane & 12) == 0) s_ml[ml_at<HS>(wave, 4 * hs + (lane >> 4), lane & 3) + 2] = off * (1.0f / kPScale);
       }
-      if (lane < 16)                     // (block, j) -> group block of head j
-        *reinterpret_cast<float2*>(s_ml + ml_at<HS>(wave, 4 * hs + (lane & 3), lane >> 2)) =
-            make_float2(run.m[hs], run.l[hs]);
+      if (lane < 16) {                   // (block, j) -> group block of head j
+        float* ml = s_ml + ml_at<HS>(wave, 4 * hs + (lane & 3), lane >> 2);
+        *reinterpret_cast<float2*>(ml) = make_float2(run.m[hs], run.l[hs]);
+        ml[3] = rest[hs];
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int head = 4 * hs + i;
@@ -954,7 +970,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
         const float2 ml = *reinterpret_cast<const float2*>(s_ml + ml_at<HS>(w, head, 0));
         const float2 acc = *reinterpret_cast<const float2*>(s_acc + (w * g + head) * kHeadDim + ch);
         const float off = BITS == 4 ? s_ml[ml_at<HS>(w, head, lane >> 4) + 2] : 0.f;
-        const float f = fast_exp2(ml.x - mm);
+        const float f = fast_exp2(ml.x - mm + s_ml[ml_at<HS>(w, head, 0) + 3]);
         l = __builtin_fmaf(ml.y, f, l);
         v0 = __builtin_fmaf(acc.x + off, f, v0);
         v1 = __builtin_fmaf(acc.y + off, f, v1);
