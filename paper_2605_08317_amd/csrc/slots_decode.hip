@@ -176,7 +176,10 @@ __device__ __forceinline__ int position(const Scoring& sc, int tile, int rows) {
 
 // What makes scores times log2(e) of what score_tile leaves: their last product, taken of the differences from the maximum, so that what is
 // rounded is small where the probability is not (8 items of 3700 slots in bf16: outputs 6.4e-7 -> 5.8e-7 off).
-__device__ __forceinline__ float last_factor(const Scoring& sc, float unit) { return sc.cap > 0.f || sc.biased ? kLog2e : unit * kRootLog2e; }
+__device__ __forceinline__ float last_factor(const Scoring& sc, float unit) {
+  const float f = sc.cap > 0.f || sc.biased ? kLog2e : unit * kRootLog2e;
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
+}
 // xt: products q k over a power of two, unit; comes back as scores over last_factor, -inf where the slot is not seen.  The slots that are.
 template <int HS>
 __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int pos, float unit, float (&xt)[HS][4]) {
