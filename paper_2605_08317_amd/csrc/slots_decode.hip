@@ -1020,7 +1020,7 @@ __device__ __forceinline__ float wave_sum(float v) {
 constexpr int kJoinThreads = 256, kJoinEach = 4, kJoinSlots = kJoinThreads * kJoinEach;
 template <int G>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int rows) {
-  __shared__ float s_lse[G], s_top[G], s_half[kHeadDim];
+  __shared__ float s_lse[G], s_top[G], s_sum[G], s_half[kHeadDim];
   const int item = blockIdx.x / rows, row = blockIdx.x % rows, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int2 of = a.parts[item];
@@ -1047,6 +1047,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
     l = wave_sum(l * fast_exp2(m - top));
     if (lane == 0) {
       s_top[head] = top;
+      s_sum[head] = l;
       s_lse[head] = total_log2(top, l);
     }
   }
@@ -1064,9 +1065,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
     __syncthreads();
     if (half == 0) {
       v += s_half[c];
-      const float l = s_lse[head];
-      a.out[(qh0 + head) * kHeadDim + c] = l == INFINITY ? 0.f : v * fast_exp2(top - l);
-      if (c == 0 && a.lse != nullptr) a.lse[qh0 + head] = l == INFINITY ? -INFINITY : l * 0.6931471805599453f;
+      const float l = s_sum[head];         // (not by the log: beside a large maximum that keeps few of the sum's digits)
+      a.out[(qh0 + head) * kHeadDim + c] = l == 0.f ? 0.f : v * (1.0f / l);
+      if (c == 0 && a.lse != nullptr) a.lse[qh0 + head] = l == 0.f ? -INFINITY : s_lse[head] * 0.6931471805599453f;
     }
     __syncthreads();
   }

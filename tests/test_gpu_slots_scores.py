@@ -1,0 +1,78 @@
+"""Slot caches on the GPU: steps whose scores are far from 0, far from their head's maximum, or far from the neighbouring head's."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_08317_amd import binding as b
+from tests import slots_plain as P
+from tests.test_gpu_slots import BF, D, F32, I32, cuda, host, tiles_of
+
+pytestmark = pytest.mark.gpu
+
+
+def codes(rng, n):
+    """V rows [n, 128] that bf16 and 4 bits hold exactly, and whose sums fp32 does: whole numbers 0 .. 15, both in every group."""
+    v = rng.integers(0, 16, (n, 4, 32))
+    v[:, :, 0], v[:, :, 1] = 0, 15
+    return v.reshape(n, D).astype(np.float32)
+
+
+def cache(K, V, lens, hq, capacity, bits, **kw):
+    """Rows [batch][hkv] of [len, 128] as a cache.  Every row is held exactly."""
+    batch, hkv = len(lens), len(K[0])
+    s = b.Slots(batch, hq, hkv, capacity, bits=bits, **kw)
+    for t, rows, side in ((s.k, K, "k"), (s.v, V, "v")):
+        for i in range(batch):
+            for h in range(hkv):
+                r = rows[i][h]
+                assert np.array_equal(P.held(r, bits), r)
+                if bits == 16:
+                    t[i, h, :lens[i]] = cuda(r, BF)
+                else:
+                    t[i, h, :(lens[i] + 63) // 64] = cuda(tiles_of(r, side))
+    s.pos.copy_(torch.arange(capacity, dtype=I32, device="cuda").expand_as(s.pos))
+    s.lens.copy_(torch.tensor(lens, dtype=I32, device="cuda")[:, None].expand_as(s.lens))
+    s.next_pos.copy_(s.lens)
+    return s
+
+
+def off(got, want):
+    """The largest difference, relative to the value; where that is 0 nothing else will do."""
+    got, want = np.broadcast_arrays(got, want)
+    assert not got[want == 0].any() and np.isfinite(got).all()
+    return np.max(np.abs(got - want)[want != 0] / np.abs(want[want != 0]))
+
+
+LENS = {300: [300, 219], 5000: [5000, 4321]}      # capacities: an item to a workgroup, and cut into pieces
+
+
+# ---- scores far from 0 -------------------------------------------------------------------------------------------------------------
+
+def equal_scores(rng, bits, g, capacity, e, biased):
+    """Every K row is 64 and the query 2^e: all scores are 2^(13 + e) / sqrt(128), and their products and sums exact."""
+    lens = LENS[capacity]
+    K = [[np.full((n, D), 64.0, np.float32)] * 2 for n in lens]
+    V = [[codes(rng, n) for _ in range(2)] for n in lens]
+    s = cache(K, V, lens, 2 * g, capacity, bits, slopes=torch.zeros(2 * g, device="cuda") if biased else None)
+    return s, V, lens, torch.full((2, 2 * g, D), 2.0 ** e, device="cuda", dtype=BF)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("g", [1, 4, 8])
+@pytest.mark.parametrize("capacity", sorted(LENS))
+@pytest.mark.parametrize("e, biased", [(1, False), (1, True), (7, False), (17, False), (17, True)])      # scores 1.4e3, 9.3e4, 9.5e7
+def test_outputs_of_equal_scores(bits, g, capacity, e, biased):
+    """The mean of V.  Exponentials are of 0, sums whole numbers below 2^24; there remain the quotient, a product, and factors near 1 of
+    the wavefronts' and the pieces' sums: 8 wavefronts or 20 pieces of 4, each two roundings of a sum that is a part of the whole."""
+    rng = np.random.default_rng(30)
+    s, V, lens, q = equal_scores(rng, bits, g, capacity, e, biased)
+    out, lse = b.rdkv_slots_decode_attn(s, q)
+    score = 2.0 ** (13 + e) / math.sqrt(D)
+    for i, n in enumerate(lens):
+        for h in range(2):
+            mean = V[i][h].astype(np.float64).mean(0)
+            got = host(out)[i, h * g:(h + 1) * g]
+            assert off(got, mean) <= 2.0 ** -20
+            assert off(host(lse)[i, h * g:(h + 1) * g], score + math.log(n)) <= 2.0 ** -22
