@@ -25,7 +25,7 @@ namespace {
 
 using namespace tile;
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRoot = 0.08838834764831845f;      // 1 / sqrt(128)
 constexpr float kRootLog2e = 0.12751743f;          // both: 0.0883883476 x 1.4426950409 = 0.12751743 (to 2^-25)
 constexpr float kLowest = -3.402823466e38f;        // a finite maximum of nothing: no score is below it
@@ -37,9 +37,11 @@ struct DecodeArgs {
   float* lse;
   float* scores;       // [items][score_rows][g], times log2(e); null: no weights are kept
   float* part_acc;     // [slot][g][128]: partials; slot = workgroup + item
-  float* part_ml;      // [slot][g][2]
+  float* part_ml;      // [slot][g][2]: maximum, before the last factor, and sum
   int2* parts;         // [items]: an item's first partial and their number, 0 where it has none
   int32_t held_bytes;  // of scores that a wavefront keeps
+  float factor;        // what makes products or, with a cap or biases, scores exponents of 2,
+  float natural;       // and what makes them scores
   int32_t items, score_rows;
   int32_t least, start;                 // of a workgroup's share, tiles; 0: a workgroup takes an item.  What a start on one is worth
 };
@@ -174,13 +176,12 @@ __device__ __forceinline__ int position(const Scoring& sc, int tile, int rows) {
   return static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(of, 4 * (threadIdx.x & 63), 0, 0));
 }
 
-// What makes scores times log2(e) of what score_tile leaves: their last product, taken of the differences from the maximum, so that what is
-// rounded is small where the probability is not (8 items of 3700 slots in bf16: outputs 6.4e-7 -> 5.8e-7 off).
-__device__ __forceinline__ float last_factor(const Scoring& sc, float unit) {
-  const float f = sc.cap > 0.f || sc.biased ? kLog2e : unit * kRootLog2e;
-  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
-}
-// xt: products q k over a power of two, unit; comes back as scores over last_factor, -inf where the slot is not seen.  The slots that are.
+// The power of two that score_tile leaves products over, unit; 1 with a cap or biases.
+__device__ __forceinline__ float left_unit(const Scoring& sc, float unit) { return sc.cap > 0.f || sc.biased ? 1.f : unit; }
+// xt: products q k over a power of two, unit; comes back as products over left_unit, or as scores, -inf where the slot is not seen.  The slots
+// that are.
+//   The last factor, DecodeArgs::factor, is for differences from a maximum alone, here and in the merges, so that what is rounded is small where
+// the probability is not (8 items of 3700 slots in bf16: outputs 6.4e-7 -> 5.8e-7 off).
 template <int HS>
 __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int pos, float unit, float (&xt)[HS][4]) {
   const int lane = threadIdx.x & 63, row = tile * kTile + lane;
@@ -241,14 +242,14 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], float fact
   }
 }
 
-// The maxima times factor at the end, and what they lose to rounding (far from 0 as much as the scores' own).
+// The end of a wavefront's tiles: maxima without the unit.  A sum is nothing where its maximum is below what an exponent of 2 can be (0 x NaN
+// stays NaN).
 template <int HS>
-__device__ __forceinline__ void end_maxima(float factor, Run<HS>& run, float (&rest)[HS]) {
+__device__ __forceinline__ void end_maxima(float unit, float factor, Run<HS>& run) {
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
-    const float m = run.m[hs] * factor;
-    rest[hs] = fabsf(m) < 1048576.f ? __builtin_fmaf(run.m[hs], factor, -m) : 0.f;
-    run.m[hs] = m;
+    run.m[hs] *= unit;
+    run.l[hs] *= run.m[hs] * factor < kLowest ? 0.f : 1.f;
   }
 }
 
@@ -358,8 +359,8 @@ __device__ __forceinline__ void pv_rows(const uint8_t* s_stage, int lane, const 
 // P V: lanes want a channel of four slots (decode_rows.h).
 template <int HS, int NWV, bool STREAM>
 __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
-                                             const Scoring& sc, int t0, int t1, uint8_t* s_stage, uint8_t* s_query, Held& held, Run<HS>& run,
-                                             float (&rest)[HS]) {
+                                             const Scoring& sc, float factor, int t0, int t1, uint8_t* s_stage, uint8_t* s_query, Held& held,
+                                             Run<HS>& run) {
   using Bf8 = __attribute__((ext_vector_type(8))) __bf16;
   const int lane = threadIdx.x & 63, j = lane & 3;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -414,7 +415,6 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
       for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(qa[hs][i].x), "+v"(qa[hs][i].y), "+v"(qa[hs][i].z), "+v"(qa[hs][i].w));
   }
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
-  const float factor = last_factor(sc, 1.f);
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
     const int next = tile + NWV, next_rows = next < t1 ? rows_known(sc, next, sc.n) : 0;
     float xt[HS][4], x[HS][4];
@@ -475,7 +475,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
     pv_rows<8, HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 8>{});
     wave_lds_sync();                    // before the next rows overwrite the region
   }
-  end_maxima<HS>(factor, run, rest);
+  end_maxima<HS>(1.f, factor, run);
 }
 
 // ---- 4-bit rows --------------------------------------------------------------------------------------------------------------------
@@ -551,7 +551,7 @@ __device__ __forceinline__ int exponent_of(float x) {      // of a number > 0; b
 
 template <int HS, int NWV, bool STREAM>
 __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, const uint8_t* __restrict__ vd, const uint16_t* __restrict__ q,
-                                               const Scoring& sc, int t0, int t1, Held& held, Run<HS>& run, float (&rest)[HS]) {
+                                               const Scoring& sc, float factor, int t0, int t1, Held& held, Run<HS>& run) {
   const int lane = threadIdx.x & 63, blk = lane >> 2, j = lane & 3;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint4 qraw[HS];
@@ -631,7 +631,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   int ve = -126;                         // exponent of the largest V scale so far
   float vf = 0.f;                        // what p is multiplied by for it
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
-  const float factor = last_factor(sc, unit);
+  const float left = left_unit(sc, unit), all = left * factor;
 
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
     const int next = tile + NWV, next_rows = next < t1 ? rows_known(sc, next, sc.n) : 0;
@@ -672,10 +672,10 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     }
     load_k(next, next_rows);
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
-    held.put<HS, NWV>(sc, tile, next >= t1, xt, factor);
+    held.put<HS, NWV>(sc, tile, next >= t1, xt, all);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
-    softmax_step<HS>(x, factor, run, p);
+    softmax_step<HS>(x, all, run, p);
 
     // ---- P V ---------------------------------------------------------------------------------------------------------
     uint4 vm = vmeta;
@@ -746,13 +746,13 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 #undef RDKV_PV_STEP
     load_v(next, next_rows);
   }
-  end_maxima<HS>(factor, run, rest);
+  end_maxima<HS>(left, factor, run);
   return ldexpf(1.0f, 1 + ve - kPUp);    // what brings the accumulators to the sums' scale, vf's inverse
 }
 
 // ---- the end of a piece --------------------------------------------------------------------------------------------------------------
 
-// LDS of the wavefronts' merge, floats: per wavefront, head and channel group (maximum, sum, offset sum, what the maximum lost), then the sums [wave][g][128];
+// LDS of the wavefronts' merge, floats: per wavefront, head and channel group (maximum, sum, offset sum, -), then the sums [wave][g][128];
 // then the heads' log-sum-exps for the weights.
 template <int NWV, int HS>
 constexpr int ml_floats() { return ml_lds_floats(NWV, HS); }
@@ -909,14 +909,14 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     const uint16_t* q = a.q + static_cast<int64_t>(item) * g * kHeadDim;
     Run<HS> run;
     init(run);
-    float scale = 1.f, rest[HS];
+    float scale = 1.f;
     Held held{s_held + wave * held_bytes, 0, kKeep ? 0 : held_bytes / (kTile * 4 * g)};
     if constexpr (BITS == 16) {
       const int64_t base = static_cast<int64_t>(item) * a.s.capacity * (kHeadDim * 2);
-      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, s_stage, reinterpret_cast<uint8_t*>(s_lse + 8), held, run, rest);
+      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, a.factor, t0, t1, s_stage, reinterpret_cast<uint8_t*>(s_lse + 8), held, run);
     } else {
       const int64_t base = static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
-      scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, t0, t1, held, run, rest);
+      scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, a.factor, t0, t1, held, run);
     }
     float w_first[4];
     if (kKeep && n > 0 && a.s.weight != nullptr) held_weights<NWV>(a.s, item, n, wave, w_first);
@@ -942,7 +942,6 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
       if (lane < 16) {                   // (block, j) -> group block of head j
         float* ml = s_ml + ml_at<HS>(wave, 4 * hs + (lane & 3), lane >> 2);
         *reinterpret_cast<float2*>(ml) = make_float2(run.m[hs], run.l[hs]);
-        ml[3] = rest[hs];
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -973,7 +972,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
         const float2 ml = *reinterpret_cast<const float2*>(s_ml + ml_at<HS>(w, head, 0));
         const float2 acc = *reinterpret_cast<const float2*>(s_acc + (w * g + head) * kHeadDim + ch);
         const float off = BITS == 4 ? s_ml[ml_at<HS>(w, head, lane >> 4) + 2] : 0.f;
-        const float f = fast_exp2(ml.x - mm + s_ml[ml_at<HS>(w, head, 0) + 3]);
+        const float f = fast_exp2((ml.x - mm) * a.factor);
         l = __builtin_fmaf(ml.y, f, l);
         v0 = __builtin_fmaf(acc.x + off, f, v0);
         v1 = __builtin_fmaf(acc.y + off, f, v1);
@@ -982,8 +981,8 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
         const float inv = 1.0f / l;
         *reinterpret_cast<float2*>(a.out + (qh0 + head) * kHeadDim + ch) = l == 0.f ? make_float2(0.f, 0.f) : make_float2(v0 * inv, v1 * inv);
         if (lane == 0) {
-          if (a.lse != nullptr) a.lse[qh0 + head] = l == 0.f ? -INFINITY : (mm + __log2f(l)) * 0.6931471805599453f;
-          s_lse[head] = total_log2(mm, l);
+          if (a.lse != nullptr) a.lse[qh0 + head] = l == 0.f ? -INFINITY : __builtin_fmaf(mm, a.natural, __log2f(l) * kLn2);
+          s_lse[head] = total_log2(mm * a.factor, l);
         }
       } else {
         *reinterpret_cast<float2*>(a.part_acc + (slot * g + head) * kHeadDim + ch) = make_float2(v0, v1);
@@ -1036,7 +1035,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
     for (int k = lane; k < parts; k += 64) {
       const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * G + head) * 2);
       const float mm = fmaxf(m, ml.x);
-      l = l * fast_exp2(m - mm) + ml.y * fast_exp2(ml.x - mm);
+      l = l * fast_exp2((m - mm) * a.factor) + ml.y * fast_exp2((ml.x - mm) * a.factor);
       m = mm;
     }
     float top = row_max(m), o = top;
@@ -1044,11 +1043,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
     top = o = fmaxf(top, o);
     swap_halves(top, o);
     top = fmaxf(top, o);
-    l = wave_sum(l * fast_exp2(m - top));
+    l = wave_sum(l * fast_exp2((m - top) * a.factor));
     if (lane == 0) {
       s_top[head] = top;
       s_sum[head] = l;
-      s_lse[head] = total_log2(top, l);
+      s_lse[head] = total_log2(top * a.factor, l);
     }
   }
   __syncthreads();
@@ -1059,7 +1058,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
     float v = 0.f;
     for (int k = half; k < parts; k += 2) {
       const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * G + head) * 2);
-      v = __builtin_fmaf(a.part_acc[((slot0 + k) * G + head) * kHeadDim + c], fast_exp2(ml.x - top), v);
+      v = __builtin_fmaf(a.part_acc[((slot0 + k) * G + head) * kHeadDim + c], fast_exp2((ml.x - top) * a.factor), v);
     }
     if (half == 1) s_half[c] = v;
     __syncthreads();
@@ -1067,7 +1066,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
       v += s_half[c];
       const float l = s_sum[head];         // (not by the log: beside a large maximum that keeps few of the sum's digits)
       a.out[(qh0 + head) * kHeadDim + c] = l == 0.f ? 0.f : v * (1.0f / l);
-      if (c == 0 && a.lse != nullptr) a.lse[qh0 + head] = l == 0.f ? -INFINITY : s_lse[head] * 0.6931471805599453f;
+      if (c == 0 && a.lse != nullptr) a.lse[qh0 + head] = l == 0.f ? -INFINITY : __builtin_fmaf(top, a.natural, __log2f(l) * kLn2);
     }
     __syncthreads();
   }
@@ -1178,6 +1177,9 @@ hipError_t launch_decode(const Args& s, int bits, int items, const uint16_t* q, 
   a.least = p.least;
   a.start = p.start;
   a.held_bytes = p.held_bytes;
+  const bool scores = s.cap > 0.f || s.slopes != nullptr;
+  a.factor = scores ? kLog2e : kRootLog2e;
+  a.natural = scores ? 1.f : kRoot;
   const hipError_t e = bits == 16 ? s.g > 4 ? launch<16, 2>(a, p, st) : launch<16, 1>(a, p, st)
                                   : s.g > 4 ? launch<4, 2>(a, p, st) : launch<4, 1>(a, p, st);
   if (e != hipSuccess || p.join_rows == 0) return e;

@@ -76,3 +76,44 @@ def test_outputs_of_equal_scores(bits, g, capacity, e, biased):
             got = host(out)[i, h * g:(h + 1) * g]
             assert off(got, mean) <= 2.0 ** -20
             assert off(host(lse)[i, h * g:(h + 1) * g], score + math.log(n)) <= 2.0 ** -22
+
+
+# ---- maxima far from 0, and others near them ----------------------------------------------------------------------------------------
+
+def two_scores(rng, bits, g, capacity, e, biased):
+    """Products with the query are 2^e, and 8 more in an item's first half: exact in fp32, as is their difference."""
+    lens = LENS[capacity]
+    K = [[np.zeros((n, D), np.float32) for _ in range(2)] for n in lens]
+    for n, two in zip(lens, K):
+        for k in two:
+            k[:, :32] = 2.0 ** (e // 2)
+            k[:n // 2, 32:64] = 8.0
+    V = [[codes(rng, n) for _ in range(2)] for n in lens]
+    s = cache(K, V, lens, 2 * g, capacity, bits, slopes=torch.zeros(2 * g, device="cuda") if biased else None)
+    q = torch.zeros((2, 2 * g, D), device="cuda", dtype=BF)
+    q[:, :, 0], q[:, :, 32] = 2.0 ** (e - e // 2), 1.0
+    return s, V, lens, q
+
+
+def two_probabilities(n):
+    p = np.where(np.arange(n) < n // 2, 1.0, math.exp(-8 / math.sqrt(D)))
+    return p / p.sum()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("g", [1, 4, 8])
+@pytest.mark.parametrize("capacity", sorted(LENS))
+@pytest.mark.parametrize("e, biased", [(10, False), (20, False), (23, False), (23, True)])
+def test_outputs_of_two_scores(bits, g, capacity, e, biased):
+    """Wavefronts and pieces have maxima that differ by 8 / sqrt(128), 1.02 in the exponent.  With biases the scores are products over
+    sqrt(128), rounded: 2^-24 of them each; else they are exact.  A probability is off by that, 1.02 x 2^-24 x ln 2 and an exponential's
+    2^-23; the sums as everywhere, relative to their terms (of 4-bit rows scale x (code - 8) and offset + 8 scale)."""
+    rng = np.random.default_rng(31)
+    s, V, lens, q = two_scores(rng, bits, g, capacity, e, biased)
+    out, _ = b.rdkv_slots_decode_attn(s, q)
+    rel = 2 * (2 * 2.0 ** (e - 24) / math.sqrt(D) if biased else 0.0) + P.sums_off(lens[0]) + 2.0 ** -20
+    for i, n in enumerate(lens):
+        for h in range(2):
+            p = two_probabilities(n)
+            worst = np.abs(host(out)[i, h * g:(h + 1) * g] - p @ V[i][h].astype(np.float64)) / (p @ P.terms(V[i][h], bits, 8) + 1e-30)
+            assert worst.max() <= rel
