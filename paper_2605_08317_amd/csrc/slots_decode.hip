@@ -35,7 +35,7 @@ struct DecodeArgs {
   const uint16_t* q;
   float* out;
   float* lse;
-  float* scores;       // [items][score_rows][g], times log2(e); null: no weights are kept
+  float* scores;       // [items][score_rows][g], before the last factor; null: no weights are kept
   float* part_acc;     // [slot][g][128]: partials; slot = workgroup + item
   float* part_ml;      // [slot][g][2]: maximum, before the last factor, and sum
   int2* parts;         // [items]: an item's first partial and their number, 0 where it has none
@@ -262,17 +262,17 @@ struct Held {
   uint8_t* at;         // of this wavefront: [tiles][64][g]
   int n, most;         // tiles there, and room; most 0: all of the item's stay
   template <int HS, int NWV>
-  __device__ __forceinline__ void put(const Scoring& sc, int tile, bool last, const float (&xt)[HS][4], float f) {
+  __device__ __forceinline__ void put(const Scoring& sc, int tile, bool last, const float (&xt)[HS][4], float unit) {
     if (!sc.tracked) return;
     const int lane = threadIdx.x & 63;
     float* dst = reinterpret_cast<float*>(at) + (n * kTile + lane) * sc.g;
     if constexpr (HS == 2) {
-      *reinterpret_cast<float4*>(dst) = make_float4(f * xt[0][0], f * xt[0][1], f * xt[0][2], f * xt[0][3]);
-      *reinterpret_cast<float4*>(dst + 4) = make_float4(f * xt[1][0], f * xt[1][1], f * xt[1][2], f * xt[1][3]);
+      *reinterpret_cast<float4*>(dst) = make_float4(unit * xt[0][0], unit * xt[0][1], unit * xt[0][2], unit * xt[0][3]);
+      *reinterpret_cast<float4*>(dst + 4) = make_float4(unit * xt[1][0], unit * xt[1][1], unit * xt[1][2], unit * xt[1][3]);
     } else {
-      if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(f * xt[0][0], f * xt[0][1], f * xt[0][2], f * xt[0][3]);
-      else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(f * xt[0][0], f * xt[0][1]);
-      else *dst = f * xt[0][0];
+      if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(unit * xt[0][0], unit * xt[0][1], unit * xt[0][2], unit * xt[0][3]);
+      else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(unit * xt[0][0], unit * xt[0][1]);
+      else *dst = unit * xt[0][0];
     }
     ++n;
     if (n == most || (last && most > 0)) {
@@ -452,7 +452,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
         }
     }
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, 1.f, xt);
-    held.put<HS, NWV>(sc, tile, next >= t1, xt, factor);
+    held.put<HS, NWV>(sc, tile, next >= t1, xt, 1.f);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
     softmax_step<HS>(x, factor, run, p);
@@ -672,7 +672,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
     }
     load_k(next, next_rows);
     const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
-    held.put<HS, NWV>(sc, tile, next >= t1, xt, all);
+    held.put<HS, NWV>(sc, tile, next >= t1, xt, left);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
     softmax_step<HS>(x, all, run, p);
@@ -753,11 +753,20 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 // ---- the end of a piece --------------------------------------------------------------------------------------------------------------
 
 // LDS of the wavefronts' merge, floats: per wavefront, head and channel group (maximum, sum, offset sum, -), then the sums [wave][g][128];
-// then the heads' log-sum-exps for the weights.
+// then the heads' maxima and sums' inverses for the weights.
 template <int NWV, int HS>
 constexpr int ml_floats() { return ml_lds_floats(NWV, HS); }
+constexpr int kHeadFloats = 16;          // of up to eight heads
+// What a head's probabilities are made of.  (By the difference from a log-sum-exp they would be off by its rounding, the same way in all slots:
+// 4e-5 at scores of 1e3.)  Where nothing is seen the inverse is 0, and every probability.
+struct HeadSum {
+  float top, inv;
+  __device__ __forceinline__ static HeadSum of(float m, float l) { return {m, l == 0.f ? 0.f : 1.0f / l}; }
+  __device__ __forceinline__ float add(float p, float x, float factor) const { return __builtin_fmaf(fast_exp2((x - top) * factor), inv, p); }
+};
+static_assert(sizeof(HeadSum) * 8 == kHeadFloats * sizeof(float), "two a head");
 
-// What a thread adds to the weights of its slots: their scores and weights are loaded before the heads' log-sum-exps are known.
+// What a thread adds to the weights of its slots: their scores and weights are loaded before the heads' sums are known.
 // EACH slots, `step` apart.
 template <int G, int EACH>
 struct WeightPart {
@@ -775,28 +784,27 @@ struct WeightPart {
       w[k] = weight[i];
     }
   }
-  // lse2: of the heads, log2
-  __device__ __forceinline__ void store(float* __restrict__ weight, float decay, const float* lse2, int i0, int step, int end) const {
-    float l[G];
+  __device__ __forceinline__ void store(float* __restrict__ weight, float decay, float factor, const HeadSum* sums, int i0, int step, int end) const {
+    HeadSum of[G];
 #pragma unroll
-    for (int h = 0; h < G; ++h) l[h] = lse2[h];
+    for (int h = 0; h < G; ++h) of[h] = sums[h];
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
       float p = 0.f;
 #pragma unroll
-      for (int h = 0; h < G; ++h) p += fast_exp2(x[k][h / kWide][h % kWide] - l[h]);
+      for (int h = 0; h < G; ++h) p = of[h].add(p, x[k][h / kWide][h % kWide], factor);
       if (i0 + k * step < end) weight[i0 + k * step] = __builtin_fmaf(decay, w[k], p);
     }
   }
 };
 template <int G>
-__device__ __forceinline__ void add_weights(const Args& a, int64_t item, const float* scores, const float* lse2, int n, int thread, int threads) {
+__device__ __forceinline__ void add_weights(const DecodeArgs& a, int64_t item, const float* scores, const HeadSum* sums, int n, int thread, int threads) {
   constexpr int kEach = G == 8 ? 2 : 4;
-  float* weight = a.weight + item * a.capacity;
+  float* weight = a.s.weight + item * a.s.capacity;
   for (int i = thread; i < n; i += kEach * threads) {
     WeightPart<G, kEach> part;
     part.load(scores, weight, i, threads, n);
-    part.store(weight, a.decay, lse2, i, threads, n);
+    part.store(weight, a.s.decay, a.factor, sums, i, threads, n);
   }
 }
 
@@ -808,30 +816,32 @@ __device__ __forceinline__ void held_weights(const Args& a, int64_t item, int n,
 }
 // w: held_weights of the first tiles
 template <int HS, int NWV>
-__device__ __forceinline__ void add_held(const Args& a, int64_t item, const float* s_held, const float* lse2, int n, int wave, int tiles, float (&w)[4]) {
-  const int lane = threadIdx.x & 63;
-  float* __restrict__ weight = a.weight + item * a.capacity;
-  float l[4 * HS];
+__device__ __forceinline__ void add_held(const DecodeArgs& a, int64_t item, const float* s_held, const HeadSum* sums, int n, int wave, int tiles, float (&w)[4]) {
+  const int lane = threadIdx.x & 63, g = a.s.g;
+  float* __restrict__ weight = a.s.weight + item * a.s.capacity;
+  HeadSum of[4 * HS];
 #pragma unroll
-  for (int h = 0; h < 4 * HS; ++h) l[h] = lse2[h < a.g ? h : 0];
+  for (int h = 0; h < 4 * HS; ++h) of[h] = sums[h < g ? h : 0];
   for (int t0 = wave, k = 0; t0 < tiles; t0 += 4 * NWV, k += 4) {
-    if (k > 0) held_weights<NWV>(a, item, n, t0, w);
+    if (k > 0) held_weights<NWV>(a.s, item, n, t0, w);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int i = (t0 + j * NWV) * kTile + lane;
       if (i >= n) break;
-      const float* x = s_held + ((k + j) * kTile + lane) * a.g;
+      const float* x = s_held + ((k + j) * kTile + lane) * g;
       float p = 0.f;
 #pragma unroll
       for (int h = 0; h < 4 * HS; ++h)
-        if (HS == 2 || h < a.g) p += fast_exp2(x[h] - l[h]);
-      weight[i] = __builtin_fmaf(a.decay, w[j], p);
+        if (HS == 2 || h < g) p = of[h].add(p, x[h], a.factor);
+      weight[i] = __builtin_fmaf(a.s.decay, w[j], p);
     }
   }
 }
 
-// log2 of the sum of 2^score over everything: sum l, relative to 2^m; +inf where nothing was seen, which makes every weight 0
-__device__ __forceinline__ float total_log2(float m, float l) { return l == 0.f ? INFINITY : m + __log2f(l); }
+// natural log-sum-exp of a head
+__device__ __forceinline__ float log_sum(const DecodeArgs& a, float m, float l) {
+  return l == 0.f ? -INFINITY : __builtin_fmaf(m, a.natural, __log2f(l) * kLn2);
+}
 
 template <int BITS, int HS, int NWV, bool STREAM>
 __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decode_kernel(DecodeArgs a) {
@@ -863,7 +873,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
   }
   int item = p.item, first = p.first, at = p.at;
   // LDS: the wavefronts' staging regions; their scores; the accumulators' area [NWV][g][128], which is the staging regions' memory, or the
-  // scores' unless they are kept; the wavefronts' maxima and sums, and the heads' log-sum-exps
+  // scores' unless they are kept; the wavefronts' maxima and sums, and the heads'
   constexpr bool kKeep = NWV == 8, kOwnAcc = BITS == 4 && kKeep;
   const int held_bytes = kKeep ? a.held_bytes : held_bytes_of_four(BITS);
   uint8_t* s_stage = smem + wave * kHalfBytes;
@@ -871,7 +881,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
   uint8_t* s_end = s_held + NWV * held_bytes;
   float* s_acc = reinterpret_cast<float*>(kOwnAcc ? s_end : smem);
   float* s_ml = reinterpret_cast<float*>(s_end) + (kOwnAcc ? NWV * g * kHeadDim : 0);
-  float* s_lse = s_ml + ml_floats<NWV, HS>();
+  HeadSum* s_sums = reinterpret_cast<HeadSum*>(s_ml + ml_floats<NWV, HS>());
   do {
     // (all the same for every lane, which buffers need to be known of)
     item = __builtin_amdgcn_readfirstlane(item);
@@ -913,7 +923,7 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     Held held{s_held + wave * held_bytes, 0, kKeep ? 0 : held_bytes / (kTile * 4 * g)};
     if constexpr (BITS == 16) {
       const int64_t base = static_cast<int64_t>(item) * a.s.capacity * (kHeadDim * 2);
-      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, a.factor, t0, t1, s_stage, reinterpret_cast<uint8_t*>(s_lse + 8), held, run);
+      rows_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, a.factor, t0, t1, s_stage, reinterpret_cast<uint8_t*>(s_sums + 8), held, run);
     } else {
       const int64_t base = static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
       scale = tiles_segment<HS, NWV, STREAM>(a.s.k + base, a.s.v + base, q, sc, a.factor, t0, t1, held, run);
@@ -978,11 +988,11 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
         v1 = __builtin_fmaf(acc.y + off, f, v1);
       }
       if (whole) {
-        const float inv = 1.0f / l;
-        *reinterpret_cast<float2*>(a.out + (qh0 + head) * kHeadDim + ch) = l == 0.f ? make_float2(0.f, 0.f) : make_float2(v0 * inv, v1 * inv);
+        const HeadSum sum = HeadSum::of(mm, l);
+        *reinterpret_cast<float2*>(a.out + (qh0 + head) * kHeadDim + ch) = l == 0.f ? make_float2(0.f, 0.f) : make_float2(v0 * sum.inv, v1 * sum.inv);
         if (lane == 0) {
-          if (a.lse != nullptr) a.lse[qh0 + head] = l == 0.f ? -INFINITY : __builtin_fmaf(mm, a.natural, __log2f(l) * kLn2);
-          s_lse[head] = total_log2(mm * a.factor, l);
+          if (a.lse != nullptr) a.lse[qh0 + head] = log_sum(a, mm, l);
+          s_sums[head] = sum;
         }
       } else {
         *reinterpret_cast<float2*>(a.part_acc + (slot * g + head) * kHeadDim + ch) = make_float2(v0, v1);
@@ -991,12 +1001,12 @@ __global__ __launch_bounds__(NWV * 64, BITS == 16 || HS == 2 ? 2 : 3) void decod
     }
     __syncthreads();
     if (kKeep && a.s.weight != nullptr) {
-      add_held<HS, NWV>(a.s, item, reinterpret_cast<const float*>(held.at), s_lse, n, wave, tiles, w_first);
+      add_held<HS, NWV>(a, item, reinterpret_cast<const float*>(held.at), s_sums, n, wave, tiles, w_first);
     } else if (!kKeep && whole && a.s.weight != nullptr) {
-      if (HS == 2) add_weights<8>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
-      else if (g == 4) add_weights<4>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
-      else if (g == 2) add_weights<2>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
-      else add_weights<1>(a.s, item, sc.scores, s_lse, n, tid, NWV * 64);
+      if (HS == 2) add_weights<8>(a, item, sc.scores, s_sums, n, tid, NWV * 64);
+      else if (g == 4) add_weights<4>(a, item, sc.scores, s_sums, n, tid, NWV * 64);
+      else if (g == 2) add_weights<2>(a, item, sc.scores, s_sums, n, tid, NWV * 64);
+      else add_weights<1>(a, item, sc.scores, s_sums, n, tid, NWV * 64);
       __syncthreads();
     }
     at = first + t1;
@@ -1019,7 +1029,8 @@ __device__ __forceinline__ float wave_sum(float v) {
 constexpr int kJoinThreads = 256, kJoinEach = 4, kJoinSlots = kJoinThreads * kJoinEach;
 template <int G>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int rows) {
-  __shared__ float s_lse[G], s_top[G], s_sum[G], s_half[kHeadDim];
+  __shared__ HeadSum s_sums[G];
+  __shared__ float s_lse[G], s_half[kHeadDim];
   const int item = blockIdx.x / rows, row = blockIdx.x % rows, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int2 of = a.parts[item];
@@ -1045,32 +1056,30 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeArgs a, int ro
     top = fmaxf(top, o);
     l = wave_sum(l * fast_exp2((m - top) * a.factor));
     if (lane == 0) {
-      s_top[head] = top;
-      s_sum[head] = l;
-      s_lse[head] = total_log2(top * a.factor, l);
+      s_sums[head] = HeadSum::of(top, l);
+      s_lse[head] = log_sum(a, top, l);
     }
   }
   __syncthreads();
   // heads among the item's workgroups: two halves of the partials, a channel a thread
   for (int head = row; head < G; head += rows) {
     const int c = tid & (kHeadDim - 1), half = tid >> 7;
-    const float top = s_top[head];
+    const HeadSum sum = s_sums[head];
     float v = 0.f;
     for (int k = half; k < parts; k += 2) {
       const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + ((slot0 + k) * G + head) * 2);
-      v = __builtin_fmaf(a.part_acc[((slot0 + k) * G + head) * kHeadDim + c], fast_exp2((ml.x - top) * a.factor), v);
+      v = __builtin_fmaf(a.part_acc[((slot0 + k) * G + head) * kHeadDim + c], fast_exp2((ml.x - sum.top) * a.factor), v);
     }
     if (half == 1) s_half[c] = v;
     __syncthreads();
     if (half == 0) {
       v += s_half[c];
-      const float l = s_sum[head];         // (not by the log: beside a large maximum that keeps few of the sum's digits)
-      a.out[(qh0 + head) * kHeadDim + c] = l == 0.f ? 0.f : v * (1.0f / l);
-      if (c == 0 && a.lse != nullptr) a.lse[qh0 + head] = l == 0.f ? -INFINITY : __builtin_fmaf(top, a.natural, __log2f(l) * kLn2);
+      a.out[(qh0 + head) * kHeadDim + c] = sum.inv == 0.f ? 0.f : v * sum.inv;
+      if (c == 0 && a.lse != nullptr) a.lse[qh0 + head] = s_lse[head];
     }
     __syncthreads();
   }
-  if (tracked) part.store(weight, a.s.decay, s_lse, i0, kJoinThreads, n);
+  if (tracked) part.store(weight, a.s.decay, a.factor, s_sums, i0, kJoinThreads, n);
 }
 
 constexpr size_t kMostLds = 160 << 10;
@@ -1095,7 +1104,7 @@ bool one_each(int64_t items, int g, int64_t tiles, int bits, bool stream) {
 }
 // LDS of a workgroup of eight wavefronts that keep `held` bytes of scores each
 size_t lds_of_eight(int bits, int g, size_t held) {
-  return 8 * (held + (bits == 16 ? kHalfBytes : g * kHeadDim * sizeof(float))) + (ml_lds_floats(8, g > 4 ? 2 : 1) + 8) * sizeof(float) +
+  return 8 * (held + (bits == 16 ? kHalfBytes : g * kHeadDim * sizeof(float))) + (ml_lds_floats(8, g > 4 ? 2 : 1) + kHeadFloats) * sizeof(float) +
          (bits == 16 && g > 4 ? kQueryBytes : 0);
 }
 struct Plan {
@@ -1137,7 +1146,7 @@ Plan make_plan(int64_t items, int g, int capacity, int bits, bool weights) {
 template <int BITS, int HS, int NWV, bool STREAM>
 hipError_t launch_one(const DecodeArgs& a, const Plan& p, hipStream_t st) {
   const size_t lds = NWV == 8 ? lds_of_eight(BITS, a.s.g, a.held_bytes)
-                              : NWV * ((BITS == 16 ? kHalfBytes : 0) + held_bytes_of_four(BITS)) + (ml_floats<NWV, HS>() + 8) * sizeof(float) +
+                              : NWV * ((BITS == 16 ? kHalfBytes : 0) + held_bytes_of_four(BITS)) + (ml_floats<NWV, HS>() + kHeadFloats) * sizeof(float) +
                                     (BITS == 16 && HS == 2 ? kQueryBytes : 0);
   static_assert(NWV * held_bytes_of_four(BITS) >= kHeldLengths * 4 + 4 * kTries * 8, "the lengths fit");
   static_assert(held_bytes_of_four(4) >= 4 * HS * kHeadDim * 4 && kHalfBytes >= 4 * HS * kHeadDim * 4, "the accumulators fit");

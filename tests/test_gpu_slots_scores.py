@@ -117,3 +117,37 @@ def test_outputs_of_two_scores(bits, g, capacity, e, biased):
             p = two_probabilities(n)
             worst = np.abs(host(out)[i, h * g:(h + 1) * g] - p @ V[i][h].astype(np.float64)) / (p @ P.terms(V[i][h], bits, 8) + 1e-30)
             assert worst.max() <= rel
+
+
+# ---- the weights -----------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("g", [1, 2, 4, 8])
+@pytest.mark.parametrize("capacity", sorted(LENS))
+@pytest.mark.parametrize("e, biased", [(1, False), (1, True), (7, False), (17, False), (17, True)])
+def test_weights_of_equal_scores(bits, g, capacity, e, biased):
+    """Every token's grows by g / n: a quotient and g - 1 additions, then one to what there was."""
+    rng = np.random.default_rng(32)
+    s, V, lens, q = equal_scores(rng, bits, g, capacity, e, biased)
+    s.weight.fill_(0.0)
+    for before in (0.0, g / 8192):
+        s.weight.fill_(before)
+        b.rdkv_slots_decode_attn(s, q)
+        for i, n in enumerate(lens):
+            assert off(host(s.weight)[i, :, :n], before + g / n) <= 2.0 ** -24 * (g + 2)
+            assert (s.weight[i, :, n:] == before).all()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("g", [1, 2, 4, 8])
+@pytest.mark.parametrize("capacity", sorted(LENS))
+@pytest.mark.parametrize("e, biased", [(10, False), (16, False), (23, False), (10, True)])
+def test_weights_of_two_scores(bits, g, capacity, e, biased):
+    """As the outputs: a probability's rounding, and the sum's."""
+    rng = np.random.default_rng(33)
+    s, V, lens, q = two_scores(rng, bits, g, capacity, e, biased)
+    b.rdkv_slots_decode_attn(s, q)
+    # the sum, of 64 slots a wavefront: four additions a tile and lane, and 4 + 3 + 20 of lanes, wavefronts and pieces
+    rel = 2 * (2 * 2.0 ** (e - 24) / math.sqrt(D) if biased else 0.0) + 2.0 ** -24 * (8 + 27 + g + 8)
+    for i, n in enumerate(lens):
+        assert off(host(s.weight)[i, :, :n], g * two_probabilities(n)) <= rel
