@@ -6,9 +6,10 @@
 //
 //   scores     lane = slot, four heads in a lane's registers: capped, biased and hidden there, and stored for the weights, which need
 //              every probability once the whole sum is known: 4 bytes per slot and query head, which stay in the caches
-//   precision  products of the query and of probabilities lose nothing that fp32 holds: bf16 rows meet a probability in three bf16 terms
-//              (24 bits), codes in two fp16 terms (22 bits), scaled so that the largest V scale seen stands just below fp16's largest
-//              and the query's largest value near 2^8
+//   precision  bf16 rows meet a probability in three bf16 terms, all of its 24 bits, codes in two fp16 terms (22 bits), scaled so that
+//              the largest V scale seen stands just below fp16's largest and a head's largest query value near 2^8.  (What fp16 terms lose
+//              of the small beside the large: a query value 2^-33 of its head's largest; of a probability times a V scale 2^-40 of the
+//              largest scale seen, so that rows whose scales are 2^20 smaller keep 20 bits)
 //   bound      HBM: 512 bytes a slot in bf16, 160 in 4 bits, and the scores.  4 x 8 items of 128K slots 6.8 and 6.1 TB/s without weights, 5.5
 //              and 4.6 with them; items one each to a workgroup 6.3 TB/s (256 of 4000 slots in bf16) and 4.8.  Small caches: latency
 //   work       lengths are on the device.  A workgroup takes an item, where there are enough for the card; otherwise it finds its piece
@@ -176,14 +177,34 @@ __device__ __forceinline__ int position(const Scoring& sc, int tile, int rows) {
   return static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(of, 4 * (threadIdx.x & 63), 0, 0));
 }
 
-// The power of two that score_tile leaves products over, unit; 1 with a cap or biases.
-__device__ __forceinline__ float left_unit(const Scoring& sc, float unit) { return sc.cap > 0.f || sc.biased ? 1.f : unit; }
-// xt: products q k over a power of two, unit; comes back as products over left_unit, or as scores, -inf where the slot is not seen.  The slots
-// that are.
+// Products q k come over a power of two of the head's, its unit.  With a cap or biases they become scores at once; otherwise that is left until
+// probabilities are made of them, or they are kept.
+struct NoUnits {                         // all 1
+  __device__ __forceinline__ float score(int, int) const { return kRoot; }
+  __device__ __forceinline__ float left(int, int) const { return 1.f; }
+};
+template <int HS>
+struct HeadUnits {
+  float of[HS][4];                       // of head 4 hs + i, in scalar registers: unit / sqrt(128), or unit if that is left
+  bool scored;
+  // unit: of the head 4 hs + lane % 4; comes back as what is left
+  __device__ __forceinline__ HeadUnits(const Scoring& sc, float (&unit)[HS]) : scored(sc.cap > 0.f || sc.biased) {
+#pragma unroll
+    for (int hs = 0; hs < HS; ++hs) {
+      const int u = __builtin_bit_cast(int, scored ? unit[hs] * kRoot : unit[hs]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) of[hs][i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(u, i));
+      if (scored) unit[hs] = 1.f;
+    }
+  }
+  __device__ __forceinline__ float score(int hs, int i) const { return of[hs][i]; }
+  __device__ __forceinline__ float left(int hs, int i) const { return scored ? 1.f : of[hs][i]; }
+};
+// xt: products over the heads' units; comes back as they are, or as scores, -inf where the slot is not seen.  The slots that are.
 //   The last factor, DecodeArgs::factor, is for differences from a maximum alone, here and in the merges, so that what is rounded is small where
 // the probability is not (8 items of 3700 slots in bf16: outputs 6.4e-7 -> 5.8e-7 off).
-template <int HS>
-__device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int pos, float unit, float (&xt)[HS][4]) {
+template <int HS, class Units>
+__device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int pos, const Units& units, float (&xt)[HS][4]) {
   const int lane = threadIdx.x & 63, row = tile * kTile + lane;
   bool seen = row < sc.n;
   const int away = sc.at - pos;
@@ -192,7 +213,7 @@ __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int 
 #pragma unroll
     for (int hs = 0; hs < HS; ++hs)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) xt[hs][i] *= unit * kRoot;
+      for (int i = 0; i < 4; ++i) xt[hs][i] *= units.score(hs, i);
   }
   if (sc.cap > 0.f) {
 #pragma unroll
@@ -215,13 +236,13 @@ __device__ __forceinline__ uint64_t score_tile(const Scoring& sc, int tile, int 
 
 // Online softmax of scores x times factor in the lanes (block, head), maxima as the x are; acc: whatever is scaled with the sums
 template <int HS>
-__device__ __forceinline__ void softmax_step(const float (&x)[HS][4], float factor, Run<HS>& run, float (&p)[HS][4]) {
+__device__ __forceinline__ void softmax_step(const float (&x)[HS][4], const float (&factor)[HS], Run<HS>& run, float (&p)[HS][4]) {
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
     const float most = max_of_four(x[hs][0], x[hs][1], x[hs][2], x[hs][3]);
     if (__any(most > run.m[hs])) {
       const float m_new = fmaxf(run.m[hs], head_max(most));
-      const float alpha = fast_exp2((run.m[hs] - m_new) * factor);
+      const float alpha = fast_exp2((run.m[hs] - m_new) * factor[hs]);
       run.l[hs] *= alpha;
       const uint32_t au = __builtin_bit_cast(uint32_t, alpha);
       const float ah[4] = {__builtin_bit_cast(float, quad_bcast<0>(au)), __builtin_bit_cast(float, quad_bcast<1>(au)),
@@ -236,7 +257,7 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], float fact
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      p[hs][i] = fast_exp2((x[hs][i] - run.m[hs]) * factor);
+      p[hs][i] = fast_exp2((x[hs][i] - run.m[hs]) * factor[hs]);
       run.l[hs] += p[hs][i];
     }
   }
@@ -245,10 +266,10 @@ __device__ __forceinline__ void softmax_step(const float (&x)[HS][4], float fact
 // The end of a wavefront's tiles: maxima without the unit.  A sum is nothing where its maximum is below what an exponent of 2 can be (0 x NaN
 // stays NaN).
 template <int HS>
-__device__ __forceinline__ void end_maxima(float unit, float factor, Run<HS>& run) {
+__device__ __forceinline__ void end_maxima(const float (&unit)[HS], float factor, Run<HS>& run) {
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
-    run.m[hs] *= unit;
+    run.m[hs] *= unit[hs];
     run.l[hs] *= run.m[hs] * factor < kLowest ? 0.f : 1.f;
   }
 }
@@ -261,18 +282,19 @@ __device__ __forceinline__ void end_maxima(float unit, float factor, Run<HS>& ru
 struct Held {
   uint8_t* at;         // of this wavefront: [tiles][64][g]
   int n, most;         // tiles there, and room; most 0: all of the item's stay
-  template <int HS, int NWV>
-  __device__ __forceinline__ void put(const Scoring& sc, int tile, bool last, const float (&xt)[HS][4], float unit) {
+  template <int HS, int NWV, class Units>
+  __device__ __forceinline__ void put(const Scoring& sc, int tile, bool last, const float (&xt)[HS][4], const Units& units) {
     if (!sc.tracked) return;
     const int lane = threadIdx.x & 63;
+    const auto x = [&](int hs, int i) __attribute__((always_inline)) { return units.left(hs, i) * xt[hs][i]; };
     float* dst = reinterpret_cast<float*>(at) + (n * kTile + lane) * sc.g;
     if constexpr (HS == 2) {
-      *reinterpret_cast<float4*>(dst) = make_float4(unit * xt[0][0], unit * xt[0][1], unit * xt[0][2], unit * xt[0][3]);
-      *reinterpret_cast<float4*>(dst + 4) = make_float4(unit * xt[1][0], unit * xt[1][1], unit * xt[1][2], unit * xt[1][3]);
+      *reinterpret_cast<float4*>(dst) = make_float4(x(0, 0), x(0, 1), x(0, 2), x(0, 3));
+      *reinterpret_cast<float4*>(dst + 4) = make_float4(x(1, 0), x(1, 1), x(1, 2), x(1, 3));
     } else {
-      if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(unit * xt[0][0], unit * xt[0][1], unit * xt[0][2], unit * xt[0][3]);
-      else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(unit * xt[0][0], unit * xt[0][1]);
-      else *dst = unit * xt[0][0];
+      if (sc.g == 4) *reinterpret_cast<float4*>(dst) = make_float4(x(0, 0), x(0, 1), x(0, 2), x(0, 3));
+      else if (sc.g == 2) *reinterpret_cast<float2*>(dst) = make_float2(x(0, 0), x(0, 1));
+      else *dst = x(0, 0);
     }
     ++n;
     if (n == most || (last && most > 0)) {
@@ -415,6 +437,12 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
       for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(qa[hs][i].x), "+v"(qa[hs][i].y), "+v"(qa[hs][i].z), "+v"(qa[hs][i].w));
   }
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
+  float all[HS], ones[HS];
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) {
+    all[hs] = factor;
+    ones[hs] = 1.f;
+  }
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
     const int next = tile + NWV, next_rows = next < t1 ? rows_known(sc, next, sc.n) : 0;
     float xt[HS][4], x[HS][4];
@@ -451,11 +479,11 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
           xt[hs][i] = half == 0 || !(lr & 2) ? (half == 0 ? v : xt[hs][i]) : v;
         }
     }
-    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, 1.f, xt);
-    held.put<HS, NWV>(sc, tile, next >= t1, xt, 1.f);
+    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, NoUnits(), xt);
+    held.put<HS, NWV>(sc, tile, next >= t1, xt, NoUnits());
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
-    softmax_step<HS>(x, factor, run, p);
+    softmax_step<HS>(x, all, run, p);
     short4v t[HS][3];
 #pragma unroll
     for (int hs = 0; hs < HS; ++hs) split_bf16_3(p[hs], t[hs]);
@@ -475,7 +503,7 @@ __device__ __forceinline__ void rows_segment(const uint8_t* __restrict__ kd, con
     pv_rows<8, HS>(s_stage, lane, t, run, std::make_integer_sequence<int, 8>{});
     wave_lds_sync();                    // before the next rows overwrite the region
   }
-  end_maxima<HS>(1.f, factor, run);
+  end_maxima<HS>(ones, factor, run);
 }
 
 // ---- 4-bit rows --------------------------------------------------------------------------------------------------------------------
@@ -578,25 +606,24 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   load_k(t0 + wave, rows_known(sc, t0 + wave, sc.sure));
   load_v(t0 + wave, rows_known(sc, t0 + wave, sc.sure));
 
-  // ---- query operands: times the power of two that puts the largest value of all heads near 2^kQUp ------------------
+  // ---- query operands: times the power of two that puts a head's largest value near 2^kQUp ------------------------------
+  // (What is 2^22 smaller has fewer digits there, what is 2^33 smaller none: 2^-33 of the largest value, as far as its own products in fp32
+  // go.)
   half4 qop[HS][2], qhi[HS], qlo[HS];
-  float most = 0.f;
+  float unit[HS];
 #pragma unroll
   for (int hs = 0; hs < HS; ++hs) {
+    float most = 0.f;
     const uint32_t w[4] = {qraw[hs].x, qraw[hs].y, qraw[hs].z, qraw[hs].w};
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const uint32_t u = (e == 0 ? w[k] << 16 : w[k] & 0xFFFF0000u) & 0x7FFFFFFFu;
-        most = fmaxf(most, u < 0x7F800000u ? __uint_as_float(u) : 0.f);      // (a head that is not finite stays by itself)
+        most = fmaxf(most, u < 0x7F800000u ? __uint_as_float(u) : 0.f);
       }
-  }
-  const int up = __builtin_amdgcn_readfirstlane(max(-120, min(120, kQUp - exponent_of(wave_max(most)))));
-  const float unit = ldexpf(1.0f, -up);
-#pragma unroll
-  for (int hs = 0; hs < HS; ++hs) {
-    const uint32_t w[4] = {qraw[hs].x, qraw[hs].y, qraw[hs].z, qraw[hs].w};
+    const int up = max(-120, min(120, kQUp - exponent_of(head_max(most))));
+    unit[hs] = ldexpf(1.0f, -up);
     float v[8];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -631,7 +658,10 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
   int ve = -126;                         // exponent of the largest V scale so far
   float vf = 0.f;                        // what p is multiplied by for it
   const floatx4 zero4 = {0.f, 0.f, 0.f, 0.f};
-  const float left = left_unit(sc, unit), all = left * factor;
+  const HeadUnits<HS> units(sc, unit);
+  float all[HS];
+#pragma unroll
+  for (int hs = 0; hs < HS; ++hs) all[hs] = unit[hs] * factor;
 
   for (int tile = t0 + wave; tile < t1; tile += NWV) {
     const int next = tile + NWV, next_rows = next < t1 ? rows_known(sc, next, sc.n) : 0;
@@ -671,8 +701,8 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 #undef RDKV_K_STEP
     }
     load_k(next, next_rows);
-    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, unit, xt);
-    held.put<HS, NWV>(sc, tile, next >= t1, xt, left);
+    const uint64_t seen = score_tile<HS>(sc, tile, pos_now, units, xt);
+    held.put<HS, NWV>(sc, tile, next >= t1, xt, units);
     to_head_lanes<HS, HS == 2>(xt, j, x);
     float p[HS][4];
     softmax_step<HS>(x, all, run, p);
@@ -746,7 +776,7 @@ __device__ __forceinline__ float tiles_segment(const uint8_t* __restrict__ kd, c
 #undef RDKV_PV_STEP
     load_v(next, next_rows);
   }
-  end_maxima<HS>(left, factor, run);
+  end_maxima<HS>(unit, factor, run);
   return ldexpf(1.0f, 1 + ve - kPUp);    // what brings the accumulators to the sums' scale, vf's inverse
 }
 

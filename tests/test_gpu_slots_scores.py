@@ -7,7 +7,7 @@ import torch
 
 from paper_2605_08317_amd import binding as b
 from tests import slots_plain as P
-from tests.test_gpu_slots import BF, D, F32, I32, cuda, host, tiles_of
+from tests.test_gpu_slots import BF, D, I32, check_step, cuda, host, loaded, tiles_of
 
 pytestmark = pytest.mark.gpu
 
@@ -151,3 +151,20 @@ def test_weights_of_two_scores(bits, g, capacity, e, biased):
     rel = 2 * (2 * 2.0 ** (e - 24) / math.sqrt(D) if biased else 0.0) + 2.0 ** -24 * (8 + 27 + g + 8)
     for i, n in enumerate(lens):
         assert off(host(s.weight)[i, :, :n], g * two_probabilities(n)) <= rel
+
+
+# ---- heads of one group far from each other ----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("e", [[30, 0], [25, 0, -8, 12], [0, 40, -3, -20, 60, 1, -60, 18]])
+@pytest.mark.parametrize("lens, capacity", [([300, 77], 300), ([5000, 64], 5000)])
+@pytest.mark.parametrize("kw", [{}, {"score_cap": 30.0}])
+def test_heads_of_different_magnitudes(bits, e, lens, capacity, kw):
+    """Queries 2^e times normal numbers: each head's scores keep their own digits."""
+    rng = np.random.default_rng(34)
+    g = len(e)
+    s, items = loaded(rng, lens, 2 * g, 2, capacity, bits, **kw)
+    q = rng.standard_normal((2, 2 * g, D)) * 2.0 ** np.array(e * 2)[None, :, None]
+    before = host(s.weight)
+    out, lse = b.rdkv_slots_decode_attn(s, cuda(q, BF))
+    check_step(s, items, cuda(q, BF), out, lse, s.weight, before, **({"cap": 30.0} if kw else {}))
