@@ -392,8 +392,8 @@ int32_t rdkv_k_row_words_max(void);
  * caches they may overlap where their workspaces are apart.  Outputs share no memory with inputs.  A len outside
  * 0..capacity is taken for the nearer of the two.
  * Rows are aligned to 16 bytes: so are k, v, q, out and the rows of prompts and new tokens.
- * Limits: batch hkv (capacity + 64) < 2^31 slots, batch hq < 2^22 heads; a fill puts less than 2^28 rows into an item, a read
- * returns less than 2^28 rows.
+ * Limits: batch hkv (capacity + 64) < 2^31 slots, batch hq < 2^22 heads; a fill puts at most 2^28 - 16 rows into an item, a
+ * read returns batch hkv (n + 64) < 2^28 rows.
  */
 typedef struct rdkv_slots {
   int32_t batch;            /* number of sequences */

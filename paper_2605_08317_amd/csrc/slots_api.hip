@@ -140,8 +140,10 @@ rdkv_status rdkv_slots_fill(const rdkv_slots* s, int32_t first, int32_t n, const
   if (longest > 0 && (!K || !V)) return fail(RDKV_ERR_INVALID_ARG, "K and V must not be null");
   if (longest > s->capacity && !w_tok)
     return fail(RDKV_ERR_INVALID_ARG, "a prompt of %d tokens for %d slots needs w_tok", longest, s->capacity);
-  // sixteen threads a row (four in tiles), an item after the other
-  if (std::min(longest, s->capacity) >= kMostThreads / 16) return fail(RDKV_ERR_SHAPE, "%d rows of an item exceed 2^28", std::min(longest, s->capacity));
+  // sixteen rows a workgroup, sixteen threads a row (fewer in tiles): a launch has less than 2^32 threads
+  const int64_t rows = std::min(longest, s->capacity);
+  if ((rows + 15) / 16 * 256 >= kMostThreads)
+    return fail(RDKV_ERR_SHAPE, "%lld rows of an item: at most 2^28 - 16", static_cast<long long>(rows));
   const SelectBytes need = select_bytes(s, n, seq_lens);
   if (need.total > 0 && (!workspace || workspace_bytes < need.total))
     return fail(RDKV_ERR_INVALID_ARG, "workspace of %zu bytes is smaller than the %zu required", workspace ? workspace_bytes : 0, need.total);

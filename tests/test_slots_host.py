@@ -145,3 +145,12 @@ def test_the_ctypes_struct_matches_the_c_header(tmp_path):
     subprocess.run(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
     out = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
     assert out == [ctypes.sizeof(b.rdkv_slots)] + [getattr(b.rdkv_slots, f).offset for f in fields]
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_the_most_rows_that_a_fill_puts_into_an_item(bits):
+    """2^28 - 16: with one more, the launch that copies rows has 2^32 threads.  (Pointers that are not aligned: nothing is launched either way.)"""
+    s = struct(batch=1, hq=1, hkv=1, capacity=2 ** 29, bits=bits)
+    for n, status in ((2 ** 28 - 16, INVALID), (2 ** 28 - 15, SHAPE), (2 ** 28 - 1, SHAPE), (2 ** 28, SHAPE)):
+        lens = (ctypes.c_int32 * 1)(n)
+        assert b.lib.rdkv_slots_fill(ctypes.byref(s), 0, 1, lens, 24, 24, 16, None, 0, None) == status, n
