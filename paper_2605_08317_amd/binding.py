@@ -447,7 +447,36 @@ class Slots:
       slopes    float32 [hq] or None
 
     The calls on it run on the current stream of its device.  A call leaves tensors it was given where they are, so that views
-    of them stay good."""
+    of them stay good.  A tensor assigned to one of these names takes the place of the one before from the next call on (graphs
+    that were captured go on with the one before); what shapes follow from stays as it was made."""
+
+    _FIELDS = {"k": "k", "v": "v", "pos": "pos", "weight": "weight", "lens": "len", "next_pos": "next", "slopes": "slopes"}
+    _FIXED = ("c", "device", "batch", "hq", "hkv", "capacity", "bits", "d", "workspace_bytes", "address")
+
+    def __setattr__(self, name, value):
+        if name in self._FIELDS:
+            if value is not None:
+                _tensor(value, *self._shapes[name], self.device, name)
+            elif name not in ("weight", "slopes"):
+                raise ValueError(f"{name} must be a tensor")
+            setattr(self.c, self._FIELDS[name], None if value is None else value.data_ptr())
+            if name == "weight":                       # (a step keeps scores for them)
+                self.__dict__["workspace_bytes"] = lib.rdkv_slots_decode_workspace_bytes(ctypes.byref(self.c))
+        elif name in self._FIXED and name in self.__dict__:
+            raise AttributeError(f"{name} of a slot cache stays as it was made")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        if name in self._FIELDS or name in self._FIXED:
+            raise AttributeError(f"{name} belongs to the slot cache")
+        super().__delattr__(name)
+
+    def __copy__(self):
+        """Another with the same tensors."""
+        c = self.c
+        return Slots(c.batch, c.hq, c.hkv, c.capacity, bits=c.bits, head_dim=c.head_dim, sinks=c.sinks, recent=c.recent, window=c.window,
+                     score_cap=c.score_cap, decay=c.decay, track=self.weight is not None, device=self.device,
+                     **{name: getattr(self, name) for name in self._FIELDS})
 
     def __init__(self, batch, hq, hkv, capacity, bits=16, head_dim=128, sinks=0, recent=0, window=0, score_cap=0.0, decay=1.0,
                  slopes=None, k=None, v=None, pos=None, weight=None, lens=None, next_pos=None, track=True, device=None):
@@ -461,28 +490,24 @@ class Slots:
         c.k = c.v = c.pos = c.len = c.next = 16        # (what the library checks of memory is that there is some)
         _check(lib.rdkv_slots_read(ctypes.byref(c), None, 0, None, None, None))
         held = [t for t in (k, v, pos, weight, lens, next_pos) if t is not None]
-        self.device = torch.device(device) if device is not None else held[0].device if held else torch.device("cuda")
-        if self.device.type == "cuda" and self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
+        device = torch.device(device) if device is not None else held[0].device if held else torch.device("cuda")
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
         self.batch, self.hq, self.hkv, self.capacity, self.bits, self.d = c.batch, c.hq, c.hkv, c.capacity, c.bits, c.head_dim
         items = (c.batch, c.hkv)
         side = items + ((c.capacity, c.head_dim) if c.bits == 16 else ((c.capacity + 63) // 64, 5120))
         kind = torch.bfloat16 if c.bits == 16 else torch.uint8
 
-        def tensor(t, shape, dtype, name):
-            if t is None:
-                return torch.zeros(shape, dtype=dtype, device=self.device)
-            return _tensor(t, shape, dtype, self.device, name)
+        self._shapes = {"k": (side, kind), "v": (side, kind), "pos": (items + (c.capacity,), torch.int32),
+                        "weight": (items + (c.capacity,), torch.float32), "lens": (items, torch.int32), "next_pos": (items, torch.int32),
+                        "slopes": ((c.hq,), torch.float32)}
 
-        self.k, self.v = tensor(k, side, kind, "k"), tensor(v, side, kind, "v")
-        self.pos = tensor(pos, items + (c.capacity,), torch.int32, "pos")
-        self.weight = tensor(weight, items + (c.capacity,), torch.float32, "weight") if track or weight is not None else None
-        self.lens, self.next_pos = tensor(lens, items, torch.int32, "lens"), tensor(next_pos, items, torch.int32, "next_pos")
-        self.slopes = None if slopes is None else _tensor(slopes, (c.hq,), torch.float32, self.device, "slopes")
-        for name, t in (("k", self.k), ("v", self.v), ("pos", self.pos), ("weight", self.weight), ("len", self.lens),
-                        ("next", self.next_pos), ("slopes", self.slopes)):
-            setattr(c, name, None if t is None else t.data_ptr())
-        self.workspace_bytes = lib.rdkv_slots_decode_workspace_bytes(ctypes.byref(c))
+        def tensor(t, name):
+            return torch.zeros(self._shapes[name][0], dtype=self._shapes[name][1], device=self.device) if t is None else t
+
+        self.k, self.v, self.pos = tensor(k, "k"), tensor(v, "v"), tensor(pos, "pos")
+        self.weight = tensor(weight, "weight") if track or weight is not None else None
+        self.lens, self.next_pos = tensor(lens, "lens"), tensor(next_pos, "next_pos")
+        self.slopes = slopes
         self.address = ctypes.addressof(c)
 
     def ref(self):

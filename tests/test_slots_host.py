@@ -1,4 +1,5 @@
 """What the slot caches' entry points refuse, without a GPU: nothing is launched for a bad argument."""
+import copy
 import ctypes
 import os
 import subprocess
@@ -154,3 +155,40 @@ def test_the_most_rows_that_a_fill_puts_into_an_item(bits):
     for n, status in ((2 ** 28 - 16, INVALID), (2 ** 28 - 15, SHAPE), (2 ** 28 - 1, SHAPE), (2 ** 28, SHAPE)):
         lens = (ctypes.c_int32 * 1)(n)
         assert b.lib.rdkv_slots_fill(ctypes.byref(s), 0, 1, lens, 24, 24, 16, None, 0, None) == status, n
+
+
+def test_a_tensor_assigned_to_a_cache_is_the_one_its_calls_use():
+    s = b.Slots(2, 8, 2, 9000, slopes=torch.zeros(8), device="cpu")
+    assert (s.c.k, s.c.weight, s.c.slopes, s.c.len) == (s.k.data_ptr(), s.weight.data_ptr(), s.slopes.data_ptr(), s.lens.data_ptr())
+    fields = {"k": "k", "v": "v", "pos": "pos", "weight": "weight", "lens": "len", "next_pos": "next", "slopes": "slopes"}
+    for name, field in fields.items():
+        new = torch.zeros_like(getattr(s, name))
+        setattr(s, name, new)
+        assert getattr(s, name) is new and getattr(s.c, field) == new.data_ptr(), name
+        for bad in (new[:1], new.double(), new.unsqueeze(0), new.transpose(0, -1) if new.dim() > 1 else new[::2]):
+            with pytest.raises(ValueError):
+                setattr(s, name, bad)
+            assert getattr(s, name) is new and getattr(s.c, field) == new.data_ptr(), name
+        with pytest.raises(AttributeError):
+            delattr(s, name)
+        if name not in ("weight", "slopes"):
+            with pytest.raises(ValueError):
+                setattr(s, name, None)
+    for name in ("c", "device", "batch", "hq", "hkv", "capacity", "bits", "d", "workspace_bytes", "address"):
+        with pytest.raises(AttributeError):
+            setattr(s, name, getattr(s, name))
+    kept = s.workspace_bytes
+    s.weight = s.slopes = None
+    assert s.c.weight is None and s.c.slopes is None and s.workspace_bytes < kept
+    s.weight = torch.zeros(2, 2, 9000)
+    assert s.workspace_bytes == kept == s.workspace().numel()
+
+
+def test_a_copy_of_a_cache_has_its_tensors_and_a_struct_of_its_own():
+    s = b.Slots(2, 8, 2, 100, bits=4, sinks=3, recent=5, window=50, score_cap=20.0, decay=0.5, slopes=torch.zeros(8), device="cpu")
+    t = copy.copy(s)
+    assert t.address != s.address and all(getattr(t.c, f[0]) == getattr(s.c, f[0]) for f in b.rdkv_slots._fields_)
+    t.k, old = torch.zeros_like(s.k), s.k
+    assert s.k is old and s.c.k == old.data_ptr() and t.c.k == t.k.data_ptr()
+    s.weight = None
+    assert copy.copy(s).weight is None
