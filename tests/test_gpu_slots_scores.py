@@ -168,3 +168,44 @@ def test_heads_of_different_magnitudes(bits, e, lens, capacity, kw):
     before = host(s.weight)
     out, lse = b.rdkv_slots_decode_attn(s, cuda(q, BF))
     check_step(s, items, cuda(q, BF), out, lse, s.weight, before, **({"cap": 30.0} if kw else {}))
+
+
+# ---- how many digits a probability has -----------------------------------------------------------------------------------------------------
+
+def a_term_less(p, bits):
+    """Probabilities as they would meet the rows with one term less: two bf16 terms, cut off, or one of fp16."""
+    p = p.astype(np.float32)
+    if bits == 4:
+        return (p * np.float32(2 ** 14)).astype(np.float16).astype(np.float64) / 2 ** 14
+    hi = (p.view(np.uint32) & np.uint32(0xFFFF0000)).view(np.float32)
+    lo = ((p - hi).view(np.uint32) & np.uint32(0xFFFF0000)).view(np.float32)
+    return hi.astype(np.float64) + lo
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("g", [1, 4, 8])
+@pytest.mark.parametrize("capacity", [300, 5000])
+def test_probabilities_keep_their_digits(bits, g, capacity):
+    """One token, and others whose products with the query are 29 less, exp(-29 / sqrt(128)) of its probability, a number that loses much
+    with a term less.  Values are not negative, so that nothing cancels.  In units of 2^-24: the exponent 3.7 is rounded by 2 and its factor
+    by 1.9, times ln 2; the exponential by 2: 5 of a probability, twice.  A wavefront's tile: 4 + 4 additions to its sum; 16 steps of three
+    terms to the outputs, each off by 2 at most; the merge 8 and 8, the quotient 2."""
+    rng = np.random.default_rng(35)
+    bound = 2.0 ** -24 * (2 * 5 + 8 + 2 * 48 + 16 + 2)
+    lens = [200, 77]
+    K = [[np.zeros((n, D), np.float32)] * 2 for n in lens]
+    for two in K:
+        two[0][0, :32] = 29.0
+    V = [[codes(rng, n) for _ in range(2)] for n in lens]
+    s = cache(K, V, lens, 2 * g, capacity, bits)
+    q = torch.zeros((2, 2 * g, D), device="cuda", dtype=BF)
+    q[:, :, 0] = 1.0
+    out, _ = b.rdkv_slots_decode_attn(s, q)
+    for i, n in enumerate(lens):
+        e = np.where(np.arange(n) == 0, 1.0, math.exp(-29 / math.sqrt(D)))
+        p = e / e.sum()
+        for h in range(2):
+            v, size = V[i][h].astype(np.float64), p @ P.terms(V[i][h], bits, 8) + 1e-30
+            assert np.max(np.abs(host(out)[i, h * g:(h + 1) * g] - p @ v) / size) <= bound
+            # (the bound would see it)
+            assert np.max(np.abs(a_term_less(e, bits) @ v / e.sum() - p @ v) / size) > 2 * bound
