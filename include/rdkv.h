@@ -461,8 +461,9 @@ rdkv_status rdkv_slots_append(const rdkv_slots* slots, const void* k_new, const 
  *   lse     DEVICE fp32 [batch][hq] or NULL: natural-log sum of exp of the scores; -inf where no token is seen
  *   weight (of the cache) becomes decay x weight + the softmax's value, summed over the heads of the group, in slots below len
  *   workspace  DEVICE scratch of at least rdkv_slots_decode_workspace_bytes(), 16-byte aligned
- * A score that is NaN or +inf makes its head's out, lse and weights NaN; one below -2.35e38 (fp32's range, in units of log 2)
- * takes no part.
+ * A score that is NaN or +inf makes its head's out, lse and weights NaN; one below -2.35e38 (fp32's range, in units of log 2), or
+ * whose q k is below fp32's range, takes no part.
+ * Probabilities come from differences of scores, each score an fp32 number: a large one common to all tokens costs them nothing.
  */
 size_t rdkv_slots_decode_workspace_bytes(const rdkv_slots* slots);
 rdkv_status rdkv_slots_decode_attn(const rdkv_slots* slots, const void* q, float* out, float* lse, void* workspace,

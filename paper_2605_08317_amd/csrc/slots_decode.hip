@@ -9,9 +9,9 @@
 //   precision  bf16 rows meet a probability in three bf16 terms, all of its 24 bits, codes in two fp16 terms (22 bits), scaled so that
 //              the largest V scale seen stands just below fp16's largest and a head's largest query value near 2^8.  (What fp16 terms lose
 //              of the small beside the large: a query value 2^-33 of its head's largest; of a probability times a V scale 2^-40 of the
-//              largest scale seen, so that rows whose scales are 2^20 smaller keep 20 bits)
+//              largest scale seen, so that a probability near 1 keeps 20 bits where its row's scale is 2^20 smaller than that)
 //   bound      HBM: 512 bytes a slot in bf16, 160 in 4 bits, and the scores.  4 x 8 items of 128K slots 6.8 and 6.1 TB/s without weights, 5.5
-//              and 4.6 with them; items one each to a workgroup 6.3 TB/s (256 of 4000 slots in bf16) and 4.8.  Small caches: latency
+//              and 4.5 with them; items one each to a workgroup 6.3 TB/s (256 of 4000 slots in bf16) and 4.8.  Small caches: latency
 //   work       lengths are on the device.  A workgroup takes an item, where there are enough for the card; otherwise it finds its piece
 //              of one by itself, nearly equal ones, which leave partial results for the launch that follows
 #include <algorithm>
@@ -277,7 +277,7 @@ __device__ __forceinline__ void end_maxima(const float (&unit)[HS], float factor
 // Scores on their way to the weights, which need them once the item's sums are known.  They wait in LDS: where a workgroup has all of an
 // item until then, otherwise until a wavefront's part is full, which then goes to the workspace at once.  Writes among the reads of rows
 // cost more than their bytes.  4 x 8 items of 128K slots, 4 heads, us, with the launch that joins them: bf16 318 without weights, 401 with a
-// store a tile, 391 so; 4 bits 110, 158, 147.  (334 and 126 of them if nothing is written; with waits that count these stores, or with
+// store a tile, 391 so; 4 bits 110, 158, 148.  (334 and 126 of them if nothing is written; with waits that count these stores, or with
 // non-temporal ones, no less.)
 struct Held {
   uint8_t* at;         // of this wavefront: [tiles][64][g]
@@ -322,7 +322,7 @@ __device__ __forceinline__ void init(Run<HS>& run) {
 }
 
 // Sixteen bytes of a tile.  STREAM: non-temporal, so that rows, which a step reads once, do not push scores out of the caches: 4 x 8 items of
-// 128K slots in bf16 432 -> 388 us, without weights 357 -> 313 (6.8 TB/s).  Small caches may still be there from the step before: 32 of 2
+// 128K slots in bf16 430 -> 391 us, without weights 361 -> 318 (6.8 TB/s).  Small caches may still be there from the step before: 32 of 2
 // items of 1000 slots 16.0 us each with it, 13.3 without, 4 of 32 items of 8K in 4 bits (40 MB) 22.3, 20.8.  The line is at 64 MiB of rows.
 // (here(): a value that the compiler sees the loop make, so that constants added to it become the loads' offsets and not registers each.)
 __device__ __forceinline__ int here(int x) {
@@ -568,7 +568,7 @@ __device__ __forceinline__ void centres(uint32_t s01, uint32_t s23, uint32_t m01
   }
 }
 
-constexpr int kQUp = 8;                  // the query's largest value is near 2^kQUp
+constexpr int kQUp = 8;                  // a head's largest query value is near 2^kQUp
 constexpr int kPUp = 15;                 // probabilities go into fp16 terms times 2^kPUp.  (Not through the exponentials: x - m + 15 has four bits
                                          // less behind the point than x - m near 0, 5e-7 of a probability)
 
