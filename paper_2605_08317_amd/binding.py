@@ -431,9 +431,9 @@ def rdkv_decode_attn_bf16_noalloc(K, V, seq_lens, hq, hkv, q, out, lse=None, hea
 
 
 def _int32(name, x):
-    """A number that ctypes would otherwise cut to 32 bits."""
-    if not -2 ** 31 <= int(x) < 2 ** 31:
-        raise ValueError(f"{name} = {x} is no 32-bit number")
+    """A number that ctypes would otherwise cut to 32 bits, or int() to a whole one."""
+    if x != x or int(x) != x or not -2 ** 31 <= int(x) < 2 ** 31:
+        raise ValueError(f"{name} = {x} is no whole 32-bit number")
     return int(x)
 
 
@@ -487,6 +487,8 @@ class Slots:
                         ("sinks", sinks), ("recent", recent), ("window", window)):
             setattr(c, name, _int32(name, x))
         c.score_cap, c.decay = float(score_cap), float(decay)
+        if c.score_cap == 0 and score_cap != 0:        # (0 is no cap)
+            raise ValueError(f"score_cap = {score_cap} is 0 in 32 bits")
         c.k = c.v = c.pos = c.len = c.next = 16        # (what the library checks of memory is that there is some)
         _check(lib.rdkv_slots_read(ctypes.byref(c), None, 0, None, None, None))
         held = [t for t in (k, v, pos, weight, lens, next_pos) if t is not None]

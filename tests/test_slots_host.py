@@ -192,3 +192,18 @@ def test_a_copy_of_a_cache_has_its_tensors_and_a_struct_of_its_own():
     assert s.k is old and s.c.k == old.data_ptr() and t.c.k == t.k.data_ptr()
     s.weight = None
     assert copy.copy(s).weight is None
+
+
+def test_numbers_that_the_struct_cannot_hold_are_refused():
+    """A cap that 32 bits make 0 would be no cap; half a slot is none."""
+    for cap in (1e-50, -1e-50, 1e-46):
+        with pytest.raises(ValueError, match="score_cap"):
+            b.Slots(2, 8, 2, 100, score_cap=cap, device="cpu")
+    for bad in (dict(capacity=100.5), dict(sinks=0.5), dict(window=1e3 + 0.25), dict(recent=float("nan"))):
+        with pytest.raises(ValueError):
+            b.Slots(**dict(dict(batch=2, hq=8, hkv=2, capacity=100, device="cpu"), **bad))
+    s, rows = b.Slots(2, 8, 2, 100.0, device="cpu"), torch.zeros(2 * 2 * 5, 128, dtype=torch.bfloat16)
+    assert s.capacity == 100
+    for call in (lambda: b.rdkv_slots_fill(s, rows, rows, [5.5, 4.5]), lambda: b.rdkv_slots_fill(s, rows, rows, [5, 5], first=0.5), lambda: b.rdkv_slots_read(s, n=2.5)):
+        with pytest.raises(ValueError, match="32-bit"):
+            call()
