@@ -380,6 +380,39 @@ int32_t rdkv_k_row_words(const uint8_t* bits_ch);
 int32_t rdkv_k_row_words_max(void);
 
 /*
+ * Causal attention of whole prompts, bf16: what comes before a cache is made of their K and V (rdkv_compress, rdkv_slots_fill, or
+ * the rows as they are, rdkv_decode_attn_bf16).  Token i of a sequence attends to its tokens j <= i; with a window to those with
+ * i - j < window, and to the first `sinks`.
+ *   score = q k / sqrt d, capped (score_cap), less slopes[h] x (i - j); tokens that are not seen take no part, whatever their
+ *   rows hold
+ *   Q, out  DEVICE bf16, hq heads;  K, V  DEVICE bf16, hkv heads.  Each has a layout of its own, named by its stride:
+ *           0: ragged [heads][T_s][d] blocks; otherwise the elements from one token's row to the next's, tokens of the batch one
+ *           after another and a row's heads side by side ([tokens][heads][d], or a part of a wider row of a joint projection)
+ *   out     softmax(scores) V; 0 where no token takes part
+ *   lse     DEVICE fp32, ragged [hq][T_s], or NULL: natural-log sum of exp of the scores; -inf where no token takes part
+ * A score that is NaN or +inf makes its row's out and lse NaN; one below -2e38, or -inf, takes no part.  Scores, maxima and sums are fp32;
+ * probabilities meet V rounded to bf16, once, over a reference of the row's.
+ * Allocates and waits for nothing; may be recorded under graph capture (lengths by value).  Pointers are aligned to 16 bytes, strides
+ * multiples of 8, from heads x 128 to 2^23; out shares no memory with the inputs.  T_s >= 0.  Limits: the sum of hq T_s is
+ * below 2^31; 64 sequences a launch, and a launch has less than 2^24 workgroups (of 32 to 256 rows of a head).
+ */
+typedef struct rdkv_prompt {
+  int32_t batch;            /* number of sequences */
+  int32_t hq, hkv;          /* query heads, KV heads; hq / hkv in {1, 2, 4, 8} */
+  int32_t head_dim;         /* must be 128 */
+  const int32_t* seq_lens;  /* HOST [batch] */
+  int32_t window, sinks;    /* 0, or: a token sees those less than `window` positions back, and those at positions below `sinks` */
+  float score_cap;          /* 0, or a normal number c > 0: scores become c tanh(score / c) */
+  const float* slopes;      /* DEVICE [hq] or NULL */
+  int64_t q_stride, k_stride, v_stride, out_stride;
+} rdkv_prompt;
+
+/* head_dim 128; everything else zero. */
+rdkv_status rdkv_prompt_default(rdkv_prompt* prompt);
+rdkv_status rdkv_prompt_attn_bf16(const rdkv_prompt* prompt, const void* Q, const void* K, const void* V, void* out, float* lse,
+                                  void* stream);
+
+/*
  * Slot caches: a cache that stays at a fixed size while a generation grows.  Every item, a (sequence, KV head), has
  * `capacity` slots; a slot holds one token's K row and V row, its position, and the attention weight it has gathered.  A
  * prompt fills the slots with its first tokens, its last ones, and those of largest weight (rdkv_slots_fill, with the weights

@@ -32,6 +32,7 @@ EXPORTED_SYMBOLS = [
     "rdkv_cache_rebudget_tail", "rdkv_cache_generations", "rdkv_cache_generation",
     "rdkv_cache_stats", "rdkv_cache_export_bytes", "rdkv_cache_export", "rdkv_cache_free",
     "rdkv_kernel_timing_enable", "rdkv_kernel_timing_read", "rdkv_k_row_words", "rdkv_k_row_words_max",
+    "rdkv_prompt_default", "rdkv_prompt_attn_bf16",
     "rdkv_slots_default", "rdkv_slots_side_bytes", "rdkv_slots_fill_workspace_bytes", "rdkv_slots_fill", "rdkv_slots_append",
     "rdkv_slots_decode_workspace_bytes", "rdkv_slots_decode_attn", "rdkv_slots_read",
 ]
@@ -64,6 +65,15 @@ class rdkv_slots(ctypes.Structure):
         ("window", ctypes.c_int32), ("score_cap", ctypes.c_float), ("decay", ctypes.c_float), ("slopes", ctypes.c_void_p),
         ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("weight", ctypes.c_void_p),
         ("len", ctypes.c_void_p), ("next", ctypes.c_void_p),
+    ]
+
+
+class rdkv_prompt(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("hq", ctypes.c_int32), ("hkv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("seq_lens", ctypes.POINTER(ctypes.c_int32)), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+        ("score_cap", ctypes.c_float), ("slopes", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
     ]
 
 
@@ -129,6 +139,8 @@ def _load():
     lib.rdkv_k_row_words.restype = i32
     lib.rdkv_k_row_words_max.argtypes = []
     lib.rdkv_k_row_words_max.restype = i32
+    lib.rdkv_prompt_default.argtypes = [ctypes.POINTER(rdkv_prompt)]
+    lib.rdkv_prompt_attn_bf16.argtypes = [ctypes.POINTER(rdkv_prompt), vp, vp, vp, vp, vp, vp]
     slp = ctypes.POINTER(rdkv_slots)
     lib.rdkv_slots_default.argtypes = [slp]
     lib.rdkv_slots_side_bytes.argtypes = [slp]
@@ -437,6 +449,48 @@ def _int32(name, x):
     return int(x)
 
 
+def _rows_of(t, name, tokens, heads, d, device):
+    """The stride that names a tensor's layout: 0 of a flat ragged one, or that of rows [tokens, heads, d] whose heads lie side by side."""
+    if t.dtype != torch.bfloat16 or t.device != device:
+        raise ValueError(f"{name} must be a torch.bfloat16 tensor on {device}: got {t.dtype} on {t.device}")
+    if t.dim() in (1, 2):
+        if not t.is_contiguous() or t.numel() != tokens * heads * d or t.dim() == 2 and t.shape[1] != d:
+            raise ValueError(f"{name} must be {tokens * heads} contiguous rows of {d}, flat, or [tokens, heads, {d}]: got {tuple(t.shape)}")
+        return 0
+    if tuple(t.shape) != (tokens, heads, d) or t.numel() > 0 and (t.stride(2) != 1 or heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name} must be [{tokens}, {heads}, {d}] with a row's heads side by side, or flat: got {tuple(t.shape)}, strides {t.stride()}")
+    return t.stride(0) if tokens > 1 else heads * d
+
+
+def rdkv_prompt_attn_bf16(Q, K, V, seq_lens, hq, hkv, head_dim=128, window=0, sinks=0, score_cap=0.0, slopes=None, out=None, lse=None):
+    """(out, lse).  Each of Q, K, V and out is either flat (ragged [heads][T_s][head_dim] blocks: one dimension, or rows of head_dim) or
+    [tokens, heads, head_dim] (tokens of the batch one after another; a view of wider rows will do); out is laid out as Q unless it is given.
+    lse: float32, ragged [hq][T_s]."""
+    c = rdkv_prompt()
+    _check(lib.rdkv_prompt_default(ctypes.byref(c)))
+    lens = (ctypes.c_int32 * max(len(seq_lens), 1))(*[_int32("seq_lens", x) for x in seq_lens])
+    c.batch, c.seq_lens = len(seq_lens), ctypes.cast(lens, ctypes.POINTER(ctypes.c_int32))
+    for name, x in (("hq", hq), ("hkv", hkv), ("head_dim", head_dim), ("window", window), ("sinks", sinks)):
+        setattr(c, name, _int32(name, x))
+    c.score_cap = float(score_cap)
+    if c.score_cap == 0 and score_cap != 0:            # (0 is no cap)
+        raise ValueError(f"score_cap = {score_cap} is 0 in 32 bits")
+    device, tokens, d = Q.device, sum(max(x, 0) for x in lens[:len(seq_lens)]), c.head_dim
+    c.q_stride, c.k_stride, c.v_stride = (_rows_of(t, name, tokens, h, d, device) for t, name, h in ((Q, "Q", c.hq), (K, "K", c.hkv), (V, "V", c.hkv)))
+    if slopes is not None:
+        c.slopes = _tensor(slopes, (c.hq,), torch.float32, device, "slopes").data_ptr()
+    if out is None:
+        out = torch.empty((tokens, c.hq, d) if Q.dim() == 3 else Q.shape, dtype=torch.bfloat16, device=device)
+    c.out_stride = _rows_of(out, "out", tokens, c.hq, d, device)
+    if lse is None:
+        lse = torch.empty(tokens * c.hq, dtype=torch.float32, device=device)
+    else:
+        _tensor(lse.view(-1), (tokens * c.hq,), torch.float32, device, "lse")
+    with _at(device):
+        _check(lib.rdkv_prompt_attn_bf16(ctypes.byref(c), Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), lse.data_ptr(), _stream()))
+    return out, lse
+
+
 class Slots:
     """A slot cache (rdkv_slots): its parameters and the device tensors that hold it, made here unless the caller brings them.
 
@@ -532,7 +586,14 @@ def _on(slots):
     """The slots' device as the current one."""
     if slots.device.type != "cuda":
         raise ValueError(f"the slots lie on {slots.device}: the calls on them run on a GPU")
-    index = slots.device.index
+    return _at(slots.device)
+
+
+def _at(device):
+    """A GPU as the current one."""
+    if device.type != "cuda":
+        raise ValueError(f"the tensors lie on {device}: the call runs on a GPU")
+    index = device.index
     return _SAME if index is None or _current_device is None or _current_device() == index else torch.cuda.device(index)
 
 

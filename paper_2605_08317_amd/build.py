@@ -42,6 +42,8 @@ SOURCES = [
     # (its copies into LDS set m0, a reserved register, and say so)
     ("weights_kernels.hip", "weights_kernels.o", ["-Wno-inline-asm"] + EXACT_PRESSURE),
     ("calib_kernels.hip", "calib_kernels.o", []),
+    ("prompt_attn.hip", "prompt_attn.o", ["-Wno-inline-asm"]),
+    ("prompt_api.hip", "prompt_api.o", []),
     ("slots_decode.hip", "slots_decode.o", []),
     ("slots_rows.hip", "slots_rows.o", []),
     ("slots_api.hip", "slots_api.o", []),

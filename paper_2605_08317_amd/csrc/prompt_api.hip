@@ -1,0 +1,90 @@
+// Host side of the attention of whole prompts (rdkv_prompt_*): argument checks and launches.
+#include <algorithm>
+#include <cmath>
+
+#include "prompt.h"
+
+using namespace rdkv;
+
+namespace {
+
+rdkv_status side_of(const char* name, int64_t stride, int heads, prompt::Side* s) {
+  *s = prompt::Side{kHeadDim, 0};
+  if (stride == 0) return RDKV_OK;
+  if (stride % 8 != 0 || stride < static_cast<int64_t>(heads) * kHeadDim || stride > (1 << 23))
+    return fail(RDKV_ERR_SHAPE, "%s_stride = %lld must be 0, or a multiple of 8 from heads * 128 to 2^23", name, static_cast<long long>(stride));
+  *s = prompt::Side{static_cast<int32_t>(stride), 1};
+  return RDKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+rdkv_status rdkv_prompt_default(rdkv_prompt* p) {
+  if (!p) return fail(RDKV_ERR_INVALID_ARG, "prompt is null");
+  *p = rdkv_prompt{};
+  p->head_dim = kHeadDim;
+  return RDKV_OK;
+}
+
+rdkv_status rdkv_prompt_attn_bf16(const rdkv_prompt* p, const void* Q, const void* K, const void* V, void* out, float* lse, void* stream) {
+  if (!p) return fail(RDKV_ERR_INVALID_ARG, "prompt is null");
+  if (p->batch < 0 || p->hq <= 0 || p->hkv <= 0) return fail(RDKV_ERR_INVALID_ARG, "batch/hq/hkv must be positive");
+  if (p->head_dim != kHeadDim) return fail(RDKV_ERR_SHAPE, "head_dim %d unsupported (must be 128)", p->head_dim);
+  if (p->hq % p->hkv != 0) return fail(RDKV_ERR_SHAPE, "hq %d is not a multiple of hkv %d", p->hq, p->hkv);
+  const int g = p->hq / p->hkv;
+  if (!(g == 1 || g == 2 || g == 4 || g == 8)) return fail(RDKV_ERR_SHAPE, "hq/hkv = %d unsupported (1,2,4,8)", g);
+  if (p->hq > 65535) return fail(RDKV_ERR_SHAPE, "hq %d unsupported (at most 65535)", p->hq);
+  if (p->window < 0 || p->sinks < 0) return fail(RDKV_ERR_INVALID_ARG, "window and sinks must not be negative");
+  if (p->score_cap != 0.f && !(p->score_cap > 0.f && std::isnormal(p->score_cap)))        // (its inverse is finite)
+    return fail(RDKV_ERR_INVALID_ARG, "score_cap must be 0 or a normal number > 0");
+  if (p->batch > 0 && !p->seq_lens) return fail(RDKV_ERR_INVALID_ARG, "seq_lens is null");
+  prompt::Args a{};
+  rdkv_status e;
+  if ((e = side_of("q", p->q_stride, p->hq, &a.q)) != RDKV_OK || (e = side_of("k", p->k_stride, p->hkv, &a.k)) != RDKV_OK ||
+      (e = side_of("v", p->v_stride, p->hkv, &a.v)) != RDKV_OK || (e = side_of("out", p->out_stride, p->hq, &a.o)) != RDKV_OK)
+    return e;
+  int64_t rows = 0;
+  for (int i = 0; i < p->batch; ++i) {
+    if (p->seq_lens[i] < 0) return fail(RDKV_ERR_SHAPE, "seq_lens[%d] = %d is negative", i, p->seq_lens[i]);
+    rows += static_cast<int64_t>(p->seq_lens[i]) * p->hq;
+  }
+  if (rows >= (1ll << 31)) return fail(RDKV_ERR_SHAPE, "sum of hq*T_s exceeds 2^31 rows");
+  for (int s0 = 0; s0 < p->batch; s0 += prompt::kSeqs) {
+    const int n = std::min(prompt::kSeqs, p->batch - s0);
+    if (prompt::workgroups(*std::max_element(p->seq_lens + s0, p->seq_lens + s0 + n), n, p->hq) >= (1ll << 24))
+      return fail(RDKV_ERR_SHAPE, "%d sequences of up to %d tokens, %d heads: a launch has at most 2^24 workgroups", n,
+                  *std::max_element(p->seq_lens + s0, p->seq_lens + s0 + n), p->hq);
+  }
+  if (rows == 0) return RDKV_OK;
+  if (!Q || !K || !V || !out) return fail(RDKV_ERR_INVALID_ARG, "Q, K, V and out must not be null");
+  if (((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V) | reinterpret_cast<uintptr_t>(out)) & 15) != 0)
+    return fail(RDKV_ERR_INVALID_ARG, "Q, K, V and out must be aligned to 16 bytes");
+  a.Q = static_cast<const uint16_t*>(Q);
+  a.K = static_cast<const uint16_t*>(K);
+  a.V = static_cast<const uint16_t*>(V);
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.slopes = p->slopes;
+  a.hq = p->hq;
+  a.hkv = p->hkv;
+  a.window = p->window;
+  a.sinks = p->sinks;
+  a.cap = p->score_cap;
+  int64_t token = 0;
+  for (int s0 = 0; s0 < p->batch; s0 += prompt::kSeqs) {
+    a.n_seqs = std::min(prompt::kSeqs, p->batch - s0);
+    int longest = 0;
+    for (int i = 0; i < a.n_seqs; ++i) {
+      a.T[i] = p->seq_lens[s0 + i];
+      a.token0[i] = token;
+      token += a.T[i];
+      longest = std::max(longest, a.T[i]);
+    }
+    if (longest > 0) RDKV_HIP(prompt::launch(a, longest, static_cast<hipStream_t>(stream)));
+  }
+  return RDKV_OK;
+}
+
+}  // extern "C"
