@@ -503,6 +503,43 @@ rdkv_status rdkv_slots_decode_attn(const rdkv_slots* slots, const void* q, float
                                    size_t workspace_bytes, void* stream);
 
 /*
+ * Drafted tokens: n of them per sequence (1 to 64), each the child of an earlier one or of the last cached token, are attended to the
+ * cache at once; the cache stays as it is.  Token i attends to the slots, to the drafted tokens that it descends from, and to itself; it sits at
+ * position next + depth, depth the number of drafted tokens that it descends from.  Scores, window and bias as of a decode step, with the
+ * position of a drafted token next + its depth; drafted K and V are bf16 whatever the slots hold.
+ *   q, out          DEVICE bf16 [batch][n][hq][d]
+ *   k_draft, v_draft  DEVICE bf16 [batch][n][hkv][d]
+ *   parent          DEVICE int32 [batch][n]: index of the token that token i follows, below i; any other number: the last cached token
+ *   counts          DEVICE int32 [batch] or NULL (n): drafted tokens of each sequence, the first ones; out and stats of the others
+ *                   stay as they are, their rows of the inputs may hold anything
+ *   out             softmax(scores) V; 0 where no token takes part
+ *   stats           DEVICE fp32 [batch][n][hq][2] or NULL: the largest score M and the sum of exp(score - M); -inf and 0 where no token
+ *                   takes part, NaN both where a score is NaN or +inf
+ *   workspace       DEVICE scratch of at least rdkv_slots_tree_workspace_bytes(), 16-byte aligned (NULL where that is 0)
+ * Scores, maxima and sums are fp32, up to 2^29 in size; probabilities meet values rounded once, to bf16 (bf16 rows), or both in fp16 (4-bit rows).  A
+ * score below -2e38 takes no part.  Every pointer is aligned to its elements, q, k_draft, v_draft, out and workspace to 16 bytes, stats to 8.
+ */
+size_t rdkv_slots_tree_workspace_bytes(const rdkv_slots* slots, int32_t n);
+rdkv_status rdkv_slots_tree_attn(const rdkv_slots* slots, int32_t n, const void* q, const void* k_draft, const void* v_draft,
+                                 const int32_t* parent, const int32_t* counts, void* out, float* stats, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * Accepted tokens: the first ones of a path through a drafted tree become part of the cache, with what they have attended to.
+ *   path      DEVICE int32 [batch][m] (1 to 64): drafted tokens in order, each the parent of the next; a sequence's path ends before the
+ *             first index that is negative or not below n
+ *   n, q, k_draft, v_draft, stats  as of rdkv_slots_tree_attn; q and stats are needed, and read, where weights are kept
+ *   slot      DEVICE int32 [batch][hkv][m] out, or NULL: the slots they took, -1 behind a path's end
+ * With c accepted tokens, the j-th at position next + j: weight becomes decay^c x weight + the sum over j of decay^(c-1-j) x the softmax's
+ * value of token j, summed over the heads of the group, in slots below len.  Then the tokens come in one after the other as by rdkv_slots_append,
+ * but that token i starts with the sum over j >= i of decay^(c-1-j) x what token j gives it.  While slots are free this is what c appends, each
+ * followed by its decode step, leave.  Where the path is as long as a token of a full cache is `recent`, an accepted token may be
+ * given up for a later one.  Rows of 4-bit caches are quantized as they come in.
+ */
+rdkv_status rdkv_slots_accept(const rdkv_slots* slots, int32_t n, int32_t m, const void* q, const void* k_draft, const void* v_draft,
+                              const int32_t* path, const float* stats, int32_t* slot, void* stream);
+
+/*
  * Rows of the slots as bf16 (4-bit rows: scale x code + offset in fp32, rounded once).
  *   index  DEVICE int32 [batch][hkv][n] or NULL (slots 0 .. n - 1): which slots; a row of zeros where an index is negative or not
  *          below len

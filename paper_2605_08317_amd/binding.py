@@ -33,6 +33,7 @@ EXPORTED_SYMBOLS = [
     "rdkv_cache_stats", "rdkv_cache_export_bytes", "rdkv_cache_export", "rdkv_cache_free",
     "rdkv_kernel_timing_enable", "rdkv_kernel_timing_read", "rdkv_k_row_words", "rdkv_k_row_words_max",
     "rdkv_prompt_default", "rdkv_prompt_attn_bf16",
+    "rdkv_slots_tree_workspace_bytes", "rdkv_slots_tree_attn", "rdkv_slots_accept",
     "rdkv_slots_default", "rdkv_slots_side_bytes", "rdkv_slots_fill_workspace_bytes", "rdkv_slots_fill", "rdkv_slots_append",
     "rdkv_slots_decode_workspace_bytes", "rdkv_slots_decode_attn", "rdkv_slots_read",
 ]
@@ -152,6 +153,10 @@ def _load():
     lib.rdkv_slots_decode_workspace_bytes.argtypes = [slp]
     lib.rdkv_slots_decode_workspace_bytes.restype = sz
     lib.rdkv_slots_decode_attn.argtypes = [slp, vp, vp, vp, vp, sz, vp]
+    lib.rdkv_slots_tree_workspace_bytes.argtypes = [slp, i32]
+    lib.rdkv_slots_tree_workspace_bytes.restype = sz
+    lib.rdkv_slots_tree_attn.argtypes = [slp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.rdkv_slots_accept.argtypes = [slp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
     lib.rdkv_slots_read.argtypes = [slp, vp, i32, vp, vp, vp]
     lib.rdkv_kernel_timing_enable.argtypes = [i32]
     lib.rdkv_kernel_timing_read.argtypes = [i32, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double)]
@@ -573,6 +578,11 @@ class Slots:
         """Scratch of a decode step, for callers that keep it."""
         return torch.empty(max(self.workspace_bytes, 16), dtype=torch.uint8, device=self.device)
 
+    def tree_workspace(self, n):
+        """Scratch of rdkv_slots_tree_attn with n drafted tokens, for callers that keep it."""
+        need = lib.rdkv_slots_tree_workspace_bytes(self.ref(), _int32("n", n))
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
+
 
 def _tensor(t, shape, dtype, device, name):
     """`t`, if it is what the library takes for `name`: it reads and writes plain memory."""
@@ -676,6 +686,55 @@ def rdkv_slots_decode_attn(slots, q, out=None, lse=None, workspace=None):
         _check(lib.rdkv_slots_decode_attn(slots.ref(), q.data_ptr(), out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
                                           workspace.numel(), _stream()))
     return out, lse
+
+
+def _drafted(slots, q, k_draft, v_draft):
+    """The number of drafted tokens per sequence."""
+    if k_draft.dim() != 4:
+        raise ValueError(f"k_draft must be [batch, n, hkv, {slots.d}]: got {tuple(k_draft.shape)}")
+    n = k_draft.shape[1]
+    for t, name, heads in ((q, "q", slots.hq), (k_draft, "k_draft", slots.hkv), (v_draft, "v_draft", slots.hkv)):
+        if t is not None:
+            _tensor(t, (slots.batch, n, heads, slots.d), torch.bfloat16, slots.device, name)
+    return n
+
+
+def rdkv_slots_tree_attn(slots, q, k_draft, v_draft, parent, counts=None, out=None, stats=None, workspace=None):
+    """(out, stats): bfloat16 [batch, n, hq, 128], float32 [batch, n, hq, 2]; what belongs to drafted tokens from counts on stays as it was."""
+    n = _drafted(slots, q, k_draft, v_draft)
+    _tensor(parent, (slots.batch, n), torch.int32, slots.device, "parent")
+    if counts is not None:
+        _tensor(counts, (slots.batch,), torch.int32, slots.device, "counts")
+    rows = (slots.batch, n, slots.hq)
+    out = torch.empty_like(q) if out is None else _tensor(out, rows + (slots.d,), torch.bfloat16, slots.device, "out")
+    if stats is None:
+        stats = torch.empty(rows + (2,), dtype=torch.float32, device=slots.device)
+    else:
+        _tensor(stats, rows + (2,), torch.float32, slots.device, "stats")
+    if workspace is None:
+        workspace = slots.tree_workspace(n)
+    elif workspace.dtype != torch.uint8 or workspace.device != slots.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {slots.device}")
+    with _on(slots):
+        _check(lib.rdkv_slots_tree_attn(slots.ref(), n, q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(), parent.data_ptr(), _ptr(counts),
+                                        out.data_ptr(), stats.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()))
+    return out, stats
+
+
+def rdkv_slots_accept(slots, q, k_draft, v_draft, path, stats, slot=None):
+    """The slots that the accepted tokens took: int32 [batch, hkv, m], -1 behind a path's end.  A cache without weights needs neither q nor stats (None)."""
+    n = _drafted(slots, q, k_draft, v_draft)
+    if path.dim() != 2:
+        raise ValueError(f"path must be [batch, m]: got {tuple(path.shape)}")
+    m = path.shape[1]
+    _tensor(path, (slots.batch, m), torch.int32, slots.device, "path")
+    if stats is not None:
+        _tensor(stats, (slots.batch, n, slots.hq, 2), torch.float32, slots.device, "stats")
+    shape = (slots.batch, slots.hkv, m)
+    slot = torch.empty(shape, dtype=torch.int32, device=slots.device) if slot is None else _tensor(slot, shape, torch.int32, slots.device, "slot")
+    with _on(slots):
+        _check(lib.rdkv_slots_accept(slots.ref(), n, m, _ptr(q), k_draft.data_ptr(), v_draft.data_ptr(), path.data_ptr(), _ptr(stats), slot.data_ptr(), _stream()))
+    return slot
 
 
 def rdkv_slots_read(slots, index=None, n=None, K=None, V=None):

@@ -44,6 +44,8 @@ SOURCES = [
     ("calib_kernels.hip", "calib_kernels.o", []),
     ("prompt_attn.hip", "prompt_attn.o", ["-Wno-inline-asm"]),
     ("prompt_api.hip", "prompt_api.o", []),
+    ("slots_tree.hip", "slots_tree.o", ["-Wno-inline-asm"]),
+    ("slots_accept.hip", "slots_accept.o", ["-Wno-inline-asm"]),
     ("slots_decode.hip", "slots_decode.o", []),
     ("slots_rows.hip", "slots_rows.o", []),
     ("slots_api.hip", "slots_api.o", []),

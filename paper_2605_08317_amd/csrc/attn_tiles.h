@@ -36,6 +36,13 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) { return static_c
 __device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds_base) : "memory", "m0");
 }
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void copy_word_to_lds(const void* base, uint32_t offset, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(base), "s"(lds_base) : "memory", "m0");
+}
+// What this wavefront has written to LDS is there for its other lanes, and stays until they have read it: the hardware keeps a wavefront's
+// order, this the compiler's.
+__device__ __forceinline__ void wave_lds_order() { asm volatile("" ::: "memory"); }
 // Barrier of the workgroup after this wavefront's vector memory operations but the last PENDING have completed.
 template <int PENDING>
 __device__ __forceinline__ void tile_barrier() {

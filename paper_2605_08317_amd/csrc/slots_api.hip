@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "slots.h"
+#include "slots_tree.h"
 
 using namespace rdkv;
 
@@ -42,6 +43,11 @@ bool aligned16(std::initializer_list<const void*> ps) {
   uintptr_t all = 0;
   for (const void* p : ps) all |= reinterpret_cast<uintptr_t>(p);
   return (all & 15) == 0;
+}
+
+// (batch hq < 2^22 keeps rows and launches far below 2^31)
+rdkv_status check_drafted(int32_t n) {
+  return n >= 1 && n <= slots::kMostDrafted ? RDKV_OK : fail(RDKV_ERR_SHAPE, "%d drafted tokens (1 to %d)", n, slots::kMostDrafted);
 }
 
 slots::Args args_of(const rdkv_slots* s) {
@@ -205,6 +211,69 @@ rdkv_status rdkv_slots_decode_attn(const rdkv_slots* s, const void* q, float* ou
     return fail(RDKV_ERR_INVALID_ARG, "workspace of %zu bytes is smaller than the %zu required", workspace_bytes, need);
   RDKV_HIP(slots::launch_decode(args_of(s), s->bits, s->batch * s->hkv, static_cast<const uint16_t*>(q), out, lse,
                                 static_cast<float*>(workspace), static_cast<hipStream_t>(stream)));
+  return RDKV_OK;
+}
+
+size_t rdkv_slots_tree_workspace_bytes(const rdkv_slots* s, int32_t n) {
+  if (check_slots(s, false) != RDKV_OK || check_drafted(n) != RDKV_OK || s->batch == 0) return 0;
+  const int64_t items = static_cast<int64_t>(s->batch) * s->hkv;
+  return slots::plan_tree(items, n * (s->hq / s->hkv), s->capacity, s->bits).floats(items) * sizeof(float);
+}
+
+rdkv_status rdkv_slots_tree_attn(const rdkv_slots* s, int32_t n, const void* q, const void* k_draft, const void* v_draft,
+                                 const int32_t* parent, const int32_t* counts, void* out, float* stats, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  rdkv_status e = check_slots(s, true);
+  if (e != RDKV_OK || (e = check_drafted(n)) != RDKV_OK) return e;
+  if (s->batch == 0) return RDKV_OK;
+  if (!q || !k_draft || !v_draft || !parent || !out) return fail(RDKV_ERR_INVALID_ARG, "q, k_draft, v_draft, parent and out must not be null");
+  const size_t need = rdkv_slots_tree_workspace_bytes(s, n);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(RDKV_ERR_INVALID_ARG, "workspace of %zu bytes is smaller than the %zu required", workspace ? workspace_bytes : 0, need);
+  if (!aligned16({q, k_draft, v_draft, out, workspace}) || (reinterpret_cast<uintptr_t>(stats) & 7) != 0)
+    return fail(RDKV_ERR_INVALID_ARG, "q, k_draft, v_draft, out and workspace must be aligned to 16 bytes, stats to 8");
+  slots::TreeArgs a{};
+  a.s = args_of(s);
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_draft = static_cast<const uint16_t*>(k_draft);
+  a.v_draft = static_cast<const uint16_t*>(v_draft);
+  a.parent = parent;
+  a.counts = counts;
+  a.out = static_cast<uint16_t*>(out);
+  a.stats = stats;
+  a.items = s->batch * s->hkv;
+  a.n = n;
+  const slots::TreePlan plan = slots::plan_tree(a.items, n * a.s.g, s->capacity, s->bits);
+  a.row_groups = plan.row_groups;
+  a.pieces = plan.pieces;
+  a.part_acc = static_cast<float*>(workspace);
+  a.part_ml = a.part_acc + plan.part_rows(a.items) * kHeadDim;
+  RDKV_HIP(slots::launch_tree(a, s->bits, static_cast<hipStream_t>(stream)));
+  return RDKV_OK;
+}
+
+rdkv_status rdkv_slots_accept(const rdkv_slots* s, int32_t n, int32_t m, const void* q, const void* k_draft, const void* v_draft,
+                              const int32_t* path, const float* stats, int32_t* slot, void* stream) {
+  rdkv_status e = check_slots(s, true);
+  if (e != RDKV_OK || (e = check_drafted(n)) != RDKV_OK) return e;
+  if (m < 1 || m > slots::kMostDrafted) return fail(RDKV_ERR_SHAPE, "paths of %d tokens (1 to %d)", m, slots::kMostDrafted);
+  if (s->batch == 0) return RDKV_OK;
+  if (!k_draft || !v_draft || !path) return fail(RDKV_ERR_INVALID_ARG, "k_draft, v_draft and path must not be null");
+  if (s->weight && (!q || !stats)) return fail(RDKV_ERR_INVALID_ARG, "a cache that keeps weights needs q and stats");
+  if (!aligned16({q, k_draft, v_draft}) || (reinterpret_cast<uintptr_t>(stats) & 7) != 0)
+    return fail(RDKV_ERR_INVALID_ARG, "q, k_draft and v_draft must be aligned to 16 bytes, stats to 8");
+  slots::AcceptArgs a{};
+  a.s = args_of(s);
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_draft = static_cast<const uint16_t*>(k_draft);
+  a.v_draft = static_cast<const uint16_t*>(v_draft);
+  a.path = path;
+  a.stats = stats;
+  a.slot = slot;
+  a.items = s->batch * s->hkv;
+  a.n = n;
+  a.m = m;
+  RDKV_HIP(slots::launch_accept(a, s->bits, static_cast<hipStream_t>(stream)));
   return RDKV_OK;
 }
 

@@ -1,0 +1,250 @@
+// Slot caches, many query rows at once: what the attention of drafted trees and the taking of accepted tokens share.  Scores of 64 slots (a
+// tile) and 32 query rows on the matrix cores, in the transposed form of attn_tiles.h.
+//
+// 4-bit rows need no LDS image: a tile's layout is an operand's already.  K codes: a product takes 16 channels of 32 slots, a lane 8
+// of one slot, which are 2 fields of 2 words; the words of a slot's other 16 channels go to the other half of the wavefront (permlane32).  The
+// slots of a product are chosen so that a lane's scores are of 16 slots in a row: result register i of lane (half, .) of product x is slot
+// 32 half + 16 x + i.  V codes: a lane's word quadruple is one channel's 32 slots of its half, so step f of P V (fields f of the four words)
+// takes slots 4 f + 0..3 and 16 + 4 f + 0..3 of the half, which are registers 4 f .. 4 f + 3 of the lane's two products.
+//   scores  K codes are bf16 numbers 1 + code / 16 and meet the query's bf16 values, exactly; a group's sums of products are added with the
+//           slots' scales in fp32.  What the 1 adds, and the offsets, are a product of their own: a slot's metadata row, four scales and four
+//           offsets in fp16, against sums of the query's values over a group, each in two fp16 terms (22 bits).  Queries are
+//           taken over a power of two, so that these terms have their bits whatever the queries' size
+//   P V     V codes less 8 are scaled to fp16 values by one fused multiply-add (rounded once, 2^-12 of the value; a group's offset plus 8
+//           scales, which it starts from, too), probabilities are fp16
+#pragma once
+#include "attn_tiles.h"
+#include "slots.h"
+
+namespace rdkv {
+namespace slots {
+
+using namespace attn;
+
+typedef __attribute__((ext_vector_type(8))) _Float16 halfx8;
+typedef __attribute__((ext_vector_type(4))) _Float16 halfx4;
+typedef __attribute__((ext_vector_type(2))) _Float16 halfx2;
+
+constexpr float kNoScore = -2e38f;       // a finite maximum of nothing, also times log2(e): no score is below it
+
+__device__ __forceinline__ floatx16 product(halfx8 a, halfx8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+using attn::product;
+
+// Sums over the wavefront's lanes whose query rows are 32 different ones: register i of v becomes, in lane (half, i % 32 of them), the sum of
+// v[i] over the half's lanes.  32 numbers a lane: each step adds what half of the lanes hand over.
+__device__ __forceinline__ float rows_sum(float (&v)[32]) {
+  const int l = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    const bool up = (l & d) != 0;
+#pragma unroll
+    for (int i = 0; i < d; ++i) {
+      const float keep = up ? v[i + d] : v[i], give = up ? v[i] : v[i + d];
+      v[i] = keep + __shfl_xor(give, d);
+    }
+  }
+  return v[0];
+}
+
+// Query rows of a wavefront as operands.
+struct Query16 {
+  bf16x8 op[8];
+  static constexpr float kUnits = 1.f;
+  float unit;                            // scores come over it
+  // q: the lane's row
+  __device__ __forceinline__ void load(const uint16_t* q) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int kb = 0; kb < 8; ++kb) op[kb] = *reinterpret_cast<const bf16x8*>(q + 16 * kb + 8 * half);
+    unit = 1.f;
+  }
+};
+struct Query4 {
+  bf16x8 op[8];                          // product 2 group + s: channels 32 group + 16 half + 8 s ..
+  halfx8 sums;                           // for a metadata row: minus a group's sum, and a sixteenth of it; high terms in the lower half's lanes, low in the upper's
+  float unit;
+  __device__ __forceinline__ void load(const uint16_t* q) {
+    const int half = (threadIdx.x & 63) >> 5;
+    float most = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 8; ++kb) {
+      op[kb] = *reinterpret_cast<const bf16x8*>(q + 32 * (kb >> 1) + 16 * half + 8 * (kb & 1));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(static_cast<float>(op[kb][i])));
+    }
+    most = halves_max(most);
+    // the largest value over the power of two is in [1, 2); of zeros, infinities and the like: as they are
+    const int e = static_cast<int>(__float_as_uint(most) >> 23);
+    const bool plain = e >= 1 && e <= 253;
+    const float inv = plain ? __uint_as_float(static_cast<uint32_t>(254 - e) << 23) : 1.f;
+    unit = 16.f * (plain ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 1.f);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float sum = 0.f;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = static_cast<float>(op[2 * g + s][i]) * inv;
+          op[2 * g + s][i] = static_cast<__bf16>(x);
+          sum += x;
+        }
+      sum = halves_add(sum);
+      const _Float16 a = static_cast<_Float16>(-sum), b = static_cast<_Float16>(sum * 0.0625f);
+      sums[g] = half == 0 ? a : static_cast<_Float16>(-sum - static_cast<float>(a));
+      sums[4 + g] = half == 0 ? b : static_cast<_Float16>(sum * 0.0625f - static_cast<float>(b));
+    }
+  }
+};
+
+// bf16 rows in LDS: products of 32 slots, register i of lane (half, .): slot 8 (i / 4) + 4 half + i % 4 of the step.
+__device__ __forceinline__ floatx16 scores16(const uint8_t* step, const Query16& q) {
+  floatx16 s = {};
+#pragma unroll
+  for (int kb = 0; kb < 8; ++kb) s = product(read_k(step, kb), q.op[kb], s);
+  return s;
+}
+
+// slot of a 4-bit tile that row r of product x is
+__device__ __forceinline__ int slot_of_row(int x, int r) { return 32 * ((r >> 2) & 1) + 16 * x + 4 * (r >> 3) + (r & 3); }
+
+// A 4-bit tile's codes and metadata of one side on their way to a wavefront.  K: the lane's 16 codes of each group are of slot slot_of_row(half, l32);
+// metadata of slot `lane`.  V: the codes of channel 32 group + l32 of the half's slots; metadata of slots 4 (lane / 4) .. + 3, group lane % 4.
+struct Side4 {
+  uint4 codes[4];
+  uint4 meta;
+  __device__ __forceinline__ void load(const uint8_t* tile, bool is_k) {
+    const int lane = threadIdx.x & 63;
+    const int at = is_k ? slot_of_row(lane >> 5, lane & 31) : lane;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) codes[g] = *reinterpret_cast<const uint4*>(tile + 1024 * g + 16 * at);
+    meta = *reinterpret_cast<const uint4*>(tile + kTileCodes + 16 * lane);
+  }
+};
+
+// K metadata into LDS (kKMeta bytes of the wavefront's), of slots from `rows` on zeros: the rows, then the scales again, [group][slot].
+constexpr int kKMeta = 1024 + 512;
+__device__ __forceinline__ void put_k_meta(uint8_t* lds, const Side4& k, int rows) {
+  const int lane = threadIdx.x & 63;
+  const bool there = lane < rows;
+  const uint4 m = make_uint4(there ? k.meta.x : 0u, there ? k.meta.y : 0u, there ? k.meta.z : 0u, there ? k.meta.w : 0u);
+  *reinterpret_cast<uint4*>(lds + 16 * lane) = m;
+  uint16_t* scales = reinterpret_cast<uint16_t*>(lds + 1024) + lane;
+  scales[0] = static_cast<uint16_t>(m.x);
+  scales[64] = static_cast<uint16_t>(m.x >> 16);
+  scales[128] = static_cast<uint16_t>(m.y);
+  scales[192] = static_cast<uint16_t>(m.y >> 16);
+}
+// V metadata: scales, and offsets plus 8 scales; of slots from `rows` on zeros.
+__device__ __forceinline__ void put_v_meta(uint8_t* lds, const Side4& v, int rows) {
+  const int lane = threadIdx.x & 63, first = 4 * (lane >> 2);
+  union { uint4 u; _Float16 h[8]; } m;
+  m.u = v.meta;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool there = first + i < rows;
+    const float s = there ? static_cast<float>(m.h[i]) : 0.f, o = there ? static_cast<float>(m.h[4 + i]) : 0.f;
+    m.h[i] = static_cast<_Float16>(s);
+    m.h[4 + i] = static_cast<_Float16>(__builtin_fmaf(8.f, s, o));
+  }
+  *reinterpret_cast<uint4*>(lds + 16 * lane) = m.u;
+}
+
+// the four words' fields at bits `at` of both halves as numbers: mask and what stands above them
+template <int SHIFT>
+__device__ __forceinline__ uint32_t shifted(uint32_t w) {
+  if constexpr (SHIFT > 0) return w >> SHIFT;
+  else return w << -SHIFT;
+}
+
+// Products of the 64 slots, register i of s[x] of lane (half, .): slot 32 half + 16 x + i; over the query's unit.
+__device__ __forceinline__ void scores4(const Side4& k, const uint8_t* k_meta, const Query4& q, floatx16 (&s)[2]) {
+  const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+  // word pair (2 half, 2 half + 1) of the slots of product 0, and of product 1
+  uint32_t w[2][4][2];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    uint32_t a = k.codes[g].x, b = k.codes[g].y, c = k.codes[g].z, d = k.codes[g].w;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(c));
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(b), "+v"(d));
+    w[0][g][0] = a;
+    w[0][g][1] = b;
+    w[1][g][0] = c;
+    w[1][g][1] = d;
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    s[x] = product(*reinterpret_cast<const halfx8*>(k_meta + 16 * slot_of_row(x, l32)), q.sums, floatx16{});
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      union { uint32_t u[4]; bf16x8 b; } op[2];
+      constexpr uint32_t kMask = 0x00780078u, kOne = 0x3F803F80u;          // bf16 1 + code / 16
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        op[0].u[j] = (shifted<-3>(w[x][g][j]) & kMask) | kOne;
+        op[0].u[2 + j] = (shifted<1>(w[x][g][j]) & kMask) | kOne;
+        op[1].u[j] = (shifted<5>(w[x][g][j]) & kMask) | kOne;
+        op[1].u[2 + j] = (shifted<9>(w[x][g][j]) & kMask) | kOne;
+      }
+      floatx16 sums = product(op[0].b, q.op[2 * g], floatx16{});
+      sums = product(op[1].b, q.op[2 * g + 1], sums);
+      const halfx8* sc = reinterpret_cast<const halfx8*>(k_meta + 1024 + 128 * g + 2 * (32 * half + 16 * x));
+      const halfx8 sc0 = sc[0], sc1 = sc[1];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[x][i] = __builtin_fmaf(static_cast<float>(i < 8 ? sc0[i & 7] : sc1[i & 7]), sums[i], s[x][i]);
+    }
+  }
+}
+
+// fp16 values of channel 32 group + l32 of slots 32 half + 4 f + 0..3 and + 16..19
+template <int F>
+__device__ __forceinline__ halfx8 values4(const uint4& codes, const uint8_t* v_meta, int group) {
+  const int half = (threadIdx.x & 63) >> 5;
+  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+  union { uint32_t u[4]; halfx2 h[4]; halfx8 v; } x;
+  constexpr uint32_t kMask = 0x03C003C0u, kSixteen = 0x4C004C00u;          // fp16 16 + code
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x.u[j] = (shifted<4 * F - 6>(w[j]) & kMask) | kSixteen;
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    union { uint4 u; halfx2 h[4]; } m;
+    m.u = *reinterpret_cast<const uint4*>(v_meta + 64 * (8 * half + 4 * p + F) + 16 * group);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) x.h[2 * p + j] = __builtin_elementwise_fma(x.h[2 * p + j] - halfx2{24, 24}, m.h[j], m.h[2 + j]);
+  }
+  return x.v;
+}
+
+// `part` of attn_tiles.h for fp16
+struct Parted4 {
+  halfx8 finite, up, down;
+  bool any;
+};
+__device__ __forceinline__ Parted4 part(halfx8 x) {
+  union { halfx8 b; uint32_t u[4]; } v, f, up, down;
+  v.b = x;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t t = ((v.u[i] & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+    const uint32_t odd = (t >> 15) * 0xFFFFu;
+    const uint32_t nan = ((((v.u[i] & 0x03FF03FFu) + 0x03FF03FFu) & 0x04000400u) >> 10) * 0xFFFFu;
+    const uint32_t neg = ((v.u[i] >> 15) & 0x00010001u) * 0xFFFFu;
+    f.u[i] = v.u[i] & ~odd;
+    up.u[i] = odd & (nan | ~neg) & 0x3C003C00u;
+    down.u[i] = odd & (nan | neg) & 0x3C003C00u;
+    any |= odd;
+  }
+  return {f.b, up.b, down.b, any != 0};
+}
+using attn::part;
+
+__device__ __forceinline__ halfx8 to_half(const float* p) {
+  halfx8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = static_cast<_Float16>(p[i]);
+  return v;
+}
+
+}  // namespace slots
+}  // namespace rdkv

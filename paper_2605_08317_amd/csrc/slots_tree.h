@@ -1,0 +1,68 @@
+// Trees of drafted tokens over slot caches (rdkv_slots_tree_attn, rdkv_slots_accept): what the host side and the kernels share.
+#pragma once
+#include <algorithm>
+
+#include "slots.h"
+
+namespace rdkv {
+namespace slots {
+
+constexpr int kMostDrafted = 64;        // tokens of a tree: a bit each
+
+struct TreeArgs {
+  Args s;
+  const uint16_t* q;                    // [batch][n][hq][128]
+  const uint16_t* k_draft;              // [batch][n][hkv][128]
+  const uint16_t* v_draft;
+  const int32_t* parent;                // [batch][n]
+  const int32_t* counts;                // [batch], or null
+  uint16_t* out;                        // [batch][n][hq][128]
+  float* stats;                         // [batch][n][hq][2], or null
+  float* part_acc;                      // [item][row group][piece][rows of a group][128]
+  float* part_ml;                       // the same rows: [4]
+  int32_t items, n, row_groups, pieces;
+};
+
+// wide: wavefronts of a workgroup that share out rows, 32 each; the others share out slots.  Pieces of an item's slots.
+struct TreePlan {
+  int32_t wide, row_groups, pieces;
+  size_t part_rows(int64_t items) const { return pieces == 1 ? 0 : static_cast<size_t>(items) * row_groups * pieces * 32 * wide; }
+  size_t floats(int64_t items) const { return part_rows(items) * (kHeadDim + 4); }
+};
+inline TreePlan plan_tree(int64_t items, int rows, int capacity, int bits) {
+  TreePlan p;
+  p.wide = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  p.row_groups = (rows + 32 * p.wide - 1) / (32 * p.wide);
+  const int64_t groups = items * p.row_groups, card = bits == 16 ? 256 : 512;
+  const int64_t least = 2 * (4 / p.wide);                     // tiles of a piece
+  const int64_t most = (static_cast<int64_t>(capacity) + kTileRows - 1) / kTileRows / least;
+  p.pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min(most, card / std::max<int64_t>(groups, 1))));
+  return p;
+}
+
+// (largest score, sum of exponentials of what is left) of a row: m, l its reference and sum over it times 2^shift, top the largest product; factor
+// makes products exponents of 2, natural scores.  The sum is over the score as it is rounded.
+__device__ __forceinline__ void store_stats(float* to, float m, float l, float top, float factor, float natural, float shift) {
+  constexpr float kLog2e_ = 1.4426950408889634f;
+  const float score = top * natural;
+  const float sum = l * __builtin_amdgcn_exp2f(__builtin_fmaf(m - top, factor, __builtin_fmaf(top, natural, -score) * kLog2e_) - shift);
+  const bool none = l == 0.f;
+  *reinterpret_cast<float2*>(to) = make_float2(none ? -INFINITY : l != l ? l : score, none ? 0.f : sum);
+}
+
+struct AcceptArgs {
+  Args s;
+  const uint16_t* q;                    // as of the tree: [batch][n]..
+  const uint16_t* k_draft;
+  const uint16_t* v_draft;
+  const int32_t* path;                  // [batch][m]
+  const float* stats;                   // [batch][n][hq][2]
+  int32_t* slot;                        // [batch][hkv][m], or null
+  int32_t items, n, m, pieces;
+};
+
+hipError_t launch_accept(const AcceptArgs& a, int bits, hipStream_t st);
+hipError_t launch_tree(const TreeArgs& a, int bits, hipStream_t st);
+
+}  // namespace slots
+}  // namespace rdkv

@@ -1,0 +1,523 @@
+// Slot caches: attention of a tree of drafted tokens.
+//
+// A workgroup of four wavefronts has up to 128 query rows (token, head) of an item and a piece of its slots.  With 32 rows or fewer the wavefronts
+// share out the slots, with 64 they are two by two, with more they share out the rows; results of slots are joined in LDS.  The last piece of an item
+// has the drafted tokens' own keys and values, bf16 rows whatever the cache holds, behind its slots.
+#include <algorithm>
+
+#include "slots_tiles.h"
+#include "slots_tree.h"
+
+namespace rdkv {
+namespace slots {
+
+namespace {
+
+constexpr float kSlack = 4.f;             // what exponents may exceed a row's reference by before it moves
+constexpr float kTopHalf = 11.f;          // fp16 probabilities are over 2^-11: with the slack below fp16's largest, and bits down to 2^-35
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kTokens = 64;
+
+// What a lane knows of its query row.
+struct Row {
+  int index;                              // of the item's n g rows; past them: of none, as the last
+  bool there;
+  int token, at;                          // its position
+  uint64_t sees;                          // drafted tokens
+  float slope;
+};
+
+struct Out {                              // of a lane's row, over 32 or 64 lanes' channels
+  floatx16 o[4];
+  float m, l, top;                        // reference, sum of exponentials (of the lane's slots) over it, largest score
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = floatx16{};
+    m = top = kNoScore;
+    l = 0.f;
+  }
+};
+
+// Scores of n products to probabilities; factor makes scores exponents of 2.  Of differences from the reference: a large number that scores have
+// in common costs nothing.
+template <int N>
+__device__ __forceinline__ void softmax(const float (&x)[N], float factor, float shift, Out& r, float (&p)[N]) {
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+  top = halves_max(top);
+  r.top = fmaxf(r.top, top);
+  if (__any((top - r.m) * factor > kSlack)) {
+    const float now = fmaxf(r.m, top), alpha = __builtin_amdgcn_exp2f((r.m - now) * factor);
+    r.m = now;
+    r.l *= alpha;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r.o[t][i] *= alpha;
+  }
+  float sum[4] = {};
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i] - r.m, factor, shift));
+    sum[i & 3] += p[i];
+  }
+  r.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// o += P V for the channels of register group t; V's operands by value(step).  PARTED: some slots are hidden from some rows, and what is not finite
+// in V must not meet their zeros.
+template <bool PARTED, int STEPS, class Op, class Value>
+__device__ __forceinline__ void add_values(const Op (&p)[STEPS], const float* probabilities, Value value, floatx16& o) {
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    const Op v = value(k);
+    if constexpr (!PARTED) {
+      o = product(v, p[k], o);
+    } else {
+      const auto parted = part(v);
+      o = product(parted.finite, p[k], o);
+      if (__any(parted.any)) {
+        Op one;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) one[i] = probabilities[8 * k + i] == 0.f ? 0.f : 1.f;
+        const floatx16 up = product(parted.up, one, floatx16{}), down = product(parted.down, one, floatx16{});
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if (up[i] > 0.f) o[i] += INFINITY;
+          if (down[i] > 0.f) o[i] -= INFINITY;
+        }
+      }
+    }
+  }
+}
+
+// bf16 rows in LDS, STEPS x 32 of them, into a row's result.  x: their scores (registers 16 step + i), -inf where hidden
+template <int STEPS, bool PARTED>
+__device__ __forceinline__ void add_rows16(const float (&x)[16 * STEPS], float factor, const uint8_t* vt, float shift, Out& r) {
+  float p[16 * STEPS];
+  softmax(x, factor, shift, r, p);
+  bf16x8 op[2 * STEPS];
+#pragma unroll
+  for (int k = 0; k < 2 * STEPS; ++k) op[k] = to_bf16(p + 8 * k);
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    add_values<PARTED>(op, p, [&](int k) __attribute__((always_inline)) { return read_v(vt + (k >> 1) * kStepKeys * kRowBytes, t, k & 1); }, r.o[t]);
+}
+
+// What scores are made of products with.
+struct Scoring {
+  float natural;                          // products to scores, with a cap or biases
+  float factor;                           // scores, or products, to exponents of 2
+  float cap, inv_cap;
+  bool scored, biased;                    // scores are made of products at once; of differences later
+  int window, sinks;
+};
+// Products to scores, -inf where hidden, a step at a time over all of them.  four(k, at): positions of products 4 k .. + 3.  hide(i): there is no slot,
+// asked if `some` are none
+template <bool GENERAL, int N, class Four, class Hide>
+__device__ __forceinline__ void to_scores(const Scoring& sc, const Row& row, float (&x)[N], bool some, Four four, Hide hide) {
+  if constexpr (GENERAL) {
+    if (sc.scored) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] *= sc.natural;
+    }
+    if (sc.cap > 0.f) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        x[i] = capped(x[i], sc.cap, sc.inv_cap);
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (all of them side by side do not fit the registers)
+      }
+    }
+    if (sc.biased || sc.window > 0) {
+#pragma unroll
+      for (int k = 0; k < N / 4; ++k) {
+        int at[4];
+        four(k, at);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int away = row.at - at[j];
+          if (sc.biased) x[4 * k + j] = __builtin_fmaf(-row.slope, static_cast<float>(away), x[4 * k + j]);
+          if (sc.window > 0 && away >= sc.window && at[j] >= sc.sinks) x[4 * k + j] = -INFINITY;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  if (some) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = hide(i) ? -INFINITY : x[i];
+  }
+}
+
+template <int WR>
+constexpr int kSteps16 = WR == 1 ? 1 : WR == 2 ? 1 : 2;         // 32-slot steps of a wavefront's tile
+template <int WR>
+constexpr int kStage = 32 * kSteps16<WR> * (kWaves / WR);       // slots of a stage
+template <int WR>
+constexpr int kStages = 256 / kStage<WR>;                       // buffers
+constexpr int kStageLds = 256 * 2 * kRowBytes;                  // of all of them: 128 KiB
+constexpr int kPosLds = kWaves * 4 * 64 * 4;                    // positions of the wavefronts' tiles, up to four buffers
+constexpr int kDraftLds = kTokens * 2 * kRowBytes;
+constexpr int kJoinLds = kWaves * 4 * 16 * 64 * 4;              // the wavefronts' results
+constexpr int kMetaLds = kWaves * (kKMeta + 1024 + 256);
+
+template <int BITS, int WR, bool GENERAL>
+__global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(TreeArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ uint64_t s_sees[kTokens];
+  __shared__ int s_depth[kTokens], s_parent[kTokens];
+  __shared__ float s_ml[kWaves][32][4];
+  constexpr int WS = kWaves / WR;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  const int wr = wave % WR, ws = wave / WR;
+  // row groups of a piece are eight workgroups apart, on one XCD
+  const int in = static_cast<int>(blockIdx.x) % (8 * a.row_groups), unit = static_cast<int>(blockIdx.x) / (8 * a.row_groups) * 8 + in % 8, rg = in / 8;
+  if (unit >= a.items * a.pieces) return;
+  const int item = unit / a.pieces, piece = unit % a.pieces, seq = item / a.s.hkv, kvh = item % a.s.hkv, g = a.s.g, n = a.n, rows = n * g;
+  const int count = a.counts ? min(max(a.counts[seq], 0), n) : n;
+  if (rg * WR * 32 >= count * g) return;
+
+  // ancestors: a bit of each, and the token's own
+  if (tid < n) s_parent[tid] = a.parent[static_cast<int64_t>(seq) * n + tid];
+  __syncthreads();
+  if (tid < n) {
+    uint64_t sees = 1ull << tid;
+    for (int t = tid, p; (p = s_parent[t]) >= 0 && p < t; t = p) sees |= 1ull << p;
+    s_sees[tid] = sees;
+    s_depth[tid] = __popcll(sees) - 1;
+  }
+  __syncthreads();
+
+  const int len = a.s.length(item), next = a.s.next[item];
+  Row row;
+  {
+    const int r = (rg * WR + wr) * 32 + l32;
+    row.there = r < count * g;
+    row.index = min(r, rows - 1);
+    row.token = row.index / g;
+    row.sees = s_sees[row.token];
+    row.at = next + s_depth[row.token];
+    row.slope = GENERAL && a.s.slopes ? a.s.slopes[kvh * g + row.index % g] : 0.f;
+  }
+  const int64_t q_row = (static_cast<int64_t>(seq) * n + row.token) * a.s.hkv * g + kvh * g + row.index % g;
+  using Query = std::conditional_t<BITS == 16, Query16, Query4>;
+  Query query;
+  query.load(a.q + q_row * kHeadDim);
+  Scoring sc;
+  sc.cap = a.s.cap;
+  sc.inv_cap = a.s.cap > 0.f ? 1.f / a.s.cap : 0.f;
+  sc.biased = a.s.slopes != nullptr;
+  sc.window = a.s.window;
+  sc.sinks = a.s.sinks;
+  sc.scored = GENERAL && (sc.cap > 0.f || sc.biased);
+  sc.natural = sc.scored ? query.unit * kRoot : 1.f;
+  sc.factor = sc.scored ? kLog2e : query.unit * kRootLog2e;
+
+  Out r;
+  // this piece's slots: whole tiles of 64
+  const int tiles = (len + kTileRows - 1) / kTileRows;
+  const int begin = static_cast<int>(static_cast<int64_t>(tiles) * piece / a.pieces) * kTileRows;
+  const int end = min(len, static_cast<int>(static_cast<int64_t>(tiles) * (piece + 1) / a.pieces) * kTileRows);
+  const int32_t* pos = a.s.pos + static_cast<int64_t>(item) * a.s.capacity;
+  const uint32_t lds0 = lds_address(smem);
+  const int prow = tid >> 4;
+  const uint32_t k_at = 16 * k_piece(prow, tid & 15), v_at = 16 * v_piece(prow, tid & 15);
+  // rows first .. of bf16 keys and values, `stride` bytes apart, into LDS: K, then V behind `most` rows of them; rows past the last are it again
+  const auto fetch_rows = [&](const uint8_t* k, const uint8_t* v, uint32_t stride, int last, int most, uint32_t to) __attribute__((always_inline)) {
+    for (int i = 0; i < most; i += 16) {
+      const uint32_t at = static_cast<uint32_t>(min(prow + i, last)) * stride;
+      copy_to_lds(k, at + k_at, to + i * kRowBytes + wave * 1024);
+      copy_to_lds(v, at + v_at, to + (most + i) * kRowBytes + wave * 1024);
+    }
+  };
+
+  // Careful: rows of V that a window hides from some query rows are kept from meeting their zeros, which make NaN of what is not finite.  Done
+  // again so where results are not finite.
+  const auto walk = [&](auto careful) __attribute__((always_inline)) {
+  constexpr bool kCareful = decltype(careful)::value;
+  r.init();
+  if constexpr (BITS == 16) {
+    constexpr int kStepsN = kSteps16<WR>, kSlots = kStage<WR>, kBuffers = kStages<WR>, kMine = 32 * kStepsN;
+    constexpr int kCopies = kSlots / 8 + (GENERAL ? 1 : 0);      // of a wavefront and stage
+    const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
+    const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
+    const int n_it = (end - begin + kSlots - 1) / kSlots;
+    uint8_t* s_pos = smem + kStageLds;
+    const auto fetch = [&](int it) __attribute__((always_inline)) {
+      const int first = begin + min(it, n_it - 1) * kSlots, buffer = it % kBuffers;
+      fetch_rows(K + static_cast<int64_t>(first) * kRowBytes, V + static_cast<int64_t>(first) * kRowBytes, kRowBytes, end - 1 - first, kSlots,
+                 lds0 + buffer * (kSlots * 2 * kRowBytes));
+      if constexpr (GENERAL) {
+        const int at = min(first + ws * kMine + lane, end - 1) - first;
+        copy_word_to_lds(pos + first, 4 * at, lds0 + kStageLds + (wave * kBuffers + buffer) * 256);
+      }
+    };
+    if (n_it > 0) {
+#pragma unroll
+      for (int it = 0; it < kBuffers - 1; ++it) fetch(it);
+      for (int it = 0; it < n_it; ++it) {
+        tile_barrier<kCopies * (kBuffers - 2)>();
+        fetch(it + kBuffers - 1);
+        const int buffer = it % kBuffers, mine = ws * kMine, left = end - begin - it * kSlots - mine - 4 * half;
+        if (left + 4 * half <= 0) continue;
+        const uint8_t* kt = smem + buffer * (kSlots * 2 * kRowBytes) + mine * kRowBytes;
+        const uint8_t* vt = kt + kSlots * kRowBytes;
+        const int4* where = reinterpret_cast<const int4*>(s_pos + (wave * kBuffers + buffer) * 256);
+        float x[16 * kStepsN];
+#pragma unroll
+        for (int k = 0; k < kStepsN; ++k) {
+          const floatx16 s = scores16(kt + k * kStepKeys * kRowBytes, query);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
+        }
+        to_scores<GENERAL>(sc, row, x, left < kMine, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[2 * k + half]; },
+                           [&](int i) __attribute__((always_inline)) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) >= left; });
+        add_rows16<kStepsN, kCareful>(x, sc.factor, vt, 0.f, r);
+      }
+      tile_barrier<0>();
+    }
+  } else {
+    uint8_t* meta = smem + kDraftLds + wave * (kMetaLds / kWaves);
+    const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
+    const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
+    const int t1 = (end + kTileRows - 1) / kTileRows;
+    Side4 k, v;
+    int at = 0;
+    int t = begin / kTileRows + ws;
+    const auto load = [&](int tile) __attribute__((always_inline)) {
+      k.load(K + static_cast<int64_t>(tile) * kTileBytes, true);
+      v.load(V + static_cast<int64_t>(tile) * kTileBytes, false);
+      if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
+    };
+    if (t < t1) load(t);
+    for (; t < t1; t += WS) {
+      const Side4 kc = k, vc = v;
+      const int left = end - t * kTileRows;
+      put_k_meta(meta, kc, left);
+      put_v_meta(meta + kKMeta, vc, left);
+      if constexpr (GENERAL) reinterpret_cast<int*>(meta + kKMeta + 1024)[lane] = at;
+      if (t + WS < t1) load(t + WS);
+      wave_lds_order();
+      floatx16 s[2];
+      scores4(kc, meta, query, s);
+      float x[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = s[i >> 4][i & 15];
+      const int4* where = reinterpret_cast<const int4*>(meta + kKMeta + 1024) + 8 * half;
+      to_scores<GENERAL>(sc, row, x, left < kTileRows, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[k]; },
+                         [&](int i) __attribute__((always_inline)) { return 32 * half + i >= left; });
+      float p[32], pf[32];
+      softmax(x, sc.factor, kTopHalf, r, p);
+      halfx8 op[4];
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          pf[8 * f + j] = p[4 * f + j];
+          pf[8 * f + 4 + j] = p[16 + 4 * f + j];
+        }
+        op[f] = to_half(pf + 8 * f);
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        add_values<kCareful>(op, pf, [&](int f) __attribute__((always_inline)) {
+          return f == 0 ? values4<0>(vc.codes[c], meta + kKMeta, c) : f == 1 ? values4<1>(vc.codes[c], meta + kKMeta, c)
+               : f == 2 ? values4<2>(vc.codes[c], meta + kKMeta, c) : values4<3>(vc.codes[c], meta + kKMeta, c);
+        }, r.o[c]);
+      wave_lds_order();
+    }
+  }
+  };
+  walk(std::false_type{});
+  if (GENERAL && sc.window > 0) {
+    float zero = r.l * 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(r.o[t][i], 0.f, zero);
+    if (__syncthreads_or(zero != 0.f)) walk(std::bool_constant<GENERAL>{});
+  }
+
+  // the drafted tokens themselves
+  if (piece == a.pieces - 1) {
+    const int64_t first = (static_cast<int64_t>(seq) * n * a.s.hkv + kvh) * kRowBytes;
+    fetch_rows(reinterpret_cast<const uint8_t*>(a.k_draft) + first, reinterpret_cast<const uint8_t*>(a.v_draft) + first, a.s.hkv * kRowBytes, n - 1, kTokens, lds0);
+    tile_barrier<0>();
+    if (ws == 0) {
+      Query16 q16;
+      q16.load(a.q + q_row * kHeadDim);
+      Scoring own = sc;
+      own.natural = sc.scored ? kRoot : 1.f / query.unit;        // as of the slots: the unit is a power of two
+      float x[32];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const floatx16 s = scores16(smem + k * kStepKeys * kRowBytes, q16);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
+      }
+      const auto token = [&](int i) __attribute__((always_inline)) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + 4 * half + (i & 3); };
+      if (!sc.scored) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] *= own.natural;
+      }
+      to_scores<GENERAL>(own, row, x, true, [&](int k, int* at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) at[j] = next + s_depth[min(token(4 * k + j), n - 1)];
+      }, [&](int i) __attribute__((always_inline)) { return (row.sees >> token(i) & 1) == 0; });
+      add_rows16<2, true>(x, sc.factor, smem + kTokens * kRowBytes, BITS == 4 ? kTopHalf : 0.f, r);
+    }
+  }
+
+  // one result of the wavefronts that have the same rows
+  r.l = halves_add(r.l);
+  int t0 = 0, t1 = 4;                     // register groups that this wavefront has of it
+  if constexpr (WS > 1) {
+    __syncthreads();
+    if (half == 0) {
+      s_ml[wave][l32][0] = r.m;
+      s_ml[wave][l32][1] = r.l;
+      s_ml[wave][l32][2] = r.top;
+    }
+    __syncthreads();
+    float m = r.m;
+#pragma unroll
+    for (int k = 0; k < WS; ++k) m = fmaxf(m, s_ml[k * WR + wr][l32][0]);
+    float l = 0.f;
+#pragma unroll
+    for (int k = 0; k < WS; ++k) {
+      const float* ml = s_ml[k * WR + wr][l32];
+      l = __builtin_fmaf(ml[1], __builtin_amdgcn_exp2f((ml[0] - m) * sc.factor), l);
+      r.top = fmaxf(r.top, ml[2]);
+    }
+    const float alpha = __builtin_amdgcn_exp2f((r.m - m) * sc.factor);
+    r.m = m;
+    r.l = l;
+    float4* mine = reinterpret_cast<float4*>(smem) + wave * 16 * 64;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        mine[(4 * t + b) * 64 + lane] = make_float4(r.o[t][4 * b] * alpha, r.o[t][4 * b + 1] * alpha, r.o[t][4 * b + 2] * alpha, r.o[t][4 * b + 3] * alpha);
+    __syncthreads();
+    t0 = ws * 4 / WS;
+    t1 = t0 + 4 / WS;
+  }
+  const int64_t slot = (static_cast<int64_t>(item) * a.row_groups + rg) * a.pieces + piece;
+  const int64_t part_row = slot * (32 * WR) + 32 * wr + l32;
+  const bool direct = a.pieces == 1;
+  const float inv = direct ? (r.l == 0.f ? 0.f : 1.f / r.l) : 1.f;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    if (t < t0 || t >= t1) continue;
+    floatx16 o = r.o[t];
+    if constexpr (WS > 1) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < WS; ++k) {
+          const float4 w = reinterpret_cast<const float4*>(smem)[(k * WR + wr) * 16 * 64 + (4 * t + b) * 64 + lane];
+          v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+        }
+        o[4 * b] = v.x;
+        o[4 * b + 1] = v.y;
+        o[4 * b + 2] = v.z;
+        o[4 * b + 3] = v.w;
+      }
+    }
+    if (!row.there) continue;
+    if (direct) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        union { __bf16 h[4]; uint2 u; } w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w.h[j] = static_cast<__bf16>(o[4 * b + j] * inv);
+        *reinterpret_cast<uint2*>(a.out + q_row * kHeadDim + 32 * t + 8 * b + 4 * half) = w.u;
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<float4*>(a.part_acc + part_row * kHeadDim + 32 * t + 8 * b + 4 * half) = make_float4(o[4 * b], o[4 * b + 1], o[4 * b + 2], o[4 * b + 3]);
+    }
+  }
+  if (row.there && half == 0 && ws == 0) {
+    if (direct) {
+      if (a.stats) store_stats(a.stats + 2 * q_row, r.m, r.l, r.top, sc.factor, sc.scored ? 1.f : query.unit * kRoot, BITS == 4 ? kTopHalf : 0.f);
+    } else {
+      *reinterpret_cast<float4*>(a.part_ml + part_row * 4) = make_float4(r.m, r.l, r.top, query.unit);
+    }
+  }
+}
+
+// The pieces' results of 8 rows.
+template <int BITS>
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_rows) {
+  const int g = a.s.g, n = a.n, rows = n * g, blocks = (rows + 7) / 8;
+  const int item = blockIdx.x / blocks, row = blockIdx.x % blocks * 8 + (threadIdx.x >> 5), c = threadIdx.x & 31;
+  const int seq = item / a.s.hkv, kvh = item % a.s.hkv;
+  const int count = a.counts ? min(max(a.counts[seq], 0), n) : n;
+  if (row >= count * g) return;
+  const int64_t slot = (static_cast<int64_t>(item) * a.row_groups + row / group_rows) * a.pieces;
+  const int64_t first = slot * group_rows + row % group_rows;
+  const bool scored = a.s.cap > 0.f || a.s.slopes;
+  float m = kNoScore, top = kNoScore, unit = 1.f;
+  for (int p = 0; p < a.pieces; ++p) {
+    const float4 ml = *reinterpret_cast<const float4*>(a.part_ml + (first + static_cast<int64_t>(p) * group_rows) * 4);
+    m = fmaxf(m, ml.x);
+    top = fmaxf(top, ml.z);
+    unit = ml.w;
+  }
+  const float factor = scored ? kLog2e : unit * kRootLog2e;
+  float l = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = 0; p < a.pieces; ++p) {
+    const int64_t at = first + static_cast<int64_t>(p) * group_rows;
+    const float4 ml = *reinterpret_cast<const float4*>(a.part_ml + at * 4);
+    const float4 w = *reinterpret_cast<const float4*>(a.part_acc + at * kHeadDim + 4 * c);
+    const float f = __builtin_amdgcn_exp2f((ml.x - m) * factor);
+    l = __builtin_fmaf(ml.y, f, l);
+    v = make_float4(__builtin_fmaf(w.x, f, v.x), __builtin_fmaf(w.y, f, v.y), __builtin_fmaf(w.z, f, v.z), __builtin_fmaf(w.w, f, v.w));
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int64_t q_row = (static_cast<int64_t>(seq) * n + row / g) * a.s.hkv * g + kvh * g + row % g;
+  union { __bf16 h[4]; uint2 u; } out;
+  out.h[0] = static_cast<__bf16>(v.x * inv);
+  out.h[1] = static_cast<__bf16>(v.y * inv);
+  out.h[2] = static_cast<__bf16>(v.z * inv);
+  out.h[3] = static_cast<__bf16>(v.w * inv);
+  *reinterpret_cast<uint2*>(a.out + q_row * kHeadDim + 4 * c) = out.u;
+  if (c == 0 && a.stats) store_stats(a.stats + 2 * q_row, m, l, top, factor, scored ? 1.f : unit * kRoot, BITS == 4 ? kTopHalf : 0.f);
+}
+
+template <int BITS, int WR, bool GENERAL>
+hipError_t start(const TreeArgs& a, hipStream_t st) {
+  constexpr int lds = BITS == 16 ? kStageLds + kPosLds : std::max(kDraftLds + kMetaLds, kJoinLds);
+  const hipError_t e = RDKV_ALLOW_LDS((tree_kernel<BITS, WR, GENERAL>), lds);
+  if (e != hipSuccess) return e;
+  const int units = (a.items * a.pieces + 7) / 8 * 8;
+  hipLaunchKernelGGL((tree_kernel<BITS, WR, GENERAL>), dim3(units * a.row_groups), dim3(kThreads), lds, st, a);
+  return hipGetLastError();
+}
+
+template <int BITS, bool GENERAL>
+hipError_t start(const TreeArgs& a, int wide, hipStream_t st) {
+  return wide == 1 ? start<BITS, 1, GENERAL>(a, st) : wide == 2 ? start<BITS, 2, GENERAL>(a, st) : start<BITS, 4, GENERAL>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_tree(const TreeArgs& a, int bits, hipStream_t st) {
+  const TreePlan p = plan_tree(a.items, a.n * a.s.g, a.s.capacity, bits);
+  const bool general = a.s.cap > 0.f || a.s.slopes || a.s.window > 0;
+  hipError_t e = bits == 16 ? (general ? start<16, true>(a, p.wide, st) : start<16, false>(a, p.wide, st))
+                            : (general ? start<4, true>(a, p.wide, st) : start<4, false>(a, p.wide, st));
+  if (e != hipSuccess || a.pieces == 1) return e;
+  const int blocks = (a.n * a.s.g + 7) / 8;
+  if (bits == 16) hipLaunchKernelGGL(tree_join_kernel<16>, dim3(a.items * blocks), dim3(256), 0, st, a, 32 * p.wide);
+  else hipLaunchKernelGGL(tree_join_kernel<4>, dim3(a.items * blocks), dim3(256), 0, st, a, 32 * p.wide);
+  return hipGetLastError();
+}
+
+}  // namespace slots
+}  // namespace rdkv
