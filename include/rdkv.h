@@ -530,14 +530,17 @@ rdkv_status rdkv_slots_tree_attn(const rdkv_slots* slots, int32_t n, const void*
  *             first index that is negative or not below n
  *   n, q, k_draft, v_draft, stats  as of rdkv_slots_tree_attn; q and stats are needed, and read, where weights are kept
  *   slot      DEVICE int32 [batch][hkv][m] out, or NULL: the slots they took, -1 behind a path's end
+ *   workspace DEVICE scratch of at least rdkv_slots_accept_workspace_bytes(), 16-byte aligned
  * With c accepted tokens, the j-th at position next + j: weight becomes decay^c x weight + the sum over j of decay^(c-1-j) x the softmax's
  * value of token j, summed over the heads of the group, in slots below len.  Then the tokens come in one after the other as by rdkv_slots_append,
  * but that token i starts with the sum over j >= i of decay^(c-1-j) x what token j gives it.  While slots are free this is what c appends, each
  * followed by its decode step, leave.  Where the path is as long as a token of a full cache is `recent`, an accepted token may be
  * given up for a later one.  Rows of 4-bit caches are quantized as they come in.
  */
+size_t rdkv_slots_accept_workspace_bytes(const rdkv_slots* slots);
 rdkv_status rdkv_slots_accept(const rdkv_slots* slots, int32_t n, int32_t m, const void* q, const void* k_draft, const void* v_draft,
-                              const int32_t* path, const float* stats, int32_t* slot, void* stream);
+                              const int32_t* path, const float* stats, int32_t* slot, void* workspace, size_t workspace_bytes,
+                              void* stream);
 
 /*
  * Rows of the slots as bf16 (4-bit rows: scale x code + offset in fp32, rounded once).

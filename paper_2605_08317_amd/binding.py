@@ -33,7 +33,7 @@ EXPORTED_SYMBOLS = [
     "rdkv_cache_stats", "rdkv_cache_export_bytes", "rdkv_cache_export", "rdkv_cache_free",
     "rdkv_kernel_timing_enable", "rdkv_kernel_timing_read", "rdkv_k_row_words", "rdkv_k_row_words_max",
     "rdkv_prompt_default", "rdkv_prompt_attn_bf16",
-    "rdkv_slots_tree_workspace_bytes", "rdkv_slots_tree_attn", "rdkv_slots_accept",
+    "rdkv_slots_tree_workspace_bytes", "rdkv_slots_tree_attn", "rdkv_slots_accept_workspace_bytes", "rdkv_slots_accept",
     "rdkv_slots_default", "rdkv_slots_side_bytes", "rdkv_slots_fill_workspace_bytes", "rdkv_slots_fill", "rdkv_slots_append",
     "rdkv_slots_decode_workspace_bytes", "rdkv_slots_decode_attn", "rdkv_slots_read",
 ]
@@ -156,7 +156,9 @@ def _load():
     lib.rdkv_slots_tree_workspace_bytes.argtypes = [slp, i32]
     lib.rdkv_slots_tree_workspace_bytes.restype = sz
     lib.rdkv_slots_tree_attn.argtypes = [slp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    lib.rdkv_slots_accept.argtypes = [slp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.rdkv_slots_accept_workspace_bytes.argtypes = [slp]
+    lib.rdkv_slots_accept_workspace_bytes.restype = sz
+    lib.rdkv_slots_accept.argtypes = [slp, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.rdkv_slots_read.argtypes = [slp, vp, i32, vp, vp, vp]
     lib.rdkv_kernel_timing_enable.argtypes = [i32]
     lib.rdkv_kernel_timing_read.argtypes = [i32, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double)]
@@ -583,6 +585,10 @@ class Slots:
         need = lib.rdkv_slots_tree_workspace_bytes(self.ref(), _int32("n", n))
         return torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
 
+    def accept_workspace(self):
+        """Scratch of rdkv_slots_accept, for callers that keep it."""
+        return torch.empty(max(lib.rdkv_slots_accept_workspace_bytes(self.ref()), 16), dtype=torch.uint8, device=self.device)
+
 
 def _tensor(t, shape, dtype, device, name):
     """`t`, if it is what the library takes for `name`: it reads and writes plain memory."""
@@ -721,7 +727,7 @@ def rdkv_slots_tree_attn(slots, q, k_draft, v_draft, parent, counts=None, out=No
     return out, stats
 
 
-def rdkv_slots_accept(slots, q, k_draft, v_draft, path, stats, slot=None):
+def rdkv_slots_accept(slots, q, k_draft, v_draft, path, stats, slot=None, workspace=None):
     """The slots that the accepted tokens took: int32 [batch, hkv, m], -1 behind a path's end.  A cache without weights needs neither q nor stats (None)."""
     n = _drafted(slots, q, k_draft, v_draft)
     if path.dim() != 2:
@@ -732,8 +738,13 @@ def rdkv_slots_accept(slots, q, k_draft, v_draft, path, stats, slot=None):
         _tensor(stats, (slots.batch, n, slots.hq, 2), torch.float32, slots.device, "stats")
     shape = (slots.batch, slots.hkv, m)
     slot = torch.empty(shape, dtype=torch.int32, device=slots.device) if slot is None else _tensor(slot, shape, torch.int32, slots.device, "slot")
+    if workspace is None:
+        workspace = slots.accept_workspace()
+    elif workspace.dtype != torch.uint8 or workspace.device != slots.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {slots.device}")
     with _on(slots):
-        _check(lib.rdkv_slots_accept(slots.ref(), n, m, _ptr(q), k_draft.data_ptr(), v_draft.data_ptr(), path.data_ptr(), _ptr(stats), slot.data_ptr(), _stream()))
+        _check(lib.rdkv_slots_accept(slots.ref(), n, m, _ptr(q), k_draft.data_ptr(), v_draft.data_ptr(), path.data_ptr(), _ptr(stats), slot.data_ptr(),
+                                     workspace.data_ptr(), workspace.numel(), _stream()))
     return slot
 
 

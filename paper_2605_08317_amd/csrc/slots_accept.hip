@@ -1,10 +1,11 @@
 // Slot caches: accepted tokens of a drafted tree become part of the cache.
 //
-// Two launches.  The first gives every slot the attention weight that the tokens' heads gave it: scores as in slots_tree.hip (the same
-// products in the same order), probabilities by the largest score and the sum that the tree's step left, summed over heads and tokens, a wavefront
-// a tile of 64 slots; V is not read.  The second, a workgroup an item, takes the tokens in one after the other as that many appends would, but
-// looks at all slots only once: a thread keeps the least of its own slots, and looks again when one of them was given away or a token has
-// become old enough to go.
+// Two launches.  The first gives every slot the attention weight that the tokens' heads gave it, and the tokens themselves what they begin with:
+// products as in slots_tree.hip, but with the query rows on their A side, so that a lane has one slot and sums over the rows are its own;
+// probabilities by the largest score and the sum that the tree's step left.  V is not read.  Where a cache will be full it leaves the least of
+// every 32 slots as well.  The second, a workgroup an item, takes the tokens in one after the other as that many appends would, from those
+// leasts: when a slot is given away only its 32 are looked at again.
+//   bound   the K side once: HBM.  The second launch: a few dependent steps for each token that takes another's slot
 #include <algorithm>
 
 #include "group_quant.h"
@@ -15,8 +16,6 @@ namespace rdkv {
 namespace slots {
 
 namespace {
-
-constexpr int kWaves = 4;
 
 // tokens of a path: up to the first index that is none
 __device__ __forceinline__ int path_length(const int32_t* path, int m, int n) {
@@ -33,238 +32,394 @@ __device__ __forceinline__ float power(float x, int k) {
   return p;
 }
 
-template <int BITS, bool GENERAL>
-__global__ __launch_bounds__(64 * kWaves, BITS == 16 ? 1 : 2) void accept_weights_kernel(AcceptArgs a) {
+constexpr int kSegment = kLeastSlots;              // slots of a product
+
+// The least of a segment's slots that may go by (weight, position), and the lowest position of those that may not yet.
+struct __align__(16) Least {
+  uint64_t key;
+  int32_t at, enters;
+};
+static_assert(sizeof(Least) == kLeastBytes, "as the workspace's size has it");
+__device__ __forceinline__ Least nothing() { return {~0ull, 0, INT32_MAX}; }
+__device__ __forceinline__ void take(Least& l, uint64_t key, int at) {
+  if (key < l.key || (key == l.key && at < l.at)) {
+    l.key = key;
+    l.at = at;
+  }
+}
+// a slot: newest is the last position that may go
+__device__ __forceinline__ void look_at(Least& l, int slot, int pos, float weight, int sinks, int newest) {
+  if (pos < sinks) return;
+  if (pos > newest) l.enters = min(l.enters, pos);
+  else take(l, static_cast<uint64_t>(weight_key(weight)) << 32 | static_cast<uint32_t>(pos), slot);
+}
+
+// Rows of a pass over the slots: up to 64, in LDS as operands, with what probabilities are made with.
+constexpr int kRows = 64;
+struct __align__(16) RowTable {
+  float most[kRows], share[kRows];                   // largest score, decay over the sum
+  float natural[kRows], slope[kRows];                // what makes products scores; bias
+  int at[kRows];                                     // position
+};
+constexpr int kQueryLds = kRows / 32 * 9 * 1024;     // [32 rows][operand][lane], the last operand 4-bit rows' sums
+constexpr int kSlotLds = kSegment * kRowBytes + 512; // bf16: a segment's keys, weights, positions
+
+template <int BITS, bool GENERAL, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ RowTable s_row;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  const int item = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, seq = item / a.s.hkv, kvh = item % a.s.hkv, g = a.s.g;
+  // the first workgroups have an item's own tokens, the others a piece of its slots
+  const bool tokens = static_cast<int>(blockIdx.x) < a.items;
+  const int unit = static_cast<int>(blockIdx.x) - a.items, item = tokens ? blockIdx.x : unit / a.pieces, piece = tokens ? 0 : unit % a.pieces;
+  const int seq = item / a.s.hkv, kvh = item % a.s.hkv, g = a.s.g;
   const int32_t* path = a.path + static_cast<int64_t>(seq) * a.m;
   const int count = path_length(path, a.m, a.n), rows = count * g;
   if (count == 0) return;
-  const int len = a.s.length(item), next = a.s.next[item], tiles = (len + kTileRows - 1) / kTileRows;
-  const bool scored = GENERAL && (a.s.cap > 0.f || a.s.slopes);
+  const int len = a.s.length(item), next = a.s.next[item], cap = a.s.capacity;
+  const bool scored = GENERAL && (a.s.cap > 0.f || a.s.slopes), full = len + count > cap;
   const float inv_cap = a.s.cap > 0.f ? 1.f / a.s.cap : 0.f, old = power(a.s.decay, count);
-  const int32_t* pos = a.s.pos + static_cast<int64_t>(item) * a.s.capacity;
-  float* weight = a.s.weight + static_cast<int64_t>(item) * a.s.capacity;
-  const uint32_t lds0 = lds_address(smem);
+  const int32_t* pos = a.s.pos + static_cast<int64_t>(item) * cap;
+  float* weight = a.s.weight + static_cast<int64_t>(item) * cap;
+  Least* leasts = reinterpret_cast<Least*>(a.leasts) + static_cast<int64_t>(item) * ((cap + kSegment - 1) / kSegment);
+  uint8_t* mine = smem + kQueryLds + wave * (BITS == 16 ? 2 * kSlotLds : 0);
   using Query = std::conditional_t<BITS == 16, Query16, Query4>;
 
-  // of the tile's slots, scores' register i of product x is slot at(x, i)
-  const auto slot_at = [&](int x, int i) __attribute__((always_inline)) {
-    return BITS == 16 ? 32 * x + 8 * (i >> 2) + 4 * half + (i & 3) : 32 * half + 16 * x + i;
-  };
-  // what every query row gives a tile's slots, into sum
-  const auto gather = [&](auto scores, int tile, float (&sum)[32]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) sum[i] = 0.f;
-    for (int r0 = 0; r0 < rows; r0 += 32) {
-      const int r = min(r0 + l32, rows - 1), j = r / g, token = path[j];
-      const int64_t q_row = (static_cast<int64_t>(seq) * a.n + token) * a.s.hkv * g + kvh * g + r % g;
-      Query q;
+  // this wavefront's segments (4 bits: tiles of two): of its piece every WAVES-th
+  constexpr int kUnit = BITS == 16 ? kSegment : kTileRows;
+  const int units = (len + kUnit - 1) / kUnit;
+  const int u0 = static_cast<int>(static_cast<int64_t>(units) * piece / a.pieces), u1 = static_cast<int>(static_cast<int64_t>(units) * (piece + 1) / a.pieces);
+
+  // rows r0 .. of the path into LDS
+  const auto rows_in = [&](auto kind, int r0) __attribute__((always_inline)) {
+    using Q = decltype(kind);
+    if (r0 > 0) __syncthreads();
+    if (wave < kRows / 32) {
+      const int r = min(r0 + 32 * wave + l32, rows - 1), j = r / g;
+      const int64_t q_row = (static_cast<int64_t>(seq) * a.n + path[j]) * a.s.hkv * g + kvh * g + r % g;
+      Q q;
       q.load(a.q + q_row * kHeadDim);
+#pragma unroll
+      for (int kb = 0; kb < 8; ++kb) *reinterpret_cast<decltype(&q.op[0])>(smem + ((wave * 9 + kb) * 64 + lane) * 16) = q.op[kb];
+      if constexpr (std::is_same_v<Q, Query4>) *reinterpret_cast<halfx8*>(smem + ((wave * 9 + 8) * 64 + lane) * 16) = q.sums;
       const float2 st = *reinterpret_cast<const float2*>(a.stats + 2 * q_row);
-      const bool there = r0 + l32 < rows && st.y != 0.f;
-      const float share = power(a.s.decay, count - 1 - j) / st.y, natural = q.unit * kRoot;
-      floatx16 s[2];
-      scores(q, s);
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float e;
-          if constexpr (GENERAL) {
-            float v = s[x][i] * natural;
-            const int p = pos[min(tile * kTileRows + slot_at(x, i), len - 1)], away = next + j - p;
-            if (a.s.cap > 0.f) v = capped(v, a.s.cap, inv_cap);
-            if (a.s.slopes) v = __builtin_fmaf(-a.s.slopes[kvh * g + r % g], static_cast<float>(away), v);
-            e = scored ? v - st.x : __builtin_fmaf(s[x][i], natural, -st.x);
-            if (a.s.window > 0 && away >= a.s.window && p >= a.s.sinks) e = -INFINITY;
-          } else {
-            e = __builtin_fmaf(s[x][i], natural, -st.x);
-          }
-          const float p = __builtin_amdgcn_exp2f(e * kLog2e) * share;
-          sum[16 * x + i] += there ? p : 0.f;
-        }
+      if (half == 0) {
+        const int to = 32 * wave + l32;
+        const bool there = r0 + to < rows && st.y != 0.f;
+        s_row.most[to] = there ? st.x : INFINITY;              // (no row: probabilities of 0)
+        s_row.share[to] = there ? power(a.s.decay, count - 1 - j) / st.y : 0.f;
+        s_row.slope[to] = a.s.slopes ? a.s.slopes[kvh * g + r % g] : 0.f;
+        s_row.at[to] = next + j;
+        s_row.natural[to] = q.unit * kRoot;
+      }
     }
+    __syncthreads();
   };
-  const auto add = [&](int tile, float (&sum)[32]) __attribute__((always_inline)) {
-    const float w = rows_sum(sum);
-    const int slot = tile * kTileRows + slot_at(l32 >> 4, l32 & 15);
-    if (slot < len) weight[slot] = __builtin_fmaf(old, weight[slot], w);
+  // What the rows in LDS give a lane's slot (TOKENS: one of the path's) at `place`; scores(block): their products.
+  const auto given = [&](auto own, int r0, int place, auto scores) __attribute__((always_inline)) {
+    float sum = 0.f;
+    for (int b = 0; b < kRows / 32 && r0 + 32 * b < rows; ++b) {
+      const floatx16 s = scores(b);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = 32 * b + 8 * k + 4 * half;
+        const float4 most = *reinterpret_cast<const float4*>(s_row.most + r), share = *reinterpret_cast<const float4*>(s_row.share + r);
+        const float4 natural = *reinterpret_cast<const float4*>(s_row.natural + r);
+        const float ms[4] = {most.x, most.y, most.z, most.w}, sh[4] = {share.x, share.y, share.z, share.w}, na[4] = {natural.x, natural.y, natural.z, natural.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float e = __builtin_fmaf(s[4 * k + j], na[j], -ms[j]);
+          if constexpr (GENERAL || decltype(own)::value) {
+            const int away = s_row.at[r + j] - place;
+            if (scored) {
+              float v = s[4 * k + j] * na[j];
+              if (a.s.cap > 0.f) v = capped(v, a.s.cap, inv_cap);
+              if (a.s.slopes) v = __builtin_fmaf(-s_row.slope[r + j], static_cast<float>(away), v);
+              e = v - ms[j];
+            }
+            if (a.s.window > 0 && away >= a.s.window && place >= a.s.sinks) e = -INFINITY;
+            if (decltype(own)::value && away < 0) e = -INFINITY;
+          }
+          sum = __builtin_fmaf(__builtin_amdgcn_exp2f(e * kLog2e), sh[j], sum);
+        }
+        if constexpr (GENERAL) __builtin_amdgcn_sched_barrier(0);        // (sixteen side by side do not fit the registers)
+      }
+    }
+    return halves_add(sum);
+  };
+  const auto operand16 = [&](int b, int k) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(smem + ((b * 9 + k) * 64 + lane) * 16); };
+  const auto operand4 = [&](int b, int k) __attribute__((always_inline)) { return *reinterpret_cast<const halfx8*>(smem + ((b * 9 + k) * 64 + lane) * 16); };
+  const auto products16 = [&](const uint8_t* keys, int b) __attribute__((always_inline)) {
+    floatx16 s = {};
+#pragma unroll
+    for (int kb = 0; kb < 8; ++kb) s = product(operand16(b, kb), read_k(keys, kb), s);
+    return s;
   };
 
-  const int t0 = static_cast<int>(static_cast<int64_t>(tiles) * piece / a.pieces), t1 = static_cast<int>(static_cast<int64_t>(tiles) * (piece + 1) / a.pieces);
-  if constexpr (BITS == 16) {
-    // each wavefront has tiles of its own in LDS, two buffers
-    constexpr int kTileLds = kTileRows * kRowBytes;
-    const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
-    const uint32_t k_at = 16 * (lane & 15);
-    const auto fetch = [&](int tile, int buffer) __attribute__((always_inline)) {
-      const int first = min(tile, t1 - 1) * kTileRows, last = len - 1 - first;
-      const uint8_t* k = K + static_cast<int64_t>(first) * kRowBytes;
+  if (tokens) {
+    // the path's keys behind the rows: wavefronts 0 and 1 have 32 tokens each
+    const int token = 32 * wave + l32;
+    uint8_t* keys = smem + kQueryLds + wave * (kSegment * kRowBytes);
+    if (wave < 2) {
+      const uint32_t to = lds_address(keys);
+      const uint8_t* k = reinterpret_cast<const uint8_t*>(a.k_draft) + (static_cast<int64_t>(seq) * a.n * a.s.hkv + kvh) * kRowBytes;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 8; ++i) {
         const int row = 4 * i + (lane >> 4);
-        copy_to_lds(k, min(row, last) * kRowBytes + (k_at ^ (16 * (row & 15))), lds0 + (2 * wave + buffer) * kTileLds + 1024 * i);
+        copy_to_lds(k, path[min(32 * wave + row, count - 1)] * a.s.hkv * kRowBytes + 16 * k_piece(row, lane & 15), to + 1024 * i);
       }
-    };
-    int t = t0 + wave, buffer = 0;
-    if (t >= t1) return;
-    fetch(t, 0);
-    for (; t < t1; t += kWaves, buffer ^= 1) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      fetch(t + kWaves, buffer ^ 1);
-      const uint8_t* kt = smem + (2 * wave + buffer) * kTileLds;
-      float sum[32];
-      gather([&](const Query& q, floatx16 (&s)[2]) __attribute__((always_inline)) {
-        s[0] = scores16(kt, q);
-        s[1] = scores16(kt + kStepKeys * kRowBytes, q);
-      }, t, sum);
-      add(t, sum);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  } else {
-    uint8_t* meta = smem + wave * kKMeta;
-    const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
-    for (int t = t0 + wave; t < t1; t += kWaves) {
+    float sum = 0.f;
+    for (int r0 = 0; r0 < rows; r0 += kRows) {
+      rows_in(Query16{}, r0);
+      if (wave < 2) sum += given(std::true_type{}, r0, next + token, [&](int b) __attribute__((always_inline)) { return products16(keys, b); });
+    }
+    if (wave < 2 && half == 0 && token < count) a.begins[static_cast<int64_t>(item) * kMostDrafted + token] = sum;
+    return;
+  }
+
+  // a lane's slot gets its weight; the least of the lanes' slots whose numbers differ in the bits of `lanes`
+  const auto put = [&](int slot, float before, int place, float sum, float keep, bool last_pass, auto lanes) __attribute__((always_inline)) {
+    const float w = __builtin_fmaf(keep, before, sum);
+    if (slot < len && half == 0) weight[slot] = w;
+    Least l = nothing();
+    if (full && last_pass) {
+      if (slot < len) look_at(l, slot, place, w, a.s.sinks, next - a.s.recent);
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        if (!(decltype(lanes)::value & d)) continue;
+        const uint64_t key = __shfl_xor(l.key, d);
+        const int at = __shfl_xor(l.at, d);
+        take(l, key, at);
+        l.enters = min(l.enters, __shfl_xor(l.enters, d));
+      }
+    }
+    return l;
+  };
+
+  for (int r0 = 0; r0 < rows; r0 += kRows) {
+    const bool last_pass = r0 + kRows >= rows;
+    const float keep = r0 == 0 ? old : 1.f;
+    rows_in(Query{}, r0);
+    if constexpr (BITS == 16) {
+      const uint8_t* K = a.s.k + static_cast<int64_t>(item) * cap * kRowBytes;
+      const uint32_t lds0 = lds_address(mine);
+      const auto fetch = [&](int unit, int buffer) __attribute__((always_inline)) {
+        const int first = min(unit, u1 - 1) * kSegment, last = len - 1 - first;
+        const uint8_t* k = K + static_cast<int64_t>(first) * kRowBytes;
+        const uint32_t to = lds0 + buffer * kSlotLds;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int row = 4 * i + (lane >> 4);
+          copy_to_lds(k, min(row, last) * kRowBytes + 16 * k_piece(row, lane & 15), to + 1024 * i);
+        }
+        copy_word_to_lds(weight + first, 4 * min(l32, last), to + kSegment * kRowBytes);
+        copy_word_to_lds(pos + first, 4 * min(l32, last), to + kSegment * kRowBytes + 256);
+      };
+      int u = u0 + wave, buffer = 0;
+      if (u < u1) {
+        fetch(u, 0);
+        for (; u < u1; u += WAVES, buffer ^= 1) {
+          fetch(u + WAVES, buffer ^ 1);
+          asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+          const uint8_t* keys = mine + buffer * kSlotLds;
+          const float before = reinterpret_cast<const float*>(keys + kSegment * kRowBytes)[l32];
+          const int place = reinterpret_cast<const int*>(keys + kSegment * kRowBytes + 256)[l32], slot = u * kSegment + l32;
+          const float sum = given(std::false_type{}, r0, place, [&](int b) __attribute__((always_inline)) { return products16(keys, b); });
+          const Least l = put(slot, before, place, sum, keep, last_pass, std::integral_constant<int, 31>{});
+          if (full && last_pass && lane == 0) leasts[u] = l;
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+    } else {
+      const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
       Side4 k;
-      k.load(K + static_cast<int64_t>(t) * kTileBytes, true);
-      put_k_meta(meta, k, len - t * kTileRows);
-      wave_lds_order();
-      float sum[32];
-      gather([&](const Query& q, floatx16 (&s)[2]) __attribute__((always_inline)) { scores4(k, meta, q, s); }, t, sum);
-      add(t, sum);
-      wave_lds_order();
+      uint4 meta[2];                               // of the lane's slots
+      float before[2];
+      int place[2];
+      const auto load = [&](int tile) __attribute__((always_inline)) {
+        const uint8_t* t = K + static_cast<int64_t>(tile) * kTileBytes;
+        k.load(t, true);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int slot = min(tile * kTileRows + slot_of_row(x, l32), len - 1);
+          meta[x] = *reinterpret_cast<const uint4*>(t + kTileCodes + 16 * (slot & (kTileRows - 1)));
+          before[x] = weight[slot];
+          place[x] = pos[slot];
+        }
+      };
+      int u = u0 + wave;
+      if (u < u1) load(u);
+      for (; u < u1; u += WAVES) {
+        const Words4 words(k);
+        union { uint4 u; halfx4 h[2]; } m[2];
+        float w[2];
+        int at[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          m[x].u = meta[x];
+          w[x] = before[x];
+          at[x] = place[x];
+        }
+        if (u + WAVES < u1) load(u + WAVES);
+        Least l = nothing();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const float sum = given(std::false_type{}, r0, at[x], [&](int b) __attribute__((always_inline)) {
+            floatx16 s = product(operand4(b, 8), centres(m[x].u), floatx16{});
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              floatx16 sums = product(operand4(b, 2 * c), words.operand(x, c, 0), floatx16{});
+              sums = product(operand4(b, 2 * c + 1), words.operand(x, c, 1), sums);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(static_cast<float>(m[x].h[0][c]), sums[i], s[i]);
+            }
+            return s;
+          });
+          // (bit 2 of a product's row is which segment its slot is in)
+          const Least some = put(u * kTileRows + slot_of_row(x, l32), w[x], at[x], sum, keep, last_pass, std::integral_constant<int, 27>{});
+          take(l, some.key, some.at);
+          l.enters = min(l.enters, some.enters);
+        }
+        const int segment = 2 * u + (lane >> 2);
+        if (full && last_pass && (lane == 0 || lane == 4) && segment * kSegment < len) leasts[segment] = l;
+      }
     }
   }
 }
 
 constexpr int kThreads = 1024;
 
+// The second launch.  Which slots go follows from three kinds of tokens, of which a lane of the first wavefront has one each at most: the least of
+// the slots that could go at once, over the lane's segments; a cached token that becomes old enough on the way; and an accepted one that does.  Only
+// where one of the first kind goes memory is read again, its segment's slots and the leasts of the lane's segments.
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void accept_append_kernel(AcceptArgs a) {
-  __shared__ float s_weight[kMostDrafted];         // what a token begins with
-  __shared__ int s_slot[kMostDrafted], s_path[kMostDrafted];
-  __shared__ uint64_t s_key[2][kThreads / 64];
-  __shared__ int s_at[2][kThreads / 64];
-  const int item = blockIdx.x, seq = item / a.s.hkv, kvh = item % a.s.hkv, g = a.s.g, cap = a.s.capacity;
+  constexpr int kWaves = kThreads / 64;
+  __shared__ int s_slot[kMostDrafted], s_late[kMostDrafted];
+  __shared__ uint64_t s_key[kWaves][64];
+  __shared__ int s_at[kWaves][64];
+  const int item = blockIdx.x, seq = item / a.s.hkv, kvh = item % a.s.hkv, cap = a.s.capacity;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int count = path_length(a.path + static_cast<int64_t>(seq) * a.m, a.m, a.n);
+  const int32_t* path = a.path + static_cast<int64_t>(seq) * a.m;
+  const int count = path_length(path, a.m, a.n);
   int32_t* out = a.slot ? a.slot + static_cast<int64_t>(item) * a.m : nullptr;
   if (out && tid < a.m && tid >= count) out[tid] = -1;
   if (count == 0) return;
-  if (tid < count) {
-    s_path[tid] = a.path[static_cast<int64_t>(seq) * a.m + tid];
-    s_weight[tid] = 0.f;
-  }
   const int len = a.s.length(item), next = a.s.next[item];
-  __syncthreads();
-  if (a.s.weight) {
-    // token i has from each head of the tokens j >= i: sixteen lanes a product
-    const int piece = tid & 15;
-    for (int i = tid >> 4; i < count; i += kThreads / 16) {
-      const uint16_t* k = a.k_draft + ((static_cast<int64_t>(seq) * a.n + s_path[i]) * a.s.hkv + kvh) * kHeadDim + 8 * piece;
-      const bf16x8 kv = *reinterpret_cast<const bf16x8*>(k);
-      float sum = 0.f;
-      for (int j = i; j < count; ++j)
-        for (int h = 0; h < g; ++h) {
-          const int64_t q_row = (static_cast<int64_t>(seq) * a.n + s_path[j]) * a.s.hkv * g + kvh * g + h;
-          const bf16x8 qv = *reinterpret_cast<const bf16x8*>(a.q + q_row * kHeadDim + 8 * piece);
-          float x = 0.f;
-#pragma unroll
-          for (int c = 0; c < 8; ++c) x = __builtin_fmaf(static_cast<float>(kv[c]), static_cast<float>(qv[c]), x);
-          x = row_sum(x);
-          const float2 st = *reinterpret_cast<const float2*>(a.stats + 2 * q_row);
-          const int away = j - i;
-          float e = __builtin_fmaf(x, kRoot, -st.x);
-          if (a.s.cap > 0.f || a.s.slopes) {
-            x *= kRoot;
-            if (a.s.cap > 0.f) x = capped(x, a.s.cap, 1.f / a.s.cap);
-            if (a.s.slopes) x = __builtin_fmaf(-a.s.slopes[kvh * g + h], static_cast<float>(away), x);
-            e = x - st.x;
-          }
-          const bool hidden = a.s.window > 0 && away >= a.s.window && next + i >= a.s.sinks;
-          if (!hidden && st.y != 0.f) sum += __builtin_amdgcn_exp2f(e * kLog2e) * (power(a.s.decay, count - 1 - j) / st.y);
-        }
-      if (piece == 0) s_weight[i] = sum;
-    }
-    __syncthreads();
-  }
+  const bool full = len + count > cap;
 
   int32_t* pos = a.s.pos + static_cast<int64_t>(item) * cap;
   float* weight = a.s.weight ? a.s.weight + static_cast<int64_t>(item) * cap : nullptr;
-  // this thread's slots: tid, tid + kThreads, ..
-  uint64_t best = ~0ull;                           // least weight, then lowest position, of those that may go
-  int at = 0, enters = INT32_MAX;                  // of the others the lowest position
-  const auto look = [&](int newest) {
-    constexpr int kEach = 8;
-    best = ~0ull;
-    at = 0;
-    enters = INT32_MAX;
-    for (int i0 = tid; i0 < cap; i0 += kEach * kThreads) {
-      int p[kEach];
-      float w[kEach];
-#pragma unroll
-      for (int k = 0; k < kEach; ++k) {
-        const int i = min(i0 + k * kThreads, cap - 1);
-        p[k] = pos[i];
-        w[k] = weight ? weight[i] : 0.f;
+  const float* begins = weight ? a.begins + static_cast<int64_t>(item) * kMostDrafted : nullptr;
+  const int segments = (cap + kSegment - 1) / kSegment, used = (len + kSegment - 1) / kSegment;
+  Least* leasts = reinterpret_cast<Least*>(a.leasts) + static_cast<int64_t>(item) * segments;
+  const int newest = next - a.s.recent;            // the last position that may go for the first token
+  if (tid < kMostDrafted) s_late[tid] = INT32_MAX;
+  __syncthreads();
+  if (full) {
+    // the leasts of the lanes' segments, lane + 64 k, a part of them each wavefront; and who becomes old enough
+    Least l = nothing();
+    for (int e = tid; e < used; e += kThreads) {
+      Least of;
+      if (weight) {
+        of = leasts[e];
+      } else {                                     // (no launch has looked: the oldest go)
+        of = nothing();
+        for (int i = e * kSegment; i < min((e + 1) * kSegment, len); ++i) look_at(of, i, pos[i], 0.f, a.s.sinks, newest);
+        leasts[e] = of;
       }
-#pragma unroll
-      for (int k = 0; k < kEach; ++k) {
-        const int i = i0 + k * kThreads;
-        if (i >= cap || p[k] < a.s.sinks) continue;
-        const uint64_t key = static_cast<uint64_t>(weight_key(w[k])) << 32 | static_cast<uint32_t>(p[k]);
-        if (p[k] > newest) enters = min(enters, p[k]);
-        else if (key < best) best = key, at = i;
+      take(l, of.key, of.at);
+      if (of.enters < newest + count) {
+        for (int i = e * kSegment; i < min((e + 1) * kSegment, len); ++i) {
+          const int after = pos[i] - newest - 1;
+          if (pos[i] >= a.s.sinks && after >= 0 && after < count) atomicMin(&s_late[after], i);
+        }
       }
     }
-  };
-  bool looked = false;
-  for (int j = 0; j < count; ++j) {
-    int slot = len + j;
-    if (slot >= cap) {
-      const int newest = next + j - a.s.recent;
-      if (!looked || enters <= newest) look(newest);
-      looked = true;
-      uint64_t key = best;
-      int where = at;
-      const auto least = [&](uint64_t other, int other_at) __attribute__((always_inline)) {
-        if (other < key || (other == key && other_at < where)) {
-          key = other;
-          where = other_at;
-        }
-      };
+    s_key[wave][lane] = l.key;
+    s_at[wave][lane] = l.at;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    Least l = nothing();
+    uint64_t late = ~0ull, mine = ~0ull;           // of the lane's token that becomes old enough, and of its accepted one
+    int late_at = 0, slot = len + lane;            // (slot: of accepted token `lane`)
+    const uint64_t begin = static_cast<uint64_t>(lane < count && weight ? weight_key(begins[lane]) : weight_key(0.f)) << 32 | static_cast<uint32_t>(next + lane);
+    if (full) {
+      for (int w = 0; w < kWaves; ++w) take(l, s_key[w][lane], s_at[w][lane]);
+      late_at = s_late[lane];
+      if (late_at != INT32_MAX) late = static_cast<uint64_t>(weight_key(weight ? weight[late_at] : 0.f)) << 32 | static_cast<uint32_t>(newest + 1 + lane);
+    }
+    const int age = max(a.s.recent, 1);
+    const int first = max(cap - len, 0);
+    for (int j = first; j < count; ++j) {
+      if (lane <= j - age && (j == first || lane == j - age) && next + lane >= a.s.sinks) mine = begin;
+      // the least of the lane's, and of the wavefront's: whose it is with it (lane, kind)
+      uint64_t key = l.key;
+      int at = l.at, who = lane;
+      if (lane < j && late < key) key = late, at = late_at, who = 64 + lane;
+      if (mine < key) key = mine, at = slot, who = 128 + lane;
+#pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t other = __shfl_xor(key, d);
-        least(other, __shfl_xor(where, d));
+        const uint64_t k = __shfl_xor(key, d);
+        const int t = __shfl_xor(at, d), w = __shfl_xor(who, d);
+        if (k < key || (k == key && (t < at || (t == at && w < who)))) key = k, at = t, who = w;
+      }
+      if (lane == j) slot = at;
+      if (key == ~0ull) continue;                  // (nobody may go: slot 0)
+      const int kind = who >> 6, whose = who & 63;
+      if (kind == 1 && lane == whose) late = ~0ull;
+      if (kind == 2 && lane == whose) mine = ~0ull;
+      if (kind != 0) continue;
+      // the segment again, without the slots that are taken: half of the wavefront its slots, all of it the leasts of the others of `whose`
+      const int segment = at / kSegment, i = segment * kSegment + (lane & 31);
+      const int p = pos[min(i, cap - 1)];
+      const float w = weight ? weight[min(i, cap - 1)] : 0.f;
+      Least again = nothing();
+      for (int e = whose + 64 * lane; e < used; e += 64 * 64) {
+        if (e == segment) continue;
+        const Least of = leasts[e];
+        take(again, of.key, of.at);
+      }
+      bool taken = i >= len;
+      for (int t = 0; t <= j; ++t) taken = taken || __builtin_amdgcn_readlane(slot, t) == i;
+      Least seg = nothing();
+      if (!taken) look_at(seg, i, p, w, a.s.sinks, newest);
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        take(seg, __shfl_xor(seg.key, d), __shfl_xor(seg.at, d));
+        take(again, __shfl_xor(again.key, d), __shfl_xor(again.at, d));
       }
       if (lane == 0) {
-        s_key[j & 1][wave] = key;
-        s_at[j & 1][wave] = where;
+        leasts[segment].key = seg.key;
+        leasts[segment].at = seg.at;
       }
-      __syncthreads();
-      key = s_key[j & 1][lane & (kThreads / 64 - 1)];
-      where = s_at[j & 1][lane & (kThreads / 64 - 1)];
-      for (int d = 1; d < kThreads / 64; d <<= 1) {
-        const uint64_t other = __shfl_xor(key, d);
-        least(other, __shfl_xor(where, d));
+      if (lane == whose) {
+        l = seg;
+        take(l, again.key, again.at);
       }
-      slot = where;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");           // (the next to look at the segment reads what lane 0 has written)
     }
-    if (slot % kThreads == tid) {                  // the thread that has the slot
-      pos[slot] = next + j;
-      if (weight) weight[slot] = s_weight[j];
-      s_slot[j] = slot;
-      if (out) out[j] = slot;
-      if (looked) look(next + j - a.s.recent);
+    if (lane < count) {
+      s_slot[lane] = slot;
+      if (out) out[lane] = slot;
+    }
+    // positions and weights: of tokens in one slot the last one's
+    bool last = lane < count;
+    for (int t = 1; t < count; ++t) last = last && !(t > lane && __builtin_amdgcn_readlane(slot, t) == slot);
+    if (last) {
+      pos[slot] = next + lane;
+      if (weight) weight[slot] = begins[lane];
+    }
+    if (lane == 0) {
+      a.s.len[item] = min(len + count, cap);
+      a.s.next[item] = next + count;
     }
   }
   __syncthreads();
-  if (tid == 0) {
-    a.s.len[item] = min(len + count, cap);
-    a.s.next[item] = next + count;
-  }
   // rows: half a wavefront a token, lanes 0..15 its K row, 16..31 its V row.  Of tokens in one slot the last stays
   for (int j = wave; j < count; j += kThreads / 64) {
     const int slot = s_slot[j];
@@ -273,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void accept_append_kernel(AcceptArgs a) {
     if (lane >= 32 || !last) continue;
     const int c16 = lane & 15, grp = c16 >> 2, p = c16 & 3;
     const bool is_v = lane >= 16;
-    const uint4 row = reinterpret_cast<const uint4*>(is_v ? a.v_draft : a.k_draft)[((static_cast<int64_t>(seq) * a.n + s_path[j]) * a.s.hkv + kvh) * 16 + c16];
+    const uint4 row = reinterpret_cast<const uint4*>(is_v ? a.v_draft : a.k_draft)[((static_cast<int64_t>(seq) * a.n + path[j]) * a.s.hkv + kvh) * 16 + c16];
     uint8_t* side = is_v ? a.s.v : a.s.k;
     if constexpr (BITS == 16) {
       reinterpret_cast<uint4*>(side)[(static_cast<int64_t>(item) * cap + slot) * 16 + c16] = row;
@@ -306,11 +461,16 @@ __global__ __launch_bounds__(kThreads) void accept_append_kernel(AcceptArgs a) {
 }
 
 template <int BITS, bool GENERAL>
-hipError_t start(const AcceptArgs& a, hipStream_t st) {
-  constexpr int lds = BITS == 16 ? kWaves * 2 * kTileRows * kRowBytes : kWaves * kKMeta;
-  const hipError_t e = RDKV_ALLOW_LDS((accept_weights_kernel<BITS, GENERAL>), lds);
+hipError_t start(AcceptArgs& a, hipStream_t st) {
+  // in bf16 eight wavefronts fill a compute unit's LDS
+  constexpr int kWaves = BITS == 16 ? 8 : 4, kUnit = BITS == 16 ? kSegment : kTileRows;
+  constexpr int lds = kQueryLds + (BITS == 16 ? kWaves * 2 * kSlotLds : 2 * kSegment * kRowBytes);
+  const auto kernel = accept_weights_kernel<BITS, GENERAL, kWaves>;
+  const hipError_t e = RDKV_ALLOW_LDS(kernel, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((accept_weights_kernel<BITS, GENERAL>), dim3(a.items * a.pieces), dim3(64 * kWaves), lds, st, a);
+  const int units = (a.s.capacity + kUnit - 1) / kUnit;
+  a.pieces = std::max(1, std::min((units + kWaves - 1) / kWaves, (BITS == 16 ? 512 : 1024) / a.items));
+  hipLaunchKernelGGL(kernel, dim3(a.items * (a.pieces + 1)), dim3(64 * kWaves), lds, st, a);
   return hipGetLastError();
 }
 
@@ -320,8 +480,6 @@ hipError_t launch_accept(const AcceptArgs& args, int bits, hipStream_t st) {
   AcceptArgs a = args;
   if (a.s.weight) {
     const bool general = a.s.cap > 0.f || a.s.slopes || a.s.window > 0;
-    const int tiles = (a.s.capacity + kTileRows - 1) / kTileRows;
-    a.pieces = std::max(1, std::min((tiles + kWaves - 1) / kWaves, 1024 / a.items));
     const hipError_t e = bits == 16 ? (general ? start<16, true>(a, st) : start<16, false>(a, st)) : (general ? start<4, true>(a, st) : start<4, false>(a, st));
     if (e != hipSuccess) return e;
   }

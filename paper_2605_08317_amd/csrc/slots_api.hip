@@ -252,16 +252,24 @@ rdkv_status rdkv_slots_tree_attn(const rdkv_slots* s, int32_t n, const void* q, 
   return RDKV_OK;
 }
 
+size_t rdkv_slots_accept_workspace_bytes(const rdkv_slots* s) {
+  if (check_slots(s, false) != RDKV_OK) return 0;
+  return slots::accept_workspace_bytes(static_cast<int64_t>(s->batch) * s->hkv, s->capacity);
+}
+
 rdkv_status rdkv_slots_accept(const rdkv_slots* s, int32_t n, int32_t m, const void* q, const void* k_draft, const void* v_draft,
-                              const int32_t* path, const float* stats, int32_t* slot, void* stream) {
+                              const int32_t* path, const float* stats, int32_t* slot, void* workspace, size_t workspace_bytes, void* stream) {
   rdkv_status e = check_slots(s, true);
   if (e != RDKV_OK || (e = check_drafted(n)) != RDKV_OK) return e;
   if (m < 1 || m > slots::kMostDrafted) return fail(RDKV_ERR_SHAPE, "paths of %d tokens (1 to %d)", m, slots::kMostDrafted);
   if (s->batch == 0) return RDKV_OK;
   if (!k_draft || !v_draft || !path) return fail(RDKV_ERR_INVALID_ARG, "k_draft, v_draft and path must not be null");
   if (s->weight && (!q || !stats)) return fail(RDKV_ERR_INVALID_ARG, "a cache that keeps weights needs q and stats");
-  if (!aligned16({q, k_draft, v_draft}) || (reinterpret_cast<uintptr_t>(stats) & 7) != 0)
-    return fail(RDKV_ERR_INVALID_ARG, "q, k_draft and v_draft must be aligned to 16 bytes, stats to 8");
+  const size_t need = rdkv_slots_accept_workspace_bytes(s);
+  if (!workspace || workspace_bytes < need)
+    return fail(RDKV_ERR_INVALID_ARG, "workspace of %zu bytes is smaller than the %zu required", workspace ? workspace_bytes : 0, need);
+  if (!aligned16({q, k_draft, v_draft, workspace}) || (reinterpret_cast<uintptr_t>(stats) & 7) != 0)
+    return fail(RDKV_ERR_INVALID_ARG, "q, k_draft, v_draft and workspace must be aligned to 16 bytes, stats to 8");
   slots::AcceptArgs a{};
   a.s = args_of(s);
   a.q = static_cast<const uint16_t*>(q);
@@ -270,6 +278,8 @@ rdkv_status rdkv_slots_accept(const rdkv_slots* s, int32_t n, int32_t m, const v
   a.path = path;
   a.stats = stats;
   a.slot = slot;
+  a.begins = static_cast<float*>(workspace);
+  a.leasts = a.begins + static_cast<int64_t>(s->batch) * s->hkv * slots::kMostDrafted;
   a.items = s->batch * s->hkv;
   a.n = n;
   a.m = m;

@@ -6,10 +6,11 @@
 // slots of a product are chosen so that a lane's scores are of 16 slots in a row: result register i of lane (half, .) of product x is slot
 // 32 half + 16 x + i.  V codes: a lane's word quadruple is one channel's 32 slots of its half, so step f of P V (fields f of the four words)
 // takes slots 4 f + 0..3 and 16 + 4 f + 0..3 of the half, which are registers 4 f .. 4 f + 3 of the lane's two products.
-//   scores  K codes are bf16 numbers 1 + code / 16 and meet the query's bf16 values, exactly; a group's sums of products are added with the
-//           slots' scales in fp32.  What the 1 adds, and the offsets, are a product of their own: a slot's metadata row, four scales and four
-//           offsets in fp16, against sums of the query's values over a group, each in two fp16 terms (22 bits).  Queries are
-//           taken over a power of two, so that these terms have their bits whatever the queries' size
+//   scores  codes less 8 are fp16 numbers and meet the query's values in fp16 (their 8 bits, over a power of two of the row's: values down to
+//           2^-23 of the row's largest keep them all), so that products are exact; a group's sums of products are added with the slots' scales
+//           in fp32.  What is left of a value, its offset plus 8 scales, in two fp16 terms, is a product of its own with sums of the query's
+//           values over a group, also two.  (With the codes themselves that product and the other sums are large and nearly cancel: 131072
+//           slots, largest scores and sums 2.6e-6 of their norm off from fp32 sums over the values)
 //   P V     V codes less 8 are scaled to fp16 values by one fused multiply-add (rounded once, 2^-12 of the value; a group's offset plus 8
 //           scales, which it starts from, too), probabilities are fp16
 #pragma once
@@ -30,22 +31,6 @@ constexpr float kNoScore = -2e38f;       // a finite maximum of nothing, also ti
 __device__ __forceinline__ floatx16 product(halfx8 a, halfx8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 using attn::product;
 
-// Sums over the wavefront's lanes whose query rows are 32 different ones: register i of v becomes, in lane (half, i % 32 of them), the sum of
-// v[i] over the half's lanes.  32 numbers a lane: each step adds what half of the lanes hand over.
-__device__ __forceinline__ float rows_sum(float (&v)[32]) {
-  const int l = threadIdx.x & 31;
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    const bool up = (l & d) != 0;
-#pragma unroll
-    for (int i = 0; i < d; ++i) {
-      const float keep = up ? v[i + d] : v[i], give = up ? v[i] : v[i + d];
-      v[i] = keep + __shfl_xor(give, d);
-    }
-  }
-  return v[0];
-}
-
 // Query rows of a wavefront as operands.
 struct Query16 {
   bf16x8 op[8];
@@ -60,24 +45,25 @@ struct Query16 {
   }
 };
 struct Query4 {
-  bf16x8 op[8];                          // product 2 group + s: channels 32 group + 16 half + 8 s ..
-  halfx8 sums;                           // for a metadata row: minus a group's sum, and a sixteenth of it; high terms in the lower half's lanes, low in the upper's
+  halfx8 op[8];                          // product 2 group + s: channels 32 group + 16 half + 8 s ..
+  halfx8 sums;                           // of the groups' values, twice four: high terms in the lower half's lanes, low ones in the upper's
   float unit;
   __device__ __forceinline__ void load(const uint16_t* q) {
     const int half = (threadIdx.x & 63) >> 5;
+    bf16x8 in[8];
     float most = 0.f;
 #pragma unroll
     for (int kb = 0; kb < 8; ++kb) {
-      op[kb] = *reinterpret_cast<const bf16x8*>(q + 32 * (kb >> 1) + 16 * half + 8 * (kb & 1));
+      in[kb] = *reinterpret_cast<const bf16x8*>(q + 32 * (kb >> 1) + 16 * half + 8 * (kb & 1));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(static_cast<float>(op[kb][i])));
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(static_cast<float>(in[kb][i])));
     }
     most = halves_max(most);
-    // the largest value over the power of two is in [1, 2); of zeros, infinities and the like: as they are
+    // the largest value over the unit is in [2^9, 2^10), a group's sum below 2^15; of zeros, infinities and the like: as they are
     const int e = static_cast<int>(__float_as_uint(most) >> 23);
     const bool plain = e >= 1 && e <= 253;
-    const float inv = plain ? __uint_as_float(static_cast<uint32_t>(254 - e) << 23) : 1.f;
-    unit = 16.f * (plain ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 1.f);
+    const float inv = 0x1p9f * (plain ? __uint_as_float(static_cast<uint32_t>(254 - e) << 23) : 1.f);
+    unit = 0x1p-9f * (plain ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 1.f);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float sum = 0.f;
@@ -85,14 +71,13 @@ struct Query4 {
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float x = static_cast<float>(op[2 * g + s][i]) * inv;
-          op[2 * g + s][i] = static_cast<__bf16>(x);
+          const float x = static_cast<float>(in[2 * g + s][i]) * inv;
+          op[2 * g + s][i] = static_cast<_Float16>(x);
           sum += x;
         }
       sum = halves_add(sum);
-      const _Float16 a = static_cast<_Float16>(-sum), b = static_cast<_Float16>(sum * 0.0625f);
-      sums[g] = half == 0 ? a : static_cast<_Float16>(-sum - static_cast<float>(a));
-      sums[4 + g] = half == 0 ? b : static_cast<_Float16>(sum * 0.0625f - static_cast<float>(b));
+      const _Float16 hi = static_cast<_Float16>(sum);
+      sums[g] = sums[4 + g] = half == 0 ? hi : static_cast<_Float16>(sum - static_cast<float>(hi));
     }
   }
 };
@@ -122,13 +107,26 @@ struct Side4 {
   }
 };
 
-// K metadata into LDS (kKMeta bytes of the wavefront's), of slots from `rows` on zeros: the rows, then the scales again, [group][slot].
+// Of a slot's four scales and offsets: the offsets plus 8 scales, in two terms.
+__device__ __forceinline__ halfx8 centres(uint4 meta) {
+  union { uint4 u; _Float16 h[8]; } m;
+  m.u = meta;
+  halfx8 c;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const float o = __builtin_fmaf(8.f, static_cast<float>(m.h[g]), static_cast<float>(m.h[4 + g]));
+    c[g] = static_cast<_Float16>(o);
+    c[4 + g] = static_cast<_Float16>(o - static_cast<float>(c[g]));
+  }
+  return c;
+}
+// K metadata into LDS (kKMeta bytes of the wavefront's), of slots from `rows` on zeros: a slot's centres, then the scales, [group][slot].
 constexpr int kKMeta = 1024 + 512;
 __device__ __forceinline__ void put_k_meta(uint8_t* lds, const Side4& k, int rows) {
   const int lane = threadIdx.x & 63;
   const bool there = lane < rows;
   const uint4 m = make_uint4(there ? k.meta.x : 0u, there ? k.meta.y : 0u, there ? k.meta.z : 0u, there ? k.meta.w : 0u);
-  *reinterpret_cast<uint4*>(lds + 16 * lane) = m;
+  *reinterpret_cast<halfx8*>(lds + 16 * lane) = centres(m);
   uint16_t* scales = reinterpret_cast<uint16_t*>(lds + 1024) + lane;
   scales[0] = static_cast<uint16_t>(m.x);
   scales[64] = static_cast<uint16_t>(m.x >> 16);
@@ -150,48 +148,62 @@ __device__ __forceinline__ void put_v_meta(uint8_t* lds, const Side4& v, int row
   *reinterpret_cast<uint4*>(lds + 16 * lane) = m.u;
 }
 
-// the four words' fields at bits `at` of both halves as numbers: mask and what stands above them
-template <int SHIFT>
-__device__ __forceinline__ uint32_t shifted(uint32_t w) {
-  if constexpr (SHIFT > 0) return w >> SHIFT;
-  else return w << -SHIFT;
+// Fields f (0 .. 3) of a word's halves, codes, less 8 as fp16: 1024 + code, or 64 + code where the field is four bits up, are a mask and an or.
+__device__ __forceinline__ halfx2 less_8(uint32_t word, int f) {
+  union { uint32_t u; halfx2 h; } x;
+  const uint32_t v = f < 2 ? word : word >> 8;
+  if (f & 1) {
+    x.u = (v & 0x00F000F0u) | 0x54005400u;
+    return x.h - halfx2{72, 72};
+  }
+  x.u = (v & 0x000F000Fu) | 0x64006400u;
+  return x.h - halfx2{1032, 1032};
 }
+
+// A lane's words of product x, and of them what a product's operand of a group's half is: fields 2 s and 2 s + 1 of two words.
+struct Words4 {
+  uint32_t w[2][4][2];
+  __device__ __forceinline__ Words4(const Side4& k) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      // word pair (2 half, 2 half + 1) of the slots of product 0, and of product 1
+      uint32_t a = k.codes[g].x, b = k.codes[g].y, c = k.codes[g].z, d = k.codes[g].w;
+      asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(c));
+      asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(b), "+v"(d));
+      w[0][g][0] = a;
+      w[0][g][1] = b;
+      w[1][g][0] = c;
+      w[1][g][1] = d;
+    }
+  }
+  __device__ __forceinline__ halfx8 operand(int x, int g, int s) const {
+    union { halfx2 p[4]; halfx8 h; } op;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      op.p[j] = less_8(w[x][g][j], 2 * s);
+      op.p[2 + j] = less_8(w[x][g][j], 2 * s + 1);
+    }
+    return op.h;
+  }
+};
 
 // Products of the 64 slots, register i of s[x] of lane (half, .): slot 32 half + 16 x + i; over the query's unit.
 __device__ __forceinline__ void scores4(const Side4& k, const uint8_t* k_meta, const Query4& q, floatx16 (&s)[2]) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-  // word pair (2 half, 2 half + 1) of the slots of product 0, and of product 1
-  uint32_t w[2][4][2];
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    uint32_t a = k.codes[g].x, b = k.codes[g].y, c = k.codes[g].z, d = k.codes[g].w;
-    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(c));
-    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(b), "+v"(d));
-    w[0][g][0] = a;
-    w[0][g][1] = b;
-    w[1][g][0] = c;
-    w[1][g][1] = d;
-  }
+  const Words4 words(k);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     s[x] = product(*reinterpret_cast<const halfx8*>(k_meta + 16 * slot_of_row(x, l32)), q.sums, floatx16{});
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      union { uint32_t u[4]; bf16x8 b; } op[2];
-      constexpr uint32_t kMask = 0x00780078u, kOne = 0x3F803F80u;          // bf16 1 + code / 16
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        op[0].u[j] = (shifted<-3>(w[x][g][j]) & kMask) | kOne;
-        op[0].u[2 + j] = (shifted<1>(w[x][g][j]) & kMask) | kOne;
-        op[1].u[j] = (shifted<5>(w[x][g][j]) & kMask) | kOne;
-        op[1].u[2 + j] = (shifted<9>(w[x][g][j]) & kMask) | kOne;
-      }
-      floatx16 sums = product(op[0].b, q.op[2 * g], floatx16{});
-      sums = product(op[1].b, q.op[2 * g + 1], sums);
+      floatx16 sums = product(words.operand(x, g, 0), q.op[2 * g], floatx16{});
+      sums = product(words.operand(x, g, 1), q.op[2 * g + 1], sums);
       const halfx8* sc = reinterpret_cast<const halfx8*>(k_meta + 1024 + 128 * g + 2 * (32 * half + 16 * x));
       const halfx8 sc0 = sc[0], sc1 = sc[1];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[x][i] = __builtin_fmaf(static_cast<float>(i < 8 ? sc0[i & 7] : sc1[i & 7]), sums[i], s[x][i]);
+      for (int i = 0; i < 16; ++i)
+        s[x][i] = __builtin_fmaf(static_cast<float>(i < 8 ? sc0[i & 7] : sc1[i & 7]), sums[i], s[x][i]);
+      if (g & 1) __builtin_amdgcn_sched_barrier(0);             // (all groups side by side do not fit the registers)
     }
   }
 }
@@ -201,16 +213,13 @@ template <int F>
 __device__ __forceinline__ halfx8 values4(const uint4& codes, const uint8_t* v_meta, int group) {
   const int half = (threadIdx.x & 63) >> 5;
   const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
-  union { uint32_t u[4]; halfx2 h[4]; halfx8 v; } x;
-  constexpr uint32_t kMask = 0x03C003C0u, kSixteen = 0x4C004C00u;          // fp16 16 + code
-#pragma unroll
-  for (int j = 0; j < 4; ++j) x.u[j] = (shifted<4 * F - 6>(w[j]) & kMask) | kSixteen;
+  union { halfx2 h[4]; halfx8 v; } x;
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     union { uint4 u; halfx2 h[4]; } m;
     m.u = *reinterpret_cast<const uint4*>(v_meta + 64 * (8 * half + 4 * p + F) + 16 * group);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) x.h[2 * p + j] = __builtin_elementwise_fma(x.h[2 * p + j] - halfx2{24, 24}, m.h[j], m.h[2 + j]);
+    for (int j = 0; j < 2; ++j) x.h[2 * p + j] = __builtin_elementwise_fma(less_8(w[2 * p + j], F), m.h[j], m.h[2 + j]);
   }
   return x.v;
 }

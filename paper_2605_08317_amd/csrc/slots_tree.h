@@ -58,8 +58,14 @@ struct AcceptArgs {
   const int32_t* path;                  // [batch][m]
   const float* stats;                   // [batch][n][hq][2]
   int32_t* slot;                        // [batch][hkv][m], or null
+  void* leasts;                         // [items][segments of kLeastSlots slots]: kLeastBytes each
+  float* begins;                        // [items][kMostDrafted]: what a token's weight begins with
   int32_t items, n, m, pieces;
 };
+constexpr int kLeastSlots = 32, kLeastBytes = 16;
+inline size_t accept_workspace_bytes(int64_t items, int capacity) {
+  return static_cast<size_t>(items) * ((static_cast<size_t>(capacity) + kLeastSlots - 1) / kLeastSlots * kLeastBytes + kMostDrafted * sizeof(float));
+}
 
 hipError_t launch_accept(const AcceptArgs& a, int bits, hipStream_t st);
 hipError_t launch_tree(const TreeArgs& a, int bits, hipStream_t st);

@@ -12,8 +12,8 @@ def attn(c, n=4, q=16, k=16, v=16, parent=4, counts=None, out=16, stats=None, ws
     return b.lib.rdkv_slots_tree_attn(ctypes.byref(c), n, q, k, v, parent, counts, out, stats, ws, ws_bytes, None)
 
 
-def accept(c, n=4, m=3, q=16, k=16, v=16, path=4, stats=8, slot=None):
-    return b.lib.rdkv_slots_accept(ctypes.byref(c), n, m, q, k, v, path, stats, slot, None)
+def accept(c, n=4, m=3, q=16, k=16, v=16, path=4, stats=8, slot=None, ws=16, ws_bytes=1 << 40):
+    return b.lib.rdkv_slots_accept(ctypes.byref(c), n, m, q, k, v, path, stats, slot, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw, status", [
@@ -22,7 +22,7 @@ def accept(c, n=4, m=3, q=16, k=16, v=16, path=4, stats=8, slot=None):
 def test_a_bad_struct_is_refused(kw, status):
     assert attn(struct(**kw)) == status and accept(struct(**kw)) == status
     assert b.lib.rdkv_slots_tree_attn(None, 4, 16, 16, 16, 4, None, 16, None, 16, 0, None) == INVALID
-    assert b.lib.rdkv_slots_accept(None, 4, 3, 16, 16, 16, 4, 8, None, None) == INVALID
+    assert b.lib.rdkv_slots_accept(None, 4, 3, 16, 16, 16, 4, 8, None, 16, 1 << 40, None) == INVALID
 
 
 def test_bad_arguments_are_refused():
@@ -43,6 +43,10 @@ def test_workspaces():
     need = b.lib.rdkv_slots_tree_workspace_bytes(r(large), 8)
     assert need > 0 and need % 16 == 0
     assert attn(large, n=8, ws=16, ws_bytes=need - 1) == INVALID and attn(large, n=8, ws=None) == INVALID and attn(large, n=8, ws=24, ws_bytes=need) == INVALID
+    need = b.lib.rdkv_slots_accept_workspace_bytes(r(large))
+    assert need > 0 and need % 16 == 0 and b.lib.rdkv_slots_accept_workspace_bytes(r(struct(hq=7))) == 0
+    for ws, n in ((16, need - 1), (None, need), (24, need)):
+        assert accept(large, ws=ws, ws_bytes=n) == INVALID
     assert b.lib.rdkv_slots_tree_workspace_bytes(r(struct(hq=7)), 8) == 0 and b.lib.rdkv_slots_tree_workspace_bytes(None, 8) == 0
 
 
@@ -66,7 +70,7 @@ def test_the_binding_refuses_tensors_the_library_would_misread():
             b.rdkv_slots_tree_attn(s, **dict(good, **bad))
     good = dict(q=q, k_draft=k, v_draft=k, path=path, stats=stats)
     for bad in (dict(q=q.float()), dict(k_draft=k[0]), dict(v_draft=k[:, :4]), dict(path=path.long()), dict(path=path[0]), dict(path=path[:1]), dict(stats=stats[:, :4]),
-                dict(stats=stats.double()), dict(slot=torch.zeros(2, 2, 4, dtype=i32)), dict(slot=torch.zeros(2, 2, 3))):
+                dict(stats=stats.double()), dict(slot=torch.zeros(2, 2, 4, dtype=i32)), dict(slot=torch.zeros(2, 2, 3)), dict(workspace=torch.zeros(4096))):
         with pytest.raises(ValueError):
             b.rdkv_slots_accept(s, **dict(good, **bad))
     for call in (lambda: b.rdkv_slots_tree_attn(s, q, k, k, parent), lambda: b.rdkv_slots_accept(s, q, k, k, path, stats)):
