@@ -49,24 +49,46 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
 }
 
+// Loads that the compiler knows of are waited for here and not at their first use, in a loop whose copies to LDS it does not know of: there it would
+// wait for those too.
+__device__ __forceinline__ void arrived(bf16x8& v) { asm volatile("" : "+v"(v)); }
+
 __device__ __forceinline__ int k_piece(int row, int piece) { return piece ^ (row & 15); }
 __device__ __forceinline__ int v_piece(int row, int piece) { return piece ^ (4 * (row & 3)) ^ (2 * ((row >> 2) & 1)); }
 
-// keys l32 of a step as the A side of product kb (channels 16 kb ..)
-__device__ __forceinline__ bf16x8 read_k(const uint8_t* step, int kb) {
+// Where a lane reads in an image at LDS address 0, whose pieces differ between products by exchanged bits alone: images begin at multiples of 256
+// bytes, so that a product's address is the lane's, a few bits flipped, and a constant.
+__device__ __forceinline__ uint32_t k_lane() {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-  return *reinterpret_cast<const bf16x8*>(step + l32 * kRowBytes + 16 * k_piece(l32, 2 * kb + half));
+  return l32 * kRowBytes + 16 * k_piece(l32, half);
 }
-// channel 32 t + l32 of the eight keys 16 s + 4 half + 0..3 and + 8..11 of a step, as the A side of P V
-__device__ __forceinline__ bf16x8 read_v(const uint8_t* step, int t, int s) {
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int r = 16 * s + 4 * half + ((lane & 15) >> 2), byte = 64 * t + 2 * (lane & 16) + 8 * (lane & 3);
+__device__ __forceinline__ uint32_t v_lane() {
+  const int lane = threadIdx.x & 63, row = 4 * (lane >> 5) + ((lane & 15) >> 2);
+  return row * kRowBytes + 16 * v_piece(row, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+}
+template <class T>
+__device__ __forceinline__ T from_lds(uint32_t at) {
+  typedef const __attribute__((address_space(3))) T* Lds;
+  return *(Lds)(uintptr_t)at;
+}
+// keys l32 of a step as the A side of product kb (channels 16 kb ..); at: the image's first row of the step, plus k_lane()
+__device__ __forceinline__ bf16x8 read_k(uint32_t at, int kb, int step = 0) { return from_lds<bf16x8>((at ^ (32 * kb)) + step * (kStepKeys * kRowBytes)); }
+// channel 32 t + l32 of the eight keys 16 s + 4 half + 0..3 and + 8..11 of a step, as the A side of P V; at: plus v_lane()
+__device__ __forceinline__ bf16x8 read_v(uint32_t at, int t, int s, int step = 0) {
   typedef __attribute__((address_space(3))) shortx4* Lds;
-  const auto at = [&](int row) { return (Lds)(uintptr_t)(lds_address(step) + row * kRowBytes + 16 * v_piece(row, byte >> 4) + (byte & 15)); };
+  const uint32_t first = (at ^ (64 * t)) + (16 * s + kStepKeys * step) * kRowBytes;
   union { shortx4 s[2]; bf16x8 b; } v;
-  v.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(r));
-  v.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(r + 8));
+  v.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(uintptr_t)first);
+  v.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(uintptr_t)(first + 8 * kRowBytes));
   return v.b;
+}
+// two numbers as bf16, nearest
+__device__ __forceinline__ uint32_t pair_bf16(float a, float b) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 Pair;
+  Pair v;
+  v[0] = static_cast<__bf16>(a);
+  v[1] = static_cast<__bf16>(b);
+  return __builtin_bit_cast(uint32_t, v);
 }
 // eight numbers as bf16, nearest
 __device__ __forceinline__ bf16x8 to_bf16(const float* p) {

@@ -66,7 +66,7 @@ constexpr int kSlotLds = kSegment * kRowBytes + 512; // bf16: a segment's keys, 
 
 template <int BITS, bool GENERAL, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArgs a) {
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(256) uint8_t smem[];
   __shared__ RowTable s_row;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
   // the first workgroups have an item's own tokens, the others a piece of its slots
@@ -149,10 +149,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
   };
   const auto operand16 = [&](int b, int k) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8*>(smem + ((b * 9 + k) * 64 + lane) * 16); };
   const auto operand4 = [&](int b, int k) __attribute__((always_inline)) { return *reinterpret_cast<const halfx8*>(smem + ((b * 9 + k) * 64 + lane) * 16); };
-  const auto products16 = [&](const uint8_t* keys, int b) __attribute__((always_inline)) {
+  const auto products16 = [&](uint32_t keys, int b) __attribute__((always_inline)) {
     floatx16 s = {};
 #pragma unroll
-    for (int kb = 0; kb < 8; ++kb) s = product(operand16(b, kb), read_k(keys, kb), s);
+    for (int kb = 0; kb < 8; ++kb) s = product(operand16(b, kb), read_k(keys + k_lane(), kb), s);
     return s;
   };
 
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
     float sum = 0.f;
     for (int r0 = 0; r0 < rows; r0 += kRows) {
       rows_in(Query16{}, r0);
-      if (wave < 2) sum += given(std::true_type{}, r0, next + token, [&](int b) __attribute__((always_inline)) { return products16(keys, b); });
+      if (wave < 2) sum += given(std::true_type{}, r0, next + token, [&](int b) __attribute__((always_inline)) { return products16(lds_address(keys), b); });
     }
     if (wave < 2 && half == 0 && token < count) a.begins[static_cast<int64_t>(item) * kMostDrafted + token] = sum;
     return;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
           const uint8_t* keys = mine + buffer * kSlotLds;
           const float before = reinterpret_cast<const float*>(keys + kSegment * kRowBytes)[l32];
           const int place = reinterpret_cast<const int*>(keys + kSegment * kRowBytes + 256)[l32], slot = u * kSegment + l32;
-          const float sum = given(std::false_type{}, r0, place, [&](int b) __attribute__((always_inline)) { return products16(keys, b); });
+          const float sum = given(std::false_type{}, r0, place, [&](int b) __attribute__((always_inline)) { return products16(lds0 + buffer * kSlotLds, b); });
           const Least l = put(slot, before, place, sum, keep, last_pass, std::integral_constant<int, 31>{});
           if (full && last_pass && lane == 0) leasts[u] = l;
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

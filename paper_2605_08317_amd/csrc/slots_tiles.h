@@ -41,6 +41,8 @@ struct Query16 {
     const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int kb = 0; kb < 8; ++kb) op[kb] = *reinterpret_cast<const bf16x8*>(q + 16 * kb + 8 * half);
+#pragma unroll
+    for (int kb = 0; kb < 8; ++kb) arrived(op[kb]);
     unit = 1.f;
   }
 };
@@ -83,10 +85,11 @@ struct Query4 {
 };
 
 // bf16 rows in LDS: products of 32 slots, register i of lane (half, .): slot 8 (i / 4) + 4 half + i % 4 of the step.
-__device__ __forceinline__ floatx16 scores16(const uint8_t* step, const Query16& q) {
+// at: LDS address of the image, plus k_lane()
+__device__ __forceinline__ floatx16 scores16(uint32_t at, int step, const Query16& q) {
   floatx16 s = {};
 #pragma unroll
-  for (int kb = 0; kb < 8; ++kb) s = product(read_k(step, kb), q.op[kb], s);
+  for (int kb = 0; kb < 8; ++kb) s = product(read_k(at, kb, step), q.op[kb], s);
   return s;
 }
 

@@ -94,7 +94,7 @@ __device__ __forceinline__ void add_values(const Op (&p)[STEPS], const float* pr
 
 // bf16 rows in LDS, STEPS x 32 of them, into a row's result.  x: their scores (registers 16 step + i), -inf where hidden
 template <int STEPS, bool PARTED>
-__device__ __forceinline__ void add_rows16(const float (&x)[16 * STEPS], float factor, const uint8_t* vt, float shift, Out& r) {
+__device__ __forceinline__ void add_rows16(const float (&x)[16 * STEPS], float factor, uint32_t vt, float shift, Out& r) {
   float p[16 * STEPS];
   softmax(x, factor, shift, r, p);
   bf16x8 op[2 * STEPS];
@@ -102,7 +102,7 @@ __device__ __forceinline__ void add_rows16(const float (&x)[16 * STEPS], float f
   for (int k = 0; k < 2 * STEPS; ++k) op[k] = to_bf16(p + 8 * k);
 #pragma unroll
   for (int t = 0; t < 4; ++t)
-    add_values<PARTED>(op, p, [&](int k) __attribute__((always_inline)) { return read_v(vt + (k >> 1) * kStepKeys * kRowBytes, t, k & 1); }, r.o[t]);
+    add_values<PARTED>(op, p, [&](int k) __attribute__((always_inline)) { return read_v(vt, t, k & 1, k >> 1); }, r.o[t]);
 }
 
 // What scores are made of products with.
@@ -164,7 +164,7 @@ constexpr int kMetaLds = kWaves * (kKMeta + 1024 + 256);
 
 template <int BITS, int WR, bool GENERAL>
 __global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(TreeArgs a) {
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(256) uint8_t smem[];
   __shared__ uint64_t s_sees[kTokens];
   __shared__ int s_depth[kTokens], s_parent[kTokens];
   __shared__ float s_ml[kWaves][32][4];
@@ -261,13 +261,12 @@ __global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(Tree
         fetch(it + kBuffers - 1);
         const int buffer = it % kBuffers, mine = ws * kMine, left = end - begin - it * kSlots - mine - 4 * half;
         if (left + 4 * half <= 0) continue;
-        const uint8_t* kt = smem + buffer * (kSlots * 2 * kRowBytes) + mine * kRowBytes;
-        const uint8_t* vt = kt + kSlots * kRowBytes;
+        const uint32_t first = lds0 + buffer * (kSlots * 2 * kRowBytes) + mine * kRowBytes, kt = first + k_lane(), vt = first + kSlots * kRowBytes + v_lane();
         const int4* where = reinterpret_cast<const int4*>(s_pos + (wave * kBuffers + buffer) * 256);
         float x[16 * kStepsN];
 #pragma unroll
         for (int k = 0; k < kStepsN; ++k) {
-          const floatx16 s = scores16(kt + k * kStepKeys * kRowBytes, query);
+          const floatx16 s = scores16(kt, k, query);
 #pragma unroll
           for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
         }
@@ -352,7 +351,7 @@ __global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(Tree
       float x[32];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const floatx16 s = scores16(smem + k * kStepKeys * kRowBytes, q16);
+        const floatx16 s = scores16(lds0 + k_lane(), k, q16);
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
       }
@@ -365,7 +364,7 @@ __global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(Tree
 #pragma unroll
         for (int j = 0; j < 4; ++j) at[j] = next + s_depth[min(token(4 * k + j), n - 1)];
       }, [&](int i) __attribute__((always_inline)) { return (row.sees >> token(i) & 1) == 0; });
-      add_rows16<2, true>(x, sc.factor, smem + kTokens * kRowBytes, BITS == 4 ? kTopHalf : 0.f, r);
+      add_rows16<2, true>(x, sc.factor, lds0 + kTokens * kRowBytes + v_lane(), BITS == 4 ? kTopHalf : 0.f, r);
     }
   }
 
