@@ -67,7 +67,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
     for (int kb = 0; kb < 8; ++kb) arrived(q_op[kb]);
   }
   const float slope = GENERAL && a.slopes ? a.slopes[head] : 0.f, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
-  constexpr float kFactor = GENERAL ? kLog2e : kRootLog2e;     // what makes scores, or products, exponents of 2
+  // What makes the numbers that are kept (products, scores over the cap, or with biases scores) scores, and those exponents of 2.
+  const float units = GENERAL && a.cap > 0.f ? a.cap : kRoot;
+  const float factor = !GENERAL ? kRootLog2e : a.slopes ? kLog2e : a.cap > 0.f ? a.cap * kLog2e : kRootLog2e;
 
   floatx16 o[4];
   float m, l;
@@ -90,14 +92,16 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
   const auto finish = [&](int it, floatx16 (&s)[2]) __attribute__((always_inline)) {
     const int key0 = key_of(it), back = row - key0 - 4 * half;           // positions from key 4 half of the tile to the row
     if constexpr (GENERAL) {
+      float v[32];
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int i = 0; i < 32; ++i) v[i] = s[i >> 4][i & 15];
+      if (a.cap > 0.f) tanh_all(v, kRoot * inv_cap);
+      if (a.slopes) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[x][i] *= kRoot;
-          if (a.cap > 0.f) s[x][i] = capped(s[x][i], a.cap, inv_cap);
-          if (a.slopes) s[x][i] = __builtin_fmaf(-slope, static_cast<float>(back - key(x, i)), s[x][i]);
-        }
+        for (int i = 0; i < 32; ++i) v[i] = __builtin_fmaf(v[i], units, -slope * static_cast<float>(back - key(i >> 4, i & 15)));
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = v[i];
     }
     if (key0 + kKeys - 1 > r0) {
 #pragma unroll
@@ -122,8 +126,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
   };
   // the row's reference, if its largest score is past it
   const auto refer = [&](float top, bool any) __attribute__((always_inline)) {
-    if (__any(any ? top > m : (top - m) * kFactor > kSlack)) {
-      const float now = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f((m - now) * kFactor);
+    if (__any(any ? top > m : (top - m) * factor > kSlack)) {
+      const float now = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f((m - now) * factor);
       m = now;
       l *= alpha;
 #pragma unroll
@@ -145,12 +149,12 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
   const auto position = [&](auto more, int it, floatx16 (&s)[2], floatx16 (&next)[2]) __attribute__((always_inline)) {
     constexpr bool kMore = decltype(more)::value;
     refer(largest(s), false);
-    const float ref = -m * kFactor;
+    const float ref = -m * factor;
     const uint32_t kt = k_first + buffer_of(it + 1), vt = v_first + buffer_of(it);
     union { uint32_t u[16]; bf16x8 op[4]; } p;
     float sums[2] = {0.f, 0.f}, before = 0.f;
     const auto make = [&](int i) __attribute__((always_inline)) {        // in order
-      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], kFactor, ref));
+      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], factor, ref));
       sums[i & 1] += e;
       if (i & 1) p.u[i >> 1] = pair_bf16(before, e);
       before = e;
@@ -233,7 +237,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
       float p[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
-        p[i] = __builtin_amdgcn_exp2f((s[i >> 4][i & 15] - m) * kFactor);
+        p[i] = __builtin_amdgcn_exp2f((s[i >> 4][i & 15] - m) * factor);
         l += p[i];
       }
       const uint32_t vt = v_first + buffer_of(it);
@@ -291,7 +295,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
       asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(w.u[1]), "+v"(w.u[3]));
       *reinterpret_cast<uint4*>(out + 32 * t + 16 * c) = make_uint4(w.u[0], w.u[1], w.u[2], w.u[3]);
     }
-  if (a.lse && half == 0) a.lse[token0 * a.hq + static_cast<int64_t>(head) * T + row] = total == 0.f ? -INFINITY : __builtin_fmaf(m * kFactor, kLn2, __logf(total));
+  if (a.lse && half == 0) a.lse[token0 * a.hq + static_cast<int64_t>(head) * T + row] = total == 0.f ? -INFINITY : __builtin_fmaf(m * factor, kLn2, __logf(total));
 }
 
 template <int NW, bool GENERAL>
@@ -307,7 +311,7 @@ hipError_t start(const Args& a, int longest, hipStream_t st) {
 }  // namespace
 
 hipError_t launch(const Args& a, int longest, hipStream_t st) {
-  const bool general = a.cap > 0.f || a.slopes;
+  const bool general = a.cap > 0.f || a.slopes;      // (a window takes no scores of its own)
   const int64_t large = static_cast<int64_t>(longest + 255) / 256 * a.n_seqs * a.hq;
   if (large >= 512) return general ? start<8, true>(a, longest, st) : start<8, false>(a, longest, st);
   return general ? start<4, true>(a, longest, st) : start<4, false>(a, longest, st);

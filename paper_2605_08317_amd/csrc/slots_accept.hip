@@ -126,22 +126,45 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
         const float4 most = *reinterpret_cast<const float4*>(s_row.most + r), share = *reinterpret_cast<const float4*>(s_row.share + r);
         const float4 natural = *reinterpret_cast<const float4*>(s_row.natural + r);
         const float ms[4] = {most.x, most.y, most.z, most.w}, sh[4] = {share.x, share.y, share.z, share.w}, na[4] = {natural.x, natural.y, natural.z, natural.w};
+        float e[4];
+        if (scored) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float e = __builtin_fmaf(s[4 * k + j], na[j], -ms[j]);
-          if constexpr (GENERAL || decltype(own)::value) {
-            const int away = s_row.at[r + j] - place;
-            if (scored) {
-              float v = s[4 * k + j] * na[j];
-              if (a.s.cap > 0.f) v = capped(v, a.s.cap, inv_cap);
-              if (a.s.slopes) v = __builtin_fmaf(-s_row.slope[r + j], static_cast<float>(away), v);
-              e = v - ms[j];
-            }
-            if (a.s.window > 0 && away >= a.s.window && place >= a.s.sinks) e = -INFINITY;
-            if (decltype(own)::value && away < 0) e = -INFINITY;
+          for (int j = 0; j < 4; ++j) e[j] = s[4 * k + j] * na[j];
+          if (a.s.cap > 0.f) {
+            tanh_all(e, inv_cap);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] *= a.s.cap;
           }
-          sum = __builtin_fmaf(__builtin_amdgcn_exp2f(e * kLog2e), sh[j], sum);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) e[j] = __builtin_fmaf(s[4 * k + j], na[j], -ms[j]);
         }
+        if constexpr (GENERAL || decltype(own)::value) {
+          const int4 ats = *reinterpret_cast<const int4*>(s_row.at + r);
+          const int away[4] = {ats.x - place, ats.y - place, ats.z - place, ats.w - place};
+          if (a.s.slopes) {
+            const float4 slope = *reinterpret_cast<const float4*>(s_row.slope + r);
+            const float sl[4] = {slope.x, slope.y, slope.z, slope.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = __builtin_fmaf(-sl[j], static_cast<float>(away[j]), e[j]);
+          }
+          if (scored) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] -= ms[j];
+          }
+          if (a.s.window > 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (away[j] >= a.s.window && place >= a.s.sinks) e[j] = -INFINITY;
+          }
+          if constexpr (decltype(own)::value) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (away[j] < 0) e[j] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum = __builtin_fmaf(__builtin_amdgcn_exp2f(e[j] * kLog2e), sh[j], sum);
         if constexpr (GENERAL) __builtin_amdgcn_sched_barrier(0);        // (sixteen side by side do not fit the registers)
       }
     }

@@ -244,6 +244,7 @@ rdkv_status rdkv_slots_tree_attn(const rdkv_slots* s, int32_t n, const void* q, 
   a.items = s->batch * s->hkv;
   a.n = n;
   const slots::TreePlan plan = slots::plan_tree(a.items, n * a.s.g, s->capacity, s->bits);
+  a.wide = plan.wide;
   a.row_groups = plan.row_groups;
   a.pieces = plan.pieces;
   a.part_acc = static_cast<float*>(workspace);

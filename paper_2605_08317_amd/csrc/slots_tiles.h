@@ -136,19 +136,25 @@ __device__ __forceinline__ void put_k_meta(uint8_t* lds, const Side4& k, int row
   scales[128] = static_cast<uint16_t>(m.y);
   scales[192] = static_cast<uint16_t>(m.y >> 16);
 }
-// V metadata: scales, and offsets plus 8 scales; of slots from `rows` on zeros.
-__device__ __forceinline__ void put_v_meta(uint8_t* lds, const Side4& v, int rows) {
+// V metadata: scales, and offsets plus 8 scales; of slots from `rows` on zeros.  FINITE: of those that are not finite as well; the lanes that had such.
+template <bool FINITE>
+__device__ __forceinline__ uint64_t put_v_meta(uint8_t* lds, const Side4& v, int rows) {
   const int lane = threadIdx.x & 63, first = 4 * (lane >> 2);
   union { uint4 u; _Float16 h[8]; } m;
   m.u = v.meta;
+  bool odd = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const bool there = first + i < rows;
     const float s = there ? static_cast<float>(m.h[i]) : 0.f, o = there ? static_cast<float>(m.h[4 + i]) : 0.f;
-    m.h[i] = static_cast<_Float16>(s);
-    m.h[4 + i] = static_cast<_Float16>(__builtin_fmaf(8.f, s, o));
+    const _Float16 centre = static_cast<_Float16>(__builtin_fmaf(8.f, s, o));
+    const bool fine = !FINITE || (fabsf(s) < INFINITY && fabsf(static_cast<float>(centre)) < INFINITY);
+    odd = odd || !fine;
+    m.h[i] = static_cast<_Float16>(fine ? s : 0.f);
+    m.h[4 + i] = fine ? centre : static_cast<_Float16>(0.f);
   }
   *reinterpret_cast<uint4*>(lds + 16 * lane) = m.u;
+  return FINITE ? __ballot(odd) : 0;
 }
 
 // Fields f (0 .. 3) of a word's halves, codes, less 8 as fp16: 1024 + code, or 64 + code where the field is four bits up, are a mask and an or.
@@ -226,30 +232,6 @@ __device__ __forceinline__ halfx8 values4(const uint4& codes, const uint8_t* v_m
   }
   return x.v;
 }
-
-// `part` of attn_tiles.h for fp16
-struct Parted4 {
-  halfx8 finite, up, down;
-  bool any;
-};
-__device__ __forceinline__ Parted4 part(halfx8 x) {
-  union { halfx8 b; uint32_t u[4]; } v, f, up, down;
-  v.b = x;
-  uint32_t any = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t t = ((v.u[i] & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
-    const uint32_t odd = (t >> 15) * 0xFFFFu;
-    const uint32_t nan = ((((v.u[i] & 0x03FF03FFu) + 0x03FF03FFu) & 0x04000400u) >> 10) * 0xFFFFu;
-    const uint32_t neg = ((v.u[i] >> 15) & 0x00010001u) * 0xFFFFu;
-    f.u[i] = v.u[i] & ~odd;
-    up.u[i] = odd & (nan | ~neg) & 0x3C003C00u;
-    down.u[i] = odd & (nan | neg) & 0x3C003C00u;
-    any |= odd;
-  }
-  return {f.b, up.b, down.b, any != 0};
-}
-using attn::part;
 
 __device__ __forceinline__ halfx8 to_half(const float* p) {
   halfx8 v;

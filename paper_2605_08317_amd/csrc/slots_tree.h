@@ -20,7 +20,8 @@ struct TreeArgs {
   float* stats;                         // [batch][n][hq][2], or null
   float* part_acc;                      // [item][row group][piece][rows of a group][128]
   float* part_ml;                       // the same rows: [4]
-  int32_t items, n, row_groups, pieces;
+  int32_t items, n;
+  int32_t wide, row_groups, pieces;     // plan_tree, as the workspace's size has it
 };
 
 // wide: wavefronts of a workgroup that share out rows, 32 each; the others share out slots.  Pieces of an item's slots.
@@ -31,10 +32,10 @@ struct TreePlan {
 };
 inline TreePlan plan_tree(int64_t items, int rows, int capacity, int bits) {
   TreePlan p;
-  p.wide = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  p.wide = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || bits == 4 ? 4 : 8;
   p.row_groups = (rows + 32 * p.wide - 1) / (32 * p.wide);
   const int64_t groups = items * p.row_groups, card = bits == 16 ? 256 : 512;
-  const int64_t least = 2 * (4 / p.wide);                     // tiles of a piece
+  const int64_t least = 2 * std::max(4 / p.wide, 1);          // tiles of a piece
   const int64_t most = (static_cast<int64_t>(capacity) + kTileRows - 1) / kTileRows / least;
   p.pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min(most, card / std::max<int64_t>(groups, 1))));
   return p;

@@ -1,8 +1,7 @@
 // Slot caches: attention of a tree of drafted tokens.
 //
-// A workgroup of four wavefronts has up to 128 query rows (token, head) of an item and a piece of its slots.  With 32 rows or fewer the wavefronts
-// share out the slots, with 64 they are two by two, with more they share out the rows; results of slots are joined in LDS.  The last piece of an item
-// has the drafted tokens' own keys and values, bf16 rows whatever the cache holds, behind its slots.
+// A workgroup of four or eight wavefronts has up to 128 (bf16: 256) query rows (token, head) of an item and a piece of its slots.  Its wavefronts share out
+// the rows, 32 each, and where these are fewer than the wavefronts the slots as well; results of slots are joined in LDS.  The last piece of an item has the drafted tokens' own keys and values, bf16 rows whatever the cache holds, behind its slots.
 #include <algorithm>
 
 #include "slots_tiles.h"
@@ -15,7 +14,6 @@ namespace {
 
 constexpr float kSlack = 4.f;             // what exponents may exceed a row's reference by before it moves
 constexpr float kTopHalf = 11.f;          // fp16 probabilities are over 2^-11: with the slack below fp16's largest, and bits down to 2^-35
-constexpr int kThreads = 256, kWaves = 4;
 constexpr int kTokens = 64;
 
 // What a lane knows of its query row.
@@ -118,16 +116,13 @@ struct Scoring {
 template <bool GENERAL, int N, class Four, class Hide>
 __device__ __forceinline__ void to_scores(const Scoring& sc, const Row& row, float (&x)[N], bool some, Four four, Hide hide) {
   if constexpr (GENERAL) {
-    if (sc.scored) {
+    if (sc.cap > 0.f) {
+      tanh_all(x, sc.natural * sc.inv_cap);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] *= sc.cap;
+    } else if (sc.biased) {
 #pragma unroll
       for (int i = 0; i < N; ++i) x[i] *= sc.natural;
-    }
-    if (sc.cap > 0.f) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        x[i] = capped(x[i], sc.cap, sc.inv_cap);
-        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (all of them side by side do not fit the registers)
-      }
     }
     if (sc.biased || sc.window > 0) {
 #pragma unroll
@@ -150,25 +145,65 @@ __device__ __forceinline__ void to_scores(const Scoring& sc, const Row& row, flo
   }
 }
 
+// Wavefronts of a workgroup.  bf16 rows take a compute unit's LDS, eight wavefronts share them: two a SIMD, one's products beside the other's
+// exponentials.  With 32 query rows or fewer eight shares of slots would be a tile more than half of the LDS holds.
+template <int BITS, int WR>
+constexpr int kWaves = BITS == 4 || WR == 1 ? 4 : 8;
 template <int WR>
-constexpr int kSteps16 = WR == 1 ? 1 : WR == 2 ? 1 : 2;         // 32-slot steps of a wavefront's tile
+constexpr int kSteps16 = WR <= 2 ? 1 : 2;                       // 32-slot steps of a wavefront's tile
 template <int WR>
-constexpr int kStage = 32 * kSteps16<WR> * (kWaves / WR);       // slots of a stage
+constexpr int kStage = 32 * kSteps16<WR> * (kWaves<16, WR> / WR);    // slots of a stage
 template <int WR>
 constexpr int kStages = 256 / kStage<WR>;                       // buffers
 constexpr int kStageLds = 256 * 2 * kRowBytes;                  // of all of them: 128 KiB
-constexpr int kPosLds = kWaves * 4 * 64 * 4;                    // positions of the wavefronts' tiles, up to four buffers
+constexpr int kPosLds = 8 * 4 * 64 * 4;                         // positions of the wavefronts' tiles, up to four buffers
 constexpr int kDraftLds = kTokens * 2 * kRowBytes;
-constexpr int kJoinLds = kWaves * 4 * 16 * 64 * 4;              // the wavefronts' results
-constexpr int kMetaLds = kWaves * (kKMeta + 1024 + 256);
+constexpr int kJoinLds = 4 * 4 * 16 * 64 * 4;                   // four wavefronts' results
+constexpr int kMetaLds = kKMeta + 1024 + 256;                   // of a wavefront
+
+// Values of a 4-bit tile that are not finite, to the rows that give their slots something.  odd: lanes 4 (slot / 4) + group whose metadata are not; lds:
+// 8 KiB of the wavefront's; p: probabilities, register i of slot 32 half + i.
+__device__ __forceinline__ void add_odd(uint64_t odd, const uint8_t* tile, int rows, uint8_t* lds, const float (&p)[32], Out& r) {
+  const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+  float* held = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) held[(32 * half + i) * 32 + l32] = p[i];
+  wave_lds_order();
+  for (; odd != 0; odd &= odd - 1) {
+    const int which = __builtin_ctzll(odd), group = which & 3;
+    for (int slot = which & ~3; slot < min((which & ~3) + 4, rows); ++slot) {
+      const _Float16* meta = reinterpret_cast<const _Float16*>(tile + kTileCodes + 16 * which);
+      const float scale = static_cast<float>(meta[slot & 3]), centre = __builtin_fmaf(8.f, scale, static_cast<float>(meta[4 + (slot & 3)]));
+      if (fabsf(scale) < INFINITY && fabsf(static_cast<float>(static_cast<_Float16>(centre))) < INFINITY) continue;
+      const bool some = held[slot * 32 + l32] != 0.f;
+      const int k = slot & 31;
+      float v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int channel = 8 * (i >> 2) + 4 * half + (i & 3);
+        const uint32_t word = *reinterpret_cast<const uint32_t*>(tile + 1024 * group + 16 * (32 * (slot >> 5) + channel) + 4 * (2 * (k >> 4) + ((k >> 1) & 1)));
+        const int code = (word >> (16 * (k & 1) + 4 * ((k >> 2) & 3))) & 15;
+        v[i] = some ? __builtin_fmaf(static_cast<float>(code - 8), scale, centre) : 0.f;
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        if (g != group) continue;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r.o[g][i] += v[i];
+      }
+    }
+  }
+  wave_lds_order();
+}
 
 template <int BITS, int WR, bool GENERAL>
-__global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(TreeArgs a) {
+__global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 1) void tree_kernel(TreeArgs a) {
+  constexpr int NW = kWaves<BITS, WR>;
   extern __shared__ __align__(256) uint8_t smem[];
   __shared__ uint64_t s_sees[kTokens];
   __shared__ int s_depth[kTokens], s_parent[kTokens];
-  __shared__ float s_ml[kWaves][32][4];
-  constexpr int WS = kWaves / WR;
+  __shared__ float s_ml[NW][32][4];
+  constexpr int WS = NW / WR;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const int wr = wave % WR, ws = wave / WR;
   // row groups of a piece are eight workgroups apart, on one XCD
@@ -225,21 +260,22 @@ __global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(Tree
   const uint32_t k_at = 16 * k_piece(prow, tid & 15), v_at = 16 * v_piece(prow, tid & 15);
   // rows first .. of bf16 keys and values, `stride` bytes apart, into LDS: K, then V behind `most` rows of them; rows past the last are it again
   const auto fetch_rows = [&](const uint8_t* k, const uint8_t* v, uint32_t stride, int last, int most, uint32_t to) __attribute__((always_inline)) {
-    for (int i = 0; i < most; i += 16) {
+#pragma unroll
+    for (int i = 0; i < most; i += 4 * NW) {
       const uint32_t at = static_cast<uint32_t>(min(prow + i, last)) * stride;
       copy_to_lds(k, at + k_at, to + i * kRowBytes + wave * 1024);
       copy_to_lds(v, at + v_at, to + (most + i) * kRowBytes + wave * 1024);
     }
   };
 
-  // Careful: rows of V that a window hides from some query rows are kept from meeting their zeros, which make NaN of what is not finite.  Done
+  // Careful (bf16): rows of V that a window hides from some query rows are kept from meeting their zeros, which make NaN of what is not finite.  Done
   // again so where results are not finite.
   const auto walk = [&](auto careful) __attribute__((always_inline)) {
   constexpr bool kCareful = decltype(careful)::value;
   r.init();
   if constexpr (BITS == 16) {
     constexpr int kStepsN = kSteps16<WR>, kSlots = kStage<WR>, kBuffers = kStages<WR>, kMine = 32 * kStepsN;
-    constexpr int kCopies = kSlots / 8 + (GENERAL ? 1 : 0);      // of a wavefront and stage
+    constexpr int kCopies = kSlots / (2 * NW) + (GENERAL ? 1 : 0);      // of a wavefront and stage
     const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
     const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
     const int n_it = (end - begin + kSlots - 1) / kSlots;
@@ -277,7 +313,7 @@ __global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(Tree
       tile_barrier<0>();
     }
   } else {
-    uint8_t* meta = smem + kDraftLds + wave * (kMetaLds / kWaves);
+    uint8_t* meta = smem + kDraftLds + wave * kMetaLds;
     const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
     const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
     const int t1 = (end + kTileRows - 1) / kTileRows;
@@ -294,7 +330,8 @@ __global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(Tree
       const Side4 kc = k, vc = v;
       const int left = end - t * kTileRows;
       put_k_meta(meta, kc, left);
-      put_v_meta(meta + kKMeta, vc, left);
+      // with a window, values that are not finite are kept out, and go to those rows that see them afterwards
+      const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, vc, left);
       if constexpr (GENERAL) reinterpret_cast<int*>(meta + kKMeta + 1024)[lane] = at;
       if (t + WS < t1) load(t + WS);
       wave_lds_order();
@@ -320,22 +357,23 @@ __global__ __launch_bounds__(kThreads, BITS == 16 ? 1 : 2) void tree_kernel(Tree
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        add_values<kCareful>(op, pf, [&](int f) __attribute__((always_inline)) {
+        add_values<false>(op, pf, [&](int f) __attribute__((always_inline)) {
           return f == 0 ? values4<0>(vc.codes[c], meta + kKMeta, c) : f == 1 ? values4<1>(vc.codes[c], meta + kKMeta, c)
                : f == 2 ? values4<2>(vc.codes[c], meta + kKMeta, c) : values4<3>(vc.codes[c], meta + kKMeta, c);
         }, r.o[c]);
+      if (GENERAL && odd != 0) add_odd(odd, V + static_cast<int64_t>(t) * kTileBytes, left, smem + wave * (kDraftLds / NW), p, r);
       wave_lds_order();
     }
   }
   };
   walk(std::false_type{});
-  if (GENERAL && sc.window > 0) {
+  if (BITS == 16 && GENERAL && sc.window > 0) {
     float zero = r.l * 0.f;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(r.o[t][i], 0.f, zero);
-    if (__syncthreads_or(zero != 0.f)) walk(std::bool_constant<GENERAL>{});
+    if (__syncthreads_or(zero != 0.f)) walk(std::bool_constant<BITS == 16 && GENERAL>{});
   }
 
   // the drafted tokens themselves
@@ -491,30 +529,33 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_ro
 
 template <int BITS, int WR, bool GENERAL>
 hipError_t start(const TreeArgs& a, hipStream_t st) {
-  constexpr int lds = BITS == 16 ? kStageLds + kPosLds : std::max(kDraftLds + kMetaLds, kJoinLds);
+  constexpr int NW = kWaves<BITS, WR>;
+  constexpr int lds = BITS == 16 ? kStageLds + kPosLds : std::max(kDraftLds + NW * kMetaLds, kJoinLds);
   const hipError_t e = RDKV_ALLOW_LDS((tree_kernel<BITS, WR, GENERAL>), lds);
   if (e != hipSuccess) return e;
   const int units = (a.items * a.pieces + 7) / 8 * 8;
-  hipLaunchKernelGGL((tree_kernel<BITS, WR, GENERAL>), dim3(units * a.row_groups), dim3(kThreads), lds, st, a);
+  hipLaunchKernelGGL((tree_kernel<BITS, WR, GENERAL>), dim3(units * a.row_groups), dim3(64 * NW), lds, st, a);
   return hipGetLastError();
 }
 
 template <int BITS, bool GENERAL>
 hipError_t start(const TreeArgs& a, int wide, hipStream_t st) {
+  if constexpr (BITS == 16) {
+    if (wide == 8) return start<BITS, 8, GENERAL>(a, st);
+  }
   return wide == 1 ? start<BITS, 1, GENERAL>(a, st) : wide == 2 ? start<BITS, 2, GENERAL>(a, st) : start<BITS, 4, GENERAL>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_tree(const TreeArgs& a, int bits, hipStream_t st) {
-  const TreePlan p = plan_tree(a.items, a.n * a.s.g, a.s.capacity, bits);
   const bool general = a.s.cap > 0.f || a.s.slopes || a.s.window > 0;
-  hipError_t e = bits == 16 ? (general ? start<16, true>(a, p.wide, st) : start<16, false>(a, p.wide, st))
-                            : (general ? start<4, true>(a, p.wide, st) : start<4, false>(a, p.wide, st));
+  hipError_t e = bits == 16 ? (general ? start<16, true>(a, a.wide, st) : start<16, false>(a, a.wide, st))
+                            : (general ? start<4, true>(a, a.wide, st) : start<4, false>(a, a.wide, st));
   if (e != hipSuccess || a.pieces == 1) return e;
   const int blocks = (a.n * a.s.g + 7) / 8;
-  if (bits == 16) hipLaunchKernelGGL(tree_join_kernel<16>, dim3(a.items * blocks), dim3(256), 0, st, a, 32 * p.wide);
-  else hipLaunchKernelGGL(tree_join_kernel<4>, dim3(a.items * blocks), dim3(256), 0, st, a, 32 * p.wide);
+  if (bits == 16) hipLaunchKernelGGL(tree_join_kernel<16>, dim3(a.items * blocks), dim3(256), 0, st, a, 32 * a.wide);
+  else hipLaunchKernelGGL(tree_join_kernel<4>, dim3(a.items * blocks), dim3(256), 0, st, a, 32 * a.wide);
   return hipGetLastError();
 }
 
