@@ -259,6 +259,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
     } else {
       const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
       Side4 k;
+      const Codes4 codes;
       uint4 meta[2];                               // of the lane's slots
       float before[2];
       int place[2];
@@ -294,8 +295,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
             floatx16 s = product(operand4(b, 8), centres(m[x].u), floatx16{});
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              floatx16 sums = product(operand4(b, 2 * c), words.operand(x, c, 0), floatx16{});
-              sums = product(operand4(b, 2 * c + 1), words.operand(x, c, 1), sums);
+              floatx16 sums = product(operand4(b, 2 * c), words.operand(codes, x, c, 0), floatx16{});
+              sums = product(operand4(b, 2 * c + 1), words.operand(codes, x, c, 1), sums);
 #pragma unroll
               for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(static_cast<float>(m[x].h[0][c]), sums[i], s[i]);
             }

@@ -157,17 +157,22 @@ __device__ __forceinline__ uint64_t put_v_meta(uint8_t* lds, const Side4& v, int
   return FINITE ? __ballot(odd) : 0;
 }
 
-// Fields f (0 .. 3) of a word's halves, codes, less 8 as fp16: 1024 + code, or 64 + code where the field is four bits up, are a mask and an or.
-__device__ __forceinline__ halfx2 less_8(uint32_t word, int f) {
-  union { uint32_t u; halfx2 h; } x;
-  const uint32_t v = f < 2 ? word : word >> 8;
-  if (f & 1) {
-    x.u = (v & 0x00F000F0u) | 0x54005400u;
-    return x.h - halfx2{72, 72};
+// What codes become numbers with.  Masks in scalar registers and what is or-ed to them in vector registers, of which an instruction takes one and one: the
+// two operations are one instruction then (of constants, which it knows, the compiler makes two).
+struct Codes4 {
+  uint32_t low, high, v1024, v64;
+  __device__ __forceinline__ Codes4() {
+    asm("s_mov_b32 %0, 0x000F000F" : "=s"(low));
+    asm("s_mov_b32 %0, 0x00F000F0" : "=s"(high));
+    asm("v_mov_b32 %0, 0x64006400" : "=v"(v1024));
+    asm("v_mov_b32 %0, 0x54005400" : "=v"(v64));
   }
-  x.u = (v & 0x000F000Fu) | 0x64006400u;
-  return x.h - halfx2{1032, 1032};
-}
+  // Fields f (0 .. 3) of a word's halves, codes, less 8 as fp16: 1024 + code, or 64 + code where the field is four bits up, less 1032 or 72.
+  __device__ __forceinline__ halfx2 less_8(uint32_t word, int f) const {
+    const uint32_t v = f < 2 ? word : word >> 8;
+    return f & 1 ? __builtin_bit_cast(halfx2, (v & high) | v64) - halfx2{72, 72} : __builtin_bit_cast(halfx2, (v & low) | v1024) - halfx2{1032, 1032};
+  }
+};
 
 // A lane's words of product x, and of them what a product's operand of a group's half is: fields 2 s and 2 s + 1 of two words.
 struct Words4 {
@@ -185,19 +190,19 @@ struct Words4 {
       w[1][g][1] = d;
     }
   }
-  __device__ __forceinline__ halfx8 operand(int x, int g, int s) const {
+  __device__ __forceinline__ halfx8 operand(const Codes4& codes, int x, int g, int s) const {
     union { halfx2 p[4]; halfx8 h; } op;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      op.p[j] = less_8(w[x][g][j], 2 * s);
-      op.p[2 + j] = less_8(w[x][g][j], 2 * s + 1);
+      op.p[j] = codes.less_8(w[x][g][j], 2 * s);
+      op.p[2 + j] = codes.less_8(w[x][g][j], 2 * s + 1);
     }
     return op.h;
   }
 };
 
 // Products of the 64 slots, register i of s[x] of lane (half, .): slot 32 half + 16 x + i; over the query's unit.
-__device__ __forceinline__ void scores4(const Side4& k, const uint8_t* k_meta, const Query4& q, floatx16 (&s)[2]) {
+__device__ __forceinline__ void scores4(const Codes4& codes, const Side4& k, const uint8_t* k_meta, const Query4& q, floatx16 (&s)[2]) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
   const Words4 words(k);
 #pragma unroll
@@ -205,30 +210,30 @@ __device__ __forceinline__ void scores4(const Side4& k, const uint8_t* k_meta, c
     s[x] = product(*reinterpret_cast<const halfx8*>(k_meta + 16 * slot_of_row(x, l32)), q.sums, floatx16{});
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      floatx16 sums = product(words.operand(x, g, 0), q.op[2 * g], floatx16{});
-      sums = product(words.operand(x, g, 1), q.op[2 * g + 1], sums);
+      floatx16 sums = product(words.operand(codes, x, g, 0), q.op[2 * g], floatx16{});
+      sums = product(words.operand(codes, x, g, 1), q.op[2 * g + 1], sums);
       const halfx8* sc = reinterpret_cast<const halfx8*>(k_meta + 1024 + 128 * g + 2 * (32 * half + 16 * x));
       const halfx8 sc0 = sc[0], sc1 = sc[1];
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         s[x][i] = __builtin_fmaf(static_cast<float>(i < 8 ? sc0[i & 7] : sc1[i & 7]), sums[i], s[x][i]);
-      if (g & 1) __builtin_amdgcn_sched_barrier(0);             // (all groups side by side do not fit the registers)
+      __builtin_amdgcn_sched_barrier(0);         // (the scheduler would have all operands first, and spill them)
     }
   }
 }
 
 // fp16 values of channel 32 group + l32 of slots 32 half + 4 f + 0..3 and + 16..19
 template <int F>
-__device__ __forceinline__ halfx8 values4(const uint4& codes, const uint8_t* v_meta, int group) {
+__device__ __forceinline__ halfx8 values4(const Codes4& codes, const uint4& words, const uint8_t* v_meta, int group) {
   const int half = (threadIdx.x & 63) >> 5;
-  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+  const uint32_t w[4] = {words.x, words.y, words.z, words.w};
   union { halfx2 h[4]; halfx8 v; } x;
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
     union { uint4 u; halfx2 h[4]; } m;
     m.u = *reinterpret_cast<const uint4*>(v_meta + 64 * (8 * half + 4 * p + F) + 16 * group);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) x.h[2 * p + j] = __builtin_elementwise_fma(less_8(w[2 * p + j], F), m.h[j], m.h[2 + j]);
+    for (int j = 0; j < 2; ++j) x.h[2 * p + j] = __builtin_elementwise_fma(codes.less_8(w[2 * p + j], F), m.h[j], m.h[2 + j]);
   }
   return x.v;
 }

@@ -162,12 +162,11 @@ constexpr int kJoinLds = 4 * 4 * 16 * 64 * 4;                   // four wavefron
 constexpr int kMetaLds = kKMeta + 1024 + 256;                   // of a wavefront
 
 // Values of a 4-bit tile that are not finite, to the rows that give their slots something.  odd: lanes 4 (slot / 4) + group whose metadata are not; lds:
-// 8 KiB of the wavefront's; p: probabilities, register i of slot 32 half + i.
+// 2 KiB of the wavefront's; p: probabilities, register i of slot 32 half + i.
 __device__ __forceinline__ void add_odd(uint64_t odd, const uint8_t* tile, int rows, uint8_t* lds, const float (&p)[32], Out& r) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-  float* held = reinterpret_cast<float*>(lds);
 #pragma unroll
-  for (int i = 0; i < 32; ++i) held[(32 * half + i) * 32 + l32] = p[i];
+  for (int i = 0; i < 32; ++i) lds[(32 * half + i) * 32 + l32] = p[i] != 0.f;
   wave_lds_order();
   for (; odd != 0; odd &= odd - 1) {
     const int which = __builtin_ctzll(odd), group = which & 3;
@@ -175,7 +174,7 @@ __device__ __forceinline__ void add_odd(uint64_t odd, const uint8_t* tile, int r
       const _Float16* meta = reinterpret_cast<const _Float16*>(tile + kTileCodes + 16 * which);
       const float scale = static_cast<float>(meta[slot & 3]), centre = __builtin_fmaf(8.f, scale, static_cast<float>(meta[4 + (slot & 3)]));
       if (fabsf(scale) < INFINITY && fabsf(static_cast<float>(static_cast<_Float16>(centre))) < INFINITY) continue;
-      const bool some = held[slot * 32 + l32] != 0.f;
+      const bool some = lds[slot * 32 + l32] != 0;
       const int k = slot & 31;
       float v[16];
 #pragma unroll
@@ -320,29 +319,34 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
     Side4 k, v;
     int at = 0;
     int t = begin / kTileRows + ws;
-    const auto load = [&](int tile) __attribute__((always_inline)) {
+    const Codes4 codes;
+    // the next tile's K comes while this one's values are added up, its V while its scores are made
+    const auto load_k = [&](int tile) __attribute__((always_inline)) {
       k.load(K + static_cast<int64_t>(tile) * kTileBytes, true);
-      v.load(V + static_cast<int64_t>(tile) * kTileBytes, false);
       if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
     };
-    if (t < t1) load(t);
+    const auto load_v = [&](int tile) __attribute__((always_inline)) { v.load(V + static_cast<int64_t>(tile) * kTileBytes, false); };
+    if (t < t1) {
+      load_k(t);
+      load_v(t);
+    }
     for (; t < t1; t += WS) {
-      const Side4 kc = k, vc = v;
       const int left = end - t * kTileRows;
-      put_k_meta(meta, kc, left);
-      // with a window, values that are not finite are kept out, and go to those rows that see them afterwards
-      const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, vc, left);
+      put_k_meta(meta, k, left);
       if constexpr (GENERAL) reinterpret_cast<int*>(meta + kKMeta + 1024)[lane] = at;
-      if (t + WS < t1) load(t + WS);
       wave_lds_order();
       floatx16 s[2];
-      scores4(kc, meta, query, s);
+      scores4(codes, k, meta, query, s);
+      load_k(min(t + WS, t1 - 1));
       float x[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = s[i >> 4][i & 15];
       const int4* where = reinterpret_cast<const int4*>(meta + kKMeta + 1024) + 8 * half;
       to_scores<GENERAL>(sc, row, x, left < kTileRows, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[k]; },
                          [&](int i) __attribute__((always_inline)) { return 32 * half + i >= left; });
+      // with a window, values that are not finite are kept out, and go to those rows that see them afterwards
+      const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v, left);
+      wave_lds_order();
       float p[32], pf[32];
       softmax(x, sc.factor, kTopHalf, r, p);
       halfx8 op[4];
@@ -356,11 +360,14 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
         op[f] = to_half(pf + 8 * f);
       }
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < 4; ++c) {
+        __builtin_amdgcn_sched_barrier(0);
         add_values<false>(op, pf, [&](int f) __attribute__((always_inline)) {
-          return f == 0 ? values4<0>(vc.codes[c], meta + kKMeta, c) : f == 1 ? values4<1>(vc.codes[c], meta + kKMeta, c)
-               : f == 2 ? values4<2>(vc.codes[c], meta + kKMeta, c) : values4<3>(vc.codes[c], meta + kKMeta, c);
+          return f == 0 ? values4<0>(codes, v.codes[c], meta + kKMeta, c) : f == 1 ? values4<1>(codes, v.codes[c], meta + kKMeta, c)
+               : f == 2 ? values4<2>(codes, v.codes[c], meta + kKMeta, c) : values4<3>(codes, v.codes[c], meta + kKMeta, c);
         }, r.o[c]);
+      }
+      load_v(min(t + WS, t1 - 1));
       if (GENERAL && odd != 0) add_odd(odd, V + static_cast<int64_t>(t) * kTileBytes, left, smem + wave * (kDraftLds / NW), p, r);
       wave_lds_order();
     }
