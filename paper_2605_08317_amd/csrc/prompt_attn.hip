@@ -12,7 +12,7 @@ namespace {
 using namespace attn;
 
 constexpr int kTileBytes = kKeys * kRowBytes;        // of K, or of V
-constexpr int kBuffers = 4;
+constexpr int kRing = 2;
 constexpr float kLowest = -2e38f;                    // a finite maximum of nothing, also times log2(e): no score is below it
 constexpr float kSlack = 8.f;                        // what exponents may exceed the reference by before it moves
 
@@ -22,9 +22,9 @@ __device__ __forceinline__ int64_t first_of(const Side& s, int64_t token0, int h
 }
 
 template <int NW, bool GENERAL>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a) {
+__global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(Args a) {
   extern __shared__ __align__(256) uint8_t smem[];
-  constexpr int kRows = 32 * NW, kCopies = 32 / NW;       // kCopies: of a wavefront and tile
+  constexpr int kRows = 32 * NW, kCopies = 16 / NW;       // kCopies: of a wavefront and tile
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
   const int items = a.n_seqs * a.hkv, pairs = a.n_seqs * a.hq;
   const int level = static_cast<int>(blockIdx.x) / pairs, pair = static_cast<int>(blockIdx.x) % pairs;
@@ -44,28 +44,25 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
   const uint32_t lds0 = lds_address(smem);
   const int prow = tid >> 4;                         // this thread's rows prow + 4 NW k
   const uint32_t k_at = 16 * k_piece(prow, tid & 15), v_at = 16 * v_piece(prow, tid & 15);
-  const auto fetch = [&](int it) __attribute__((always_inline)) {
+  const auto slot = [](int it) { return static_cast<uint32_t>(it % kRing) * kTileBytes; };
+  const auto fetch = [&](const uint16_t* from, const Side& side, uint32_t at, int it, uint32_t to) __attribute__((always_inline)) {
     const int key0 = tile_of(min(it, n_it - 1)) * kKeys, last = T - 1 - key0;
-    const uint16_t* ks = Kh + static_cast<int64_t>(key0) * a.k.row;
-    const uint16_t* vs = Vh + static_cast<int64_t>(key0) * a.v.row;
-    const uint32_t to = lds0 + (it % kBuffers) * (2 * kTileBytes) + wave * 1024;
+    from += static_cast<int64_t>(key0) * side.row;
+    to += slot(it) + wave * 1024;
 #pragma unroll
-    for (int k = 0; k < 16 / NW; ++k) {
-      const int row = min(prow + 4 * NW * k, last);
-      copy_to_lds(ks, static_cast<uint32_t>(row * a.k.row) * 2 + k_at, to + 1024 * NW * k);
-      copy_to_lds(vs, static_cast<uint32_t>(row * a.v.row) * 2 + v_at, to + kTileBytes + 1024 * NW * k);
-    }
+    for (int k = 0; k < kCopies; ++k)
+      copy_to_lds(from, static_cast<uint32_t>(min(prow + 4 * NW * k, last) * side.row) * 2 + at, to + 1024 * NW * k);
   };
+  const auto fetch_k = [&](int it) __attribute__((always_inline)) { fetch(Kh, a.k, k_at, it, lds0); };
+  const auto fetch_v = [&](int it) __attribute__((always_inline)) { fetch(Vh, a.v, v_at, it, lds0 + kRing * kTileBytes); };
 
-  const int r0 = q0 + 32 * wave, row = r0 + l32;     // this wavefront's first row, and the lane's
+  const int r0 = q0 + 32 * wave, row = r0 + l32; // this wavefront's first row, and the lane's
   bf16x8 q_op[8];
-  {
-    const uint16_t* q = a.Q + first_of(a.q, token0, a.hq, head, T) + static_cast<int64_t>(min(row, T - 1)) * a.q.row + 8 * half;
+  const uint16_t* q = a.Q + first_of(a.q, token0, a.hq, head, T) + static_cast<int64_t>(min(row, T - 1)) * a.q.row + 8 * half;
 #pragma unroll
-    for (int kb = 0; kb < 8; ++kb) q_op[kb] = *reinterpret_cast<const bf16x8*>(q + 16 * kb);
+  for (int kb = 0; kb < 8; ++kb) q_op[kb] = *reinterpret_cast<const bf16x8*>(q + 16 * kb);
 #pragma unroll
-    for (int kb = 0; kb < 8; ++kb) arrived(q_op[kb]);
-  }
+  for (int kb = 0; kb < 8; ++kb) arrived(q_op[kb]);
   const float slope = GENERAL && a.slopes ? a.slopes[head] : 0.f, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
   // What makes the numbers that are kept (products, scores over the cap, or with biases scores) scores, and those exponents of 2.
   const float units = GENERAL && a.cap > 0.f ? a.cap : kRoot;
@@ -74,8 +71,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
   floatx16 o[4];
   float m, l;
   const auto key_of = [&](int it) { return tile_of(it) * kKeys; };
-  const uint32_t k_first = lds0 + k_lane(), v_first = lds0 + kTileBytes + v_lane();
-  const auto buffer_of = [&](int it) { return static_cast<uint32_t>(it % kBuffers) * (2 * kTileBytes); };
+  const uint32_t k_first = lds0 + k_lane(), v_first = lds0 + kRing * kTileBytes + v_lane();
   // The tiles that this wavefront has to do with: until its last row, and from its first row's window on (where there are sinks, from those on).
   const int it_end = min(n_it, (r0 + 31) / kKeys - first + n_sink + 1);
   const int it_begin = a.window > 0 && a.sinks == 0 ? min(it_end - 1, max(0, r0 - a.window + 1) / kKeys - first) : 0;
@@ -84,11 +80,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
     for (int t = 0; t < 4; ++t) o[t] = floatx16{};
     m = kLowest;
     l = 0.f;
-#pragma unroll
-    for (int it = 0; it < kBuffers - 1; ++it) fetch(it);
   };
   const auto key = [](int x, int i) { return 32 * x + 8 * (i >> 2) + (i & 3); };
-  // Products of a tile to scores, -inf where hidden.
+  // Products of a tile to scores, -inf where hidden; whether it did something.
   const auto finish = [&](int it, floatx16 (&s)[2]) __attribute__((always_inline)) {
     const int key0 = key_of(it), back = row - key0 - 4 * half;           // positions from key 4 half of the tile to the row
     if constexpr (GENERAL) {
@@ -103,26 +97,29 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
 #pragma unroll
       for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = v[i];
     }
-    if (key0 + kKeys - 1 > r0) {
+    const bool edge = key0 + kKeys - 1 > r0, far = a.window > 0 && r0 + 31 - key0 >= a.window;
+    if (edge) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[x][i] = key(x, i) > back ? -INFINITY : s[x][i];
     }
-    if (a.window > 0 && r0 + 31 - key0 >= a.window) {
+    if (far) {
       const int sink = a.sinks - key0 - 4 * half;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[x][i] = back - key(x, i) >= a.window && key(x, i) >= sink ? -INFINITY : s[x][i];
     }
+    return GENERAL || edge || far;
   };
   const auto multiply = [&](int it, floatx16 (&s)[2]) __attribute__((always_inline)) {
-    const uint32_t kt = k_first + buffer_of(it);
+    const uint32_t kt = k_first + slot(it);
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int kb = 0; kb < 8; ++kb) s[x] = product(read_k(kt, kb, x), q_op[kb], kb == 0 ? floatx16{} : s[x]);
+    for (int i = 0; i < 16; ++i) {
+      const bf16x8 k = read_k(kt, i & 7, i >> 3);
+      s[i >> 3] = product(k, q_op[i & 7], (i & 7) == 0 ? floatx16{} : s[i >> 3]);
+    }
   };
   // the row's reference, if its largest score is past it
   const auto refer = [&](float top, bool any) __attribute__((always_inline)) {
@@ -140,84 +137,105 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
     float top = s[0][0];
 #pragma unroll
     for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-    return halves_max(top);
+    return top;
   };
 
   // A tile's softmax and P V, and between their instructions the next tile's products (MORE), so that the matrix cores have work while
   // exponentials are made: 16 of those stand between the 16 products, 16 between the first 8 of P V.  Each line is one product and what the plain ALUs
   // do meanwhile.
-  const auto position = [&](auto more, int it, floatx16 (&s)[2], floatx16 (&next)[2]) __attribute__((always_inline)) {
+  // top: the lane's largest score of the tile; the next one's comes back.
+  const auto position = [&](auto more, int it, floatx16 (&s)[2], floatx16 (&next)[2], float& top) __attribute__((always_inline)) {
     constexpr bool kMore = decltype(more)::value;
-    refer(largest(s), false);
-    const float ref = -m * factor;
-    const uint32_t kt = k_first + buffer_of(it + 1), vt = v_first + buffer_of(it);
+    float sums[2] = {}, tops;
     union { uint32_t u[16]; bf16x8 op[4]; } p;
-    float sums[2] = {0.f, 0.f}, before = 0.f;
-    const auto make = [&](int i) __attribute__((always_inline)) {        // in order
-      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], factor, ref));
-      sums[i & 1] += e;
-      if (i & 1) p.u[i >> 1] = pair_bf16(before, e);
-      before = e;
+    refer(halves_max(top), false);
+    const float ref = -m * factor;
+    const uint32_t kt = k_first + slot(it + 1), vt = v_first + slot(it);
+    // Exponential i, in order; what hangs on another one's result stands behind it, so that nothing waits for it.
+    float x = __builtin_fmaf(s[0][0], factor, ref), e[3];
+    const auto make = [&](int i) __attribute__((always_inline)) {
+      const float now = x;
+      if (i < 31) x = __builtin_fmaf(s[(i + 1) >> 4][(i + 1) & 15], factor, ref);
+      if (i < 32) e[i % 3] = __builtin_amdgcn_exp2f(now);
+      if (i > 0) sums[i & 1] += e[(i - 1) % 3];
+      if (i > 0 && (i & 1) == 0) p.u[(i >> 1) - 1] = pair_bf16(e[(i - 2) % 3], e[(i - 1) % 3]);
     };
+    // operands on their way from LDS, of products 0 .. 15 (K) and 16 .. 31 (V: keys 16 (i / 4) .., channels 32 (i % 4) ..)
     constexpr int kAhead = 3;
-    bf16x8 k_op[kAhead], v_op[kAhead];
-    const auto k_at = [&](int i) __attribute__((always_inline)) { return read_k(kt, i & 7, i >> 3); };
-    const auto v_at = [&](int i) __attribute__((always_inline)) { return read_v(vt, i & 3, (i >> 2) & 1, i >> 3); };    // keys 16 (i / 4) .., channels 32 (i % 4) ..
+    bf16x8 op[kAhead];
+    const auto ask = [&](int i) __attribute__((always_inline)) {
+      if (i < 16) op[i % kAhead] = read_k(kt, i & 7, i >> 3);
+      else if (i < 32) op[i % kAhead] = read_v(vt, i & 3, (i >> 2) & 1, (i - 16) >> 3);
+    };
     if constexpr (kMore) {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) k_op[i] = k_at(i);
+      for (int i = 0; i < kAhead; ++i) ask(i);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        next[i >> 3] = product(k_op[i % kAhead], q_op[i & 7], (i & 7) == 0 ? floatx16{} : next[i >> 3]);
-        if (i + kAhead < 16) k_op[i % kAhead] = k_at(i + kAhead);
-        else v_op[(i + kAhead) % 16] = v_at((i + kAhead) % 16);
+        next[i >> 3] = product(op[i % kAhead], q_op[i & 7], (i & 7) == 0 ? floatx16{} : next[i >> 3]);
+        ask(i + kAhead);
         make(i);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) v_op[i] = v_at(i);
+      for (int i = 16; i < 16 + kAhead; ++i) ask(i);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) make(i);
+      for (int i = 0; i < 16; ++i)
+        make(i);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      o[i & 3] = product(v_op[i % kAhead], p.op[i >> 2], o[i & 3]);
-      if (i + kAhead < 16) v_op[i % kAhead] = v_at(i + kAhead);
+      o[i & 3] = product(op[(i + 16) % kAhead], p.op[i >> 2], o[i & 3]);
+      ask(i + 16 + kAhead);
       if (i < 8) {
         make(16 + 2 * i);
         make(17 + 2 * i);
+      } else {
+        if (i == 8) make(32);
+        if (!kMore) continue;
+        const int j = 4 * (i - 8);
+        const floatx16& n = next[j >> 4];
+        const float a = n[j & 15], b = n[(j & 15) + 1], c = n[(j & 15) + 2], d = n[(j & 15) + 3];
+        tops = fmaxf(fmaxf(i == 8 ? a : fmaxf(tops, a), b), fmaxf(c, d));
       }
       __builtin_amdgcn_sched_barrier(0);
     }
     l += sums[0] + sums[1];
-    if constexpr (kMore) finish(it + 1, next);
+    __builtin_amdgcn_s_setprio(0);
+    if constexpr (kMore) top = finish(it + 1, next) ? largest(next) : tops;
   };
   const auto walk = [&]() __attribute__((always_inline)) {
     begin();
-    tile_barrier<kCopies * (kBuffers - 2)>();
+    fetch_k(0);
+    fetch_v(0);
+    fetch_k(1);
+    tile_barrier<2 * kCopies>();
     floatx16 even[2], odd[2];
-    const auto open = [&](int it) __attribute__((always_inline)) {       // tile it + 1 is there, and the buffer of tile it - 1 free
-      tile_barrier<kCopies * (kBuffers - 3)>();
-      fetch(it + kBuffers - 1);
+    const auto open = [&](int it) __attribute__((always_inline)) {       // K of tile it + 1 and V of tile it are there, K of tile it and V of tile it - 1 done with
+      tile_barrier<0>();
+      fetch_k(it + 2);
+      fetch_v(it + 1);
+      __builtin_amdgcn_s_setprio(1);                 // (the other workgroup of the compute unit is elsewhere in its tile)
     };
     int it = 0;
     for (; it < it_begin; ++it) open(it);
     multiply(it, even);
     finish(it, even);
+    float top = largest(even);
     for (; it + 2 < it_end; it += 2) {
       open(it);
-      position(std::true_type{}, it, even, odd);
+      position(std::true_type{}, it, even, odd, top);
       open(it + 1);
-      position(std::true_type{}, it + 1, odd, even);
+      position(std::true_type{}, it + 1, odd, even, top);
     }
     open(it);
     if (it + 1 < it_end) {
-      position(std::true_type{}, it, even, odd);
+      position(std::true_type{}, it, even, odd, top);
       open(++it);
-      position(std::false_type{}, it, odd, even);
+      position(std::false_type{}, it, odd, even, top);
     } else {
-      position(std::false_type{}, it, even, odd);
+      position(std::false_type{}, it, even, odd, top);
     }
     for (++it; it < n_it; ++it) open(it);
     tile_barrier<0>();                               // (copies of tiles past the last have landed as well)
@@ -227,20 +245,22 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
   const auto walk_with_care = [&]() __attribute__((always_inline)) {
     begin();
     for (int it = 0; it < n_it; ++it) {
-      tile_barrier<kCopies * (kBuffers - 2)>();
-      fetch(it + kBuffers - 1);
+      tile_barrier<0>();
+      fetch_k(it);
+      fetch_v(it);
+      tile_barrier<0>();
       if (it < it_begin || it >= it_end) continue;
       floatx16 s[2];
       multiply(it, s);
+      const uint32_t vt = v_first + slot(it);
       finish(it, s);
-      refer(largest(s), true);
+      refer(halves_max(largest(s)), true);
       float p[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         p[i] = __builtin_amdgcn_exp2f((s[i >> 4][i & 15] - m) * factor);
         l += p[i];
       }
-      const uint32_t vt = v_first + buffer_of(it);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         floatx16 up = {}, down = {};
@@ -267,7 +287,6 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
         }
       }
     }
-    tile_barrier<0>();
   };
   walk();
   float sum = 0.f;
@@ -285,22 +304,23 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 2) void prompt_kernel(Args a
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      float v[8];
+    float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = o[t][8 * c + i] * inv;
-      union { bf16x8 b; uint32_t u[4]; } w;
-      w.b = to_bf16(v);
-      // channels 16 c + 0..7 to the lower half, 8..15 to the upper
-      asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(w.u[0]), "+v"(w.u[2]));
-      asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(w.u[1]), "+v"(w.u[3]));
-      *reinterpret_cast<uint4*>(out + 32 * t + 16 * c) = make_uint4(w.u[0], w.u[1], w.u[2], w.u[3]);
-    }
-  if (a.lse && half == 0) a.lse[token0 * a.hq + static_cast<int64_t>(head) * T + row] = total == 0.f ? -INFINITY : __builtin_fmaf(m * factor, kLn2, __logf(total));
+    for (int i = 0; i < 8; ++i) v[i] = o[t][8 * c + i] * inv;
+    union { bf16x8 b; uint32_t u[4]; } w;
+    w.b = to_bf16(v);
+    // channels 16 c + 0..7 to the lower half, 8..15 to the upper
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(w.u[0]), "+v"(w.u[2]));
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(w.u[1]), "+v"(w.u[3]));
+    *reinterpret_cast<uint4*>(out + 32 * t + 16 * c) = make_uint4(w.u[0], w.u[1], w.u[2], w.u[3]);
+  }
+  if (a.lse && half == 0)
+    a.lse[token0 * a.hq + static_cast<int64_t>(head) * T + row] = total == 0.f ? -INFINITY : __builtin_fmaf(m * factor, kLn2, __logf(total));
 }
 
 template <int NW, bool GENERAL>
 hipError_t start(const Args& a, int longest, hipStream_t st) {
-  constexpr int lds = 2 * kBuffers * kTileBytes;
+  constexpr int lds = 2 * kRing * kTileBytes;
   const hipError_t e = RDKV_ALLOW_LDS((prompt_kernel<NW, GENERAL>), lds);
   if (e != hipSuccess) return e;
   const int tiles = (longest + 32 * NW - 1) / (32 * NW);
@@ -312,8 +332,6 @@ hipError_t start(const Args& a, int longest, hipStream_t st) {
 
 hipError_t launch(const Args& a, int longest, hipStream_t st) {
   const bool general = a.cap > 0.f || a.slopes;      // (a window takes no scores of its own)
-  const int64_t large = static_cast<int64_t>(longest + 255) / 256 * a.n_seqs * a.hq;
-  if (large >= 512) return general ? start<8, true>(a, longest, st) : start<8, false>(a, longest, st);
   return general ? start<4, true>(a, longest, st) : start<4, false>(a, longest, st);
 }
 
