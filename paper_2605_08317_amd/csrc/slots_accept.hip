@@ -4,8 +4,8 @@
 // products as in slots_tree.hip, but with the query rows on their A side, so that a lane has one slot and sums over the rows are its own;
 // probabilities by the largest score and the sum that the tree's step left.  V is not read.  Where a cache will be full it leaves the least of
 // every 32 slots as well.  The second, a workgroup an item, takes the tokens in one after the other as that many appends would, from those
-// leasts: when a slot is given away only its 32 are looked at again.
-//   bound   the K side once: HBM.  The second launch: a few dependent steps for each token that takes another's slot
+// leasts.
+//   bound   the K side once: HBM.  The second launch: a chain of steps, a few for each token that takes another's slot
 #include <algorithm>
 
 #include "group_quant.h"
@@ -314,26 +314,81 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
   }
 }
 
-constexpr int kThreads = 1024;
+// The least of the wavefront's by (key, at), and a lane that has it.
+struct First {
+  uint64_t key;
+  int at, lane;
+};
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lower(uint32_t v) {
+  return min(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(-1, static_cast<int>(v), CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) {
+  v = lower<0x118, 0xf>(lower<0x114, 0xf>(lower<0x112, 0xf>(lower<0x111, 0xf>(v))));           // rows of 16
+  return __builtin_amdgcn_readlane(lower<0x143, 0xc>(lower<0x142, 0xa>(v)), 63);
+}
+__device__ __forceinline__ First first_of_wave(uint64_t key, int at) {
+  const uint32_t high = wave_min(static_cast<uint32_t>(key >> 32)), low = wave_min(static_cast<uint32_t>(key >> 32) == high ? static_cast<uint32_t>(key) : ~0u);
+  First f;
+  f.key = static_cast<uint64_t>(high) << 32 | low;
+  uint64_t have = __ballot(key == f.key);
+  if (have & (have - 1)) {
+    const uint32_t lowest = wave_min(key == f.key ? static_cast<uint32_t>(at) : ~0u);
+    have = __ballot(key == f.key && static_cast<uint32_t>(at) == lowest);
+  }
+  f.lane = __builtin_ctzll(have);
+  f.at = __builtin_amdgcn_readlane(at, f.lane);
+  return f;
+}
 
-// The second launch.  Which slots go follows from three kinds of tokens, of which a lane of the first wavefront has one each at most: the least of
-// the slots that could go at once, over the lane's segments; a cached token that becomes old enough on the way; and an accepted one that does.  Only
-// where one of the first kind goes memory is read again, its segment's slots and the leasts of the lane's segments.
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+
+// Lists of the wavefronts, each in order, and the walk over all of them: wavefront w's list is lane w's.
+struct Lists {
+  uint64_t key[kWaves][kMostDrafted];
+  int at[kWaves][kMostDrafted];
+};
+struct Walk {
+  const Lists& lists;
+  uint64_t key = ~0ull;
+  int at = 0, next = 0;
+  __device__ __forceinline__ explicit Walk(const Lists& l) : lists(l) { step(); }
+  __device__ __forceinline__ void step() {
+    const int lane = threadIdx.x & 63;
+    key = lane < kWaves && next < kMostDrafted ? lists.key[lane][next] : ~0ull;
+    if (key != ~0ull) at = lists.at[lane][next];
+    ++next;
+  }
+};
+
+// The second launch.  Which slots go follows from three kinds of tokens: slots that could go at once, cached tokens that become old enough on the
+// way, and accepted ones that do; of the first kind only the least `want` matter, one for each token that takes another's slot.  They are in the
+// `want` segments whose leasts are least, so those are found first, then the slots in them; both times each wavefront makes a list of its own least
+// ones and a walk over the sixteen lists gives the order.  The tokens' turns then are a walk in which a lane adds the token of the other two kinds
+// that it has, and nothing is read from memory.
+//   measured   4 tokens in 1000 slots 9.6 us, 8 in each of 256 items' 8192 slots of 4 bits 23 us; a turn that looked at the slots and leasts again in
+//              memory took 2 us more (18 and 39)
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void accept_append_kernel(AcceptArgs a) {
-  constexpr int kWaves = kThreads / 64;
-  __shared__ int s_slot[kMostDrafted], s_late[kMostDrafted];
-  __shared__ uint64_t s_key[kWaves][64];
-  __shared__ int s_at[kWaves][64];
+  __shared__ int s_slot[kMostDrafted], s_late[kMostDrafted], s_enters[kMostDrafted], s_n;
+  __shared__ Lists s_segments, s_slots;
   const int item = blockIdx.x, seq = item / a.s.hkv, kvh = item % a.s.hkv, cap = a.s.capacity;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int32_t* path = a.path + static_cast<int64_t>(seq) * a.m;
+  const int len = a.s.length(item), next = a.s.next[item];
   const int count = path_length(path, a.m, a.n);
   int32_t* out = a.slot ? a.slot + static_cast<int64_t>(item) * a.m : nullptr;
   if (out && tid < a.m && tid >= count) out[tid] = -1;
   if (count == 0) return;
-  const int len = a.s.length(item), next = a.s.next[item];
-  const bool full = len + count > cap;
+  const int first = max(cap - len, 0), want = count - first;           // the first token that takes another's slot, and how many do
+
+  // rows: half a wavefront a token, lanes 0..15 its K row, 16..31 its V row
+  const int c16 = lane & 15;
+  const bool is_v = lane >= 16;
+  const auto row_of = [&](int j) {
+    return reinterpret_cast<const uint4*>(is_v ? a.v_draft : a.k_draft)[((static_cast<int64_t>(seq) * a.n + path[min(j, count - 1)]) * a.s.hkv + kvh) * 16 + c16];
+  };
+  const uint4 first_row = row_of(wave);
 
   int32_t* pos = a.s.pos + static_cast<int64_t>(item) * cap;
   float* weight = a.s.weight ? a.s.weight + static_cast<int64_t>(item) * cap : nullptr;
@@ -341,91 +396,114 @@ __global__ __launch_bounds__(kThreads) void accept_append_kernel(AcceptArgs a) {
   const int segments = (cap + kSegment - 1) / kSegment, used = (len + kSegment - 1) / kSegment;
   Least* leasts = reinterpret_cast<Least*>(a.leasts) + static_cast<int64_t>(item) * segments;
   const int newest = next - a.s.recent;            // the last position that may go for the first token
-  if (tid < kMostDrafted) s_late[tid] = INT32_MAX;
-  __syncthreads();
-  if (full) {
-    // the leasts of the lanes' segments, lane + 64 k, a part of them each wavefront; and who becomes old enough
+  const auto key_of = [](float w, int p) { return static_cast<uint64_t>(weight_key(w)) << 32 | static_cast<uint32_t>(p); };
+  if (want > 0) {
+    if (tid < kMostDrafted) s_late[tid] = INT32_MAX;
+    if (tid == 0) s_n = 0;
+    s_segments.key[wave][lane] = s_slots.key[wave][lane] = ~0ull;
+    __syncthreads();
+    // the leasts of the lane's segments, and which segments have somebody who becomes old enough
     Least l = nothing();
     for (int e = tid; e < used; e += kThreads) {
       Least of;
       if (weight) {
         of = leasts[e];
       } else {                                     // (no launch has looked: the oldest go)
+        int p[kSegment];
+#pragma unroll
+        for (int i = 0; i < kSegment; ++i) p[i] = pos[min(e * kSegment + i, len - 1)];
         of = nothing();
-        for (int i = e * kSegment; i < min((e + 1) * kSegment, len); ++i) look_at(of, i, pos[i], 0.f, a.s.sinks, newest);
+#pragma unroll
+        for (int i = 0; i < kSegment; ++i)
+          if (e * kSegment + i < len) look_at(of, e * kSegment + i, p[i], 0.f, a.s.sinks, newest);
         leasts[e] = of;
       }
       take(l, of.key, of.at);
       if (of.enters < newest + count) {
-        for (int i = e * kSegment; i < min((e + 1) * kSegment, len); ++i) {
-          const int after = pos[i] - newest - 1;
-          if (pos[i] >= a.s.sinks && after >= 0 && after < count) atomicMin(&s_late[after], i);
+        const int n = atomicAdd(&s_n, 1);
+        if (n < kMostDrafted) s_enters[n] = e;     // (as many positions, and so no more segments)
+      }
+    }
+    for (int i = 0; i < want; ++i) {
+      const First f = first_of_wave(l.key, l.at);
+      if (f.key == ~0ull) break;
+      if (lane == 0) {
+        s_segments.key[wave][i] = f.key;
+        s_segments.at[wave][i] = f.at;
+      }
+      if (lane == f.lane) {
+        l = nothing();
+        for (int e = tid; e < used && used > kThreads; e += kThreads) {
+          const Least of = leasts[e];
+          if (of.key > f.key || (of.key == f.key && of.at > f.at)) take(l, of.key, of.at);
         }
       }
     }
-    s_key[wave][lane] = l.key;
-    s_at[wave][lane] = l.at;
+    __syncthreads();
+    int segment = -1;                              // lane i: the i-th
+    Walk order(s_segments);
+    for (int i = 0; i < want; ++i) {
+      const First f = first_of_wave(order.key, order.at);
+      if (f.key == ~0ull) break;
+      if (lane == i) segment = f.at / kSegment;
+      if (lane == f.lane) order.step();
+    }
+    // half of the wavefront a segment, twice; segments that become old enough likewise
+    uint64_t key[2];
+    int at[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int which = 2 * wave + (lane >> 5) + 2 * kWaves * k, e = __shfl(segment, which), slot = e * kSegment + (lane & 31);
+      key[k] = ~0ull;
+      at[k] = slot;
+      if (e >= 0 && slot < len) {
+        const int p = pos[slot];
+        const float w = weight ? weight[slot] : 0.f;
+        if (p >= a.s.sinks && p <= newest) key[k] = key_of(w, p);
+      }
+      if (which < s_n) {
+        const int i = s_enters[which] * kSegment + (lane & 31), p = i < len ? pos[i] : -1, after = p - newest - 1;
+        if (p >= a.s.sinks && after >= 0 && after < count) atomicMin(&s_late[after], i);
+      }
+    }
+    for (int i = 0; i < want; ++i) {
+      const bool second = key[1] < key[0] || (key[1] == key[0] && at[1] < at[0]);
+      const First f = first_of_wave(second ? key[1] : key[0], second ? at[1] : at[0]);
+      if (f.key == ~0ull) break;
+      if (lane == 0) {
+        s_slots.key[wave][i] = f.key;
+        s_slots.at[wave][i] = f.at;
+      }
+      if (lane == f.lane) (second ? key[1] : key[0]) = ~0ull;
+    }
   }
   __syncthreads();
   if (wave == 0) {
-    Least l = nothing();
-    uint64_t late = ~0ull, mine = ~0ull;           // of the lane's token that becomes old enough, and of its accepted one
-    int late_at = 0, slot = len + lane;            // (slot: of accepted token `lane`)
-    const uint64_t begin = static_cast<uint64_t>(lane < count && weight ? weight_key(begins[lane]) : weight_key(0.f)) << 32 | static_cast<uint32_t>(next + lane);
-    if (full) {
-      for (int w = 0; w < kWaves; ++w) take(l, s_key[w][lane], s_at[w][lane]);
-      late_at = s_late[lane];
-      if (late_at != INT32_MAX) late = static_cast<uint64_t>(weight_key(weight ? weight[late_at] : 0.f)) << 32 | static_cast<uint32_t>(newest + 1 + lane);
-    }
-    const int age = max(a.s.recent, 1);
-    const int first = max(cap - len, 0);
-    for (int j = first; j < count; ++j) {
-      if (lane <= j - age && (j == first || lane == j - age) && next + lane >= a.s.sinks) mine = begin;
-      // the least of the lane's, and of the wavefront's: whose it is with it (lane, kind)
-      uint64_t key = l.key;
-      int at = l.at, who = lane;
-      if (lane < j && late < key) key = late, at = late_at, who = 64 + lane;
-      if (mine < key) key = mine, at = slot, who = 128 + lane;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t k = __shfl_xor(key, d);
-        const int t = __shfl_xor(at, d), w = __shfl_xor(who, d);
-        if (k < key || (k == key && (t < at || (t == at && w < who)))) key = k, at = t, who = w;
+    int slot = len + lane;                         // of accepted token `lane`
+    if (want > 0) {
+      const int late_at = s_late[lane];
+      const uint64_t begin = key_of(lane < count && weight ? begins[lane] : 0.f, next + lane);
+      uint64_t late = ~0ull, mine = ~0ull;         // of the lane's token that becomes old enough, and of its accepted one
+      if (late_at != INT32_MAX) late = key_of(weight ? weight[late_at] : 0.f, newest + 1 + lane);
+      const int age = max(a.s.recent, 1);
+      Walk order(s_slots);
+      for (int j = first; j < count; ++j) {
+        if (lane <= j - age && (j == first || lane == j - age) && next + lane >= a.s.sinks) mine = begin;
+        uint64_t key = order.key;
+        int at = key == ~0ull ? 0 : order.at, kind = 0;
+        const auto look = [&](uint64_t k, int t, int kd) {
+          if (k < key || (k == key && k != ~0ull && t < at)) key = k, at = t, kind = kd;
+        };
+        if (lane < j) look(late, late_at, 1);
+        look(mine, slot, 2);
+        const First f = first_of_wave(key, at);
+        if (lane == j) slot = f.at;                // (nobody may go: slot 0)
+        if (lane == f.lane) {
+          if (kind == 0) order.step();
+          if (kind == 1) late = ~0ull;
+          if (kind == 2) mine = ~0ull;
+        }
       }
-      if (lane == j) slot = at;
-      if (key == ~0ull) continue;                  // (nobody may go: slot 0)
-      const int kind = who >> 6, whose = who & 63;
-      if (kind == 1 && lane == whose) late = ~0ull;
-      if (kind == 2 && lane == whose) mine = ~0ull;
-      if (kind != 0) continue;
-      // the segment again, without the slots that are taken: half of the wavefront its slots, all of it the leasts of the others of `whose`
-      const int segment = at / kSegment, i = segment * kSegment + (lane & 31);
-      const int p = pos[min(i, cap - 1)];
-      const float w = weight ? weight[min(i, cap - 1)] : 0.f;
-      Least again = nothing();
-      for (int e = whose + 64 * lane; e < used; e += 64 * 64) {
-        if (e == segment) continue;
-        const Least of = leasts[e];
-        take(again, of.key, of.at);
-      }
-      bool taken = i >= len;
-      for (int t = 0; t <= j; ++t) taken = taken || __builtin_amdgcn_readlane(slot, t) == i;
-      Least seg = nothing();
-      if (!taken) look_at(seg, i, p, w, a.s.sinks, newest);
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        take(seg, __shfl_xor(seg.key, d), __shfl_xor(seg.at, d));
-        take(again, __shfl_xor(again.key, d), __shfl_xor(again.at, d));
-      }
-      if (lane == 0) {
-        leasts[segment].key = seg.key;
-        leasts[segment].at = seg.at;
-      }
-      if (lane == whose) {
-        l = seg;
-        take(l, again.key, again.at);
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");           // (the next to look at the segment reads what lane 0 has written)
     }
     if (lane < count) {
       s_slot[lane] = slot;
@@ -444,15 +522,14 @@ __global__ __launch_bounds__(kThreads) void accept_append_kernel(AcceptArgs a) {
     }
   }
   __syncthreads();
-  // rows: half a wavefront a token, lanes 0..15 its K row, 16..31 its V row.  Of tokens in one slot the last stays
-  for (int j = wave; j < count; j += kThreads / 64) {
+  // of tokens in one slot the last stays
+  for (int j = wave; j < count; j += kWaves) {
     const int slot = s_slot[j];
     bool last = true;
     for (int k = j + 1; k < count; ++k) last = last && s_slot[k] != slot;
     if (lane >= 32 || !last) continue;
-    const int c16 = lane & 15, grp = c16 >> 2, p = c16 & 3;
-    const bool is_v = lane >= 16;
-    const uint4 row = reinterpret_cast<const uint4*>(is_v ? a.v_draft : a.k_draft)[((static_cast<int64_t>(seq) * a.n + path[j]) * a.s.hkv + kvh) * 16 + c16];
+    const int grp = c16 >> 2, p = c16 & 3;
+    const uint4 row = j == wave ? first_row : row_of(j);
     uint8_t* side = is_v ? a.s.v : a.s.k;
     if constexpr (BITS == 16) {
       reinterpret_cast<uint4*>(side)[(static_cast<int64_t>(item) * cap + slot) * 16 + c16] = row;
