@@ -171,6 +171,8 @@ try:
     _call.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.rdkv_decode_attn, lib.rdkv_cache_append)))
     _call.bind_slots(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.rdkv_slots_append, lib.rdkv_slots_decode_attn, lib.rdkv_slots_read, lib.rdkv_slots_fill, lib.rdkv_slots_fill_workspace_bytes)))
+    _call.bind_tree(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.rdkv_slots_tree_attn, lib.rdkv_slots_tree_workspace_bytes, lib.rdkv_slots_accept, lib.rdkv_slots_accept_workspace_bytes)))
 except ImportError as e:
     _call = None
     warnings.warn(f"_rdkv_call.so is not built or does not fit this PyTorch ({e}): a decode step takes the host 2 us more; "
@@ -473,26 +475,23 @@ def rdkv_prompt_attn_bf16(Q, K, V, seq_lens, hq, hkv, head_dim=128, window=0, si
     """(out, lse).  Each of Q, K, V and out is either flat (ragged [heads][T_s][head_dim] blocks: one dimension, or rows of head_dim) or
     [tokens, heads, head_dim] (tokens of the batch one after another; a view of wider rows will do); out is laid out as Q unless it is given.
     lse: float32, ragged [hq][T_s]."""
-    c = rdkv_prompt()
-    _check(lib.rdkv_prompt_default(ctypes.byref(c)))
-    lens = (ctypes.c_int32 * max(len(seq_lens), 1))(*[_int32("seq_lens", x) for x in seq_lens])
-    c.batch, c.seq_lens = len(seq_lens), ctypes.cast(lens, ctypes.POINTER(ctypes.c_int32))
-    for name, x in (("hq", hq), ("hkv", hkv), ("head_dim", head_dim), ("window", window), ("sinks", sinks)):
-        setattr(c, name, _int32(name, x))
-    c.score_cap = float(score_cap)
-    if c.score_cap == 0 and score_cap != 0:            # (0 is no cap)
+    n, hq, hkv, d = len(seq_lens), _int32("hq", hq), _int32("hkv", hkv), _int32("head_dim", head_dim)
+    lens = (ctypes.c_int32 * max(n, 1))(*[_int32("seq_lens", x) for x in seq_lens])
+    cap = float(score_cap)
+    if cap != 0 and ctypes.c_float(cap).value == 0:    # (0 is no cap)
         raise ValueError(f"score_cap = {score_cap} is 0 in 32 bits")
-    device, tokens, d = Q.device, sum(max(x, 0) for x in lens[:len(seq_lens)]), c.head_dim
-    c.q_stride, c.k_stride, c.v_stride = (_rows_of(t, name, tokens, h, d, device) for t, name, h in ((Q, "Q", c.hq), (K, "K", c.hkv), (V, "V", c.hkv)))
+    device, tokens = Q.device, sum(max(x, 0) for x in lens[:n])
+    strides = _rows_of(Q, "Q", tokens, hq, d, device), _rows_of(K, "K", tokens, hkv, d, device), _rows_of(V, "V", tokens, hkv, d, device)
     if slopes is not None:
-        c.slopes = _tensor(slopes, (c.hq,), torch.float32, device, "slopes").data_ptr()
+        _tensor(slopes, (hq,), torch.float32, device, "slopes")
     if out is None:
-        out = torch.empty((tokens, c.hq, d) if Q.dim() == 3 else Q.shape, dtype=torch.bfloat16, device=device)
-    c.out_stride = _rows_of(out, "out", tokens, c.hq, d, device)
+        out = torch.empty((tokens, hq, d) if Q.dim() == 3 else Q.shape, dtype=torch.bfloat16, device=device)
+    out_stride = _rows_of(out, "out", tokens, hq, d, device)
     if lse is None:
-        lse = torch.empty(tokens * c.hq, dtype=torch.float32, device=device)
+        lse = torch.empty(tokens * hq, dtype=torch.float32, device=device)
     else:
-        _tensor(lse.view(-1), (tokens * c.hq,), torch.float32, device, "lse")
+        _tensor(lse.view(-1), (tokens * hq,), torch.float32, device, "lse")
+    c = rdkv_prompt(n, hq, hkv, d, lens, _int32("window", window), _int32("sinks", sinks), cap, _ptr(slopes), *strides, out_stride)
     with _at(device):
         _check(lib.rdkv_prompt_attn_bf16(ctypes.byref(c), Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), lse.data_ptr(), _stream()))
     return out, lse
@@ -707,6 +706,11 @@ def _drafted(slots, q, k_draft, v_draft):
 
 def rdkv_slots_tree_attn(slots, q, k_draft, v_draft, parent, counts=None, out=None, stats=None, workspace=None):
     """(out, stats): bfloat16 [batch, n, hq, 128], float32 [batch, n, hq, 2]; what belongs to drafted tokens from counts on stays as it was."""
+    done = _fast(slots) and _call.slots_tree(slots.address, _stream(), slots.device.index, q, k_draft, v_draft, parent, counts, out, stats, workspace)
+    if done:
+        if done[0] != RDKV_OK:
+            _check(done[0])
+        return done[1:]
     n = _drafted(slots, q, k_draft, v_draft)
     _tensor(parent, (slots.batch, n), torch.int32, slots.device, "parent")
     if counts is not None:
@@ -729,6 +733,11 @@ def rdkv_slots_tree_attn(slots, q, k_draft, v_draft, parent, counts=None, out=No
 
 def rdkv_slots_accept(slots, q, k_draft, v_draft, path, stats, slot=None, workspace=None):
     """The slots that the accepted tokens took: int32 [batch, hkv, m], -1 behind a path's end.  A cache without weights needs neither q nor stats (None)."""
+    done = _fast(slots) and _call.slots_accept(slots.address, _stream(), slots.device.index, q, k_draft, v_draft, path, stats, slot, workspace)
+    if done:
+        if done[0] != RDKV_OK:
+            _check(done[0])
+        return done[1]
     n = _drafted(slots, q, k_draft, v_draft)
     if path.dim() != 2:
         raise ValueError(f"path must be [batch, m]: got {tuple(path.shape)}")

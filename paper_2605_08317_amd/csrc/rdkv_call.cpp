@@ -1,5 +1,5 @@
 // The calls of a decode loop, from Python in native code: rdkv_decode_attn and rdkv_cache_append, and rdkv_slots_append,
-// rdkv_slots_decode_attn, rdkv_slots_read and rdkv_slots_fill.
+// rdkv_slots_decode_attn, rdkv_slots_read, rdkv_slots_fill, rdkv_slots_tree_attn and rdkv_slots_accept.
 //
 // A decode step of a short context takes the GPU 5.2 us.  Through ctypes it took the host 7.4: 3.6 in the call itself, 2.5 for
 // two result tensors made from Python and the rest for converting arguments one by one.  Here the tensors are unpacked and
@@ -32,6 +32,10 @@ decltype(&rdkv_slots_decode_attn) g_slots_decode = nullptr;
 decltype(&rdkv_slots_read) g_slots_read = nullptr;
 decltype(&rdkv_slots_fill) g_slots_fill = nullptr;
 decltype(&rdkv_slots_fill_workspace_bytes) g_slots_fill_bytes = nullptr;
+decltype(&rdkv_slots_tree_attn) g_slots_tree = nullptr;
+decltype(&rdkv_slots_tree_workspace_bytes) g_slots_tree_bytes = nullptr;
+decltype(&rdkv_slots_accept) g_slots_accept = nullptr;
+decltype(&rdkv_slots_accept_workspace_bytes) g_slots_accept_bytes = nullptr;
 
 // a contiguous tensor's memory
 bool pointer(PyObject* o, void** p) {
@@ -145,6 +149,20 @@ PyObject* bind_slots(PyObject*, PyObject* const* args, Py_ssize_t n) {
   g_slots_read = reinterpret_cast<decltype(g_slots_read)>(a[2]);
   g_slots_fill = reinterpret_cast<decltype(g_slots_fill)>(a[3]);
   g_slots_fill_bytes = reinterpret_cast<decltype(g_slots_fill_bytes)>(a[4]);
+  Py_RETURN_NONE;
+}
+
+// bind_tree(addresses of rdkv_slots_tree_attn, rdkv_slots_tree_workspace_bytes, rdkv_slots_accept, rdkv_slots_accept_workspace_bytes)
+PyObject* bind_tree(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  long long a[4];
+  if (n != 4 || !integers(args, 4, a)) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "bind_tree takes four addresses");
+    return nullptr;
+  }
+  g_slots_tree = reinterpret_cast<decltype(g_slots_tree)>(a[0]);
+  g_slots_tree_bytes = reinterpret_cast<decltype(g_slots_tree_bytes)>(a[1]);
+  g_slots_accept = reinterpret_cast<decltype(g_slots_accept)>(a[2]);
+  g_slots_accept_bytes = reinterpret_cast<decltype(g_slots_accept_bytes)>(a[3]);
   Py_RETURN_NONE;
 }
 
@@ -325,6 +343,100 @@ PyObject* slots_fill(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// The drafted tokens of a tree: q (or None), k_draft, v_draft; n of them a sequence
+struct Drafted {
+  void *q = nullptr, *k, *v;
+  int64_t n = 0;
+  bool ok = false;
+  Drafted(const SlotsCall& c, PyObject* const* args) {
+    if (!THPVariable_CheckExact(args[1])) return;
+    const at::Tensor& t = THPVariable_Unpack(args[1]);
+    if (t.dim() != 4 || t.size(1) > INT32_MAX) return;
+    n = t.size(1);
+    const int64_t row[4] = {c.s->batch, n, c.s->hkv, c.s->head_dim}, q_row[4] = {row[0], n, c.s->hq, row[3]};
+    ok = (args[0] == Py_None || c.plain(args[0], at::kBFloat16, at::IntArrayRef(q_row, 4), &q)) &&
+         c.plain(args[1], at::kBFloat16, at::IntArrayRef(row, 4), &k) && c.plain(args[2], at::kBFloat16, at::IntArrayRef(row, 4), &v);
+  }
+};
+// a workspace: the tensor given, or a new one of so many bytes (`made`)
+bool workspace(const SlotsCall& c, PyObject* o, size_t* bytes, void** p, at::Tensor* made) {
+  if (o == Py_None) {
+    *made = at::empty({std::max<int64_t>(static_cast<int64_t>(*bytes), 16)}, c.options(at::kByte));
+    *p = made->data_ptr();
+    return true;
+  }
+  if (!THPVariable_CheckExact(o)) return false;
+  *bytes = static_cast<size_t>(THPVariable_Unpack(o).numel());
+  return c.plain(o, at::kByte, THPVariable_Unpack(o).sizes(), p);
+}
+
+// slots_tree(.., q, k_draft, v_draft, parent, counts or None, out or None, stats or None, workspace or None) -> (status, out, stats) or None
+PyObject* slots_tree(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  const SlotsCall c(args, n_args, 11);
+  if (!c.ok) return nullptr;
+  const Drafted d(c, args + 3);
+  if (!g_slots_tree || !g_slots_tree_bytes || !d.ok || !d.q) Py_RETURN_NONE;
+  const int64_t batch = c.s->batch, row[4] = {batch, d.n, c.s->hq, c.s->head_dim}, stat[4] = {batch, d.n, c.s->hq, 2}, tokens[2] = {batch, d.n};
+  const at::IntArrayRef rows(row, 4), pairs(stat, 4);
+  void *parent, *counts = nullptr, *out, *stats, *ws;
+  if (!c.plain(args[6], at::kInt, at::IntArrayRef(tokens, 2), &parent) ||
+      (args[7] != Py_None && !c.plain(args[7], at::kInt, at::IntArrayRef(tokens, 1), &counts)) ||
+      (args[8] != Py_None && !c.plain(args[8], at::kBFloat16, rows, &out)) || (args[9] != Py_None && !c.plain(args[9], at::kFloat, pairs, &stats)))
+    Py_RETURN_NONE;
+  size_t bytes = g_slots_tree_bytes(c.s, static_cast<int32_t>(d.n));
+  at::Tensor new_out, new_stats, new_ws;
+  if (!workspace(c, args[10], &bytes, &ws, &new_ws)) Py_RETURN_NONE;
+  if (args[8] == Py_None) {
+    new_out = at::empty(rows, c.options(at::kBFloat16));
+    out = new_out.data_ptr();
+  }
+  if (args[9] == Py_None) {
+    new_stats = at::empty(pairs, c.options(at::kFloat));
+    stats = new_stats.data_ptr();
+  }
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = g_slots_tree(c.s, static_cast<int32_t>(d.n), d.q, d.k, d.v, static_cast<const int32_t*>(parent), static_cast<const int32_t*>(counts), out,
+                        static_cast<float*>(stats), ws, bytes, c.stream);
+  Py_END_ALLOW_THREADS
+  THPObjectPtr py_out(result(std::move(new_out), args[8])), py_stats(result(std::move(new_stats), args[9]));
+  return py_out && py_stats ? Py_BuildValue("(iNN)", status, py_out.release(), py_stats.release()) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
+// slots_accept(.., q or None, k_draft, v_draft, path, stats or None, slot or None, workspace or None) -> (status, slot) or None
+PyObject* slots_accept(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  const SlotsCall c(args, n_args, 10);
+  if (!c.ok) return nullptr;
+  const Drafted d(c, args + 3);
+  if (!g_slots_accept || !g_slots_accept_bytes || !d.ok || !THPVariable_CheckExact(args[6])) Py_RETURN_NONE;
+  const at::Tensor& t = THPVariable_Unpack(args[6]);
+  if (t.dim() != 2 || t.size(1) > INT32_MAX) Py_RETURN_NONE;
+  const int64_t batch = c.s->batch, m = t.size(1), tokens[2] = {batch, m}, stat[4] = {batch, d.n, c.s->hq, 2}, taken[3] = {batch, c.s->hkv, m};
+  const at::IntArrayRef slots(taken, 3);
+  void *path, *stats = nullptr, *slot, *ws;
+  if (!c.plain(args[6], at::kInt, at::IntArrayRef(tokens, 2), &path) ||
+      (args[7] != Py_None && !c.plain(args[7], at::kFloat, at::IntArrayRef(stat, 4), &stats)) || (args[8] != Py_None && !c.plain(args[8], at::kInt, slots, &slot)))
+    Py_RETURN_NONE;
+  size_t bytes = g_slots_accept_bytes(c.s);
+  at::Tensor made, new_ws;
+  if (!workspace(c, args[9], &bytes, &ws, &new_ws)) Py_RETURN_NONE;
+  if (args[8] == Py_None) {
+    made = at::empty(slots, c.options(at::kInt));
+    slot = made.data_ptr();
+  }
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = g_slots_accept(c.s, static_cast<int32_t>(d.n), static_cast<int32_t>(m), d.q, d.k, d.v, static_cast<const int32_t*>(path), static_cast<const float*>(stats),
+                          static_cast<int32_t*>(slot), ws, bytes, c.stream);
+  Py_END_ALLOW_THREADS
+  THPObjectPtr out(result(std::move(made), args[8]));
+  return out ? Py_BuildValue("(iN)", status, out.release()) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode)), METH_FASTCALL, nullptr},
@@ -334,6 +446,9 @@ PyMethodDef methods[] = {
     {"slots_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_decode)), METH_FASTCALL, nullptr},
     {"slots_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_read)), METH_FASTCALL, nullptr},
     {"slots_fill", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_fill)), METH_FASTCALL, nullptr},
+    {"bind_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind_tree)), METH_FASTCALL, nullptr},
+    {"slots_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_tree)), METH_FASTCALL, nullptr},
+    {"slots_accept", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_accept)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rdkv_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

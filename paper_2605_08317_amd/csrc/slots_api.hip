@@ -246,6 +246,7 @@ rdkv_status rdkv_slots_tree_attn(const rdkv_slots* s, int32_t n, const void* q, 
   const slots::TreePlan plan = slots::plan_tree(a.items, n * a.s.g, s->capacity, s->bits);
   a.wide = plan.wide;
   a.row_groups = plan.row_groups;
+  a.slot_pieces = plan.slot_pieces;
   a.pieces = plan.pieces;
   a.part_acc = static_cast<float*>(workspace);
   a.part_ml = a.part_acc + plan.part_rows(a.items) * kHeadDim;

@@ -21,12 +21,14 @@ struct TreeArgs {
   float* part_acc;                      // [item][row group][piece][rows of a group][128]
   float* part_ml;                       // the same rows: [4]
   int32_t items, n;
-  int32_t wide, row_groups, pieces;     // plan_tree, as the workspace's size has it
+  int32_t wide, row_groups, slot_pieces, pieces;        // plan_tree, as the workspace's size has it
 };
 
-// wide: wavefronts of a workgroup that share out rows, 32 each; the others share out slots.  Pieces of an item's slots.
+// wide: wavefronts of a workgroup that share out rows, 32 each; the others share out slots.  Pieces of an item's slots, and all of them: with one
+// for the drafted tokens where the card has room for it, else these go with the last.
+constexpr int kLeast = 1;
 struct TreePlan {
-  int32_t wide, row_groups, pieces;
+  int32_t wide, row_groups, slot_pieces, pieces;
   size_t part_rows(int64_t items) const { return pieces == 1 ? 0 : static_cast<size_t>(items) * row_groups * pieces * 32 * wide; }
   size_t floats(int64_t items) const { return part_rows(items) * (kHeadDim + 4); }
 };
@@ -35,9 +37,10 @@ inline TreePlan plan_tree(int64_t items, int rows, int capacity, int bits) {
   p.wide = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || bits == 4 ? 4 : 8;
   p.row_groups = (rows + 32 * p.wide - 1) / (32 * p.wide);
   const int64_t groups = items * p.row_groups, card = bits == 16 ? 256 : 512;
-  const int64_t least = 2 * std::max(4 / p.wide, 1);          // tiles of a piece
+  const int64_t least = kLeast * (bits == 16 ? (p.wide == 8 ? 1 : 2) : 4 / p.wide);        // tiles of a piece
   const int64_t most = (static_cast<int64_t>(capacity) + kTileRows - 1) / kTileRows / least;
-  p.pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min(most, card / std::max<int64_t>(groups, 1))));
+  p.slot_pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min(most, card / std::max<int64_t>(groups, 1))));
+  p.pieces = p.slot_pieces > 1 && groups * (p.slot_pieces + 1) <= card ? p.slot_pieces + 1 : p.slot_pieces;
   return p;
 }
 

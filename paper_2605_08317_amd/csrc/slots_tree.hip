@@ -199,8 +199,7 @@ template <int BITS, int WR, bool GENERAL>
 __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 1) void tree_kernel(TreeArgs a) {
   constexpr int NW = kWaves<BITS, WR>;
   extern __shared__ __align__(256) uint8_t smem[];
-  __shared__ uint64_t s_sees[kTokens];
-  __shared__ int s_depth[kTokens], s_parent[kTokens];
+  __shared__ int s_depth[kTokens];
   __shared__ float s_ml[NW][32][4];
   constexpr int WS = NW / WR;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
@@ -212,32 +211,37 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
   const int count = a.counts ? min(max(a.counts[seq], 0), n) : n;
   if (rg * WR * 32 >= count * g) return;
 
-  // ancestors: a bit of each, and the token's own
-  if (tid < n) s_parent[tid] = a.parent[static_cast<int64_t>(seq) * n + tid];
-  __syncthreads();
-  if (tid < n) {
-    uint64_t sees = 1ull << tid;
-    for (int t = tid, p; (p = s_parent[t]) >= 0 && p < t; t = p) sees |= 1ull << p;
-    s_sees[tid] = sees;
-    s_depth[tid] = __popcll(sees) - 1;
-  }
-  __syncthreads();
-
   const int len = a.s.length(item), next = a.s.next[item];
+  int parent = lane < n ? a.parent[static_cast<int64_t>(seq) * n + lane] : -1;
   Row row;
   {
     const int r = (rg * WR + wr) * 32 + l32;
     row.there = r < count * g;
     row.index = min(r, rows - 1);
     row.token = row.index / g;
-    row.sees = s_sees[row.token];
-    row.at = next + s_depth[row.token];
     row.slope = GENERAL && a.s.slopes ? a.s.slopes[kvh * g + row.index % g] : 0.f;
   }
   const int64_t q_row = (static_cast<int64_t>(seq) * n + row.token) * a.s.hkv * g + kvh * g + row.index % g;
   using Query = std::conditional_t<BITS == 16, Query16, Query4>;
   Query query;
   query.load(a.q + q_row * kHeadDim);
+  // ancestors: a bit of each, and the token's own; lane t token t's, twice as far up in each turn
+  {
+    uint64_t sees = 1ull << lane;
+    if (parent >= lane) parent = -1;
+#pragma unroll
+    for (int k = 1; k < kTokens; k *= 2) {
+      const uint64_t theirs = __shfl(sees, max(parent, 0));
+      const int further = __shfl(parent, max(parent, 0));
+      if (parent >= 0) {
+        sees |= theirs;
+        parent = further;
+      }
+    }
+    row.sees = __shfl(sees, row.token);
+    row.at = next + __popcll(row.sees) - 1;
+    if (wave == 0) s_depth[lane] = __popcll(sees) - 1;                   // (read behind the barriers of the drafted tokens)
+  }
   Scoring sc;
   sc.cap = a.s.cap;
   sc.inv_cap = a.s.cap > 0.f ? 1.f / a.s.cap : 0.f;
@@ -251,8 +255,9 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
   Out r;
   // this piece's slots: whole tiles of 64
   const int tiles = (len + kTileRows - 1) / kTileRows;
-  const int begin = static_cast<int>(static_cast<int64_t>(tiles) * piece / a.pieces) * kTileRows;
-  const int end = min(len, static_cast<int>(static_cast<int64_t>(tiles) * (piece + 1) / a.pieces) * kTileRows);
+  const int from = min(piece, a.slot_pieces), to = min(piece + 1, a.slot_pieces);                // (of the drafted tokens' own piece: none)
+  const int begin = static_cast<int>(static_cast<int64_t>(tiles) * from / a.slot_pieces) * kTileRows;
+  const int end = min(len, static_cast<int>(static_cast<int64_t>(tiles) * to / a.slot_pieces) * kTileRows);
   const int32_t* pos = a.s.pos + static_cast<int64_t>(item) * a.s.capacity;
   const uint32_t lds0 = lds_address(smem);
   const int prow = tid >> 4;
@@ -506,6 +511,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_ro
   const int64_t first = slot * group_rows + row % group_rows;
   const bool scored = a.s.cap > 0.f || a.s.slopes;
   float m = kNoScore, top = kNoScore, unit = 1.f;
+#pragma unroll 4
   for (int p = 0; p < a.pieces; ++p) {
     const float4 ml = *reinterpret_cast<const float4*>(a.part_ml + (first + static_cast<int64_t>(p) * group_rows) * 4);
     m = fmaxf(m, ml.x);
@@ -515,6 +521,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_ro
   const float factor = scored ? kLog2e : unit * kRootLog2e;
   float l = 0.f;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
   for (int p = 0; p < a.pieces; ++p) {
     const int64_t at = first + static_cast<int64_t>(p) * group_rows;
     const float4 ml = *reinterpret_cast<const float4*>(a.part_ml + at * 4);
