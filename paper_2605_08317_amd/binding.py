@@ -172,7 +172,8 @@ try:
     _call.bind_slots(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.rdkv_slots_append, lib.rdkv_slots_decode_attn, lib.rdkv_slots_read, lib.rdkv_slots_fill, lib.rdkv_slots_fill_workspace_bytes)))
     _call.bind_tree(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-        lib.rdkv_slots_tree_attn, lib.rdkv_slots_tree_workspace_bytes, lib.rdkv_slots_accept, lib.rdkv_slots_accept_workspace_bytes)))
+        lib.rdkv_slots_tree_attn, lib.rdkv_slots_tree_workspace_bytes, lib.rdkv_slots_accept, lib.rdkv_slots_accept_workspace_bytes,
+        lib.rdkv_prompt_attn_bf16)))
 except ImportError as e:
     _call = None
     warnings.warn(f"_rdkv_call.so is not built or does not fit this PyTorch ({e}): a decode step takes the host 2 us more; "
@@ -475,6 +476,11 @@ def rdkv_prompt_attn_bf16(Q, K, V, seq_lens, hq, hkv, head_dim=128, window=0, si
     """(out, lse).  Each of Q, K, V and out is either flat (ragged [heads][T_s][head_dim] blocks: one dimension, or rows of head_dim) or
     [tokens, heads, head_dim] (tokens of the batch one after another; a view of wider rows will do); out is laid out as Q unless it is given.
     lse: float32, ragged [hq][T_s]."""
+    done = _fast(Q) and _call.prompt(_stream(), Q.device.index, Q, K, V, seq_lens, hq, hkv, head_dim, window, sinks, score_cap, slopes, out, lse)
+    if done:
+        if done[0] != RDKV_OK:
+            _check(done[0])
+        return done[1:]
     n, hq, hkv, d = len(seq_lens), _int32("hq", hq), _int32("hkv", hkv), _int32("head_dim", head_dim)
     lens = (ctypes.c_int32 * max(n, 1))(*[_int32("seq_lens", x) for x in seq_lens])
     cap = float(score_cap)
@@ -613,7 +619,7 @@ def _at(device):
 
 
 def _fast(slots):
-    """Whether a call may go through the native code, which looks at the tensors itself: the slots lie on the current device."""
+    """Whether a call may go through the native code, which looks at the tensors itself: the slots (or a tensor) lie on the current device."""
     index = slots.device.index
     return _call is not None and index is not None and _current_device is not None and _current_device() == index
 

@@ -1,5 +1,6 @@
 // The calls of a decode loop, from Python in native code: rdkv_decode_attn and rdkv_cache_append, and rdkv_slots_append,
-// rdkv_slots_decode_attn, rdkv_slots_read, rdkv_slots_fill, rdkv_slots_tree_attn and rdkv_slots_accept.
+// rdkv_slots_decode_attn, rdkv_slots_read, rdkv_slots_fill, rdkv_slots_tree_attn and rdkv_slots_accept; and
+// rdkv_prompt_attn_bf16.
 //
 // A decode step of a short context takes the GPU 5.2 us.  Through ctypes it took the host 7.4: 3.6 in the call itself, 2.5 for
 // two result tensors made from Python and the rest for converting arguments one by one.  Here the tensors are unpacked and
@@ -7,7 +8,8 @@
 // given 1054 -> 988 us.  What is not a plain tensor call (an argument that is no tensor, one of a subclass, one that is not
 // contiguous) is left to the ctypes path, which says what is wrong with it: the functions then return None.  (On slot
 // caches, host us with results made: append 6.8 -> 4.3, step 9.3 -> 6.5, read 8.7 -> 5.3, a fill of four launches 19.7 -> 14.4.  The GPU
-// takes 4.6 for an append to 2 items of 1000 slots, 3.0 for a read of a few rows.)
+// takes 4.6 for an append to 2 items of 1000 slots, 3.0 for a read of a few rows.  Trees 12.1 -> 8.2 of 13, accepting 15.3 -> 10.0 of 15,
+// prompts 14.0 -> 7.5 of 10.4 for 600 tokens.)
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -34,6 +36,7 @@ decltype(&rdkv_slots_fill) g_slots_fill = nullptr;
 decltype(&rdkv_slots_fill_workspace_bytes) g_slots_fill_bytes = nullptr;
 decltype(&rdkv_slots_tree_attn) g_slots_tree = nullptr;
 decltype(&rdkv_slots_tree_workspace_bytes) g_slots_tree_bytes = nullptr;
+decltype(&rdkv_prompt_attn_bf16) g_prompt = nullptr;
 decltype(&rdkv_slots_accept) g_slots_accept = nullptr;
 decltype(&rdkv_slots_accept_workspace_bytes) g_slots_accept_bytes = nullptr;
 
@@ -152,17 +155,19 @@ PyObject* bind_slots(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// bind_tree(addresses of rdkv_slots_tree_attn, rdkv_slots_tree_workspace_bytes, rdkv_slots_accept, rdkv_slots_accept_workspace_bytes)
+// bind_tree(addresses of rdkv_slots_tree_attn, rdkv_slots_tree_workspace_bytes, rdkv_slots_accept, rdkv_slots_accept_workspace_bytes,
+//           rdkv_prompt_attn_bf16)
 PyObject* bind_tree(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  long long a[4];
-  if (n != 4 || !integers(args, 4, a)) {
-    if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "bind_tree takes four addresses");
+  long long a[5];
+  if (n != 5 || !integers(args, 5, a)) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "bind_tree takes five addresses");
     return nullptr;
   }
   g_slots_tree = reinterpret_cast<decltype(g_slots_tree)>(a[0]);
   g_slots_tree_bytes = reinterpret_cast<decltype(g_slots_tree_bytes)>(a[1]);
   g_slots_accept = reinterpret_cast<decltype(g_slots_accept)>(a[2]);
   g_slots_accept_bytes = reinterpret_cast<decltype(g_slots_accept_bytes)>(a[3]);
+  g_prompt = reinterpret_cast<decltype(g_prompt)>(a[4]);
   Py_RETURN_NONE;
 }
 
@@ -303,18 +308,20 @@ PyObject* slots_read(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// a whole number of 32 bits
+bool number(PyObject* o, int32_t* x) {
+  int over = 0;
+  const long long v = PyLong_CheckExact(o) ? PyLong_AsLongLongAndOverflow(o, &over) : -1 - static_cast<long long>(INT32_MAX) - 1;
+  *x = static_cast<int32_t>(v);
+  return over == 0 && v >= INT32_MIN && v <= INT32_MAX;
+}
+
 // slots_fill(.., K, V, seq_lens, w_tok or None, first) -> status or None
 PyObject* slots_fill(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   const SlotsCall c(args, n_args, 8);
   if (!c.ok) return nullptr;
   if (!g_slots_fill || !g_slots_fill_bytes || !PyList_CheckExact(args[5]) || !PyLong_CheckExact(args[7])) Py_RETURN_NONE;
-  const auto number = [](PyObject* o, int32_t* x) {
-    int over = 0;
-    const long long v = PyLong_CheckExact(o) ? PyLong_AsLongLongAndOverflow(o, &over) : -1 - static_cast<long long>(INT32_MAX) - 1;
-    *x = static_cast<int32_t>(v);
-    return over == 0 && v >= INT32_MIN && v <= INT32_MAX;
-  };
   const Py_ssize_t n = PyList_GET_SIZE(args[5]);
   int32_t first;
   if (n > INT32_MAX || !number(args[7], &first)) Py_RETURN_NONE;
@@ -340,6 +347,82 @@ PyObject* slots_fill(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   status = g_slots_fill(c.s, first, static_cast<int32_t>(n), lens.data(), k, v, static_cast<const float*>(w), bytes > 0 ? ws.data_ptr() : nullptr, bytes, c.stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(status);
+  END_HANDLE_TH_ERRORS
+}
+
+// prompt(stream, index of the device, Q, K, V, seq_lens, hq, hkv, head_dim, window, sinks, score_cap, slopes or None, out or None, lse or None)
+//   -> (status, out, lse) or None
+PyObject* prompt(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  long long a[2];
+  if (n_args != 15 || !integers(args, 2, a)) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "prompt takes fifteen arguments");
+    return nullptr;
+  }
+  void* stream = reinterpret_cast<void*>(a[0]);
+  const auto device = static_cast<at::DeviceIndex>(a[1]);
+  rdkv_prompt c = {};
+  if (!g_prompt || !PyList_CheckExact(args[5]) || !number(args[6], &c.hq) || !number(args[7], &c.hkv) || !number(args[8], &c.head_dim) ||
+      !number(args[9], &c.window) || !number(args[10], &c.sinks) || !(PyFloat_CheckExact(args[11]) || PyLong_CheckExact(args[11])))
+    Py_RETURN_NONE;
+  const Py_ssize_t n = PyList_GET_SIZE(args[5]);
+  if (n > INT32_MAX || c.hq < 1 || c.hkv < 1 || c.head_dim < 1) Py_RETURN_NONE;
+  std::vector<int32_t> lens(n + 1);
+  int64_t tokens = 0;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (!number(PyList_GET_ITEM(args[5], i), &lens[i])) Py_RETURN_NONE;
+    tokens += std::max(lens[i], 0);
+  }
+  constexpr int32_t kMany = 65536;                 // (so that no product of sizes overflows)
+  if (tokens > INT32_MAX || c.hq > kMany || c.hkv > kMany || c.head_dim > kMany) Py_RETURN_NONE;
+  c.batch = static_cast<int32_t>(n);
+  c.seq_lens = lens.data();
+  const double cap = PyFloat_AsDouble(args[11]);
+  if (cap == -1.0 && PyErr_Occurred()) return nullptr;
+  c.score_cap = static_cast<float>(cap);
+  if (c.score_cap == 0.f && cap != 0.0) Py_RETURN_NONE;
+  // flat rows, or [tokens, heads, head_dim] of rows whose heads lie side by side
+  const auto rows = [&](PyObject* o, int64_t heads, int64_t* stride, void** p) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.device().index() != device || t.scalar_type() != at::kBFloat16) return false;
+    const int64_t d = c.head_dim;
+    *p = t.data_ptr();
+    *stride = 0;
+    if (t.dim() == 1 || t.dim() == 2) return t.is_contiguous() && t.numel() == tokens * heads * d && (t.dim() == 1 || t.size(1) == d);
+    if (t.dim() != 3 || t.size(0) != tokens || t.size(1) != heads || t.size(2) != d) return false;
+    *stride = tokens > 1 ? t.stride(0) : heads * d;
+    return tokens == 0 || (t.stride(2) == 1 && (heads == 1 || t.stride(1) == d));
+  };
+  void *q, *k, *v, *out, *lse, *slopes = nullptr;
+  if (!rows(args[2], c.hq, &c.q_stride, &q) || !rows(args[3], c.hkv, &c.k_stride, &k) || !rows(args[4], c.hkv, &c.v_stride, &v)) Py_RETURN_NONE;
+  const auto plain = [&](PyObject* o, int64_t numbers, void** p) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    *p = t.data_ptr();
+    return t.is_cuda() && t.device().index() == device && t.scalar_type() == at::kFloat && t.is_contiguous() && t.numel() == numbers;
+  };
+  if (args[12] != Py_None && (!plain(args[12], c.hq, &slopes) || THPVariable_Unpack(args[12]).dim() != 1)) Py_RETURN_NONE;
+  c.slopes = static_cast<const float*>(slopes);
+  if ((args[13] != Py_None && !rows(args[13], c.hq, &c.out_stride, &out)) || (args[14] != Py_None && !plain(args[14], tokens * c.hq, &lse))) Py_RETURN_NONE;
+  const auto options = at::TensorOptions().device(at::kCUDA, device);
+  at::Tensor new_out, new_lse;
+  if (args[13] == Py_None) {
+    const at::Tensor& t = THPVariable_Unpack(args[2]);
+    new_out = at::empty(t.sizes(), options.dtype(at::kBFloat16));
+    out = new_out.data_ptr();
+    c.out_stride = t.dim() == 3 ? static_cast<int64_t>(c.hq) * c.head_dim : 0;
+  }
+  if (args[14] == Py_None) {
+    new_lse = at::empty({tokens * c.hq}, options.dtype(at::kFloat));
+    lse = new_lse.data_ptr();
+  }
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = g_prompt(&c, q, k, v, out, static_cast<float*>(lse), stream);
+  Py_END_ALLOW_THREADS
+  THPObjectPtr py_out(result(std::move(new_out), args[13])), py_lse(result(std::move(new_lse), args[14]));
+  return py_out && py_lse ? Py_BuildValue("(iNN)", status, py_out.release(), py_lse.release()) : nullptr;
   END_HANDLE_TH_ERRORS
 }
 
@@ -447,6 +530,7 @@ PyMethodDef methods[] = {
     {"slots_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_read)), METH_FASTCALL, nullptr},
     {"slots_fill", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_fill)), METH_FASTCALL, nullptr},
     {"bind_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind_tree)), METH_FASTCALL, nullptr},
+    {"prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prompt)), METH_FASTCALL, nullptr},
     {"slots_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_tree)), METH_FASTCALL, nullptr},
     {"slots_accept", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(slots_accept)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

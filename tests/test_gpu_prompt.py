@@ -211,3 +211,42 @@ def test_the_same_twice():
     x = [laid(t, lens, h, False) for t, h in zip(inputs(23, lens, hq, hkv), (hq, hkv, hkv))]
     first, again = (b.rdkv_prompt_attn_bf16(*x, lens, hq, hkv) for _ in range(2))
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_native_calls_do_as_the_others(monkeypatch):
+    """Layouts, results made and given, and refusals, through the native code and without it."""
+    lens, hq, hkv = [70, 0, 33], 8, 2
+    q, k, v = inputs(61, lens, hq, hkv)
+    slopes, tokens = torch.rand(hq, device="cuda"), sum(lens)
+    rows = [laid(x, lens, h, True) for x, h in ((q, hq), (k, hkv), (v, hkv))]
+    flat = [laid(x, lens, h, False) for x, h in ((q, hq), (k, hkv), (v, hkv))]
+
+    def every():
+        made = [*b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv), *b.rdkv_prompt_attn_bf16(*flat, lens, hq, hkv, window=20, sinks=2, score_cap=9, slopes=slopes),
+                *b.rdkv_prompt_attn_bf16(flat[0].view(-1, D), rows[1], flat[2], lens, hq, hkv, 128, score_cap=9.5)]
+        assert [x.shape for x in made[::2]] == [(tokens, hq, D), (tokens * hq * D,), (tokens * hq, D)]
+        out, lse = torch.full((tokens, hq + 1, D), 7.0, dtype=BF, device="cuda"), torch.zeros((hq, tokens), device="cuda")
+        r = b.rdkv_prompt_attn_bf16(flat[0], rows[1], rows[2], tuple(lens), hq, hkv, out=out[:, 1:], lse=lse)
+        assert r[1] is lse and torch.all(out[:, 0] == 7)
+        empty = b.rdkv_prompt_attn_bf16(*(x[:0] for x in rows), [0, 0], hq, hkv)
+        assert empty[0].shape == (0, hq, D) and empty[1].shape == (0,)
+        for bad in (lambda: b.rdkv_prompt_attn_bf16(rows[0].float(), *rows[1:], lens, hq, hkv), lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hq),
+                    lambda: b.rdkv_prompt_attn_bf16(*rows, [70, 33, 1], hq, hkv), lambda: b.rdkv_prompt_attn_bf16(rows[0], flat[1].cpu(), rows[2], lens, hq, hkv),
+                    lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv, score_cap=1e-60), lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv, window=2.5),
+                    lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv, slopes=slopes[:4]), lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv, out=rows[1]),
+                    lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv, lse=lse.double()), lambda: b.rdkv_prompt_attn_bf16(*(x[:, ::2] for x in rows), lens, hq // 2, hkv // 2),
+                    lambda: b.rdkv_prompt_attn_bf16(*rows, [70, 2 ** 32, 33], hq, hkv)):
+            with pytest.raises(ValueError):
+                bad()
+        for bad in (lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv, window=-1), lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv, score_cap=-1.0),
+                    lambda: b.rdkv_prompt_attn_bf16(*rows, lens, hq, hkv, score_cap=math.nan), lambda: b.rdkv_prompt_attn_bf16(*rows, [70, -1, 33], hq, hkv)):
+            with pytest.raises(b.RdkvError):
+                bad()
+        return made + [out, lse]
+    assert b._call is not None
+    native = every()
+    monkeypatch.setattr(b, "_call", None)
+    for x, y in zip(native, every()):
+        assert x.dtype == y.dtype and x.shape == y.shape
+        same = torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+        assert same

@@ -321,6 +321,13 @@ def test_accepting_with_all_that_a_cache_has(bits, kw):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("kw", [dict(), dict(recent=200, sinks=4, decay=0.99), dict(recent=100, tracked=False)], ids=str)
+def test_long_paths_into_long_caches(bits, kw):
+    """More segments than a workgroup has threads, and tokens that become old enough on the way in many of them."""
+    accept(np.random.default_rng(33), [33100, 500], 1, 1, 33100, bits, 64, [range(64), range(30)], **kw)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 def test_paths_that_end_and_paths_that_repeat(bits):
     """A path ends at the first index that is none; one that names a token twice takes it in twice."""
     rng = np.random.default_rng(29)
@@ -440,6 +447,62 @@ def test_on_another_stream_and_twice_the_same(bits):
         got = b.rdkv_slots_tree_attn(s, q, k, v, parent)
     torch.cuda.current_stream().wait_stream(stream)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_native_calls_do_as_the_others(monkeypatch):
+    """Results made and given, with and without counts and a workspace, through the native code and without it."""
+    rng = np.random.default_rng(53)
+    s, _ = cached(rng, [300, 290], 8, 2, 300, 16)
+    q, k, v = drafted(rng, 2, 9, 8, 2)
+    parent, path, counts = cuda(np.stack([tree(rng, 9)] * 2), I32), cuda([[0, 1, 2], [3, -1, 0]], I32), cuda([9, 4], I32)
+
+    def every():
+        t = s.__copy__()
+        for name in ("k", "v", "pos", "weight", "lens", "next_pos"):
+            setattr(t, name, getattr(s, name).clone())
+        made = [*b.rdkv_slots_tree_attn(t, q, k, v, parent)]
+        given = [torch.zeros_like(x) for x in made]
+        r = b.rdkv_slots_tree_attn(t, q, k, v, parent, counts, given[0], given[1], t.tree_workspace(9))
+        assert r[0] is given[0] and r[1] is given[1]
+        one = b.rdkv_slots_tree_attn(t, q, k, v, parent, stats=given[1].clone())
+        a = b.rdkv_slots_accept(t, q, k, v, path, made[1])
+        slot = torch.zeros_like(a)
+        assert b.rdkv_slots_accept(t, q, k, v, path, made[1], slot, t.accept_workspace()) is slot
+        assert torch.equal(a[1, :, 1:], torch.full_like(a[1, :, 1:], -1))
+        return made + given + [one[0], a, slot, t.k, t.v, t.pos, t.weight, t.lens, t.next_pos]
+    assert b._call is not None
+    native = every()
+    monkeypatch.setattr(b, "_call", None)
+    for x, y in zip(native, every()):
+        assert x.dtype == y.dtype and x.shape == y.shape
+        same = torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+        assert same
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_the_binding_refuses(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(b, "_call", None)
+    s, q = b.Slots(2, 8, 2, 100), torch.zeros((2, 3, 8, D), device="cuda", dtype=BF)
+    k, wide = torch.zeros((2, 3, 2, D), device="cuda", dtype=BF), torch.zeros((2, 3, 8, 2 * D), device="cuda", dtype=BF)[..., ::2]
+    parent, path, stats = torch.zeros((2, 3), device="cuda", dtype=I32), torch.zeros((2, 2), device="cuda", dtype=I32), torch.zeros((2, 3, 8, 2), device="cuda")
+    small = torch.zeros(64, device="cuda", dtype=torch.uint8)
+    for call in (lambda: b.rdkv_slots_tree_attn(s, q.float(), k, k, parent), lambda: b.rdkv_slots_tree_attn(s, q, k, k[:, :2], parent), lambda: b.rdkv_slots_tree_attn(s, wide, k, k, parent),
+                 lambda: b.rdkv_slots_tree_attn(s, q, k.cpu(), k, parent), lambda: b.rdkv_slots_tree_attn(s, q, k[0], k, parent), lambda: b.rdkv_slots_tree_attn(s, q, k, k, parent.long()),
+                 lambda: b.rdkv_slots_tree_attn(s, q, k, k, parent, counts=parent), lambda: b.rdkv_slots_tree_attn(s, q, k, k, parent, out=stats),
+                 lambda: b.rdkv_slots_tree_attn(s, q, k, k, parent, stats=stats[..., 0]), lambda: b.rdkv_slots_tree_attn(s, q, k, k, parent, workspace=stats),
+                 lambda: b.rdkv_slots_accept(s, q, k, k, path[0], stats), lambda: b.rdkv_slots_accept(s, q, k, k, path.float(), stats), lambda: b.rdkv_slots_accept(s, q, k, k, path, stats[:1]),
+                 lambda: b.rdkv_slots_accept(s, q[:, :2], k, k, path, stats), lambda: b.rdkv_slots_accept(s, q, k, k, path, stats, slot=path), lambda: b.rdkv_slots_accept(s, q, k, k, path, stats, workspace=small.cpu())):
+        with pytest.raises(ValueError):
+            call()
+    many = torch.zeros((2, 65, 2, D), device="cuda", dtype=BF)
+    for call in (lambda: b.rdkv_slots_accept(s, None, k, k, path, stats), lambda: b.rdkv_slots_accept(s, q, k, k, path, None),
+                 lambda: b.rdkv_slots_accept(s, torch.zeros((2, 65, 8, D), device="cuda", dtype=BF), many, many, path, torch.zeros((2, 65, 8, 2), device="cuda")),
+                 lambda: b.rdkv_slots_accept(s, q, k, k, torch.zeros((2, 65), device="cuda", dtype=I32), stats),
+                 lambda: b.rdkv_slots_accept(s, q, k, k, path, stats, workspace=small), lambda: b.rdkv_slots_tree_attn(b.Slots(2, 8, 2, 9000), q, k, k, parent, workspace=small)):
+        with pytest.raises(b.RdkvError):
+            call()
+    assert not s.lens.any() and not s.next_pos.any()
 
 
 @pytest.mark.parametrize("bits", [16, 4])
