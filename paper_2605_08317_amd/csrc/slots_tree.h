@@ -26,7 +26,6 @@ struct TreeArgs {
 
 // wide: wavefronts of a workgroup that share out rows, 32 each; the others share out slots.  Pieces of an item's slots, and all of them: with one
 // for the drafted tokens where the card has room for it, else these go with the last.
-constexpr int kLeast = 1;
 struct TreePlan {
   int32_t wide, row_groups, slot_pieces, pieces;
   size_t part_rows(int64_t items) const { return pieces == 1 ? 0 : static_cast<size_t>(items) * row_groups * pieces * 32 * wide; }
@@ -36,10 +35,14 @@ inline TreePlan plan_tree(int64_t items, int rows, int capacity, int bits) {
   TreePlan p;
   p.wide = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || bits == 4 ? 4 : 8;
   p.row_groups = (rows + 32 * p.wide - 1) / (32 * p.wide);
-  const int64_t groups = items * p.row_groups, card = bits == 16 ? 256 : 512;
-  const int64_t least = kLeast * (bits == 16 ? (p.wide == 8 ? 1 : 2) : 4 / p.wide);        // tiles of a piece
-  const int64_t most = (static_cast<int64_t>(capacity) + kTileRows - 1) / kTileRows / least;
-  p.slot_pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min(most, card / std::max<int64_t>(groups, 1))));
+  const int64_t groups = items * p.row_groups;
+  const int64_t tiles = (static_cast<int64_t>(capacity) + kTileRows - 1) / kTileRows;
+  const int64_t stage = bits == 16 ? (p.wide == 8 ? 1 : 2) : 4 / p.wide;            // tiles that a workgroup has at once: no piece is smaller
+  // As many workgroups as run at once: one a compute unit in bf16, two in 4 bits; in 4 bits twice as many, for items of different lengths, where a piece
+  // still has 32 stages (32 x 8 x 5000 .. 8192 slots 358 -> 342 us; 4 x 8 x 131072 of 16 stages 164 -> 170).
+  int64_t card = bits == 16 ? 256 : 512;
+  if (bits == 4 && 2 * card / std::max<int64_t>(groups, 1) * 32 * stage <= tiles) card *= 2;
+  p.slot_pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min(tiles / stage, card / std::max<int64_t>(groups, 1))));
   p.pieces = p.slot_pieces > 1 && groups * (p.slot_pieces + 1) <= card ? p.slot_pieces + 1 : p.slot_pieces;
   return p;
 }

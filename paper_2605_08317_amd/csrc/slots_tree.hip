@@ -22,7 +22,7 @@ struct Row {
   bool there;
   int token, at;                          // its position
   uint64_t sees;                          // drafted tokens
-  float slope;
+  float slope, bias;                      // bias: of a key at the cache's next position
 };
 
 struct Out {                              // of a lane's row, over 32 or 64 lanes' channels
@@ -111,30 +111,34 @@ struct Scoring {
   bool scored, biased;                    // scores are made of products at once; of differences later
   int window, sinks;
 };
-// Products to scores, -inf where hidden, a step at a time over all of them.  four(k, at): positions of products 4 k .. + 3.  hide(i): there is no slot,
-// asked if `some` are none
-template <bool GENERAL, int N, class Four, class Hide>
-__device__ __forceinline__ void to_scores(const Scoring& sc, const Row& row, float (&x)[N], bool some, Four four, Hide hide) {
+// Products to scores, -inf where hidden, a step at a time over all of them.  Of products 4 k .. + 3: away(k, d), how far their positions are from the
+// cache's next one; four(k, at), their positions.  hide(i): there is no slot, asked if `some` are none
+template <bool GENERAL, int N, class Away, class Four, class Hide>
+__device__ __forceinline__ void to_scores(const Scoring& sc, const Row& row, float (&x)[N], bool some, Away away, Four four, Hide hide) {
   if constexpr (GENERAL) {
-    if (sc.cap > 0.f) {
-      tanh_all(x, sc.natural * sc.inv_cap);
+    const float unit = sc.cap > 0.f ? sc.cap : sc.natural;
+    if (sc.cap > 0.f) tanh_all(x, sc.natural * sc.inv_cap);
+    if (sc.biased) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] *= sc.cap;
-    } else if (sc.biased) {
+      for (int k = 0; k < N / 4; ++k) {
+        float d[4];
+        away(k, d);
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] *= sc.natural;
+        for (int j = 0; j < 4; ++j) x[4 * k + j] = __builtin_fmaf(x[4 * k + j], unit, __builtin_fmaf(-row.slope, d[j], row.bias));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else if (sc.cap > 0.f) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] *= unit;
     }
-    if (sc.biased || sc.window > 0) {
+    if (sc.window > 0) {
 #pragma unroll
       for (int k = 0; k < N / 4; ++k) {
         int at[4];
         four(k, at);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int away = row.at - at[j];
-          if (sc.biased) x[4 * k + j] = __builtin_fmaf(-row.slope, static_cast<float>(away), x[4 * k + j]);
-          if (sc.window > 0 && away >= sc.window && at[j] >= sc.sinks) x[4 * k + j] = -INFINITY;
-        }
+        for (int j = 0; j < 4; ++j)
+          if (row.at - at[j] >= sc.window && at[j] >= sc.sinks) x[4 * k + j] = -INFINITY;
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -159,7 +163,7 @@ constexpr int kStageLds = 256 * 2 * kRowBytes;                  // of all of the
 constexpr int kPosLds = 8 * 4 * 64 * 4;                         // positions of the wavefronts' tiles, up to four buffers
 constexpr int kDraftLds = kTokens * 2 * kRowBytes;
 constexpr int kJoinLds = 4 * 4 * 16 * 64 * 4;                   // four wavefronts' results
-constexpr int kMetaLds = kKMeta + 1024 + 256;                   // of a wavefront
+constexpr int kMetaLds = kKMeta + 1024 + 512;                   // of a wavefront
 
 // Values of a 4-bit tile that are not finite, to the rows that give their slots something.  odd: lanes 4 (slot / 4) + group whose metadata are not; lds:
 // 2 KiB of the wavefront's; p: probabilities, register i of slot 32 half + i.
@@ -240,6 +244,7 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
     }
     row.sees = __shfl(sees, row.token);
     row.at = next + __popcll(row.sees) - 1;
+    row.bias = -row.slope * static_cast<float>(row.at - next);
     if (wave == 0) s_depth[lane] = __popcll(sees) - 1;                   // (read behind the barriers of the drafted tokens)
   }
   Scoring sc;
@@ -310,7 +315,13 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
 #pragma unroll
           for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
         }
-        to_scores<GENERAL>(sc, row, x, left < kMine, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[2 * k + half]; },
+        to_scores<GENERAL>(sc, row, x, left < kMine, [&](int k, float* d) __attribute__((always_inline)) {
+          const int4 at = where[2 * k + half];
+          d[0] = static_cast<float>(next - at.x);
+          d[1] = static_cast<float>(next - at.y);
+          d[2] = static_cast<float>(next - at.z);
+          d[3] = static_cast<float>(next - at.w);
+        }, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[2 * k + half]; },
                            [&](int i) __attribute__((always_inline)) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) >= left; });
         add_rows16<kStepsN, kCareful>(x, sc.factor, vt, 0.f, r);
       }
@@ -338,7 +349,10 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
     for (; t < t1; t += WS) {
       const int left = end - t * kTileRows;
       put_k_meta(meta, k, left);
-      if constexpr (GENERAL) reinterpret_cast<int*>(meta + kKMeta + 1024)[lane] = at;
+      if constexpr (GENERAL) {
+        reinterpret_cast<int*>(meta + kKMeta + 1024)[lane] = at;
+        reinterpret_cast<float*>(meta + kKMeta + 1024 + 256)[lane] = static_cast<float>(next - at);
+      }
       wave_lds_order();
       floatx16 s[2];
       scores4(codes, k, meta, query, s);
@@ -347,7 +361,9 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = s[i >> 4][i & 15];
       const int4* where = reinterpret_cast<const int4*>(meta + kKMeta + 1024) + 8 * half;
-      to_scores<GENERAL>(sc, row, x, left < kTileRows, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[k]; },
+      to_scores<GENERAL>(sc, row, x, left < kTileRows,
+                         [&](int k, float* d) __attribute__((always_inline)) { *reinterpret_cast<int4*>(d) = where[16 + k]; },
+                         [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[k]; },
                          [&](int i) __attribute__((always_inline)) { return 32 * half + i >= left; });
       // with a window, values that are not finite are kept out, and go to those rows that see them afterwards
       const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v, left);
@@ -410,7 +426,10 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
 #pragma unroll
         for (int i = 0; i < 32; ++i) x[i] *= own.natural;
       }
-      to_scores<GENERAL>(own, row, x, true, [&](int k, int* at) __attribute__((always_inline)) {
+      to_scores<GENERAL>(own, row, x, true, [&](int k, float* d) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[j] = -static_cast<float>(s_depth[min(token(4 * k + j), n - 1)]);
+      }, [&](int k, int* at) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) at[j] = next + s_depth[min(token(4 * k + j), n - 1)];
       }, [&](int i) __attribute__((always_inline)) { return (row.sees >> token(i) & 1) == 0; });
