@@ -57,8 +57,8 @@ __device__ __forceinline__ void look_at(Least& l, int slot, int pos, float weigh
 // Rows of a pass over the slots: up to 64, in LDS as operands, with what probabilities are made with.
 constexpr int kRows = 64;
 struct __align__(16) RowTable {
-  float most[kRows], share[kRows];                   // largest score, decay over the sum
-  float natural[kRows], slope[kRows];                // what makes products scores; bias
+  float less[kRows], share[kRows];                   // minus the largest score, and the bias at the cache's next position; decay over the sum
+  float natural[kRows], slope[kRows];                // what makes products scores; the bias of a step further
   int at[kRows];                                     // position
 };
 constexpr int kQueryLds = kRows / 32 * 9 * 1024;     // [32 rows][operand][lane], the last operand 4-bit rows' sums
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
   const int count = path_length(path, a.m, a.n), rows = count * g;
   if (count == 0) return;
   const int len = a.s.length(item), next = a.s.next[item], cap = a.s.capacity;
-  const bool scored = GENERAL && (a.s.cap > 0.f || a.s.slopes), full = len + count > cap;
+  const bool full = len + count > cap;
   const float inv_cap = a.s.cap > 0.f ? 1.f / a.s.cap : 0.f, old = power(a.s.decay, count);
   const int32_t* pos = a.s.pos + static_cast<int64_t>(item) * cap;
   float* weight = a.s.weight + static_cast<int64_t>(item) * cap;
@@ -106,9 +106,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
       if (half == 0) {
         const int to = 32 * wave + l32;
         const bool there = r0 + to < rows && st.y != 0.f;
-        s_row.most[to] = there ? st.x : INFINITY;              // (no row: probabilities of 0)
+        const float slope = a.s.slopes ? a.s.slopes[kvh * g + r % g] : 0.f;
+        s_row.less[to] = there ? -slope * static_cast<float>(j) - st.x : -INFINITY;        // (no row: probabilities of 0)
         s_row.share[to] = there ? power(a.s.decay, count - 1 - j) / st.y : 0.f;
-        s_row.slope[to] = a.s.slopes ? a.s.slopes[kvh * g + r % g] : 0.f;
+        s_row.slope[to] = slope;
         s_row.at[to] = next + j;
         s_row.natural[to] = q.unit * kRoot;
       }
@@ -117,42 +118,37 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
   };
   // What the rows in LDS give a lane's slot (TOKENS: one of the path's) at `place`; scores(block): their products.
   const auto given = [&](auto own, int r0, int place, auto scores) __attribute__((always_inline)) {
+    const float back = GENERAL ? static_cast<float>(next - place) : 0.f;
     float sum = 0.f;
     for (int b = 0; b < kRows / 32 && r0 + 32 * b < rows; ++b) {
       const floatx16 s = scores(b);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int r = 32 * b + 8 * k + 4 * half;
-        const float4 most = *reinterpret_cast<const float4*>(s_row.most + r), share = *reinterpret_cast<const float4*>(s_row.share + r);
+        const float4 less = *reinterpret_cast<const float4*>(s_row.less + r), share = *reinterpret_cast<const float4*>(s_row.share + r);
         const float4 natural = *reinterpret_cast<const float4*>(s_row.natural + r);
-        const float ms[4] = {most.x, most.y, most.z, most.w}, sh[4] = {share.x, share.y, share.z, share.w}, na[4] = {natural.x, natural.y, natural.z, natural.w};
-        float e[4];
-        if (scored) {
+        const float sh[4] = {share.x, share.y, share.z, share.w}, na[4] = {natural.x, natural.y, natural.z, natural.w};
+        float e[4], le[4] = {less.x, less.y, less.z, less.w};
+        if (GENERAL && a.s.slopes) {
+          const float4 slope = *reinterpret_cast<const float4*>(s_row.slope + r);
+          const float sl[4] = {slope.x, slope.y, slope.z, slope.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) le[j] = __builtin_fmaf(-sl[j], back, le[j]);
+        }
+        if (GENERAL && a.s.cap > 0.f) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) e[j] = s[4 * k + j] * na[j];
-          if (a.s.cap > 0.f) {
-            tanh_all(e, inv_cap);
+          tanh_all(e, inv_cap);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] *= a.s.cap;
-          }
+          for (int j = 0; j < 4; ++j) e[j] = __builtin_fmaf(e[j], a.s.cap, le[j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) e[j] = __builtin_fmaf(s[4 * k + j], na[j], -ms[j]);
+          for (int j = 0; j < 4; ++j) e[j] = __builtin_fmaf(s[4 * k + j], na[j], le[j]);
         }
-        if constexpr (GENERAL || decltype(own)::value) {
+        if ((GENERAL && a.s.window > 0) || decltype(own)::value) {
           const int4 ats = *reinterpret_cast<const int4*>(s_row.at + r);
           const int away[4] = {ats.x - place, ats.y - place, ats.z - place, ats.w - place};
-          if (a.s.slopes) {
-            const float4 slope = *reinterpret_cast<const float4*>(s_row.slope + r);
-            const float sl[4] = {slope.x, slope.y, slope.z, slope.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = __builtin_fmaf(-sl[j], static_cast<float>(away[j]), e[j]);
-          }
-          if (scored) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] -= ms[j];
-          }
-          if (a.s.window > 0) {
+          if (GENERAL && a.s.window > 0) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               if (away[j] >= a.s.window && place >= a.s.sinks) e[j] = -INFINITY;
