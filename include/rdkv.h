@@ -394,7 +394,7 @@ int32_t rdkv_k_row_words_max(void);
  * probabilities meet V rounded to bf16, once, over a reference of the row's.
  * Allocates and waits for nothing; may be recorded under graph capture (lengths by value).  Pointers are aligned to 16 bytes, strides
  * multiples of 8, from heads x 128 to 2^23; out shares no memory with the inputs.  T_s >= 0.  Limits: the sum of hq T_s is
- * below 2^31; 64 sequences a launch, and a launch has less than 2^24 workgroups (of 32 to 256 rows of a head).
+ * below 2^31; 64 sequences a launch, and a launch has less than 2^24 workgroups (each 128 rows of a head or less).
  */
 typedef struct rdkv_prompt {
   int32_t batch;            /* number of sequences */

@@ -26,12 +26,14 @@ struct Args {
   int32_t window, sinks;
   float cap;
   int32_t T[kSeqs];
+  int32_t first[kSeqs];                 // its first workgroup
   int64_t token0[kSeqs];                // tokens of the batch before the sequence's first
 };
 
-// rows of a workgroup's, and its workgroups at most, of a launch
-inline int64_t workgroups(int longest, int n_seqs, int hq) { return (static_cast<int64_t>(longest) + 127) / 128 * n_seqs * hq; }
-hipError_t launch(const Args& a, int longest, hipStream_t st);
+constexpr int kRows = 128;              // of a workgroup
+// a sequence's workgroups: of an XCD as many as of another, so that the same heads of all sequences are on the same one
+inline int64_t workgroups(int T, int hq) { return ((static_cast<int64_t>(T) + kRows - 1) / kRows * hq + 7) / 8 * 8; }
+hipError_t launch(const Args& a, int grid, hipStream_t st);
 
 }  // namespace prompt
 }  // namespace rdkv

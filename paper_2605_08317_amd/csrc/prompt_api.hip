@@ -1,6 +1,7 @@
 // Host side of the attention of whole prompts (rdkv_prompt_*): argument checks and launches.
 #include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "prompt.h"
 
@@ -52,10 +53,9 @@ rdkv_status rdkv_prompt_attn_bf16(const rdkv_prompt* p, const void* Q, const voi
   }
   if (rows >= (1ll << 31)) return fail(RDKV_ERR_SHAPE, "sum of hq*T_s exceeds 2^31 rows");
   for (int s0 = 0; s0 < p->batch; s0 += prompt::kSeqs) {
-    const int n = std::min(prompt::kSeqs, p->batch - s0);
-    if (prompt::workgroups(*std::max_element(p->seq_lens + s0, p->seq_lens + s0 + n), n, p->hq) >= (1ll << 24))
-      return fail(RDKV_ERR_SHAPE, "%d sequences of up to %d tokens, %d heads: a launch has at most 2^24 workgroups", n,
-                  *std::max_element(p->seq_lens + s0, p->seq_lens + s0 + n), p->hq);
+    int64_t grid = 0;
+    for (int i = s0; i < std::min(s0 + prompt::kSeqs, p->batch); ++i) grid += prompt::workgroups(p->seq_lens[i], p->hq);
+    if (grid >= (1ll << 24)) return fail(RDKV_ERR_SHAPE, "sequences %d .. take %lld workgroups: a launch has less than 2^24", s0, static_cast<long long>(grid));
   }
   if (rows == 0) return RDKV_OK;
   if (!Q || !K || !V || !out) return fail(RDKV_ERR_INVALID_ARG, "Q, K, V and out must not be null");
@@ -72,17 +72,23 @@ rdkv_status rdkv_prompt_attn_bf16(const rdkv_prompt* p, const void* Q, const voi
   a.window = p->window;
   a.sinks = p->sinks;
   a.cap = p->score_cap;
-  int64_t token = 0;
+  int64_t token0 = 0;
   for (int s0 = 0; s0 < p->batch; s0 += prompt::kSeqs) {
     a.n_seqs = std::min(prompt::kSeqs, p->batch - s0);
-    int longest = 0;
+    std::pair<int32_t, int64_t> seqs[prompt::kSeqs];                // (length, first token), the longest first
     for (int i = 0; i < a.n_seqs; ++i) {
-      a.T[i] = p->seq_lens[s0 + i];
-      a.token0[i] = token;
-      token += a.T[i];
-      longest = std::max(longest, a.T[i]);
+      seqs[i] = {p->seq_lens[s0 + i], token0};
+      token0 += seqs[i].first;
     }
-    if (longest > 0) RDKV_HIP(prompt::launch(a, longest, static_cast<hipStream_t>(stream)));
+    std::stable_sort(seqs, seqs + a.n_seqs, [](const auto& x, const auto& y) { return x.first > y.first; });
+    int grid = 0;
+    for (int i = 0; i < a.n_seqs; ++i) {
+      a.T[i] = seqs[i].first;
+      a.token0[i] = seqs[i].second;
+      a.first[i] = grid;
+      grid += static_cast<int>(prompt::workgroups(a.T[i], p->hq));
+    }
+    if (grid > 0) RDKV_HIP(prompt::launch(a, grid, static_cast<hipStream_t>(stream)));
   }
   return RDKV_OK;
 }

@@ -21,17 +21,17 @@ __device__ __forceinline__ int64_t first_of(const Side& s, int64_t token0, int h
   return s.tokens ? token0 * s.row + head * kHeadDim : (token0 * heads + static_cast<int64_t>(head) * T) * kHeadDim;
 }
 
-template <int NW, bool GENERAL>
-__global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(Args a) {
+template <bool GENERAL>
+__global__ __launch_bounds__(2 * kRows, 2) void prompt_kernel(Args a) {
   extern __shared__ __align__(256) uint8_t smem[];
-  constexpr int kRows = 32 * NW, kCopies = 16 / NW;       // kCopies: of a wavefront and tile
+  constexpr int NW = kRows / 32, kCopies = 16 / NW;         // kCopies: of a wavefront, for a tile of K or V
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  const int items = a.n_seqs * a.hkv, pairs = a.n_seqs * a.hq;
-  const int level = static_cast<int>(blockIdx.x) / pairs, pair = static_cast<int>(blockIdx.x) % pairs;
-  const int item = pair % items, seq = item / a.hkv, kvh = item % a.hkv, head = kvh * (a.hq / a.hkv) + pair / items;
-  const int T = a.T[seq];
-  const int q0 = (static_cast<int>(gridDim.x) / pairs - 1 - level) * kRows;
-  if (q0 >= T) return;
+  // The sequence, the longest is first; of that all heads' last rows first.  Heads of a KV head are beside each other on an XCD where that can be.
+  const int mine = static_cast<int>(blockIdx.x), seq = __popcll(__ballot(lane < a.n_seqs && a.first[lane] <= mine)) - 1;
+  const int T = a.T[seq], unit = mine - a.first[seq], levels = (T + kRows - 1) / kRows;
+  const int level = unit / a.hq, kvh = unit % a.hq % a.hkv, head = kvh * (a.hq / a.hkv) + unit % a.hq / a.hkv;
+  if (level >= levels) return;
+  const int q0 = (levels - 1 - level) * kRows;
   const int64_t token0 = a.token0[seq];
   const uint16_t* Kh = a.K + first_of(a.k, token0, a.hkv, kvh, T);
   const uint16_t* Vh = a.V + first_of(a.v, token0, a.hkv, kvh, T);
@@ -61,6 +61,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(Args a) {
   const uint16_t* q = a.Q + first_of(a.q, token0, a.hq, head, T) + static_cast<int64_t>(min(row, T - 1)) * a.q.row + 8 * half;
 #pragma unroll
   for (int kb = 0; kb < 8; ++kb) q_op[kb] = *reinterpret_cast<const bf16x8*>(q + 16 * kb);
+  fetch_k(0);                                        // (on their way together with the queries)
+  fetch_v(0);
+  fetch_k(1);
 #pragma unroll
   for (int kb = 0; kb < 8; ++kb) arrived(q_op[kb]);
   const float slope = GENERAL && a.slopes ? a.slopes[head] : 0.f, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
@@ -207,9 +210,6 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(Args a) {
   };
   const auto walk = [&]() __attribute__((always_inline)) {
     begin();
-    fetch_k(0);
-    fetch_v(0);
-    fetch_k(1);
     tile_barrier<2 * kCopies>();
     floatx16 even[2], odd[2];
     const auto open = [&](int it) __attribute__((always_inline)) {       // K of tile it + 1 and V of tile it are there, K of tile it and V of tile it - 1 done with
@@ -318,21 +318,20 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(Args a) {
     a.lse[token0 * a.hq + static_cast<int64_t>(head) * T + row] = total == 0.f ? -INFINITY : __builtin_fmaf(m * factor, kLn2, __logf(total));
 }
 
-template <int NW, bool GENERAL>
-hipError_t start(const Args& a, int longest, hipStream_t st) {
+template <bool GENERAL>
+hipError_t start(const Args& a, int grid, hipStream_t st) {
   constexpr int lds = 2 * kRing * kTileBytes;
-  const hipError_t e = RDKV_ALLOW_LDS((prompt_kernel<NW, GENERAL>), lds);
+  const hipError_t e = RDKV_ALLOW_LDS(prompt_kernel<GENERAL>, lds);
   if (e != hipSuccess) return e;
-  const int tiles = (longest + 32 * NW - 1) / (32 * NW);
-  hipLaunchKernelGGL((prompt_kernel<NW, GENERAL>), dim3(tiles * a.n_seqs * a.hq), dim3(64 * NW), lds, st, a);
+  hipLaunchKernelGGL(prompt_kernel<GENERAL>, dim3(grid), dim3(2 * kRows), lds, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch(const Args& a, int longest, hipStream_t st) {
+hipError_t launch(const Args& a, int grid, hipStream_t st) {
   const bool general = a.cap > 0.f || a.slopes;      // (a window takes no scores of its own)
-  return general ? start<4, true>(a, longest, st) : start<4, false>(a, longest, st);
+  return general ? start<true>(a, grid, st) : start<false>(a, grid, st);
 }
 
 }  // namespace prompt
