@@ -406,6 +406,7 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
 
   // the drafted tokens themselves
   if (piece == a.pieces - 1) {
+    if constexpr (BITS == 4 && GENERAL) __syncthreads();           // (add_odd's flags lie where the rows come)
     const int64_t first = (static_cast<int64_t>(seq) * n * a.s.hkv + kvh) * kRowBytes;
     fetch_rows(reinterpret_cast<const uint8_t*>(a.k_draft) + first, reinterpret_cast<const uint8_t*>(a.v_draft) + first, a.s.hkv * kRowBytes, n - 1, kTokens, lds0);
     tile_barrier<0>();
