@@ -39,7 +39,7 @@ struct Out {                              // of a lane's row, over 32 or 64 lane
 // Scores of n products to probabilities; factor makes scores exponents of 2.  Of differences from the reference: a large number that scores have
 // in common costs nothing.
 template <int N>
-__device__ __forceinline__ void softmax(const float (&x)[N], float factor, float shift, Out& r, float (&p)[N]) {
+__device__ __forceinline__ void refer(const float (&x)[N], float factor, Out& r) {
   float top = x[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
@@ -54,13 +54,17 @@ __device__ __forceinline__ void softmax(const float (&x)[N], float factor, float
 #pragma unroll
       for (int i = 0; i < 16; ++i) r.o[t][i] *= alpha;
   }
-  float sum[4] = {};
+}
+template <int N>
+__device__ __forceinline__ void softmax(const float (&x)[N], float factor, float shift, Out& r, float (&p)[N]) {
+  refer(x, factor, r);
+  float sums[2] = {};                                // (as elsewhere: the same sum of the same scores)
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i] - r.m, factor, shift));
-    sum[i & 3] += p[i];
+    sums[i & 1] += p[i];
   }
-  r.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  r.l += sums[0] + sums[1];
 }
 
 // o += P V for the channels of register group t; V's operands by value(step).  PARTED: some slots are hidden from some rows, and what is not finite
@@ -267,14 +271,10 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
   const uint32_t lds0 = lds_address(smem);
   const int prow = tid >> 4;
   const uint32_t k_at = 16 * k_piece(prow, tid & 15), v_at = 16 * v_piece(prow, tid & 15);
-  // rows first .. of bf16 keys and values, `stride` bytes apart, into LDS: K, then V behind `most` rows of them; rows past the last are it again
-  const auto fetch_rows = [&](const uint8_t* k, const uint8_t* v, uint32_t stride, int last, int most, uint32_t to) __attribute__((always_inline)) {
+  // `most` bf16 rows, `stride` bytes apart, into LDS; rows past the last are it again
+  const auto fetch_rows = [&](const uint8_t* from, uint32_t at, uint32_t stride, int last, int most, uint32_t to) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < most; i += 4 * NW) {
-      const uint32_t at = static_cast<uint32_t>(min(prow + i, last)) * stride;
-      copy_to_lds(k, at + k_at, to + i * kRowBytes + wave * 1024);
-      copy_to_lds(v, at + v_at, to + (most + i) * kRowBytes + wave * 1024);
-    }
+    for (int i = 0; i < most; i += 4 * NW) copy_to_lds(from, static_cast<uint32_t>(min(prow + i, last)) * stride + at, to + i * kRowBytes + wave * 1024);
   };
 
   // Careful (bf16): rows of V that a window hides from some query rows are kept from meeting their zeros, which make NaN of what is not finite.  Done
@@ -287,43 +287,154 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
     constexpr int kCopies = kSlots / (2 * NW) + (GENERAL ? 1 : 0);      // of a wavefront and stage
     const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
     const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
-    const int n_it = (end - begin + kSlots - 1) / kSlots;
+    constexpr uint32_t kSide = kSlots * kRowBytes;
+    const int n_it = (end - begin + kSlots - 1) / kSlots, mine = ws * kMine;
     uint8_t* s_pos = smem + kStageLds;
-    const auto fetch = [&](int it) __attribute__((always_inline)) {
-      const int first = begin + min(it, n_it - 1) * kSlots, buffer = it % kBuffers;
-      fetch_rows(K + static_cast<int64_t>(first) * kRowBytes, V + static_cast<int64_t>(first) * kRowBytes, kRowBytes, end - 1 - first, kSlots,
-                 lds0 + buffer * (kSlots * 2 * kRowBytes));
-      if constexpr (GENERAL) {
-        const int at = min(first + ws * kMine + lane, end - 1) - first;
-        copy_word_to_lds(pos + first, 4 * at, lds0 + kStageLds + (wave * kBuffers + buffer) * 256);
+    const auto k_of = [&](int it) { return lds0 + it % kBuffers * kSide; };
+    const auto v_of = [&](int it) { return lds0 + (kBuffers + it % kBuffers) * kSide; };
+    const auto fetch_k = [&](int it) __attribute__((always_inline)) {
+      const int first = begin + min(it, n_it - 1) * kSlots;
+      fetch_rows(K + static_cast<int64_t>(first) * kRowBytes, k_at, kRowBytes, end - 1 - first, kSlots, k_of(it));
+      if constexpr (GENERAL) copy_word_to_lds(pos + first, 4 * (min(first + mine + lane, end - 1) - first), lds0 + kStageLds + (wave * kBuffers + it % kBuffers) * 256);
+    };
+    const auto fetch_v = [&](int it) __attribute__((always_inline)) {
+      const int first = begin + min(it, n_it - 1) * kSlots;
+      fetch_rows(V + static_cast<int64_t>(first) * kRowBytes, v_at, kRowBytes, end - 1 - first, kSlots, v_of(it));
+    };
+    const auto left_of = [&](int it) { return end - begin - it * kSlots - mine - 4 * half; };
+    const auto finish = [&](int it, float (&x)[16 * kStepsN]) __attribute__((always_inline)) {
+      const int left = left_of(it);
+      const int4* where = reinterpret_cast<const int4*>(s_pos + (wave * kBuffers + it % kBuffers) * 256);
+      to_scores<GENERAL>(sc, row, x, left < kMine, [&](int k, float* d) __attribute__((always_inline)) {
+        const int4 at = where[2 * k + half];
+        d[0] = static_cast<float>(next - at.x);
+        d[1] = static_cast<float>(next - at.y);
+        d[2] = static_cast<float>(next - at.z);
+        d[3] = static_cast<float>(next - at.w);
+      }, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[2 * k + half]; },
+                         [&](int i) __attribute__((always_inline)) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) >= left; });
+    };
+    const auto multiply = [&](int it, float (&x)[16 * kStepsN]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int k = 0; k < kStepsN; ++k) {
+        const floatx16 s = scores16(k_of(it) + mine * kRowBytes + k_lane(), k, query);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
       }
     };
-    if (n_it > 0) {
+    if constexpr (kStepsN == 2 && !kCareful && !GENERAL) {
+      // a stage's softmax and P V, and between their instructions the products of the next (MORE): a line is one product and what the plain ALUs do
+      // meanwhile
+      const auto position = [&](auto more, int it, float (&x)[32], float (&next)[32]) __attribute__((always_inline)) {
+        constexpr bool kMore = decltype(more)::value;
+        refer(x, sc.factor, r);
+        float sums[2] = {}, e[3], y = (x[0] - r.m) * sc.factor;
+        union { uint32_t u[16]; bf16x8 op[4]; } p;
+        // exponential i, in order; what hangs on another one's result stands behind it
+        const auto make = [&](int i) __attribute__((always_inline)) {
+          const float now = y;
+          if (i < 31) y = (x[i + 1] - r.m) * sc.factor;
+          if (i < 32) e[i % 3] = __builtin_amdgcn_exp2f(now);
+          if (i > 0) sums[i & 1] += e[(i - 1) % 3];
+          if (i > 0 && (i & 1) == 0) p.u[(i >> 1) - 1] = pair_bf16(e[(i - 2) % 3], e[(i - 1) % 3]);
+        };
+        const uint32_t kt = k_of(it + 1) + mine * kRowBytes + k_lane(), vt = v_of(it) + mine * kRowBytes + v_lane();
+        constexpr int kAhead = 3;
+        bf16x8 op[kAhead];
+        const auto ask = [&](int i) __attribute__((always_inline)) {
+          if (i < 16) op[i % kAhead] = read_k(kt, i & 7, i >> 3);
+          else if (i < 32) op[i % kAhead] = read_v(vt, i & 3, (i >> 2) & 1, (i - 16) >> 3);
+        };
+        if constexpr (kMore) {
+          floatx16 s[2];
 #pragma unroll
-      for (int it = 0; it < kBuffers - 1; ++it) fetch(it);
+          for (int i = 0; i < kAhead; ++i) ask(i);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[i >> 3] = product(op[i % kAhead], query.op[i & 7], (i & 7) == 0 ? floatx16{} : s[i >> 3]);
+            ask(i + kAhead);
+            make(i);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) next[i] = s[i >> 4][i & 15];
+        } else {
+#pragma unroll
+          for (int i = 16; i < 16 + kAhead; ++i) ask(i);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) make(i);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          r.o[i & 3] = product(op[(i + 16) % kAhead], p.op[i >> 2], r.o[i & 3]);
+          ask(i + 16 + kAhead);
+          if (i < 8) {
+            make(16 + 2 * i);
+            make(17 + 2 * i);
+          } else if (i == 8) {
+            make(32);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        r.l += sums[0] + sums[1];
+        if constexpr (kMore) finish(it + 1, next);
+      };
+      // K of stage it + 1 and V of stage it are there, K of stage it and V of the one before are done with
+      const auto open = [&](int it) __attribute__((always_inline)) {
+        tile_barrier<kCopies * (kBuffers - 2)>();
+        fetch_k(it + kBuffers);
+        fetch_v(it + kBuffers - 1);
+      };
+      if (n_it > 0) {
+        fetch_k(0);
+#pragma unroll
+        for (int it = 0; it < kBuffers - 1; ++it) {
+          fetch_k(it + 1);
+          fetch_v(it);
+        }
+        tile_barrier<kCopies * (kBuffers - 1)>();
+        const int n_mine = max(0, (end - begin - mine + kSlots - 1) / kSlots);         // stages in which this wavefront has slots
+        float even[32], odd[32];
+        int it = 0;
+        if (n_mine > 0) {
+          multiply(0, even);
+          finish(0, even);
+        }
+        for (; it + 2 < n_mine; it += 2) {
+          open(it);
+          position(std::true_type{}, it, even, odd);
+          open(it + 1);
+          position(std::true_type{}, it + 1, odd, even);
+        }
+        if (it < n_mine) {
+          open(it);
+          if (it + 1 < n_mine) {
+            position(std::true_type{}, it, even, odd);
+            open(++it);
+            position(std::false_type{}, it, odd, even);
+          } else {
+            position(std::false_type{}, it, even, odd);
+          }
+          ++it;
+        }
+        for (; it < n_it; ++it) open(it);
+        tile_barrier<0>();
+      }
+    } else if (n_it > 0) {
+#pragma unroll
+      for (int it = 0; it < kBuffers - 1; ++it) {
+        fetch_k(it);
+        fetch_v(it);
+      }
       for (int it = 0; it < n_it; ++it) {
         tile_barrier<kCopies * (kBuffers - 2)>();
-        fetch(it + kBuffers - 1);
-        const int buffer = it % kBuffers, mine = ws * kMine, left = end - begin - it * kSlots - mine - 4 * half;
-        if (left + 4 * half <= 0) continue;
-        const uint32_t first = lds0 + buffer * (kSlots * 2 * kRowBytes) + mine * kRowBytes, kt = first + k_lane(), vt = first + kSlots * kRowBytes + v_lane();
-        const int4* where = reinterpret_cast<const int4*>(s_pos + (wave * kBuffers + buffer) * 256);
+        fetch_k(it + kBuffers - 1);
+        fetch_v(it + kBuffers - 1);
+        if (left_of(it) + 4 * half <= 0) continue;
         float x[16 * kStepsN];
-#pragma unroll
-        for (int k = 0; k < kStepsN; ++k) {
-          const floatx16 s = scores16(kt, k, query);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
-        }
-        to_scores<GENERAL>(sc, row, x, left < kMine, [&](int k, float* d) __attribute__((always_inline)) {
-          const int4 at = where[2 * k + half];
-          d[0] = static_cast<float>(next - at.x);
-          d[1] = static_cast<float>(next - at.y);
-          d[2] = static_cast<float>(next - at.z);
-          d[3] = static_cast<float>(next - at.w);
-        }, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[2 * k + half]; },
-                           [&](int i) __attribute__((always_inline)) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) >= left; });
-        add_rows16<kStepsN, kCareful>(x, sc.factor, vt, 0.f, r);
+        multiply(it, x);
+        finish(it, x);
+        add_rows16<kStepsN, kCareful>(x, sc.factor, v_of(it) + mine * kRowBytes + v_lane(), 0.f, r);
       }
       tile_barrier<0>();
     }
@@ -395,20 +506,21 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
   }
   };
   walk(std::false_type{});
-  if (BITS == 16 && GENERAL && sc.window > 0) {
+  if constexpr (BITS == 16) {
     float zero = r.l * 0.f;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(r.o[t][i], 0.f, zero);
-    if (__syncthreads_or(zero != 0.f)) walk(std::bool_constant<BITS == 16 && GENERAL>{});
+    if (__syncthreads_or(zero != 0.f)) walk(std::true_type{});
   }
 
   // the drafted tokens themselves
   if (piece == a.pieces - 1) {
     if constexpr (BITS == 4 && GENERAL) __syncthreads();           // (add_odd's flags lie where the rows come)
     const int64_t first = (static_cast<int64_t>(seq) * n * a.s.hkv + kvh) * kRowBytes;
-    fetch_rows(reinterpret_cast<const uint8_t*>(a.k_draft) + first, reinterpret_cast<const uint8_t*>(a.v_draft) + first, a.s.hkv * kRowBytes, n - 1, kTokens, lds0);
+    fetch_rows(reinterpret_cast<const uint8_t*>(a.k_draft) + first, k_at, a.s.hkv * kRowBytes, n - 1, kTokens, lds0);
+    fetch_rows(reinterpret_cast<const uint8_t*>(a.v_draft) + first, v_at, a.s.hkv * kRowBytes, n - 1, kTokens, lds0 + kTokens * kRowBytes);
     tile_barrier<0>();
     if (ws == 0) {
       Query16 q16;

@@ -197,6 +197,29 @@ def test_slots_behind_a_window_may_hold_anything(bits, n, hq):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("n, hq", [(6, 4), (20, 8), (40, 8)])
+def test_an_infinite_value_that_is_seen(bits, n, hq):
+    """The last slot's, in a tile that ends there: infinite in its channel, and nothing else changes."""
+    rng = np.random.default_rng(14)
+    s, items = cached(rng, [150], hq, 2, 160, bits)
+    q, k, v = drafted(rng, 1, n, hq, 2)
+    parent = cuda(tree(rng, n)[None], I32)
+    want, stats = b.rdkv_slots_tree_attn(s, q, k, v, parent)
+    for it in range(2):
+        if bits == 16:
+            s.v[0, it, 149, 9] = math.inf
+        else:
+            sc, of = O.tile64_meta_positions("v")
+            s.v[0, it].view(-1, 5120)[149 // 64, 4096:].view(torch.float16)[int(of[149 % 64].ravel()[0])] = math.inf
+    got, same = b.rdkv_slots_tree_attn(s, q, k, v, parent)
+    assert torch.equal(same, stats)
+    at = torch.zeros(D, dtype=torch.bool, device="cuda")
+    at[9 if bits == 16 else slice(0, 32)] = True           # (a group of 32 channels has one offset)
+    assert torch.all(got[..., at] == math.inf)
+    assert (got[..., ~at].float() - want[..., ~at].float()).abs().max() <= 2 * T.HALF_BF16 * 8
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 def test_a_tree_that_sees_nothing(bits):
     """No slot, and scores of -inf for the token itself."""
     s, _ = cached(np.random.default_rng(17), [0], 4, 2, 10, bits)
