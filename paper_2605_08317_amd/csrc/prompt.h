@@ -30,10 +30,10 @@ struct Args {
   int64_t token0[kSeqs];                // tokens of the batch before the sequence's first
 };
 
-constexpr int kRows = 128;              // of a workgroup
+constexpr int kRows = 128;              // of a workgroup, or half as many, whose keys two wavefronts share out
 // a sequence's workgroups: of an XCD as many as of another, so that the same heads of all sequences are on the same one
-inline int64_t workgroups(int T, int hq) { return ((static_cast<int64_t>(T) + kRows - 1) / kRows * hq + 7) / 8 * 8; }
-hipError_t launch(const Args& a, int grid, hipStream_t st);
+inline int64_t workgroups(int T, int hq, int rows = kRows) { return ((static_cast<int64_t>(T) + rows - 1) / rows * hq + 7) / 8 * 8; }
+hipError_t launch(const Args& a, int grid, bool shared, hipStream_t st);
 
 }  // namespace prompt
 }  // namespace rdkv

@@ -21,10 +21,12 @@ __device__ __forceinline__ int64_t first_of(const Side& s, int64_t token0, int h
   return s.tokens ? token0 * s.row + head * kHeadDim : (token0 * heads + static_cast<int64_t>(head) * T) * kHeadDim;
 }
 
-template <bool GENERAL>
-__global__ __launch_bounds__(2 * kRows, 2) void prompt_kernel(Args a) {
+// WS: wavefronts that share the tiles of 32 rows.  A stage is as many tiles, one each.
+template <bool GENERAL, int WS>
+__global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
   extern __shared__ __align__(256) uint8_t smem[];
-  constexpr int NW = kRows / 32, kCopies = 16 / NW;         // kCopies: of a wavefront, for a tile of K or V
+  constexpr int NW = prompt::kRows / 32, kRows = prompt::kRows / WS, kCopies = WS * 16 / NW;       // kCopies: of a wavefront, for a stage of K or V
+  constexpr uint32_t kStage = WS * kTileBytes;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
   // The sequence, the longest is first; of that all heads' last rows first.  Heads of a KV head are beside each other on an XCD where that can be.
   const int mine = static_cast<int>(blockIdx.x), seq = __popcll(__ballot(lane < a.n_seqs && a.first[lane] <= mine)) - 1;
@@ -38,25 +40,28 @@ __global__ __launch_bounds__(2 * kRows, 2) void prompt_kernel(Args a) {
 
   // the tiles that some row of the workgroup sees: the sinks', and those from the first row's window on
   const int first = a.window > 0 ? max(0, q0 - a.window + 1) / kKeys : 0, n_sink = a.window > 0 ? min((min(a.sinks, T) + kKeys - 1) / kKeys, first) : 0;
-  const int n_it = (min(T, q0 + kRows) + kKeys - 1) / kKeys - first + n_sink;
-  const auto tile_of = [&](int it) { return it < n_sink ? it : it - n_sink + first; };
+  const int n_tiles = (min(T, q0 + kRows) + kKeys - 1) / kKeys - first + n_sink, n_it = (n_tiles + WS - 1) / WS;
+  const auto tile_of = [&](int t) { return t < n_sink ? t : t - n_sink + first; };
 
   const uint32_t lds0 = lds_address(smem);
   const int prow = tid >> 4;                         // this thread's rows prow + 4 NW k
   const uint32_t k_at = 16 * k_piece(prow, tid & 15), v_at = 16 * v_piece(prow, tid & 15);
-  const auto slot = [](int it) { return static_cast<uint32_t>(it % kRing) * kTileBytes; };
+  const auto slot = [](int it) { return static_cast<uint32_t>(it % kRing) * kStage; };
   const auto fetch = [&](const uint16_t* from, const Side& side, uint32_t at, int it, uint32_t to) __attribute__((always_inline)) {
-    const int key0 = tile_of(min(it, n_it - 1)) * kKeys, last = T - 1 - key0;
-    from += static_cast<int64_t>(key0) * side.row;
     to += slot(it) + wave * 1024;
 #pragma unroll
-    for (int k = 0; k < kCopies; ++k)
-      copy_to_lds(from, static_cast<uint32_t>(min(prow + 4 * NW * k, last) * side.row) * 2 + at, to + 1024 * NW * k);
+    for (int x = 0; x < WS; ++x) {
+      const int key0 = tile_of(min(it * WS + x, n_tiles - 1)) * kKeys, last = T - 1 - key0;
+      const uint16_t* first_key = from + static_cast<int64_t>(key0) * side.row;
+#pragma unroll
+      for (int k = 0; k < 16 / NW; ++k)
+        copy_to_lds(first_key, static_cast<uint32_t>(min(prow + 4 * NW * k, last) * side.row) * 2 + at, to + x * kTileBytes + 1024 * NW * k);
+    }
   };
   const auto fetch_k = [&](int it) __attribute__((always_inline)) { fetch(Kh, a.k, k_at, it, lds0); };
-  const auto fetch_v = [&](int it) __attribute__((always_inline)) { fetch(Vh, a.v, v_at, it, lds0 + kRing * kTileBytes); };
+  const auto fetch_v = [&](int it) __attribute__((always_inline)) { fetch(Vh, a.v, v_at, it, lds0 + kRing * kStage); };
 
-  const int r0 = q0 + 32 * wave, row = r0 + l32; // this wavefront's first row, and the lane's
+  const int ws = wave % WS, r0 = q0 + 32 * (wave / WS), row = r0 + l32;              // this wavefront's first row, and the lane's
   bf16x8 q_op[8];
   const uint16_t* q = a.Q + first_of(a.q, token0, a.hq, head, T) + static_cast<int64_t>(min(row, T - 1)) * a.q.row + 8 * half;
 #pragma unroll
@@ -73,11 +78,13 @@ __global__ __launch_bounds__(2 * kRows, 2) void prompt_kernel(Args a) {
 
   floatx16 o[4];
   float m, l;
-  const auto key_of = [&](int it) { return tile_of(it) * kKeys; };
-  const uint32_t k_first = lds0 + k_lane(), v_first = lds0 + kRing * kTileBytes + v_lane();
-  // The tiles that this wavefront has to do with: until its last row, and from its first row's window on (where there are sinks, from those on).
-  const int it_end = min(n_it, (r0 + 31) / kKeys - first + n_sink + 1);
-  const int it_begin = a.window > 0 && a.sinks == 0 ? min(it_end - 1, max(0, r0 - a.window + 1) / kKeys - first) : 0;
+  const auto key_of = [&](int it) { return tile_of(it * WS + ws) * kKeys; };
+  const uint32_t k_first = lds0 + ws * kTileBytes + k_lane(), v_first = lds0 + kRing * kStage + ws * kTileBytes + v_lane();
+  // The tiles that this wavefront's rows have to do with: until its last row, and from its first row's window on (where there are sinks, from those
+  // on).  Of those its own stages.
+  const int t_end = min(n_tiles, (r0 + 31) / kKeys - first + n_sink + 1);
+  const int t_begin = a.window > 0 && a.sinks == 0 ? min(t_end - 1, max(0, r0 - a.window + 1) / kKeys - first) : 0;
+  const int it_end = (t_end - ws + WS - 1) / WS, it_begin = (t_begin - ws + WS - 1) / WS;
   const auto begin = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[t] = floatx16{};
@@ -220,24 +227,27 @@ __global__ __launch_bounds__(2 * kRows, 2) void prompt_kernel(Args a) {
     };
     int it = 0;
     for (; it < it_begin; ++it) open(it);
-    multiply(it, even);
-    finish(it, even);
-    float top = largest(even);
-    for (; it + 2 < it_end; it += 2) {
+    if (WS == 1 || it < it_end) {
+      multiply(it, even);
+      finish(it, even);
+      float top = largest(even);
+      for (; it + 2 < it_end; it += 2) {
+        open(it);
+        position(std::true_type{}, it, even, odd, top);
+        open(it + 1);
+        position(std::true_type{}, it + 1, odd, even, top);
+      }
       open(it);
-      position(std::true_type{}, it, even, odd, top);
-      open(it + 1);
-      position(std::true_type{}, it + 1, odd, even, top);
+      if (it + 1 < it_end) {
+        position(std::true_type{}, it, even, odd, top);
+        open(++it);
+        position(std::false_type{}, it, odd, even, top);
+      } else {
+        position(std::false_type{}, it, even, odd, top);
+      }
+      ++it;
     }
-    open(it);
-    if (it + 1 < it_end) {
-      position(std::true_type{}, it, even, odd, top);
-      open(++it);
-      position(std::false_type{}, it, odd, even, top);
-    } else {
-      position(std::false_type{}, it, even, odd, top);
-    }
-    for (++it; it < n_it; ++it) open(it);
+    for (; it < n_it; ++it) open(it);
     tile_barrier<0>();                               // (copies of tiles past the last have landed as well)
   };
   // Again, with care, where a result is not finite: rows of V that some rows of a tile do not see are kept from meeting their zeros, which make NaN of
@@ -297,7 +307,31 @@ __global__ __launch_bounds__(2 * kRows, 2) void prompt_kernel(Args a) {
   sum = __builtin_fmaf(l, 0.f, sum);
   if (__syncthreads_or(sum != 0.f)) walk_with_care();
 
-  const float total = halves_add(l), inv = total == 0.f ? 0.f : 1.f / total;
+  l = halves_add(l);
+  if constexpr (WS == 2) {
+    // the other's result, over the larger reference, to the first one's
+    __syncthreads();
+    float* theirs = reinterpret_cast<float*>(smem) + wave / WS * (66 * 64) + lane;
+    if (ws == 1) {
+      theirs[64 * 64] = m;
+      theirs[65 * 64] = l;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) theirs[(16 * t + i) * 64] = o[t][i];
+    }
+    __syncthreads();
+    if (ws == 1) return;
+    const float other = theirs[64 * 64], now = fmaxf(m, other);
+    const float mine = __builtin_amdgcn_exp2f((m - now) * factor), its = __builtin_amdgcn_exp2f((other - now) * factor);
+    m = now;
+    l = __builtin_fmaf(theirs[65 * 64], its, l * mine);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][i] = __builtin_fmaf(theirs[(16 * t + i) * 64], its, o[t][i] * mine);
+  }
+  const float total = l, inv = total == 0.f ? 0.f : 1.f / total;
   if (row >= T) return;
   uint16_t* out = a.out + first_of(a.o, token0, a.hq, head, T) + static_cast<int64_t>(row) * a.o.row + 8 * half;
 #pragma unroll
@@ -318,20 +352,21 @@ __global__ __launch_bounds__(2 * kRows, 2) void prompt_kernel(Args a) {
     a.lse[token0 * a.hq + static_cast<int64_t>(head) * T + row] = total == 0.f ? -INFINITY : __builtin_fmaf(m * factor, kLn2, __logf(total));
 }
 
-template <bool GENERAL>
+template <bool GENERAL, int WS>
 hipError_t start(const Args& a, int grid, hipStream_t st) {
-  constexpr int lds = 2 * kRing * kTileBytes;
-  const hipError_t e = RDKV_ALLOW_LDS(prompt_kernel<GENERAL>, lds);
+  constexpr int lds = 2 * kRing * WS * kTileBytes;
+  const hipError_t e = RDKV_ALLOW_LDS((prompt_kernel<GENERAL, WS>), lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(prompt_kernel<GENERAL>, dim3(grid), dim3(2 * kRows), lds, st, a);
+  hipLaunchKernelGGL((prompt_kernel<GENERAL, WS>), dim3(grid), dim3(2 * kRows), lds, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch(const Args& a, int grid, hipStream_t st) {
+hipError_t launch(const Args& a, int grid, bool shared, hipStream_t st) {
   const bool general = a.cap > 0.f || a.slopes;      // (a window takes no scores of its own)
-  return general ? start<true>(a, grid, st) : start<false>(a, grid, st);
+  if (shared) return general ? start<true, 2>(a, grid, st) : start<false, 2>(a, grid, st);
+  return general ? start<true, 1>(a, grid, st) : start<false, 1>(a, grid, st);
 }
 
 }  // namespace prompt

@@ -81,14 +81,23 @@ def test_windows_caps_and_biases(lens, hq, hkv, kw):
         run(7, lens, hq, hkv, tokens, **kw)
 
 
-@pytest.mark.parametrize("kw", [{}, dict(window=150, sinks=2), dict(cap=25.0)], ids=str)
-def test_enough_prompts_for_the_largest_workgroups(kw):
-    """Launches of many workgroups take 256 rows each; more than 64 sequences are several launches."""
+SLOPES = (2.0 ** (-8.0 * (np.arange(8) + 1) / 8)).astype(np.float32).astype(np.float64)
+
+
+@pytest.mark.parametrize("kw", [{}, dict(window=150, sinks=2), dict(window=64), dict(cap=25.0), dict(slopes=SLOPES, cap=30.0, window=100, sinks=70)], ids=str)
+def test_more_workgroups_than_compute_units(kw):
+    """Fewer than that share their rows' tiles between wavefronts; here each has its rows to itself.  More than 64 sequences are several launches."""
     rng = np.random.default_rng(3)
     run(9, [int(x) for x in rng.integers(0, 400, 70)], 8, 2, True, **kw)
 
 
-@pytest.mark.parametrize("hq, n", [(4, 1), (8, 70)])           # of either workgroup size
+@pytest.mark.parametrize("kw", [{}, dict(window=700, sinks=100), dict(cap=25.0)], ids=str)
+@pytest.mark.parametrize("hq, hkv", [(4, 2), (32, 4)])         # with shared tiles, and without
+def test_longer_prompts(hq, hkv, kw):
+    run(10, [1500, 33, 900], hq, hkv, False, **kw)
+
+
+@pytest.mark.parametrize("hq, n", [(4, 1), (8, 70)])           # with shared tiles, and without
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 def test_what_hidden_rows_hold_does_not_matter(hq, n, bad):
     """Rows of K and V that a token does not see may hold anything; a token that does see such a row has no finite outputs."""
