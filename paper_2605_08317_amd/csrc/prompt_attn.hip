@@ -72,6 +72,7 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
 #pragma unroll
   for (int kb = 0; kb < 8; ++kb) arrived(q_op[kb]);
   const float slope = GENERAL && a.slopes ? a.slopes[head] : 0.f, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
+  const TanhSmall small(kRoot * inv_cap);
   // What makes the numbers that are kept (products, scores over the cap, or with biases scores) scores, and those exponents of 2.
   const float units = GENERAL && a.cap > 0.f ? a.cap : kRoot;
   const float factor = !GENERAL ? kRootLog2e : a.slopes ? kLog2e : a.cap > 0.f ? a.cap * kLog2e : kRootLog2e;
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
       float v[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] = s[i >> 4][i & 15];
-      if (a.cap > 0.f) tanh_all(v, kRoot * inv_cap);
+      if (a.cap > 0.f) tanh_all(v, kRoot * inv_cap, small);
       if (a.slopes) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = __builtin_fmaf(v[i], units, -slope * static_cast<float>(back - key(i >> 4, i & 15)));

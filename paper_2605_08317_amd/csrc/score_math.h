@@ -18,35 +18,38 @@ __device__ __forceinline__ float capped(float s, float cap, float inv_cap) {
   return cap * (fabsf(y) < 0.8f ? small : __builtin_copysignf(large, y));
 }
 
-// tanh y for |y| < 0.8: y times a polynomial of degree 6 in its square, fitted at Chebyshev's points (off by 4e-9 of the value, 1e-7 as fp32 rounds it).
-__device__ __forceinline__ float tanh_small(float y) {
-  const float z = y * y;
-  float p = 0.0015656708f;
-  p = __builtin_fmaf(p, z, -0.0073702540f);
-  p = __builtin_fmaf(p, z, 0.0212719534f);
-  p = __builtin_fmaf(p, z, -0.0538406223f);
-  p = __builtin_fmaf(p, z, 0.1333200783f);
-  p = __builtin_fmaf(p, z, -0.3333328068f);
-  p = __builtin_fmaf(p, z, 1.0f);
-  return p * y;
-}
-// x: products, scale: what makes them scores over the cap -> tanh of those.  A wavefront whose scores are all below 0.8 of the cap, which most are,
-// has the polynomial alone: 11 instructions a score instead of 20, three of them of a quarter of the rate.
+// tanh(x scale) for |x scale| < 0.5: x times a polynomial of degree 4 in its square, fitted at Chebyshev's points (off by 3e-8 of the value, 1.4e-7
+// with fp32's roundings); the powers of the scale are in its coefficients.
+struct TanhSmall {
+  float c[5], below;                      // below: what |x| may be
+  __device__ __forceinline__ explicit TanhSmall(float scale) {
+    const float s2 = scale * scale, s4 = s2 * s2, s5 = s4 * scale;
+    c[0] = scale;
+    c[1] = -0.3333306909f * s2 * scale;
+    c[2] = 0.1332475096f * s5;
+    c[3] = -0.0529842377f * s2 * s5;
+    c[4] = 0.0171313453f * s4 * s5;
+    below = scale > 0x1p-12f && scale < 0x1p12f ? 0.5f / scale : 0.f;         // (so that no power leaves fp32's normal numbers)
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    const float z = x * x;
+    return x * __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(__builtin_fmaf(c[4], z, c[3]), z, c[2]), z, c[1]), z, c[0]);
+  }
+};
+// x: products, scale: what makes them scores over the cap -> tanh of those.  A wavefront whose scores are all below half of the cap, which most are,
+// has the polynomial alone: 7 instructions a score instead of 20, three of them of a quarter of the rate.
 template <int N>
-__device__ __forceinline__ void tanh_all(float (&x)[N], float scale) {
+__device__ __forceinline__ void tanh_all(float (&x)[N], float scale, const TanhSmall& small) {
   float most = 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    x[i] *= scale;
-    most = fmaxf(most, fabsf(x[i]));
-  }
-  if (__all(most < 0.8f)) {
+  for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(x[i]));
+  if (__all(most < small.below)) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = tanh_small(x[i]);
+    for (int i = 0; i < N; ++i) x[i] = small(x[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      x[i] = capped(x[i], 1.f, 1.f);
+      x[i] = capped(x[i] * scale, 1.f, 1.f);
       if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (all of them side by side do not fit the registers)
     }
   }

@@ -138,7 +138,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
         if (GENERAL && a.s.cap > 0.f) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) e[j] = s[4 * k + j] * na[j];
-          tanh_all(e, inv_cap);
+          tanh_all(e, inv_cap, TanhSmall(inv_cap));
 #pragma unroll
           for (int j = 0; j < 4; ++j) e[j] = __builtin_fmaf(e[j], a.s.cap, le[j]);
         } else {

@@ -121,7 +121,7 @@ template <bool GENERAL, int N, class Away, class Four, class Hide>
 __device__ __forceinline__ void to_scores(const Scoring& sc, const Row& row, float (&x)[N], bool some, Away away, Four four, Hide hide) {
   if constexpr (GENERAL) {
     const float unit = sc.cap > 0.f ? sc.cap : sc.natural;
-    if (sc.cap > 0.f) tanh_all(x, sc.natural * sc.inv_cap);
+    if (sc.cap > 0.f) tanh_all(x, sc.natural * sc.inv_cap, TanhSmall(sc.natural * sc.inv_cap));
     if (sc.biased) {
 #pragma unroll
       for (int k = 0; k < N / 4; ++k) {
