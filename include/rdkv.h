@@ -534,8 +534,9 @@ rdkv_status rdkv_slots_tree_attn(const rdkv_slots* slots, int32_t n, const void*
  * With c accepted tokens, the j-th at position next + j: weight becomes decay^c x weight + the sum over j of decay^(c-1-j) x the softmax's
  * value of token j, summed over the heads of the group, in slots below len.  Then the tokens come in one after the other as by rdkv_slots_append,
  * but that token i starts with the sum over j >= i of decay^(c-1-j) x what token j gives it.  While slots are free this is what c appends, each
- * followed by its decode step, leave.  Where the path is as long as a token of a full cache is `recent`, an accepted token may be
- * given up for a later one.  Rows of 4-bit caches are quantized as they come in.
+ * followed by its decode step, leave.  An accepted token that is no longer among the `recent` ones may be given up for a later one of the path;
+ * its slot then holds the later one's row, and both name it in `slot`.  A path may name a token twice: it comes in twice.  Positions within an item
+ * are taken to differ.  Rows of 4-bit caches are quantized as they come in.
  */
 size_t rdkv_slots_accept_workspace_bytes(const rdkv_slots* slots);
 rdkv_status rdkv_slots_accept(const rdkv_slots* slots, int32_t n, int32_t m, const void* q, const void* k_draft, const void* v_draft,

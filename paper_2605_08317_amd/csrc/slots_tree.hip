@@ -1,7 +1,15 @@
 // Slot caches: attention of a tree of drafted tokens.
 //
-// A workgroup of four or eight wavefronts has up to 128 (bf16: 256) query rows (token, head) of an item and a piece of its slots.  Its wavefronts share out
-// the rows, 32 each, and where these are fewer than the wavefronts the slots as well; results of slots are joined in LDS.  The last piece of an item has the drafted tokens' own keys and values, bf16 rows whatever the cache holds, behind its slots.
+// A token sees the slots, its ancestors and itself: what the steps of a chain would compute, with what the slots cost once for all tokens.  A workgroup
+// of four or eight wavefronts has up to 128 (bf16: 256) query rows (token, head) of an item and a piece of its slots.  Its wavefronts share out
+// the rows, 32 each, and where these are fewer than the wavefronts the slots as well; results of slots are joined in LDS, those of pieces
+// by a second launch.  The last piece of an item has the drafted tokens' own keys and values, bf16 rows whatever the cache holds, behind its slots or
+// to itself.  Products and probabilities as of prompts (a lane has one query row); of 4-bit tiles a wavefront's own, codes less 8 as fp16 with
+// group sums in fp32, so that scores keep fp32's digits.
+//   bound   bf16: HBM up to 64 rows (8 tokens of 4 heads on 4 x 8 x 131072 slots 390 us, 5.5 TB/s), from 128 on the matrix cores at the clock that the
+//           power leaves them (64 tokens 650 us, 830 TFLOP/s at 1.6 GHz).  4 bits: vector instructions, 64 % of the cycles issue one, about 640
+//           a tile and 32 rows (32 tokens on 32 x 8 x 5000..8192 slots with biases 300 us; 8 tokens on 4 x 8 x 131072 150)
+//   tried   query operands in LDS and tiles loaded a tile ahead twice over in 4 bits: slower, they cost the registers of a second wavefront a SIMD
 #include <algorithm>
 
 #include "slots_tiles.h"
