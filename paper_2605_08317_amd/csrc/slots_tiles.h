@@ -125,10 +125,10 @@ __device__ __forceinline__ halfx8 centres(uint4 meta) {
 }
 // K metadata into LDS (kKMeta bytes of the wavefront's), of slots from `rows` on zeros: a slot's centres, then the scales, [group][slot].
 constexpr int kKMeta = 1024 + 512;
-__device__ __forceinline__ void put_k_meta(uint8_t* lds, const Side4& k, int rows) {
+__device__ __forceinline__ void put_k_meta(uint8_t* lds, const uint4& meta, int rows) {
   const int lane = threadIdx.x & 63;
   const bool there = lane < rows;
-  const uint4 m = make_uint4(there ? k.meta.x : 0u, there ? k.meta.y : 0u, there ? k.meta.z : 0u, there ? k.meta.w : 0u);
+  const uint4 m = make_uint4(there ? meta.x : 0u, there ? meta.y : 0u, there ? meta.z : 0u, there ? meta.w : 0u);
   *reinterpret_cast<halfx8*>(lds + 16 * lane) = centres(m);
   uint16_t* scales = reinterpret_cast<uint16_t*>(lds + 1024) + lane;
   scales[0] = static_cast<uint16_t>(m.x);
@@ -138,10 +138,10 @@ __device__ __forceinline__ void put_k_meta(uint8_t* lds, const Side4& k, int row
 }
 // V metadata: scales, and offsets plus 8 scales; of slots from `rows` on zeros.  FINITE: of those that are not finite as well; the lanes that had such.
 template <bool FINITE>
-__device__ __forceinline__ uint64_t put_v_meta(uint8_t* lds, const Side4& v, int rows) {
+__device__ __forceinline__ uint64_t put_v_meta(uint8_t* lds, const uint4& meta, int rows) {
   const int lane = threadIdx.x & 63, first = 4 * (lane >> 2);
   union { uint4 u; _Float16 h[8]; } m;
-  m.u = v.meta;
+  m.u = meta;
   bool odd = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -175,43 +175,49 @@ struct Codes4 {
 };
 
 // A lane's words of product x, and of them what a product's operand of a group's half is: fields 2 s and 2 s + 1 of two words.
-struct Words4 {
-  uint32_t w[2][4][2];
-  __device__ __forceinline__ Words4(const Side4& k) {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      // word pair (2 half, 2 half + 1) of the slots of product 0, and of product 1
-      uint32_t a = k.codes[g].x, b = k.codes[g].y, c = k.codes[g].z, d = k.codes[g].w;
-      asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(c));
-      asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(b), "+v"(d));
-      w[0][g][0] = a;
-      w[0][g][1] = b;
-      w[1][g][0] = c;
-      w[1][g][1] = d;
-    }
+struct Group4 {
+  uint32_t w[2][2];
+  Group4() = default;
+  // word pair (2 half, 2 half + 1) of the slots of product 0, and of product 1
+  __device__ __forceinline__ explicit Group4(const uint4& k) {
+    uint32_t a = k.x, b = k.y, c = k.z, d = k.w;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(c));
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(b), "+v"(d));
+    w[0][0] = a;
+    w[0][1] = b;
+    w[1][0] = c;
+    w[1][1] = d;
   }
-  __device__ __forceinline__ halfx8 operand(const Codes4& codes, int x, int g, int s) const {
+  __device__ __forceinline__ halfx8 operand(const Codes4& codes, int x, int s) const {
     union { halfx2 p[4]; halfx8 h; } op;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      op.p[j] = codes.less_8(w[x][g][j], 2 * s);
-      op.p[2 + j] = codes.less_8(w[x][g][j], 2 * s + 1);
+      op.p[j] = codes.less_8(w[x][j], 2 * s);
+      op.p[2 + j] = codes.less_8(w[x][j], 2 * s + 1);
     }
     return op.h;
   }
 };
+struct Words4 {
+  Group4 group[4];
+  __device__ __forceinline__ explicit Words4(const Side4& k) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) group[g] = Group4(k.codes[g]);
+  }
+  __device__ __forceinline__ halfx8 operand(const Codes4& codes, int x, int g, int s) const { return group[g].operand(codes, x, s); }
+};
 
-// Products of the 64 slots, register i of s[x] of lane (half, .): slot 32 half + 16 x + i; over the query's unit.
-__device__ __forceinline__ void scores4(const Codes4& codes, const Side4& k, const uint8_t* k_meta, const Query4& q, floatx16 (&s)[2]) {
+// Products of the 64 slots, register i of s[x] of lane (half, .): slot 32 half + 16 x + i; over the query's unit.  operand(x, group, half of the group)
+template <class Operand>
+__device__ __forceinline__ void scores4(const uint8_t* k_meta, const Query4& q, floatx16 (&s)[2], Operand operand) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-  const Words4 words(k);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     s[x] = product(*reinterpret_cast<const halfx8*>(k_meta + 16 * slot_of_row(x, l32)), q.sums, floatx16{});
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      floatx16 sums = product(words.operand(codes, x, g, 0), q.op[2 * g], floatx16{});
-      sums = product(words.operand(codes, x, g, 1), q.op[2 * g + 1], sums);
+      floatx16 sums = product(operand(x, g, 0), q.op[2 * g], floatx16{});
+      sums = product(operand(x, g, 1), q.op[2 * g + 1], sums);
       const halfx8* sc = reinterpret_cast<const halfx8*>(k_meta + 1024 + 128 * g + 2 * (32 * half + 16 * x));
       const halfx8 sc0 = sc[0], sc1 = sc[1];
 #pragma unroll

@@ -175,14 +175,20 @@ constexpr int kStageLds = 256 * 2 * kRowBytes;                  // of all of the
 constexpr int kPosLds = 8 * 4 * 64 * 4;                         // positions of the wavefronts' tiles, up to four buffers
 constexpr int kDraftLds = kTokens * 2 * kRowBytes;
 constexpr int kJoinLds = 4 * 4 * 16 * 64 * 4;                   // four wavefronts' results
-constexpr int kMetaLds = kKMeta + 1024 + 512;                   // of a wavefront
+constexpr int kMetaLds = kKMeta + 1024 + 512 + 256;             // of a wavefront: K's, V's, positions and distances, add_odd's flags
+constexpr int kImageLds = 32 * 1024;                            // a 4-bit tile's operands, K's, then V's, where wavefronts share them
 
 // Values of a 4-bit tile that are not finite, to the rows that give their slots something.  odd: lanes 4 (slot / 4) + group whose metadata are not; lds:
-// 2 KiB of the wavefront's; p: probabilities, register i of slot 32 half + i.
+// 256 bytes of the wavefront's; p: probabilities, register i of slot 32 half + i.
 __device__ __forceinline__ void add_odd(uint64_t odd, const uint8_t* tile, int rows, uint8_t* lds, const float (&p)[32], Out& r) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+  uint32_t* rows_of = reinterpret_cast<uint32_t*>(lds);          // [slot]: a bit a row
 #pragma unroll
-  for (int i = 0; i < 32; ++i) lds[(32 * half + i) * 32 + l32] = p[i] != 0.f;
+  for (int i = 0; i < 32; ++i) {
+    const uint64_t some = __ballot(p[i] != 0.f);
+    rows_of[i] = static_cast<uint32_t>(some);
+    rows_of[32 + i] = static_cast<uint32_t>(some >> 32);
+  }
   wave_lds_order();
   for (; odd != 0; odd &= odd - 1) {
     const int which = __builtin_ctzll(odd), group = which & 3;
@@ -190,7 +196,7 @@ __device__ __forceinline__ void add_odd(uint64_t odd, const uint8_t* tile, int r
       const _Float16* meta = reinterpret_cast<const _Float16*>(tile + kTileCodes + 16 * which);
       const float scale = static_cast<float>(meta[slot & 3]), centre = __builtin_fmaf(8.f, scale, static_cast<float>(meta[4 + (slot & 3)]));
       if (fabsf(scale) < INFINITY && fabsf(static_cast<float>(static_cast<_Float16>(centre))) < INFINITY) continue;
-      const bool some = lds[slot * 32 + l32] != 0;
+      const bool some = (rows_of[slot] >> l32 & 1) != 0;
       const int k = slot & 31;
       float v[16];
 #pragma unroll
@@ -447,36 +453,20 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
       tile_barrier<0>();
     }
   } else {
-    uint8_t* meta = smem + kDraftLds + wave * kMetaLds;
+    constexpr bool kShared = WR == 4;                  // every wavefront has the same tiles
+    uint8_t* meta = smem + (kShared ? 2 * kImageLds : kDraftLds) + wave * kMetaLds;
     const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
     const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
     const int t1 = (end + kTileRows - 1) / kTileRows;
-    Side4 k, v;
-    int at = 0;
-    int t = begin / kTileRows + ws;
     const Codes4 codes;
-    // the next tile's K comes while this one's values are added up, its V while its scores are made
-    const auto load_k = [&](int tile) __attribute__((always_inline)) {
-      k.load(K + static_cast<int64_t>(tile) * kTileBytes, true);
-      if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
-    };
-    const auto load_v = [&](int tile) __attribute__((always_inline)) { v.load(V + static_cast<int64_t>(tile) * kTileBytes, false); };
-    if (t < t1) {
-      load_k(t);
-      load_v(t);
-    }
-    for (; t < t1; t += WS) {
-      const int left = end - t * kTileRows;
-      put_k_meta(meta, k, left);
+    // a tile's scores, softmax and P V
+    const auto put_positions = [&](int at) __attribute__((always_inline)) {
       if constexpr (GENERAL) {
         reinterpret_cast<int*>(meta + kKMeta + 1024)[lane] = at;
         reinterpret_cast<float*>(meta + kKMeta + 1024 + 256)[lane] = static_cast<float>(next - at);
       }
-      wave_lds_order();
-      floatx16 s[2];
-      scores4(codes, k, meta, query, s);
-      load_k(min(t + WS, t1 - 1));
-      float x[32];
+    };
+    const auto finish = [&](int left, const floatx16 (&s)[2], float (&x)[32]) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = s[i >> 4][i & 15];
       const int4* where = reinterpret_cast<const int4*>(meta + kKMeta + 1024) + 8 * half;
@@ -484,9 +474,9 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
                          [&](int k, float* d) __attribute__((always_inline)) { *reinterpret_cast<int4*>(d) = where[16 + k]; },
                          [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[k]; },
                          [&](int i) __attribute__((always_inline)) { return 32 * half + i >= left; });
-      // with a window, values that are not finite are kept out, and go to those rows that see them afterwards
-      const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v, left);
-      wave_lds_order();
+    };
+    // value(channel group, step)
+    const auto add = [&](const float (&x)[32], int tile, int left, uint64_t odd, auto value) __attribute__((always_inline)) {
       float p[32], pf[32];
       softmax(x, sc.factor, kTopHalf, r, p);
       halfx8 op[4];
@@ -502,14 +492,99 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         __builtin_amdgcn_sched_barrier(0);
-        add_values<false>(op, pf, [&](int f) __attribute__((always_inline)) {
-          return f == 0 ? values4<0>(codes, v.codes[c], meta + kKMeta, c) : f == 1 ? values4<1>(codes, v.codes[c], meta + kKMeta, c)
-               : f == 2 ? values4<2>(codes, v.codes[c], meta + kKMeta, c) : values4<3>(codes, v.codes[c], meta + kKMeta, c);
-        }, r.o[c]);
+        add_values<false>(op, pf, [&](int f) __attribute__((always_inline)) { return value(c, f); }, r.o[c]);
       }
-      load_v(min(t + WS, t1 - 1));
-      if (GENERAL && odd != 0) add_odd(odd, V + static_cast<int64_t>(t) * kTileBytes, left, smem + wave * (kDraftLds / NW), p, r);
-      wave_lds_order();
+      if (GENERAL && odd != 0) add_odd(odd, V + static_cast<int64_t>(tile) * kTileBytes, left, meta + kMetaLds - 256, p, r);
+    };
+    const auto values = [&](const uint4& words, int c, int f) __attribute__((always_inline)) {
+      return f == 0 ? values4<0>(codes, words, meta + kKMeta, c) : f == 1 ? values4<1>(codes, words, meta + kKMeta, c)
+           : f == 2 ? values4<2>(codes, words, meta + kKMeta, c) : values4<3>(codes, words, meta + kKMeta, c);
+    };
+    int t = begin / kTileRows + ws;
+    if constexpr (!kShared) {
+      Side4 k, v;
+      int at = 0;
+      // the next tile's K comes while this one's values are added up, its V while its scores are made
+      const auto load_k = [&](int tile) __attribute__((always_inline)) {
+        k.load(K + static_cast<int64_t>(tile) * kTileBytes, true);
+        if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
+      };
+      const auto load_v = [&](int tile) __attribute__((always_inline)) { v.load(V + static_cast<int64_t>(tile) * kTileBytes, false); };
+      if (t < t1) {
+        load_k(t);
+        load_v(t);
+      }
+      for (; t < t1; t += WS) {
+        const int left = end - t * kTileRows;
+        put_k_meta(meta, k.meta, left);
+        put_positions(at);
+        wave_lds_order();
+        floatx16 s[2];
+        {
+          const Words4 words(k);
+          scores4(meta, query, s, [&](int x, int g, int h) __attribute__((always_inline)) { return words.operand(codes, x, g, h); });
+        }
+        load_k(min(t + WS, t1 - 1));
+        float x[32];
+        finish(left, s, x);
+        // with a window, values that are not finite are kept out, and go to those rows that see them afterwards
+        const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v.meta, left);
+        wave_lds_order();
+        add(x, t, left, odd, [&](int c, int f) __attribute__((always_inline)) { return values(v.codes[c], c, f); });
+        load_v(min(t + WS, t1 - 1));
+        wave_lds_order();
+      }
+    } else if (t < t1) {
+      // Each wavefront makes operands of a group's codes for all four, a tile ahead, into one of two images in LDS.
+      uint4 k_codes, k_meta, v_codes, v_meta;
+      int at = 0;
+      const auto load = [&](int tile) __attribute__((always_inline)) {
+        const uint8_t *kt = K + static_cast<int64_t>(tile) * kTileBytes, *vt = V + static_cast<int64_t>(tile) * kTileBytes;
+        k_codes = *reinterpret_cast<const uint4*>(kt + 1024 * wave + 16 * slot_of_row(half, l32));
+        k_meta = *reinterpret_cast<const uint4*>(kt + kTileCodes + 16 * lane);
+        v_codes = *reinterpret_cast<const uint4*>(vt + 1024 * wave + 16 * lane);
+        v_meta = *reinterpret_cast<const uint4*>(vt + kTileCodes + 16 * lane);
+        if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
+      };
+      const auto image = [&](int tile) { return smem + (tile & 1) * kImageLds + 16 * lane; };
+      const auto make = [&](int tile) __attribute__((always_inline)) {
+        const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v_meta, end - tile * kTileRows);
+        wave_lds_order();
+        uint8_t* to = image(tile);
+        const Group4 group(k_codes);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) *reinterpret_cast<halfx8*>(to + ((4 * x + wave) * 2 + h) * 1024) = group.operand(codes, x, h);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) *reinterpret_cast<halfx8*>(to + kImageLds / 2 + (4 * wave + f) * 1024) = values(v_codes, wave, f);
+        return odd;
+      };
+      load(t);
+      uint64_t odd = make(t);
+      uint4 meta_now = k_meta;
+      int at_now = at;
+      load(min(t + 1, t1 - 1));
+      tile_barrier<63>();
+      for (; t < t1; ++t) {
+        const int left = end - t * kTileRows;
+        put_k_meta(meta, meta_now, left);
+        put_positions(at_now);
+        uint64_t odd_next = 0;
+        if (t + 1 < t1) odd_next = make(t + 1);
+        meta_now = k_meta;
+        at_now = at;
+        load(min(t + 2, t1 - 1));
+        wave_lds_order();
+        const uint8_t* from = image(t);
+        floatx16 s[2];
+        scores4(meta, query, s, [&](int x, int g, int h) __attribute__((always_inline)) { return *reinterpret_cast<const halfx8*>(from + ((4 * x + g) * 2 + h) * 1024); });
+        float x[32];
+        finish(left, s, x);
+        add(x, t, left, odd, [&](int c, int f) __attribute__((always_inline)) { return *reinterpret_cast<const halfx8*>(from + kImageLds / 2 + (4 * c + f) * 1024); });
+        odd = odd_next;
+        tile_barrier<63>();
+      }
     }
   }
   };
@@ -525,7 +600,6 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
 
   // the drafted tokens themselves
   if (piece == a.pieces - 1) {
-    if constexpr (BITS == 4 && GENERAL) __syncthreads();           // (add_odd's flags lie where the rows come)
     const int64_t first = (static_cast<int64_t>(seq) * n * a.s.hkv + kvh) * kRowBytes;
     fetch_rows(reinterpret_cast<const uint8_t*>(a.k_draft) + first, k_at, a.s.hkv * kRowBytes, n - 1, kTokens, lds0);
     fetch_rows(reinterpret_cast<const uint8_t*>(a.v_draft) + first, v_at, a.s.hkv * kRowBytes, n - 1, kTokens, lds0 + kTokens * kRowBytes);
@@ -684,7 +758,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_ro
 template <int BITS, int WR, bool GENERAL>
 hipError_t start(const TreeArgs& a, hipStream_t st) {
   constexpr int NW = kWaves<BITS, WR>;
-  constexpr int lds = BITS == 16 ? kStageLds + kPosLds : std::max(kDraftLds + NW * kMetaLds, kJoinLds);
+  constexpr int lds = BITS == 16 ? kStageLds + kPosLds : WR == 4 ? 2 * kImageLds + NW * kMetaLds : std::max(kDraftLds + NW * kMetaLds, kJoinLds);
   const hipError_t e = RDKV_ALLOW_LDS((tree_kernel<BITS, WR, GENERAL>), lds);
   if (e != hipSuccess) return e;
   const int units = (a.items * a.pieces + 7) / 8 * 8;
