@@ -211,19 +211,25 @@ struct Words4 {
 template <class Operand>
 __device__ __forceinline__ void scores4(const uint8_t* k_meta, const Query4& q, floatx16 (&s)[2], Operand operand) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+  // (a group's products before the one before's sums are scaled; the scheduler left alone would have all operands first, and spill them)
+  floatx16 sums[2];
+  const auto multiply = [&](int n) __attribute__((always_inline)) {
+    floatx16 p = product(operand(n >> 2, n & 3, 0), q.op[2 * (n & 3)], floatx16{});
+    sums[n & 1] = product(operand(n >> 2, n & 3, 1), q.op[2 * (n & 3) + 1], p);
+  };
+  multiply(0);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     s[x] = product(*reinterpret_cast<const halfx8*>(k_meta + 16 * slot_of_row(x, l32)), q.sums, floatx16{});
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      floatx16 sums = product(operand(x, g, 0), q.op[2 * g], floatx16{});
-      sums = product(operand(x, g, 1), q.op[2 * g + 1], sums);
+      if (4 * x + g < 7) multiply(4 * x + g + 1);
       const halfx8* sc = reinterpret_cast<const halfx8*>(k_meta + 1024 + 128 * g + 2 * (32 * half + 16 * x));
       const halfx8 sc0 = sc[0], sc1 = sc[1];
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        s[x][i] = __builtin_fmaf(static_cast<float>(i < 8 ? sc0[i & 7] : sc1[i & 7]), sums[i], s[x][i]);
-      __builtin_amdgcn_sched_barrier(0);         // (the scheduler would have all operands first, and spill them)
+        s[x][i] = __builtin_fmaf(static_cast<float>(i < 8 ? sc0[i & 7] : sc1[i & 7]), sums[g & 1][i], s[x][i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 }

@@ -472,6 +472,60 @@ def test_on_another_stream_and_twice_the_same(bits):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+def test_graphs_that_share_a_workspace_and_streams_that_do_not(bits):
+    """Two graphs of steps on two caches, replayed in turn over one workspace; the same calls at once on two streams with a workspace each."""
+    rng = np.random.default_rng(59)
+    made = []
+    for lens, n in (([900, 40], 9), ([300, 900], 33)):
+        s, _ = cached(rng, lens, 8, 2, 900, bits)
+        q, k, v = drafted(rng, 2, n, 8, 2)
+        made.append((s, q, k, v, cuda(np.stack([tree(rng, n)] * 2), I32), cuda([[0, -1], [0, 1]], I32)))
+    kept = [[t.clone() for t in (m[0].k, m[0].v, m[0].pos, m[0].weight, m[0].lens, m[0].next_pos)] for m in made]
+
+    def back():
+        for m, ts in zip(made, kept):
+            for t, name in zip(ts, ("k", "v", "pos", "weight", "lens", "next_pos")):
+                getattr(m[0], name).copy_(t)
+
+    def step(m, ws):
+        s, q, k, v, parent, path = m
+        out, stats = b.rdkv_slots_tree_attn(s, q, k, v, parent, workspace=ws)
+        return [out, stats, b.rdkv_slots_accept(s, q, k, v, path, stats, workspace=ws)]
+
+    def state(m):
+        return [t.clone() for t in (m[0].k, m[0].v, m[0].pos, m[0].weight, m[0].lens, m[0].next_pos)]
+
+    def same(a, c):
+        return all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, c))
+    size = max(max(m[0].tree_workspace(m[1].shape[1]).numel(), m[0].accept_workspace().numel()) for m in made)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    want = [[x.clone() for x in step(m, ws)] + state(m) for m in made]
+    twice = [[x.clone() for x in step(m, ws)] + state(m) for m in made]
+    back()
+    graphs, results = [], []
+    for m in made:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            results.append(step(m, ws))
+        graphs.append(g)
+    back()
+    for expected in (want, twice):
+        for g, r, m, w in zip(graphs, results, made, expected):
+            g.replay()
+            assert same([x.clone() for x in r] + state(m), w)
+    back()
+    streams, others = [torch.cuda.Stream() for _ in made], [torch.empty_like(ws) for _ in made]
+    torch.cuda.synchronize()
+    got = []
+    for m, st, w in zip(made, streams, others):
+        with torch.cuda.stream(st):
+            got.append(step(m, w))
+    torch.cuda.synchronize()
+    for m, r, w in zip(made, got, want):
+        assert same(r + state(m), w)
+
+
 def test_native_calls_do_as_the_others(monkeypatch):
     """Results made and given, with and without counts and a workspace, through the native code and without it."""
     rng = np.random.default_rng(53)
