@@ -220,7 +220,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
   for (int r0 = 0; r0 < rows; r0 += kRows) {
     const bool last_pass = r0 + kRows >= rows;
     const float keep = r0 == 0 ? old : 1.f;
-    rows_in(Query{}, r0);
+    int u = u0 + wave;                               // (the first segment is on its way with the rows)
     if constexpr (BITS == 16) {
       const uint8_t* K = a.s.k + static_cast<int64_t>(item) * cap * kRowBytes;
       const uint32_t lds0 = lds_address(mine);
@@ -236,9 +236,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
         copy_word_to_lds(weight + first, 4 * min(l32, last), to + kSegment * kRowBytes);
         copy_word_to_lds(pos + first, 4 * min(l32, last), to + kSegment * kRowBytes + 256);
       };
-      int u = u0 + wave, buffer = 0;
+      int buffer = 0;
+      if (u < u1) fetch(u, 0);
+      rows_in(Query{}, r0);
       if (u < u1) {
-        fetch(u, 0);
         for (; u < u1; u += WAVES, buffer ^= 1) {
           fetch(u + WAVES, buffer ^ 1);
           asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
@@ -270,8 +271,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void accept_weights_kernel(AcceptArg
           place[x] = pos[slot];
         }
       };
-      int u = u0 + wave;
       if (u < u1) load(u);
+      rows_in(Query{}, r0);
       for (; u < u1; u += WAVES) {
         const Words4 words(k);
         union { uint4 u; halfx4 h[2]; } m[2];
