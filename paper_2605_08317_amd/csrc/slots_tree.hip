@@ -337,19 +337,20 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
         for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
       }
     };
-    if constexpr (kStepsN == 2 && !kCareful && !GENERAL) {
+    if constexpr (!kCareful && !GENERAL) {
+      constexpr int N = 16 * kStepsN, kHalf = N / 2;   // scores of a stage; products of each kind
       // a stage's softmax and P V, and between their instructions the products of the next (MORE): a line is one product and what the plain ALUs do
       // meanwhile
-      const auto position = [&](auto more, int it, float (&x)[32], float (&next)[32]) __attribute__((always_inline)) {
+      const auto position = [&](auto more, int it, float (&x)[N], float (&next)[N]) __attribute__((always_inline)) {
         constexpr bool kMore = decltype(more)::value;
         refer(x, sc.factor, r);
         float sums[2] = {}, e[3], y = (x[0] - r.m) * sc.factor;
-        union { uint32_t u[16]; bf16x8 op[4]; } p;
+        union { uint32_t u[N / 2]; bf16x8 op[N / 8]; } p;
         // exponential i, in order; what hangs on another one's result stands behind it
         const auto make = [&](int i) __attribute__((always_inline)) {
           const float now = y;
-          if (i < 31) y = (x[i + 1] - r.m) * sc.factor;
-          if (i < 32) e[i % 3] = __builtin_amdgcn_exp2f(now);
+          if (i < N - 1) y = (x[i + 1] - r.m) * sc.factor;
+          if (i < N) e[i % 3] = __builtin_amdgcn_exp2f(now);
           if (i > 0) sums[i & 1] += e[(i - 1) % 3];
           if (i > 0 && (i & 1) == 0) p.u[(i >> 1) - 1] = pair_bf16(e[(i - 2) % 3], e[(i - 1) % 3]);
         };
@@ -357,37 +358,36 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
         constexpr int kAhead = 3;
         bf16x8 op[kAhead];
         const auto ask = [&](int i) __attribute__((always_inline)) {
-          if (i < 16) op[i % kAhead] = read_k(kt, i & 7, i >> 3);
-          else if (i < 32) op[i % kAhead] = read_v(vt, i & 3, (i >> 2) & 1, (i - 16) >> 3);
+          if (i < kHalf) op[i % kAhead] = read_k(kt, i & 7, i >> 3);
+          else if (i < N) op[i % kAhead] = read_v(vt, i & 3, (i >> 2) & 1, (i - kHalf) >> 3);
         };
         if constexpr (kMore) {
-          floatx16 s[2];
+          floatx16 s[kStepsN];
 #pragma unroll
           for (int i = 0; i < kAhead; ++i) ask(i);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          for (int i = 0; i < kHalf; ++i) {
             s[i >> 3] = product(op[i % kAhead], query.op[i & 7], (i & 7) == 0 ? floatx16{} : s[i >> 3]);
             ask(i + kAhead);
             make(i);
+            if (i == kHalf - 1) make(kHalf);
             __builtin_amdgcn_sched_barrier(0);
           }
 #pragma unroll
-          for (int i = 0; i < 32; ++i) next[i] = s[i >> 4][i & 15];
+          for (int i = 0; i < N; ++i) next[i] = s[i >> 4][i & 15];
         } else {
 #pragma unroll
-          for (int i = 16; i < 16 + kAhead; ++i) ask(i);
+          for (int i = kHalf; i < kHalf + kAhead; ++i) ask(i);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) make(i);
+          for (int i = 0; i <= kHalf; ++i) make(i);
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          r.o[i & 3] = product(op[(i + 16) % kAhead], p.op[i >> 2], r.o[i & 3]);
-          ask(i + 16 + kAhead);
-          if (i < 8) {
-            make(16 + 2 * i);
-            make(17 + 2 * i);
-          } else if (i == 8) {
-            make(32);
+        for (int i = 0; i < kHalf; ++i) {
+          r.o[i & 3] = product(op[(i + kHalf) % kAhead], p.op[i >> 2], r.o[i & 3]);
+          ask(i + kHalf + kAhead);
+          if (i < kHalf / 2) {
+            make(kHalf + 1 + 2 * i);
+            make(kHalf + 2 + 2 * i);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
         }
         tile_barrier<kCopies * (kBuffers - 1)>();
         const int n_mine = max(0, (end - begin - mine + kSlots - 1) / kSlots);         // stages in which this wavefront has slots
-        float even[32], odd[32];
+        float even[N], odd[N];
         int it = 0;
         if (n_mine > 0) {
           multiply(0, even);
