@@ -714,20 +714,24 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
   }
 }
 
-// The pieces' results of 8 rows.
-template <int BITS>
+// The pieces' results of 8 / PARTS rows, whose pieces PARTS groups of 32 lanes share out.
+template <int BITS, int PARTS>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_rows) {
-  const int g = a.s.g, n = a.n, rows = n * g, blocks = (rows + 7) / 8;
-  const int item = blockIdx.x / blocks, row = blockIdx.x % blocks * 8 + (threadIdx.x >> 5), c = threadIdx.x & 31;
+  constexpr int kRowsN = 8 / PARTS;
+  __shared__ float4 s_v[8][32], s_ml[8];
+  const int g = a.s.g, n = a.n, rows = n * g, blocks = (rows + kRowsN - 1) / kRowsN;
+  const int group = threadIdx.x >> 5, part = group % PARTS, c = threadIdx.x & 31;
+  const int item = blockIdx.x / blocks, row = blockIdx.x % blocks * kRowsN + group / PARTS;
   const int seq = item / a.s.hkv, kvh = item % a.s.hkv;
   const int count = a.counts ? min(max(a.counts[seq], 0), n) : n;
-  if (row >= count * g) return;
+  const bool there = row < count * g;
   const int64_t slot = (static_cast<int64_t>(item) * a.row_groups + row / group_rows) * a.pieces;
   const int64_t first = slot * group_rows + row % group_rows;
   const bool scored = a.s.cap > 0.f || a.s.slopes;
+  const int pieces = there ? a.pieces : 0;
   float m = kNoScore, top = kNoScore, unit = 1.f;
 #pragma unroll 4
-  for (int p = 0; p < a.pieces; ++p) {
+  for (int p = part; p < pieces; p += PARTS) {
     const float4 ml = *reinterpret_cast<const float4*>(a.part_ml + (first + static_cast<int64_t>(p) * group_rows) * 4);
     m = fmaxf(m, ml.x);
     top = fmaxf(top, ml.z);
@@ -736,15 +740,36 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_ro
   const float factor = scored ? kLog2e : unit * kRootLog2e;
   float l = 0.f;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int p = 0; p < a.pieces; ++p) {
-    const int64_t at = first + static_cast<int64_t>(p) * group_rows;
-    const float4 ml = *reinterpret_cast<const float4*>(a.part_ml + at * 4);
-    const float4 w = *reinterpret_cast<const float4*>(a.part_acc + at * kHeadDim + 4 * c);
-    const float f = __builtin_amdgcn_exp2f((ml.x - m) * factor);
+  const auto add = [&](const float4& ml, const float4& w, float over, float scale) {
+    const float f = __builtin_amdgcn_exp2f((ml.x - over) * scale);
     l = __builtin_fmaf(ml.y, f, l);
     v = make_float4(__builtin_fmaf(w.x, f, v.x), __builtin_fmaf(w.y, f, v.y), __builtin_fmaf(w.z, f, v.z), __builtin_fmaf(w.w, f, v.w));
+  };
+#pragma unroll 4
+  for (int p = part; p < pieces; p += PARTS) {
+    const int64_t at = first + static_cast<int64_t>(p) * group_rows;
+    add(*reinterpret_cast<const float4*>(a.part_ml + at * 4), *reinterpret_cast<const float4*>(a.part_acc + at * kHeadDim + 4 * c), m, factor);
   }
+  if constexpr (PARTS > 1) {
+    s_v[group][c] = v;
+    if (c == 0) s_ml[group] = make_float4(m, l, top, unit);
+    __syncthreads();
+    if (part != 0) return;
+    const float mine = m;
+#pragma unroll
+    for (int k = 1; k < PARTS; ++k) {
+      m = fmaxf(m, s_ml[group + k].x);
+      top = fmaxf(top, s_ml[group + k].z);
+    }
+    const float4 own = v;
+    const float own_l = l;
+    l = 0.f;
+    v = make_float4(0.f, 0.f, 0.f, 0.f);
+    add(make_float4(mine, own_l, 0.f, 0.f), own, m, factor);
+#pragma unroll
+    for (int k = 1; k < PARTS; ++k) add(s_ml[group + k], s_v[group + k][c], m, factor);
+  }
+  if (!there) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int64_t q_row = (static_cast<int64_t>(seq) * n + row / g) * a.s.hkv * g + kvh * g + row % g;
   union { __bf16 h[4]; uint2 u; } out;
@@ -754,6 +779,13 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_ro
   out.h[3] = static_cast<__bf16>(v.w * inv);
   *reinterpret_cast<uint2*>(a.out + q_row * kHeadDim + 4 * c) = out.u;
   if (c == 0 && a.stats) store_stats(a.stats + 2 * q_row, m, l, top, factor, scored ? 1.f : unit * kRoot, BITS == 4 ? kTopHalf : 0.f);
+}
+template <int BITS>
+hipError_t join(const TreeArgs& a, hipStream_t st) {
+  const int rows = a.n * a.s.g;
+  if (a.pieces <= 4) hipLaunchKernelGGL((tree_join_kernel<BITS, 1>), dim3(a.items * ((rows + 7) / 8)), dim3(256), 0, st, a, 32 * a.wide);
+  else hipLaunchKernelGGL((tree_join_kernel<BITS, 8>), dim3(a.items * rows), dim3(256), 0, st, a, 32 * a.wide);
+  return hipGetLastError();
 }
 
 template <int BITS, int WR, bool GENERAL>
@@ -782,10 +814,7 @@ hipError_t launch_tree(const TreeArgs& a, int bits, hipStream_t st) {
   hipError_t e = bits == 16 ? (general ? start<16, true>(a, a.wide, st) : start<16, false>(a, a.wide, st))
                             : (general ? start<4, true>(a, a.wide, st) : start<4, false>(a, a.wide, st));
   if (e != hipSuccess || a.pieces == 1) return e;
-  const int blocks = (a.n * a.s.g + 7) / 8;
-  if (bits == 16) hipLaunchKernelGGL(tree_join_kernel<16>, dim3(a.items * blocks), dim3(256), 0, st, a, 32 * a.wide);
-  else hipLaunchKernelGGL(tree_join_kernel<4>, dim3(a.items * blocks), dim3(256), 0, st, a, 32 * a.wide);
-  return hipGetLastError();
+  return bits == 16 ? join<16>(a, st) : join<4>(a, st);
 }
 
 }  // namespace slots
