@@ -1,6 +1,7 @@
 // Trees of drafted tokens over slot caches (rdkv_slots_tree_attn, rdkv_slots_accept): what the host side and the kernels share.
 #pragma once
 #include <algorithm>
+#include <cmath>
 
 #include "slots.h"
 
@@ -42,7 +43,10 @@ inline TreePlan plan_tree(int64_t items, int rows, int capacity, int bits) {
   // still has 32 stages (32 x 8 x 5000 .. 8192 slots 358 -> 342 us; 4 x 8 x 131072 of 16 stages 164 -> 170).
   int64_t card = bits == 16 ? 256 : 512;
   if (bits == 4 && 2 * card / std::max<int64_t>(groups, 1) * 32 * stage <= tiles) card *= 2;
-  p.slot_pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min(tiles / stage, card / std::max<int64_t>(groups, 1))));
+  // Nor more than 4 roots of the stages: a piece costs the join what a sixteenth of a stage costs (one item of 131072 slots, 256 pieces -> 128 or 90: bf16
+  // 29.0 -> 24.2 us, 4 bits 32.2 -> 27.1; with 2.4 roots 27.1 and 34.3).
+  const int64_t most = std::min(tiles / stage, static_cast<int64_t>(4.0 * std::sqrt(static_cast<double>(tiles / stage))));
+  p.slot_pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min(most, card / std::max<int64_t>(groups, 1))));
   p.pieces = p.slot_pieces > 1 && groups * (p.slot_pieces + 1) <= card ? p.slot_pieces + 1 : p.slot_pieces;
   return p;
 }
