@@ -715,7 +715,7 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
 }
 
 // The pieces' results of 8 / PARTS rows, whose pieces PARTS groups of 32 lanes share out: a chain of loads, so that many pieces need several groups
-// (256 of them 75 us by one, 8 by eight).
+// (a call with 256 of them 97 us by one, 32 by eight).
 template <int BITS, int PARTS>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_rows) {
   constexpr int kRowsN = 8 / PARTS;
