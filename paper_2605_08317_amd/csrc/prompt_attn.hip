@@ -179,7 +179,10 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
       const float now = x;
       if (i < 31) x = __builtin_fmaf(s[(i + 1) >> 4][(i + 1) & 15], factor, ref);
       if (i < 32) e[i % 3] = __builtin_amdgcn_exp2f(now);
-      if (i > 0) sums[i & 1] += e[(i - 1) % 3];
+      if (i > 0) {
+        sums[i & 1] += e[(i - 1) % 3];
+        here(sums[i & 1]);
+      }
       if (i > 0 && (i & 1) == 0) p.u[(i >> 1) - 1] = pair_bf16(e[(i - 2) % 3], e[(i - 1) % 3]);
     };
     // operands on their way from LDS, of products 0 .. 15 (K) and 16 .. 31 (V: keys 16 (i / 4) .., channels 32 (i % 4) ..)
@@ -203,8 +206,7 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
 #pragma unroll
       for (int i = 16; i < 16 + kAhead; ++i) ask(i);
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        make(i);
+      for (int i = 0; i < 16; ++i) make(i);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -220,6 +222,7 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
         const floatx16& n = next[j >> 4];
         const float a = n[j & 15], b = n[(j & 15) + 1], c = n[(j & 15) + 2], d = n[(j & 15) + 3];
         tops = fmaxf(fmaxf(i == 8 ? a : fmaxf(tops, a), b), fmaxf(c, d));
+        if (!GENERAL) here(tops);
       }
       __builtin_amdgcn_sched_barrier(0);
     }

@@ -351,7 +351,10 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
           const float now = y;
           if (i < N - 1) y = (x[i + 1] - r.m) * sc.factor;
           if (i < N) e[i % 3] = __builtin_amdgcn_exp2f(now);
-          if (i > 0) sums[i & 1] += e[(i - 1) % 3];
+          if (i > 0) {
+            sums[i & 1] += e[(i - 1) % 3];
+            here(sums[i & 1]);
+          }
           if (i > 0 && (i & 1) == 0) p.u[(i >> 1) - 1] = pair_bf16(e[(i - 2) % 3], e[(i - 1) % 3]);
         };
         const uint32_t kt = k_of(it + 1) + mine * kRowBytes + k_lane(), vt = v_of(it) + mine * kRowBytes + v_lane();
