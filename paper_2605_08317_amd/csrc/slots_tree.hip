@@ -292,305 +292,310 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
     for (int i = 0; i < most; i += 4 * NW) copy_to_lds(from, static_cast<uint32_t>(min(prow + i, last)) * stride + at, to + i * kRowBytes + wave * 1024);
   };
 
-  // Careful (bf16): rows of V that a window hides from some query rows are kept from meeting their zeros, which make NaN of what is not finite.  Done
-  // again so where results are not finite.
+  // Careful (bf16): rows of V that a window hides from some query rows, and those behind the last that are the last again, are kept from meeting their
+  // zeros, which make NaN of what is not finite.  Done again so where results are not finite.
   const auto walk = [&](auto careful) __attribute__((always_inline)) {
-  constexpr bool kCareful = decltype(careful)::value;
-  r.init();
-  if constexpr (BITS == 16) {
-    constexpr int kStepsN = kSteps16<WR>, kSlots = kStage<WR>, kBuffers = kStages<WR>, kMine = 32 * kStepsN;
-    constexpr int kCopies = kSlots / (2 * NW) + (GENERAL ? 1 : 0);      // of a wavefront and stage
-    const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
-    const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
-    constexpr uint32_t kSide = kSlots * kRowBytes;
-    const int n_it = (end - begin + kSlots - 1) / kSlots, mine = ws * kMine;
-    uint8_t* s_pos = smem + kStageLds;
-    const auto k_of = [&](int it) { return lds0 + it % kBuffers * kSide; };
-    const auto v_of = [&](int it) { return lds0 + (kBuffers + it % kBuffers) * kSide; };
-    const auto fetch_k = [&](int it) __attribute__((always_inline)) {
-      const int first = begin + min(it, n_it - 1) * kSlots;
-      fetch_rows(K + static_cast<int64_t>(first) * kRowBytes, k_at, kRowBytes, end - 1 - first, kSlots, k_of(it));
-      if constexpr (GENERAL) copy_word_to_lds(pos + first, 4 * (min(first + mine + lane, end - 1) - first), lds0 + kStageLds + (wave * kBuffers + it % kBuffers) * 256);
-    };
-    const auto fetch_v = [&](int it) __attribute__((always_inline)) {
-      const int first = begin + min(it, n_it - 1) * kSlots;
-      fetch_rows(V + static_cast<int64_t>(first) * kRowBytes, v_at, kRowBytes, end - 1 - first, kSlots, v_of(it));
-    };
-    const auto left_of = [&](int it) { return end - begin - it * kSlots - mine - 4 * half; };
-    const auto finish = [&](int it, float (&x)[16 * kStepsN]) __attribute__((always_inline)) {
-      const int left = left_of(it);
-      const int4* where = reinterpret_cast<const int4*>(s_pos + (wave * kBuffers + it % kBuffers) * 256);
-      to_scores<GENERAL>(sc, row, x, left < kMine, [&](int k, float* d) __attribute__((always_inline)) {
-        const int4 at = where[2 * k + half];
-        d[0] = static_cast<float>(next - at.x);
-        d[1] = static_cast<float>(next - at.y);
-        d[2] = static_cast<float>(next - at.z);
-        d[3] = static_cast<float>(next - at.w);
-      }, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[2 * k + half]; },
-                         [&](int i) __attribute__((always_inline)) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) >= left; });
-    };
-    const auto multiply = [&](int it, float (&x)[16 * kStepsN]) __attribute__((always_inline)) {
+    constexpr bool kCareful = decltype(careful)::value;
+    r.init();
+    if constexpr (BITS == 16) {
+      constexpr int kStepsN = kSteps16<WR>, kSlots = kStage<WR>, kBuffers = kStages<WR>, kMine = 32 * kStepsN;
+      constexpr int kCopies = kSlots / (2 * NW) + (GENERAL ? 1 : 0);      // of a wavefront and stage
+      const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
+      const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.capacity * kRowBytes;
+      constexpr uint32_t kSide = kSlots * kRowBytes;
+      const int n_it = (end - begin + kSlots - 1) / kSlots, mine = ws * kMine;
+      uint8_t* s_pos = smem + kStageLds;
+      const auto k_of = [&](int it) { return lds0 + it % kBuffers * kSide; };
+      const auto v_of = [&](int it) { return lds0 + (kBuffers + it % kBuffers) * kSide; };
+      const auto fetch_k = [&](int it) __attribute__((always_inline)) {
+        const int first = begin + min(it, n_it - 1) * kSlots;
+        fetch_rows(K + static_cast<int64_t>(first) * kRowBytes, k_at, kRowBytes, end - 1 - first, kSlots, k_of(it));
+        if constexpr (GENERAL) copy_word_to_lds(pos + first, 4 * (min(first + mine + lane, end - 1) - first),
+                                                lds0 + kStageLds + (wave * kBuffers + it % kBuffers) * 256);
+      };
+      const auto fetch_v = [&](int it) __attribute__((always_inline)) {
+        const int first = begin + min(it, n_it - 1) * kSlots;
+        fetch_rows(V + static_cast<int64_t>(first) * kRowBytes, v_at, kRowBytes, end - 1 - first, kSlots, v_of(it));
+      };
+      const auto left_of = [&](int it) { return end - begin - it * kSlots - mine - 4 * half; };
+      const auto finish = [&](int it, float (&x)[16 * kStepsN]) __attribute__((always_inline)) {
+        const int left = left_of(it);
+        const int4* where = reinterpret_cast<const int4*>(s_pos + (wave * kBuffers + it % kBuffers) * 256);
+        to_scores<GENERAL>(sc, row, x, left < kMine, [&](int k, float* d) __attribute__((always_inline)) {
+          const int4 at = where[2 * k + half];
+          d[0] = static_cast<float>(next - at.x);
+          d[1] = static_cast<float>(next - at.y);
+          d[2] = static_cast<float>(next - at.z);
+          d[3] = static_cast<float>(next - at.w);
+        }, [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[2 * k + half]; },
+                           [&](int i) __attribute__((always_inline)) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) >= left; });
+      };
+      const auto multiply = [&](int it, float (&x)[16 * kStepsN]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int k = 0; k < kStepsN; ++k) {
-        const floatx16 s = scores16(k_of(it) + mine * kRowBytes + k_lane(), k, query);
+        for (int k = 0; k < kStepsN; ++k) {
+          const floatx16 s = scores16(k_of(it) + mine * kRowBytes + k_lane(), k, query);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
-      }
-    };
-    if constexpr (!kCareful && !GENERAL) {
-      constexpr int N = 16 * kStepsN, kHalf = N / 2;   // scores of a stage; products of each kind
-      // a stage's softmax and P V, and between their instructions the products of the next (MORE): a line is one product and what the plain ALUs do
-      // meanwhile
-      const auto position = [&](auto more, int it, float (&x)[N], float (&next)[N]) __attribute__((always_inline)) {
-        constexpr bool kMore = decltype(more)::value;
-        refer(x, sc.factor, r);
-        float sums[2] = {}, e[3], y = (x[0] - r.m) * sc.factor;
-        union { uint32_t u[N / 2]; bf16x8 op[N / 8]; } p;
-        // exponential i, in order; what hangs on another one's result stands behind it
-        const auto make = [&](int i) __attribute__((always_inline)) {
-          const float now = y;
-          if (i < N - 1) y = (x[i + 1] - r.m) * sc.factor;
-          if (i < N) e[i % 3] = __builtin_amdgcn_exp2f(now);
-          if (i > 0) {
-            sums[i & 1] += e[(i - 1) % 3];
-            here(sums[i & 1]);
+          for (int i = 0; i < 16; ++i) x[16 * k + i] = s[i];
+        }
+      };
+      if constexpr (!kCareful && !GENERAL) {
+        constexpr int N = 16 * kStepsN, kHalf = N / 2;   // scores of a stage; products of each kind
+        // a stage's softmax and P V, and between their instructions the products of the next (MORE): a line is one product and what the plain ALUs do
+        // meanwhile
+        const auto position = [&](auto more, int it, float (&x)[N], float (&next)[N]) __attribute__((always_inline)) {
+          constexpr bool kMore = decltype(more)::value;
+          refer(x, sc.factor, r);
+          float sums[2] = {}, e[3], y = (x[0] - r.m) * sc.factor;
+          union { uint32_t u[N / 2]; bf16x8 op[N / 8]; } p;
+          // exponential i, in order; what hangs on another one's result stands behind it
+          const auto make = [&](int i) __attribute__((always_inline)) {
+            const float now = y;
+            if (i < N - 1) y = (x[i + 1] - r.m) * sc.factor;
+            if (i < N) e[i % 3] = __builtin_amdgcn_exp2f(now);
+            if (i > 0) {
+              sums[i & 1] += e[(i - 1) % 3];
+              here(sums[i & 1]);
+            }
+            if (i > 0 && (i & 1) == 0) p.u[(i >> 1) - 1] = pair_bf16(e[(i - 2) % 3], e[(i - 1) % 3]);
+          };
+          const uint32_t kt = k_of(it + 1) + mine * kRowBytes + k_lane(), vt = v_of(it) + mine * kRowBytes + v_lane();
+          constexpr int kAhead = 3;
+          bf16x8 op[kAhead];
+          const auto ask = [&](int i) __attribute__((always_inline)) {
+            if (i < kHalf) op[i % kAhead] = read_k(kt, i & 7, i >> 3);
+            else if (i < N) op[i % kAhead] = read_v(vt, i & 3, (i >> 2) & 1, (i - kHalf) >> 3);
+          };
+          if constexpr (kMore) {
+            floatx16 s[kStepsN];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) ask(i);
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) {
+              s[i >> 3] = product(op[i % kAhead], query.op[i & 7], (i & 7) == 0 ? floatx16{} : s[i >> 3]);
+              ask(i + kAhead);
+              make(i);
+              if (i == kHalf - 1) make(kHalf);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) next[i] = s[i >> 4][i & 15];
+          } else {
+#pragma unroll
+            for (int i = kHalf; i < kHalf + kAhead; ++i) ask(i);
+#pragma unroll
+            for (int i = 0; i <= kHalf; ++i) make(i);
           }
-          if (i > 0 && (i & 1) == 0) p.u[(i >> 1) - 1] = pair_bf16(e[(i - 2) % 3], e[(i - 1) % 3]);
-        };
-        const uint32_t kt = k_of(it + 1) + mine * kRowBytes + k_lane(), vt = v_of(it) + mine * kRowBytes + v_lane();
-        constexpr int kAhead = 3;
-        bf16x8 op[kAhead];
-        const auto ask = [&](int i) __attribute__((always_inline)) {
-          if (i < kHalf) op[i % kAhead] = read_k(kt, i & 7, i >> 3);
-          else if (i < N) op[i % kAhead] = read_v(vt, i & 3, (i >> 2) & 1, (i - kHalf) >> 3);
-        };
-        if constexpr (kMore) {
-          floatx16 s[kStepsN];
-#pragma unroll
-          for (int i = 0; i < kAhead; ++i) ask(i);
 #pragma unroll
           for (int i = 0; i < kHalf; ++i) {
-            s[i >> 3] = product(op[i % kAhead], query.op[i & 7], (i & 7) == 0 ? floatx16{} : s[i >> 3]);
-            ask(i + kAhead);
-            make(i);
-            if (i == kHalf - 1) make(kHalf);
+            r.o[i & 3] = product(op[(i + kHalf) % kAhead], p.op[i >> 2], r.o[i & 3]);
+            ask(i + kHalf + kAhead);
+            if (i < kHalf / 2) {
+              make(kHalf + 1 + 2 * i);
+              make(kHalf + 2 + 2 * i);
+            }
             __builtin_amdgcn_sched_barrier(0);
           }
+          r.l += sums[0] + sums[1];
+          if constexpr (kMore) finish(it + 1, next);
+        };
+        // K of stage it + 1 and V of stage it are there, K of stage it and V of the one before are done with
+        const auto open = [&](int it) __attribute__((always_inline)) {
+          tile_barrier<kCopies * (kBuffers - 2)>();
+          fetch_k(it + kBuffers);
+          fetch_v(it + kBuffers - 1);
+        };
+        if (n_it > 0) {
+          fetch_k(0);
 #pragma unroll
-          for (int i = 0; i < N; ++i) next[i] = s[i >> 4][i & 15];
-        } else {
-#pragma unroll
-          for (int i = kHalf; i < kHalf + kAhead; ++i) ask(i);
-#pragma unroll
-          for (int i = 0; i <= kHalf; ++i) make(i);
-        }
-#pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-          r.o[i & 3] = product(op[(i + kHalf) % kAhead], p.op[i >> 2], r.o[i & 3]);
-          ask(i + kHalf + kAhead);
-          if (i < kHalf / 2) {
-            make(kHalf + 1 + 2 * i);
-            make(kHalf + 2 + 2 * i);
+          for (int it = 0; it < kBuffers - 1; ++it) {
+            fetch_k(it + 1);
+            fetch_v(it);
           }
-          __builtin_amdgcn_sched_barrier(0);
+          tile_barrier<kCopies * (kBuffers - 1)>();
+          const int n_mine = max(0, (end - begin - mine + kSlots - 1) / kSlots);         // stages in which this wavefront has slots
+          float even[N], odd[N];
+          int it = 0;
+          if (n_mine > 0) {
+            multiply(0, even);
+            finish(0, even);
+          }
+          for (; it + 2 < n_mine; it += 2) {
+            open(it);
+            position(std::true_type{}, it, even, odd);
+            open(it + 1);
+            position(std::true_type{}, it + 1, odd, even);
+          }
+          if (it < n_mine) {
+            open(it);
+            if (it + 1 < n_mine) {
+              position(std::true_type{}, it, even, odd);
+              open(++it);
+              position(std::false_type{}, it, odd, even);
+            } else {
+              position(std::false_type{}, it, even, odd);
+            }
+            ++it;
+          }
+          for (; it < n_it; ++it) open(it);
+          tile_barrier<0>();
         }
-        r.l += sums[0] + sums[1];
-        if constexpr (kMore) finish(it + 1, next);
-      };
-      // K of stage it + 1 and V of stage it are there, K of stage it and V of the one before are done with
-      const auto open = [&](int it) __attribute__((always_inline)) {
-        tile_barrier<kCopies * (kBuffers - 2)>();
-        fetch_k(it + kBuffers);
-        fetch_v(it + kBuffers - 1);
-      };
-      if (n_it > 0) {
-        fetch_k(0);
+      } else if (n_it > 0) {
 #pragma unroll
         for (int it = 0; it < kBuffers - 1; ++it) {
-          fetch_k(it + 1);
+          fetch_k(it);
           fetch_v(it);
         }
-        tile_barrier<kCopies * (kBuffers - 1)>();
-        const int n_mine = max(0, (end - begin - mine + kSlots - 1) / kSlots);         // stages in which this wavefront has slots
-        float even[N], odd[N];
-        int it = 0;
-        if (n_mine > 0) {
-          multiply(0, even);
-          finish(0, even);
+        for (int it = 0; it < n_it; ++it) {
+          tile_barrier<kCopies * (kBuffers - 2)>();
+          fetch_k(it + kBuffers - 1);
+          fetch_v(it + kBuffers - 1);
+          if (left_of(it) + 4 * half <= 0) continue;
+          float x[16 * kStepsN];
+          multiply(it, x);
+          finish(it, x);
+          add_rows16<kStepsN, kCareful>(x, sc.factor, v_of(it) + mine * kRowBytes + v_lane(), 0.f, r);
         }
-        for (; it + 2 < n_mine; it += 2) {
-          open(it);
-          position(std::true_type{}, it, even, odd);
-          open(it + 1);
-          position(std::true_type{}, it + 1, odd, even);
-        }
-        if (it < n_mine) {
-          open(it);
-          if (it + 1 < n_mine) {
-            position(std::true_type{}, it, even, odd);
-            open(++it);
-            position(std::false_type{}, it, odd, even);
-          } else {
-            position(std::false_type{}, it, even, odd);
-          }
-          ++it;
-        }
-        for (; it < n_it; ++it) open(it);
         tile_barrier<0>();
       }
-    } else if (n_it > 0) {
-#pragma unroll
-      for (int it = 0; it < kBuffers - 1; ++it) {
-        fetch_k(it);
-        fetch_v(it);
-      }
-      for (int it = 0; it < n_it; ++it) {
-        tile_barrier<kCopies * (kBuffers - 2)>();
-        fetch_k(it + kBuffers - 1);
-        fetch_v(it + kBuffers - 1);
-        if (left_of(it) + 4 * half <= 0) continue;
-        float x[16 * kStepsN];
-        multiply(it, x);
-        finish(it, x);
-        add_rows16<kStepsN, kCareful>(x, sc.factor, v_of(it) + mine * kRowBytes + v_lane(), 0.f, r);
-      }
-      tile_barrier<0>();
-    }
-  } else {
-    constexpr bool kShared = WR == 4;                  // every wavefront has the same tiles
-    uint8_t* meta = smem + (kShared ? 2 * kImageLds : kDraftLds) + wave * kMetaLds;
-    const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
-    const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
-    const int t1 = (end + kTileRows - 1) / kTileRows;
-    const Codes4 codes;
-    // a tile's scores, softmax and P V
-    const auto put_positions = [&](int at) __attribute__((always_inline)) {
-      if constexpr (GENERAL) {
-        reinterpret_cast<int*>(meta + kKMeta + 1024)[lane] = at;
-        reinterpret_cast<float*>(meta + kKMeta + 1024 + 256)[lane] = static_cast<float>(next - at);
-      }
-    };
-    const auto finish = [&](int left, const floatx16 (&s)[2], float (&x)[32]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = s[i >> 4][i & 15];
-      const int4* where = reinterpret_cast<const int4*>(meta + kKMeta + 1024) + 8 * half;
-      to_scores<GENERAL>(sc, row, x, left < kTileRows,
-                         [&](int k, float* d) __attribute__((always_inline)) { *reinterpret_cast<int4*>(d) = where[16 + k]; },
-                         [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[k]; },
-                         [&](int i) __attribute__((always_inline)) { return 32 * half + i >= left; });
-    };
-    // value(channel group, step)
-    const auto add = [&](const float (&x)[32], int tile, int left, uint64_t odd, auto value) __attribute__((always_inline)) {
-      float p[32], pf[32];
-      softmax(x, sc.factor, kTopHalf, r, p);
-      halfx8 op[4];
-#pragma unroll
-      for (int f = 0; f < 4; ++f) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          pf[8 * f + j] = p[4 * f + j];
-          pf[8 * f + 4 + j] = p[16 + 4 * f + j];
+    } else {
+      constexpr bool kShared = WR == 4;                  // every wavefront has the same tiles
+      uint8_t* meta = smem + (kShared ? 2 * kImageLds : kDraftLds) + wave * kMetaLds;
+      const uint8_t* K = a.s.k + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
+      const uint8_t* V = a.s.v + static_cast<int64_t>(item) * a.s.tiles * kTileBytes;
+      const int t1 = (end + kTileRows - 1) / kTileRows;
+      const Codes4 codes;
+      // a tile's scores, softmax and P V
+      const auto put_positions = [&](int at) __attribute__((always_inline)) {
+        if constexpr (GENERAL) {
+          reinterpret_cast<int*>(meta + kKMeta + 1024)[lane] = at;
+          reinterpret_cast<float*>(meta + kKMeta + 1024 + 256)[lane] = static_cast<float>(next - at);
         }
-        op[f] = to_half(pf + 8 * f);
-      }
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        __builtin_amdgcn_sched_barrier(0);
-        add_values<false>(op, pf, [&](int f) __attribute__((always_inline)) { return value(c, f); }, r.o[c]);
-      }
-      if (GENERAL && odd != 0) add_odd(odd, V + static_cast<int64_t>(tile) * kTileBytes, left, meta + kMetaLds - 256, p, r);
-    };
-    const auto values = [&](const uint4& words, int c, int f) __attribute__((always_inline)) {
-      return f == 0 ? values4<0>(codes, words, meta + kKMeta, c) : f == 1 ? values4<1>(codes, words, meta + kKMeta, c)
-           : f == 2 ? values4<2>(codes, words, meta + kKMeta, c) : values4<3>(codes, words, meta + kKMeta, c);
-    };
-    int t = begin / kTileRows + ws;
-    if constexpr (!kShared) {
-      Side4 k, v;
-      int at = 0;
-      // the next tile's K comes while this one's values are added up, its V while its scores are made
-      const auto load_k = [&](int tile) __attribute__((always_inline)) {
-        k.load(K + static_cast<int64_t>(tile) * kTileBytes, true);
-        if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
       };
-      const auto load_v = [&](int tile) __attribute__((always_inline)) { v.load(V + static_cast<int64_t>(tile) * kTileBytes, false); };
-      if (t < t1) {
-        load_k(t);
-        load_v(t);
-      }
-      for (; t < t1; t += WS) {
-        const int left = end - t * kTileRows;
-        put_k_meta(meta, k.meta, left);
-        put_positions(at);
-        wave_lds_order();
-        floatx16 s[2];
-        {
-          const Words4 words(k);
-          scores4(meta, query, s, [&](int x, int g, int h) __attribute__((always_inline)) { return words.operand(codes, x, g, h); });
+      const auto finish = [&](int left, const floatx16 (&s)[2], float (&x)[32]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = s[i >> 4][i & 15];
+        const int4* where = reinterpret_cast<const int4*>(meta + kKMeta + 1024) + 8 * half;
+        to_scores<GENERAL>(sc, row, x, left < kTileRows,
+                           [&](int k, float* d) __attribute__((always_inline)) { *reinterpret_cast<int4*>(d) = where[16 + k]; },
+                           [&](int k, int* at) __attribute__((always_inline)) { *reinterpret_cast<int4*>(at) = where[k]; },
+                           [&](int i) __attribute__((always_inline)) { return 32 * half + i >= left; });
+      };
+      // value(channel group, step)
+      const auto add = [&](const float (&x)[32], int tile, int left, uint64_t odd, auto value) __attribute__((always_inline)) {
+        float p[32], pf[32];
+        softmax(x, sc.factor, kTopHalf, r, p);
+        halfx8 op[4];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            pf[8 * f + j] = p[4 * f + j];
+            pf[8 * f + 4 + j] = p[16 + 4 * f + j];
+          }
+          op[f] = to_half(pf + 8 * f);
         }
-        load_k(min(t + WS, t1 - 1));
-        float x[32];
-        finish(left, s, x);
-        // with a window, values that are not finite are kept out, and go to those rows that see them afterwards
-        const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v.meta, left);
-        wave_lds_order();
-        add(x, t, left, odd, [&](int c, int f) __attribute__((always_inline)) { return values(v.codes[c], c, f); });
-        load_v(min(t + WS, t1 - 1));
-        wave_lds_order();
-      }
-    } else if (t < t1) {
-      // Each wavefront makes operands of a group's codes for all four, a tile ahead, into one of two images in LDS.
-      uint4 k_codes, k_meta, v_codes, v_meta;
-      int at = 0;
-      const auto load = [&](int tile) __attribute__((always_inline)) {
-        const uint8_t *kt = K + static_cast<int64_t>(tile) * kTileBytes, *vt = V + static_cast<int64_t>(tile) * kTileBytes;
-        k_codes = *reinterpret_cast<const uint4*>(kt + 1024 * wave + 16 * slot_of_row(half, l32));
-        k_meta = *reinterpret_cast<const uint4*>(kt + kTileCodes + 16 * lane);
-        v_codes = *reinterpret_cast<const uint4*>(vt + 1024 * wave + 16 * lane);
-        v_meta = *reinterpret_cast<const uint4*>(vt + kTileCodes + 16 * lane);
-        if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          __builtin_amdgcn_sched_barrier(0);
+          add_values<false>(op, pf, [&](int f) __attribute__((always_inline)) { return value(c, f); }, r.o[c]);
+        }
+        if (GENERAL && odd != 0) add_odd(odd, V + static_cast<int64_t>(tile) * kTileBytes, left, meta + kMetaLds - 256, p, r);
       };
-      const auto image = [&](int tile) { return smem + (tile & 1) * kImageLds + 16 * lane; };
-      const auto make = [&](int tile) __attribute__((always_inline)) {
-        const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v_meta, end - tile * kTileRows);
-        wave_lds_order();
-        uint8_t* to = image(tile);
-        const Group4 group(k_codes);
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) *reinterpret_cast<halfx8*>(to + ((4 * x + wave) * 2 + h) * 1024) = group.operand(codes, x, h);
-#pragma unroll
-        for (int f = 0; f < 4; ++f) *reinterpret_cast<halfx8*>(to + kImageLds / 2 + (4 * wave + f) * 1024) = values(v_codes, wave, f);
-        return odd;
+      const auto values = [&](const uint4& words, int c, int f) __attribute__((always_inline)) {
+        return f == 0 ? values4<0>(codes, words, meta + kKMeta, c) : f == 1 ? values4<1>(codes, words, meta + kKMeta, c)
+             : f == 2 ? values4<2>(codes, words, meta + kKMeta, c) : values4<3>(codes, words, meta + kKMeta, c);
       };
-      load(t);
-      uint64_t odd = make(t);
-      uint4 meta_now = k_meta;
-      int at_now = at;
-      load(min(t + 1, t1 - 1));
-      tile_barrier<63>();
-      for (; t < t1; ++t) {
-        const int left = end - t * kTileRows;
-        put_k_meta(meta, meta_now, left);
-        put_positions(at_now);
-        uint64_t odd_next = 0;
-        if (t + 1 < t1) odd_next = make(t + 1);
-        meta_now = k_meta;
-        at_now = at;
-        load(min(t + 2, t1 - 1));
-        wave_lds_order();
-        const uint8_t* from = image(t);
-        floatx16 s[2];
-        scores4(meta, query, s, [&](int x, int g, int h) __attribute__((always_inline)) { return *reinterpret_cast<const halfx8*>(from + ((4 * x + g) * 2 + h) * 1024); });
-        float x[32];
-        finish(left, s, x);
-        add(x, t, left, odd, [&](int c, int f) __attribute__((always_inline)) { return *reinterpret_cast<const halfx8*>(from + kImageLds / 2 + (4 * c + f) * 1024); });
-        odd = odd_next;
+      int t = begin / kTileRows + ws;
+      if constexpr (!kShared) {
+        Side4 k, v;
+        int at = 0;
+        // the next tile's K comes while this one's values are added up, its V while its scores are made
+        const auto load_k = [&](int tile) __attribute__((always_inline)) {
+          k.load(K + static_cast<int64_t>(tile) * kTileBytes, true);
+          if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
+        };
+        const auto load_v = [&](int tile) __attribute__((always_inline)) { v.load(V + static_cast<int64_t>(tile) * kTileBytes, false); };
+        if (t < t1) {
+          load_k(t);
+          load_v(t);
+        }
+        for (; t < t1; t += WS) {
+          const int left = end - t * kTileRows;
+          put_k_meta(meta, k.meta, left);
+          put_positions(at);
+          wave_lds_order();
+          floatx16 s[2];
+          {
+            const Words4 words(k);
+            scores4(meta, query, s, [&](int x, int g, int h) __attribute__((always_inline)) { return words.operand(codes, x, g, h); });
+          }
+          load_k(min(t + WS, t1 - 1));
+          float x[32];
+          finish(left, s, x);
+          // with a window, values that are not finite are kept out, and go to those rows that see them afterwards
+          const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v.meta, left);
+          wave_lds_order();
+          add(x, t, left, odd, [&](int c, int f) __attribute__((always_inline)) { return values(v.codes[c], c, f); });
+          load_v(min(t + WS, t1 - 1));
+          wave_lds_order();
+        }
+      } else if (t < t1) {
+        // Each wavefront makes operands of a group's codes for all four, a tile ahead, into one of two images in LDS.
+        uint4 k_codes, k_meta, v_codes, v_meta;
+        int at = 0;
+        const auto load = [&](int tile) __attribute__((always_inline)) {
+          const uint8_t *kt = K + static_cast<int64_t>(tile) * kTileBytes, *vt = V + static_cast<int64_t>(tile) * kTileBytes;
+          k_codes = *reinterpret_cast<const uint4*>(kt + 1024 * wave + 16 * slot_of_row(half, l32));
+          k_meta = *reinterpret_cast<const uint4*>(kt + kTileCodes + 16 * lane);
+          v_codes = *reinterpret_cast<const uint4*>(vt + 1024 * wave + 16 * lane);
+          v_meta = *reinterpret_cast<const uint4*>(vt + kTileCodes + 16 * lane);
+          if constexpr (GENERAL) at = pos[min(tile * kTileRows + lane, len - 1)];
+        };
+        const auto image = [&](int tile) { return smem + (tile & 1) * kImageLds + 16 * lane; };
+        const auto make = [&](int tile) __attribute__((always_inline)) {
+          const uint64_t odd = put_v_meta<GENERAL>(meta + kKMeta, v_meta, end - tile * kTileRows);
+          wave_lds_order();
+          uint8_t* to = image(tile);
+          const Group4 group(k_codes);
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) *reinterpret_cast<halfx8*>(to + ((4 * x + wave) * 2 + h) * 1024) = group.operand(codes, x, h);
+#pragma unroll
+          for (int f = 0; f < 4; ++f) *reinterpret_cast<halfx8*>(to + kImageLds / 2 + (4 * wave + f) * 1024) = values(v_codes, wave, f);
+          return odd;
+        };
+        load(t);
+        uint64_t odd = make(t);
+        uint4 meta_now = k_meta;
+        int at_now = at;
+        load(min(t + 1, t1 - 1));
         tile_barrier<63>();
+        for (; t < t1; ++t) {
+          const int left = end - t * kTileRows;
+          put_k_meta(meta, meta_now, left);
+          put_positions(at_now);
+          uint64_t odd_next = 0;
+          if (t + 1 < t1) odd_next = make(t + 1);
+          meta_now = k_meta;
+          at_now = at;
+          load(min(t + 2, t1 - 1));
+          wave_lds_order();
+          const uint8_t* from = image(t);
+          floatx16 s[2];
+          scores4(meta, query, s, [&](int x, int g, int h) __attribute__((always_inline)) {
+            return *reinterpret_cast<const halfx8*>(from + ((4 * x + g) * 2 + h) * 1024);
+          });
+          float x[32];
+          finish(left, s, x);
+          add(x, t, left, odd, [&](int c, int f) __attribute__((always_inline)) {
+            return *reinterpret_cast<const halfx8*>(from + kImageLds / 2 + (4 * c + f) * 1024);
+          });
+          odd = odd_next;
+          tile_barrier<63>();
+        }
       }
     }
-  }
   };
   walk(std::false_type{});
   if constexpr (BITS == 16) {
