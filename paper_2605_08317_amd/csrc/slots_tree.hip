@@ -791,8 +791,10 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int group_ro
 }
 template <int BITS>
 hipError_t join(const TreeArgs& a, hipStream_t st) {
-  const int rows = a.n * a.s.g;
-  if (a.pieces <= 4) hipLaunchKernelGGL((tree_join_kernel<BITS, 1>), dim3(a.items * ((rows + 7) / 8)), dim3(256), 0, st, a, 32 * a.wide);
+  // where eight rows a workgroup fill the card, or pieces are few, one group has a row (8 pieces of 32 x 256 rows 10 us, by eight groups 19)
+  const int rows = a.n * a.s.g, eights = (rows + 7) / 8;
+  if (a.pieces <= 4 || static_cast<int64_t>(a.items) * eights >= 512)
+    hipLaunchKernelGGL((tree_join_kernel<BITS, 1>), dim3(a.items * eights), dim3(256), 0, st, a, 32 * a.wide);
   else hipLaunchKernelGGL((tree_join_kernel<BITS, 8>), dim3(a.items * rows), dim3(256), 0, st, a, 32 * a.wide);
   return hipGetLastError();
 }
