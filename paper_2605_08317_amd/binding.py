@@ -460,7 +460,8 @@ def _int32(name, x):
 
 
 def _rows_of(t, name, tokens, heads, d, device):
-    """The stride that names a tensor's layout: 0 of a flat ragged one, or that of rows [tokens, heads, d] whose heads lie side by side."""
+    """The stride that names a tensor's layout: 0 of a flat ragged one, or that of rows [tokens, heads, d] whose heads lie side by side, and one row behind
+    another (rows of an expanded view have a stride of 0 as well, which would name the other layout)."""
     if t.dtype != torch.bfloat16 or t.device != device:
         raise ValueError(f"{name} must be a torch.bfloat16 tensor on {device}: got {t.dtype} on {t.device}")
     if t.dim() in (1, 2):
@@ -469,6 +470,8 @@ def _rows_of(t, name, tokens, heads, d, device):
         return 0
     if tuple(t.shape) != (tokens, heads, d) or t.numel() > 0 and (t.stride(2) != 1 or heads > 1 and t.stride(1) != d):
         raise ValueError(f"{name} must be [{tokens}, {heads}, {d}] with a row's heads side by side, or flat: got {tuple(t.shape)}, strides {t.stride()}")
+    if tokens > 1 and t.stride(0) < heads * d:
+        raise ValueError(f"{name}: the rows of its tokens overlap: strides {t.stride()} of [{tokens}, {heads}, {d}]")
     return t.stride(0) if tokens > 1 else heads * d
 
 

@@ -381,7 +381,7 @@ PyObject* prompt(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   if (cap == -1.0 && PyErr_Occurred()) return nullptr;
   c.score_cap = static_cast<float>(cap);
   if (c.score_cap == 0.f && cap != 0.0) Py_RETURN_NONE;
-  // flat rows, or [tokens, heads, head_dim] of rows whose heads lie side by side
+  // flat rows, or [tokens, heads, head_dim] of rows whose heads lie side by side, none of which overlap
   const auto rows = [&](PyObject* o, int64_t heads, int64_t* stride, void** p) {
     if (!THPVariable_CheckExact(o)) return false;
     const at::Tensor& t = THPVariable_Unpack(o);
@@ -392,7 +392,7 @@ PyObject* prompt(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     if (t.dim() == 1 || t.dim() == 2) return t.is_contiguous() && t.numel() == tokens * heads * d && (t.dim() == 1 || t.size(1) == d);
     if (t.dim() != 3 || t.size(0) != tokens || t.size(1) != heads || t.size(2) != d) return false;
     *stride = tokens > 1 ? t.stride(0) : heads * d;
-    return tokens == 0 || (t.stride(2) == 1 && (heads == 1 || t.stride(1) == d));
+    return tokens == 0 || (*stride >= heads * d && t.stride(2) == 1 && (heads == 1 || t.stride(1) == d));
   };
   void *q, *k, *v, *out, *lse, *slopes = nullptr;
   if (!rows(args[2], c.hq, &c.q_stride, &q) || !rows(args[3], c.hkv, &c.k_stride, &k) || !rows(args[4], c.hkv, &c.v_stride, &v)) Py_RETURN_NONE;

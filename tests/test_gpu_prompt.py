@@ -222,6 +222,26 @@ def test_the_same_twice():
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("native", [True, False])
+def test_rows_that_overlap_are_refused(native, monkeypatch):
+    """A view that is expanded over tokens has the row stride that names flat blocks; nothing is launched."""
+    if not native:
+        monkeypatch.setattr(b, "_call", None)
+    lens, hq, hkv = [40, 24], 4, 2
+    q, k, v = (x.cuda() for x in inputs(67, lens, hq, hkv))
+    good = dict(Q=q, K=k, V=v, seq_lens=lens, hq=hq, hkv=hkv)
+    for side, heads in (("Q", hq), ("K", hkv), ("V", hkv), ("out", hq)):
+        row = torch.full((heads * D + 64 * 8,), 7.0, dtype=BF, device="cuda")
+        for bad in (row[:heads * D].view(1, heads, D).expand(64, heads, D), row.as_strided((64, heads, D), (8, D, 1))):
+            with pytest.raises(ValueError, match=side):
+                b.rdkv_prompt_attn_bf16(**dict(good, **{side: bad}))
+        assert torch.all(row == 7)
+    one = [x[:1] for x in (q, k, v)]
+    want = b.rdkv_prompt_attn_bf16(*one, [1], hq, hkv)
+    got = b.rdkv_prompt_attn_bf16(*(x.as_strided(x.shape, (0, D, 1)) for x in one), [1], hq, hkv)      # (of one token the stride means nothing)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_native_calls_do_as_the_others(monkeypatch):
     """Layouts, results made and given, and refusals, through the native code and without it."""
     lens, hq, hkv = [70, 0, 33], 8, 2

@@ -64,6 +64,22 @@ def test_the_binding_refuses_tensors_the_library_would_misread():
         b.rdkv_prompt_attn_bf16(q, k, k, lens, 8, 2)
 
 
+@pytest.mark.parametrize("side, heads", [("Q", 8), ("K", 2), ("V", 2), ("out", 8)])
+def test_the_binding_refuses_rows_that_overlap(side, heads):
+    """A view that is expanded over tokens has a row stride of 0, which the library takes for flat blocks: rows behind the view's memory.  So do rows that
+    begin inside the one before, which are no layout of their own either; of one token the stride means nothing."""
+    bf = torch.bfloat16
+    q, k = torch.zeros(12, 8, 128, dtype=bf), torch.zeros(12, 2, 128, dtype=bf)
+    good = dict(Q=q, K=k, V=k, seq_lens=[5, 7], hq=8, hkv=2)
+    row = torch.zeros(heads * 128 + 12 * 8, dtype=bf)
+    for bad in (row[:heads * 128].view(1, heads, 128).expand(12, heads, 128), row.as_strided((12, heads, 128), (8, 128, 1))):
+        with pytest.raises(ValueError, match=side):
+            b.rdkv_prompt_attn_bf16(**dict(good, **{side: bad}))
+    one = dict(Q=q[:1], K=k[:1], V=k[:1], seq_lens=[1], hq=8, hkv=2)
+    with pytest.raises(ValueError, match="cpu"):           # (it is where the tensors lie that is wrong)
+        b.rdkv_prompt_attn_bf16(**dict(one, **{side: row.as_strided((1, heads, 128), (0, 128, 1))}))
+
+
 def test_the_ctypes_struct_matches_the_c_header(tmp_path):
     fields = [f[0] for f in b.rdkv_prompt._fields_]
     src = tmp_path / "layout.c"
