@@ -61,11 +61,11 @@ struct Query4 {
       for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(static_cast<float>(in[kb][i])));
     }
     most = halves_max(most);
-    // the largest value over the unit is in [2^9, 2^10), a group's sum below 2^15; of zeros, infinities and the like: as they are
-    const int e = static_cast<int>(__float_as_uint(most) >> 23);
-    const bool plain = e >= 1 && e <= 253;
-    const float inv = 0x1p9f * (plain ? __uint_as_float(static_cast<uint32_t>(254 - e) << 23) : 1.f);
-    unit = 0x1p-9f * (plain ? __uint_as_float(static_cast<uint32_t>(e) << 23) : 1.f);
+    // The largest value over the unit is in [2^9, 2^10), a group's sum below 2^15; below 2^-111 less, where the unit and one over it, of which the drafted
+    // tokens' products take the second, would leave fp32's normal numbers (values down to 2^-126 are 2^-6 there and keep their bits).
+    const uint32_t e = min(max(__float_as_uint(most) >> 23, 16u), 254u);
+    const float inv = __uint_as_float((263u - e) << 23);              // 2^(136 - e)
+    unit = __uint_as_float((e - 9u) << 23);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float sum = 0.f;

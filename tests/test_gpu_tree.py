@@ -237,6 +237,54 @@ def test_queries_of_any_size(bits, size):
     run(np.random.default_rng(19), [130, 70], 4, 1, 130, bits, 5, big=size)
 
 
+def tiny(rng, shape, size):
+    """Queries of a few sizes beside each other and zeros, all of them exact and no value between 0 and 2^-126."""
+    return cuda(size * rng.choice([-2.0, -1.5, -1.0, 0.0, 0.0, 1.0, 1.5, 2.0], shape), BF)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("size", [2.0 ** -112, 2.0 ** -119, 2.0 ** -121, 2.0 ** -126])
+@pytest.mark.parametrize("kw", [dict(), dict(cap=20.0, window=100, sinks=2)], ids=str)
+def test_queries_of_the_smallest_sizes(bits, size, kw):
+    """Down to the smallest normal number, with zeros among them, beside a row of zeros and rows of ordinary size: scores are 0 or next to it, and a tree
+    and what is accepted of it are an even share."""
+    rng, lens, hq, hkv, n = np.random.default_rng(71), [130, 70], 4, 1, 5
+    s, items = cached(rng, lens, hq, hkv, 140, bits, window=kw.get("window", 0), sinks=kw.get("sinks", 0), score_cap=kw.get("cap", 0.0))
+    q, k, v = drafted(rng, 2, n, hq, hkv)
+    q[:, :3] = tiny(rng, (2, 3, hq, D), size)
+    q[0, 0, 1] = 0
+    parent = np.stack([tree(rng, n, "chain")] * 2)
+    out, stats = b.rdkv_slots_tree_attn(s, q, k, v, cuda(parent, I32))
+    assert torch.isfinite(out.float()).all() and torch.isfinite(stats).all()
+    plain = {x: kw[x] for x in ("window", "cap") if x in kw}
+    for i, it in enumerate(items):
+        o, M, S, o_off, M_off, S_off = T.attend(it, f64(q)[i], f64(k)[i, :, 0], f64(v)[i, :, 0], T.ways(parent[i], n), sinks=s.c.sinks, **plain)
+        assert np.all(np.abs(f64(out)[i] - o) <= o_off)
+        # products, their sums and scores below 2^-126 may be taken for 0: less than 300 of them
+        assert np.all(np.abs(f64(stats)[i, ..., 0] - M) <= M_off + 300 * 2.0 ** -126)
+        assert np.all(np.abs(f64(stats)[i, ..., 1] - S) <= (S_off + M_off) * S)
+    paths = [[0, 1, 2, 3, 4], [0, 1, -1, -1, -1]]
+    slot = b.rdkv_slots_accept(s, q, k, v, cuda(paths, I32), stats)
+    check_accept(s, items, q, k, v, paths, stats, slot, **plain)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_queries_of_the_largest_size_against_keys_of_zero(bits):
+    """Scores of 0 whatever the queries are: the mean of the values that are seen."""
+    rng = np.random.default_rng(73)
+    s, items = cached(rng, [130], 4, 1, 140, bits)
+    q, k, v = drafted(rng, 1, 5, 4, 1)
+    s.k.zero_(), k.zero_()
+    for it in items:
+        it.K[:] = 0
+        it.K_size4 = np.zeros((140, D))
+    q[0, 1:3] = tiny(rng, (2, 4, D), 2.0 ** 126)
+    q[0, 3] = 0
+    parent = tree(rng, 5, "chain")[None]
+    out, stats = b.rdkv_slots_tree_attn(s, q, k, v, cuda(parent, I32))
+    check_tree(s, items, q, k, v, parent, [5], out, stats)
+
+
 def test_the_size_of_queries_against_keys_is_nothing():
     """Queries times a power of two, keys over it: the same bits."""
     rng = np.random.default_rng(20)
