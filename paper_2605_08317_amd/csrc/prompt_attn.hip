@@ -25,6 +25,7 @@ using namespace attn;
 constexpr int kTileBytes = kKeys * kRowBytes;        // of K, or of V
 constexpr int kRing = 2;
 constexpr float kLowest = -2e38f;                    // a finite maximum of nothing, also times log2(e): no score is below it
+constexpr float kMostOver = 1e38f;                   // the largest cap that scores are kept over: times log2(e) it is finite
 constexpr float kSlack = 8.f;                        // what exponents may exceed the reference by before it moves
 
 // element (head, token 0, channel 0) of a sequence
@@ -84,9 +85,12 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
   for (int kb = 0; kb < 8; ++kb) arrived(q_op[kb]);
   const float slope = GENERAL && a.slopes ? a.slopes[head] : 0.f, inv_cap = GENERAL && a.cap > 0.f ? 1.f / a.cap : 0.f;
   const TanhSmall small(kRoot * inv_cap);
-  // What makes the numbers that are kept (products, scores over the cap, or with biases scores) scores, and those exponents of 2.
+  // What makes the numbers that are kept (products, scores over the cap, or with biases and caps past kMostOver scores) scores, and those exponents of 2;
+  // a maximum of nothing among them, in their units: with the factor it stays finite as well.
+  const bool scored = GENERAL && (a.slopes || a.cap > kMostOver);
   const float units = GENERAL && a.cap > 0.f ? a.cap : kRoot;
-  const float factor = !GENERAL ? kRootLog2e : a.slopes ? kLog2e : a.cap > 0.f ? a.cap * kLog2e : kRootLog2e;
+  const float factor = !GENERAL ? kRootLog2e : scored ? kLog2e : units * kLog2e;
+  const float lowest = GENERAL && !scored ? kLowest / fmaxf(units, 1.f) : kLowest;
 
   floatx16 o[4];
   float m, l;
@@ -100,7 +104,7 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
   const auto begin = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[t] = floatx16{};
-    m = kLowest;
+    m = lowest;
     l = 0.f;
   };
   const auto key = [](int x, int i) { return 32 * x + 8 * (i >> 2) + (i & 3); };
@@ -112,7 +116,7 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] = s[i >> 4][i & 15];
       if (a.cap > 0.f) tanh_all(v, kRoot * inv_cap, small);
-      if (a.slopes) {
+      if (scored) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = __builtin_fmaf(v[i], units, -slope * static_cast<float>(back - key(i >> 4, i & 15)));
       }

@@ -81,6 +81,34 @@ def test_windows_caps_and_biases(lens, hq, hkv, kw):
         run(7, lens, hq, hkv, tokens, **kw)
 
 
+@pytest.mark.parametrize("kw", [dict(cap=30.0, window=64), dict(cap=30.0, window=100, sinks=2), dict(cap=1.5, window=40), dict(cap=0.25, window=33, sinks=1),
+                                dict(cap=50.0, window=400), dict(cap=1e30, window=100)], ids=str)
+@pytest.mark.parametrize("lens, hq, hkv", [([700, 33], 8, 2), ([300] * 12, 8, 2), ([1500], 2, 1)])         # with shared tiles, without, and with
+def test_caps_with_windows(lens, hq, hkv, kw):
+    """Rows whose first tile is hidden from them as a whole, while scores are kept over the cap."""
+    run(31, lens, hq, hkv, True, **kw)
+
+
+@pytest.mark.parametrize("cap", [1e37, 9.9e37, 1.01e38, 2.3e38, 2.4e38, 3.4e38])
+@pytest.mark.parametrize("kw", [dict(), dict(window=50), dict(window=50, sinks=2)], ids=str)
+def test_caps_up_to_the_largest_number(cap, kw):
+    """A cap far above the scores changes nothing.  Over the cap a product's factor is a number below fp32's normal ones, of 18 bits at least, and what it makes may
+    be off by 2^-150, times the cap 2^-22: scores are off by 2^-17 of themselves and 2^-20 at most."""
+    lens, hq, hkv = [300, 1, 70], 4, 2
+    q, k, v = inputs(37, lens, hq, hkv)
+    out, lse = b.rdkv_prompt_attn_bf16(q.cuda(), k.cuda(), v.cuda(), lens, hq, hkv, score_cap=cap, **kw)
+    out, lse, at = out.double().cpu().numpy(), lse.double().cpu().numpy(), 0
+    q, k, v = (x.double().numpy() for x in (q, k, v))
+    for s, T in enumerate(lens):
+        seq = slice(sum(lens[:s]), sum(lens[:s + 1]))
+        for h in range(hq):
+            o, l, o_off, l_off = P.attend(q[seq, h][None], k[seq, h // 2], v[seq, h // 2], **kw)
+            most = 2.0 ** -17 * np.abs(q[seq, h] @ k[seq, h // 2].T).max() / math.sqrt(D) + 2.0 ** -20
+            assert np.all(np.abs(out[seq, h] - o[0]) <= o_off[0] + 2 * most * np.abs(v[seq, h // 2]).max(0))
+            assert np.all(np.abs(lse[at:at + T] - l[0]) <= l_off[0] + most)
+            at += T
+
+
 SLOPES = (2.0 ** (-8.0 * (np.arange(8) + 1) / 8)).astype(np.float32).astype(np.float64)
 
 
