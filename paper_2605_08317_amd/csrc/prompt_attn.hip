@@ -147,10 +147,13 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
       s[i >> 3] = product(k, q_op[i & 7], (i & 7) == 0 ? floatx16{} : s[i >> 3]);
     }
   };
+  // The exponent of 2 that a change of the reference takes: with care of a difference, as exponents are there; else the difference of what exponents are
+  // made with, the references times the factor as they are rounded, so that tiles of different references weigh the same.
+  const auto between = [&](float from, float to, bool care) { return care ? (from - to) * factor : from * factor - to * factor; };
   // the row's reference, if its largest score is past it
-  const auto refer = [&](float top, bool any) __attribute__((always_inline)) {
-    if (__any(any ? top > m : (top - m) * factor > kSlack)) {
-      const float now = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f((m - now) * factor);
+  const auto refer = [&](float top, bool care) __attribute__((always_inline)) {
+    if (__any(care ? top > m : (top - m) * factor > kSlack)) {
+      const float now = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(between(m, now, care));
       m = now;
       l *= alpha;
 #pragma unroll
@@ -269,8 +272,9 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
     for (; it < n_it; ++it) open(it);
     tile_barrier<0>();                               // (copies of tiles past the last have landed as well)
   };
-  // Again, with care, where a result is not finite: rows of V that some rows of a tile do not see are kept from meeting their zeros, which make NaN of
-  // what is not finite, and exponents are differences, so that scores may be of any size.
+  // Again, with care, where a result is not finite or a row that saw something has next to none of it: rows of V that some rows of a tile do not see are kept
+  // from meeting their zeros, which make NaN of what is not finite, and exponents are of differences, so that scores may be of any size (a reference of 2^30
+  // times the factor is off by up to 8 when rounded, and from 2^34 on all that a row sees could be below fp32's least, or past its largest).
   const auto walk_with_care = [&]() __attribute__((always_inline)) {
     begin();
     for (int it = 0; it < n_it; ++it) {
@@ -324,7 +328,9 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum = __builtin_fmaf(o[t][i], 0.f, sum);
   sum = __builtin_fmaf(l, 0.f, sum);
-  if (__syncthreads_or(sum != 0.f)) walk_with_care();
+  const bool lost = m != lowest && halves_add(l) < 0x1p-20f;
+  const bool care = __syncthreads_or(sum != 0.f || lost);
+  if (care) walk_with_care();
 
   l = halves_add(l);
   if constexpr (WS == 2) {
@@ -342,7 +348,7 @@ __global__ __launch_bounds__(2 * kRows, 3 - WS) void prompt_kernel(Args a) {
     __syncthreads();
     if (ws == 1) return;
     const float other = theirs[64 * 64], now = fmaxf(m, other);
-    const float mine = __builtin_amdgcn_exp2f((m - now) * factor), its = __builtin_amdgcn_exp2f((other - now) * factor);
+    const float mine = __builtin_amdgcn_exp2f(between(m, now, care)), its = __builtin_amdgcn_exp2f(between(other, now, care));
     m = now;
     l = __builtin_fmaf(theirs[65 * 64], its, l * mine);
 #pragma unroll

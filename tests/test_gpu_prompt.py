@@ -194,6 +194,32 @@ def test_a_large_number_common_to_all_scores_costs_nothing(size):
         assert torch.all((got - want).abs() <= (2 * P.HALF_BF16 + 2.0 ** -18 + 2.0 ** -22 * unit) * size_of + P.HALF_BF16 * want.abs())
 
 
+@pytest.mark.parametrize("n", [1, 40])                         # with shared tiles, and without
+@pytest.mark.parametrize("most", [0, 3, 4, 5, 6, 7])
+@pytest.mark.parametrize("size", [2.0 ** 12, 2.0 ** 16, 2.0 ** 19, 2.0 ** 22, 2.0 ** 40, 2.0 ** 60])
+def test_scores_of_any_size(size, most, n):
+    """A number common to all scores, up to 2^120, and up to `most` units of its 20th bit for each key, so that fp32 products and sums are exact.  Exponents are
+    the difference of a product times a factor and a number that the row's keys share, rounded once: off by 2^-24 of their own size, which with a reference
+    that is rounded itself stays below 2^7 where it is not done again.  lse has a few roundings of its size."""
+    T, hq, gen = 200, 2, torch.Generator().manual_seed(most)
+    lens = [T] * n
+    unit = size * size * 2.0 ** -20
+    q, k = torch.zeros((n * T, hq, D)), torch.zeros((n * T, 1, D))
+    q[..., 0], k[..., 0], q[..., 1] = size, size, 1.0
+    k[:, 0, 1] = torch.randint(0, most + 1, (n * T,), generator=gen).float() * unit
+    v = torch.randn((n * T, 1, D), generator=gen).to(BF)
+    out, lse = b.rdkv_prompt_attn_bf16(q.to(BF).cuda(), k.to(BF).cuda(), v.cuda(), lens, hq, 1)
+    out, lse = out.double().cpu(), lse.view(n, hq, T).double().cpu()
+    for s in range(n):
+        seq = slice(s * T, s * T + T)
+        x = torch.where(torch.ones(T, T).tril() > 0, k[seq, 0, 1].double() / math.sqrt(D), -math.inf)
+        p, rows = torch.softmax(x, -1), v[seq, 0].double()
+        want, want_lse = p @ rows, torch.logsumexp(x, -1) + size * size / math.sqrt(D)
+        for h in range(hq):
+            assert torch.all((out[seq, h] - want).abs() <= (P.HALF_BF16 + 2.0 ** -16) * (p @ rows.abs()) + P.HALF_BF16 * want.abs() + 2.0 ** -16 * rows.abs().max()), (s, h)
+            assert torch.all((lse[s, h] - want_lse).abs() <= 2.0 ** -22 * want_lse.abs() + 2.0 ** -16), (s, h)
+
+
 def test_strides_past_32_bits():
     """Rows of 2^21 elements: bytes past 2^31 and, in K, past 2^32."""
     lens, hq, hkv = [1100, 30], 2, 1
