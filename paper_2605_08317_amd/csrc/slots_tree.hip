@@ -27,7 +27,7 @@ constexpr int kTokens = 64;
 
 // What a lane knows of its query row.
 struct Row {
-  int index;                              // of the item's n g rows; past them: of none, as the last
+  int index;                              // of the item's rows, those of its drafted tokens; past them: of none, as the last
   bool there;
   int token, at;                          // its position
   uint64_t sees;                          // drafted tokens
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
   // row groups of a piece are eight workgroups apart, on one XCD
   const int in = static_cast<int>(blockIdx.x) % (8 * a.row_groups), unit = static_cast<int>(blockIdx.x) / (8 * a.row_groups) * 8 + in % 8, rg = in / 8;
   if (unit >= a.items * a.pieces) return;
-  const int item = unit / a.pieces, piece = unit % a.pieces, seq = item / a.s.hkv, kvh = item % a.s.hkv, g = a.s.g, n = a.n, rows = n * g;
+  const int item = unit / a.pieces, piece = unit % a.pieces, seq = item / a.s.hkv, kvh = item % a.s.hkv, g = a.s.g, n = a.n;
   const int count = a.counts ? min(max(a.counts[seq], 0), n) : n;
   if (rg * WR * 32 >= count * g) return;
 
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
   {
     const int r = (rg * WR + wr) * 32 + l32;
     row.there = r < count * g;
-    row.index = min(r, rows - 1);
+    row.index = min(r, count * g - 1);                                    // (rows of tokens from `count` on may hold anything)
     row.token = row.index / g;
     row.slope = GENERAL && a.s.slopes ? a.s.slopes[kvh * g + row.index % g] : 0.f;
   }
@@ -610,8 +610,8 @@ __global__ __launch_bounds__(64 * (kWaves<BITS, WR>), BITS == 4 || WR > 1 ? 2 : 
   // the drafted tokens themselves
   if (piece == a.pieces - 1) {
     const int64_t first = (static_cast<int64_t>(seq) * n * a.s.hkv + kvh) * kRowBytes;
-    fetch_rows(reinterpret_cast<const uint8_t*>(a.k_draft) + first, k_at, a.s.hkv * kRowBytes, n - 1, kTokens, lds0);
-    fetch_rows(reinterpret_cast<const uint8_t*>(a.v_draft) + first, v_at, a.s.hkv * kRowBytes, n - 1, kTokens, lds0 + kTokens * kRowBytes);
+    fetch_rows(reinterpret_cast<const uint8_t*>(a.k_draft) + first, k_at, a.s.hkv * kRowBytes, count - 1, kTokens, lds0);
+    fetch_rows(reinterpret_cast<const uint8_t*>(a.v_draft) + first, v_at, a.s.hkv * kRowBytes, count - 1, kTokens, lds0 + kTokens * kRowBytes);
     tile_barrier<0>();
     if (ws == 0) {
       Query16 q16;

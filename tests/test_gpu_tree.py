@@ -167,6 +167,30 @@ def test_drafted_rows_that_are_hidden_may_hold_anything(bits, bad, n, hq):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("kw", [dict(), dict(score_cap=20.0, window=100, sinks=2)], ids=str)
+@pytest.mark.parametrize("n, hq, counts", [(8, 8, [5, 8, 1]), (20, 8, [13, 1, 0]), (40, 8, [33, 17, 40]), (64, 8, [1, 50, 64])])
+def test_what_is_behind_the_last_drafted_token_changes_no_bits(bits, kw, n, hq, counts):
+    """Whatever rows from counts on hold, the others' numbers are the same to the bit: what is not finite there sends no one over the slots again, and no
+    row's reference moves for a large score of theirs."""
+    rng = np.random.default_rng(79)
+    s, _ = cached(rng, [700, 130, 65], hq, 1, 720, bits, **kw)
+    q, k, v = drafted(rng, 3, n, hq, 1)
+    parent = cuda(np.stack([tree(rng, n) for _ in range(3)]), I32)
+    got = []
+    for fill in (0.0, math.nan, math.inf, -math.inf, 1e4, 3e38):
+        q2, k2, v2 = q.clone(), k.clone(), v.clone()
+        for t in (q2, k2, v2):
+            for sq, c in enumerate(counts):
+                t[sq, c:] = fill * t[sq, c:].sign() if math.isfinite(fill) else fill
+        out, stats = torch.full_like(q, 7.0), torch.full((3, n, hq, 2), 7.0, device="cuda")
+        b.rdkv_slots_tree_attn(s, q2, k2, v2, parent, counts=cuda(counts, I32), out=out, stats=stats)
+        got.append((out, stats))
+    assert torch.isfinite(got[0][0].float()).all()
+    for out, stats in got[1:]:
+        assert torch.equal(out, got[0][0]) and torch.equal(stats, got[0][1])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("n, hq", [(6, 4), (40, 8)])
 def test_slots_behind_a_window_may_hold_anything(bits, n, hq):
     """Some tokens of the tree see a slot, and those further along do not."""
