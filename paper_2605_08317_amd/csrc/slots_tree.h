@@ -39,10 +39,10 @@ inline TreePlan plan_tree(int64_t items, int rows, int capacity, int bits) {
   const int64_t groups = items * p.row_groups;
   const int64_t tiles = (static_cast<int64_t>(capacity) + kTileRows - 1) / kTileRows;
   const int64_t stage = bits == 16 ? (p.wide == 8 ? 1 : 2) : 4 / p.wide;            // tiles that a workgroup has at once: no piece is smaller
-  // As many workgroups as run at once: one a compute unit in bf16, two in 4 bits; in 4 bits twice as many, for items of different lengths, where a piece
-  // still has 32 stages (32 x 8 x 5000 .. 8192 slots 358 -> 342 us; 4 x 8 x 131072 of 16 stages 164 -> 170).
-  int64_t card = bits == 16 ? 256 : 512;
-  if (bits == 4 && 2 * card / std::max<int64_t>(groups, 1) * 32 * stage <= tiles) card *= 2;
+  // As many workgroups as run at once: one a compute unit in bf16, two in 4 bits.  (Twice as many in 4 bits, for items of different lengths: 32 tokens of 4 heads on
+  // 32 x 8 x 5/8 C .. C slots 5 % slower at C = 4096 to 7168, the same at 8192 and 12288, 3 % faster at 16384, 4 % at 32768; of equal lengths 1 to 11 %
+  // slower at all of them, 8 tokens at 8192 11 %.)
+  const int64_t card = bits == 16 ? 256 : 512;
   // Nor more than 4 roots of the stages: a piece costs the join what a sixteenth of a stage costs (one item of 131072 slots, 256 pieces -> 128 or 90: bf16
   // 29.0 -> 24.2 us, 4 bits 32.2 -> 27.1; with 2.4 roots 27.1 and 34.3).
   const int64_t most = std::min(tiles / stage, static_cast<int64_t>(4.0 * std::sqrt(static_cast<double>(tiles / stage))));
