@@ -477,6 +477,23 @@ def test_nan_weights_go_first():
     assert slot[0, 0, 0] == (33 if items[0].pos[33] <= items[0].next - 2 else slot[0, 0, 0])
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("m", [1, 2])
+def test_a_nan_weight_goes_before_all_others(bits, m):
+    """Of two slots that may go and have none for a weight the older one first, whatever the others have gathered."""
+    rng = np.random.default_rng(83)
+    s, items = cached(rng, [150], 2, 1, 150, bits, sinks=2, recent=2)
+    it = items[0]
+    may = np.nonzero((it.pos >= 2) & (it.pos <= it.next - 40))[0]
+    old, young = sorted((int(x) for x in (may[3], may[-5])), key=lambda x: it.pos[x])
+    s.weight[0, 0, old] = s.weight[0, 0, young] = math.nan
+    s.weight[0, 0, int(may[0])] = -1e30                     # (less than any that is gathered, and still a number)
+    q, k, v = drafted(rng, 1, 2, 2, 1)
+    _, stats = b.rdkv_slots_tree_attn(s, q, k, v, cuda([[-1, 0]], I32))
+    slot = b.rdkv_slots_accept(s, q, k, v, cuda([[0, 1][:m]], I32), stats)
+    assert slot.flatten().tolist() == [old, young][:m]
+
+
 # ---- together ------------------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("bits", [16, 4])
