@@ -516,7 +516,8 @@ def run(st):
     if op == "tree":
         return list(b.rdkv_slots_tree_attn(slots, st["q"], st["k_draft"], st["v_draft"], st["parent"], counts=st["counts"], out=st["out"],
                                            stats=st["stats"], workspace=st["workspace"]))
-    slot = b.rdkv_slots_accept(slots, st["q"], st["k_draft"], st["v_draft"], st["path"], st["stats"])
+    # (the statistics of one head a KV head come from the plain form in another order)
+    slot = b.rdkv_slots_accept(slots, st["q"], st["k_draft"], st["v_draft"], st["path"], st["stats"].contiguous())
     return _accepted(st, slot, b.rdkv_slots_read(slots, slot) if case["bits"] == 4 else [st["k"], st["v"]])
 
 
