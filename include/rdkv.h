@@ -535,8 +535,8 @@ rdkv_status rdkv_slots_tree_attn(const rdkv_slots* slots, int32_t n, const void*
  * value of token j, summed over the heads of the group, in slots below len.  Then the tokens come in one after the other as by rdkv_slots_append,
  * but that token i starts with the sum over j >= i of decay^(c-1-j) x what token j gives it.  While slots are free this is what c appends, each
  * followed by its decode step, leave.  An accepted token that is no longer among the `recent` ones may be given up for a later one of the path;
- * its slot then holds the later one's row, and both name it in `slot`.  A path may name a token twice: it comes in twice.  Positions within an item
- * are taken to differ.  Rows of 4-bit caches are quantized as they come in.
+ * its slot then holds the later one's row, and both name it in `slot`.  A path may name a token twice: it comes in twice; one behind the tree's
+ * `counts` has no stats, so that no path names it.  Positions within an item are taken to differ.  Rows of 4-bit caches are quantized as they come in.
  */
 size_t rdkv_slots_accept_workspace_bytes(const rdkv_slots* slots);
 rdkv_status rdkv_slots_accept(const rdkv_slots* slots, int32_t n, int32_t m, const void* q, const void* k_draft, const void* v_draft,

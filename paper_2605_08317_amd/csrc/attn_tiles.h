@@ -49,10 +49,10 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
 }
 
-// Loads that the compiler knows of are waited for here and not at their first use, in a loop whose copies to LDS it does not know of: there it would
-// wait for those too.
 // The number is computed here, not where it is needed (the compiler moves what has time to a later block).
 __device__ __forceinline__ void here(float& v) { asm volatile("" : "+v"(v)); }
+// Loads that the compiler knows of are waited for here and not at their first use, in a loop whose copies to LDS it does not know of: there it would
+// wait for those too.
 __device__ __forceinline__ void arrived(bf16x8& v) { asm volatile("" : "+v"(v)); }
 
 __device__ __forceinline__ int k_piece(int row, int piece) { return piece ^ (row & 15); }

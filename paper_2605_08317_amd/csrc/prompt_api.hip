@@ -75,7 +75,7 @@ rdkv_status rdkv_prompt_attn_bf16(const rdkv_prompt* p, const void* Q, const voi
   int64_t token0 = 0;
   for (int s0 = 0; s0 < p->batch; s0 += prompt::kSeqs) {
     a.n_seqs = std::min(prompt::kSeqs, p->batch - s0);
-    std::pair<int32_t, int64_t> seqs[prompt::kSeqs];                // (length, first token), the longest first
+    std::pair<int32_t, int64_t> seqs[prompt::kSeqs];                // (length, first token), the longest of the launch first
     for (int i = 0; i < a.n_seqs; ++i) {
       seqs[i] = {p->seq_lens[s0 + i], token0};
       token0 += seqs[i].first;

@@ -5,8 +5,9 @@
 // has one row: maxima and sums are its own but for one exchange between the halves, and its probabilities, packed where they are, are P V's
 // other operand.  K and V go straight into LDS, two tiles of each; a wavefront issues the next tile's 16 products between a tile's first 16
 // exponentials, and the other 16 between P V's products.
-//   bound   the matrix cores, at the clock that the card's power leaves them: 32768 tokens of 32 heads take 8.0 ms, 1.09 PFLOP/s at 1.69 GHz (a library's
-//           product of two matrices of 16384 rows reaches 1.59); matrix cores 62 % busy, vector 65 %.  With a cap vector instructions are, at 81 %.
+//   bound   the matrix cores, at the clock that the card's power leaves them: 32768 tokens of 32 heads take 7.8 to 8.5 ms from card to card, 1.13 PFLOP/s at
+//           1.70 GHz (a library's product of two matrices of 16384 rows reaches 1.59); matrix cores 63 % busy, vector 66 %.  With a cap vector instructions
+//           are, at 80 %.
 //   tried   256 rows in eight wavefronts with four tiles on their way: as fast for one long prompt, 10 % slower for many (one barrier for all of a
 //           compute unit).  64 rows a wavefront, half the reads from LDS: does not fit the registers, 15 ms.  A tile's exponentials without the
 //           next one's products between them: 8.4 ms

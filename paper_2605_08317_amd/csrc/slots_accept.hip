@@ -5,7 +5,7 @@
 // probabilities by the largest score and the sum that the tree's step left.  V is not read.  Where a cache will be full it leaves the least of
 // every 32 slots as well.  The second, a workgroup an item, takes the tokens in one after the other as that many appends would, from those
 // leasts.
-//   bound   the K side once: HBM.  The second launch: a chain of steps, a few for each token that takes another's slot
+//   bound   the K side, once for every 64 rows (token, head) of a path: HBM.  The second launch: a chain of steps, a few for each token that takes another's slot
 #include <algorithm>
 
 #include "group_quant.h"

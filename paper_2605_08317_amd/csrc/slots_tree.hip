@@ -6,10 +6,11 @@
 // by a second launch.  The last piece of an item has the drafted tokens' own keys and values, bf16 rows whatever the cache holds, behind its slots or
 // to itself.  Products and probabilities as of prompts (a lane has one query row); of 4-bit tiles a wavefront's own, codes less 8 as fp16 with
 // group sums in fp32, so that scores keep fp32's digits.
-//   bound   bf16: HBM up to 64 rows (8 tokens of 4 heads on 4 x 8 x 131072 slots 390 us, 5.5 TB/s), from 128 on the matrix cores at the clock that the
-//           power leaves them (64 tokens 650 us, 830 TFLOP/s at 1.6 GHz).  4 bits: vector instructions, 63 % of the cycles issue one, about 640
-//           a tile and 32 rows (8 tokens on 4 x 8 x 131072 slots 150 us); above 64 rows four wavefronts share what takes the codes apart, 49 %, and
-//           wait for each other (32 tokens on 32 x 8 x 5000..8192 slots with biases 307 -> 282 us)
+//   bound   bf16: HBM up to 64 rows (8 tokens of 4 heads on 4 x 8 x 131072 slots 390 us, 5.5 TB/s), from 128 on the matrix cores, 54 % busy, at the clock that
+//           the power leaves them, and waits, 29 % (64 tokens 600 us in a long row of calls, 920 TFLOP/s; the first few 540, those behind them up to 900).
+//           4 bits: vector instructions, 63 % of the cycles issue one, about 640 a tile and 32 rows (8 tokens on 4 x 8 x 90001..131072 slots 147 us); above
+//           64 rows four wavefronts share what takes the codes apart, 47 %, and wait for each other, 35 % (32 tokens on 32 x 8 x 5000..8192 slots with
+//           biases 250 us)
 //   tried   query operands in LDS and tiles loaded a tile ahead twice over in 4 bits: slower, they cost the registers of a second wavefront a SIMD
 #include <algorithm>
 
